@@ -353,6 +353,75 @@ brisk_status brisk_isd_costs(int32_t M, double *g, double *c);
  * (2 + sum_{i=1}^{N-2} (1-r)^i) / (2 - (1-r)^{N-1}); NaN for N < 2 or r outside [0, 1]. */
 double brisk_tpf_isd(int32_t N, double r);
 
+/* ---- Attention over a shared prefix and own caches; eviction by attention weight ----
+ *
+ * What the backbone pass in front of a decode tail does with its context cache. B sequences share a
+ * prefix of P entries (keys and values held once, computed once for all of them) and have own
+ * caches of room S behind it, of which own_len[b] entries are in use; the queries are the L
+ * positions of every sequence's block (L = 1: single tokens), Hq query heads over Hkv key heads
+ * (head hq reads key head hq / (Hq / Hkv)) of width D. The paper takes the backbone as given;
+ * these calls have no counterpart in it.
+ * Limits: 1 <= B <= 4096; L >= 1; Hq a multiple of Hkv; B * L * Hq <= 2^30; 8 <= D <= 128 and
+ * D % 8 == 0; 0 <= P, S <= 2^30. dtype: q, keys, values and out (fp32 or bf16). */
+typedef struct brisk_cache_dims {
+  int32_t B, L, Hq, Hkv, D, P, S;
+  int32_t dtype;
+} brisk_cache_dims;
+
+/* A strided tensor: element (s, t, h, :) at ptr + s * seq + t * tok + h * head, D elements wide
+ * and contiguous, strides in elements. Any order of the dimensions and any padding goes (also keys
+ * and values side by side in one buffer). ptr and the strides are multiples of 16 bytes; the
+ * strides of dimensions longer than 1 are at least D and below 2^39 bytes. `seq` is unused by
+ * the prefix's tensors, and the stride of a dimension of length 1 by any. */
+typedef struct brisk_view {
+  const void *ptr;
+  int64_t seq, tok, head;
+} brisk_view;
+
+/* Bytes of workspace the three calls below need for `dims` (256-byte multiple; 0 if invalid). Its
+ * status word is read with brisk_last_device_status(). */
+size_t brisk_cache_workspace_bytes(const brisk_cache_dims *dims);
+
+/* For every query row (b, i, hq), with s_t = scale q . k_t: lse = log sum_t exp(s_t) and
+ * out = sum_t exp(s_t - lse) v_t over all P prefix entries and the own entries t that the position
+ * sees: t < min(own_len[b], visible[b, i]); visible NULL: all that are in use. A position with
+ * visible < 0 is padding: it sees nothing, not even the prefix. A row that sees nothing has
+ * out = 0 and lse = -inf. Entries that a row does not see do not reach its result, whatever they
+ * hold (infinities and NaN too).
+ * q [B, L, Hq]; k_prefix, v_prefix [P, Hkv] (NULL if P == 0); k_own, v_own [B, S, Hkv] (NULL if
+ * S == 0); own_len [B], visible [B, L] int32; out [B, L, Hq, D] dense, 16-byte aligned; lse
+ * [B, L, Hq] f32 or NULL. 0 <= scale < inf. With bf16 the probabilities enter the sum of values rounded to
+ * bf16; scores, maxima and sums are fp32. A length outside 0..S is clamped and reported as
+ * BRISK_ERR_INVALID_ARG in the device status. Two kernels. */
+brisk_status brisk_prefix_attend(const brisk_cache_dims *dims, const brisk_view *q,
+                                 const brisk_view *k_prefix, const brisk_view *v_prefix,
+                                 const brisk_view *k_own, const brisk_view *v_own,
+                                 const int32_t *own_len, const int32_t *visible, float scale,
+                                 void *out, float *lse, void *workspace, void *stream);
+
+/* The attention weight every own entry got, added up: acc_out[b, h, t] = decay * acc_in[b, h, t] +
+ * the sum over the block's positions that see t and the query heads of key head h of
+ * exp(scale q . k_t - lse), for t < own_len[b]; 0 for the rest of the S places. lse [B, L, Hq] f32 as
+ * brisk_prefix_attend left it for the same queries and entries (a row with -inf gives nothing);
+ * acc_in [B, Hkv, S] f32 or NULL (zeros; also the same buffer as acc_out); decay finite. The
+ * sums' order does not depend on timing. */
+brisk_status brisk_cache_weights(const brisk_cache_dims *dims, const brisk_view *q, const float *lse,
+                                 const brisk_view *k_own, const int32_t *own_len,
+                                 const int32_t *visible, float scale, float decay,
+                                 const float *acc_in, float *acc_out, void *workspace, void *stream);
+
+/* Cuts the own caches to `keep` entries. Of a sequence's n = own_len[b] entries, each key head keeps
+ * all if n <= keep; else the `recent` newest and the keep - recent of largest acc among the others
+ * (ties to the lowest index; NaN below every number). What is kept moves, in its old order, to the
+ * first places of k_to, v_to [B, >= keep, Hkv] and acc_to [B, Hkv, keep]; kept [B, Hkv, keep] int32
+ * gets the old indices and len_to [B] int32 min(n, keep). Of the first `keep` places those from
+ * len_to on get zeros (kept: -1). The targets must not overlap what is read (BRISK_ERR_INVALID_ARG
+ * where they start at the same address). keep >= 1, 0 <= recent <= keep; L, Hq and P are unused. */
+brisk_status brisk_cache_evict(const brisk_cache_dims *dims, const brisk_view *k, const brisk_view *v,
+                               const float *acc, const int32_t *own_len, int32_t keep, int32_t recent,
+                               const brisk_view *k_to, const brisk_view *v_to, float *acc_to,
+                               int32_t *len_to, int32_t *kept, void *workspace, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

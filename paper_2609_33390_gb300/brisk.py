@@ -48,6 +48,15 @@ class Events(ctypes.Structure):
                 ("sweep_p_end", _vp)]
 
 
+class CacheDims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "Hq", "Hkv", "D", "P", "S", "dtype")]
+
+
+class View(ctypes.Structure):
+    _fields_ = [("ptr", _vp), ("seq", ctypes.c_int64), ("tok", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
 class BriskError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -92,6 +101,17 @@ _SIGS = [
       _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     ("brisk_distill_loss", ctypes.c_int,
      [ctypes.POINTER(Dims), _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    ("brisk_cache_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(CacheDims)]),
+    ("brisk_prefix_attend", ctypes.c_int,
+     [ctypes.POINTER(CacheDims)] + [ctypes.POINTER(View)] * 5 +
+     [_vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    ("brisk_cache_weights", ctypes.c_int,
+     [ctypes.POINTER(CacheDims), ctypes.POINTER(View), _vp, ctypes.POINTER(View), _vp, _vp,
+      ctypes.c_float, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    ("brisk_cache_evict", ctypes.c_int,
+     [ctypes.POINTER(CacheDims), ctypes.POINTER(View), ctypes.POINTER(View), _vp, _vp,
+      ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(View), ctypes.POINTER(View), _vp, _vp, _vp,
+      _vp, _vp]),
 ]
 
 
@@ -403,3 +423,128 @@ def isd_costs(M: int):
 
 def tpf_isd(N: int, r: float) -> float:
     return float(lib().brisk_tpf_isd(int(N), float(r)))
+
+
+# ---------------------------------------------------------------- context cache
+
+class PrefixAttention:
+    """Attention of a batch's blocks over a shared prefix and the sequences' own caches, the weight
+    it gave each own entry, and the eviction by that weight, for one problem size.
+
+    B sequences of L query positions, ``Hq`` query heads over ``Hkv`` key heads of width ``D``, ``P``
+    shared prefix entries, room for ``S`` own entries a sequence; queries, keys and values in
+    ``dtype`` (bf16 or fp32). Tensors are [.., positions, heads, D] with any strides whose rows
+    start on 16 bytes (a transposed cache, a slice of a fused projection); lengths, sums and
+    outputs are contiguous. The workspace is allocated once here, so calls of one object must not overlap.
+    """
+
+    def __init__(self, B, L, Hq, Hkv, D, P, S, dtype, device="cuda"):
+        self.dims = CacheDims(B, L, Hq, Hkv, D, P, S, _dt(dtype))
+        self.B, self.L, self.Hq, self.Hkv, self.D, self.P, self.S = B, L, Hq, Hkv, D, P, S
+        self.dtype, self.device = dtype, torch.device(device)
+        ws = int(lib().brisk_cache_workspace_bytes(ctypes.byref(self.dims)))
+        if ws == 0:
+            raise BriskError(ERR_INVALID_ARG, "dims")
+        self.workspace = torch.zeros(ws, dtype=torch.uint8, device=self.device)
+        self.scale = D ** -0.5
+        self._d = ctypes.byref(self.dims)
+        self._ws = self.workspace.data_ptr()
+
+    def _view(self, t, shape, what):
+        """The tensor's address and strides; None for one that a size of zero leaves out."""
+        if t is None:
+            if 0 in shape:
+                return None
+            raise ValueError(f"{what} is missing")
+        if t.shape != shape or t.dtype != self.dtype:
+            raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {self.dtype}")
+        st = t.stride()
+        if not t.is_cuda:
+            raise ValueError(f"{what} is not on the GPU")
+        if st[-1] != 1:
+            raise ValueError(f"{what}: the last dimension must be contiguous")
+        return ctypes.byref(View(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2]))
+
+    @staticmethod
+    def _plain(t, shape, dtype, what):
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype != dtype:
+            raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
+        if not t.is_cuda:
+            raise ValueError(f"{what} is not on the GPU")
+        return _p(t)
+
+    def attend(self, q, k_prefix, v_prefix, k_own, v_own, own_len, visible=None, scale=None,
+               out=None, stream=None):
+        """out [B, L, Hq, D] and lse [B, L, Hq] of the queries q [B, L, Hq, D] over k/v_prefix
+        [P, Hkv, D] and the entries of k/v_own [B, S, Hkv, D] that own_len [B] and visible [B, L]
+        (int32; see brisk_prefix_attend) let them see. scale: D^-1/2 unless given. ``out``: a dict
+        of tensors to write to instead of new ones."""
+        B, L, Hq, Hkv, D, P, S = self.B, self.L, self.Hq, self.Hkv, self.D, self.P, self.S
+        if out is None:
+            out = {"out": torch.empty((B, L, Hq, D), dtype=self.dtype, device=self.device),
+                   "lse": torch.empty((B, L, Hq), dtype=torch.float32, device=self.device)}
+        pre, own = (P, Hkv, D), (B, S, Hkv, D)
+        _check(lib().brisk_prefix_attend(
+            self._d, self._view(q, (B, L, Hq, D), "q"), self._view(k_prefix, pre, "k_prefix"),
+            self._view(v_prefix, pre, "v_prefix"), self._view(k_own, own, "k_own"),
+            self._view(v_own, own, "v_own"), self._plain(own_len, (B,), torch.int32, "own_len"),
+            self._plain(visible, (B, L), torch.int32, "visible"),
+            self.scale if scale is None else float(scale),
+            self._plain(out["out"], (B, L, Hq, D), self.dtype, "out"),
+            self._plain(out["lse"], (B, L, Hq), torch.float32, "lse"), self._ws,
+            _stream(stream)), "prefix_attend")
+        return out
+
+    def weights(self, q, lse, k_own, own_len, acc=None, decay=1.0, visible=None, scale=None,
+                out=None, stream=None):
+        """decay * acc plus the attention weight every own entry got from the queries whose
+        log-sums ``lse`` attend() left: [B, Hkv, S] fp32, in ``out`` (which may be ``acc``) or a
+        new tensor. acc None: zeros."""
+        B, L, Hq, Hkv, D, S = self.B, self.L, self.Hq, self.Hkv, self.D, self.S
+        if out is None:
+            out = torch.empty((B, Hkv, S), dtype=torch.float32, device=self.device)
+        f32, i32 = torch.float32, torch.int32
+        _check(lib().brisk_cache_weights(
+            self._d, self._view(q, (B, L, Hq, D), "q"), self._plain(lse, (B, L, Hq), f32, "lse"),
+            self._view(k_own, (B, S, Hkv, D), "k_own"), self._plain(own_len, (B,), i32, "own_len"),
+            self._plain(visible, (B, L), i32, "visible"),
+            self.scale if scale is None else float(scale), float(decay),
+            self._plain(acc, (B, Hkv, S), f32, "acc"), self._plain(out, (B, Hkv, S), f32, "out"),
+            self._ws, _stream(stream)), "cache_weights")
+        return out
+
+    def alloc_evicted(self, keep, room=None):
+        """Targets of evict(): caches [B, room, Hkv, D] (room: ``keep`` unless given), sums and kept
+        indices [B, Hkv, keep], lengths [B]."""
+        B, Hkv, D = self.B, self.Hkv, self.D
+        room = keep if room is None else room
+        new = lambda shape, dt: torch.zeros(shape, dtype=dt, device=self.device)
+        return {"k": new((B, room, Hkv, D), self.dtype), "v": new((B, room, Hkv, D), self.dtype),
+                "acc": new((B, Hkv, keep), torch.float32),
+                "own_len": new((B,), torch.int32), "kept": new((B, Hkv, keep), torch.int32)}
+
+    def evict(self, k_own, v_own, acc, own_len, keep, recent, out=None, stream=None):
+        """Moves the ``recent`` newest entries and those of largest ``acc`` [B, Hkv, S], ``keep`` in
+        all, to the caches of ``out`` (see alloc_evicted and brisk_cache_evict): between two layers,
+        one spare pair of caches serves them all in turn."""
+        B, Hkv, D, S = self.B, self.Hkv, self.D, self.S
+        if out is None:
+            out = self.alloc_evicted(keep)
+        room, f32, i32 = out["k"].shape[1], torch.float32, torch.int32
+        if room < keep:
+            raise ValueError(f"the targets hold {room} entries, keep is {keep}")
+        own, to = (B, S, Hkv, D), (B, room, Hkv, D)
+        _check(lib().brisk_cache_evict(
+            self._d, self._view(k_own, own, "k_own"), self._view(v_own, own, "v_own"),
+            self._plain(acc, (B, Hkv, S), f32, "acc"), self._plain(own_len, (B,), i32, "own_len"),
+            int(keep), int(recent), self._view(out["k"], to, "k"), self._view(out["v"], to, "v"),
+            self._plain(out["acc"], (B, Hkv, keep), f32, "out acc"),
+            self._plain(out["own_len"], (B,), i32, "out own_len"),
+            self._plain(out["kept"], (B, Hkv, keep), i32, "kept"), self._ws,
+            _stream(stream)), "cache_evict")
+        return out
+
+    def device_status(self, clear=True, stream=None) -> int:
+        return int(lib().brisk_last_device_status(self._ws, int(clear), _stream(stream)))

@@ -1,0 +1,175 @@
+// C ABI of attention over a shared prefix, the attention weights of own entries and the eviction by
+// them: argument checks, workspace layout, launches.
+#include <math.h>
+
+#include "cache.cuh"
+
+using namespace brisk;
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+inline size_t up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+inline bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+inline size_t esize(int dt) { return dt == BRISK_DT_BF16 ? 2 : 4; }
+
+bool dims_ok(const brisk_cache_dims* d) {
+  if (!d || d->B < 1 || d->B > CACHE_MAX_B || d->L < 1 || d->Hkv < 1 || d->Hq < d->Hkv || d->Hq % d->Hkv != 0)
+    return false;
+  if (d->D < 8 || d->D > CACHE_MAX_D || d->D % 8 != 0 || d->P < 0 || d->S < 0) return false;
+  if (d->P > (1 << 30) || d->S > (1 << 30)) return false;
+  if (d->dtype != BRISK_DT_F32 && d->dtype != BRISK_DT_BF16) return false;
+  // query rows, and tiles of them over all keys, are counted in 32 and 62 bits
+  return (long long)d->B * d->L <= (1 << 30) / d->Hq;
+}
+
+// Element strides of a tensor of the given extents: rows start on 16 bytes, no dimension runs
+// backwards or stands still. An extent of one needs no stride (it is set to the row's).
+bool view_ok(const brisk_view* v, const brisk_cache_dims* d, long long seqs, long long toks, long long heads,
+             CacheView* out) {
+  *out = CacheView{};
+  if (seqs == 0 || toks == 0) return true;
+  if (!v || !v->ptr || !aligned(v->ptr, 16)) return false;
+  const long long ext[3] = {seqs, toks, heads}, in[3] = {v->seq, v->tok, v->head};
+  long long s[3];
+  const long long per16 = 16 / (long long)esize(d->dtype), most = (1LL << 39) / (long long)esize(d->dtype);
+  for (int i = 0; i < 3; ++i) {
+    s[i] = ext[i] > 1 ? in[i] : d->D;
+    if (s[i] < d->D || s[i] % per16 != 0 || s[i] >= most) return false;
+  }
+  out->p = v->ptr;
+  out->seq = s[0];
+  out->tok = s[1];
+  out->head = s[2];
+  return true;
+}
+
+struct CacheWs {
+  size_t status, errs, cum, part_p, ml_p, part_o, ml_o, total;
+};
+
+CacheWs cache_ws(const brisk_cache_dims* d) {
+  CacheWs w{};
+  const long long G = d->Hq / d->Hkv, LG = d->L * G, R = d->B * LG, rt = attend_rt(d->dtype);
+  const long long tiles_p = d->P > 0 ? (R + rt - 1) / rt * d->Hkv : 0;
+  const long long tiles_o = d->S > 0 ? (LG + rt - 1) / rt * d->Hkv * d->B : 0;
+  const long long rows_p = (tiles_p + CACHE_SMS) * (R < rt ? R : rt), rows_o = (tiles_o + CACHE_SMS) * (LG < rt ? LG : rt);
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t q = o; o = up(o + bytes); return q; };
+  w.status = take(ALIGN);
+  w.errs = take(sizeof(int32_t) * CACHE_SMS);
+  w.cum = take(sizeof(int32_t) * (d->B + 1));
+  w.ml_p = take(sizeof(float2) * rows_p);
+  w.ml_o = take(sizeof(float2) * rows_o);
+  w.part_p = take(sizeof(float) * rows_p * d->D);
+  w.part_o = take(sizeof(float) * rows_o * d->D);
+  w.total = o;
+  return w;
+}
+
+template <typename T>
+inline T* at(void* base, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(base) + off); }
+
+bool scale_ok(float s) { return s >= 0.f && s <= 3.0e38f; }
+
+}  // namespace
+
+extern "C" {
+
+size_t brisk_cache_workspace_bytes(const brisk_cache_dims* dims) {
+  return dims_ok(dims) ? cache_ws(dims).total : 0;
+}
+
+brisk_status brisk_prefix_attend(const brisk_cache_dims* d, const brisk_view* q, const brisk_view* k_prefix,
+                                 const brisk_view* v_prefix, const brisk_view* k_own, const brisk_view* v_own,
+                                 const int32_t* own_len, const int32_t* visible, float scale, void* out,
+                                 float* lse, void* ws, void* stream) {
+  if (!dims_ok(d) || !own_len || !out || !aligned(out, 16) || !ws || !aligned(ws, ALIGN) || !scale_ok(scale))
+    return BRISK_ERR_INVALID_ARG;
+  AttendArgs a{};
+  if (!view_ok(q, d, d->B, d->L, d->Hq, &a.q) || !view_ok(k_prefix, d, 1, d->P, d->Hkv, &a.kp) ||
+      !view_ok(v_prefix, d, 1, d->P, d->Hkv, &a.vp) || !view_ok(k_own, d, d->B, d->S, d->Hkv, &a.ko) ||
+      !view_ok(v_own, d, d->B, d->S, d->Hkv, &a.vo))
+    return BRISK_ERR_INVALID_ARG;
+  const CacheWs w = cache_ws(d);
+  a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.P = d->P; a.S = d->S;
+  a.dt = d->dtype;
+  a.own_len = own_len;
+  a.visible = visible;
+  a.sl2 = scale * LOG2E;
+  a.out = out;
+  a.lse = lse;
+  a.part_p = at<float>(ws, w.part_p);
+  a.part_o = at<float>(ws, w.part_o);
+  a.ml_p = at<float2>(ws, w.ml_p);
+  a.ml_o = at<float2>(ws, w.ml_o);
+  a.cum = at<int32_t>(ws, w.cum);
+  a.errs = at<int32_t>(ws, w.errs);
+  a.status = at<int32_t>(ws, w.status);
+  a.grid = CACHE_SMS;
+  a.wait_limit = wait_limit_cycles();
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (launch_attend_f32(a, st) != cudaSuccess) return BRISK_ERR_CUDA;
+  if (launch_merge(a, st) != cudaSuccess) return BRISK_ERR_CUDA;
+  return BRISK_OK;
+}
+
+brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q, const float* lse,
+                                 const brisk_view* k_own, const int32_t* own_len, const int32_t* visible,
+                                 float scale, float decay, const float* acc_in, float* acc_out, void* ws,
+                                 void* stream) {
+  if (!dims_ok(d) || !lse || !own_len || (d->S > 0 && !acc_out) || !ws || !aligned(ws, ALIGN) ||
+      !scale_ok(scale) || !isfinite(decay))
+    return BRISK_ERR_INVALID_ARG;
+  WeightArgs a{};
+  if (!view_ok(q, d, d->B, d->L, d->Hq, &a.q) || !view_ok(k_own, d, d->B, d->S, d->Hkv, &a.ko))
+    return BRISK_ERR_INVALID_ARG;
+  // one CTA a key tile: their number is a grid's first dimension
+  if ((long long)d->B * d->Hkv * ((d->S + 63) / 64) > 0x7fffffffLL) return BRISK_ERR_UNSUPPORTED;
+  a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.S = d->S; a.dt = d->dtype;
+  a.own_len = own_len;
+  a.visible = visible;
+  a.lse = lse;
+  a.sl2 = scale * LOG2E;
+  a.decay = decay;
+  a.acc_in = acc_in;
+  a.acc_out = acc_out;
+  a.status = at<int32_t>(ws, cache_ws(d).status);
+  a.wait_limit = wait_limit_cycles();
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
+  return launch_weights_simt(a, st) == cudaSuccess ? BRISK_OK : BRISK_ERR_CUDA;
+}
+
+brisk_status brisk_cache_evict(const brisk_cache_dims* d, const brisk_view* k, const brisk_view* v,
+                               const float* acc, const int32_t* own_len, int32_t keep, int32_t recent,
+                               const brisk_view* k_to, const brisk_view* v_to, float* acc_to,
+                               int32_t* len_to, int32_t* kept, void* ws, void* stream) {
+  if (!dims_ok(d) || keep < 1 || keep > (1 << 30) || recent < 0 || recent > keep || (d->S > 0 && !acc) ||
+      !own_len || !acc_to || !len_to || !kept || !ws || !aligned(ws, ALIGN))
+    return BRISK_ERR_INVALID_ARG;
+  EvictArgs a{};
+  if (!view_ok(k, d, d->B, d->S, d->Hkv, &a.k) || !view_ok(v, d, d->B, d->S, d->Hkv, &a.v) ||
+      !view_ok(k_to, d, d->B, keep, d->Hkv, &a.k_to) || !view_ok(v_to, d, d->B, keep, d->Hkv, &a.v_to))
+    return BRISK_ERR_INVALID_ARG;
+  // entries move between buffers: a place may be written before it is read
+  const void *from[2] = {a.k.p, a.v.p}, *to[2] = {a.k_to.p, a.v_to.p};
+  for (const void* f : from)
+    for (const void* t : to)
+      if (f == t) return BRISK_ERR_INVALID_ARG;
+  if (acc == acc_to || own_len == len_to || a.k_to.p == a.v_to.p) return BRISK_ERR_INVALID_ARG;
+  const long long vecs = (long long)d->B * keep * d->Hkv * (d->D * (long long)esize(d->dtype) / 16);
+  if (vecs / 1024 >= 0x7fffffffLL) return BRISK_ERR_UNSUPPORTED;
+  a.B = d->B; a.Hkv = d->Hkv; a.D = d->D; a.S = d->S; a.dt = d->dtype; a.keep = keep; a.recent = recent;
+  a.acc = acc;
+  a.own_len = own_len;
+  a.acc_to = acc_to;
+  a.len_to = len_to;
+  a.kept = kept;
+  a.status = at<int32_t>(ws, cache_ws(d).status);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
+  return launch_evict(a, st) == cudaSuccess ? BRISK_OK : BRISK_ERR_CUDA;
+}
+
+}  // extern "C"
