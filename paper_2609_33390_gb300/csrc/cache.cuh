@@ -203,12 +203,13 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
 }
 
-// Rows and keys of a tile of the fp32 kernel.
-constexpr int ATTEND_KT_F32 = 64;
-constexpr int ATTEND_RT_F32 = 64;
-int attend_rt(int dt);
-int attend_kt(int dt);
+// Rows and keys of a tile: bf16 on the tensor cores, fp32 on the FMA units.
+constexpr int ATTEND_RT_TC = 256, ATTEND_KT_TC = 128;
+constexpr int ATTEND_RT_F32 = 64, ATTEND_KT_F32 = 64;
+inline int attend_rt(int dt) { return dt == BRISK_DT_BF16 ? ATTEND_RT_TC : ATTEND_RT_F32; }
+inline int attend_kt(int dt) { return dt == BRISK_DT_BF16 ? ATTEND_KT_TC : ATTEND_KT_F32; }
 
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream);
 

@@ -109,7 +109,10 @@ brisk_status brisk_prefix_attend(const brisk_cache_dims* d, const brisk_view* q,
   a.grid = CACHE_SMS;
   a.wait_limit = wait_limit_cycles();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (launch_attend_f32(a, st) != cudaSuccess) return BRISK_ERR_CUDA;
+  // a scale of 0 would make NaN of the masked scores' -inf; this one leaves every finite score at 0
+  if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
+  if ((d->dtype == BRISK_DT_BF16 ? launch_attend_tc(a, st) : launch_attend_f32(a, st)) != cudaSuccess)
+    return BRISK_ERR_CUDA;
   if (launch_merge(a, st) != cudaSuccess) return BRISK_ERR_CUDA;
   return BRISK_OK;
 }

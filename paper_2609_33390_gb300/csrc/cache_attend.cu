@@ -300,9 +300,6 @@ merge_kernel(const __grid_constant__ AttendArgs a, int rt, int kt) {
 
 }  // namespace
 
-int attend_rt(int) { return ATTEND_RT_F32; }
-int attend_kt(int) { return ATTEND_KT_F32; }
-
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
   auto run = [&](auto kernel, size_t smem) {
     cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
@@ -310,7 +307,6 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
     kernel<<<a.grid, SIMT_THREADS, smem, stream>>>(a);
     return cudaGetLastError();
   };
-  if (a.dt == BRISK_DT_BF16) return run(attend_simt_kernel<__nv_bfloat16, ATTEND_RT_F32>, simt_smem(ATTEND_RT_F32));
   return run(attend_simt_kernel<float, ATTEND_RT_F32>, simt_smem(ATTEND_RT_F32));
 }
 
