@@ -24,7 +24,7 @@ struct AttendArgs {
   float sl2;                         // scale * log2(e)
   void* out;                         // [B, L, Hkv * G, D]
   float* lse;                        // [B, L, Hkv * G] or nullptr
-  // workspace: parts of rows whose keys were divided, by slot (see Plan): sums [rows][D] and
+  // workspace: parts of rows whose keys were divided, by slot (see Plan): sums (see part_at) and
   // (running maximum in log2 units, sum of exponentials)
   float *part_p, *part_o;
   float2 *ml_p, *ml_o;
@@ -41,15 +41,14 @@ struct AttendArgs {
 // sequences form common tiles (its keys are read once for RT rows, whichever sequence they are of);
 // over the own caches, the rows of one sequence. All units stand in one sequence: first the prefix's
 // (by head, row tile, key tile), then the own caches' (by sequence, head, row tile, key tile), and
-// each of N CTAs takes the same share of it, wherever that begins and ends. A row tile's keys may so
+// each CTA takes `share` of them, wherever that begins and ends. A row tile's keys may so
 // be divided over several CTAs, each of which leaves a part; the parts are joined by merge_kernel.
 // Slots: walking through the sequence, (item index + CTA) grows with every (item, CTA) pair, so it
-// numbers the parts.
+// numbers the parts. Counts of units fit 31 bits (checked on the host).
 struct Plan {
-  int B, LG, Hkv, P, RT, KT, N;
+  int B, LG, Hkv, P, RT, KT;
   int nPT, kP, nLT;                  // row tiles and key tiles of the prefix; row tiles of a sequence
-  int R;                             // rows a key head
-  long long UP, T;                   // units of the prefix; all units
+  int R, UP, T, share;               // rows a key head; units of the prefix; all units; units a CTA
 
   __device__ Plan(const AttendArgs& a, int rt, int kt, int own_tiles) {
     B = a.B; LG = a.L * a.G; Hkv = a.Hkv; P = a.P; RT = rt; KT = kt;
@@ -57,39 +56,34 @@ struct Plan {
     kP = (P + KT - 1) / KT;
     nPT = P > 0 ? (R + RT - 1) / RT : 0;
     nLT = (LG + RT - 1) / RT;
-    UP = (long long)Hkv * nPT * kP;
-    T = UP + (long long)Hkv * nLT * own_tiles;
-    N = T < a.grid ? (int)T : a.grid;
+    UP = Hkv * nPT * kP;
+    T = UP + Hkv * nLT * own_tiles;
+    share = max(1, (int)(((unsigned)T + a.grid - 1) / a.grid));
   }
-  __device__ long long first_unit(int c) const { return (long long)c * T / N; }
-  __device__ int cta_of(long long u) const { return (int)(((u + 1) * N - 1) / T); }
-  __device__ long long own_start(const int32_t* cum, int b, int h, int lt) const {
-    const long long n = cum[b + 1] - cum[b];
-    return UP + (long long)Hkv * nLT * cum[b] + (h * nLT + lt) * n;
+  __device__ int cta_of(int u) const { return u / share; }
+  __device__ int own_start(const int32_t* cum, int b, int h, int lt) const {
+    return UP + Hkv * nLT * cum[b] + (h * nLT + lt) * (cum[b + 1] - cum[b]);
   }
 };
 
 // A CTA's share of one item (a row tile's keys): key tiles [k0, k0 + n).
 struct Frag {
-  bool prefix, whole;                // whole: no other part for these rows exists
+  int prefix, whole;                 // whole: no other part for these rows exists
   int h, b, tile, k0, n;
   int row0, rows;                    // rows of the head over the prefix, of the sequence else
-  long long slot;
+  int slot;
 };
 
 struct Walk {
-  long long u, end;
-  int c, b;
+  int u, end, c, b;
 
   __device__ Walk(const Plan& p, const int32_t* cum, int cta) {
     c = cta;
     b = 0;
-    u = end = 0;
-    if (cta >= p.N) return;
-    u = p.first_unit(cta);
-    end = p.first_unit(cta + 1);
+    u = (int)min((long long)p.T, (long long)cta * p.share);
+    end = (int)min((long long)p.T, (long long)u + p.share);
     if (end > p.UP) {                // the sequence of the first unit behind the prefix's
-      const long long v = (u > p.UP ? u - p.UP : 0) / (p.Hkv * p.nLT);
+      const int v = (u > p.UP ? u - p.UP : 0) / (p.Hkv * p.nLT);
       int lo = 0, hi = p.B - 1;      // the last b with cum[b] <= v
       while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
@@ -101,43 +95,48 @@ struct Walk {
   __device__ bool next(const Plan& p, const int32_t* cum, Frag& f) {
     if (u >= end) return false;
     if (u < p.UP) {
-      const int item = (int)(u / p.kP);
-      f.prefix = true;
-      f.k0 = (int)(u - (long long)item * p.kP);
-      f.n = (int)min((long long)(p.kP - f.k0), end - u);
+      const int item = u / p.kP;
+      f.prefix = 1;
+      f.k0 = u - item * p.kP;
+      f.n = min(p.kP - f.k0, end - u);
       f.h = item / p.nPT;
       f.tile = item - f.h * p.nPT;
       f.b = 0;
       f.row0 = f.tile * p.RT;
       f.rows = min(p.RT, p.R - f.row0);
-      f.slot = (long long)item + c;
+      f.slot = item + c;
       const int b0 = f.row0 / p.LG, b1 = (f.row0 + f.rows - 1) / p.LG;
       f.whole = f.n == p.kP && cum[b1 + 1] == cum[b0];
     } else {
       const int per = p.Hkv * p.nLT;
-      long long base = p.UP + (long long)per * cum[b];
-      int n = cum[b + 1] - cum[b];
-      while (u >= base + (long long)per * n) {
-        base += (long long)per * n;
+      int base = p.UP + per * cum[b], n = cum[b + 1] - cum[b];
+      while (u >= base + per * n) {
+        base += per * n;
         ++b;
         n = cum[b + 1] - cum[b];
       }
-      const int r = (int)((u - base) / n);
-      f.prefix = false;
+      const int r = (u - base) / n;
+      f.prefix = 0;
       f.b = b;
       f.h = r / p.nLT;
       f.tile = r - f.h * p.nLT;
-      f.k0 = (int)(u - base - (long long)r * n);
-      f.n = (int)min((long long)(n - f.k0), end - u);
+      f.k0 = u - base - r * n;
+      f.n = min(n - f.k0, end - u);
       f.row0 = f.tile * p.RT;
       f.rows = min(p.RT, p.LG - f.row0);
-      f.slot = ((long long)b * p.Hkv + f.h) * p.nLT + f.tile + c;
+      f.slot = (b * p.Hkv + f.h) * p.nLT + f.tile + c;
       f.whole = f.n == n && p.P == 0;
     }
     u += f.n;
     return true;
   }
 };
+
+// A part's sums lie by groups of four columns, then rows: [D / 4][rows of a slot][4], so that neighbouring
+// rows, which are neighbouring lanes of the kernels on both sides, lie side by side.
+__device__ __forceinline__ long long part_at(long long slot, int per, int D, int row, int c) {
+  return slot * per * D + ((long long)(c >> 2) * per + row) * 4;
+}
 
 __device__ __forceinline__ int clamped_len(const AttendArgs& a, int b) {
   return min(max(a.own_len[b], 0), a.S);

@@ -67,6 +67,14 @@ CacheWs cache_ws(const brisk_cache_dims* d) {
   return w;
 }
 
+// Whether attention's units of work, all caches full, are counted in 31 bits.
+bool units_ok(const brisk_cache_dims* d) {
+  const long long G = d->Hq / d->Hkv, LG = d->L * G, R = d->B * LG, rt = attend_rt(d->dtype), kt = attend_kt(d->dtype);
+  const double pre = (double)d->Hkv * ((R + rt - 1) / rt) * ((d->P + kt - 1) / kt);
+  const double own = (double)d->Hkv * d->B * ((LG + rt - 1) / rt) * ((d->S + kt - 1) / kt);
+  return pre + own < 2.0e9;
+}
+
 template <typename T>
 inline T* at(void* base, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(base) + off); }
 
@@ -91,6 +99,7 @@ brisk_status brisk_prefix_attend(const brisk_cache_dims* d, const brisk_view* q,
       !view_ok(v_prefix, d, 1, d->P, d->Hkv, &a.vp) || !view_ok(k_own, d, d->B, d->S, d->Hkv, &a.ko) ||
       !view_ok(v_own, d, d->B, d->S, d->Hkv, &a.vo))
     return BRISK_ERR_INVALID_ARG;
+  if (!units_ok(d)) return BRISK_ERR_UNSUPPORTED;
   const CacheWs w = cache_ws(d);
   a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.P = d->P; a.S = d->S;
   a.dt = d->dtype;

@@ -203,14 +203,13 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
           a.lse[(long long)token * (a.Hkv * a.G) + head] = none ? -INFINITY : (m[i] + log2f(l[i])) * (1.f / LOG2E);
       } else {
         const int per = f.prefix ? min(RT, plan.R) : min(RT, plan.LG);
-        const long long at = f.slot * per + r;
-        float* to = (f.prefix ? a.part_p : a.part_o) + at * D;
+        float* to = f.prefix ? a.part_p : a.part_o;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int c = 64 * j + 4 * tx;
-          if (c < D) store4(to + c, make_float4(o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]));
+          if (c < D) store4(to + part_at(f.slot, per, D, r, c), make_float4(o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]));
         }
-        if (tx == 0) (f.prefix ? a.ml_p : a.ml_o)[at] = make_float2(m[i], l[i]);
+        if (tx == 0) (f.prefix ? a.ml_p : a.ml_o)[(long long)f.slot * per + r] = make_float2(m[i], l[i]);
       }
     }
   }
@@ -221,80 +220,90 @@ constexpr size_t simt_smem(int rt) {
          sizeof(int32_t) * (CACHE_MAX_B + 1);
 }
 
-// Joins the parts of the rows whose keys were divided: one warp a row, a lane four columns.
+// Joins the parts of the rows whose keys were divided. A warp takes 8 neighbouring rows of a key head,
+// 4 lanes a row, each with every fourth group of four columns: its loads are runs of 128 bytes.
+// Bound by the parts' bytes, which the kernel before left in L2 where there is room.
 constexpr int MERGE_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(MERGE_THREADS)
 merge_kernel(const __grid_constant__ AttendArgs a, int rt, int kt) {
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, cq = lane >> 3;
   const Plan plan(a, rt, kt, a.cum[a.B]);
-  const int Hq = a.Hkv * a.G;
-  const int rows = a.B * a.L * Hq, per_p = min(rt, plan.R), per_o = min(rt, plan.LG);
-  for (int row = (int)blockIdx.x * (MERGE_THREADS / 32) + (threadIdx.x >> 5); row < rows;
-       row += (int)gridDim.x * (MERGE_THREADS / 32)) {
-    const int token = row / Hq, head = row - token * Hq, h = head / a.G, g = head - h * a.G;
-    const int b = token / a.L;
+  const int per_p = min(rt, plan.R), per_o = min(rt, plan.LG), D = a.D;
+  const int groups = (plan.R + 7) / 8;             // of a key head
+  for (int w = (int)blockIdx.x * (MERGE_THREADS / 32) + (threadIdx.x >> 5); w < groups * a.Hkv;
+       w += (int)gridDim.x * (MERGE_THREADS / 32)) {
+    const int h = w / groups, r = (w - h * groups) * 8 + (lane & 7);
     // the parts over the prefix, then those over the own cache: a run of slots each
-    long long at_p = 0, at_o = 0;
-    int np = 0, no = 0;
-    bool written = false;                           // by the only CTA that had these rows' keys
-    if (plan.kP > 0) {
-      const int r = token * a.G + g, pt = r / rt;
-      const long long item = h * plan.nPT + pt;
-      const int c0 = plan.cta_of(item * plan.kP), c1 = plan.cta_of(item * plan.kP + plan.kP - 1);
-      np = c1 - c0 + 1;
-      at_p = (item + c0) * per_p + (r - pt * rt);
-      const int b0 = pt * rt / plan.LG, b1 = min(pt * rt + rt, plan.R) - 1;
-      written = np == 1 && a.cum[b1 / plan.LG + 1] == a.cum[b0];
-    }
-    const int n = a.cum[b + 1] - a.cum[b];
-    if (n > 0) {
-      const int r = (token - b * a.L) * a.G + g, lt = r / rt;
-      const long long u = plan.own_start(a.cum, b, h, lt);
-      const int c0 = plan.cta_of(u), c1 = plan.cta_of(u + n - 1);
-      no = c1 - c0 + 1;
-      at_o = (((long long)b * a.Hkv + h) * plan.nLT + lt + c0) * per_o + (r - lt * rt);
-    }
-    if (written || (np == 0 && no == 1)) continue;
-    float top = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!row_idle(a, token))
-      for (int i0 = 0; i0 < np + no; i0 += 32) {
-        const int i = i0 + lane;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (i < np) ml = a.ml_p[at_p + i * per_p];
-        else if (i < np + no) ml = a.ml_o[at_o + (i - np) * per_o];
-        const float mn = fmaxf(top, warp_max(ml.x));
-        const float ms = mn == -INFINITY ? 0.f : mn;
-        const float w = ex2(ml.x - ms), was = ex2(top - ms);
-        l = l * was + warp_sum((ml.x == mn ? 1.f : w) * ml.y);   // (a part without a finite score: 0, or NaN)
-        o.x *= was; o.y *= was; o.z *= was; o.w *= was;
-        top = mn;
-        const int cnt = min(32, np + no - i0);
-#pragma unroll 4
-        for (int j = 0; j < cnt; ++j) {
-          const float wj = __shfl_sync(FULL_MASK, w, j);
-          const int k = i0 + j;
-          const float* src = k < np ? a.part_p + (at_p + k * per_p) * a.D : a.part_o + (at_o + (k - np) * per_o) * a.D;
-          if (4 * lane < a.D && wj != 0.f) {
-            const float4 x = load4(src + 4 * lane);
-            o.x = fmaf(wj, x.x, o.x);
-            o.y = fmaf(wj, x.y, o.y);
-            o.z = fmaf(wj, x.z, o.z);
-            o.w = fmaf(wj, x.w, o.w);
-          }
-        }
+    const float *src_p = nullptr, *src_o = nullptr;
+    const float2 *ml_p = nullptr, *ml_o = nullptr;
+    int np = 0, no = 0, token = 0;
+    bool mine = r < plan.R;                        // (and not written by the only CTA that had its keys)
+    if (mine) {
+      token = r / a.G;
+      const int b = r / plan.LG, n = a.cum[b + 1] - a.cum[b];
+      if (plan.kP > 0) {
+        const int pt = r / rt, item = h * plan.nPT + pt, c0 = plan.cta_of(item * plan.kP);
+        np = plan.cta_of(item * plan.kP + plan.kP - 1) - c0 + 1;
+        src_p = a.part_p + part_at(item + c0, per_p, D, r - pt * rt, 4 * cq);
+        ml_p = a.ml_p + (long long)(item + c0) * per_p + (r - pt * rt);
+        const int b0 = pt * rt / plan.LG, b1 = (min(pt * rt + rt, plan.R) - 1) / plan.LG;
+        if (np == 1 && a.cum[b1 + 1] == a.cum[b0]) mine = false;
       }
+      if (n > 0) {
+        const int ro = r - b * plan.LG, lt = ro / rt, u = plan.own_start(a.cum, b, h, lt);
+        const int c0 = plan.cta_of(u), slot = (b * a.Hkv + h) * plan.nLT + lt + c0;
+        no = plan.cta_of(u + n - 1) - c0 + 1;
+        src_o = a.part_o + part_at(slot, per_o, D, ro - lt * rt, 4 * cq);
+        ml_o = a.ml_o + (long long)slot * per_o + (ro - lt * rt);
+        if (np == 0 && no == 1) mine = false;
+      }
+    }
+    const bool idle = mine && row_idle(a, token);
+    const int parts = mine && !idle ? np + no : 0;
+    float m = -INFINITY, l = 0.f;
+    float4 o[CACHE_MAX_D / 16];
+#pragma unroll
+    for (int k = 0; k < CACHE_MAX_D / 16; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < parts; ++i) {
+      const bool pre = i < np;
+      const int per = pre ? per_p : per_o, at = pre ? i : i - np;
+      const float2 ml = (pre ? ml_p : ml_o)[(long long)at * per];
+      const float* src = (pre ? src_p : src_o) + (long long)at * per * D;
+      float4 x[CACHE_MAX_D / 16];
+#pragma unroll
+      for (int k = 0; k < CACHE_MAX_D / 16; ++k)
+        x[k] = 4 * cq + 16 * k < D ? load4(src + (long long)k * per * 16) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.f : mn;
+      // (a part without a finite score has sums of 0, or NaN, which pass)
+      const float was = m == mn ? 1.f : ex2(m - ms), wi = ml.x == mn ? 1.f : ex2(ml.x - ms);
+      m = mn;
+      l = l * was + wi * ml.y;
+#pragma unroll
+      for (int k = 0; k < CACHE_MAX_D / 16; ++k) {
+        o[k].x = fmaf(wi, x[k].x, o[k].x * was);
+        o[k].y = fmaf(wi, x[k].y, o[k].y * was);
+        o[k].z = fmaf(wi, x[k].z, o[k].z * was);
+        o[k].w = fmaf(wi, x[k].w, o[k].w * was);
+      }
+    }
+    if (!mine) continue;
     const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
-    if (4 * lane < a.D)
-      store4(static_cast<T*>(a.out) + (long long)row * a.D + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (a.lse && lane == 0) a.lse[row] = none ? -INFINITY : (top + log2f(l)) * (1.f / LOG2E);
+    const long long row = (long long)token * (a.Hkv * a.G) + h * a.G + (r - token * a.G);
+    T* to = static_cast<T*>(a.out) + row * D + 4 * cq;
+#pragma unroll
+    for (int k = 0; k < CACHE_MAX_D / 16; ++k)
+      if (4 * cq + 16 * k < D)
+        store4(to + 16 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                 : make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
+    if (a.lse && cq == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    int code = BRISK_OK;
-    for (int c = 0; c < a.grid && code == BRISK_OK; ++c) code = a.errs[c];
-    *a.status = code;
+  if (blockIdx.x == 0 && threadIdx.x < 32) {
+    int code = BRISK_OK;                           // the largest: a wait that gave up before a bad length
+    for (int c = lane; c < a.grid; c += 32) code = max(code, a.errs[c]);
+    code = __reduce_max_sync(FULL_MASK, code);
+    if (lane == 0) *a.status = code;
   }
 }
 
@@ -311,7 +320,7 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {
-  const int rows = a.B * a.L * a.Hkv * a.G, ctas = (rows + MERGE_THREADS / 32 - 1) / (MERGE_THREADS / 32);
+  const int warps = (a.B * a.L * a.G + 7) / 8 * a.Hkv, ctas = (warps + MERGE_THREADS / 32 - 1) / (MERGE_THREADS / 32);
   const int grid = ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS;
   if (a.dt == BRISK_DT_BF16)
     merge_kernel<__nv_bfloat16><<<grid, MERGE_THREADS, 0, stream>>>(a, attend_rt(a.dt), attend_kt(a.dt));

@@ -27,7 +27,7 @@ namespace {
 
 constexpr int KT = ATTEND_KT_TC, RT = ATTEND_RT_TC, SLOT = 128;
 constexpr int SOFT_THREADS = 2 * SLOT;
-constexpr int ATT_THREADS = SOFT_THREADS + 64;     // and a copying and an issuing warp
+constexpr int ATT_THREADS = SOFT_THREADS + 128;    // and a copying, an issuing and two planning warps
 constexpr float LAZY = 8.f;                        // log2 of what a score may exceed the held maximum by
 constexpr uint32_t TMEM_COLS = 512;                // S0 | S1 | O0 | O1, 128 columns each
 constexpr int PANEL = KT * 128;                    // bytes of 64 columns of a tile
@@ -52,9 +52,6 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(su32(bar)) : "memory");
 }
-// The barrier of the two slots' warps.
-__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
 // Places of the key and value tiles of a fragment of n tiles in the ring's order, which is the order
 // in which the issuing thread takes them.
 __device__ __forceinline__ int k_place(bool pair, int j) { return pair ? 2 * j : (j == 0 ? 0 : 2 * j - 1); }
@@ -71,20 +68,62 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t x) {
   return x;
 }
 
+// Two fp32 in one 64-bit register: one instruction for both.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pack2(float x, float y) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& x, float& y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 x, f32x2 y, f32x2 z) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 x, f32x2 y) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
+
+// Adds the infinities and NaN of the own values t0 <= t < t1 to a row's 32 columns from c on.
+__device__ __noinline__ void add_odd(const AttendArgs& a, int b, int h, int c, int t0, int t1, float (&o)[32]) {
+  for (int t = t0; t < t1; ++t) {
+    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.vo.p) + b * a.vo.seq + t * a.vo.tok + h * a.vo.head + c;
+    for (int i = 0; i < 32 && c + i < a.D; ++i) {
+      const float x = __bfloat162float(v[i]);
+      if (!isfinite(x)) o[i] += x;
+    }
+  }
+}
+
+// What the planning warps tell the others of a fragment.
+struct FragInfo {
+  Frag f;
+  int len;                                         // entries of the prefix, or in use of the own cache
+  int low[2];                                      // entries from here on are hidden from some row
+};
+
 template <int DP>
 __global__ void __launch_bounds__(ATT_THREADS, 1)
 attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant__ AttendArgs a) {
   using Sh = Shape<DP>;
-  constexpr int STAGES = Sh::STAGES, TILE = Sh::TILE;
+  constexpr int STAGES = Sh::STAGES, TILE = Sh::TILE, VPR = DP / 8;   // 16-byte pieces of a row
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = base;                              // [2][DP / 64][128 rows][128 B], swizzled
   uint8_t* ring = base + 2 * TILE;
   int32_t* cum = reinterpret_cast<int32_t*>(ring + STAGES * TILE);
-  __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2], o_full[2], q_full, done;
+  __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2], o_full[2];
+  __shared__ uint64_t frag_full[2], frag_empty[2], q_free[2], slots, done;
+  __shared__ FragInfo info[2];
+  __shared__ int row_id[2][RT], row_lim[2][RT];    // token * Hq + head (its complement: padding), keys seen
   __shared__ uint32_t tmem_slot;
-  __shared__ int aborted, bad, warp_sum[ATT_THREADS / 32], low_of[8], odd_of[8];
-  __shared__ float2 ml_of[2][SLOT];
+  __shared__ int aborted, bad, warp_sum[ATT_THREADS / 32], odd_of[2][8];
+  __shared__ float2 ml_of[2][2][SLOT];
   volatile int* abort_flag = &aborted;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -97,8 +136,11 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
       mbar_init(&s_full[s], 1);
       mbar_init(&p_ready[s], 4);                   // a lane of each of the slot's warps
       mbar_init(&o_full[s], 1);
+      mbar_init(&frag_full[s], 2);                 // the planning warps
+      mbar_init(&frag_empty[s], 8);                // the slots' warps
+      mbar_init(&q_free[s], 1);
     }
-    mbar_init(&q_full, 1);
+    mbar_init(&slots, 8);
     mbar_init(&done, 1);
     aborted = 0;
     bad = 0;
@@ -116,198 +158,268 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
   if (blockIdx.x == 0)
     for (int b = tid; b <= a.B; b += ATT_THREADS) a.cum[b] = cum[b];
 
+  // Waits for a phase; true if this or another wait gave up, the same answer for the whole warp: each
+  // warp then leaves its loop for the barrier at the end.
   auto wait = [&](uint64_t* bar, int phase) {
-    if (*abort_flag) return false;
-    if (mbar_wait(bar, phase & 1, abort_flag, a.wait_limit)) return true;
-    *abort_flag = 1;
-    return false;
+    if (!*abort_flag && !mbar_wait(bar, phase & 1, abort_flag, a.wait_limit)) *abort_flag = 1;
+    return __any_sync(FULL_MASK, *abort_flag != 0) != 0;
   };
-  Walk walk(plan, cum, blockIdx.x);
-  Frag f;
   int pos = 0;                                     // ring places of the fragments before this one
+  int nf = 0;                                      // fragments before this one: it uses the words nf & 1
 
-  if (warp == 8) {
-    if (lane == 0) {
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 8) {
       // copies: a key or value tile at a time, in the ring's order
+      Walk walk(plan, cum, blockIdx.x);
+      Frag f;
       int issued = 0;
-      while (walk.next(plan, cum, f)) {
+      bool off = false;
+      while (!off && walk.next(plan, cum, f)) {
         const bool pair = f.rows > SLOT;
         const CUtensorMap* mk = f.prefix ? &maps.kp : &maps.ko;
         const CUtensorMap* mv = f.prefix ? &maps.vp : &maps.vo;
-        int nk = 0, nvt = 0;
+        int nk = 0, nv = 0;
         for (int i = 0; i < 2 * f.n; ++i) {
           const bool key = nk < f.n && k_place(pair, nk) == i;
-          const int t0 = (f.k0 + (key ? nk++ : nvt++)) * KT, p = pos + i, st = p % STAGES;
-          if (p >= STAGES) wait(&empty[st], p / STAGES - 1);
-          if (*abort_flag) break;
-          mbar_expect_tx(&full[st], TILE);
-          for (int c = 0; c < DP / 64; ++c)
-            tma_load_4d(ring + st * TILE + c * PANEL, key ? mk : mv, &full[st], c * 64, f.h, t0, f.b);
+          const int t0 = (f.k0 + (key ? nk++ : nv++)) * KT, p = pos + i, st = p % STAGES;
+          off = p >= STAGES && wait(&empty[st], p / STAGES - 1);
+          if (off) break;
+          if (elect_one()) {
+            mbar_expect_tx(&full[st], TILE);
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c)
+              tma_load_4d(ring + st * TILE + c * PANEL, key ? mk : mv, &full[st], c * 64, f.h, t0, f.b);
+          }
+          __syncwarp();
           issued = p + 1;
         }
         pos += 2 * f.n;
       }
-      if (*abort_flag)
+      if (off)
         for (int p = issued > STAGES ? issued - STAGES : 0; p < issued; ++p)
           mbar_drain(&full[p % STAGES], (p / STAGES) & 1);
-    }
-  } else if (warp == 9) {
-    if (lane == 0) {
-      // products
+    } else if (warp == 9) {
+      // products, issued by one lane; the warp stays together around it
       const int nd = (a.D + 15) / 16;              // 16 columns a step of Q K^T, and a unit of O's width
       const uint32_t id_s = idesc_bf16(SLOT, KT), id_o = idesc_bf16(SLOT, 16 * nd) | IDESC_B_MN;
-      int nfrag = 0, nready[2] = {0, 0};
-      auto scores = [&](int s, int qslot, int st) {
-        if (*abort_flag) return;
-        const uint32_t qa = su32(sQ + qslot * TILE), ka = su32(ring + st * TILE);
-        for (int kk = 0; kk < nd; ++kk) {
-          const uint64_t off = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
-          umma(tmem + s * 128, sw128_desc(qa) + off, sw128_desc(ka) + off, id_s, kk > 0);
-        }
-        umma_commit(&s_full[s]);
+      const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
+      int nready[2] = {0, 0};
+      const int places = 2 * (min(plan.T, ((int)blockIdx.x + 1) * plan.share) - (int)blockIdx.x * plan.share);
+      bool off = false;                            // a wait gave up: nothing more is issued
+      auto commit = [&](uint64_t* bar) {
+        if (off) return;
+        if (elect_one()) umma_commit(bar);
+        __syncwarp();
       };
-      while (walk.next(plan, cum, f)) {
-        const bool pair = f.rows > SLOT;
-        const int end = f.prefix ? a.P : clamped_len(a, f.b);
+      auto scores = [&](int s, int qslot, int st) {
+        if (off) return;
+        const uint32_t q = q_lo + qslot * (TILE >> 4), k = k_lo + st * (TILE >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
+            if (kk < nd) umma(tmem + s * 128, sw128(q + off), sw128(k + off), id_s, kk > 0);
+          }
+          umma_commit(&s_full[s]);
+        }
+        __syncwarp();
+      };
+      for (; pos < places; ++nf) {
+        const int fs = nf & 1;
+        off = wait(&frag_full[fs], nf >> 1);
+        if (off) break;
+        const int n = info[fs].f.n, k0 = info[fs].f.k0, len = info[fs].len;
+        const bool pair = info[fs].f.rows > SLOT;
         auto stage = [&](int place) {
           const int p = pos + place;
-          wait(&full[p % STAGES], p / STAGES);
+          if (!off) off = wait(&full[p % STAGES], p / STAGES);
+          tc_fence_after();
           return p % STAGES;
         };
         auto values = [&](int s, int j, int st, bool first) {
-          wait(&p_ready[s], nready[s]++);
-          if (*abort_flag) return;
+          if (!off) off = wait(&p_ready[s], nready[s]++);
+          if (off) return;
           tc_fence_after();
-          const int keys = min(KT, end - (f.k0 + j) * KT);
-          const uint64_t vd = sw128_desc_mn(su32(ring + st * TILE), PANEL);
-          for (int kk = 0; kk < (keys + 15) / 16; ++kk)
-            umma_ts(tmem + 256 + s * 128, tmem + s * 128 + 8 * kk, vd + kk * 128, id_o, !first || kk > 0);
+          const int keys = len - (k0 + j) * KT;
+          const uint32_t v = v_lo + st * (TILE >> 4);
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < KT / 16; ++kk)
+              if (16 * kk < keys)
+                umma_ts(tmem + 256 + s * 128, tmem + s * 128 + 8 * kk, sw128(v + kk * 128), id_o, !first || kk > 0);
+          }
+          __syncwarp();
         };
-        auto release = [&](int st) { if (!*abort_flag) umma_commit(&empty[st]); };
-        wait(&q_full, nfrag++);
         tc_fence_after();
         if (pair) {
-          int st = stage(0);
-          tc_fence_after();
-          scores(0, 0, st);
-          scores(1, 1, st);
-          release(st);
-          for (int j = 0; j < f.n; ++j) {
-            const int sv = stage(v_place(true, j, f.n));
-            int sk = 0;
-            for (int s = 0; s < 2; ++s) {
-              values(s, j, sv, j == 0);
-              if (s == 1) release(sv);
-              if (j + 1 < f.n) {
-                if (s == 0) sk = stage(k_place(true, j + 1));
-                tc_fence_after();
-                scores(s, s, sk);
-                if (s == 1) release(sk);
-              } else if (!*abort_flag) {
-                umma_commit(&o_full[s]);
-              }
+          int sk = stage(0);
+          scores(0, 0, sk);
+          scores(1, 1, sk);
+          commit(&empty[sk]);
+          if (n == 1) commit(&q_free[fs]);
+          for (int j = 0; j < n; ++j) {
+            const int sv = stage(v_place(true, j, n));
+            values(0, j, sv, j == 0);
+            if (j + 1 < n) {
+              sk = stage(k_place(true, j + 1));
+              scores(0, 0, sk);
+            } else {
+              commit(&o_full[0]);
+            }
+            values(1, j, sv, j == 0);
+            commit(&empty[sv]);
+            if (j + 1 < n) {
+              scores(1, 1, sk);
+              commit(&empty[sk]);
+              if (j + 2 == n) commit(&q_free[fs]);
+            } else {
+              commit(&o_full[1]);
             }
           }
         } else {
-          for (int j = 0; j < 2 && j < f.n; ++j) {
-            const int st = stage(k_place(false, j));
-            tc_fence_after();
-            scores(j, 0, st);
-            release(st);
+          for (int j = 0; j < 2 && j < n; ++j) {
+            const int sk = stage(k_place(false, j));
+            scores(j, fs, sk);
+            commit(&empty[sk]);
           }
-          for (int j = 0; j < f.n; ++j) {
-            const int s = j & 1, sv = stage(v_place(false, j, f.n));
+          if (n <= 2) commit(&q_free[fs]);
+          for (int j = 0; j < n; ++j) {
+            const int s = j & 1, sv = stage(v_place(false, j, n));
             values(s, j, sv, j < 2);
-            release(sv);
-            if (j + 2 < f.n) {
+            commit(&empty[sv]);
+            if (j + 2 < n) {
               const int sk = stage(k_place(false, j + 2));
-              tc_fence_after();
-              scores(s, 0, sk);
-              release(sk);
-            } else if (!*abort_flag) {
-              umma_commit(&o_full[s]);
+              scores(s, fs, sk);
+              commit(&empty[sk]);
+              if (j + 3 == n) commit(&q_free[fs]);
+            } else {
+              commit(&o_full[s]);
             }
           }
         }
-        pos += 2 * f.n;
+        pos += 2 * n;
+        if (off) break;
       }
-      umma_commit(&done);
+      if (elect_one()) umma_commit(&done);
+      __syncwarp();
       mbar_drain(&done, 0);
+    } else {
+      // plan: the fragments in turn, their rows and their queries, one fragment ahead of the products
+      const int pw = warp - 10, np = 2 * ((a.D + 15) / 16);          // 16-byte pieces that the products read
+      Walk walk(plan, cum, blockIdx.x);
+      FragInfo x;
+      bool was_pair = false;
+      while (walk.next(plan, cum, x.f)) {
+        const int fs = nf & 1;
+        const bool pair = x.f.rows > SLOT;
+        if (nf >= 2 && (wait(&frag_empty[fs], (nf >> 1) - 1) || wait(&q_free[fs], (nf >> 1) - 1))) break;
+        if (nf >= 1 && (pair || was_pair) && wait(&q_free[fs ^ 1], (nf - 1) >> 1)) break;
+        was_pair = pair;
+        x.len = x.f.prefix ? a.P : clamped_len(a, x.f.b);
+        int low = x.len;
+        for (int r0 = 32 * pw; r0 < x.f.rows; r0 += 64) {
+          const int r = r0 + lane;
+          const __nv_bfloat16* src = nullptr;
+          if (r < x.f.rows) {
+            int token, head;
+            row_of(a, x.f, r, token, head);
+            const int b = token / a.L, i = token - b * a.L, id = token * (a.Hkv * a.G) + head;
+            const int lim = row_limit(a, x.f, token, x.len);
+            const bool idle = row_idle(a, token);
+            row_id[fs][r] = idle ? ~id : id;
+            row_lim[fs][r] = lim;
+            if (!idle) low = min(low, lim);
+            src = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head;
+          }
+          // 16 lanes a row: the queries of 32 rows, two at a time
+          const int c = lane & 15;
+          uint8_t* dst = sQ + (pair ? r0 >> 7 : fs) * TILE + (c >> 3) * PANEL;
+          const int last = min(32, x.f.rows - r0);
+          for (int i = 0; i < last; i += 2) {
+            const int in = i + (lane >> 4), at = (r0 & (SLOT - 1)) + in;
+            const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(src), in);
+            if (c >= np || in >= last) continue;
+            const uint32_t to = su32(dst + at * 128 + ((c & 7) ^ (at & 7)) * 16);
+            if (8 * c < a.D)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
+            else
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+          }
+          __syncwarp();
+        }
+        low = __reduce_min_sync(FULL_MASK, low);
+        if (lane == 0) {
+          if (pw == 0) {
+            info[fs].f = x.f;
+            info[fs].len = x.len;
+          }
+          info[fs].low[pw] = low;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&frag_full[fs]);
+        ++nf;
+      }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int s = warp >> 2, r = tid & (SLOT - 1), D = a.D;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + s * 128 + lanes, tO = tmem + 256 + lanes;
-    int nS = 0, nO = 0;                            // tiles and fragments this slot had
-    while (walk.next(plan, cum, f)) {
-      const bool pair = f.rows > SLOT;
-      const int len = f.prefix ? a.P : clamped_len(a, f.b);
+    const int places = 2 * (min(plan.T, ((int)blockIdx.x + 1) * plan.share) - (int)blockIdx.x * plan.share);
+    int nS = 0, nO = 0, nsync = 0;                 // tiles and fragments this slot had; meetings of the slots
+    bool off = false;
+    auto meet = [&]() {                            // both slots' warps
       tc_fence_before();
-      soft_sync();                                 // the last fragment's Q, O and words are done with
-      // Q: 16 bytes a thread, rows beyond the fragment's and columns beyond D zero
-      constexpr int VPR = DP / 8;                  // 16-byte pieces of a row
-      for (int e = tid; e < (pair ? 2 : 1) * SLOT * VPR; e += SOFT_THREADS) {
-        const int row = e / VPR, c = e % VPR;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < f.rows && 8 * c < D) {
-          int token, head;
-          row_of(a, f, row, token, head);
-          const int b = token / a.L, i = token - b * a.L;
-          v = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.seq +
-                                              i * a.q.tok + head * a.q.head + 8 * c);
-        }
-        const int in = row & (SLOT - 1);
-        *reinterpret_cast<uint4*>(sQ + (row >> 7) * TILE + (c >> 3) * PANEL + in * 128 + ((c & 7) ^ (in & 7)) * 16) = v;
-      }
-      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&slots);
+      off = wait(&slots, nsync++);
+      tc_fence_after();
+    };
+    for (; pos < places && !off; ++nf) {
+      const int fs = nf & 1;
+      off = wait(&frag_full[fs], nf >> 1);
+      if (off) break;
+      const Frag& f = info[fs].f;
+      const int len = info[fs].len, low = min(info[fs].low[0], info[fs].low[1]), n = f.n, k0 = f.k0;
+      const bool pair = f.rows > SLOT;
       const int my = pair ? s * SLOT + r : r;      // this thread's row
       const bool mine = my < f.rows;
-      int token = 0, head = 0, lim = 0;
-      if (mine) {
-        row_of(a, f, my, token, head);
-        lim = row_limit(a, f, token, len);
-      }
-      const int warp_low = __reduce_min_sync(FULL_MASK, mine ? lim : len);
-      if (lane == 0) {
-        low_of[warp] = warp_low;
-        odd_of[warp] = 0;
-      }
-      soft_sync();
-      if (tid == 0) mbar_arrive(&q_full);
-      int low = len;                               // entries from here on are hidden from some row
-#pragma unroll
-      for (int w = 0; w < 8; ++w) low = min(low, low_of[w]);
+      const int lim = mine ? row_lim[fs][my] : 0;
       const bool warp_live = __any_sync(FULL_MASK, mine);
+      if (lane == 0) odd_of[fs][warp] = 0;
 
       float m = -INFINITY, l = 0.f;
       int tiles = 0;
-      for (int j = pair ? 0 : s; j < f.n; j += pair ? 1 : 2, ++tiles) {
-        const int t0 = (f.k0 + j) * KT, end = min(len - t0, KT);   // entries in use of the tile
-        wait(&s_full[s], nS++);
-        __syncwarp();
+      for (int j = pair ? 0 : s; j < n; j += pair ? 1 : 2, ++tiles) {
+        const int t0 = (k0 + j) * KT, end = min(len - t0, KT);     // entries in use of the tile
+        off = wait(&s_full[s], nS++);
+        if (off) break;
         tc_fence_after();
         if (warp_live) {
           float v[KT];
           tmem_ld128(tS, v);
           if (__any_sync(FULL_MASK, mine && lim - t0 < KT)) {
-            const int n = lim - t0;
+            const int seen_here = lim - t0;
 #pragma unroll
-            for (int c = 0; c < KT; ++c) v[c] = c < n ? v[c] : -INFINITY;
+            for (int c = 0; c < KT; ++c) v[c] = c < seen_here ? v[c] : -INFINITY;
           }
-          float top = v[0], top1 = v[1], top2 = v[2], top3 = v[3];
+          float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int c = 4; c < KT; c += 4) {
-            top = fmaxf(top, v[c]);
-            top1 = fmaxf(top1, v[c + 1]);
-            top2 = fmaxf(top2, v[c + 2]);
-            top3 = fmaxf(top3, v[c + 3]);
-          }
-          const float t = fmaxf(fmaxf(top, top1), fmaxf(top2, top3)) * a.sl2;
+          for (int c = 4; c + 8 <= KT; c += 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top[i] = fmaxf(fmaxf(top[i], v[c + i]), v[c + 4 + i]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], v[KT - 4 + i]);
+          const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.sl2;
           if (__any_sync(FULL_MASK, t > m + LAZY)) {
             const float mn = fmaxf(m, t), alpha = ex2(m - (mn == -INFINITY ? 0.f : mn));
             m = mn;
             l *= alpha;
             if (tiles > 0)
+#pragma unroll 1
               for (int c = 0; c < D; c += 16) {
                 float o[16];
                 tmem_ld16(tO + s * 128 + c, o);
@@ -318,103 +430,96 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
               }
           }
           const float ms = m == -INFINITY ? 0.f : m;
-          float sum0 = 0.f, sum1 = 0.f;
+          const f32x2 scale2 = pack2(a.sl2, a.sl2), minus2 = pack2(-ms, -ms);
+          f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
           for (int c0 = 0; c0 < KT; c0 += 32) {
             uint32_t p[16];
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-              const float p0 = ex2(fmaf(v[c0 + c], a.sl2, -ms)), p1 = ex2(fmaf(v[c0 + c + 1], a.sl2, -ms));
-              sum0 += p0;
-              sum1 += p1;
-              const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-              p[c / 2] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int c = 0; c < 32; c += 4) {
+              float x[4];
+              unpack2(fma2(pack2(v[c0 + c], v[c0 + c + 1]), scale2, minus2), x[0], x[1]);
+              unpack2(fma2(pack2(v[c0 + c + 2], v[c0 + c + 3]), scale2, minus2), x[2], x[3]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = ex2(x[i]);
+              sum0 = add2(sum0, pack2(x[0], x[1]));
+              sum1 = add2(sum1, pack2(x[2], x[3]));
+              const __nv_bfloat162 h0 = __floats2bfloat162_rn(x[0], x[1]), h1 = __floats2bfloat162_rn(x[2], x[3]);
+              p[c / 2] = *reinterpret_cast<const uint32_t*>(&h0);
+              p[c / 2 + 1] = *reinterpret_cast<const uint32_t*>(&h1);
             }
             tmem_st16(tS + c0 / 2, p);
           }
-          l += sum0 + sum1;
+          float x[2];
+          unpack2(add2(sum0, sum1), x[0], x[1]);
+          l += x[0] + x[1];
           tmem_st_wait();
         }
         // values that some row does not see, and those behind the last entry that the last step reads
         const int v0 = max(low - t0, 0), v1 = min((end + 15) & ~15, KT);
         if (v0 < v1) {
-          const int pl = pos + v_place(pair, j, f.n), st = pl % STAGES;
-          wait(&full[st], pl / STAGES);
-          __syncwarp();
+          const int pl = pos + v_place(pair, j, n), st = pl % STAGES;
+          off = wait(&full[st], pl / STAGES);
+          if (off) break;
           bool odd = false;
           for (int e = r; e < (v1 - v0) * VPR; e += SLOT) {
             const int row = v0 + e / VPR, c = e % VPR;
             uint4* at = reinterpret_cast<uint4*>(ring + st * TILE + (c >> 3) * PANEL + row * 128 +
                                                  ((c & 7) ^ (row & 7)) * 16);
-            uint4 x = *at;
+            const uint4 x = *at;
             if (odd_bf16x2(x.x) || odd_bf16x2(x.y) || odd_bf16x2(x.z) || odd_bf16x2(x.w)) {
               *at = make_uint4(without_odd(x.x), without_odd(x.y), without_odd(x.z), without_odd(x.w));
               odd |= row < end;
             }
           }
-          if (__any_sync(FULL_MASK, odd) && lane == 0) odd_of[warp] = 1;
-          fence_async_smem();
-          // the slot's four warps: all of them have cleaned their share
-          asm volatile("bar.sync %0, 128;" ::"r"(2 + s) : "memory");
+          if (__any_sync(FULL_MASK, odd) && lane == 0) odd_of[fs][warp] = 1;
+          fence_async_smem();                      // (the product waits for all four warps)
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_ready[s]);
       }
-      if (tiles > 0) wait(&o_full[s], nO++);
-      __syncwarp();
+      if (off || (tiles > 0 && (off = wait(&o_full[s], nO++)))) break;
       tc_fence_after();
-      float w0 = pair && s == 1 ? 0.f : 1.f, w1 = 1.f - w0;        // weights of the slots' sums
+      float w0 = 1.f, w1 = 0.f;                    // weights of this slot's sums, and of the other's
+      if (!pair) ml_of[fs][s][r] = make_float2(m, l);
+      // for the other slot's sums, or to know what its warps found among the values
+      const bool cleaned = !f.prefix && low < len;
+      if (!pair || cleaned) meet();
+      if (off) break;
       if (!pair) {
-        ml_of[s][r] = make_float2(m, l);
-        tc_fence_before();
-      }
-      soft_sync();
-      tc_fence_after();
-      if (!pair) {
-        const float2 x = ml_of[0][r], y = ml_of[1][r];
+        const float2 x = ml_of[fs][0][r], y = ml_of[fs][1][r];
         m = fmaxf(x.x, y.x);
         const float ms = m == -INFINITY ? 0.f : m;
-        w0 = ex2(x.x - ms);
-        w1 = f.n > 1 ? ex2(y.x - ms) : 0.f;
-        l = (x.x == m ? 1.f : w0) * x.y + (y.x == m ? 1.f : w1) * y.y;
+        w0 = x.x == m ? 1.f : ex2(x.x - ms);
+        w1 = y.x == m ? 1.f : ex2(y.x - ms);
+        l = w0 * x.y + w1 * y.y;
       }
       int odd = 0;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) odd |= odd_of[w];
+      if (cleaned)
+        for (int w = 0; w < 8; ++w) odd |= odd_of[fs][w];
 
-      const bool none = l == 0.f || (mine && row_idle(a, token));
-      const float inv = none ? 0.f : 1.f / l;
-      const long long at = f.slot * min(RT, f.prefix ? plan.R : plan.LG) + my;
-      const long long row = (long long)token * (a.Hkv * a.G) + head;
-      if (warp_live)
+      if (warp_live) {
+        const int id = mine ? row_id[fs][my] : -1, row = id < 0 ? ~id : id;
+        const bool whole = f.whole, none = l == 0.f || id < 0;
+        const float inv = none ? 0.f : 1.f / l;
+        const int per = min(RT, f.prefix ? plan.R : plan.LG);
+        float* part = (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, D, my, 0);
+#pragma unroll 1
         for (int c = pair ? 0 : 32 * s; c < D; c += pair ? 32 : 64) {
           float o[32];
-          if (pair) {
-            tmem_ld32(tO + s * 128 + c, o);
-          } else {
-            tmem_ld32(tO + c, o);
-            if (f.n > 1) {
-              float y[32];
-              tmem_ld32(tO + 128 + c, y);
+          tmem_ld32(tO + (pair ? s * 128 : 0) + c, o);
+          if (!pair && n > 1) {
+            float y[32];
+            tmem_ld32(tO + 128 + c, y);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = (w0 != 0.f ? w0 * o[i] : 0.f) + (w1 != 0.f ? w1 * y[i] : 0.f);
-            }
+            for (int i = 0; i < 32; ++i) o[i] = fmaf(w1, y[i], w0 * o[i]);
           }
           if (mine) {
-            if (odd && !f.prefix)
-              for (int t = max(low, f.k0 * KT); t < min(lim, (f.k0 + f.n) * KT); ++t) {
-                const __nv_bfloat16* vr = static_cast<const __nv_bfloat16*>(a.vo.p) + f.b * a.vo.seq +
-                                          t * a.vo.tok + f.h * a.vo.head + c;
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (c + i < D) {
-                    const float x = __bfloat162float(vr[i]);
-                    if (!isfinite(x)) o[i] += x;
-                  }
-              }
-            if (f.whole) {
-              __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + row * D + c;
+            if (odd)
+              add_odd(a, f.b, f.h, c, max(low, k0 * KT), min(lim, (k0 + n) * KT), o);
+            if (whole) {
+              __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + (long long)row * D + c;
 #pragma unroll
               for (int i = 0; i < 32; i += 8)
                 if (c + i < D) {
@@ -428,22 +533,22 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
                   *reinterpret_cast<uint4*>(to + i) = make_uint4(x[0], x[1], x[2], x[3]);
                 }
             } else {
-              float* to = (f.prefix ? a.part_p : a.part_o) + at * D + c;
 #pragma unroll
               for (int i = 0; i < 32; i += 4)
-                if (c + i < D) store4(to + i, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
+                if (c + i < D) store4(part + (long long)(c + i) * per, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
             }
           }
           __syncwarp();
         }
-      if (mine && (pair || s == 0)) {
-        if (f.whole) {
-          if (a.lse) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
-        } else {
-          (f.prefix ? a.ml_p : a.ml_o)[at] = make_float2(m, l);
+        if (mine && (pair || s == 0)) {
+          if (!whole) (f.prefix ? a.ml_p : a.ml_o)[(long long)f.slot * per + my] = make_float2(m, l);
+          else if (a.lse) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
         }
       }
-      pos += 2 * f.n;
+      if (!pair) meet();                           // both slots have read both sums
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&frag_empty[fs]);
+      pos += 2 * n;
     }
   }
   tc_fence_before();

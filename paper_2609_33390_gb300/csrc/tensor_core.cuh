@@ -45,6 +45,13 @@ __device__ __forceinline__ void tc_fence_before() {
 __device__ __forceinline__ void tc_fence_after() {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 }
+// True in one lane of a converged warp. (Issuing from a branch on it, and not on the lane's number, keeps
+// the operands of the instructions below in uniform registers.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 // D(tmem) (+)= A(smem desc) * B(smem desc)^T, kind::f16 (bf16 inputs), fp32 accumulator.
 __device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
                                      uint32_t accumulate) {
@@ -166,17 +173,15 @@ __device__ __forceinline__ uint64_t sw128_desc(uint32_t saddr) {
   return d;
 }
 
-// The same swizzle atoms as an MN-major operand: rows of the tile are k, the 64 columns of a panel
-// are m or n. 1024 B between 8-row groups along k, `panel` bytes between panels of 64 columns.
-__device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr, uint32_t panel) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(panel >> 4) << 16;
-  d |= static_cast<uint64_t>(1024 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
+// The same as two words, of which only the lower moves with the address: K-major, and MN-major (rows of
+// the tile are k, the 64 columns of a panel are m or n; `panel` bytes between panels of 64 columns,
+// 1024 B between 8-row groups along k).
+constexpr uint32_t SW128_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t sw128_lo(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t sw128_lo_mn(uint32_t saddr, uint32_t panel) {
+  return ((saddr & 0x3FFFFu) >> 4) | ((panel >> 4) << 16);
 }
+__device__ __forceinline__ uint64_t sw128(uint32_t lo) { return static_cast<uint64_t>(SW128_HI) << 32 | lo; }
 
 // Instruction descriptor of kind::f16: fp32 accumulator, bf16 A and B, both K-major, M x N.
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N) {
