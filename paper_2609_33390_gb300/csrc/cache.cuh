@@ -2,6 +2,8 @@
 // eviction by it: arguments, the division of attention's work over the SMs, and the join of its parts.
 #pragma once
 
+#include <cuda.h>
+
 #include "brisk_internal.cuh"
 
 namespace brisk {
@@ -50,15 +52,20 @@ struct Plan {
   int nPT, kP, nLT;                  // row tiles and key tiles of the prefix; row tiles of a sequence
   int R, UP, T, share;               // rows a key head; units of the prefix; all units; units a CTA
 
-  __device__ Plan(const AttendArgs& a, int rt, int kt, int own_tiles) {
-    B = a.B; LG = a.L * a.G; Hkv = a.Hkv; P = a.P; RT = rt; KT = kt;
+  __device__ Plan(int b, int lg, int hkv, int p, int rt, int kt, int own_tiles, int grid) {
+    B = b; LG = lg; Hkv = hkv; P = p; RT = rt; KT = kt;
     R = B * LG;
     kP = (P + KT - 1) / KT;
     nPT = P > 0 ? (R + RT - 1) / RT : 0;
     nLT = (LG + RT - 1) / RT;
     UP = Hkv * nPT * kP;
     T = UP + Hkv * nLT * own_tiles;
-    share = max(1, (int)(((unsigned)T + a.grid - 1) / a.grid));
+    share = max(1, (int)(((unsigned)T + grid - 1) / grid));
+  }
+  __device__ Plan(const AttendArgs& a, int rt, int kt, int own_tiles)
+      : Plan(a.B, a.L * a.G, a.Hkv, a.P, rt, kt, own_tiles, a.grid) {}
+  __device__ int units_of(int cta) const {
+    return (int)(min((long long)T, (cta + 1LL) * share) - min((long long)T, (long long)cta * share));
   }
   __device__ int cta_of(int u) const { return u / share; }
   __device__ int own_start(const int32_t* cum, int b, int h, int lt) const {
@@ -138,7 +145,8 @@ __device__ __forceinline__ long long part_at(long long slot, int per, int D, int
   return slot * per * D + ((long long)(c >> 2) * per + row) * 4;
 }
 
-__device__ __forceinline__ int clamped_len(const AttendArgs& a, int b) {
+template <typename Args>
+__device__ __forceinline__ int clamped_len(const Args& a, int b) {
   return min(max(a.own_len[b], 0), a.S);
 }
 // Token (b * L + i) and query head of a fragment's row, and how many keys the row sees.
@@ -157,8 +165,8 @@ __device__ __forceinline__ bool row_idle(const AttendArgs& a, int token) {
 
 // Key tiles before each sequence, by all THREADS threads of a CTA; returns their sum. *bad is set
 // where a length lies outside 0..S (the caller clears it before a barrier).
-template <int THREADS>
-__device__ int count_tiles(const AttendArgs& a, int kt, int32_t* cum, int* warp_sum, int* bad) {
+template <int THREADS, typename Args>
+__device__ int count_tiles(const Args& a, int kt, int32_t* cum, int* warp_sum, int* bad) {
   const int per = (a.B + THREADS - 1) / THREADS, tid = threadIdx.x, lane = tid & 31;
   const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
   int sum = 0;
@@ -208,6 +216,9 @@ constexpr int ATTEND_RT_F32 = 64, ATTEND_KT_F32 = 64;
 inline int attend_rt(int dt) { return dt == BRISK_DT_BF16 ? ATTEND_RT_TC : ATTEND_RT_F32; }
 inline int attend_kt(int dt) { return dt == BRISK_DT_BF16 ? ATTEND_KT_TC : ATTEND_KT_F32; }
 
+// Tensor map of a cache's tiles of 64 columns x 128 entries (cache_attend_tc.cu).
+bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int toks, int seqs);
+
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream);
@@ -222,8 +233,10 @@ struct WeightArgs {
   const float* acc_in;     // [B, Hkv, S] or nullptr (zeros)
   float* acc_out;          // [B, Hkv, S]
   int32_t* status;
+  int grid;
   long long wait_limit;
 };
+cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream);
 cudaError_t launch_weights_simt(const WeightArgs& a, cudaStream_t stream);
 
 // ---------------------------------------------------------------- eviction

@@ -137,7 +137,7 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   if (!view_ok(q, d, d->B, d->L, d->Hq, &a.q) || !view_ok(k_own, d, d->B, d->S, d->Hkv, &a.ko))
     return BRISK_ERR_INVALID_ARG;
   // one CTA a key tile: their number is a grid's first dimension
-  if ((long long)d->B * d->Hkv * ((d->S + 63) / 64) > 0x7fffffffLL) return BRISK_ERR_UNSUPPORTED;
+  if (!units_ok(d) || (long long)d->B * d->Hkv * ((d->S + 63) / 64) > 0x7fffffffLL) return BRISK_ERR_UNSUPPORTED;
   a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.S = d->S; a.dt = d->dtype;
   a.own_len = own_len;
   a.visible = visible;
@@ -150,7 +150,11 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   a.wait_limit = wait_limit_cycles();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
-  return launch_weights_simt(a, st) == cudaSuccess ? BRISK_OK : BRISK_ERR_CUDA;
+  if (d->S == 0) return BRISK_OK;
+  if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
+  a.grid = CACHE_SMS;
+  return (d->dtype == BRISK_DT_BF16 ? launch_weights_tc(a, st) : launch_weights_simt(a, st)) == cudaSuccess
+             ? BRISK_OK : BRISK_ERR_CUDA;
 }
 
 brisk_status brisk_cache_evict(const brisk_cache_dims* d, const brisk_view* k, const brisk_view* v,

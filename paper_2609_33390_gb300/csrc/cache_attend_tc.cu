@@ -41,17 +41,6 @@ struct Shape {
   static constexpr int SMEM = 1024 + (2 + STAGES) * TILE + (CACHE_MAX_B + 1) * 4;
 };
 
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y,
-                                            int z, int w) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(su32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(su32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
-      : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(su32(bar)) : "memory");
-}
 // Places of the key and value tiles of a fragment of n tiles in the ring's order, which is the order
 // in which the issuing thread takes them.
 __device__ __forceinline__ int k_place(bool pair, int j) { return pair ? 2 * j : (j == 0 ? 0 : 2 * j - 1); }
@@ -66,27 +55,6 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t x) {
   if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
   if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
   return x;
-}
-
-// Two fp32 in one 64-bit register: one instruction for both.
-using f32x2 = unsigned long long;
-__device__ __forceinline__ f32x2 pack2(float x, float y) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ void unpack2(f32x2 v, float& x, float& y) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v));
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 x, f32x2 y, f32x2 z) {
-  f32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
-  return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 x, f32x2 y) {
-  f32x2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-  return r;
 }
 
 // Adds the infinities and NaN of the own values t0 <= t < t1 to a row's 32 columns from c on.
@@ -205,7 +173,7 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
       const uint32_t id_s = idesc_bf16(SLOT, KT), id_o = idesc_bf16(SLOT, 16 * nd) | IDESC_B_MN;
       const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
       int nready[2] = {0, 0};
-      const int places = 2 * (min(plan.T, ((int)blockIdx.x + 1) * plan.share) - (int)blockIdx.x * plan.share);
+      const int places = 2 * plan.units_of(blockIdx.x);
       bool off = false;                            // a wait gave up: nothing more is issued
       auto commit = [&](uint64_t* bar) {
         if (off) return;
@@ -368,7 +336,7 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
     const int s = warp >> 2, r = tid & (SLOT - 1), D = a.D;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + s * 128 + lanes, tO = tmem + 256 + lanes;
-    const int places = 2 * (min(plan.T, ((int)blockIdx.x + 1) * plan.share) - (int)blockIdx.x * plan.share);
+    const int places = 2 * plan.units_of(blockIdx.x);
     int nS = 0, nO = 0, nsync = 0;                 // tiles and fragments this slot had; meetings of the slots
     bool off = false;
     auto meet = [&]() {                            // both slots' warps
@@ -558,6 +526,8 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
     a.errs[blockIdx.x] = aborted ? BRISK_ERR_TIMEOUT : (bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK);
 }
 
+}  // namespace
+
 // Tiles of 64 columns x 128 entries of one head and sequence, 128-byte swizzle, zeros outside.
 bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int toks, int seqs) {
   if (!v.p) {                                      // no such entries: never read
@@ -576,8 +546,6 @@ bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int 
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-}  // namespace
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   AttendMaps maps;

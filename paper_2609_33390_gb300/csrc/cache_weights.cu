@@ -5,6 +5,7 @@
 // with the rows' log-sums lse that attention left. The keys are the tile's rows here: a key's sum
 // over the query rows stays with its threads, so there are no atomics and the sums' order is fixed.
 #include "cache.cuh"
+#include "tensor_core.cuh"
 
 namespace brisk {
 namespace {
@@ -13,7 +14,6 @@ constexpr int W_THREADS = 256;
 constexpr int W_KEYS = 64, W_ROWS = 64;
 constexpr int WS = CACHE_MAX_D + 4;
 
-template <typename T>
 __global__ void __launch_bounds__(W_THREADS)
 weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   extern __shared__ __align__(16) float smem[];
@@ -30,7 +30,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   const int rows = a.L * a.G;
   if (t0 < len) {
-    const T* kb = static_cast<const T*>(a.ko.p) + b * a.ko.seq + h * a.ko.head;
+    const float* kb = static_cast<const float*>(a.ko.p) + b * a.ko.seq + h * a.ko.head;
     for (int e = tid; e < W_KEYS * nv; e += W_THREADS) {
       const int r = e / nv, c = 4 * (e - r * nv);
       store4(sK + r * WS + c, t0 + r < len ? load4(kb + (t0 + r) * a.ko.tok + c) : make_float4(0.f, 0.f, 0.f, 0.f));
@@ -41,7 +41,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
         const int r = e / nv, c = 4 * (e - r * nv), i = (r0 + r) / a.G;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (r0 + r < rows)
-          v = load4(static_cast<const T*>(a.q.p) + b * a.q.seq + i * a.q.tok +
+          v = load4(static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok +
                     (h * a.G + (r0 + r - i * a.G)) * a.q.head + c);
         store4(sQ + r * CACHE_MAX_D + c, v);
       }
@@ -106,7 +106,323 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- bf16, on the tensor cores
+// S^T = K Q^T: 128 keys are the rows of the product, up to 128 query rows its columns, so that a thread
+// holds one key's scores and adds up its weights. The CTAs share the units (sequence, head, key tile)
+// evenly. One warp streams key tiles by TMA, one issues the products into four score buffers in TMEM,
+// two put blocks of 128 queries with their log-sums into a ring, and two groups of four warps take
+// the key tiles in turn. Up to two blocks of queries stay for all key tiles of a head; more are read again
+// for every tile. Bound by the keys' bytes up to about 256 query rows a head.
+constexpr int KT = 128, QB = 128, Q_STAGES = 3;
+constexpr int WT_THREADS = 384;
+constexpr int PANEL = KT * 128;
+
+template <int DP>
+struct WShape {
+  static constexpr int TILE = KT * DP * 2;
+  static constexpr int STAGES = DP == 128 ? 3 : 6;
+  static constexpr int SMEM = 1024 + (Q_STAGES + STAGES) * TILE + (CACHE_MAX_B + 1) * 4;
+};
+
+struct WInfo {
+  int b, h, k0, n, len, low, last;       // low: entries from here on are hidden from some row; last: the
+};                                       // sequence's last tile is among these
+
+template <int DP>
+__global__ void __launch_bounds__(WT_THREADS, 1)
+weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ WeightArgs a) {
+  using Sh = WShape<DP>;
+  constexpr int STAGES = Sh::STAGES, TILE = Sh::TILE;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = base;
+  uint8_t* ring = base + Q_STAGES * TILE;
+  int32_t* cum = reinterpret_cast<int32_t*>(ring + STAGES * TILE);
+  __shared__ __align__(16) float neg_lse[Q_STAGES][QB];    // -lse, log2 units
+  __shared__ __align__(16) int row_lim[Q_STAGES][QB];
+  __shared__ uint64_t k_full[STAGES], k_empty[STAGES], q_full[Q_STAGES], q_empty[Q_STAGES];
+  __shared__ uint64_t s_full[4], s_empty[4], f_full[2], f_empty[2], done;
+  __shared__ WInfo info[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int aborted, bad, warp_sum[WT_THREADS / 32];
+  volatile int* abort_flag = &aborted;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&k_full[s], 1);
+      mbar_init(&k_empty[s], 1);
+    }
+    for (int s = 0; s < Q_STAGES; ++s) {
+      mbar_init(&q_full[s], 2);                    // the planning warps
+      mbar_init(&q_empty[s], 9);                   // the eight summing warps and the products
+    }
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&s_full[s], 1);
+      mbar_init(&s_empty[s], 4);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&f_full[s], 2);
+      mbar_init(&f_empty[s], 9);                   // the summing warps and the issuing one
+    }
+    mbar_init(&done, 1);
+    aborted = 0;
+    bad = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == 0) tmem_alloc(&tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  const int own = count_tiles<WT_THREADS>(a, KT, cum, warp_sum, &bad);
+  const int rows = a.L * a.G, nb = (rows + QB - 1) / QB;
+  const Plan plan(a.B, rows, a.Hkv, 0, rows, KT, own, a.grid);
+  const int units = plan.units_of(blockIdx.x);
+  // sequences without entries have no units: zeros everywhere
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+    if (cum[b + 1] == cum[b])
+      for (long long t = tid; t < (long long)a.Hkv * a.S; t += WT_THREADS) a.acc_out[(long long)b * a.Hkv * a.S + t] = 0.f;
+
+  // (see attend_tc_kernel)
+  auto wait = [&](uint64_t* bar, int phase) {
+    if (!*abort_flag && !mbar_wait(bar, phase & 1, abort_flag, a.wait_limit)) *abort_flag = 1;
+    return __any_sync(FULL_MASK, *abort_flag != 0) != 0;
+  };
+  int unit = 0, nf = 0, nq = 0;                    // units, fragments and blocks of queries before
+  bool off = false;
+
+  if (warp == 8) {
+    Walk walk(plan, cum, blockIdx.x);
+    Frag f;
+    while (!off && walk.next(plan, cum, f))
+      for (int j = 0; j < f.n; ++j, ++unit) {
+        const int st = unit % STAGES;
+        off = unit >= STAGES && wait(&k_empty[st], unit / STAGES - 1);
+        if (off) break;
+        if (elect_one()) {
+          mbar_expect_tx(&k_full[st], TILE);
+#pragma unroll
+          for (int c = 0; c < DP / 64; ++c)
+            tma_load_4d(ring + st * TILE + c * PANEL, &map, &k_full[st], c * 64, f.h, (f.k0 + j) * KT, f.b);
+        }
+        __syncwarp();
+      }
+    if (off)
+      for (int p = unit > STAGES ? unit - STAGES : 0; p < unit; ++p) mbar_drain(&k_full[p % STAGES], (p / STAGES) & 1);
+  } else if (warp == 9) {
+    const int nd = (a.D + 15) / 16;
+    const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring));
+    int ns[2] = {0, 0};                            // score buffers a group was given
+    auto commit = [&](uint64_t* bar) {
+      if (elect_one()) umma_commit(bar);
+      __syncwarp();
+    };
+    while (unit < units && !off) {
+      const int fs = nf & 1;
+      off = wait(&f_full[fs], nf >> 1);
+      if (off) break;
+      const int n = info[fs].n;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&f_empty[fs]);
+      ++nf;
+      for (int j = 0; j < n && !off; ++j, ++unit) {
+        const int g = unit & 1, st = unit % STAGES;
+        off = wait(&k_full[st], unit / STAGES);
+        for (int blk = 0; blk < nb && !off; ++blk) {
+          const int qi = nq + (nb > 2 ? j * nb : 0) + blk, qs = qi % Q_STAGES;
+          const int buf = 2 * g + (ns[g] & 1);
+          off = wait(&q_full[qs], qi / Q_STAGES) || (ns[g] >= 2 && wait(&s_empty[buf], (ns[g] >> 1) - 1));
+          if (off) break;
+          ++ns[g];
+          tc_fence_after();
+          const int cols = (min(QB, rows - blk * QB) + 15) & ~15;
+          const uint32_t id = idesc_bf16(KT, cols), q = q_lo + qs * (TILE >> 4), k = k_lo + st * (TILE >> 4);
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < DP / 16; ++kk) {
+              const uint32_t o = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
+              if (kk < nd) umma(tmem + buf * 128, sw128(k + o), sw128(q + o), id, kk > 0);
+            }
+            umma_commit(&s_full[buf]);
+          }
+          __syncwarp();
+          if (nb > 2) commit(&q_empty[qs]);
+        }
+        if (!off) commit(&k_empty[st]);
+      }
+      if (nb <= 2 && !off)
+        for (int blk = 0; blk < nb; ++blk) commit(&q_empty[(nq + blk) % Q_STAGES]);
+      nq += nb > 2 ? n * nb : nb;
+    }
+    commit(&done);
+    mbar_drain(&done, 0);
+  } else if (warp >= 10) {
+    const int pw = warp - 10, np = 2 * ((a.D + 15) / 16);
+    Walk walk(plan, cum, blockIdx.x);
+    Frag f;
+    while (!off && walk.next(plan, cum, f)) {
+      const int fs = nf & 1, len = clamped_len(a, f.b), loads = nb > 2 ? f.n * nb : nb;
+      if (nf >= 2 && (off = wait(&f_empty[fs], (nf >> 1) - 1))) break;
+      // what no row of the head is kept from: needed before the first block is there
+      int low = len;
+      for (int r = lane; r < rows; r += 32) {
+        const int i = r / a.G, g = r - i * a.G;
+        const long long token = (long long)f.b * a.L + i;
+        if (a.visible) low = min(low, max(0, a.visible[token]));
+        if (a.lse[token * (a.Hkv * a.G) + f.h * a.G + g] == -INFINITY) low = 0;
+      }
+      low = __reduce_min_sync(FULL_MASK, low);
+      if (pw == 0 && lane == 0) info[fs] = WInfo{f.b, f.h, f.k0, f.n, len, low, f.k0 + f.n == cum[f.b + 1] - cum[f.b]};
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&f_full[fs]);
+      ++nf;
+      for (int x = 0; x < loads; ++x, ++nq) {
+        const int qs = nq % Q_STAGES, first = (x % nb) * QB, count = min(QB, rows - first), padded = (count + 15) & ~15;
+        if (nq >= Q_STAGES && (off = wait(&q_empty[qs], nq / Q_STAGES - 1))) break;
+        for (int r0 = 32 * pw; r0 < padded; r0 += 64) {
+          const int r = r0 + lane;
+          const __nv_bfloat16* src = nullptr;
+          if (r < padded) {
+            float ls = 0.f;
+            int lim = 0;
+            if (r < count) {
+              const int i = (first + r) / a.G, head = f.h * a.G + (first + r - i * a.G);
+              const long long token = (long long)f.b * a.L + i;
+              ls = a.lse[token * (a.Hkv * a.G) + head] * LOG2E;
+              lim = a.visible ? min(len, a.visible[token]) : len;
+              if (ls == -INFINITY) ls = 0.f, lim = 0;        // a row that saw nothing
+              src = static_cast<const __nv_bfloat16*>(a.q.p) + f.b * a.q.seq + i * a.q.tok + head * a.q.head;
+            }
+            neg_lse[qs][r] = -ls;
+            row_lim[qs][r] = lim;
+          }
+          const int c = lane & 15, last = min(32, padded - r0);
+          uint8_t* dst = sQ + qs * TILE + (c >> 3) * PANEL;
+          for (int i = 0; i < last; i += 2) {
+            const int in = i + (lane >> 4), at = r0 + in;
+            const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(src), in);
+            if (c >= np || in >= last) continue;
+            const uint32_t to = su32(dst + at * 128 + ((c & 7) ^ (at & 7)) * 16);
+            if (8 * c < a.D && from)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
+            else
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+          }
+          __syncwarp();
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[qs]);
+      }
+    }
+  } else {
+    const int g = warp >> 2;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const f32x2 scale2 = pack2(a.sl2, a.sl2);
+    int ns = 0;
+    while (unit < units && !off) {
+      const int fs = nf & 1;
+      off = wait(&f_full[fs], nf >> 1);
+      if (off) break;
+      const WInfo x = info[fs];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&f_empty[fs]);
+      ++nf;
+      float* out = a.acc_out + ((long long)x.b * a.Hkv + x.h) * a.S;
+      const float* in = a.acc_in ? a.acc_in + ((long long)x.b * a.Hkv + x.h) * a.S : nullptr;
+      for (int j = 0; j < x.n && !off; ++j, ++unit) {
+        const bool mine = (unit & 1) == g;
+        const int t = (x.k0 + j) * KT + (warp & 3) * 32 + lane, t1 = (x.k0 + j + 1) * KT;
+        float old = 0.f;
+        if (mine && in && t < x.len) old = in[t];
+        f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+        for (int blk = 0; blk < nb && (mine || nb > 2); ++blk) {
+          const int qi = nq + (nb > 2 ? j * nb : 0) + blk, qs = qi % Q_STAGES;
+          off = wait(&q_full[qs], qi / Q_STAGES);
+          if (off) break;
+          if (mine) {
+            const int buf = 2 * g + (ns & 1), count = min(QB, rows - blk * QB);
+            off = wait(&s_full[buf], ns >> 1);
+            if (off) break;
+            ++ns;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < count; c += 32) {
+              float v[32];
+              tmem_ld32(tmem + buf * 128 + lanes + c, v);
+              if (x.low < t1 || c + 32 > count) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                  const float4 ls = *reinterpret_cast<const float4*>(&neg_lse[qs][c + i]);
+                  const int4 lim = *reinterpret_cast<const int4*>(&row_lim[qs][c + i]);
+                  const float w0 = ex2(fmaf(v[i], a.sl2, ls.x)), w1 = ex2(fmaf(v[i + 1], a.sl2, ls.y));
+                  const float w2 = ex2(fmaf(v[i + 2], a.sl2, ls.z)), w3 = ex2(fmaf(v[i + 3], a.sl2, ls.w));
+                  const int left = count - c - i;
+                  sum0 = add2(sum0, pack2(t < lim.x && left > 0 ? w0 : 0.f, t < lim.y && left > 1 ? w1 : 0.f));
+                  sum1 = add2(sum1, pack2(t < lim.z && left > 2 ? w2 : 0.f, t < lim.w && left > 3 ? w3 : 0.f));
+                }
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                  const float4 ls = *reinterpret_cast<const float4*>(&neg_lse[qs][c + i]);
+                  float y[4];
+                  unpack2(fma2(pack2(v[i], v[i + 1]), scale2, pack2(ls.x, ls.y)), y[0], y[1]);
+                  unpack2(fma2(pack2(v[i + 2], v[i + 3]), scale2, pack2(ls.z, ls.w)), y[2], y[3]);
+                  sum0 = add2(sum0, pack2(ex2(y[0]), ex2(y[1])));
+                  sum1 = add2(sum1, pack2(ex2(y[2]), ex2(y[3])));
+                }
+              }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s_empty[buf]);
+          }
+          if (nb > 2) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_empty[qs]);
+          }
+        }
+        if (mine && !off && t < a.S) {
+          float y[2];
+          unpack2(add2(sum0, sum1), y[0], y[1]);
+          out[t] = t < x.len ? fmaf(a.decay, old, y[0] + y[1]) : 0.f;
+        }
+      }
+      if (nb <= 2)
+        for (int blk = 0; blk < nb && !off; ++blk) {
+          const int qi = nq + blk, qs = qi % Q_STAGES;
+          off = wait(&q_full[qs], qi / Q_STAGES);
+          if (!off && lane == 0) mbar_arrive(&q_empty[qs]);
+        }
+      nq += nb > 2 ? x.n * nb : nb;
+      if (x.last && g == 0)                        // the places behind the last tile
+        for (int t = (x.k0 + x.n) * KT + tid; t < a.S; t += 128) out[t] = 0.f;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, 512);
+  if (tid == 0 && aborted) set_status(a.status, BRISK_ERR_TIMEOUT);
+  if (tid == 0 && blockIdx.x == 0 && bad) set_status(a.status, BRISK_ERR_INVALID_ARG);
+}
+
 }  // namespace
+
+cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream) {
+  CUtensorMap map;
+  if (!make_cache_map(&map, a.ko, a.D, a.Hkv, a.S, a.B)) return cudaErrorInvalidValue;
+  auto run = [&](auto kernel, size_t smem) {
+    cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<a.grid, WT_THREADS, smem, stream>>>(map, a);
+    return cudaGetLastError();
+  };
+  return a.D > 64 ? run(weights_tc_kernel<128>, WShape<128>::SMEM) : run(weights_tc_kernel<64>, WShape<64>::SMEM);
+}
 
 cudaError_t launch_weights_simt(const WeightArgs& a, cudaStream_t stream) {
   const size_t smem = sizeof(float) * (W_KEYS * WS + W_ROWS * CACHE_MAX_D + 2 * W_ROWS);
@@ -117,8 +433,7 @@ cudaError_t launch_weights_simt(const WeightArgs& a, cudaStream_t stream) {
     kernel<<<(unsigned)grid, W_THREADS, smem, stream>>>(a);
     return cudaGetLastError();
   };
-  if (grid == 0) return cudaSuccess;
-  return a.dt == BRISK_DT_BF16 ? run(weights_simt_kernel<__nv_bfloat16>) : run(weights_simt_kernel<float>);
+  return run(weights_simt_kernel);
 }
 
 }  // namespace brisk
