@@ -27,7 +27,7 @@ namespace {
 
 constexpr int KT = ATTEND_KT_TC, RT = ATTEND_RT_TC, SLOT = 128;
 constexpr int SOFT_THREADS = 2 * SLOT;
-constexpr int ATT_THREADS = SOFT_THREADS + 128;    // and a copying, an issuing and two planning warps
+constexpr int ATT_THREADS = SOFT_THREADS + 128;    // and a copying, an issuing two issuing and a planning warp
 constexpr float LAZY = 8.f;                        // log2 of what a score may exceed the held maximum by
 constexpr uint32_t TMEM_COLS = 512;                // S0 | S1 | O0 | O1, 128 columns each
 constexpr int PANEL = KT * 128;                    // bytes of 64 columns of a tile
@@ -57,14 +57,20 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t x) {
   return x;
 }
 
-// Adds the infinities and NaN of the own values t0 <= t < t1 to a row's 32 columns from c on.
-__device__ __noinline__ void add_odd(const AttendArgs& a, int b, int h, int c, int t0, int t1, float (&o)[32]) {
-  for (int t = t0; t < t1; ++t) {
-    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.vo.p) + b * a.vo.seq + t * a.vo.tok + h * a.vo.head + c;
-    for (int i = 0; i < 32 && c + i < a.D; ++i) {
-      const float x = __bfloat162float(v[i]);
-      if (!isfinite(x)) o[i] += x;
+// Adds the infinities and NaN of the own values t0 <= t < t1 to the columns of a row that its thread has
+// stored: to a part's (by groups of four, `per` apart) or to the result's. Out of the way: it is seldom run.
+__device__ __noinline__ void add_odd(const AttendArgs& a, int b, int h, int t0, int t1, int c, int c1, float* part,
+                                     int per, __nv_bfloat16* out) {
+  for (; c < c1; ++c) {
+    float sum = 0.f;
+    for (int t = t0; t < t1; ++t) {
+      const float x = __bfloat162float(*(static_cast<const __nv_bfloat16*>(a.vo.p) + b * a.vo.seq + t * a.vo.tok +
+                                         h * a.vo.head + c));
+      if (!isfinite(x)) sum += x;
     }
+    if (sum == 0.f) continue;
+    if (part) part[(long long)(c & ~3) * per + (c & 3)] += sum;
+    else out[c] = __float2bfloat16_rn(__bfloat162float(out[c]) + sum);
   }
 }
 
@@ -72,7 +78,7 @@ __device__ __noinline__ void add_odd(const AttendArgs& a, int b, int h, int c, i
 struct FragInfo {
   Frag f;
   int len;                                         // entries of the prefix, or in use of the own cache
-  int low[2];                                      // entries from here on are hidden from some row
+  int low;                                         // entries from here on are hidden from some row
 };
 
 template <int DP>
@@ -85,8 +91,8 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
   uint8_t* sQ = base;                              // [2][DP / 64][128 rows][128 B], swizzled
   uint8_t* ring = base + 2 * TILE;
   int32_t* cum = reinterpret_cast<int32_t*>(ring + STAGES * TILE);
-  __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2], o_full[2];
-  __shared__ uint64_t frag_full[2], frag_empty[2], q_free[2], slots, done;
+  __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2][2], o_full[2];
+  __shared__ uint64_t frag_full[2], frag_empty[2], q_free[2], turn[2], slots, done;
   __shared__ FragInfo info[2];
   __shared__ int row_id[2][RT], row_lim[2][RT];    // token * Hq + head (its complement: padding), keys seen
   __shared__ uint32_t tmem_slot;
@@ -98,18 +104,20 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+      mbar_init(&empty[s], 2);                     // both slots' products
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&s_full[s], 1);
-      mbar_init(&p_ready[s], 4);                   // a lane of each of the slot's warps
+      mbar_init(&p_ready[s][0], 4);                // a lane of each of the slot's warps, for either half
+      mbar_init(&p_ready[s][1], 4);
       mbar_init(&o_full[s], 1);
-      mbar_init(&frag_full[s], 2);                 // the planning warps
+      mbar_init(&frag_full[s], 1);
       mbar_init(&frag_empty[s], 8);                // the slots' warps
-      mbar_init(&q_free[s], 1);
+      mbar_init(&q_free[s], 2);
+      mbar_init(&turn[s], 1);
     }
     mbar_init(&slots, 8);
-    mbar_init(&done, 1);
+    mbar_init(&done, 2);
     aborted = 0;
     bad = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -126,12 +134,8 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
   if (blockIdx.x == 0)
     for (int b = tid; b <= a.B; b += ATT_THREADS) a.cum[b] = cum[b];
 
-  // Waits for a phase; true if this or another wait gave up, the same answer for the whole warp: each
-  // warp then leaves its loop for the barrier at the end.
-  auto wait = [&](uint64_t* bar, int phase) {
-    if (!*abort_flag && !mbar_wait(bar, phase & 1, abort_flag, a.wait_limit)) *abort_flag = 1;
-    return __any_sync(FULL_MASK, *abort_flag != 0) != 0;
-  };
+  // (a warp that is told that a wait gave up leaves its loop for the barrier at the end)
+  auto wait = [&](uint64_t* bar, int phase) { return warp_wait(bar, phase, abort_flag, a.wait_limit); };
   int pos = 0;                                     // ring places of the fragments before this one
   int nf = 0;                                      // fragments before this one: it uses the words nf & 1
 
@@ -150,7 +154,8 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
         int nk = 0, nv = 0;
         for (int i = 0; i < 2 * f.n; ++i) {
           const bool key = nk < f.n && k_place(pair, nk) == i;
-          const int t0 = (f.k0 + (key ? nk++ : nv++)) * KT, p = pos + i, st = p % STAGES;
+          const int t0 = (f.k0 + (key ? nk++ : nv++)) * KT;
+          const unsigned p = pos + i, st = p % STAGES;
           off = p >= STAGES && wait(&empty[st], p / STAGES - 1);
           if (off) break;
           if (elect_one()) {
@@ -160,170 +165,162 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
               tma_load_4d(ring + st * TILE + c * PANEL, key ? mk : mv, &full[st], c * 64, f.h, t0, f.b);
           }
           __syncwarp();
-          issued = p + 1;
+          issued = (int)p + 1;
         }
         pos += 2 * f.n;
       }
       if (off)
         for (int p = issued > STAGES ? issued - STAGES : 0; p < issued; ++p)
           mbar_drain(&full[p % STAGES], (p / STAGES) & 1);
-    } else if (warp == 9) {
-      // products, issued by one lane; the warp stays together around it
+    } else if (warp != 10) {
+      // products of a slot, issued by one lane; the warp stays together around it. A warp a slot: one's
+      // waits do not keep the tensor cores from the other's products. Both go through every place of the
+      // ring in order, also through those that only the other one reads, and both hand it back: a barrier's
+      // phase is known by its parity alone, so that none may be left out.
+      const int s = warp == 9 ? 0 : 1;
       const int nd = (a.D + 15) / 16;              // 16 columns a step of Q K^T, and a unit of O's width
       const uint32_t id_s = idesc_bf16(SLOT, KT), id_o = idesc_bf16(SLOT, 16 * nd) | IDESC_B_MN;
       const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
-      int nready[2] = {0, 0};
-      const int places = 2 * plan.units_of(blockIdx.x);
+      const uint32_t tS = tmem + s * 128, tO = tmem + 256 + s * 128;
+      unsigned cur = 0;                            // ring places taken
+      int nready = 0, nturn = 0;
+      const unsigned places = 2 * plan.units_of(blockIdx.x);
       bool off = false;                            // a wait gave up: nothing more is issued
-      auto commit = [&](uint64_t* bar) {
-        if (off) return;
-        if (elect_one()) umma_commit(bar);
-        __syncwarp();
-      };
-      auto scores = [&](int s, int qslot, int st) {
-        if (off) return;
-        const uint32_t q = q_lo + qslot * (TILE >> 4), k = k_lo + st * (TILE >> 4);
-        if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < DP / 16; ++kk) {
-            const uint32_t off = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
-            if (kk < nd) umma(tmem + s * 128, sw128(q + off), sw128(k + off), id_s, kk > 0);
-          }
-          umma_commit(&s_full[s]);
-        }
-        __syncwarp();
-      };
-      for (; pos < places; ++nf) {
+      for (; cur < places && !off; ++nf) {
         const int fs = nf & 1;
         off = wait(&frag_full[fs], nf >> 1);
         if (off) break;
+        tc_fence_after();
         const int n = info[fs].f.n, k0 = info[fs].f.k0, len = info[fs].len;
         const bool pair = info[fs].f.rows > SLOT;
-        auto stage = [&](int place) {
-          const int p = pos + place;
-          if (!off) off = wait(&full[p % STAGES], p / STAGES);
-          tc_fence_after();
-          return p % STAGES;
-        };
-        auto values = [&](int s, int j, int st, bool first) {
-          if (!off) off = wait(&p_ready[s], nready[s]++);
-          if (off) return;
-          tc_fence_after();
-          const int keys = len - (k0 + j) * KT;
-          const uint32_t v = v_lo + st * (TILE >> 4);
-          if (elect_one()) {
+        const int step = pair ? 1 : 2;
+        const uint32_t q = q_lo + (pair ? s : fs) * (TILE >> 4);
+        int left = pair ? n : (n + 1 - s) / 2;     // tiles of the slot whose scores are still to come
+        if (left == 0 && elect_one()) umma_commit(&q_free[fs]);
+        __syncwarp();
+        bool begun = false;
+        for (int j = -step; j < n; ++j) {          // values of tile j, scores of tile j + step
+          const bool any = j >= 0, more = j + step < n;
+          unsigned sv = 0, sk = 0;
+          if (any) {
+            sv = cur % STAGES;
+            off = wait(&full[sv], cur / STAGES);
+            ++cur;
+          }
+          if (more && !off) {
+            sk = cur % STAGES;
+            off = wait(&full[sk], cur / STAGES);
+            ++cur;
+          }
+          if (off) break;
+          if (!pair && (j & 1) != s) {
+            if (lane == 0) {
+              if (any) mbar_arrive(&empty[sv]);
+              if (more) mbar_arrive(&empty[sk]);
+            }
+            __syncwarp();
+            continue;
+          }
+          const uint32_t v = v_lo + sv * (TILE >> 4), k = k_lo + sk * (TILE >> 4);
+          const int steps = (len - (k0 + j) * KT + 15) / 16;   // of 16 keys: entries in use
+          if (any) {
+            off = wait(&p_ready[s][0], nready);
+            // a pair's products go slot by slot: taken together, both slots would get their scores, and
+            // take their exponentials, at the same time, and then wait at the same time
+            if (pair && !off && (s == 1 || nturn > 0)) off = wait(&turn[s], nturn - 1 + s);
+            if (off) break;
+            tc_fence_after();
+            if (elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < KT / 16; ++kk)
-              if (16 * kk < keys)
-                umma_ts(tmem + 256 + s * 128, tmem + s * 128 + 8 * kk, sw128(v + kk * 128), id_o, !first || kk > 0);
+              for (int kk = 0; kk < KT / 32; ++kk)
+                if (kk < steps) umma_ts(tO, tS + 8 * kk, sw128(v + kk * 128), id_o, begun || kk > 0);
+            }
+            __syncwarp();
+            off = wait(&p_ready[s][1], nready++);
+            if (off) break;
+            begun = true;
+          }
+          tc_fence_after();
+          --left;
+          if (elect_one()) {
+            if (any) {
+#pragma unroll
+              for (int kk = KT / 32; kk < KT / 16; ++kk)
+                if (kk < steps) umma_ts(tO, tS + 8 * kk, sw128(v + kk * 128), id_o, 1);
+              umma_commit(&empty[sv]);
+              if (!more) umma_commit(&o_full[s]);
+            }
+            if (more) {
+#pragma unroll
+              for (int kk = 0; kk < DP / 16; ++kk) {
+                const uint32_t o = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
+                if (kk < nd) umma(tS, sw128(q + o), sw128(k + o), id_s, kk > 0);
+              }
+              umma_commit(&s_full[s]);
+              umma_commit(&empty[sk]);
+              if (left == 0) umma_commit(&q_free[fs]);
+            }
+            if (pair && any) mbar_arrive(&turn[s ^ 1]);
           }
           __syncwarp();
-        };
-        tc_fence_after();
-        if (pair) {
-          int sk = stage(0);
-          scores(0, 0, sk);
-          scores(1, 1, sk);
-          commit(&empty[sk]);
-          if (n == 1) commit(&q_free[fs]);
-          for (int j = 0; j < n; ++j) {
-            const int sv = stage(v_place(true, j, n));
-            values(0, j, sv, j == 0);
-            if (j + 1 < n) {
-              sk = stage(k_place(true, j + 1));
-              scores(0, 0, sk);
-            } else {
-              commit(&o_full[0]);
-            }
-            values(1, j, sv, j == 0);
-            commit(&empty[sv]);
-            if (j + 1 < n) {
-              scores(1, 1, sk);
-              commit(&empty[sk]);
-              if (j + 2 == n) commit(&q_free[fs]);
-            } else {
-              commit(&o_full[1]);
-            }
-          }
-        } else {
-          for (int j = 0; j < 2 && j < n; ++j) {
-            const int sk = stage(k_place(false, j));
-            scores(j, fs, sk);
-            commit(&empty[sk]);
-          }
-          if (n <= 2) commit(&q_free[fs]);
-          for (int j = 0; j < n; ++j) {
-            const int s = j & 1, sv = stage(v_place(false, j, n));
-            values(s, j, sv, j < 2);
-            commit(&empty[sv]);
-            if (j + 2 < n) {
-              const int sk = stage(k_place(false, j + 2));
-              scores(s, fs, sk);
-              commit(&empty[sk]);
-              if (j + 3 == n) commit(&q_free[fs]);
-            } else {
-              commit(&o_full[s]);
-            }
-          }
+          if (any) ++nturn;
         }
-        pos += 2 * n;
-        if (off) break;
       }
       if (elect_one()) umma_commit(&done);
-      __syncwarp();
       mbar_drain(&done, 0);
     } else {
       // plan: the fragments in turn, their rows and their queries, one fragment ahead of the products
-      const int pw = warp - 10, np = 2 * ((a.D + 15) / 16);          // 16-byte pieces that the products read
+      const int np = 2 * ((a.D + 15) / 16);        // 16-byte pieces that the products read
       Walk walk(plan, cum, blockIdx.x);
       FragInfo x;
       bool was_pair = false;
       while (walk.next(plan, cum, x.f)) {
         const int fs = nf & 1;
         const bool pair = x.f.rows > SLOT;
+        x.len = x.f.prefix ? a.P : clamped_len(a, x.f.b);
         if (nf >= 2 && (wait(&frag_empty[fs], (nf >> 1) - 1) || wait(&q_free[fs], (nf >> 1) - 1))) break;
         if (nf >= 1 && (pair || was_pair) && wait(&q_free[fs ^ 1], (nf - 1) >> 1)) break;
         was_pair = pair;
-        x.len = x.f.prefix ? a.P : clamped_len(a, x.f.b);
-        int low = x.len;
-        for (int r0 = 32 * pw; r0 < x.f.rows; r0 += 64) {
+        x.low = x.len;
+        for (int r0 = 0; r0 < x.f.rows; r0 += 32) {
           const int r = r0 + lane;
           const __nv_bfloat16* src = nullptr;
+          int token = 0, id = 0;
           if (r < x.f.rows) {
-            int token, head;
+            int head;
             row_of(a, x.f, r, token, head);
-            const int b = token / a.L, i = token - b * a.L, id = token * (a.Hkv * a.G) + head;
+            const int b = token / a.L, i = token - b * a.L;
+            id = token * (a.Hkv * a.G) + head;
+            src = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head;
+          }
+          // 4 lanes a row, 64 bytes of it at a time: the queries of 32 rows, eight at a time
+          const int last = min(32, x.f.rows - r0), q4 = lane & 3;
+#pragma unroll 1
+          for (int i = 0; i < last; i += 8) {
+            const int in = i + (lane >> 2), at = (r0 & (SLOT - 1)) + in;
+            const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(src), in);
+            const uint32_t to = su32(sQ + (pair ? r0 >> 7 : fs) * TILE + at * 128);
+            if (in < last)
+#pragma unroll
+              for (int k = 0; k < VPR / 4; ++k) {
+                const int c = 4 * k + q4;
+                const uint32_t dst = to + (c >> 3) * PANEL + ((c ^ at) & 7) * 16;
+                if (8 * c < a.D)
+                  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from + 16 * c) : "memory");
+                else if (c < np)
+                  asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
+              }
+          }
+          if (r < x.f.rows) {
             const int lim = row_limit(a, x.f, token, x.len);
             const bool idle = row_idle(a, token);
             row_id[fs][r] = idle ? ~id : id;
             row_lim[fs][r] = lim;
-            if (!idle) low = min(low, lim);
-            src = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head;
+            if (!idle) x.low = min(x.low, lim);
           }
-          // 16 lanes a row: the queries of 32 rows, two at a time
-          const int c = lane & 15;
-          uint8_t* dst = sQ + (pair ? r0 >> 7 : fs) * TILE + (c >> 3) * PANEL;
-          const int last = min(32, x.f.rows - r0);
-          for (int i = 0; i < last; i += 2) {
-            const int in = i + (lane >> 4), at = (r0 & (SLOT - 1)) + in;
-            const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(src), in);
-            if (c >= np || in >= last) continue;
-            const uint32_t to = su32(dst + at * 128 + ((c & 7) ^ (at & 7)) * 16);
-            if (8 * c < a.D)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
-            else
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
-          }
-          __syncwarp();
         }
-        low = __reduce_min_sync(FULL_MASK, low);
-        if (lane == 0) {
-          if (pw == 0) {
-            info[fs].f = x.f;
-            info[fs].len = x.len;
-          }
-          info[fs].low[pw] = low;
-        }
+        x.low = __reduce_min_sync(FULL_MASK, x.low);
+        if (lane == 0) info[fs] = x;
         asm volatile("cp.async.wait_all;" ::: "memory");
         fence_async_smem();
         __syncwarp();
@@ -351,7 +348,7 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
       off = wait(&frag_full[fs], nf >> 1);
       if (off) break;
       const Frag& f = info[fs].f;
-      const int len = info[fs].len, low = min(info[fs].low[0], info[fs].low[1]), n = f.n, k0 = f.k0;
+      const int len = info[fs].len, low = info[fs].low, n = f.n, k0 = f.k0;
       const bool pair = f.rows > SLOT;
       const int my = pair ? s * SLOT + r : r;      // this thread's row
       const bool mine = my < f.rows;
@@ -366,6 +363,32 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
         off = wait(&s_full[s], nS++);
         if (off) break;
         tc_fence_after();
+        // values that some row does not see, and those behind the last entry that the last step reads
+        const int v0 = max(low - t0, 0), v1 = min((end + 15) & ~15, KT);
+        if (v0 < v1) {
+          const int pl = pos + v_place(pair, j, n), st = pl % STAGES;
+          off = wait(&full[st], pl / STAGES);
+          if (off) break;
+          bool odd = false;
+#pragma unroll 1
+          for (int e = r; e < (v1 - v0) * VPR; e += SLOT) {
+            const int row = v0 + e / VPR, c = e % VPR;
+            uint4* at = reinterpret_cast<uint4*>(ring + st * TILE + (c >> 3) * PANEL + row * 128 +
+                                                 ((c & 7) ^ (row & 7)) * 16);
+            const uint4 x = *at;
+            if (odd_bf16x2(x.x) || odd_bf16x2(x.y) || odd_bf16x2(x.z) || odd_bf16x2(x.w)) {
+              *at = make_uint4(without_odd(x.x), without_odd(x.y), without_odd(x.z), without_odd(x.w));
+              odd |= row < end;
+            }
+          }
+          if (__any_sync(FULL_MASK, odd) && lane == 0) odd_of[fs][warp] = 1;
+          fence_async_smem();                      // (the product waits for all four warps)
+        }
+        auto ready = [&](int half) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_ready[s][half]);
+        };
         if (warp_live) {
           float v[KT];
           tmem_ld128(tS, v);
@@ -417,35 +440,19 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
               p[c / 2 + 1] = *reinterpret_cast<const uint32_t*>(&h1);
             }
             tmem_st16(tS + c0 / 2, p);
+            if (c0 == 32) {                        // half of the keys: their product may begin
+              tmem_st_wait();
+              ready(0);
+            }
           }
           float x[2];
           unpack2(add2(sum0, sum1), x[0], x[1]);
           l += x[0] + x[1];
           tmem_st_wait();
+        } else {
+          ready(0);
         }
-        // values that some row does not see, and those behind the last entry that the last step reads
-        const int v0 = max(low - t0, 0), v1 = min((end + 15) & ~15, KT);
-        if (v0 < v1) {
-          const int pl = pos + v_place(pair, j, n), st = pl % STAGES;
-          off = wait(&full[st], pl / STAGES);
-          if (off) break;
-          bool odd = false;
-          for (int e = r; e < (v1 - v0) * VPR; e += SLOT) {
-            const int row = v0 + e / VPR, c = e % VPR;
-            uint4* at = reinterpret_cast<uint4*>(ring + st * TILE + (c >> 3) * PANEL + row * 128 +
-                                                 ((c & 7) ^ (row & 7)) * 16);
-            const uint4 x = *at;
-            if (odd_bf16x2(x.x) || odd_bf16x2(x.y) || odd_bf16x2(x.z) || odd_bf16x2(x.w)) {
-              *at = make_uint4(without_odd(x.x), without_odd(x.y), without_odd(x.z), without_odd(x.w));
-              odd |= row < end;
-            }
-          }
-          if (__any_sync(FULL_MASK, odd) && lane == 0) odd_of[fs][warp] = 1;
-          fence_async_smem();                      // (the product waits for all four warps)
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_ready[s]);
+        ready(1);
       }
       if (off || (tiles > 0 && (off = wait(&o_full[s], nO++)))) break;
       tc_fence_after();
@@ -474,22 +481,20 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
         const int per = min(RT, f.prefix ? plan.R : plan.LG);
         float* part = (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, D, my, 0);
 #pragma unroll 1
-        for (int c = pair ? 0 : 32 * s; c < D; c += pair ? 32 : 64) {
-          float o[32];
-          tmem_ld32(tO + (pair ? s * 128 : 0) + c, o);
+        for (int c = pair ? 0 : 16 * s; c < D; c += pair ? 16 : 32) {
+          float o[16];
+          tmem_ld16(tO + (pair ? s * 128 : 0) + c, o);
           if (!pair && n > 1) {
-            float y[32];
-            tmem_ld32(tO + 128 + c, y);
+            float y[16];
+            tmem_ld16(tO + 128 + c, y);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = fmaf(w1, y[i], w0 * o[i]);
+            for (int i = 0; i < 16; ++i) o[i] = fmaf(w1, y[i], w0 * o[i]);
           }
           if (mine) {
-            if (odd)
-              add_odd(a, f.b, f.h, c, max(low, k0 * KT), min(lim, (k0 + n) * KT), o);
             if (whole) {
               __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.out) + (long long)row * D + c;
 #pragma unroll
-              for (int i = 0; i < 32; i += 8)
+              for (int i = 0; i < 16; i += 8)
                 if (c + i < D) {
                   uint32_t x[4];
 #pragma unroll
@@ -502,9 +507,12 @@ attend_tc_kernel(const __grid_constant__ AttendMaps maps, const __grid_constant_
                 }
             } else {
 #pragma unroll
-              for (int i = 0; i < 32; i += 4)
+              for (int i = 0; i < 16; i += 4)
                 if (c + i < D) store4(part + (long long)(c + i) * per, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
             }
+            if (odd && !none)
+              add_odd(a, f.b, f.h, max(low, k0 * KT), min(lim, (k0 + n) * KT), c, min(c + 16, D), whole ? nullptr : part,
+                      per, static_cast<__nv_bfloat16*>(a.out) + (long long)row * D);
           }
           __syncwarp();
         }

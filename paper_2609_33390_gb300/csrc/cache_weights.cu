@@ -186,11 +186,8 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     if (cum[b + 1] == cum[b])
       for (long long t = tid; t < (long long)a.Hkv * a.S; t += WT_THREADS) a.acc_out[(long long)b * a.Hkv * a.S + t] = 0.f;
 
-  // (see attend_tc_kernel)
-  auto wait = [&](uint64_t* bar, int phase) {
-    if (!*abort_flag && !mbar_wait(bar, phase & 1, abort_flag, a.wait_limit)) *abort_flag = 1;
-    return __any_sync(FULL_MASK, *abort_flag != 0) != 0;
-  };
+  // (a warp that is told that a wait gave up leaves its loop for the barrier at the end)
+  auto wait = [&](uint64_t* bar, int phase) { return warp_wait(bar, phase, abort_flag, a.wait_limit); };
   int unit = 0, nf = 0, nq = 0;                    // units, fragments and blocks of queries before
   bool off = false;
 

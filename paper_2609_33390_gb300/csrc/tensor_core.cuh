@@ -29,6 +29,23 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
+// Waits, as a whole warp, for phase number `phase` of a barrier. True if this wait gave up or had to wait
+// and found that another one of the CTA had (which then ends the CTA's work), the same answer for all lanes.
+// The common case touches shared memory once: beside the tensor cores' operands every access takes
+// about a hundred cycles, and the issuing warp's waits stand between the products.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, int phase, volatile int* abort_flag, long long limit) {
+  const bool brief = limit < SHORT_WAIT_CYCLES;    // (tests of the failure path: see mbar_wait)
+  if (!brief && __all_sync(FULL_MASK, mbar_try_wait(bar, phase & 1))) return false;
+  const long long t0 = clock64();
+#pragma unroll 1
+  do {
+    const bool ok = brief ? mbar_test(bar, phase & 1) : mbar_try_wait(bar, phase & 1);
+    if (__all_sync(FULL_MASK, ok)) return __any_sync(FULL_MASK, *abort_flag != 0) != 0;
+  } while (__all_sync(FULL_MASK, *abort_flag == 0 && clock64() - t0 <= limit));
+  *abort_flag = 1;
+  return true;
+}
+
 __device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t ncols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(slot)),
                "r"(ncols)
