@@ -10,7 +10,7 @@ namespace brisk {
 
 constexpr int CACHE_MAX_B = 4096;    // sequences of a call (every CTA holds their tile counts)
 constexpr int CACHE_MAX_D = 128;     // width of a head
-constexpr int CACHE_SMS = 152;       // CTAs that share attention's work, at most
+constexpr int CACHE_SMS = 152;
 
 struct CacheView {   // element (s, t, h, :) at p + s*seq + t*tok + h*head, strides in elements
   const void* p;
@@ -20,6 +20,9 @@ struct CacheView {   // element (s, t, h, :) at p + s*seq + t*tok + h*head, stri
 struct AttendArgs {
   int B, L, G, Hkv, D, P, S;         // G query heads a key head
   int dt;                            // brisk_dtype of q, keys, values and out
+  // division of the work (see Plan): rows and keys of a tile; CTAs of the kernel for the prefix (0: the one
+  // for the own caches has both) and of the one for the own caches
+  int rt_p, rt_o, kt, grid_p, grid_o;
   CacheView q, kp, vp, ko, vo;
   const int32_t* own_len;            // [B]
   const int32_t* visible;            // [B, L] or nullptr
@@ -31,108 +34,121 @@ struct AttendArgs {
   float *part_p, *part_o;
   float2 *ml_p, *ml_o;
   int32_t* cum;                      // [B + 1] key tiles of the sequences before each
-  int32_t* errs;                     // [grid] what a CTA found wrong
+  int32_t* errs;                     // [grid_p + grid_o] what a CTA found wrong
   int32_t* status;
-  int grid;
   long long wait_limit;
 };
 
 // ---------------------------------------------------------------- division of the work
-// The unit of work is a tile of KT keys for a tile of up to RT query rows of one key head. A row is a
+// The unit of work is a tile of `kt` keys for a tile of up to `rt` query rows of one key head. A row is a
 // (token, query head of the group) pair: row = token * G + g. Over the prefix, the rows of all
-// sequences form common tiles (its keys are read once for RT rows, whichever sequence they are of);
-// over the own caches, the rows of one sequence. All units stand in one sequence: first the prefix's
+// sequences form common tiles (its keys are read once for rt_p rows, whichever sequence they are of);
+// over the own caches, the rows of one sequence. The units stand in one sequence: first the prefix's
 // (by head, row tile, key tile), then the own caches' (by sequence, head, row tile, key tile), and
-// each CTA takes `share` of them, wherever that begins and ends. A row tile's keys may so
-// be divided over several CTAs, each of which leaves a part; the parts are joined by merge_kernel.
-// Slots: walking through the sequence, (item index + CTA) grows with every (item, CTA) pair, so it
+// each CTA takes `share` of them, wherever that begins and ends; or the prefix's and the own caches' are
+// two sequences of two kernels (apart). A row tile's keys may so be divided over several CTAs, each of
+// which leaves a part; the parts are joined by merge_kernel.
+// Slots: walking through a sequence, (item index + CTA) grows with every (item, CTA) pair, so it
 // numbers the parts. Counts of units fit 31 bits (checked on the host).
 struct Plan {
-  int B, LG, Hkv, P, RT, KT;
+  int B, LG, Hkv, rt_p, rt_o, kt;
   int nPT, kP, nLT;                  // row tiles and key tiles of the prefix; row tiles of a sequence
-  int R, UP, T, share;               // rows a key head; units of the prefix; all units; units a CTA
+  int R, UP, UO;                     // rows a key head; units of the prefix and of the own caches
+  int own0;                          // number of the own caches' first unit
+  int share_p, share_o;              // units a CTA
 
-  __device__ Plan(int b, int lg, int hkv, int p, int rt, int kt, int own_tiles, int grid) {
-    B = b; LG = lg; Hkv = hkv; P = p; RT = rt; KT = kt;
+  __device__ Plan(int b, int lg, int hkv, int p, int rtp, int rto, int kt_, int own_tiles, int grid_p, int grid_o) {
+    B = b; LG = lg; Hkv = hkv; rt_p = rtp; rt_o = rto; kt = kt_;
     R = B * LG;
-    kP = (P + KT - 1) / KT;
-    nPT = P > 0 ? (R + RT - 1) / RT : 0;
-    nLT = (LG + RT - 1) / RT;
+    kP = (p + kt - 1) / kt;
+    nPT = p > 0 ? (R + rt_p - 1) / rt_p : 0;
+    nLT = (LG + rt_o - 1) / rt_o;
     UP = Hkv * nPT * kP;
-    T = UP + Hkv * nLT * own_tiles;
-    share = max(1, (int)(((unsigned)T + grid - 1) / grid));
+    UO = Hkv * nLT * own_tiles;
+    const bool apart = grid_p > 0;
+    own0 = apart ? 0 : UP;
+    share_o = max(1, (int)(((unsigned)own0 + UO + grid_o - 1) / grid_o));
+    share_p = apart ? max(1, (int)(((unsigned)UP + grid_p - 1) / grid_p)) : share_o;
   }
-  __device__ Plan(const AttendArgs& a, int rt, int kt, int own_tiles)
-      : Plan(a.B, a.L * a.G, a.Hkv, a.P, rt, kt, own_tiles, a.grid) {}
-  __device__ int units_of(int cta) const {
-    return (int)(min((long long)T, (cta + 1LL) * share) - min((long long)T, (long long)cta * share));
-  }
-  __device__ int cta_of(int u) const { return u / share; }
-  __device__ int own_start(const int32_t* cum, int b, int h, int lt) const {
-    return UP + Hkv * nLT * cum[b] + (h * nLT + lt) * (cum[b + 1] - cum[b]);
-  }
+  __device__ Plan(const AttendArgs& a, int own_tiles)
+      : Plan(a.B, a.L * a.G, a.Hkv, a.P, a.rt_p, a.rt_o, a.kt, own_tiles, a.grid_p, a.grid_o) {}
+  __device__ int tiles(int len) const { return (len + kt - 1) / kt; }
 };
+
+// The units a CTA has of a sequence of `all`.
+__device__ __forceinline__ int2 units_of(int cta, int share, int all) {
+  const long long first = (long long)cta * share;
+  return make_int2((int)min(first, (long long)all), (int)min(first + share, (long long)all));
+}
 
 // A CTA's share of one item (a row tile's keys): key tiles [k0, k0 + n).
 struct Frag {
   int prefix, whole;                 // whole: no other part for these rows exists
-  int h, b, tile, k0, n;
+  int h, b, k0, n;
   int row0, rows;                    // rows of the head over the prefix, of the sequence else
-  int slot;
+  int slot, len;                     // len: entries of the prefix, or in use of the own cache
 };
 
-struct Walk {
-  int u, end, c, b;
+// The sequence of a CTA's first own unit, and the key tiles of the sequences before it (see scan_lengths).
+struct Start { int b, before; };
 
-  __device__ Walk(const Plan& p, const int32_t* cum, int cta) {
+template <typename Args>
+__device__ __forceinline__ int clamped_len(const Args& a, int b) {
+  return min(max(a.own_len[b], 0), a.S);
+}
+
+// Walks through the units of a kernel that has the own caches' (and, unless apart, the prefix's).
+struct Walk {
+  int u, end, c, b, base, n, len;    // b: sequence whose units begin at `base`, n key tiles
+
+  template <typename Args>
+  __device__ Walk(const Args& a, const Plan& p, int cta, const Start& start) {
+    const int2 r = units_of(cta, p.share_o, p.own0 + p.UO);
+    u = r.x;
+    end = r.y;
     c = cta;
-    b = 0;
-    u = (int)min((long long)p.T, (long long)cta * p.share);
-    end = (int)min((long long)p.T, (long long)u + p.share);
-    if (end > p.UP) {                // the sequence of the first unit behind the prefix's
-      const int v = (u > p.UP ? u - p.UP : 0) / (p.Hkv * p.nLT);
-      int lo = 0, hi = p.B - 1;      // the last b with cum[b] <= v
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (cum[mid] <= v) lo = mid; else hi = mid - 1;
-      }
-      b = lo;
+    b = base = n = len = 0;
+    if (u < end && end > p.own0) {   // (a CTA without own units has no start)
+      b = start.b;
+      base = p.own0 + p.Hkv * p.nLT * start.before;
+      len = clamped_len(a, b);
+      n = p.tiles(len);
     }
   }
-  __device__ bool next(const Plan& p, const int32_t* cum, Frag& f) {
+  template <typename Args>
+  __device__ bool next(const Args& a, const Plan& p, Frag& f) {
     if (u >= end) return false;
-    if (u < p.UP) {
+    if (u < p.own0) {
       const int item = u / p.kP;
       f.prefix = 1;
       f.k0 = u - item * p.kP;
       f.n = min(p.kP - f.k0, end - u);
       f.h = item / p.nPT;
-      f.tile = item - f.h * p.nPT;
       f.b = 0;
-      f.row0 = f.tile * p.RT;
-      f.rows = min(p.RT, p.R - f.row0);
+      f.row0 = (item - f.h * p.nPT) * p.rt_p;
+      f.rows = min(p.rt_p, p.R - f.row0);
       f.slot = item + c;
-      const int b0 = f.row0 / p.LG, b1 = (f.row0 + f.rows - 1) / p.LG;
-      f.whole = f.n == p.kP && cum[b1 + 1] == cum[b0];
+      f.whole = f.n == p.kP && a.S == 0;
+      f.len = a.P;
     } else {
       const int per = p.Hkv * p.nLT;
-      int base = p.UP + per * cum[b], n = cum[b + 1] - cum[b];
       while (u >= base + per * n) {
         base += per * n;
         ++b;
-        n = cum[b + 1] - cum[b];
+        len = clamped_len(a, b);
+        n = p.tiles(len);
       }
-      const int r = (u - base) / n;
+      const int r = (u - base) / n, tile = r % p.nLT;
       f.prefix = 0;
       f.b = b;
       f.h = r / p.nLT;
-      f.tile = r - f.h * p.nLT;
       f.k0 = u - base - r * n;
       f.n = min(n - f.k0, end - u);
-      f.row0 = f.tile * p.RT;
-      f.rows = min(p.RT, p.LG - f.row0);
-      f.slot = (b * p.Hkv + f.h) * p.nLT + f.tile + c;
-      f.whole = f.n == n && p.P == 0;
+      f.row0 = tile * p.rt_o;
+      f.rows = min(p.rt_o, p.LG - f.row0);
+      f.slot = b * per + r + c;
+      f.whole = f.n == n && p.UP == 0;
+      f.len = len;
     }
     u += f.n;
     return true;
@@ -145,10 +161,6 @@ __device__ __forceinline__ long long part_at(long long slot, int per, int D, int
   return slot * per * D + ((long long)(c >> 2) * per + row) * 4;
 }
 
-template <typename Args>
-__device__ __forceinline__ int clamped_len(const Args& a, int b) {
-  return min(max(a.own_len[b], 0), a.S);
-}
 // Token (b * L + i) and query head of a fragment's row, and how many keys the row sees.
 __device__ __forceinline__ void row_of(const AttendArgs& a, const Frag& f, int r, int& token, int& head) {
   const int row = f.row0 + r, t = row / a.G;
@@ -163,10 +175,13 @@ __device__ __forceinline__ bool row_idle(const AttendArgs& a, int token) {
   return a.visible && a.visible[token] < 0;
 }
 
-// Key tiles before each sequence, by all THREADS threads of a CTA; returns their sum. *bad is set
-// where a length lies outside 0..S (the caller clears it before a barrier).
-template <int THREADS, typename Args>
-__device__ int count_tiles(const Args& a, int kt, int32_t* cum, int* warp_sum, int* bad) {
+// Sums the sequences' key tiles, by all THREADS threads of a CTA, and finds the sequence of key tile
+// first_own(sum) (of all sequences' in a row) in shared memory, valid after the call. The tiles before each
+// sequence go to `cum` unless that is nullptr; *bad is set where a length lies outside 0..S (the caller
+// clears it before a barrier).
+template <int THREADS, typename Args, typename First>
+__device__ void scan_lengths(const Args& a, int kt, int32_t* cum, int* warp_sum, int* bad, Start* start,
+                             First first_own) {
   const int per = (a.B + THREADS - 1) / THREADS, tid = threadIdx.x, lane = tid & 31;
   const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
   int sum = 0;
@@ -188,13 +203,15 @@ __device__ int count_tiles(const Args& a, int kt, int32_t* cum, int* warp_sum, i
     if (w < (tid >> 5)) before += warp_sum[w];
     total += warp_sum[w];
   }
+  const int at = first_own(total);
   for (int b = b0; b < b1; ++b) {
-    cum[b] = before;
-    before += (clamped_len(a, b) + kt - 1) / kt;
+    const int n = (clamped_len(a, b) + kt - 1) / kt;
+    if (cum) cum[b] = before;
+    if (at >= before && at < before + n) *start = Start{b, before};
+    before += n;
   }
-  if (tid == 0) cum[a.B] = total;
+  if (cum && tid == 0) cum[a.B] = total;
   __syncthreads();
-  return total;
 }
 
 // Four elements of a row, as fp32, and back.
@@ -210,14 +227,26 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
 }
 
-// Rows and keys of a tile: bf16 on the tensor cores, fp32 on the FMA units.
-constexpr int ATTEND_RT_TC = 256, ATTEND_KT_TC = 128;
-constexpr int ATTEND_RT_F32 = 64, ATTEND_KT_F32 = 64;
-inline int attend_rt(int dt) { return dt == BRISK_DT_BF16 ? ATTEND_RT_TC : ATTEND_RT_F32; }
-inline int attend_kt(int dt) { return dt == BRISK_DT_BF16 ? ATTEND_KT_TC : ATTEND_KT_F32; }
+// Keys of a tile, rows of it, and CTAs: bf16 on the tensor cores, fp32 on the FMA units. With bf16 and more
+// than SLOT_ROWS query rows a key head, the prefix has a kernel of its own.
+constexpr int TC_KT = 128, SLOT_ROWS = 128, PAIR_ROWS = 256, SIMT_KT = 64, SIMT_ROWS = 64;
+constexpr int SLOT_CTAS = 2 * CACHE_SMS;
+inline void divide(AttendArgs* a) {
+  const bool tc = a->dt == BRISK_DT_BF16, apart = tc && a->P > 0 && (long long)a->B * a->L * a->G > SLOT_ROWS;
+  a->kt = tc ? TC_KT : SIMT_KT;
+  a->rt_o = tc ? SLOT_ROWS : SIMT_ROWS;
+  a->rt_p = apart ? PAIR_ROWS : a->rt_o;
+  a->grid_p = apart ? CACHE_SMS : 0;
+  a->grid_o = tc ? SLOT_CTAS : CACHE_SMS;
+}
 
 // Tensor map of a cache's tiles of 64 columns x 128 entries (cache_attend_tc.cu).
 bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int toks, int seqs);
+
+// The next kernel of the stream may be set up once all of this one's CTAs have begun; the wait until
+// the kernel before has ended, and what it wrote can be read.
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream);
@@ -225,7 +254,7 @@ cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream);
 
 // ---------------------------------------------------------------- attention weight of own entries
 struct WeightArgs {
-  int B, L, G, Hkv, D, S, dt;
+  int B, L, G, Hkv, D, P, S, dt;     // P: 0 (no units of the prefix's)
   CacheView q, ko;
   const int32_t *own_len, *visible;
   const float* lse;        // [B, L, Hkv * G]

@@ -48,16 +48,26 @@ struct CacheWs {
   size_t status, errs, cum, part_p, ml_p, part_o, ml_o, total;
 };
 
+AttendArgs sizes_of(const brisk_cache_dims* d) {
+  AttendArgs a{};
+  a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.P = d->P; a.S = d->S;
+  a.dt = d->dtype;
+  divide(&a);
+  return a;
+}
+
 CacheWs cache_ws(const brisk_cache_dims* d) {
   CacheWs w{};
-  const long long G = d->Hq / d->Hkv, LG = d->L * G, R = d->B * LG, rt = attend_rt(d->dtype);
-  const long long tiles_p = d->P > 0 ? (R + rt - 1) / rt * d->Hkv : 0;
-  const long long tiles_o = d->S > 0 ? (LG + rt - 1) / rt * d->Hkv * d->B : 0;
-  const long long rows_p = (tiles_p + CACHE_SMS) * (R < rt ? R : rt), rows_o = (tiles_o + CACHE_SMS) * (LG < rt ? LG : rt);
+  const AttendArgs a = sizes_of(d);
+  const long long LG = a.L * a.G, R = d->B * LG;
+  const long long tiles_p = d->P > 0 ? (R + a.rt_p - 1) / a.rt_p * d->Hkv : 0;
+  const long long tiles_o = d->S > 0 ? (LG + a.rt_o - 1) / a.rt_o * d->Hkv * d->B : 0;
+  const long long rows_p = (tiles_p + (a.grid_p ? a.grid_p : a.grid_o)) * (R < a.rt_p ? R : a.rt_p);
+  const long long rows_o = (tiles_o + a.grid_o) * (LG < a.rt_o ? LG : a.rt_o);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t q = o; o = up(o + bytes); return q; };
   w.status = take(ALIGN);
-  w.errs = take(sizeof(int32_t) * CACHE_SMS);
+  w.errs = take(sizeof(int32_t) * (a.grid_p + a.grid_o));
   w.cum = take(sizeof(int32_t) * (d->B + 1));
   w.ml_p = take(sizeof(float2) * rows_p);
   w.ml_o = take(sizeof(float2) * rows_o);
@@ -69,9 +79,10 @@ CacheWs cache_ws(const brisk_cache_dims* d) {
 
 // Whether attention's units of work, all caches full, are counted in 31 bits.
 bool units_ok(const brisk_cache_dims* d) {
-  const long long G = d->Hq / d->Hkv, LG = d->L * G, R = d->B * LG, rt = attend_rt(d->dtype), kt = attend_kt(d->dtype);
-  const double pre = (double)d->Hkv * ((R + rt - 1) / rt) * ((d->P + kt - 1) / kt);
-  const double own = (double)d->Hkv * d->B * ((LG + rt - 1) / rt) * ((d->S + kt - 1) / kt);
+  const AttendArgs a = sizes_of(d);
+  const long long LG = a.L * a.G, R = d->B * LG;
+  const double pre = (double)d->Hkv * ((R + a.rt_p - 1) / a.rt_p) * ((d->P + a.kt - 1) / a.kt);
+  const double own = (double)d->Hkv * d->B * ((LG + a.rt_o - 1) / a.rt_o) * ((d->S + a.kt - 1) / a.kt);
   return pre + own < 2.0e9;
 }
 
@@ -94,15 +105,13 @@ brisk_status brisk_prefix_attend(const brisk_cache_dims* d, const brisk_view* q,
                                  float* lse, void* ws, void* stream) {
   if (!dims_ok(d) || !own_len || !out || !aligned(out, 16) || !ws || !aligned(ws, ALIGN) || !scale_ok(scale))
     return BRISK_ERR_INVALID_ARG;
-  AttendArgs a{};
+  AttendArgs a = sizes_of(d);
   if (!view_ok(q, d, d->B, d->L, d->Hq, &a.q) || !view_ok(k_prefix, d, 1, d->P, d->Hkv, &a.kp) ||
       !view_ok(v_prefix, d, 1, d->P, d->Hkv, &a.vp) || !view_ok(k_own, d, d->B, d->S, d->Hkv, &a.ko) ||
       !view_ok(v_own, d, d->B, d->S, d->Hkv, &a.vo))
     return BRISK_ERR_INVALID_ARG;
   if (!units_ok(d)) return BRISK_ERR_UNSUPPORTED;
   const CacheWs w = cache_ws(d);
-  a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.P = d->P; a.S = d->S;
-  a.dt = d->dtype;
   a.own_len = own_len;
   a.visible = visible;
   a.sl2 = scale * LOG2E;
@@ -115,7 +124,6 @@ brisk_status brisk_prefix_attend(const brisk_cache_dims* d, const brisk_view* q,
   a.cum = at<int32_t>(ws, w.cum);
   a.errs = at<int32_t>(ws, w.errs);
   a.status = at<int32_t>(ws, w.status);
-  a.grid = CACHE_SMS;
   a.wait_limit = wait_limit_cycles();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   // a scale of 0 would make NaN of the masked scores' -inf; this one leaves every finite score at 0

@@ -12,38 +12,40 @@ namespace brisk {
 namespace {
 
 constexpr int SIMT_THREADS = 256;
-constexpr int KT = ATTEND_KT_F32;
+constexpr int KT = SIMT_KT, RT = SIMT_ROWS, RPT = RT / 16;
 constexpr int KS = CACHE_MAX_D + 4;    // floats between the key tile's rows: 16 rows' float4s in two wavefronts
 
 // Rows x keys on the FMA units: 16 x 16 threads, RT/16 rows and 4 keys each for the scores, the
 // same rows and 8 columns each for the sums of values. A row's 16 threads are half a warp, so
 // its maximum, its sum and the exchange of its probabilities need no barrier of the CTA.
-template <typename T, int RT>
 __global__ void __launch_bounds__(SIMT_THREADS)
 attend_simt_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int RPT = RT / 16;
+  using T = float;
   extern __shared__ __align__(16) float smem[];
   float* sQ = smem;                               // [RT][CACHE_MAX_D]
   float* sK = sQ + RT * CACHE_MAX_D;              // [KT][KS]
   float* sV = sK + KT * KS;                       // [KT][CACHE_MAX_D]
   float* sP = sV + KT * CACHE_MAX_D;              // [RT][KT + 4]
-  int32_t* cum = reinterpret_cast<int32_t*>(sP + RT * (KT + 4));
   __shared__ int warp_sum[SIMT_THREADS / 32], bad, lowest;
+  __shared__ Start start;
 
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   if (tid == 0) bad = 0;
   __syncthreads();
-  const int own = count_tiles<SIMT_THREADS>(a, KT, cum, warp_sum, &bad);
-  const Plan plan(a, RT, KT, own);
-  if (blockIdx.x == 0)
-    for (int b = tid; b <= a.B; b += SIMT_THREADS) a.cum[b] = cum[b];
+  int own = 0;
+  scan_lengths<SIMT_THREADS>(a, KT, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start, [&](int total) {
+    own = total;
+    const Plan p(a, total);
+    return max(0, units_of(blockIdx.x, p.share_o, p.own0 + p.UO).x - p.own0) / (p.Hkv * p.nLT);
+  });
+  const Plan plan(a, own);
   if (tid == 0) a.errs[blockIdx.x] = bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK;
 
   const int D = a.D, nv = D / 4;
-  Walk walk(plan, cum, blockIdx.x);
+  Walk walk(a, plan, blockIdx.x, start);
   Frag f;
-  while (walk.next(plan, cum, f)) {
-    const int len = f.prefix ? a.P : clamped_len(a, f.b);
+  while (walk.next(a, plan, f)) {
+    const int len = f.len;
     const T* kb = static_cast<const T*>(f.prefix ? a.kp.p : a.ko.p) +
                   (f.prefix ? f.h * a.kp.head : f.b * a.ko.seq + f.h * a.ko.head);
     const T* vb = static_cast<const T*>(f.prefix ? a.vp.p : a.vo.p) +
@@ -202,7 +204,7 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
         if (a.lse && tx == 0)
           a.lse[(long long)token * (a.Hkv * a.G) + head] = none ? -INFINITY : (m[i] + log2f(l[i])) * (1.f / LOG2E);
       } else {
-        const int per = f.prefix ? min(RT, plan.R) : min(RT, plan.LG);
+        const int per = min(RT, f.prefix ? plan.R : plan.LG);
         float* to = f.prefix ? a.part_p : a.part_o;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -215,10 +217,7 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   }
 }
 
-constexpr size_t simt_smem(int rt) {
-  return sizeof(float) * (rt * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D + rt * (KT + 4)) +
-         sizeof(int32_t) * (CACHE_MAX_B + 1);
-}
+constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D + RT * (KT + 4));
 
 // Joins the parts of the rows whose keys were divided. A warp takes 8 neighbouring rows of a key head,
 // 4 lanes a row, each with every fourth group of four columns: its loads are runs of 128 bytes.
@@ -226,10 +225,10 @@ constexpr size_t simt_smem(int rt) {
 constexpr int MERGE_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(MERGE_THREADS)
-merge_kernel(const __grid_constant__ AttendArgs a, int rt, int kt) {
+merge_kernel(const __grid_constant__ AttendArgs a) {
   const int lane = threadIdx.x & 31, cq = lane >> 3;
-  const Plan plan(a, rt, kt, a.cum[a.B]);
-  const int per_p = min(rt, plan.R), per_o = min(rt, plan.LG), D = a.D;
+  const Plan plan(a, a.cum[a.B]);
+  const int rt_p = a.rt_p, rt_o = a.rt_o, per_p = min(rt_p, plan.R), per_o = min(rt_o, plan.LG), D = a.D;
   const int groups = (plan.R + 7) / 8;             // of a key head
   for (int w = (int)blockIdx.x * (MERGE_THREADS / 32) + (threadIdx.x >> 5); w < groups * a.Hkv;
        w += (int)gridDim.x * (MERGE_THREADS / 32)) {
@@ -243,19 +242,18 @@ merge_kernel(const __grid_constant__ AttendArgs a, int rt, int kt) {
       token = r / a.G;
       const int b = r / plan.LG, n = a.cum[b + 1] - a.cum[b];
       if (plan.kP > 0) {
-        const int pt = r / rt, item = h * plan.nPT + pt, c0 = plan.cta_of(item * plan.kP);
-        np = plan.cta_of(item * plan.kP + plan.kP - 1) - c0 + 1;
-        src_p = a.part_p + part_at(item + c0, per_p, D, r - pt * rt, 4 * cq);
-        ml_p = a.ml_p + (long long)(item + c0) * per_p + (r - pt * rt);
-        const int b0 = pt * rt / plan.LG, b1 = (min(pt * rt + rt, plan.R) - 1) / plan.LG;
-        if (np == 1 && a.cum[b1 + 1] == a.cum[b0]) mine = false;
+        const int pt = r / rt_p, item = h * plan.nPT + pt, c0 = item * plan.kP / plan.share_p;
+        np = (item * plan.kP + plan.kP - 1) / plan.share_p - c0 + 1;
+        src_p = a.part_p + part_at(item + c0, per_p, D, r - pt * rt_p, 4 * cq);
+        ml_p = a.ml_p + (long long)(item + c0) * per_p + (r - pt * rt_p);
+        if (np == 1 && a.S == 0) mine = false;
       }
       if (n > 0) {
-        const int ro = r - b * plan.LG, lt = ro / rt, u = plan.own_start(a.cum, b, h, lt);
-        const int c0 = plan.cta_of(u), slot = (b * a.Hkv + h) * plan.nLT + lt + c0;
-        no = plan.cta_of(u + n - 1) - c0 + 1;
-        src_o = a.part_o + part_at(slot, per_o, D, ro - lt * rt, 4 * cq);
-        ml_o = a.ml_o + (long long)slot * per_o + (ro - lt * rt);
+        const int ro = r - b * plan.LG, lt = ro / rt_o, of = h * plan.nLT + lt, per = a.Hkv * plan.nLT;
+        const int u = plan.own0 + per * a.cum[b] + of * n, c0 = u / plan.share_o, slot = b * per + of + c0;
+        no = (u + n - 1) / plan.share_o - c0 + 1;
+        src_o = a.part_o + part_at(slot, per_o, D, ro - lt * rt_o, 4 * cq);
+        ml_o = a.ml_o + (long long)slot * per_o + (ro - lt * rt_o);
         if (np == 0 && no == 1) mine = false;
       }
     }
@@ -301,7 +299,7 @@ merge_kernel(const __grid_constant__ AttendArgs a, int rt, int kt) {
   }
   if (blockIdx.x == 0 && threadIdx.x < 32) {
     int code = BRISK_OK;                           // the largest: a wait that gave up before a bad length
-    for (int c = lane; c < a.grid; c += 32) code = max(code, a.errs[c]);
+    for (int c = lane; c < a.grid_p + a.grid_o; c += 32) code = max(code, a.errs[c]);
     code = __reduce_max_sync(FULL_MASK, code);
     if (lane == 0) *a.status = code;
   }
@@ -310,22 +308,17 @@ merge_kernel(const __grid_constant__ AttendArgs a, int rt, int kt) {
 }  // namespace
 
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
-  auto run = [&](auto kernel, size_t smem) {
-    cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
-    if (e != cudaSuccess) return e;
-    kernel<<<a.grid, SIMT_THREADS, smem, stream>>>(a);
-    return cudaGetLastError();
-  };
-  return run(attend_simt_kernel<float, ATTEND_RT_F32>, simt_smem(ATTEND_RT_F32));
+  cudaError_t e = set_up_kernel(attend_simt_kernel, CARVEOUT_FULL_KB, SIMT_SMEM);
+  if (e != cudaSuccess) return e;
+  attend_simt_kernel<<<a.grid_o, SIMT_THREADS, SIMT_SMEM, stream>>>(a);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {
   const int warps = (a.B * a.L * a.G + 7) / 8 * a.Hkv, ctas = (warps + MERGE_THREADS / 32 - 1) / (MERGE_THREADS / 32);
   const int grid = ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS;
-  if (a.dt == BRISK_DT_BF16)
-    merge_kernel<__nv_bfloat16><<<grid, MERGE_THREADS, 0, stream>>>(a, attend_rt(a.dt), attend_kt(a.dt));
-  else
-    merge_kernel<float><<<grid, MERGE_THREADS, 0, stream>>>(a, attend_rt(a.dt), attend_kt(a.dt));
+  if (a.dt == BRISK_DT_BF16) merge_kernel<__nv_bfloat16><<<grid, MERGE_THREADS, 0, stream>>>(a);
+  else merge_kernel<float><<<grid, MERGE_THREADS, 0, stream>>>(a);
   return cudaGetLastError();
 }
 

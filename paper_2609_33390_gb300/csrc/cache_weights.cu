@@ -121,7 +121,7 @@ template <int DP>
 struct WShape {
   static constexpr int TILE = KT * DP * 2;
   static constexpr int STAGES = DP == 128 ? 3 : 6;
-  static constexpr int SMEM = 1024 + (Q_STAGES + STAGES) * TILE + (CACHE_MAX_B + 1) * 4;
+  static constexpr int SMEM = 1024 + (Q_STAGES + STAGES) * TILE;
 };
 
 struct WInfo {
@@ -137,7 +137,6 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = base;
   uint8_t* ring = base + Q_STAGES * TILE;
-  int32_t* cum = reinterpret_cast<int32_t*>(ring + STAGES * TILE);
   __shared__ __align__(16) float neg_lse[Q_STAGES][QB];    // -lse, log2 units
   __shared__ __align__(16) int row_lim[Q_STAGES][QB];
   __shared__ uint64_t k_full[STAGES], k_empty[STAGES], q_full[Q_STAGES], q_empty[Q_STAGES];
@@ -145,6 +144,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ WInfo info[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int aborted, bad, warp_sum[WT_THREADS / 32];
+  __shared__ Start start;
   volatile int* abort_flag = &aborted;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -177,13 +177,19 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
 
-  const int own = count_tiles<WT_THREADS>(a, KT, cum, warp_sum, &bad);
   const int rows = a.L * a.G, nb = (rows + QB - 1) / QB;
-  const Plan plan(a.B, rows, a.Hkv, 0, rows, KT, own, a.grid);
-  const int units = plan.units_of(blockIdx.x);
+  int own = 0;
+  scan_lengths<WT_THREADS>(a, KT, nullptr, warp_sum, &bad, &start, [&](int total) {
+    own = total;
+    const Plan p(a.B, rows, a.Hkv, 0, 1, rows, KT, total, 0, a.grid);
+    return units_of(blockIdx.x, p.share_o, p.UO).x / a.Hkv;
+  });
+  const Plan plan(a.B, rows, a.Hkv, 0, 1, rows, KT, own, 0, a.grid);
+  const int2 range = units_of(blockIdx.x, plan.share_o, plan.UO);
+  const int units = range.y - range.x;
   // sequences without entries have no units: zeros everywhere
   for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-    if (cum[b + 1] == cum[b])
+    if (clamped_len(a, b) == 0)
       for (long long t = tid; t < (long long)a.Hkv * a.S; t += WT_THREADS) a.acc_out[(long long)b * a.Hkv * a.S + t] = 0.f;
 
   // (a warp that is told that a wait gave up leaves its loop for the barrier at the end)
@@ -192,9 +198,9 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   bool off = false;
 
   if (warp == 8) {
-    Walk walk(plan, cum, blockIdx.x);
+    Walk walk(a, plan, blockIdx.x, start);
     Frag f;
-    while (!off && walk.next(plan, cum, f))
+    while (!off && walk.next(a, plan, f))
       for (int j = 0; j < f.n; ++j, ++unit) {
         const int st = unit % STAGES;
         off = unit >= STAGES && wait(&k_empty[st], unit / STAGES - 1);
@@ -258,10 +264,10 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     mbar_drain(&done, 0);
   } else if (warp >= 10) {
     const int pw = warp - 10, np = 2 * ((a.D + 15) / 16);
-    Walk walk(plan, cum, blockIdx.x);
+    Walk walk(a, plan, blockIdx.x, start);
     Frag f;
-    while (!off && walk.next(plan, cum, f)) {
-      const int fs = nf & 1, len = clamped_len(a, f.b), loads = nb > 2 ? f.n * nb : nb;
+    while (!off && walk.next(a, plan, f)) {
+      const int fs = nf & 1, len = f.len, loads = nb > 2 ? f.n * nb : nb;
       if (nf >= 2 && (off = wait(&f_empty[fs], (nf >> 1) - 1))) break;
       // what no row of the head is kept from: needed before the first block is there
       int low = len;
@@ -272,7 +278,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         if (a.lse[token * (a.Hkv * a.G) + f.h * a.G + g] == -INFINITY) low = 0;
       }
       low = __reduce_min_sync(FULL_MASK, low);
-      if (pw == 0 && lane == 0) info[fs] = WInfo{f.b, f.h, f.k0, f.n, len, low, f.k0 + f.n == cum[f.b + 1] - cum[f.b]};
+      if (pw == 0 && lane == 0) info[fs] = WInfo{f.b, f.h, f.k0, f.n, len, low, f.k0 + f.n == plan.tiles(len)};
       __syncwarp();
       if (lane == 0) mbar_arrive(&f_full[fs]);
       ++nf;
