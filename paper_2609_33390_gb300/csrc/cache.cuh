@@ -83,7 +83,8 @@ __device__ __forceinline__ int2 units_of(int cta, int share, int all) {
 
 // A CTA's share of one item (a row tile's keys): key tiles [k0, k0 + n).
 struct Frag {
-  int prefix, whole;                 // whole: no other part for these rows exists
+  int prefix, whole;                 // whole: the rows' result is written with it (own entries: with the
+                                     // prefix's parts, where another kernel has left them)
   int h, b, k0, n;
   int row0, rows;                    // rows of the head over the prefix, of the sequence else
   int slot, len;                     // len: entries of the prefix, or in use of the own cache
@@ -147,7 +148,7 @@ struct Walk {
       f.row0 = tile * p.rt_o;
       f.rows = min(p.rt_o, p.LG - f.row0);
       f.slot = b * per + r + c;
-      f.whole = f.n == n && p.UP == 0;
+      f.whole = f.n == n && (p.UP == 0 || p.own0 == 0);
       f.len = len;
     }
     u += f.n;
@@ -214,6 +215,29 @@ __device__ void scan_lengths(const Args& a, int kt, int32_t* cum, int* warp_sum,
   __syncthreads();
 }
 
+// Parts over the prefix that the kernel for the own caches joins itself, where it has all own entries of a
+// row; with more, whose loads would wait for one another, it leaves a part too.
+constexpr int JOIN_PARTS = 2;
+
+// The parts that the prefix's kernel, or the prefix's units of a common one, leave of row `r` of a head: a
+// run of `n` slots.
+struct PrefixParts {
+  int n, per;
+  const float* sums;                 // column 0 of the first part; the next one is per * D further
+  const float2* ml;
+  __device__ PrefixParts(const AttendArgs& a, const Plan& p, int h, int r) {
+    n = 0;
+    per = min(p.rt_p, p.R);
+    sums = nullptr;
+    ml = nullptr;
+    if (p.kP == 0) return;
+    const int pt = r / p.rt_p, first = (h * p.nPT + pt) * p.kP, c0 = first / p.share_p, slot = h * p.nPT + pt + c0;
+    n = (first + p.kP - 1) / p.share_p - c0 + 1;
+    sums = a.part_p + part_at(slot, per, a.D, r - pt * p.rt_p, 0);
+    ml = a.ml_p + (long long)slot * per + (r - pt * p.rt_p);
+  }
+};
+
 // Four elements of a row, as fp32, and back.
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
@@ -247,6 +271,23 @@ bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int 
 // the kernel before has ended, and what it wrote can be read.
 __device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Launches a kernel that may be set up while the one before it on the stream still runs.
+template <typename Kernel, typename... Args>
+inline cudaError_t launch_early(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t stream, bool early,
+                                const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream);

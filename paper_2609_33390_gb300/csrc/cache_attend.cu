@@ -32,6 +32,7 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   if (tid == 0) bad = 0;
   __syncthreads();
+  let_next_begin();
   int own = 0;
   scan_lengths<SIMT_THREADS>(a, KT, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start, [&](int total) {
     own = total;
@@ -220,82 +221,123 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
 constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D + RT * (KT + 4));
 
 // Joins the parts of the rows whose keys were divided. A warp takes 8 neighbouring rows of a key head,
-// 4 lanes a row, each with every fourth group of four columns: its loads are runs of 128 bytes.
-// Bound by the parts' bytes, which the kernel before left in L2 where there is room.
-constexpr int MERGE_THREADS = 256;
-template <typename T>
+// 4 lanes a row, each with every fourth group of four columns: its loads are runs of 128 bytes, a part's
+// all in flight at once. With few rows the 8 warps of a CTA take the rows' parts in turn (SPLIT) and meet in
+// shared memory: one part after another is a load's latency each (one block of 32 positions over 4096 + 1100
+// entries, 21 parts a row: a warp a row group 54 us).
+constexpr int MERGE_WARPS = 8, MERGE_THREADS = 32 * MERGE_WARPS;
+template <typename T, int SPLIT>
 __global__ void __launch_bounds__(MERGE_THREADS)
 merge_kernel(const __grid_constant__ AttendArgs a) {
-  const int lane = threadIdx.x & 31, cq = lane >> 3;
+  constexpr int NG = CACHE_MAX_D / 16;             // groups of four columns of a lane
+  __shared__ __align__(16) float sum_of[SPLIT > 1 ? SPLIT : 1][SPLIT > 1 ? 8 : 1][CACHE_MAX_D + 4];
+  __shared__ float2 ml_of[SPLIT > 1 ? SPLIT : 1][8];
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cq = lane >> 3, sub = warp % SPLIT;
   const Plan plan(a, a.cum[a.B]);
-  const int rt_p = a.rt_p, rt_o = a.rt_o, per_p = min(rt_p, plan.R), per_o = min(rt_o, plan.LG), D = a.D;
+  const int rt_o = a.rt_o, per_o = min(rt_o, plan.LG), D = a.D, Hq = a.Hkv * a.G;
   const int groups = (plan.R + 7) / 8;             // of a key head
-  for (int w = (int)blockIdx.x * (MERGE_THREADS / 32) + (threadIdx.x >> 5); w < groups * a.Hkv;
-       w += (int)gridDim.x * (MERGE_THREADS / 32)) {
+  const bool joined = a.grid_p > 0;                // (see JOIN_PARTS)
+  for (int w0 = (int)blockIdx.x * (MERGE_WARPS / SPLIT); w0 < groups * a.Hkv; w0 += (int)gridDim.x * (MERGE_WARPS / SPLIT)) {
+    const int w = w0 + warp / SPLIT;
     const int h = w / groups, r = (w - h * groups) * 8 + (lane & 7);
     // the parts over the prefix, then those over the own cache: a run of slots each
-    const float *src_p = nullptr, *src_o = nullptr;
-    const float2 *ml_p = nullptr, *ml_o = nullptr;
-    int np = 0, no = 0, token = 0;
-    bool mine = r < plan.R;                        // (and not written by the only CTA that had its keys)
+    PrefixParts pre(a, plan, h, r < plan.R ? r : 0);
+    const float* src_o = nullptr;
+    const float2* ml_o = nullptr;
+    int no = 0, token = 0;
+    bool mine = w < groups * a.Hkv && r < plan.R;  // (and not written with the only part)
     if (mine) {
       token = r / a.G;
       const int b = r / plan.LG, n = a.cum[b + 1] - a.cum[b];
-      if (plan.kP > 0) {
-        const int pt = r / rt_p, item = h * plan.nPT + pt, c0 = item * plan.kP / plan.share_p;
-        np = (item * plan.kP + plan.kP - 1) / plan.share_p - c0 + 1;
-        src_p = a.part_p + part_at(item + c0, per_p, D, r - pt * rt_p, 4 * cq);
-        ml_p = a.ml_p + (long long)(item + c0) * per_p + (r - pt * rt_p);
-        if (np == 1 && a.S == 0) mine = false;
-      }
+      if (pre.n == 1 && a.S == 0) mine = false;
       if (n > 0) {
         const int ro = r - b * plan.LG, lt = ro / rt_o, of = h * plan.nLT + lt, per = a.Hkv * plan.nLT;
         const int u = plan.own0 + per * a.cum[b] + of * n, c0 = u / plan.share_o, slot = b * per + of + c0;
         no = (u + n - 1) / plan.share_o - c0 + 1;
-        src_o = a.part_o + part_at(slot, per_o, D, ro - lt * rt_o, 4 * cq);
+        src_o = a.part_o + part_at(slot, per_o, D, ro - lt * rt_o, 0);
         ml_o = a.ml_o + (long long)slot * per_o + (ro - lt * rt_o);
-        if (np == 0 && no == 1) mine = false;
+        if (no == 1 && (pre.n == 0 || (joined && pre.n <= JOIN_PARTS))) mine = false;
       }
     }
     const bool idle = mine && row_idle(a, token);
-    const int parts = mine && !idle ? np + no : 0;
+    const int parts = mine && !idle ? pre.n + no : 0;
     float m = -INFINITY, l = 0.f;
-    float4 o[CACHE_MAX_D / 16];
+    float4 o[NG];
 #pragma unroll
-    for (int k = 0; k < CACHE_MAX_D / 16; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < parts; ++i) {
-      const bool pre = i < np;
-      const int per = pre ? per_p : per_o, at = pre ? i : i - np;
-      const float2 ml = (pre ? ml_p : ml_o)[(long long)at * per];
-      const float* src = (pre ? src_p : src_o) + (long long)at * per * D;
-      float4 x[CACHE_MAX_D / 16];
+    for (int k = 0; k < NG; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = sub; i < parts; i += SPLIT) {
+      const bool first = i < pre.n;
+      const int per = first ? pre.per : per_o, at = first ? i : i - pre.n;
+      const float2 ml = (first ? pre.ml : ml_o)[(long long)at * per];
+      const float* src = (first ? pre.sums : src_o) + (long long)at * per * D;
+      float4 x[NG];
 #pragma unroll
-      for (int k = 0; k < CACHE_MAX_D / 16; ++k)
-        x[k] = 4 * cq + 16 * k < D ? load4(src + (long long)k * per * 16) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < NG; ++k) {               // (columns beyond D: others again, not stored)
+        const int c = 4 * cq + 16 * k;
+        x[k] = load4(src + (long long)(c < D ? c : 0) * per);
+      }
       const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.f : mn;
       // (a part without a finite score has sums of 0, or NaN, which pass)
       const float was = m == mn ? 1.f : ex2(m - ms), wi = ml.x == mn ? 1.f : ex2(ml.x - ms);
       m = mn;
       l = l * was + wi * ml.y;
 #pragma unroll
-      for (int k = 0; k < CACHE_MAX_D / 16; ++k) {
+      for (int k = 0; k < NG; ++k) {
         o[k].x = fmaf(wi, x[k].x, o[k].x * was);
         o[k].y = fmaf(wi, x[k].y, o[k].y * was);
         o[k].z = fmaf(wi, x[k].z, o[k].z * was);
         o[k].w = fmaf(wi, x[k].w, o[k].w * was);
       }
     }
-    if (!mine) continue;
-    const bool none = l == 0.f;
-    const float inv = none ? 0.f : 1.f / l;
-    const long long row = (long long)token * (a.Hkv * a.G) + h * a.G + (r - token * a.G);
-    T* to = static_cast<T*>(a.out) + row * D + 4 * cq;
+    const long long row = (long long)token * Hq + h * a.G + (r - token * a.G);
+    if constexpr (SPLIT == 1) {
+      if (!mine) continue;
+      const bool none = l == 0.f;
+      const float inv = none ? 0.f : 1.f / l;
+      T* to = static_cast<T*>(a.out) + row * D + 4 * cq;
 #pragma unroll
-    for (int k = 0; k < CACHE_MAX_D / 16; ++k)
-      if (4 * cq + 16 * k < D)
-        store4(to + 16 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                 : make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
-    if (a.lse && cq == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
+      for (int k = 0; k < NG; ++k)
+        if (4 * cq + 16 * k < D)
+          store4(to + 16 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                   : make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
+      if (a.lse && cq == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
+    } else {
+      // warp j has the sums of parts j, j + SPLIT, ..: of row j it joins all of them, a lane four columns
+      __syncthreads();                             // (the last group's are read)
+#pragma unroll
+      for (int k = 0; k < NG; ++k)
+        if (4 * cq + 16 * k < D) store4(&sum_of[warp][lane & 7][4 * cq + 16 * k], o[k]);
+      if (cq == 0) ml_of[warp][lane & 7] = make_float2(m, l);
+      __syncthreads();
+      const bool row_mine = __shfl_sync(FULL_MASK, (int)mine, warp) != 0;
+      const long long to_row = __shfl_sync(FULL_MASK, row, warp);
+      if (!row_mine) continue;
+      float top = -INFINITY, all = 0.f;
+#pragma unroll
+      for (int j = 0; j < SPLIT; ++j) top = fmaxf(top, ml_of[j][warp].x);
+      const float ms = top == -INFINITY ? 0.f : top;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < SPLIT; ++j) {
+        const float2 ml = ml_of[j][warp];
+        const float wj = ml.x == top ? 1.f : ex2(ml.x - ms);
+        all += wj * ml.y;
+        if (4 * lane < D) {
+          const float4 x = load4(&sum_of[j][warp][4 * lane]);
+          v.x = fmaf(wj, x.x, v.x);
+          v.y = fmaf(wj, x.y, v.y);
+          v.z = fmaf(wj, x.z, v.z);
+          v.w = fmaf(wj, x.w, v.w);
+        }
+      }
+      const bool none = all == 0.f;
+      const float inv = none ? 0.f : 1.f / all;
+      if (4 * lane < D)
+        store4(static_cast<T*>(a.out) + to_row * D + 4 * lane,
+               none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+      if (a.lse && lane == 0) a.lse[to_row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
+    }
   }
   if (blockIdx.x == 0 && threadIdx.x < 32) {
     int code = BRISK_OK;                           // the largest: a wait that gave up before a bad length
@@ -315,11 +357,14 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {
-  const int warps = (a.B * a.L * a.G + 7) / 8 * a.Hkv, ctas = (warps + MERGE_THREADS / 32 - 1) / (MERGE_THREADS / 32);
-  const int grid = ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS;
-  if (a.dt == BRISK_DT_BF16) merge_kernel<__nv_bfloat16><<<grid, MERGE_THREADS, 0, stream>>>(a);
-  else merge_kernel<float><<<grid, MERGE_THREADS, 0, stream>>>(a);
-  return cudaGetLastError();
+  // a warp a group of 8 rows, or a CTA a group where that leaves SMs without work
+  const long long groups = (long long)((a.B * a.L * a.G + 7) / 8) * a.Hkv;
+  const bool split = groups <= 4 * CACHE_SMS;
+  const long long ctas = split ? groups : (groups + MERGE_WARPS - 1) / MERGE_WARPS;
+  const int grid = (int)(ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS);
+  auto run = [&](auto kernel) { return launch_early(kernel, grid, MERGE_THREADS, 0, stream, true, a); };
+  if (a.dt == BRISK_DT_BF16) return split ? run(merge_kernel<__nv_bfloat16, 8>) : run(merge_kernel<__nv_bfloat16, 1>);
+  return split ? run(merge_kernel<float, 8>) : run(merge_kernel<float, 1>);
 }
 
 }  // namespace brisk

@@ -195,6 +195,47 @@ __device__ __forceinline__ void row_weights(uint32_t tS, uint32_t tO, int D, int
   tmem_st_wait();
 }
 
+// A row's beginning where the prefix's kernel left few parts of it: their join, as if the slot had gone through
+// the prefix's keys itself. O goes to tO (zeros without parts); complete after tmem_st_wait.
+__device__ __forceinline__ void begin_row(const PrefixParts& pre, bool has, uint32_t tO, int D, float& m, float& l) {
+  float w0 = 0.f, w1 = 0.f;
+  m = -INFINITY;
+  l = 0.f;
+  const bool two = has && pre.n > 1;
+  const float* src1 = pre.sums + (long long)(two ? pre.per : 0) * D;
+  if (has) {
+    const float2 x = pre.ml[0], y = two ? pre.ml[pre.per] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(x.x, y.x);
+    const float ms = m == -INFINITY ? 0.f : m;
+    w0 = x.x == m ? 1.f : ex2(x.x - ms);
+    w1 = !two ? 0.f : (y.x == m ? 1.f : ex2(y.x - ms));
+    l = w0 * x.y + w1 * y.y;
+  }
+#pragma unroll 1
+  for (int c = 0; c < D; c += 32) {
+    float4 x[8], y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const long long at = (long long)min(c + 4 * k, D - 4) * pre.per;
+      x[k] = has ? load4(pre.sums + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+      y[k] = two ? load4(src1 + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t v[16];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float4 p = x[4 * h + k], q = y[4 * h + k];
+        v[4 * k] = __float_as_uint(fmaf(w1, q.x, w0 * p.x));
+        v[4 * k + 1] = __float_as_uint(fmaf(w1, q.y, w0 * p.y));
+        v[4 * k + 2] = __float_as_uint(fmaf(w1, q.z, w0 * p.z));
+        v[4 * k + 3] = __float_as_uint(fmaf(w1, q.w, w0 * p.w));
+      }
+      tmem_st16(tO + c + 16 * h, v);
+    }
+  }
+}
+
 // A row's end: its result, or its part, from O at tO. `part`: column 0 of the row in the slot of parts,
 // nullptr for the result.
 __device__ __forceinline__ void store_row(const AttendArgs& a, uint32_t tO, Row x, bool mine, float m, float l,
@@ -564,6 +605,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       off = wait(&q_full, nf++);                   // (info_full came before it)
       if (off) break;
       const int n = info[fs].n, k0 = info[fs].k0, len = info[fs].len;
+      const bool resume = info[fs].whole && a.grid_p > 0;
       for (int j = 0; j < n && !off; ++j, ++unit) {
         const unsigned sk = cur % STAGES, sv = (cur + 1) % STAGES;
         off = wait(&full[sk], cur / STAGES);
@@ -580,7 +622,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         off = wait(&full[sv], (cur + 1) / STAGES) || wait(&p_ready[0], unit);
         if (off) break;
         tc_fence_after();
-        if (elect_one()) issue_values<0>(tO, tS, v, steps, id_o, j > 0);
+        if (elect_one()) issue_values<0>(tO, tS, v, steps, id_o, resume || j > 0);
         __syncwarp();
         off = wait(&p_ready[1], unit);
         if (off) break;
@@ -631,6 +673,15 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
 #pragma unroll
       for (int w = 0; w < 4; ++w) low = min(low, low_of[fs][w]);
       float m = -INFINITY, l = 0.f;
+      // all own entries of the rows, and another kernel had the prefix: go on from there
+      const bool resume = f.whole && a.grid_p > 0;
+      bool joined = false;
+      if (resume && live) {
+        const PrefixParts pre(a, plan, f.h, mine ? f.b * plan.LG + f.row0 + tid : 0);
+        joined = mine && pre.n <= JOIN_PARTS;
+        wait_for_previous();
+        begin_row(pre, joined, tO, a.D, m, l);
+      }
       auto ready = [&](int half) {
         tc_fence_before();
         __syncwarp();
@@ -645,7 +696,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         if (off) break;
         tc_fence_after();
         if (live)
-          row_weights(tS, tO, a.D, mine ? y.lim - t0 : KT, a.sl2, j == 0, m, l, [&]() { if (!clean) ready(0); });
+          row_weights(tS, tO, a.D, mine ? y.lim - t0 : KT, a.sl2, j == 0 && !resume, m, l, [&]() { if (!clean) ready(0); });
         if (clean) {
           const unsigned pl = 2 * unit + 1, st = pl % STAGES;
           off = wait(&full[st], pl / STAGES);
@@ -666,7 +717,8 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       if (next) fetched(nf + 1);
       if (live) {
         const int per = min(SLOT, f.prefix ? plan.R : plan.LG);
-        float* part = f.whole ? nullptr : (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, a.D, tid, 0);
+        float* part = f.whole && (!resume || joined) ? nullptr
+                                                     : (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, a.D, tid, 0);
         store_row(a, tO, y, mine, m, l, part, (f.prefix ? a.ml_p : a.ml_o) + (long long)f.slot * per + tid, per);
         // (the warps' words of this fragment were written before the products that o_full tells of)
         if (!f.prefix && low < f.len && (odd_of[fs][0] | odd_of[fs][1] | odd_of[fs][2] | odd_of[fs][3]) && mine && y.id >= 0)
@@ -708,23 +760,6 @@ bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int 
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(v.p), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Launches a kernel that may be set up while the one before it on the stream still runs.
-template <typename Kernel, typename... Args>
-static cudaError_t launch_early(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t stream, bool early,
-                                const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = early ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
