@@ -17,6 +17,27 @@ struct CacheView {   // element (s, t, h, :) at p + s*seq + t*tok + h*head, stri
   long long seq, tok, head;
 };
 
+// Division of 0 <= x < 2^31 by a constant of the call: floor(x / d) = (x * mul) >> (32 + shift) with
+// mul = ceil(2^(32 + shift) / d) and 2^shift >= d, whose error is below x / 2^31 / d (Granlund and
+// Montgomery, "Division by invariant integers using multiplication", PLDI'94). A dozen instructions fewer
+// each than the compiler's division, in kernels that outgrow the instruction cache.
+struct Divisor {
+  unsigned long long mul;   // up to 2^33
+  int d, shift;
+  void set(int by) {
+    d = by;
+    shift = 0;
+    while ((1LL << shift) < by) ++shift;
+    mul = (unsigned long long)((((unsigned __int128)1 << (32 + shift)) + by - 1) / by);
+  }
+  __device__ __forceinline__ int of(int x) const {
+    // mul = 2^32 + lo or less: x * mul in 64 bits
+    const unsigned lo = (unsigned)mul, hi = (unsigned)(mul >> 32);
+    const unsigned long long y = (unsigned long long)__umulhi((unsigned)x, lo) + (unsigned long long)(unsigned)x * hi;
+    return (int)(y >> shift);
+  }
+};
+
 struct AttendArgs {
   int B, L, G, Hkv, D, P, S;         // G query heads a key head
   int dt;                            // brisk_dtype of q, keys, values and out
@@ -24,6 +45,7 @@ struct AttendArgs {
   // for the own caches has both) and of the one for the own caches
   int rt_p, rt_o, kt, grid_p, grid_o;
   CacheView q, kp, vp, ko, vo;
+  Divisor by_L, by_G, by_LG;         // L, G and L * G
   const int32_t* own_len;            // [B]
   const int32_t* visible;            // [B, L] or nullptr
   float sl2;                         // scale * log2(e)
@@ -46,7 +68,7 @@ struct AttendArgs {
 // over the own caches, the rows of one sequence. The units stand in one sequence: first the prefix's
 // (by head, row tile, key tile), then the own caches' (by sequence, head, row tile, key tile), and
 // each CTA takes `share` of them, wherever that begins and ends; or the prefix's and the own caches' are
-// two sequences of two kernels (apart). A row tile's keys may so be divided over several CTAs, each of
+// two sequences of two kernels (apart), the own caches' first. A row tile's keys may so be divided over several CTAs, each of
 // which leaves a part; the parts are joined by merge_kernel.
 // Slots: walking through a sequence, (item index + CTA) grows with every (item, CTA) pair, so it
 // numbers the parts. Counts of units fit 31 bits (checked on the host).
@@ -83,8 +105,7 @@ __device__ __forceinline__ int2 units_of(int cta, int share, int all) {
 
 // A CTA's share of one item (a row tile's keys): key tiles [k0, k0 + n).
 struct Frag {
-  int prefix, whole;                 // whole: the rows' result is written with it (own entries: with the
-                                     // prefix's parts, where another kernel has left them)
+  int prefix, whole;                 // whole: no other part for these rows exists
   int h, b, k0, n;
   int row0, rows;                    // rows of the head over the prefix, of the sequence else
   int slot, len;                     // len: entries of the prefix, or in use of the own cache
@@ -148,7 +169,7 @@ struct Walk {
       f.row0 = tile * p.rt_o;
       f.rows = min(p.rt_o, p.LG - f.row0);
       f.slot = b * per + r + c;
-      f.whole = f.n == n && (p.UP == 0 || p.own0 == 0);
+      f.whole = f.n == n && p.UP == 0;
       f.len = len;
     }
     u += f.n;
@@ -164,7 +185,7 @@ __device__ __forceinline__ long long part_at(long long slot, int per, int D, int
 
 // Token (b * L + i) and query head of a fragment's row, and how many keys the row sees.
 __device__ __forceinline__ void row_of(const AttendArgs& a, const Frag& f, int r, int& token, int& head) {
-  const int row = f.row0 + r, t = row / a.G;
+  const int row = f.row0 + r, t = a.by_G.of(row);
   head = f.h * a.G + (row - t * a.G);
   token = f.prefix ? t : f.b * a.L + t;
 }
@@ -215,28 +236,37 @@ __device__ void scan_lengths(const Args& a, int kt, int32_t* cum, int* warp_sum,
   __syncthreads();
 }
 
-// Parts over the prefix that the kernel for the own caches joins itself, where it has all own entries of a
-// row; with more, whose loads would wait for one another, it leaves a part too.
+// Parts of a row's own entries that the prefix's kernel joins itself, where it has all the prefix for the row;
+// with more, whose loads would wait for one another, it leaves a part too.
 constexpr int JOIN_PARTS = 2;
 
-// The parts that the prefix's kernel, or the prefix's units of a common one, leave of row `r` of a head: a
-// run of `n` slots.
-struct PrefixParts {
+// The parts of row `r` of a head, over the prefix or over the own entries: a run of `n` slots.
+struct Parts {
   int n, per;
   const float* sums;                 // column 0 of the first part; the next one is per * D further
   const float2* ml;
-  __device__ PrefixParts(const AttendArgs& a, const Plan& p, int h, int r) {
-    n = 0;
-    per = min(p.rt_p, p.R);
-    sums = nullptr;
-    ml = nullptr;
-    if (p.kP == 0) return;
-    const int pt = r / p.rt_p, first = (h * p.nPT + pt) * p.kP, c0 = first / p.share_p, slot = h * p.nPT + pt + c0;
-    n = (first + p.kP - 1) / p.share_p - c0 + 1;
-    sums = a.part_p + part_at(slot, per, a.D, r - pt * p.rt_p, 0);
-    ml = a.ml_p + (long long)slot * per + (r - pt * p.rt_p);
-  }
 };
+__device__ __forceinline__ Parts prefix_parts(const AttendArgs& a, const Plan& p, int h, int r) {
+  Parts x{0, min(p.rt_p, p.R), nullptr, nullptr};
+  if (p.kP == 0) return x;
+  const int pt = r / p.rt_p, first = (h * p.nPT + pt) * p.kP, c0 = first / p.share_p, slot = h * p.nPT + pt + c0;
+  x.n = (first + p.kP - 1) / p.share_p - c0 + 1;
+  x.sums = a.part_p + part_at(slot, x.per, a.D, r - pt * p.rt_p, 0);
+  x.ml = a.ml_p + (long long)slot * x.per + (r - pt * p.rt_p);
+  return x;
+}
+// (cum as scan_lengths leaves it)
+__device__ __forceinline__ Parts own_parts(const AttendArgs& a, const Plan& p, const int32_t* cum, int h, int r) {
+  Parts x{0, min(p.rt_o, p.LG), nullptr, nullptr};
+  const int b = a.by_LG.of(r), before = cum[b], n = cum[b + 1] - before;
+  if (n == 0) return x;
+  const int ro = r - b * p.LG, lt = ro / p.rt_o, of = h * p.nLT + lt, per = p.Hkv * p.nLT;
+  const int u = p.own0 + per * before + of * n, c0 = u / p.share_o, slot = b * per + of + c0;
+  x.n = (u + n - 1) / p.share_o - c0 + 1;
+  x.sums = a.part_o + part_at(slot, x.per, a.D, ro - lt * p.rt_o, 0);
+  x.ml = a.ml_o + (long long)slot * x.per + (ro - lt * p.rt_o);
+  return x;
+}
 
 // Four elements of a row, as fp32, and back.
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }

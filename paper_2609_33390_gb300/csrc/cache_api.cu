@@ -52,6 +52,9 @@ AttendArgs sizes_of(const brisk_cache_dims* d) {
   AttendArgs a{};
   a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.P = d->P; a.S = d->S;
   a.dt = d->dtype;
+  a.by_L.set(a.L);
+  a.by_G.set(a.G);
+  a.by_LG.set(a.L * a.G);
   divide(&a);
   return a;
 }

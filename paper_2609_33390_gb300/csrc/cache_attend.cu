@@ -60,7 +60,7 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
       if (r < f.rows) {
         int token, head;
         row_of(a, f, r, token, head);
-        const int b = token / a.L, i = token - b * a.L;
+        const int b = a.by_L.of(token), i = token - b * a.L;
         v = load4(static_cast<const T*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head + c);
       }
       store4(sQ + r * CACHE_MAX_D + c, v);
@@ -220,62 +220,60 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
 
 constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D + RT * (KT + 4));
 
-// Joins the parts of the rows whose keys were divided. A warp takes 8 neighbouring rows of a key head,
-// 4 lanes a row, each with every fourth group of four columns: its loads are runs of 128 bytes, a part's
+// Joins the parts of the rows whose keys were divided. A warp takes 4 neighbouring rows of a key head,
+// 8 lanes a row, each with every eighth group of four columns: its loads are runs of 64 bytes, a part's
 // all in flight at once. With few rows the 8 warps of a CTA take the rows' parts in turn (SPLIT) and meet in
 // shared memory: one part after another is a load's latency each (one block of 32 positions over 4096 + 1100
 // entries, 21 parts a row: a warp a row group 54 us).
 constexpr int MERGE_WARPS = 8, MERGE_THREADS = 32 * MERGE_WARPS;
 template <typename T, int SPLIT>
-__global__ void __launch_bounds__(MERGE_THREADS)
+__global__ void __launch_bounds__(MERGE_THREADS, 4)
 merge_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int NG = CACHE_MAX_D / 16;             // groups of four columns of a lane
-  __shared__ __align__(16) float sum_of[SPLIT > 1 ? SPLIT : 1][SPLIT > 1 ? 8 : 1][CACHE_MAX_D + 4];
-  __shared__ float2 ml_of[SPLIT > 1 ? SPLIT : 1][8];
-  wait_for_previous();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cq = lane >> 3, sub = warp % SPLIT;
-  const Plan plan(a, a.cum[a.B]);
-  const int rt_o = a.rt_o, per_o = min(rt_o, plan.LG), D = a.D, Hq = a.Hkv * a.G;
-  const int groups = (plan.R + 7) / 8;             // of a key head
-  const bool joined = a.grid_p > 0;                // (see JOIN_PARTS)
+  constexpr int NG = CACHE_MAX_D / 32;             // groups of four columns of a lane
+  __shared__ __align__(16) float sum_of[SPLIT > 1 ? SPLIT : 1][SPLIT > 1 ? 4 : 1][CACHE_MAX_D + 4];
+  __shared__ float2 ml_of[SPLIT > 1 ? SPLIT : 1][4];
+  extern __shared__ int32_t cum[];                 // [B + 1] key tiles before each sequence
+  __shared__ int warp_sum[MERGE_WARPS], bad;
+  __shared__ Start start;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cq = lane >> 2, sub = warp % SPLIT;
+  // the division of the work, while the kernels before are still running
+  scan_lengths<MERGE_THREADS>(a, a.kt, cum, warp_sum, &bad, &start, [](int) { return -1; });
+  const Plan plan(a, cum[a.B]);
+  const int D = a.D, Hq = a.Hkv * a.G;
+  const int groups = (plan.R + 3) / 4;             // of a key head
+  bool waited = false;
   for (int w0 = (int)blockIdx.x * (MERGE_WARPS / SPLIT); w0 < groups * a.Hkv; w0 += (int)gridDim.x * (MERGE_WARPS / SPLIT)) {
     const int w = w0 + warp / SPLIT;
-    const int h = w / groups, r = (w - h * groups) * 8 + (lane & 7);
-    // the parts over the prefix, then those over the own cache: a run of slots each
-    PrefixParts pre(a, plan, h, r < plan.R ? r : 0);
-    const float* src_o = nullptr;
-    const float2* ml_o = nullptr;
-    int no = 0, token = 0;
-    bool mine = w < groups * a.Hkv && r < plan.R;  // (and not written with the only part)
+    const int h = w / groups, r = (w - h * groups) * 4 + (lane & 3);
+    // the parts over the prefix, then those over the own cache
+    bool mine = w < groups * a.Hkv && r < plan.R;  // (and not written by one of the kernels before)
+    Parts pre{}, own{};
+    int token = 0;
     if (mine) {
-      token = r / a.G;
-      const int b = r / plan.LG, n = a.cum[b + 1] - a.cum[b];
-      if (pre.n == 1 && a.S == 0) mine = false;
-      if (n > 0) {
-        const int ro = r - b * plan.LG, lt = ro / rt_o, of = h * plan.nLT + lt, per = a.Hkv * plan.nLT;
-        const int u = plan.own0 + per * a.cum[b] + of * n, c0 = u / plan.share_o, slot = b * per + of + c0;
-        no = (u + n - 1) / plan.share_o - c0 + 1;
-        src_o = a.part_o + part_at(slot, per_o, D, ro - lt * rt_o, 0);
-        ml_o = a.ml_o + (long long)slot * per_o + (ro - lt * rt_o);
-        if (no == 1 && (pre.n == 0 || (joined && pre.n <= JOIN_PARTS))) mine = false;
-      }
+      token = a.by_G.of(r);
+      pre = prefix_parts(a, plan, h, r);
+      own = own_parts(a, plan, cum, h, r);
+      if (a.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0))
+        mine = false;
     }
+    if (!waited) wait_for_previous();
+    waited = true;
     const bool idle = mine && row_idle(a, token);
-    const int parts = mine && !idle ? pre.n + no : 0;
+    const int parts = mine && !idle ? pre.n + own.n : 0;
     float m = -INFINITY, l = 0.f;
     float4 o[NG];
 #pragma unroll
     for (int k = 0; k < NG; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = sub; i < parts; i += SPLIT) {
       const bool first = i < pre.n;
-      const int per = first ? pre.per : per_o, at = first ? i : i - pre.n;
-      const float2 ml = (first ? pre.ml : ml_o)[(long long)at * per];
-      const float* src = (first ? pre.sums : src_o) + (long long)at * per * D;
+      const int per = first ? pre.per : own.per, at = first ? i : i - pre.n;
+      const float2 ml = (first ? pre.ml : own.ml)[at * per];
+      const float* src = (first ? pre.sums : own.sums) + (long long)at * per * D;
       float4 x[NG];
 #pragma unroll
       for (int k = 0; k < NG; ++k) {               // (columns beyond D: others again, not stored)
-        const int c = 4 * cq + 16 * k;
-        x[k] = load4(src + (long long)(c < D ? c : 0) * per);
+        const int c = 4 * cq + 32 * k;
+        x[k] = load4(src + (c < D ? c : 0) * per);
       }
       const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.f : mn;
       // (a part without a finite score has sums of 0, or NaN, which pass)
@@ -298,8 +296,8 @@ merge_kernel(const __grid_constant__ AttendArgs a) {
       T* to = static_cast<T*>(a.out) + row * D + 4 * cq;
 #pragma unroll
       for (int k = 0; k < NG; ++k)
-        if (4 * cq + 16 * k < D)
-          store4(to + 16 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f)
+        if (4 * cq + 32 * k < D)
+          store4(to + 32 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f)
                                    : make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
       if (a.lse && cq == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
     } else {
@@ -307,24 +305,25 @@ merge_kernel(const __grid_constant__ AttendArgs a) {
       __syncthreads();                             // (the last group's are read)
 #pragma unroll
       for (int k = 0; k < NG; ++k)
-        if (4 * cq + 16 * k < D) store4(&sum_of[warp][lane & 7][4 * cq + 16 * k], o[k]);
-      if (cq == 0) ml_of[warp][lane & 7] = make_float2(m, l);
+        if (4 * cq + 32 * k < D) store4(&sum_of[warp][lane & 3][4 * cq + 32 * k], o[k]);
+      if (cq == 0) ml_of[warp][lane & 3] = make_float2(m, l);
       __syncthreads();
-      const bool row_mine = __shfl_sync(FULL_MASK, (int)mine, warp) != 0;
-      const long long to_row = __shfl_sync(FULL_MASK, row, warp);
+      const int rw = warp & 3;                     // (warps 4.. have no row left)
+      const bool row_mine = __shfl_sync(FULL_MASK, (int)mine, rw) != 0 && warp < 4;
+      const long long to_row = __shfl_sync(FULL_MASK, row, rw);
       if (!row_mine) continue;
       float top = -INFINITY, all = 0.f;
 #pragma unroll
-      for (int j = 0; j < SPLIT; ++j) top = fmaxf(top, ml_of[j][warp].x);
+      for (int j = 0; j < SPLIT; ++j) top = fmaxf(top, ml_of[j][rw].x);
       const float ms = top == -INFINITY ? 0.f : top;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < SPLIT; ++j) {
-        const float2 ml = ml_of[j][warp];
+        const float2 ml = ml_of[j][rw];
         const float wj = ml.x == top ? 1.f : ex2(ml.x - ms);
         all += wj * ml.y;
         if (4 * lane < D) {
-          const float4 x = load4(&sum_of[j][warp][4 * lane]);
+          const float4 x = load4(&sum_of[j][rw][4 * lane]);
           v.x = fmaf(wj, x.x, v.x);
           v.y = fmaf(wj, x.y, v.y);
           v.z = fmaf(wj, x.z, v.z);
@@ -339,6 +338,7 @@ merge_kernel(const __grid_constant__ AttendArgs a) {
       if (a.lse && lane == 0) a.lse[to_row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
     }
   }
+  if (!waited) wait_for_previous();
   if (blockIdx.x == 0 && threadIdx.x < 32) {
     int code = BRISK_OK;                           // the largest: a wait that gave up before a bad length
     for (int c = lane; c < a.grid_p + a.grid_o; c += 32) code = max(code, a.errs[c]);
@@ -357,12 +357,16 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {
-  // a warp a group of 8 rows, or a CTA a group where that leaves SMs without work
-  const long long groups = (long long)((a.B * a.L * a.G + 7) / 8) * a.Hkv;
+  // a warp a group of 4 rows, or a CTA a group where that leaves SMs without work
+  const long long groups = (long long)((a.B * a.L * a.G + 3) / 4) * a.Hkv;
   const bool split = groups <= 4 * CACHE_SMS;
   const long long ctas = split ? groups : (groups + MERGE_WARPS - 1) / MERGE_WARPS;
   const int grid = (int)(ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS);
-  auto run = [&](auto kernel) { return launch_early(kernel, grid, MERGE_THREADS, 0, stream, true, a); };
+  const size_t smem = sizeof(int32_t) * (a.B + 1);
+  auto run = [&](auto kernel) {
+    cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
+    return e != cudaSuccess ? e : launch_early(kernel, grid, MERGE_THREADS, smem, stream, true, a);
+  };
   if (a.dt == BRISK_DT_BF16) return split ? run(merge_kernel<__nv_bfloat16, 8>) : run(merge_kernel<__nv_bfloat16, 1>);
   return split ? run(merge_kernel<float, 8>) : run(merge_kernel<float, 1>);
 }

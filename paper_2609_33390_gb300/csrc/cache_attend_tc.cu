@@ -12,8 +12,8 @@
 // attend_slot_kernel, over the own caches (and over the prefix where all sequences' rows fit a slot): two
 // CTAs an SM, each working through fragments of its own. Bound by the entries' bytes where the caches are
 // long, by what a fragment costs around its tiles where they are short.
-// The CTAs share the units of work evenly (see Plan). Where both kernels run, the second is set up while the
-// first runs and takes over SM by SM.
+// The CTAs share the units of work evenly (see Plan). Where both kernels run, the own caches' is first; the
+// prefix's takes over SM by SM and joins the own entries' parts at the end of its fragments, which are long.
 //
 // The maximum a row subtracts is held back until a score exceeds it by 2^8: P and the sums then stay
 // below 2^8 times their number, and O is seldom rescaled. Rounding P to bf16 costs at most 2^-9 of each
@@ -84,45 +84,49 @@ __device__ __noinline__ void add_odd(const AttendArgs& a, int b, int h, int t0, 
   }
 }
 
-// A slot's row of a thread: token * Hq + head (its complement: padding, -1: none) and the keys it sees.
-struct Row { int id, lim; };
+// A slot's row of a thread: token * Hq + head (its complement: padding, -1: none), the keys it sees, its query.
+struct Row {
+  int id, lim;
+  const __nv_bfloat16* q;
+};
 
-// Row `row0 + r` of a fragment for thread r of a slot, and the slot's queries on their way to `dst`
-// ([DP / 64][128 rows][128 B], swizzled): 4 lanes a row, 64 bytes of it at a time.
-template <int DP>
-__device__ __forceinline__ Row fetch_rows(const AttendArgs& a, const Frag& f, int row, int rows, uint8_t* dst, int warp) {
-  const int lane = threadIdx.x & 31;
-  const __nv_bfloat16* src = nullptr;
-  Row x{-1, f.len};
-  if (row < rows) {
+__device__ __forceinline__ Row find_row(const AttendArgs& a, const Frag& f, int row) {
+  Row x{-1, f.len, nullptr};
+  if (row < f.rows) {
     int token, head;
     row_of(a, f, row, token, head);
-    const int b = token / a.L, i = token - b * a.L;
+    const int b = a.by_L.of(token), i = token - b * a.L;
     x.id = token * (a.Hkv * a.G) + head;
-    src = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head;
+    x.q = static_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head;
     if (a.visible) {
       const int v = a.visible[token];
       if (v < 0) x.id = ~x.id;
       if (!f.prefix) x.lim = max(0, min(x.lim, v));
     }
   }
-  const int np = 2 * ((a.D + 15) / 16);            // 16-byte pieces that the products read
+  return x;
+}
+
+// The queries of a warp's 32 rows on their way to `dst` ([DP / 64][128 rows][128 B], swizzled): 4 lanes a
+// row, 64 bytes of it at a time.
+template <int DP>
+__device__ __forceinline__ void fetch_queries(const Row& x, int D, uint8_t* dst, int warp) {
+  const int lane = threadIdx.x & 31, np = 2 * ((D + 15) / 16);       // 16-byte pieces that the products read
 #pragma unroll 1
   for (int i = 0; i < 32; i += 8) {
     const int in = i + (lane >> 2), at = warp * 32 + in;
-    const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(src), in);
+    const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(x.q), in);
     if (from)
 #pragma unroll
       for (int k = 0; k < DP / 32; ++k) {
         const int c = 4 * k + (lane & 3);
         const uint32_t to = su32(dst + at * 128 + (c >> 3) * PANEL + ((c ^ at) & 7) * 16);
-        if (8 * c < a.D)
+        if (8 * c < D)
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
         else if (c < np)
           asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
       }
   }
-  return x;
 }
 __device__ __forceinline__ void rows_fetched() {
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -195,79 +199,83 @@ __device__ __forceinline__ void row_weights(uint32_t tS, uint32_t tO, int D, int
   tmem_st_wait();
 }
 
-// A row's beginning where the prefix's kernel left few parts of it: their join, as if the slot had gone through
-// the prefix's keys itself. O goes to tO (zeros without parts); complete after tmem_st_wait.
-__device__ __forceinline__ void begin_row(const PrefixParts& pre, bool has, uint32_t tO, int D, float& m, float& l) {
-  float w0 = 0.f, w1 = 0.f;
-  m = -INFINITY;
-  l = 0.f;
-  const bool two = has && pre.n > 1;
-  const float* src1 = pre.sums + (long long)(two ? pre.per : 0) * D;
-  if (has) {
-    const float2 x = pre.ml[0], y = two ? pre.ml[pre.per] : make_float2(-INFINITY, 0.f);
-    m = fmaxf(x.x, y.x);
-    const float ms = m == -INFINITY ? 0.f : m;
-    w0 = x.x == m ? 1.f : ex2(x.x - ms);
-    w1 = !two ? 0.f : (y.x == m ? 1.f : ex2(y.x - ms));
-    l = w0 * x.y + w1 * y.y;
+// The rows' end: their results, or their parts, from O at tO. `part`: column 0 of the row in the slot of
+// parts, nullptr for the result, which (JOIN) the first `others.n` <= 2 parts of other keys then join. Results go through `stage` (2 KB a warp), so that 4 lanes write 64 bytes of a
+// row: a row a lane, every store would touch 32 lines.
+constexpr int STAGE_BYTES = 32 * 64;
+template <bool JOIN>
+__device__ __forceinline__ void store_rows(const AttendArgs& a, uint32_t tO, const Row& x, bool mine, float m, float l,
+                                           float* part, float2* ml, int per, uint8_t* stage, const Parts& others) {
+  const int lane = threadIdx.x & 31, D = a.D;
+  const int row = x.id < 0 ? ~x.id : x.id;
+  float w = 1.f, w0 = 0.f, w1 = 0.f;               // weights of this part and the others
+  const bool one = JOIN && mine && !part && others.n > 0, two = one && others.n > 1;
+  const float* src0 = others.sums;
+  const float* src1 = others.sums + (two ? others.per * D : 0);
+  if (one) {
+    const float2 y = others.ml[0], z = two ? others.ml[others.per] : make_float2(-INFINITY, 0.f);
+    const float top = fmaxf(m, fmaxf(y.x, z.x)), ms = top == -INFINITY ? 0.f : top;
+    w = m == top ? 1.f : ex2(m - ms);
+    w0 = y.x == top ? 1.f : ex2(y.x - ms);
+    w1 = !two ? 0.f : (z.x == top ? 1.f : ex2(z.x - ms));
+    m = top;
+    l = w * l + w0 * y.y + w1 * z.y;
   }
-#pragma unroll 1
-  for (int c = 0; c < D; c += 32) {
-    float4 x[8], y[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const long long at = (long long)min(c + 4 * k, D - 4) * pre.per;
-      x[k] = has ? load4(pre.sums + at) : make_float4(0.f, 0.f, 0.f, 0.f);
-      y[k] = two ? load4(src1 + at) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t v[16];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float4 p = x[4 * h + k], q = y[4 * h + k];
-        v[4 * k] = __float_as_uint(fmaf(w1, q.x, w0 * p.x));
-        v[4 * k + 1] = __float_as_uint(fmaf(w1, q.y, w0 * p.y));
-        v[4 * k + 2] = __float_as_uint(fmaf(w1, q.z, w0 * p.z));
-        v[4 * k + 3] = __float_as_uint(fmaf(w1, q.w, w0 * p.w));
-      }
-      tmem_st16(tO + c + 16 * h, v);
-    }
-  }
-}
-
-// A row's end: its result, or its part, from O at tO. `part`: column 0 of the row in the slot of parts,
-// nullptr for the result.
-__device__ __forceinline__ void store_row(const AttendArgs& a, uint32_t tO, Row x, bool mine, float m, float l,
-                                          float* part, float2* ml, int per) {
-  const long long row = x.id < 0 ? ~x.id : x.id;
   const bool none = l == 0.f || x.id < 0;
   const float inv = none ? 0.f : 1.f / l;
-  const int D = a.D;
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + row * D;
+  const bool direct = mine && !part;
+  const int to_row = direct ? row : -1;
+  const bool any_direct = __any_sync(FULL_MASK, direct);
 #pragma unroll 1
-  for (int c = 0; c < D; c += 16) {
-    float o[16];
-    tmem_ld16(tO + c, o);
+  for (int c = 0; c < D; c += 32) {
+    float o[32];
+    if (JOIN && __any_sync(FULL_MASK, one)) {      // (all loads on their way before the first is used)
+      float4 y[8], z[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int at = min(c + 4 * k, D - 4) * others.per;
+        y[k] = one ? load4(src0 + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+        z[k] = two ? load4(src1 + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      tmem_ld32(tO + c, o);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        o[4 * k] = fmaf(w1, z[k].x, fmaf(w0, y[k].x, w * o[4 * k]));
+        o[4 * k + 1] = fmaf(w1, z[k].y, fmaf(w0, y[k].y, w * o[4 * k + 1]));
+        o[4 * k + 2] = fmaf(w1, z[k].z, fmaf(w0, y[k].z, w * o[4 * k + 2]));
+        o[4 * k + 3] = fmaf(w1, z[k].w, fmaf(w0, y[k].w, w * o[4 * k + 3]));
+      }
+    } else {
+      tmem_ld32(tO + c, o);
+    }
     if (mine && part) {
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        if (c + i < D) store4(part + (long long)(c + i) * per, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
-    } else if (mine) {
-#pragma unroll
-      for (int i = 0; i < 16; i += 8)
-        if (c + i < D) {
-          uint32_t y[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const __nv_bfloat162 h = none ? __floats2bfloat162_rn(0.f, 0.f)
-                                          : __floats2bfloat162_rn(o[i + 2 * k] * inv, o[i + 2 * k + 1] * inv);
-            y[k] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-          *reinterpret_cast<uint4*>(out + c + i) = make_uint4(y[0], y[1], y[2], y[3]);
-        }
+      for (int i = 0; i < 32; i += 4)
+        if (c + i < D) store4(part + (c + i) * per, make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]));
     }
     __syncwarp();
+    if (any_direct) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                // 16-byte pieces of the row, swizzled over its 64 bytes
+        uint32_t y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const __nv_bfloat162 h = none ? __floats2bfloat162_rn(0.f, 0.f)
+                                        : __floats2bfloat162_rn(o[8 * i + 2 * k] * inv, o[8 * i + 2 * k + 1] * inv);
+          y[k] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ (lane >> 1)) & 3) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        const int r = i + (lane >> 2), to = __shfl_sync(FULL_MASK, to_row, r), q = lane & 3;
+        const uint4 y = *reinterpret_cast<const uint4*>(stage + r * 64 + ((q ^ (r >> 1)) & 3) * 16);
+        if (to >= 0 && c + 8 * q < D)
+          *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + (long long)to * D + c + 8 * q) = y;
+      }
+      __syncwarp();
+    }
   }
   if (!mine) return;
   if (part) *ml = make_float2(m, l);
@@ -304,7 +312,7 @@ template <int DP>
 struct PairShape {
   static constexpr int TILE = KT * DP * 2;         // bytes of a tile of 128 rows
   static constexpr int STAGES = DP == 128 ? 4 : 8;
-  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE;
+  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE + 8 * STAGE_BYTES;
 };
 
 template <int DP>
@@ -313,7 +321,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   constexpr int STAGES = PairShape<DP>::STAGES, TILE = PairShape<DP>::TILE;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = sQ + 2 * TILE;
+  uint8_t *ring = sQ + 2 * TILE, *stage = ring + STAGES * TILE;
   __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2][2], o_full[2], q_full[2], turn[2], done;
   __shared__ uint32_t tmem_slot;
   __shared__ int aborted;
@@ -446,7 +454,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       f.row0 = (item - f.h * nPT) * PAIR_ROWS;
       f.rows = min(PAIR_ROWS, R - f.row0);
       f.slot = item + blockIdx.x;
-      f.whole = f.n == kP && a.S == 0;
+      f.whole = 0;                                 // (see the end of a fragment)
       f.len = a.P;
     };
     auto fetched = [&]() {
@@ -456,10 +464,11 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       if (lane == 0) mbar_arrive(&q_full[s]);
     };
     Frag f;
-    Row x{-1, 0};
+    Row x{-1, 0, nullptr};
     if (u < range.y) {
       frag_at(u, f);
-      x = fetch_rows<DP>(a, f, s * SLOT + r, f.rows, sQ + s * TILE, w);
+      x = find_row(a, f, s * SLOT + r);
+      fetch_queries<DP>(x, a.D, sQ + s * TILE, w);
       fetched();
     }
     while (u < range.y) {
@@ -485,7 +494,8 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       u += f.n;
       if (u < range.y) {
         frag_at(u, f);
-        x = fetch_rows<DP>(a, f, s * SLOT + r, f.rows, sQ + s * TILE, w);
+        x = find_row(a, f, s * SLOT + r);
+        fetch_queries<DP>(x, a.D, sQ + s * TILE, w);
       }
       off = wait(&o_full[s], nf++);
       if (off) break;
@@ -493,8 +503,16 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       if (u < range.y) fetched();
       if (live) {
         const int per = min(PAIR_ROWS, R);
-        store_row(a, tO, y, mine, m, l, g.whole ? nullptr : a.part_p + part_at(g.slot, per, a.D, s * SLOT + r, 0),
-                  a.ml_p + (long long)g.slot * per + s * SLOT + r, per);
+        Parts own{};
+        bool part = g.n < kP;
+        if (!part) {                               // all of the prefix: the own entries' parts join here
+          wait_for_previous();
+          const Plan plan(a, a.cum[a.B]);
+          if (mine) own = own_parts(a, plan, a.cum, g.h, g.row0 + s * SLOT + r);
+          part = own.n > JOIN_PARTS;
+        }
+        store_rows<true>(a, tO, y, mine, m, l, part ? a.part_p + part_at(g.slot, per, a.D, s * SLOT + r, 0) : nullptr,
+                         a.ml_p + (long long)g.slot * per + s * SLOT + r, per, stage + warp * STAGE_BYTES, own);
       }
       tc_fence_before();
     }
@@ -503,6 +521,8 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, 512);
   if (tid == 0) a.errs[blockIdx.x] = aborted ? BRISK_ERR_TIMEOUT : BRISK_OK;
+  // the join of what is left reads the other kernel's parts, and waits for this one alone
+  wait_for_previous();
 }
 
 // ---------------------------------------------------------------- a slot a CTA
@@ -511,7 +531,7 @@ template <int DP>
 struct SlotShape {
   static constexpr int TILE = KT * DP * 2;
   static constexpr int STAGES = DP == 128 ? 2 : 4; // key and value tiles in turn
-  static constexpr int SMEM = 1024 + (1 + STAGES) * TILE;
+  static constexpr int SMEM = 1024 + (1 + STAGES) * TILE + 4 * STAGE_BYTES;
 };
 
 template <int DP>
@@ -520,9 +540,9 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   constexpr int STAGES = SlotShape<DP>::STAGES, TILE = SlotShape<DP>::TILE;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = sQ + TILE;
-  __shared__ uint64_t full[STAGES], empty[STAGES], s_full, p_ready[2], o_full, q_full, info_full[2], info_empty[2], done;
-  __shared__ Frag info[2];
+  uint8_t *ring = sQ + TILE, *stage = ring + STAGES * TILE;
+  __shared__ uint64_t full[STAGES], empty[STAGES], s_full, p_ready[2], o_full, q_full, info_full[4], info_empty[4], done;
+  __shared__ Frag info[4];
   __shared__ uint32_t tmem_slot;
   __shared__ Start start;
   __shared__ int aborted, bad, warp_sum[SLOT_THREADS / 32], low_of[2][4], odd_of[2][4];
@@ -536,6 +556,8 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&p_ready[s], 4);                   // the slot's warps, for either half of the keys
+    }
+    for (int s = 0; s < 4; ++s) {
       mbar_init(&info_full[s], 1);
       mbar_init(&info_empty[s], 4);
     }
@@ -569,19 +591,25 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   bool off = false;
 
   if (warp == 4) {
-    // copies, key and value tiles in turn, and the fragments for the others, two ahead of the slot at most
+    // copies, key and value tiles in turn, and the fragments for the others: each a fragment before its tiles
     Walk walk(a, plan, blockIdx.x, start);
-    Frag f;
+    Frag f, ahead;
     unsigned cur = 0;
-    for (; !off && walk.next(a, plan, f); ++nf) {
-      const int fs = nf & 1;
-      off = nf >= 2 && wait(&info_empty[fs], (nf >> 1) - 1);
-      if (off) break;
-      if (lane == 0) {
-        info[fs] = f;
-        mbar_arrive(&info_full[fs]);
+    bool more = walk.next(a, plan, ahead);
+    auto publish = [&](int k) {
+      off = k >= 4 && wait(&info_empty[k & 3], (k >> 2) - 1);
+      if (!off && lane == 0) {
+        info[k & 3] = ahead;
+        mbar_arrive(&info_full[k & 3]);
       }
       __syncwarp();
+    };
+    if (more) publish(0);
+    for (; !off && more; ++nf) {
+      f = ahead;
+      more = walk.next(a, plan, ahead);
+      if (more) publish(nf + 1);
+      if (off) break;
       const CUtensorMap* mk = f.prefix ? &maps.k2 : &maps.k;
       const CUtensorMap* mv = f.prefix ? &maps.v2 : &maps.v;
       for (int i = 0; i < 2 * f.n; ++i, ++cur) {
@@ -601,11 +629,10 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     const uint32_t tS = tmem, tO = tmem + 128;
     unsigned cur = 0;
     while (unit < units && !off) {
-      const int fs = nf & 1;
+      const int fs = nf & 3;
       off = wait(&q_full, nf++);                   // (info_full came before it)
       if (off) break;
       const int n = info[fs].n, k0 = info[fs].k0, len = info[fs].len;
-      const bool resume = info[fs].whole && a.grid_p > 0;
       for (int j = 0; j < n && !off; ++j, ++unit) {
         const unsigned sk = cur % STAGES, sv = (cur + 1) % STAGES;
         off = wait(&full[sk], cur / STAGES);
@@ -622,7 +649,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         off = wait(&full[sv], (cur + 1) / STAGES) || wait(&p_ready[0], unit);
         if (off) break;
         tc_fence_after();
-        if (elect_one()) issue_values<0>(tO, tS, v, steps, id_o, resume || j > 0);
+        if (elect_one()) issue_values<0>(tO, tS, v, steps, id_o, j > 0);
         __syncwarp();
         off = wait(&p_ready[1], unit);
         if (off) break;
@@ -641,94 +668,96 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   } else {
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     const uint32_t tS = tmem + lanes, tO = tmem + 128 + lanes;
-    Row x{-1, 0};
-    // the rows and queries of fragment number k, once the scores that read the last one's are there
-    auto fetch = [&](int k) {
-      off = wait(&info_full[k & 1], k >> 1);
-      if (!off) x = fetch_rows<DP>(a, info[k & 1], tid, info[k & 1].rows, sQ, warp);
-    };
-    auto fetched = [&](int k) {
-      const int low = __reduce_min_sync(FULL_MASK, x.id >= 0 ? x.lim : info[k & 1].len);
-      if (lane == 0) {
-        low_of[k & 1][warp] = low;
-        odd_of[k & 1][warp] = 0;
+    // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
+    // this one's are there), this one's end. The first turn has no fragment yet, the last no next one.
+    Row y{-1, 0, nullptr};
+    Frag f{};
+    bool have = false;
+    int u = 0;                                     // tiles up to the end of this fragment
+    for (;; ++nf) {                                // this fragment is number nf - 1
+      const bool next = u < units;
+      Row x{-1, 0, nullptr};
+      if (next) {
+        off = wait(&info_full[nf & 3], nf >> 2);
+        if (off) break;
+        x = find_row(a, info[nf & 3], tid);
       }
-      rows_fetched();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_full);
-    };
-    if (units > 0) {
-      fetch(0);
-      if (!off) fetched(0);
-    }
-    while (unit < units && !off) {
-      const int fs = nf & 1;
-      off = wait(&q_full, nf);
-      if (off) break;
-      const Frag f = info[fs];
-      const Row y = x;
-      const bool mine = tid < f.rows, live = __any_sync(FULL_MASK, mine);
-      int low = f.len;                             // entries from here on are hidden from some row
-#pragma unroll
-      for (int w = 0; w < 4; ++w) low = min(low, low_of[fs][w]);
+      const int fs = (nf - 1) & 1;
+      const bool mine = have && tid < f.rows, live = __any_sync(FULL_MASK, mine);
       float m = -INFINITY, l = 0.f;
-      // all own entries of the rows, and another kernel had the prefix: go on from there
-      const bool resume = f.whole && a.grid_p > 0;
-      bool joined = false;
-      if (resume && live) {
-        const PrefixParts pre(a, plan, f.h, mine ? f.b * plan.LG + f.row0 + tid : 0);
-        joined = mine && pre.n <= JOIN_PARTS;
-        wait_for_previous();
-        begin_row(pre, joined, tO, a.D, m, l);
+      int low = f.len;                             // entries from here on are hidden from some row
+      if (have) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) low = min(low, low_of[fs][w]);
+        auto ready = [&](int half) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_ready[half]);
+        };
+        for (int j = 0; j < f.n; ++j, ++unit) {
+          const int t0 = (f.k0 + j) * KT, end = min(f.len - t0, KT);   // entries in use of the tile
+          // values that some row does not see, and those behind the last entry that the last step reads
+          const int v0 = max(low - t0, 0), v1 = min((end + 15) & ~15, KT);
+          const bool clean = !f.prefix && v0 < v1;   // (behind the prefix's last entry there are zeros)
+          off = wait(&s_full, unit);
+          if (off) break;
+          tc_fence_after();
+          if (live)
+            row_weights(tS, tO, a.D, mine ? y.lim - t0 : KT, a.sl2, j == 0, m, l,
+                        [&]() { if (!clean) ready(0); });
+          if (clean) {
+            const unsigned pl = 2 * unit + 1, st = pl % STAGES;
+            off = wait(&full[st], pl / STAGES);
+            if (off) break;
+            const bool odd = clean_values<DP>(ring + st * TILE, v0, v1, end, tid);
+            if (__any_sync(FULL_MASK, odd) && lane == 0) odd_of[fs][warp] = 1;
+          }
+          if (clean || !live) ready(0);
+          ready(1);
+        }
+        if (off) break;
       }
-      auto ready = [&](int half) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_ready[half]);
-      };
-      for (int j = 0; j < f.n; ++j, ++unit) {
-        const int t0 = (f.k0 + j) * KT, end = min(f.len - t0, KT);   // entries in use of the tile
-        // values that some row does not see, and those behind the last entry that the last step reads
-        const int v0 = max(low - t0, 0), v1 = min((end + 15) & ~15, KT);
-        const bool clean = !f.prefix && v0 < v1;   // (behind the prefix's last entry there are zeros)
-        off = wait(&s_full, unit);
+      if (next) fetch_queries<DP>(x, a.D, sQ, warp);
+      if (have) {
+        off = wait(&o_full, nf - 1);
         if (off) break;
         tc_fence_after();
-        if (live)
-          row_weights(tS, tO, a.D, mine ? y.lim - t0 : KT, a.sl2, j == 0 && !resume, m, l, [&]() { if (!clean) ready(0); });
-        if (clean) {
-          const unsigned pl = 2 * unit + 1, st = pl % STAGES;
-          off = wait(&full[st], pl / STAGES);
-          if (off) break;
-          const bool odd = clean_values<DP>(ring + st * TILE, v0, v1, end, tid);
-          if (__any_sync(FULL_MASK, odd) && lane == 0) odd_of[fs][warp] = 1;
+      }
+      if (next) {
+        const int low_next = __reduce_min_sync(FULL_MASK, x.id >= 0 ? x.lim : info[nf & 3].len);
+        if (lane == 0) {
+          low_of[nf & 1][warp] = low_next;
+          odd_of[nf & 1][warp] = 0;
         }
-        if (clean || !live) ready(0);
-        ready(1);
+        rows_fetched();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full);
       }
-      if (off) break;
-      const bool next = unit < units;
-      if (next) fetch(nf + 1);
-      if (off) break;
-      off = wait(&o_full, nf);
-      if (off) break;
-      tc_fence_after();
-      if (next) fetched(nf + 1);
-      if (live) {
-        const int per = min(SLOT, f.prefix ? plan.R : plan.LG);
-        float* part = f.whole && (!resume || joined) ? nullptr
-                                                     : (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, a.D, tid, 0);
-        store_row(a, tO, y, mine, m, l, part, (f.prefix ? a.ml_p : a.ml_o) + (long long)f.slot * per + tid, per);
-        // (the warps' words of this fragment were written before the products that o_full tells of)
-        if (!f.prefix && low < f.len && (odd_of[fs][0] | odd_of[fs][1] | odd_of[fs][2] | odd_of[fs][3]) && mine && y.id >= 0)
-          add_odd(a, f.b, f.h, max(low, f.k0 * KT), min(y.lim, (f.k0 + f.n) * KT), part, per,
-                  static_cast<__nv_bfloat16*>(a.out) + (long long)y.id * a.D);
+      if (have) {
+        if (live) {
+          const int per = min(SLOT, f.prefix ? plan.R : plan.LG);
+          float* part = f.whole ? nullptr : (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, a.D, tid, 0);
+          store_rows<false>(a, tO, y, mine, m, l, part, (f.prefix ? a.ml_p : a.ml_o) + (long long)f.slot * per + tid, per,
+                            stage + warp * STAGE_BYTES, Parts{});
+          __syncwarp();
+          // (the warps' words of this fragment were written before the products that o_full tells of, and other
+          // lanes may have stored this row)
+          if (!f.prefix && low < f.len && (odd_of[fs][0] | odd_of[fs][1] | odd_of[fs][2] | odd_of[fs][3]) && mine && y.id >= 0)
+            add_odd(a, f.b, f.h, max(low, f.k0 * KT), min(y.lim, (f.k0 + f.n) * KT), part, per,
+                    static_cast<__nv_bfloat16*>(a.out) + (long long)y.id * a.D);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&info_empty[(nf - 1) & 3]);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&info_empty[fs]);
-      ++nf;
+      if (!next) break;
+      off = wait(&q_full, nf);
+      if (off) break;
+      f = info[nf & 3];
+      y = x;
+      have = true;
+      u += f.n;
     }
   }
   tc_fence_before();
@@ -737,8 +766,6 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   if (tid == 0)
     a.errs[a.grid_p + blockIdx.x] =
         aborted ? BRISK_ERR_TIMEOUT : (bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK);
-  // the join reads the prefix kernel's parts, and waits for this kernel alone
-  wait_for_previous();
 }
 
 }  // namespace
@@ -774,14 +801,13 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   auto slot = a.D > 64 ? attend_slot_kernel<128> : attend_slot_kernel<64>;
   const size_t pair_smem = a.D > 64 ? PairShape<128>::SMEM : PairShape<64>::SMEM;
   const size_t slot_smem = a.D > 64 ? SlotShape<128>::SMEM : SlotShape<64>::SMEM;
-  cudaError_t e = cudaSuccess;
-  if (a.grid_p > 0) {
+  cudaError_t e = set_up_kernel(slot, CARVEOUT_FULL_KB, slot_smem);
+  if (e == cudaSuccess) e = launch_early(slot, a.grid_o, SLOT_THREADS, slot_smem, stream, false, maps, a);
+  if (e == cudaSuccess && a.grid_p > 0) {
     const AttendMaps first{kp, vp, kp, vp};
     e = set_up_kernel(pair, CARVEOUT_FULL_KB, pair_smem);
-    if (e == cudaSuccess) e = launch_early(pair, a.grid_p, PAIR_THREADS, pair_smem, stream, false, first, a);
+    if (e == cudaSuccess) e = launch_early(pair, a.grid_p, PAIR_THREADS, pair_smem, stream, true, first, a);
   }
-  if (e == cudaSuccess) e = set_up_kernel(slot, CARVEOUT_FULL_KB, slot_smem);
-  if (e == cudaSuccess) e = launch_early(slot, a.grid_o, SLOT_THREADS, slot_smem, stream, a.grid_p > 0, maps, a);
   return e;
 }
 
