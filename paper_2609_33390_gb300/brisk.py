@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Dict, Optional
 
@@ -103,15 +104,11 @@ _SIGS = [
      [ctypes.POINTER(Dims), _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
     ("brisk_cache_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(CacheDims)]),
     ("brisk_prefix_attend", ctypes.c_int,
-     [ctypes.POINTER(CacheDims)] + [ctypes.POINTER(View)] * 5 +
-     [_vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+     [_vp] * 8 + [ctypes.c_float, _vp, _vp, _vp, _vp]),
     ("brisk_cache_weights", ctypes.c_int,
-     [ctypes.POINTER(CacheDims), ctypes.POINTER(View), _vp, ctypes.POINTER(View), _vp, _vp,
-      ctypes.c_float, ctypes.c_float, _vp, _vp, _vp, _vp]),
+     [_vp] * 6 + [ctypes.c_float, ctypes.c_float, _vp, _vp, _vp, _vp]),
     ("brisk_cache_evict", ctypes.c_int,
-     [ctypes.POINTER(CacheDims), ctypes.POINTER(View), ctypes.POINTER(View), _vp, _vp,
-      ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(View), ctypes.POINTER(View), _vp, _vp, _vp,
-      _vp, _vp]),
+     [_vp] * 5 + [ctypes.c_int32, ctypes.c_int32] + [_vp] * 7),
 ]
 
 
@@ -427,6 +424,9 @@ def tpf_isd(N: int, r: float) -> float:
 
 # ---------------------------------------------------------------- context cache
 
+_PACK2, _PACK4, _PACK5 = (struct.Struct(f"{4 * n}q").pack_into for n in (2, 4, 5))   # n Views
+_NONE = (0, 0, 0, 0)
+
 class PrefixAttention:
     """Attention of a batch's blocks over a shared prefix and the sequences' own caches, the weight
     it gave each own entry, and the eviction by that weight, for one problem size.
@@ -447,9 +447,17 @@ class PrefixAttention:
             raise BriskError(ERR_INVALID_ARG, "dims")
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=self.device)
         self.scale = D ** -0.5
-        self._d = ctypes.byref(self.dims)
+        self._d = ctypes.addressof(self.dims)
         self._ws = self.workspace.data_ptr()
+        # the views of a call's strided tensors, written anew by every call
+        self._views = ctypes.create_string_buffer(5 * ctypes.sizeof(View))
+        at = ctypes.addressof(self._views)
+        self._at = [at + i * ctypes.sizeof(View) for i in range(5)]
+        self._shape_q, self._shape_pre, self._shape_own = (B, L, Hq, D), (P, Hkv, D), (B, S, Hkv, D)
+        self._shape_lse, self._shape_acc, self._shape_b, self._shape_vis = (B, L, Hq), (B, Hkv, S), (B,), (B, L)
 
+    # Marshalling is most of a small call, so a tensor's checks are few comparisons, and the views of a call
+    # are packed at once.
     def _view(self, t, shape, what):
         """The tensor's address and strides; None for one that a size of zero leaves out."""
         if t is None:
@@ -458,12 +466,12 @@ class PrefixAttention:
             raise ValueError(f"{what} is missing")
         if t.shape != shape or t.dtype != self.dtype:
             raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {self.dtype}")
-        st = t.stride()
         if not t.is_cuda:
             raise ValueError(f"{what} is not on the GPU")
+        st = t.stride()
         if st[-1] != 1:
             raise ValueError(f"{what}: the last dimension must be contiguous")
-        return ctypes.byref(View(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2]))
+        return (t.data_ptr(), *st[:3]) if len(st) == 4 else (t.data_ptr(), 0, st[0], st[1])
 
     @staticmethod
     def _plain(t, shape, dtype, what):
@@ -481,20 +489,22 @@ class PrefixAttention:
         [P, Hkv, D] and the entries of k/v_own [B, S, Hkv, D] that own_len [B] and visible [B, L]
         (int32; see brisk_prefix_attend) let them see. scale: D^-1/2 unless given. ``out``: a dict
         of tensors to write to instead of new ones."""
-        B, L, Hq, Hkv, D, P, S = self.B, self.L, self.Hq, self.Hkv, self.D, self.P, self.S
+        pre, own, view, plain, at = self._shape_pre, self._shape_own, self._view, self._plain, self._at
         if out is None:
-            out = {"out": torch.empty((B, L, Hq, D), dtype=self.dtype, device=self.device),
-                   "lse": torch.empty((B, L, Hq), dtype=torch.float32, device=self.device)}
-        pre, own = (P, Hkv, D), (B, S, Hkv, D)
-        _check(lib().brisk_prefix_attend(
-            self._d, self._view(q, (B, L, Hq, D), "q"), self._view(k_prefix, pre, "k_prefix"),
-            self._view(v_prefix, pre, "v_prefix"), self._view(k_own, own, "k_own"),
-            self._view(v_own, own, "v_own"), self._plain(own_len, (B,), torch.int32, "own_len"),
-            self._plain(visible, (B, L), torch.int32, "visible"),
-            self.scale if scale is None else float(scale),
-            self._plain(out["out"], (B, L, Hq, D), self.dtype, "out"),
-            self._plain(out["lse"], (B, L, Hq), torch.float32, "lse"), self._ws,
-            _stream(stream)), "prefix_attend")
+            out = {"out": torch.empty(self._shape_q, dtype=self.dtype, device=self.device),
+                   "lse": torch.empty(self._shape_lse, dtype=torch.float32, device=self.device)}
+        _PACK5(self._views, 0, *view(q, self._shape_q, "q"), *(view(k_prefix, pre, "k_prefix") or _NONE),
+               *(view(v_prefix, pre, "v_prefix") or _NONE), *(view(k_own, own, "k_own") or _NONE),
+               *(view(v_own, own, "v_own") or _NONE))
+        s = lib().brisk_prefix_attend(
+            self._d, at[0], at[1], at[2], at[3], at[4],
+            plain(own_len, self._shape_b, torch.int32, "own_len"),
+            plain(visible, self._shape_vis, torch.int32, "visible"),
+            self.scale if scale is None else scale,
+            plain(out["out"], self._shape_q, self.dtype, "out"),
+            plain(out["lse"], self._shape_lse, torch.float32, "lse"), self._ws, _stream(stream))
+        if s:
+            raise BriskError(s, "prefix_attend")
         return out
 
     def weights(self, q, lse, k_own, own_len, acc=None, decay=1.0, visible=None, scale=None,
@@ -502,17 +512,19 @@ class PrefixAttention:
         """decay * acc plus the attention weight every own entry got from the queries whose
         log-sums ``lse`` attend() left: [B, Hkv, S] fp32, in ``out`` (which may be ``acc``) or a
         new tensor. acc None: zeros."""
-        B, L, Hq, Hkv, D, S = self.B, self.L, self.Hq, self.Hkv, self.D, self.S
+        plain, at, f32, i32 = self._plain, self._at, torch.float32, torch.int32
         if out is None:
-            out = torch.empty((B, Hkv, S), dtype=torch.float32, device=self.device)
-        f32, i32 = torch.float32, torch.int32
-        _check(lib().brisk_cache_weights(
-            self._d, self._view(q, (B, L, Hq, D), "q"), self._plain(lse, (B, L, Hq), f32, "lse"),
-            self._view(k_own, (B, S, Hkv, D), "k_own"), self._plain(own_len, (B,), i32, "own_len"),
-            self._plain(visible, (B, L), i32, "visible"),
-            self.scale if scale is None else float(scale), float(decay),
-            self._plain(acc, (B, Hkv, S), f32, "acc"), self._plain(out, (B, Hkv, S), f32, "out"),
-            self._ws, _stream(stream)), "cache_weights")
+            out = torch.empty(self._shape_acc, dtype=f32, device=self.device)
+        _PACK2(self._views, 0, *self._view(q, self._shape_q, "q"),
+               *(self._view(k_own, self._shape_own, "k_own") or _NONE))
+        s = lib().brisk_cache_weights(
+            self._d, at[0], plain(lse, self._shape_lse, f32, "lse"), at[1],
+            plain(own_len, self._shape_b, i32, "own_len"),
+            plain(visible, self._shape_vis, i32, "visible"), self.scale if scale is None else scale,
+            decay, plain(acc, self._shape_acc, f32, "acc"), plain(out, self._shape_acc, f32, "out"),
+            self._ws, _stream(stream))
+        if s:
+            raise BriskError(s, "cache_weights")
         return out
 
     def alloc_evicted(self, keep, room=None):
@@ -529,21 +541,23 @@ class PrefixAttention:
         """Moves the ``recent`` newest entries and those of largest ``acc`` [B, Hkv, S], ``keep`` in
         all, to the caches of ``out`` (see alloc_evicted and brisk_cache_evict): between two layers,
         one spare pair of caches serves them all in turn."""
-        B, Hkv, D, S = self.B, self.Hkv, self.D, self.S
         if out is None:
             out = self.alloc_evicted(keep)
-        room, f32, i32 = out["k"].shape[1], torch.float32, torch.int32
+        plain, view, at, f32, i32 = self._plain, self._view, self._at, torch.float32, torch.int32
+        k_to, B, Hkv = out["k"], self.B, self.Hkv
+        room = k_to.shape[1]
         if room < keep:
             raise ValueError(f"the targets hold {room} entries, keep is {keep}")
-        own, to = (B, S, Hkv, D), (B, room, Hkv, D)
-        _check(lib().brisk_cache_evict(
-            self._d, self._view(k_own, own, "k_own"), self._view(v_own, own, "v_own"),
-            self._plain(acc, (B, Hkv, S), f32, "acc"), self._plain(own_len, (B,), i32, "own_len"),
-            int(keep), int(recent), self._view(out["k"], to, "k"), self._view(out["v"], to, "v"),
-            self._plain(out["acc"], (B, Hkv, keep), f32, "out acc"),
-            self._plain(out["own_len"], (B,), i32, "out own_len"),
-            self._plain(out["kept"], (B, Hkv, keep), i32, "kept"), self._ws,
-            _stream(stream)), "cache_evict")
+        own, to, kept = self._shape_own, (B, room, Hkv, self.D), (B, Hkv, keep)
+        _PACK4(self._views, 0, *(view(k_own, own, "k_own") or _NONE), *(view(v_own, own, "v_own") or _NONE),
+               *view(k_to, to, "k"), *view(out["v"], to, "v"))
+        s = lib().brisk_cache_evict(
+            self._d, at[0], at[1], plain(acc, self._shape_acc, f32, "acc"),
+            plain(own_len, self._shape_b, i32, "own_len"), keep, recent, at[2], at[3],
+            plain(out["acc"], kept, f32, "out acc"), plain(out["own_len"], self._shape_b, i32, "out own_len"),
+            plain(out["kept"], kept, i32, "kept"), self._ws, _stream(stream))
+        if s:
+            raise BriskError(s, "cache_evict")
         return out
 
     def device_status(self, clear=True, stream=None) -> int:

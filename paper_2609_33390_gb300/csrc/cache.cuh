@@ -24,11 +24,11 @@ struct CacheView {   // element (s, t, h, :) at p + s*seq + t*tok + h*head, stri
 struct Divisor {
   unsigned long long mul;   // up to 2^33
   int d, shift;
-  void set(int by) {
+  __host__ __device__ void set(int by) {
     d = by;
     shift = 0;
     while ((1LL << shift) < by) ++shift;
-    mul = (unsigned long long)((((unsigned __int128)1 << (32 + shift)) + by - 1) / by);
+    mul = ((1ull << (32 + shift)) - 1) / by + 1;
   }
   __device__ __forceinline__ int of(int x) const {
     // mul = 2^32 + lo or less: x * mul in 64 bits
@@ -45,7 +45,7 @@ struct AttendArgs {
   // for the own caches has both) and of the one for the own caches
   int rt_p, rt_o, kt, grid_p, grid_o;
   CacheView q, kp, vp, ko, vo;
-  Divisor by_L, by_G, by_LG;         // L, G and L * G
+  Divisor by_L, by_G, by_LG, by_R4;  // L, G, L * G, and the groups of 4 rows of a key head
   const int32_t* own_len;            // [B]
   const int32_t* visible;            // [B, L] or nullptr
   float sl2;                         // scale * log2(e)
@@ -78,6 +78,7 @@ struct Plan {
   int R, UP, UO;                     // rows a key head; units of the prefix and of the own caches
   int own0;                          // number of the own caches' first unit
   int share_p, share_o;              // units a CTA
+  int log_p, log_o;                  // rt_p and rt_o as powers of two, where they are
 
   __device__ Plan(int b, int lg, int hkv, int p, int rtp, int rto, int kt_, int own_tiles, int grid_p, int grid_o) {
     B = b; LG = lg; Hkv = hkv; rt_p = rtp; rt_o = rto; kt = kt_;
@@ -90,6 +91,8 @@ struct Plan {
     const bool apart = grid_p > 0;
     own0 = apart ? 0 : UP;
     share_o = max(1, (int)(((unsigned)own0 + UO + grid_o - 1) / grid_o));
+    log_p = 31 - __clz(rt_p);
+    log_o = 31 - __clz(rt_o);
     share_p = apart ? max(1, (int)(((unsigned)UP + grid_p - 1) / grid_p)) : share_o;
   }
   __device__ Plan(const AttendArgs& a, int own_tiles)
@@ -246,25 +249,27 @@ struct Parts {
   const float* sums;                 // column 0 of the first part; the next one is per * D further
   const float2* ml;
 };
-__device__ __forceinline__ Parts prefix_parts(const AttendArgs& a, const Plan& p, int h, int r) {
+// (by_share_p, by_share_o: the plan's)
+__device__ __forceinline__ Parts prefix_parts(const AttendArgs& a, const Plan& p, const Divisor& by_share_p, int h, int r) {
   Parts x{0, min(p.rt_p, p.R), nullptr, nullptr};
   if (p.kP == 0) return x;
-  const int pt = r / p.rt_p, first = (h * p.nPT + pt) * p.kP, c0 = first / p.share_p, slot = h * p.nPT + pt + c0;
-  x.n = (first + p.kP - 1) / p.share_p - c0 + 1;
-  x.sums = a.part_p + part_at(slot, x.per, a.D, r - pt * p.rt_p, 0);
-  x.ml = a.ml_p + (long long)slot * x.per + (r - pt * p.rt_p);
+  const int pt = r >> p.log_p, first = (h * p.nPT + pt) * p.kP, c0 = by_share_p.of(first), slot = h * p.nPT + pt + c0;
+  x.n = by_share_p.of(first + p.kP - 1) - c0 + 1;
+  x.sums = a.part_p + part_at(slot, x.per, a.D, r - (pt << p.log_p), 0);
+  x.ml = a.ml_p + (long long)slot * x.per + (r - (pt << p.log_p));
   return x;
 }
 // (cum as scan_lengths leaves it)
-__device__ __forceinline__ Parts own_parts(const AttendArgs& a, const Plan& p, const int32_t* cum, int h, int r) {
+__device__ __forceinline__ Parts own_parts(const AttendArgs& a, const Plan& p, const Divisor& by_share_o, const int32_t* cum,
+                                           int h, int r) {
   Parts x{0, min(p.rt_o, p.LG), nullptr, nullptr};
   const int b = a.by_LG.of(r), before = cum[b], n = cum[b + 1] - before;
   if (n == 0) return x;
-  const int ro = r - b * p.LG, lt = ro / p.rt_o, of = h * p.nLT + lt, per = p.Hkv * p.nLT;
-  const int u = p.own0 + per * before + of * n, c0 = u / p.share_o, slot = b * per + of + c0;
-  x.n = (u + n - 1) / p.share_o - c0 + 1;
-  x.sums = a.part_o + part_at(slot, x.per, a.D, ro - lt * p.rt_o, 0);
-  x.ml = a.ml_o + (long long)slot * x.per + (ro - lt * p.rt_o);
+  const int ro = r - b * p.LG, lt = ro >> p.log_o, of = h * p.nLT + lt, per = p.Hkv * p.nLT;
+  const int u = p.own0 + per * before + of * n, c0 = by_share_o.of(u), slot = b * per + of + c0;
+  x.n = by_share_o.of(u + n - 1) - c0 + 1;
+  x.sums = a.part_o + part_at(slot, x.per, a.D, ro - (lt << p.log_o), 0);
+  x.ml = a.ml_o + (long long)slot * x.per + (ro - (lt << p.log_o));
   return x;
 }
 

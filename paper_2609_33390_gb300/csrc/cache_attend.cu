@@ -227,7 +227,7 @@ constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * 
 // entries, 21 parts a row: a warp a row group 54 us).
 constexpr int MERGE_WARPS = 8, MERGE_THREADS = 32 * MERGE_WARPS;
 template <typename T, int SPLIT>
-__global__ void __launch_bounds__(MERGE_THREADS, 4)
+__global__ void __launch_bounds__(MERGE_THREADS, 3)
 merge_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int NG = CACHE_MAX_D / 32;             // groups of four columns of a lane
   __shared__ __align__(16) float sum_of[SPLIT > 1 ? SPLIT : 1][SPLIT > 1 ? 4 : 1][CACHE_MAX_D + 4];
@@ -239,20 +239,24 @@ merge_kernel(const __grid_constant__ AttendArgs a) {
   // the division of the work, while the kernels before are still running
   scan_lengths<MERGE_THREADS>(a, a.kt, cum, warp_sum, &bad, &start, [](int) { return -1; });
   const Plan plan(a, cum[a.B]);
+  __shared__ Divisor by_share_p, by_share_o;
+  if (threadIdx.x == 0) by_share_p.set(plan.share_p);
+  if (threadIdx.x == 32) by_share_o.set(plan.share_o);
+  __syncthreads();
   const int D = a.D, Hq = a.Hkv * a.G;
   const int groups = (plan.R + 3) / 4;             // of a key head
   bool waited = false;
   for (int w0 = (int)blockIdx.x * (MERGE_WARPS / SPLIT); w0 < groups * a.Hkv; w0 += (int)gridDim.x * (MERGE_WARPS / SPLIT)) {
     const int w = w0 + warp / SPLIT;
-    const int h = w / groups, r = (w - h * groups) * 4 + (lane & 3);
+    const int h = a.by_R4.of(w), r = (w - h * groups) * 4 + (lane & 3);
     // the parts over the prefix, then those over the own cache
     bool mine = w < groups * a.Hkv && r < plan.R;  // (and not written by one of the kernels before)
     Parts pre{}, own{};
     int token = 0;
     if (mine) {
       token = a.by_G.of(r);
-      pre = prefix_parts(a, plan, h, r);
-      own = own_parts(a, plan, cum, h, r);
+      pre = prefix_parts(a, plan, by_share_p, h, r);
+      own = own_parts(a, plan, by_share_o, cum, h, r);
       if (a.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0))
         mine = false;
     }
@@ -264,28 +268,47 @@ merge_kernel(const __grid_constant__ AttendArgs a) {
     float4 o[NG];
 #pragma unroll
     for (int k = 0; k < NG; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = sub; i < parts; i += SPLIT) {
-      const bool first = i < pre.n;
-      const int per = first ? pre.per : own.per, at = first ? i : i - pre.n;
-      const float2 ml = (first ? pre.ml : own.ml)[at * per];
-      const float* src = (first ? pre.sums : own.sums) + (long long)at * per * D;
-      float4 x[NG];
+    for (int i0 = sub; i0 < parts; i0 += 2 * SPLIT) {
+      float2 ml[2];
+      float4 x[2][NG];
 #pragma unroll
-      for (int k = 0; k < NG; ++k) {               // (columns beyond D: others again, not stored)
-        const int c = 4 * cq + 32 * k;
-        x[k] = load4(src + (c < D ? c : 0) * per);
+      for (int e = 0; e < 2; ++e) {                // two parts' loads on their way at once
+        const int i = min(i0 + e * SPLIT, parts - 1);
+        const bool first = i < pre.n;
+        const int per = first ? pre.per : own.per, at = first ? i : i - pre.n;
+        ml[e] = (first ? pre.ml : own.ml)[at * per];
+        if (i0 + e * SPLIT >= parts) ml[e] = make_float2(-INFINITY, 0.f);
+        const float* src = (first ? pre.sums : own.sums) + (long long)at * per * D;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {             // (columns beyond D: others again, not stored)
+          const int c = 4 * cq + 32 * k;
+          x[e][k] = load4(src + (c < D ? c : 0) * per);
+        }
       }
-      const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.f : mn;
+      const float mn = fmaxf(m, fmaxf(ml[0].x, ml[1].x)), ms = mn == -INFINITY ? 0.f : mn;
       // (a part without a finite score has sums of 0, or NaN, which pass)
-      const float was = m == mn ? 1.f : ex2(m - ms), wi = ml.x == mn ? 1.f : ex2(ml.x - ms);
+      const float was = m == mn ? 1.f : ex2(m - ms);
       m = mn;
-      l = l * was + wi * ml.y;
+      l *= was;
 #pragma unroll
       for (int k = 0; k < NG; ++k) {
-        o[k].x = fmaf(wi, x[k].x, o[k].x * was);
-        o[k].y = fmaf(wi, x[k].y, o[k].y * was);
-        o[k].z = fmaf(wi, x[k].z, o[k].z * was);
-        o[k].w = fmaf(wi, x[k].w, o[k].w * was);
+        o[k].x *= was;
+        o[k].y *= was;
+        o[k].z *= was;
+        o[k].w *= was;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (i0 + e * SPLIT >= parts) continue;
+        const float wi = ml[e].x == mn ? 1.f : ex2(ml[e].x - ms);
+        l += wi * ml[e].y;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+          o[k].x = fmaf(wi, x[e][k].x, o[k].x);
+          o[k].y = fmaf(wi, x[e][k].y, o[k].y);
+          o[k].z = fmaf(wi, x[e][k].z, o[k].z);
+          o[k].w = fmaf(wi, x[e][k].w, o[k].w);
+        }
       }
     }
     const long long row = (long long)token * Hq + h * a.G + (r - token * a.G);
@@ -359,7 +382,7 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {
   // a warp a group of 4 rows, or a CTA a group where that leaves SMs without work
   const long long groups = (long long)((a.B * a.L * a.G + 3) / 4) * a.Hkv;
-  const bool split = groups <= 4 * CACHE_SMS;
+  const bool split = groups <= 8 * CACHE_SMS;
   const long long ctas = split ? groups : (groups + MERGE_WARPS - 1) / MERGE_WARPS;
   const int grid = (int)(ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS);
   const size_t smem = sizeof(int32_t) * (a.B + 1);

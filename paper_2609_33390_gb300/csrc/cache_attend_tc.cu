@@ -508,7 +508,9 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         if (!part) {                               // all of the prefix: the own entries' parts join here
           wait_for_previous();
           const Plan plan(a, a.cum[a.B]);
-          if (mine) own = own_parts(a, plan, a.cum, g.h, g.row0 + s * SLOT + r);
+          Divisor by_share;
+          by_share.set(plan.share_o);
+          if (mine) own = own_parts(a, plan, by_share, a.cum, g.h, g.row0 + s * SLOT + r);
           part = own.n > JOIN_PARTS;
         }
         store_rows<true>(a, tO, y, mine, m, l, part ? a.part_p + part_at(g.slot, per, a.D, s * SLOT + r, 0) : nullptr,
