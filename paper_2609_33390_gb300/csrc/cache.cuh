@@ -309,10 +309,10 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 
 // Launches a kernel that may be set up while the one before it on the stream still runs.
 template <typename Kernel, typename... Args>
-inline cudaError_t launch_early(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t stream, bool early,
+inline cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, bool early,
                                 const Args&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

@@ -161,7 +161,8 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   a.status = at<int32_t>(ws, cache_ws(d).status);
   a.wait_limit = wait_limit_cycles();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
+  if (d->S == 0 || d->dtype == BRISK_DT_BF16)   // (the fp32 kernel writes the word itself)
+    if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
   if (d->S == 0) return BRISK_OK;
   if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
   a.grid = CACHE_SMS;
@@ -186,8 +187,9 @@ brisk_status brisk_cache_evict(const brisk_cache_dims* d, const brisk_view* k, c
     for (const void* t : to)
       if (f == t) return BRISK_ERR_INVALID_ARG;
   if (acc == acc_to || own_len == len_to || a.k_to.p == a.v_to.p) return BRISK_ERR_INVALID_ARG;
-  const long long vecs = (long long)d->B * keep * d->Hkv * (d->D * (long long)esize(d->dtype) / 16);
-  if (vecs / 1024 >= 0x7fffffffLL) return BRISK_ERR_UNSUPPORTED;
+  // a sequence's 16-byte pieces, and the kernel that moves them one beyond its last CTA, in 31 bits
+  const double vecs = (double)keep * d->Hkv * (d->D * (double)esize(d->dtype) / 16);
+  if (vecs >= 2.0e9) return BRISK_ERR_UNSUPPORTED;
   a.B = d->B; a.Hkv = d->Hkv; a.D = d->D; a.S = d->S; a.dt = d->dtype; a.keep = keep; a.recent = recent;
   a.acc = acc;
   a.own_len = own_len;
@@ -196,7 +198,6 @@ brisk_status brisk_cache_evict(const brisk_cache_dims* d, const brisk_view* k, c
   a.kept = kept;
   a.status = at<int32_t>(ws, cache_ws(d).status);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
   return launch_evict(a, st) == cudaSuccess ? BRISK_OK : BRISK_ERR_CUDA;
 }
 

@@ -6,7 +6,9 @@
 namespace brisk {
 namespace {
 
-constexpr int SELECT_THREADS = 1024;
+constexpr int SELECT_THREADS = 1024, SELECT_EACH = 4;
+constexpr int SELECT_BLOCK = SELECT_THREADS * SELECT_EACH;   // entries a pass takes at a time
+constexpr int BINS = 2048;
 
 // Order-preserving key of a weight: larger weights have larger keys, -0 equals 0, NaN is below all.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -37,16 +39,17 @@ __device__ __forceinline__ int block_scan(int x, int* part, int* total) {
   return x + (warp > 0 ? before : 0);
 }
 
-// One CTA a (sequence, key head): the smallest kept key by four passes over 8 bits each, then the
-// kept indices in order.
+// One CTA a (sequence, key head): the smallest kept key by three passes over 11, 11 and 10 of its bits,
+// then the kept indices in order. Bound by the barriers and the passes' latency: the weights, a
+// hundredth of the entries' bytes, stay in L1 after the first pass.
 __global__ void __launch_bounds__(SELECT_THREADS)
 select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int hist[256], part[32];
+  __shared__ int hist[BINS], part[32];
   __shared__ uint32_t s_prefix;
   __shared__ int s_room;
+  let_next_begin();
   const int b = blockIdx.x / a.Hkv, h = blockIdx.x - b * a.Hkv, tid = threadIdx.x;
-  const int raw = a.own_len[b], n = min(max(raw, 0), a.S);
-  if (raw != n && tid == 0) set_status(a.status, BRISK_ERR_INVALID_ARG);
+  const int n = clamped_len(a, b);
   if (h == 0 && tid == 0) a.len_to[b] = min(n, a.keep);
   const float* acc = a.acc + (long long)blockIdx.x * a.S;
   float* acc_to = a.acc_to + (long long)blockIdx.x * a.keep;
@@ -61,90 +64,130 @@ select_kernel(const __grid_constant__ EvictArgs a) {
   const int m = n - a.recent;              // entries that may go; n > keep, so m > room
   int room = a.keep - a.recent;            // how many of them stay
   // the key of the last one that stays, and how many of its equals do
-  uint32_t prefix = 0;
-  if (room > 0)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
+  uint32_t prefix = 0, known = 0;          // known: the bits of it that are
+  const bool some = room > 0;
+  if (some)
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : BINS;
+      hist[tid] = 0;
+      hist[tid + 1024] = 0;
       __syncthreads();
       for (int i = tid; i < m; i += SELECT_THREADS) {
         const uint32_t k = weight_key(acc[i]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+        if ((k & known) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
       }
       __syncthreads();
-      // bins from the largest: thread j holds bin 255 - j
-      const int mine = tid < 256 ? hist[255 - tid] : 0;
+      // bins from the largest: thread j holds bins - 1 - 2j and the next lower one
+      const int top = bins - 1 - 2 * tid;
+      const int first = top > 0 ? hist[top] : 0, second = top > 0 ? hist[top - 1] : 0;
       int total;
-      const int upto = block_scan(mine, part, &total);
-      if (tid < 256 && upto >= room && upto - mine < room) {
-        s_prefix = prefix | ((uint32_t)(255 - tid) << shift);
-        s_room = room - (upto - mine);
+      const int upto = block_scan(first + second, part, &total), before = upto - first - second;
+      if (before < room && upto >= room) {
+        const bool in_first = before + first >= room;
+        s_prefix = prefix | ((uint32_t)(in_first ? top : top - 1) << shift);
+        s_room = room - before - (in_first ? 0 : first);
       }
       __syncthreads();
       prefix = s_prefix;
       room = s_room;
+      known |= (uint32_t)(bins - 1) << shift;
       __syncthreads();
     }
-  int done = 0, equal = 0;                 // entries kept, and equals of the last key seen, so far
-  for (int i0 = 0; i0 < n; i0 += SELECT_THREADS) {
-    const int i = i0 + tid;
-    const float w = i < n ? acc[i] : 0.f;
-    const uint32_t k = weight_key(w);
-    const bool old = i < m, tie = old && room > 0 && k == prefix;
-    int total;
-    const int rank = block_scan(tie ? 1 : 0, part, &total);
-    const bool stay = i < n && (!old || (a.keep > a.recent && k > prefix) || (tie && equal + rank <= room));
-    equal += total;
-    const int at = block_scan(stay ? 1 : 0, part, &total);
-    if (stay) {
-      kept[done + at - 1] = i;
-      acc_to[done + at - 1] = w;
+  int done = 0, equal = 0;                 // entries above the last key (and newest) seen, and its equals
+  for (int i0 = 0; i0 < n; i0 += SELECT_BLOCK) {
+    const int i = i0 + tid * SELECT_EACH;
+    float w[SELECT_EACH];
+    int is = 0, in = 0;                    // two bits an entry: stays, equals
+#pragma unroll
+    for (int j = 0; j < SELECT_EACH; ++j) {
+      w[j] = i + j < n ? acc[i + j] : 0.f;
+      const uint32_t k = weight_key(w[j]);
+      const bool old = i + j < m;
+      if (i + j < n && (!old || (some && k > prefix))) is |= 1 << j;
+      if (old && some && k == prefix) in |= 1 << j;
     }
-    done += total;
+    // both counts in one scan (a block has less than 2^15 entries)
+    int total;
+    const int mine = __popc(is) | __popc(in) << 16;
+    const int upto = block_scan(mine, part, &total) - mine;
+    int above = done + (upto & 0xffff), ties = equal + (upto >> 16);
+#pragma unroll
+    for (int j = 0; j < SELECT_EACH; ++j) {
+      const bool tie = in >> j & 1, stay = (is >> j & 1) || (tie && ties < room);
+      if (stay) {
+        const int at = above + min(ties, room);
+        kept[at] = i + j;
+        acc_to[at] = w[j];
+      }
+      above += is >> j & 1;
+      ties += tie;
+    }
+    done += total & 0xffff;
+    equal += total >> 16;
   }
 }
 
-// The kept rows of keys and values, 16 bytes a thread at a time; zeros where there is none.
+// The kept rows of keys and values, 16 bytes a thread at a time; zeros where there is none. The pieces of a
+// sequence's (place, head) rows lie as in the target's token-major order, so that writes are runs of whole
+// tokens; a thread's loads, of four pieces of the keys and of the values, are all on their way at once. Bound
+// by the rows' bytes, read and written once.
 constexpr int MOVE_THREADS = 256, MOVE_EACH = 4;
 __global__ void __launch_bounds__(MOVE_THREADS)
-move_kernel(const __grid_constant__ EvictArgs a, int nvec, int es) {
-  const long long per = (long long)a.B * a.keep * a.Hkv * nvec;
-  const long long first = (long long)blockIdx.x * MOVE_THREADS * MOVE_EACH + threadIdx.x;
-  const CacheView& from = blockIdx.y ? a.v : a.k;
-  const CacheView& to = blockIdx.y ? a.v_to : a.k_to;
-  const int ev = 16 / es;                  // elements of 16 bytes
-  uint4 x[MOVE_EACH];
-  char* dst[MOVE_EACH];
+move_kernel(const __grid_constant__ EvictArgs a, Divisor by_vec, Divisor by_heads) {
+  __shared__ int bad;
+  const int b = blockIdx.y, first = (int)blockIdx.x * MOVE_THREADS * MOVE_EACH + threadIdx.x;
+  const int rows = a.keep * a.Hkv, es = a.dt == BRISK_DT_BF16 ? 2 : 4, step = 16 / es;
+  const char *kf = static_cast<const char*>(a.k.p) + b * a.k.seq * es, *vf = static_cast<const char*>(a.v.p) + b * a.v.seq * es;
+  char *kt = static_cast<char*>(const_cast<void*>(a.k_to.p)) + b * a.k_to.seq * es;
+  char *vt = static_cast<char*>(const_cast<void*>(a.v_to.p)) + b * a.v_to.seq * es;
+  if (blockIdx.x == 0 && b == 0) {         // the call's status: the lengths that were clamped
+    if (threadIdx.x == 0) bad = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.B; i += MOVE_THREADS)
+      if (a.own_len[i] < 0 || a.own_len[i] > a.S) bad = 1;
+    __syncthreads();
+    if (threadIdx.x == 0) *a.status = bad ? BRISK_ERR_INVALID_ARG : BRISK_OK;
+  }
+  wait_for_previous();
+  int h[MOVE_EACH], at[MOVE_EACH], c[MOVE_EACH], src[MOVE_EACH];
 #pragma unroll
   for (int j = 0; j < MOVE_EACH; ++j) {
-    const long long e = first + j * MOVE_THREADS;
-    dst[j] = nullptr;
-    x[j] = make_uint4(0, 0, 0, 0);
-    if (e >= per) continue;
-    const long long row = e / nvec;        // (sequence, place, head)
-    const int c = (int)(e - row * nvec) * ev;
-    const long long bj = row / a.Hkv;
-    const int h = (int)(row - bj * a.Hkv), b = (int)(bj / a.keep), at = (int)(bj - (long long)b * a.keep);
-    const int src = a.kept[((long long)b * a.Hkv + h) * a.keep + at];
-    dst[j] = static_cast<char*>(const_cast<void*>(to.p)) + (b * to.seq + at * to.tok + h * to.head + c) * es;
-    if (src >= 0)
-      x[j] = *reinterpret_cast<const uint4*>(static_cast<const char*>(from.p) +
-                                             (b * from.seq + src * from.tok + h * from.head + c) * es);
+    const int e = first + j * MOVE_THREADS, row = by_vec.of(e);
+    at[j] = by_heads.of(row);
+    h[j] = row - at[j] * a.Hkv;
+    c[j] = (e - row * by_vec.d) * step;
+    src[j] = row < rows ? __ldg(a.kept + ((long long)b * a.Hkv + h[j]) * a.keep + at[j]) : -2;
+  }
+  uint4 x[MOVE_EACH], y[MOVE_EACH];
+#pragma unroll
+  for (int j = 0; j < MOVE_EACH; ++j) {
+    x[j] = y[j] = make_uint4(0, 0, 0, 0);
+    if (src[j] >= 0) {
+      x[j] = ld_stream_v4(kf + (src[j] * a.k.tok + h[j] * a.k.head + c[j]) * es);
+      y[j] = ld_stream_v4(vf + (src[j] * a.v.tok + h[j] * a.v.head + c[j]) * es);
+    }
   }
 #pragma unroll
   for (int j = 0; j < MOVE_EACH; ++j)
-    if (dst[j]) *reinterpret_cast<uint4*>(dst[j]) = x[j];
+    if (src[j] >= -1) {
+      __stcs(reinterpret_cast<uint4*>(kt + (at[j] * a.k_to.tok + h[j] * a.k_to.head + c[j]) * es), x[j]);
+      __stcs(reinterpret_cast<uint4*>(vt + (at[j] * a.v_to.tok + h[j] * a.v_to.head + c[j]) * es), y[j]);
+    }
 }
 
 }  // namespace
 
 cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
   const int es = a.dt == BRISK_DT_BF16 ? 2 : 4, nvec = a.D * es / 16;
+  Divisor by_vec, by_heads;
+  by_vec.set(nvec);
+  by_heads.set(a.Hkv);
   select_kernel<<<a.B * a.Hkv, SELECT_THREADS, 0, stream>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const long long per = (long long)a.B * a.keep * a.Hkv * nvec, each = MOVE_THREADS * MOVE_EACH;
-  move_kernel<<<dim3((unsigned)((per + each - 1) / each), 2), MOVE_THREADS, 0, stream>>>(a, nvec, es);
-  return cudaGetLastError();
+  const long long vecs = (long long)a.keep * a.Hkv * nvec, each = MOVE_THREADS * MOVE_EACH;
+  return launch_early(move_kernel, dim3((unsigned)((vecs + each - 1) / each), a.B), MOVE_THREADS, 0, stream, true, a, by_vec,
+                      by_heads);
 }
 
 }  // namespace brisk

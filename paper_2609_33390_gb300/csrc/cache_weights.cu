@@ -25,8 +25,13 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   const int tiles = (a.S + W_KEYS - 1) / W_KEYS, D = a.D, nv = D / 4;
   const long long item = blockIdx.x / tiles;
   const int t0 = (int)(blockIdx.x % tiles) * W_KEYS, b = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
-  const int raw = a.own_len[b], len = min(max(raw, 0), a.S);
-  if (raw != len && tid == 0) set_status(a.status, BRISK_ERR_INVALID_ARG);
+  const int len = clamped_len(a, b);
+  if (blockIdx.x == 0) {                   // the call's status: the lengths that were clamped
+    bool bad = false;
+    for (int i = tid; i < a.B; i += W_THREADS) bad |= a.own_len[i] < 0 || a.own_len[i] > a.S;
+    bad = __syncthreads_or(bad);
+    if (tid == 0) *a.status = bad ? BRISK_ERR_INVALID_ARG : BRISK_OK;
+  }
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   const int rows = a.L * a.G;
   if (t0 < len) {
