@@ -45,7 +45,7 @@ struct AttendArgs {
   // for the own caches has both) and of the one for the own caches
   int rt_p, rt_o, kt, grid_p, grid_o;
   CacheView q, kp, vp, ko, vo;
-  Divisor by_L, by_G, by_LG, by_R4;  // L, G, L * G, and the groups of 4 rows of a key head
+  Divisor by_L, by_G, by_LG;         // L, G and L * G
   const int32_t* own_len;            // [B]
   const int32_t* visible;            // [B, L] or nullptr
   float sl2;                         // scale * log2(e)

@@ -55,7 +55,6 @@ AttendArgs sizes_of(const brisk_cache_dims* d) {
   a.by_L.set(a.L);
   a.by_G.set(a.G);
   a.by_LG.set(a.L * a.G);
-  a.by_R4.set((a.B * a.L * a.G + 3) / 4);
   divide(&a);
   return a;
 }

@@ -220,65 +220,183 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
 
 constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D + RT * (KT + 4));
 
-// Joins the parts of the rows whose keys were divided. A warp takes 4 neighbouring rows of a key head,
-// 8 lanes a row, each with every eighth group of four columns: its loads are runs of 64 bytes, a part's
-// all in flight at once. With few rows the 8 warps of a CTA take the rows' parts in turn (SPLIT) and meet in
-// shared memory: one part after another is a load's latency each (one block of 32 positions over 4096 + 1100
-// entries, 21 parts a row: a warp a row group 54 us).
+// Joins the parts of the rows whose keys were divided.
+//
+// Many rows: a CTA takes 32 neighbouring rows of a key head, a row a lane and 16 columns a warp, so that loads
+// are runs of 512 bytes as the parts lie; four parts' are on their way at once. Few rows: a CTA takes 4 rows, 8
+// lanes each, and its 8 warps the rows' parts in turn, which meet in shared memory: one load after
+// another is a latency each (one block of 32 positions over 4096 + 1100 entries, 21 parts a row: parts one by
+// one 54 us). Either way the division of the work is looked up while the kernels before still run.
 constexpr int MERGE_WARPS = 8, MERGE_THREADS = 32 * MERGE_WARPS;
-template <typename T, int SPLIT>
-__global__ void __launch_bounds__(MERGE_THREADS, 3)
-merge_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int NG = CACHE_MAX_D / 32;             // groups of four columns of a lane
-  __shared__ __align__(16) float sum_of[SPLIT > 1 ? SPLIT : 1][SPLIT > 1 ? 4 : 1][CACHE_MAX_D + 4];
-  __shared__ float2 ml_of[SPLIT > 1 ? SPLIT : 1][4];
-  extern __shared__ int32_t cum[];                 // [B + 1] key tiles before each sequence
-  __shared__ int warp_sum[MERGE_WARPS], bad;
-  __shared__ Start start;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cq = lane >> 2, sub = warp % SPLIT;
-  // the division of the work, while the kernels before are still running
-  scan_lengths<MERGE_THREADS>(a, a.kt, cum, warp_sum, &bad, &start, [](int) { return -1; });
+
+struct Merge {                                     // what both forms know, in shared memory
+  Divisor by_share_p, by_share_o;
+  int warp_sum[MERGE_WARPS], bad;
+  Start start;
+};
+__device__ __forceinline__ Plan begin_merge(const AttendArgs& a, int32_t* cum, Merge* k) {
+  scan_lengths<MERGE_THREADS>(a, a.kt, cum, k->warp_sum, &k->bad, &k->start, [](int) { return -1; });
   const Plan plan(a, cum[a.B]);
-  __shared__ Divisor by_share_p, by_share_o;
-  if (threadIdx.x == 0) by_share_p.set(plan.share_p);
-  if (threadIdx.x == 32) by_share_o.set(plan.share_o);
+  if (threadIdx.x == 0) k->by_share_p.set(plan.share_p);
+  if (threadIdx.x == 32) k->by_share_o.set(plan.share_o);
   __syncthreads();
-  const int D = a.D, Hq = a.Hkv * a.G;
-  const int groups = (plan.R + 3) / 4;             // of a key head
+  return plan;
+}
+// Whether a kernel before has written a row with these parts.
+__device__ __forceinline__ bool written(const AttendArgs& a, const Parts& pre, const Parts& own) {
+  return a.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0);
+}
+__device__ __forceinline__ void merge_status(const AttendArgs& a) {
+  if (blockIdx.x != 0 || threadIdx.x >= 32) return;
+  int code = BRISK_OK;                             // the largest: a wait that gave up before a bad length
+  for (int c = threadIdx.x; c < a.grid_p + a.grid_o; c += 32) code = max(code, a.errs[c]);
+  code = __reduce_max_sync(FULL_MASK, code);
+  if (threadIdx.x == 0) *a.status = code;
+}
+__device__ __forceinline__ float4 fma4(float w, float4 x, float4 o) {
+  return make_float4(fmaf(w, x.x, o.x), fmaf(w, x.y, o.y), fmaf(w, x.z, o.z), fmaf(w, x.w, o.w));
+}
+__device__ __forceinline__ float4 mul4(float w, float4 x) { return make_float4(w * x.x, w * x.y, w * x.z, w * x.w); }
+
+template <typename T>
+__global__ void __launch_bounds__(MERGE_THREADS, 2)
+merge_many_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int AHEAD = 4, COLS = 16;
+  extern __shared__ int32_t cum[];                 // [B + 1] key tiles before each sequence
+  __shared__ Merge known;
+  const Plan plan = begin_merge(a, cum, &known);
+  const int lane = threadIdx.x & 31, D = a.D, Hq = a.Hkv * a.G;
+  // where the head is narrow, several groups of rows share the warps
+  const int slices = (D + COLS - 1) / COLS, groups = MERGE_WARPS / slices;
+  const int sub = (threadIdx.x >> 5) / slices, c0 = ((threadIdx.x >> 5) - sub * slices) * COLS;
+  // Where the prefix's kernel leaves only rows whose prefix was divided, and a CTA of it has at least an item's
+  // units, those are the items in which a CTA's units end: they alone are gone through, so that CTAs have
+  // the same work.
+  bool many = false;
+  for (int b = threadIdx.x; b < a.B; b += MERGE_THREADS) many |= cum[b + 1] - cum[b] > plan.share_o;
+  const bool ends = !__syncthreads_or(many) && a.grid_p > 0 && plan.share_p >= plan.kP;
+  const int per_head = (plan.R + 31) / 32, per_item = a.rt_p / 32;
+  const int all = ends ? (plan.UP - 1) / plan.share_p * per_item : per_head * a.Hkv;
   bool waited = false;
-  for (int w0 = (int)blockIdx.x * (MERGE_WARPS / SPLIT); w0 < groups * a.Hkv; w0 += (int)gridDim.x * (MERGE_WARPS / SPLIT)) {
-    const int w = w0 + warp / SPLIT;
-    const int h = a.by_R4.of(w), r = (w - h * groups) * 4 + (lane & 3);
-    // the parts over the prefix, then those over the own cache
-    bool mine = w < groups * a.Hkv && r < plan.R;  // (and not written by one of the kernels before)
-    Parts pre{}, own{};
+  for (int w = (int)blockIdx.x * groups + sub; w - sub < all; w += (int)gridDim.x * groups) {
+    bool mine = w < all && sub < groups;           // (and not written by one of the kernels before)
+    int h, r;
+    if (ends) {
+      const int u = (w / per_item + 1) * plan.share_p, item = u / plan.kP;
+      h = item / plan.nPT;
+      r = (item - h * plan.nPT) * a.rt_p + (w % per_item) * 32 + lane;
+      mine = mine && u != item * plan.kP;
+    } else {
+      h = w / per_head;
+      r = (w - h * per_head) * 32 + lane;
+    }
+    mine = mine && r < plan.R;
+    Parts pre{}, own{};                            // over the prefix, over the own entries
     int token = 0;
     if (mine) {
       token = a.by_G.of(r);
-      pre = prefix_parts(a, plan, by_share_p, h, r);
-      own = own_parts(a, plan, by_share_o, cum, h, r);
-      if (a.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0))
-        mine = false;
+      pre = prefix_parts(a, plan, known.by_share_p, h, r);
+      own = own_parts(a, plan, known.by_share_o, cum, h, r);
+      if (written(a, pre, own)) mine = false;
+    }
+    if (!waited) wait_for_previous();
+    waited = true;
+    const bool idle = mine && row_idle(a, token);  // (used at the end: its load and the parts' go together)
+    const int parts = mine ? pre.n + own.n : 0;
+    float m = -INFINITY, l = 0.f;
+    float4 o[COLS / 4];
+#pragma unroll
+    for (int k = 0; k < COLS / 4; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < parts; i0 += AHEAD) {
+      float2 ml[AHEAD];
+      float4 x[AHEAD][COLS / 4];
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e) {
+        const int i = min(i0 + e, parts - 1);
+        const bool first = i < pre.n;
+        const int per = first ? pre.per : own.per, at = (first ? i : i - pre.n) * per;
+        const float* src = (first ? pre.sums : own.sums) + (long long)at * D;
+        ml[e] = make_float2(-INFINITY, 0.f);
+        if (i0 + e >= parts) continue;
+        ml[e] = (first ? pre.ml : own.ml)[at];
+#pragma unroll
+        for (int k = 0; k < COLS / 4; ++k) x[e][k] = load4(src + min(c0 + 4 * k, D - 4) * per);
+      }
+      float mn = m;
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e) mn = fmaxf(mn, ml[e].x);
+      const float ms = mn == -INFINITY ? 0.f : mn;
+      // (a part without a finite score has sums of 0, or NaN, which pass)
+      const float was = m == mn ? 1.f : ex2(m - ms);
+      m = mn;
+      l *= was;
+#pragma unroll
+      for (int k = 0; k < COLS / 4; ++k) o[k] = mul4(was, o[k]);
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e) {
+        if (i0 + e >= parts) continue;
+        const float wi = ml[e].x == mn ? 1.f : ex2(ml[e].x - ms);
+        l += wi * ml[e].y;
+#pragma unroll
+        for (int k = 0; k < COLS / 4; ++k) o[k] = fma4(wi, x[e][k], o[k]);
+      }
+    }
+    if (!mine) continue;
+    const bool none = l == 0.f || idle;
+    const float inv = none ? 0.f : 1.f / l;
+    const long long row = (long long)token * Hq + h * a.G + (r - token * a.G);
+    T* to = static_cast<T*>(a.out) + row * D;
+#pragma unroll
+    for (int k = 0; k < COLS / 4; ++k)
+      if (c0 + 4 * k < D) store4(to + c0 + 4 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f) : mul4(inv, o[k]));
+    if (a.lse && c0 == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
+  }
+  if (!waited) wait_for_previous();
+  merge_status(a);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(MERGE_THREADS, 3)
+merge_few_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int NG = CACHE_MAX_D / 32, ROWS = 4;   // groups of four columns of a lane; rows of a CTA
+  extern __shared__ int32_t cum[];                 // [B + 1] key tiles before each sequence
+  __shared__ Merge known;
+  __shared__ __align__(16) float sum_of[MERGE_WARPS][ROWS][CACHE_MAX_D + 4];
+  __shared__ float2 ml_of[MERGE_WARPS][ROWS];
+  const Plan plan = begin_merge(a, cum, &known);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.D, Hq = a.Hkv * a.G;
+  const int groups = (plan.R + ROWS - 1) / ROWS;   // of a key head
+  bool waited = false;
+  for (int w = blockIdx.x; w < groups * a.Hkv; w += gridDim.x) {
+    const int h = w / groups, r = (w - h * groups) * ROWS + (lane & 3), cq = lane >> 2;
+    Parts pre{}, own{};
+    bool mine = r < plan.R;
+    int token = 0;
+    if (mine) {
+      token = a.by_G.of(r);
+      pre = prefix_parts(a, plan, known.by_share_p, h, r);
+      own = own_parts(a, plan, known.by_share_o, cum, h, r);
+      if (written(a, pre, own)) mine = false;
     }
     if (!waited) wait_for_previous();
     waited = true;
     const bool idle = mine && row_idle(a, token);
-    const int parts = mine && !idle ? pre.n + own.n : 0;
+    const int parts = mine ? pre.n + own.n : 0;
     float m = -INFINITY, l = 0.f;
     float4 o[NG];
 #pragma unroll
     for (int k = 0; k < NG; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = sub; i0 < parts; i0 += 2 * SPLIT) {
+    for (int i0 = warp; i0 < parts; i0 += 2 * MERGE_WARPS) {
       float2 ml[2];
       float4 x[2][NG];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {                // two parts' loads on their way at once
-        const int i = min(i0 + e * SPLIT, parts - 1);
+        const int i = min(i0 + e * MERGE_WARPS, parts - 1);
         const bool first = i < pre.n;
-        const int per = first ? pre.per : own.per, at = first ? i : i - pre.n;
-        ml[e] = (first ? pre.ml : own.ml)[at * per];
-        if (i0 + e * SPLIT >= parts) ml[e] = make_float2(-INFINITY, 0.f);
-        const float* src = (first ? pre.sums : own.sums) + (long long)at * per * D;
+        const int per = first ? pre.per : own.per, at = (first ? i : i - pre.n) * per;
+        const float* src = (first ? pre.sums : own.sums) + (long long)at * D;
+        ml[e] = (first ? pre.ml : own.ml)[at];
+        if (i0 + e * MERGE_WARPS >= parts) ml[e] = make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int k = 0; k < NG; ++k) {             // (columns beyond D: others again, not stored)
           const int c = 4 * cq + 32 * k;
@@ -286,88 +404,52 @@ merge_kernel(const __grid_constant__ AttendArgs a) {
         }
       }
       const float mn = fmaxf(m, fmaxf(ml[0].x, ml[1].x)), ms = mn == -INFINITY ? 0.f : mn;
-      // (a part without a finite score has sums of 0, or NaN, which pass)
       const float was = m == mn ? 1.f : ex2(m - ms);
       m = mn;
       l *= was;
 #pragma unroll
-      for (int k = 0; k < NG; ++k) {
-        o[k].x *= was;
-        o[k].y *= was;
-        o[k].z *= was;
-        o[k].w *= was;
-      }
+      for (int k = 0; k < NG; ++k) o[k] = mul4(was, o[k]);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        if (i0 + e * SPLIT >= parts) continue;
+        if (i0 + e * MERGE_WARPS >= parts) continue;
         const float wi = ml[e].x == mn ? 1.f : ex2(ml[e].x - ms);
         l += wi * ml[e].y;
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-          o[k].x = fmaf(wi, x[e][k].x, o[k].x);
-          o[k].y = fmaf(wi, x[e][k].y, o[k].y);
-          o[k].z = fmaf(wi, x[e][k].z, o[k].z);
-          o[k].w = fmaf(wi, x[e][k].w, o[k].w);
-        }
+        for (int k = 0; k < NG; ++k) o[k] = fma4(wi, x[e][k], o[k]);
       }
     }
+    __syncthreads();                               // (the last rows' are read)
+#pragma unroll
+    for (int k = 0; k < NG; ++k)
+      if (4 * cq + 32 * k < D) store4(&sum_of[warp][lane & 3][4 * cq + 32 * k], o[k]);
+    if (cq == 0) ml_of[warp][lane & 3] = idle ? make_float2(-INFINITY, 0.f) : make_float2(m, l);
+    __syncthreads();
+    // warp j joins row j, a lane four columns
+    const int rw = warp & 3;
     const long long row = (long long)token * Hq + h * a.G + (r - token * a.G);
-    if constexpr (SPLIT == 1) {
-      if (!mine) continue;
-      const bool none = l == 0.f;
-      const float inv = none ? 0.f : 1.f / l;
-      T* to = static_cast<T*>(a.out) + row * D + 4 * cq;
+    const bool row_mine = __shfl_sync(FULL_MASK, (int)mine, rw) != 0 && warp < ROWS;
+    const long long to_row = __shfl_sync(FULL_MASK, row, rw);
+    if (!row_mine) continue;
+    float top = -INFINITY, all = 0.f;
 #pragma unroll
-      for (int k = 0; k < NG; ++k)
-        if (4 * cq + 32 * k < D)
-          store4(to + 32 * k, none ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                   : make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
-      if (a.lse && cq == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * (1.f / LOG2E);
-    } else {
-      // warp j has the sums of parts j, j + SPLIT, ..: of row j it joins all of them, a lane four columns
-      __syncthreads();                             // (the last group's are read)
+    for (int j = 0; j < MERGE_WARPS; ++j) top = fmaxf(top, ml_of[j][rw].x);
+    const float ms = top == -INFINITY ? 0.f : top;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < NG; ++k)
-        if (4 * cq + 32 * k < D) store4(&sum_of[warp][lane & 3][4 * cq + 32 * k], o[k]);
-      if (cq == 0) ml_of[warp][lane & 3] = make_float2(m, l);
-      __syncthreads();
-      const int rw = warp & 3;                     // (warps 4.. have no row left)
-      const bool row_mine = __shfl_sync(FULL_MASK, (int)mine, rw) != 0 && warp < 4;
-      const long long to_row = __shfl_sync(FULL_MASK, row, rw);
-      if (!row_mine) continue;
-      float top = -INFINITY, all = 0.f;
-#pragma unroll
-      for (int j = 0; j < SPLIT; ++j) top = fmaxf(top, ml_of[j][rw].x);
-      const float ms = top == -INFINITY ? 0.f : top;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int j = 0; j < SPLIT; ++j) {
-        const float2 ml = ml_of[j][rw];
-        const float wj = ml.x == top ? 1.f : ex2(ml.x - ms);
-        all += wj * ml.y;
-        if (4 * lane < D) {
-          const float4 x = load4(&sum_of[j][rw][4 * lane]);
-          v.x = fmaf(wj, x.x, v.x);
-          v.y = fmaf(wj, x.y, v.y);
-          v.z = fmaf(wj, x.z, v.z);
-          v.w = fmaf(wj, x.w, v.w);
-        }
-      }
-      const bool none = all == 0.f;
-      const float inv = none ? 0.f : 1.f / all;
-      if (4 * lane < D)
-        store4(static_cast<T*>(a.out) + to_row * D + 4 * lane,
-               none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-      if (a.lse && lane == 0) a.lse[to_row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
+    for (int j = 0; j < MERGE_WARPS; ++j) {
+      const float2 ml = ml_of[j][rw];
+      const float wj = ml.x == top ? 1.f : ex2(ml.x - ms);
+      all += wj * ml.y;
+      if (4 * lane < D) v = fma4(wj, load4(&sum_of[j][rw][4 * lane]), v);
     }
+    const bool none = all == 0.f;
+    const float inv = none ? 0.f : 1.f / all;
+    if (4 * lane < D)
+      store4(static_cast<T*>(a.out) + to_row * D + 4 * lane, none ? make_float4(0.f, 0.f, 0.f, 0.f) : mul4(inv, v));
+    if (a.lse && lane == 0) a.lse[to_row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
   }
   if (!waited) wait_for_previous();
-  if (blockIdx.x == 0 && threadIdx.x < 32) {
-    int code = BRISK_OK;                           // the largest: a wait that gave up before a bad length
-    for (int c = lane; c < a.grid_p + a.grid_o; c += 32) code = max(code, a.errs[c]);
-    code = __reduce_max_sync(FULL_MASK, code);
-    if (lane == 0) *a.status = code;
-  }
+  merge_status(a);
 }
 
 }  // namespace
@@ -380,18 +462,18 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {
-  // a warp a group of 4 rows, or a CTA a group where that leaves SMs without work
-  const long long groups = (long long)((a.B * a.L * a.G + 3) / 4) * a.Hkv;
-  const bool split = groups <= 8 * CACHE_SMS;
-  const long long ctas = split ? groups : (groups + MERGE_WARPS - 1) / MERGE_WARPS;
-  const int grid = (int)(ctas < 8 * CACHE_SMS ? ctas : 8 * CACHE_SMS);
+  // the form for few rows while its CTAs fit the chip a few times over (see merge_few_kernel)
+  const long long rows = (long long)a.B * a.L * a.G * a.Hkv;
+  const bool few = rows <= 32 * CACHE_SMS;
+  const long long ctas = few ? (long long)((a.B * a.L * a.G + 3) / 4) * a.Hkv : (long long)((a.B * a.L * a.G + 31) / 32) * a.Hkv;
+  const int fit = (few ? 3 : 2) * CACHE_SMS, grid = (int)(ctas < fit ? ctas : fit);
   const size_t smem = sizeof(int32_t) * (a.B + 1);
   auto run = [&](auto kernel) {
     cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
     return e != cudaSuccess ? e : launch_early(kernel, grid, MERGE_THREADS, smem, stream, true, a);
   };
-  if (a.dt == BRISK_DT_BF16) return split ? run(merge_kernel<__nv_bfloat16, 8>) : run(merge_kernel<__nv_bfloat16, 1>);
-  return split ? run(merge_kernel<float, 8>) : run(merge_kernel<float, 1>);
+  if (a.dt == BRISK_DT_BF16) return few ? run(merge_few_kernel<__nv_bfloat16>) : run(merge_many_kernel<__nv_bfloat16>);
+  return few ? run(merge_few_kernel<float>) : run(merge_many_kernel<float>);
 }
 
 }  // namespace brisk
