@@ -289,14 +289,14 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
 // Keys of a tile, rows of it, and CTAs: bf16 on the tensor cores, fp32 on the FMA units. With bf16 and more
 // than SLOT_ROWS query rows a key head, the prefix has a kernel of its own.
 constexpr int TC_KT = 128, SLOT_ROWS = 128, PAIR_ROWS = 256, SIMT_KT = 64, SIMT_ROWS = 64;
-constexpr int SLOT_CTAS = 2 * CACHE_SMS;
+constexpr int SLOT_CTAS = 2 * CACHE_SMS;             // (the fp32 kernel's, too)
 inline void divide(AttendArgs* a) {
   const bool tc = a->dt == BRISK_DT_BF16, apart = tc && a->P > 0 && (long long)a->B * a->L * a->G > SLOT_ROWS;
   a->kt = tc ? TC_KT : SIMT_KT;
   a->rt_o = tc ? SLOT_ROWS : SIMT_ROWS;
   a->rt_p = apart ? PAIR_ROWS : a->rt_o;
   a->grid_p = apart ? CACHE_SMS : 0;
-  a->grid_o = tc ? SLOT_CTAS : CACHE_SMS;
+  a->grid_o = SLOT_CTAS;
 }
 
 // Tensor map of a cache's tiles of 64 columns x 128 entries (cache_attend_tc.cu).

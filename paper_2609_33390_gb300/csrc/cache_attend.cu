@@ -7,30 +7,207 @@
 // parts of one row join by l = sum_i l_i exp(m_i - m), O likewise, with m the largest of the m_i.
 // Scores, sums and parts are fp32; maxima and scores are held in log2 units.
 #include "cache.cuh"
+#include "tensor_core.cuh"
 
 namespace brisk {
 namespace {
 
 constexpr int SIMT_THREADS = 256;
-constexpr int KT = SIMT_KT, RT = SIMT_ROWS, RPT = RT / 16;
+constexpr int KT = SIMT_KT, RT = SIMT_ROWS;
 constexpr int KS = CACHE_MAX_D + 4;    // floats between the key tile's rows: 16 rows' float4s in two wavefronts
+constexpr int PS = KT + 4;
 
-// Rows x keys on the FMA units: 16 x 16 threads, RT/16 rows and 4 keys each for the scores, the
-// same rows and 8 columns each for the sums of values. A row's 16 threads are half a warp, so
-// its maximum, its sum and the exchange of its probabilities need no barrier of the CTA.
-__global__ void __launch_bounds__(SIMT_THREADS)
+// fp32: rows x keys on the FMA units. 16 x 16 threads, RPT rows and 4 keys each for the scores, the same rows
+// and 8 columns each for the sums of values, two products an instruction. A row's 16 threads are half a warp, so
+// its maximum, its sum and the exchange of its probabilities need no barrier of the CTA. RPT is 4, or 1
+// where a fragment has at most 16 rows (single tokens: the other rows would be padding). The probabilities lie
+// over the keys, so that two CTAs fit an SM and one computes while the other's tile arrives. Bound by
+// shared-memory reads and FMA issue, about evenly, with 64 rows; by shared-memory reads with few.
+struct SimtTile {
+  float *q, *k, *v;                    // [RT][CACHE_MAX_D], [KT][KS], [KT][CACHE_MAX_D]
+};
+
+template <int RPT>
+__device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Plan& plan, const Frag& f, const SimtTile& t,
+                                              int* lowest) {
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, D = a.D, nv = D / 4, len = f.len;
+  float* sP = t.k;                     // [RT][PS]
+  const CacheView &kc = f.prefix ? a.kp : a.ko, &vc = f.prefix ? a.vp : a.vo;
+  const float* kb = static_cast<const float*>(kc.p) + (f.prefix ? 0 : f.b * kc.seq) + f.h * kc.head;
+  const float* vb = static_cast<const float*>(vc.p) + (f.prefix ? 0 : f.b * vc.seq) + f.h * vc.head;
+  __syncthreads();                     // the last fragment's reads are done
+  if (tid == 0) *lowest = len;
+  for (int e = tid; e < RPT * 16 * nv; e += SIMT_THREADS) {
+    const int r = e / nv, c = 4 * (e - r * nv);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < f.rows) {
+      int token, head;
+      row_of(a, f, r, token, head);
+      const int b = a.by_L.of(token), i = token - b * a.L;
+      v = load4(static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head + c);
+    }
+    store4(t.q + r * CACHE_MAX_D + c, v);
+  }
+  __syncthreads();
+  int lim[RPT];
+  float m[RPT], l[RPT];
+  f32x2 o[RPT][4];                     // columns 4 tx .. 4 tx + 3 and 64 more
+#pragma unroll
+  for (int i = 0; i < RPT; ++i) {
+    const int r = ty * RPT + i;
+    lim[i] = 0;
+    if (r < f.rows) {
+      int token, head;
+      row_of(a, f, r, token, head);
+      lim[i] = row_limit(a, f, token, len);
+      if (tx == 0 && lim[i] < len) atomicMin(lowest, lim[i]);
+    }
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[i][j] = pack2(0.f, 0.f);
+  }
+  __syncthreads();
+  const int low = *lowest;             // entries from here on are hidden from some row
+
+  for (int kt = f.k0; kt < f.k0 + f.n; ++kt) {
+    const int t0 = kt * KT;
+    bool odd = false;                  // an infinity or NaN that some row must not see
+#pragma unroll 4
+    for (int e = tid; e < KT * nv; e += SIMT_THREADS) {
+      const int r = e / nv, c = 4 * (e - r * nv), key = t0 + r;
+      float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
+      if (key < len) {
+        k = load4(kb + key * kc.tok + c);
+        v = load4(vb + key * vc.tok + c);
+        if (key >= low) odd |= !(isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w));
+      }
+      store4(t.k + r * KS + c, k);
+      store4(t.v + r * CACHE_MAX_D + c, v);
+    }
+    odd = __syncthreads_or(odd);
+
+    f32x2 s2[RPT][4];                  // sums over the even and the odd columns
+#pragma unroll
+    for (int i = 0; i < RPT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s2[i][j] = pack2(0.f, 0.f);
+#pragma unroll 2
+    for (int d = 0; d < D; d += 4) {
+      ulonglong2 q[RPT], k[4];
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(t.q + (ty * RPT + i) * CACHE_MAX_D + d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const ulonglong2*>(t.k + (tx + 16 * j) * KS + d);
+#pragma unroll
+      for (int i = 0; i < RPT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s2[i][j] = fma2(q[i].y, k[j].y, fma2(q[i].x, k[j].x, s2[i][j]));
+    }
+    __syncthreads();                   // the keys are read: the probabilities take their place
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      float s[4], top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float x, y;
+        unpack2(s2[i][j], x, y);
+        s[j] = t0 + tx + 16 * j < lim[i] ? (x + y) * a.sl2 : -INFINITY;
+        top = fmaxf(top, s[j]);
+      }
+#pragma unroll
+      for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, x));
+      const float mn = fmaxf(m[i], top), ms = mn == -INFINITY ? 0.f : mn, alpha = ex2(m[i] - ms);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = ex2(s[j] - ms);
+        sum += p;
+        sP[(ty * RPT + i) * PS + tx + 16 * j] = p;
+      }
+#pragma unroll
+      for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor_sync(FULL_MASK, sum, x);
+      l[i] = l[i] * alpha + sum;
+      m[i] = mn;
+      const f32x2 alpha2 = pack2(alpha, alpha);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = fma2(alpha2, o[i][j], pack2(0.f, 0.f));
+    }
+    __syncwarp();
+    const int c0 = 4 * tx, c1 = 64 + 4 * tx;
+    if (!odd) {
+#pragma unroll 2
+      for (int y = 0; y < KT; y += 4) {
+        float4 p[RPT];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) p[i] = load4(sP + (ty * RPT + i) * PS + y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const ulonglong2 v0 = *reinterpret_cast<const ulonglong2*>(t.v + (y + e) * CACHE_MAX_D + c0);
+          const ulonglong2 v1 = *reinterpret_cast<const ulonglong2*>(t.v + (y + e) * CACHE_MAX_D + c1);
+#pragma unroll
+          for (int i = 0; i < RPT; ++i) {
+            const float w = e == 0 ? p[i].x : (e == 1 ? p[i].y : (e == 2 ? p[i].z : p[i].w));
+            const f32x2 w2 = pack2(w, w);
+            o[i][0] = fma2(w2, v0.x, o[i][0]);
+            o[i][1] = fma2(w2, v0.y, o[i][1]);
+            o[i][2] = fma2(w2, v1.x, o[i][2]);
+            o[i][3] = fma2(w2, v1.y, o[i][3]);
+          }
+        }
+      }
+    } else {
+      for (int y = 0; y < KT; ++y)
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          if (t0 + y >= lim[i]) continue;
+          const float w = sP[(ty * RPT + i) * PS + y];
+          const f32x2 w2 = pack2(w, w);
+          const ulonglong2 v0 = *reinterpret_cast<const ulonglong2*>(t.v + y * CACHE_MAX_D + c0);
+          const ulonglong2 v1 = *reinterpret_cast<const ulonglong2*>(t.v + y * CACHE_MAX_D + c1);
+          o[i][0] = fma2(w2, v0.x, o[i][0]);
+          o[i][1] = fma2(w2, v0.y, o[i][1]);
+          o[i][2] = fma2(w2, v1.x, o[i][2]);
+          o[i][3] = fma2(w2, v1.y, o[i][3]);
+        }
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int i = 0; i < RPT; ++i) {
+    const int r = ty * RPT + i;
+    if (r >= f.rows) continue;
+    int token, head;
+    row_of(a, f, r, token, head);
+    const bool none = f.whole && (row_idle(a, token) || l[i] == 0.f);
+    const float w = !f.whole ? 1.f : (none ? 0.f : 1.f / l[i]);
+    const int per = min(RT, f.prefix ? plan.R : plan.LG);
+    const long long row = (long long)token * (a.Hkv * a.G) + head;
+    float* part = (f.prefix ? a.part_p : a.part_o) + part_at(f.slot, per, D, r, 0);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int c = 64 * j + 4 * tx;
+      if (c >= D) continue;
+      float4 x;
+      unpack2(o[i][2 * j], x.x, x.y);
+      unpack2(o[i][2 * j + 1], x.z, x.w);
+      x = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(w * x.x, w * x.y, w * x.z, w * x.w);
+      store4(f.whole ? static_cast<float*>(a.out) + row * D + c : part + (long long)c * per, x);
+    }
+    if (tx > 0) continue;
+    if (!f.whole) (f.prefix ? a.ml_p : a.ml_o)[(long long)f.slot * per + r] = make_float2(m[i], l[i]);
+    else if (a.lse) a.lse[row] = none ? -INFINITY : (m[i] + log2f(l[i])) * (1.f / LOG2E);
+  }
+}
+
+__global__ void __launch_bounds__(SIMT_THREADS, 2)
 attend_simt_kernel(const __grid_constant__ AttendArgs a) {
-  using T = float;
   extern __shared__ __align__(16) float smem[];
-  float* sQ = smem;                               // [RT][CACHE_MAX_D]
-  float* sK = sQ + RT * CACHE_MAX_D;              // [KT][KS]
-  float* sV = sK + KT * KS;                       // [KT][CACHE_MAX_D]
-  float* sP = sV + KT * CACHE_MAX_D;              // [RT][KT + 4]
+  const SimtTile t{smem, smem + RT * CACHE_MAX_D, smem + RT * CACHE_MAX_D + KT * KS};
   __shared__ int warp_sum[SIMT_THREADS / 32], bad, lowest;
   __shared__ Start start;
-
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  if (tid == 0) bad = 0;
+  if (threadIdx.x == 0) bad = 0;
   __syncthreads();
   let_next_begin();
   int own = 0;
@@ -40,185 +217,16 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
     return max(0, units_of(blockIdx.x, p.share_o, p.own0 + p.UO).x - p.own0) / (p.Hkv * p.nLT);
   });
   const Plan plan(a, own);
-  if (tid == 0) a.errs[blockIdx.x] = bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK;
-
-  const int D = a.D, nv = D / 4;
+  if (threadIdx.x == 0) a.errs[blockIdx.x] = bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK;
   Walk walk(a, plan, blockIdx.x, start);
   Frag f;
   while (walk.next(a, plan, f)) {
-    const int len = f.len;
-    const T* kb = static_cast<const T*>(f.prefix ? a.kp.p : a.ko.p) +
-                  (f.prefix ? f.h * a.kp.head : f.b * a.ko.seq + f.h * a.ko.head);
-    const T* vb = static_cast<const T*>(f.prefix ? a.vp.p : a.vo.p) +
-                  (f.prefix ? f.h * a.vp.head : f.b * a.vo.seq + f.h * a.vo.head);
-    const long long ktok = f.prefix ? a.kp.tok : a.ko.tok, vtok = f.prefix ? a.vp.tok : a.vo.tok;
-    __syncthreads();                               // the last fragment's reads are done
-    if (tid == 0) lowest = len;
-    for (int e = tid; e < RT * nv; e += SIMT_THREADS) {
-      const int r = e / nv, c = 4 * (e - r * nv);
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < f.rows) {
-        int token, head;
-        row_of(a, f, r, token, head);
-        const int b = a.by_L.of(token), i = token - b * a.L;
-        v = load4(static_cast<const T*>(a.q.p) + b * a.q.seq + i * a.q.tok + head * a.q.head + c);
-      }
-      store4(sQ + r * CACHE_MAX_D + c, v);
-    }
-    __syncthreads();
-    int lim[RPT];
-    float m[RPT], l[RPT], o[RPT][8];
-#pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-      const int r = ty * RPT + i;
-      lim[i] = 0;
-      if (r < f.rows) {
-        int token, head;
-        row_of(a, f, r, token, head);
-        lim[i] = row_limit(a, f, token, len);
-        if (tx == 0 && lim[i] < len) atomicMin(&lowest, lim[i]);
-      }
-      m[i] = -INFINITY;
-      l[i] = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[i][j] = 0.f;
-    }
-    __syncthreads();
-    const int low = lowest;                        // entries from here on are hidden from some row
-
-    for (int kt = f.k0; kt < f.k0 + f.n; ++kt) {
-      const int t0 = kt * KT;
-      bool odd = false;                            // an infinity or NaN that some row must not see
-      for (int e = tid; e < KT * nv; e += SIMT_THREADS) {
-        const int r = e / nv, c = 4 * (e - r * nv), t = t0 + r;
-        float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-        if (t < len) {
-          k = load4(kb + t * ktok + c);
-          v = load4(vb + t * vtok + c);
-          if (t >= low) odd |= !(isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w));
-        }
-        store4(sK + r * KS + c, k);
-        store4(sV + r * CACHE_MAX_D + c, v);
-      }
-      odd = __syncthreads_or(odd);
-
-      float s[RPT][4];
-#pragma unroll
-      for (int i = 0; i < RPT; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-      for (int d = 0; d < D; d += 4) {
-        float4 q[RPT], k[4];
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) q[i] = load4(sQ + (ty * RPT + i) * CACHE_MAX_D + d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) k[j] = load4(sK + (tx + 16 * j) * KS + d);
-#pragma unroll
-        for (int i = 0; i < RPT; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            s[i][j] = fmaf(q[i].x, k[j].x, s[i][j]);
-            s[i][j] = fmaf(q[i].y, k[j].y, s[i][j]);
-            s[i][j] = fmaf(q[i].z, k[j].z, s[i][j]);
-            s[i][j] = fmaf(q[i].w, k[j].w, s[i][j]);
-          }
-      }
-#pragma unroll
-      for (int i = 0; i < RPT; ++i) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[i][j] = t0 + tx + 16 * j < lim[i] ? s[i][j] * a.sl2 : -INFINITY;
-          top = fmaxf(top, s[i][j]);
-        }
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, x));
-        const float mn = fmaxf(m[i], top), ms = mn == -INFINITY ? 0.f : mn;
-        const float alpha = ex2(m[i] - ms);
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = ex2(s[i][j] - ms);
-          sum += p;
-          sP[(ty * RPT + i) * (KT + 4) + tx + 16 * j] = p;
-        }
-#pragma unroll
-        for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor_sync(FULL_MASK, sum, x);
-        l[i] = l[i] * alpha + sum;
-        m[i] = mn;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[i][j] *= alpha;
-      }
-      __syncwarp();
-      const int c0 = 4 * tx, c1 = 64 + 4 * tx;
-      if (!odd) {
-#pragma unroll 4
-        for (int t = 0; t < KT; ++t) {
-          const float4 v0 = load4(sV + t * CACHE_MAX_D + c0), v1 = load4(sV + t * CACHE_MAX_D + c1);
-#pragma unroll
-          for (int i = 0; i < RPT; ++i) {
-            const float p = sP[(ty * RPT + i) * (KT + 4) + t];
-            o[i][0] = fmaf(p, v0.x, o[i][0]);
-            o[i][1] = fmaf(p, v0.y, o[i][1]);
-            o[i][2] = fmaf(p, v0.z, o[i][2]);
-            o[i][3] = fmaf(p, v0.w, o[i][3]);
-            o[i][4] = fmaf(p, v1.x, o[i][4]);
-            o[i][5] = fmaf(p, v1.y, o[i][5]);
-            o[i][6] = fmaf(p, v1.z, o[i][6]);
-            o[i][7] = fmaf(p, v1.w, o[i][7]);
-          }
-        }
-      } else {
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-          for (int i = 0; i < RPT; ++i) {
-            const float p = sP[(ty * RPT + i) * (KT + 4) + t];
-            if (t0 + t >= lim[i]) continue;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              o[i][j] = fmaf(p, sV[t * CACHE_MAX_D + c0 + j], o[i][j]);
-              o[i][4 + j] = fmaf(p, sV[t * CACHE_MAX_D + c1 + j], o[i][4 + j]);
-            }
-          }
-      }
-      __syncthreads();
-    }
-
-#pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-      const int r = ty * RPT + i;
-      if (r >= f.rows) continue;
-      int token, head;
-      row_of(a, f, r, token, head);
-      if (f.whole) {
-        const bool none = row_idle(a, token) || l[i] == 0.f;
-        const float inv = none ? 0.f : 1.f / l[i];
-        T* to = static_cast<T*>(a.out) + ((long long)token * (a.Hkv * a.G) + head) * D;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int c = 64 * j + 4 * tx;
-          if (c >= D) continue;
-          store4(to + c, none ? make_float4(0.f, 0.f, 0.f, 0.f)
-                              : make_float4(o[i][4 * j] * inv, o[i][4 * j + 1] * inv, o[i][4 * j + 2] * inv,
-                                            o[i][4 * j + 3] * inv));
-        }
-        if (a.lse && tx == 0)
-          a.lse[(long long)token * (a.Hkv * a.G) + head] = none ? -INFINITY : (m[i] + log2f(l[i])) * (1.f / LOG2E);
-      } else {
-        const int per = min(RT, f.prefix ? plan.R : plan.LG);
-        float* to = f.prefix ? a.part_p : a.part_o;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int c = 64 * j + 4 * tx;
-          if (c < D) store4(to + part_at(f.slot, per, D, r, c), make_float4(o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]));
-        }
-        if (tx == 0) (f.prefix ? a.ml_p : a.ml_o)[(long long)f.slot * per + r] = make_float2(m[i], l[i]);
-      }
-    }
+    if (f.rows > 16) simt_fragment<4>(a, plan, f, t, &lowest);
+    else simt_fragment<1>(a, plan, f, t, &lowest);
   }
 }
 
-constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D + RT * (KT + 4));
+constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D);
 
 // Joins the parts of the rows whose keys were divided.
 //

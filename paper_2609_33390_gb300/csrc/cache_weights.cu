@@ -4,6 +4,8 @@
 //
 // with the rows' log-sums lse that attention left. The keys are the tile's rows here: a key's sum
 // over the query rows stays with its threads, so there are no atomics and the sums' order is fixed.
+#include <type_traits>
+
 #include "cache.cuh"
 #include "tensor_core.cuh"
 
@@ -42,7 +44,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
     }
     for (int r0 = 0; r0 < rows; r0 += W_ROWS) {
       __syncthreads();
-      for (int e = tid; e < W_ROWS * nv; e += W_THREADS) {
+      for (int e = tid; e < (rows - r0 > 16 ? W_ROWS : 16) * nv; e += W_THREADS) {
         const int r = e / nv, c = 4 * (e - r * nv), i = (r0 + r) / a.G;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (r0 + r < rows)
@@ -64,35 +66,40 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
         sL[tid] = ls;
       }
       __syncthreads();
-      float s[4][4];
+      // 4 rows and 4 keys a thread, two products an instruction; a row where there are 16 at most
+      auto add = [&](auto rows_each) {
+        constexpr int RPT = decltype(rows_each)::value;
+        f32x2 s2[RPT][4];                  // sums over the even and the odd columns
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RPT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-      for (int d = 0; d < D; d += 4) {
-        float4 q[4], k[4];
+          for (int j = 0; j < 4; ++j) s2[i][j] = pack2(0.f, 0.f);
+#pragma unroll 2
+        for (int d = 0; d < D; d += 4) {
+          ulonglong2 q[RPT], k[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = load4(sQ + (ty * 4 + i) * CACHE_MAX_D + d);
+          for (int i = 0; i < RPT; ++i) q[i] = *reinterpret_cast<const ulonglong2*>(sQ + (ty * RPT + i) * CACHE_MAX_D + d);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) k[j] = load4(sK + (tx + 16 * j) * WS + d);
+          for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const ulonglong2*>(sK + (tx + 16 * j) * WS + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < RPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s2[i][j] = fma2(q[i].y, k[j].y, fma2(q[i].x, k[j].x, s2[i][j]));
+        }
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          const int lim = sLim[ty * RPT + i];
+          const float ls = sL[ty * RPT + i];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            s[i][j] = fmaf(q[i].x, k[j].x, s[i][j]);
-            s[i][j] = fmaf(q[i].y, k[j].y, s[i][j]);
-            s[i][j] = fmaf(q[i].z, k[j].z, s[i][j]);
-            s[i][j] = fmaf(q[i].w, k[j].w, s[i][j]);
+            float x, y;
+            unpack2(s2[i][j], x, y);
+            if (t0 + tx + 16 * j < lim) sum[j] += ex2((x + y) * a.sl2 - ls);
           }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int lim = sLim[ty * 4 + i];
-        const float ls = sL[ty * 4 + i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (t0 + tx + 16 * j < lim) sum[j] += ex2(s[i][j] * a.sl2 - ls);
-      }
+        }
+      };
+      if (rows - r0 > 16) add(std::integral_constant<int, 4>{});
+      else add(std::integral_constant<int, 1>{});
     }
   }
   __syncthreads();
