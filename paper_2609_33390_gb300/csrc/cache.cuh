@@ -299,6 +299,31 @@ inline void divide(AttendArgs* a) {
   a->grid_o = SLOT_CTAS;
 }
 
+// A tile of 128 rows in shared memory, as the products read it: panels of 64 columns, 128 bytes a row, the
+// 16-byte pieces of which are swizzled.
+constexpr int TILE_PANEL = 128 * 128;
+// A warp's 32 queries (a row a lane, from nullptr: none) on their way to rows row0.. of a tile: 4 lanes a row, 64
+// bytes of it at a time. Columns up to a multiple of 16, which the products read, are zeros.
+template <int DP>
+__device__ __forceinline__ void fetch_queries(const __nv_bfloat16* q, int D, uint8_t* tile, int row0) {
+  const int lane = threadIdx.x & 31, np = 2 * ((D + 15) / 16);       // 16-byte pieces that the products read
+#pragma unroll 1
+  for (int i = 0; i < 32; i += 8) {
+    const int in = i + (lane >> 2), at = row0 + in;
+    const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(q), in);
+    if (from)
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) {
+        const int c = 4 * k + (lane & 3);
+        const uint32_t to = su32(tile + at * 128 + (c >> 3) * TILE_PANEL + ((c ^ at) & 7) * 16);
+        if (8 * c < D)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
+        else if (c < np)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+      }
+  }
+}
+
 // Tensor map of a cache's tiles of 64 columns x 128 entries (cache_attend_tc.cu).
 bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int toks, int seqs);
 
@@ -332,6 +357,7 @@ cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream);
 struct WeightArgs {
   int B, L, G, Hkv, D, P, S, dt;     // P: 0 (no units of the prefix's)
   CacheView q, ko;
+  Divisor by_G;
   const int32_t *own_len, *visible;
   const float* lse;        // [B, L, Hkv * G]
   float sl2, decay;

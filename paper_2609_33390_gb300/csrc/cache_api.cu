@@ -150,6 +150,7 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   // one CTA a key tile: their number is a grid's first dimension
   if (!units_ok(d) || (long long)d->B * d->Hkv * ((d->S + 63) / 64) > 0x7fffffffLL) return BRISK_ERR_UNSUPPORTED;
   a.B = d->B; a.L = d->L; a.G = d->Hq / d->Hkv; a.Hkv = d->Hkv; a.D = d->D; a.S = d->S; a.dt = d->dtype;
+  a.by_G.set(a.G);
   a.own_len = own_len;
   a.visible = visible;
   a.lse = lse;

@@ -34,7 +34,7 @@ namespace {
 
 constexpr int KT = TC_KT, SLOT = SLOT_ROWS;
 constexpr float LAZY = 8.f;                        // log2 of what a score may exceed the held maximum by
-constexpr int PANEL = KT * 128;                    // bytes of 64 columns of a tile
+constexpr int PANEL = TILE_PANEL;
 
 struct AttendMaps { CUtensorMap k, v, k2, v2; };   // of a kernel's first and second caches
 
@@ -107,27 +107,6 @@ __device__ __forceinline__ Row find_row(const AttendArgs& a, const Frag& f, int 
   return x;
 }
 
-// The queries of a warp's 32 rows on their way to `dst` ([DP / 64][128 rows][128 B], swizzled): 4 lanes a
-// row, 64 bytes of it at a time.
-template <int DP>
-__device__ __forceinline__ void fetch_queries(const Row& x, int D, uint8_t* dst, int warp) {
-  const int lane = threadIdx.x & 31, np = 2 * ((D + 15) / 16);       // 16-byte pieces that the products read
-#pragma unroll 1
-  for (int i = 0; i < 32; i += 8) {
-    const int in = i + (lane >> 2), at = warp * 32 + in;
-    const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(x.q), in);
-    if (from)
-#pragma unroll
-      for (int k = 0; k < DP / 32; ++k) {
-        const int c = 4 * k + (lane & 3);
-        const uint32_t to = su32(dst + at * 128 + (c >> 3) * PANEL + ((c ^ at) & 7) * 16);
-        if (8 * c < D)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
-        else if (c < np)
-          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
-      }
-  }
-}
 __device__ __forceinline__ void rows_fetched() {
   asm volatile("cp.async.wait_all;" ::: "memory");
   fence_async_smem();
@@ -468,7 +447,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     if (u < range.y) {
       frag_at(u, f);
       x = find_row(a, f, s * SLOT + r);
-      fetch_queries<DP>(x, a.D, sQ + s * TILE, w);
+      fetch_queries<DP>(x.q, a.D, sQ + s * TILE, 32 * w);
       fetched();
     }
     while (u < range.y) {
@@ -495,7 +474,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       if (u < range.y) {
         frag_at(u, f);
         x = find_row(a, f, s * SLOT + r);
-        fetch_queries<DP>(x, a.D, sQ + s * TILE, w);
+        fetch_queries<DP>(x.q, a.D, sQ + s * TILE, 32 * w);
       }
       off = wait(&o_full[s], nf++);
       if (off) break;
@@ -719,7 +698,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         }
         if (off) break;
       }
-      if (next) fetch_queries<DP>(x, a.D, sQ, warp);
+      if (next) fetch_queries<DP>(x.q, a.D, sQ, 32 * warp);
       if (have) {
         off = wait(&o_full, nf - 1);
         if (off) break;

@@ -127,7 +127,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
 // for every tile. Bound by the keys' bytes up to about 256 query rows a head.
 constexpr int KT = 128, QB = 128, Q_STAGES = 3;
 constexpr int WT_THREADS = 384;
-constexpr int PANEL = KT * 128;
+constexpr int PANEL = TILE_PANEL;
 
 template <int DP>
 struct WShape {
@@ -275,7 +275,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     commit(&done);
     mbar_drain(&done, 0);
   } else if (warp >= 10) {
-    const int pw = warp - 10, np = 2 * ((a.D + 15) / 16);
+    const int pw = warp - 10;
     Walk walk(a, plan, blockIdx.x, start);
     Frag f;
     while (!off && walk.next(a, plan, f)) {
@@ -284,7 +284,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       // what no row of the head is kept from: needed before the first block is there
       int low = len;
       for (int r = lane; r < rows; r += 32) {
-        const int i = r / a.G, g = r - i * a.G;
+        const int i = a.by_G.of(r), g = r - i * a.G;
         const long long token = (long long)f.b * a.L + i;
         if (a.visible) low = min(low, max(0, a.visible[token]));
         if (a.lse[token * (a.Hkv * a.G) + f.h * a.G + g] == -INFINITY) low = 0;
@@ -295,38 +295,24 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       if (lane == 0) mbar_arrive(&f_full[fs]);
       ++nf;
       for (int x = 0; x < loads; ++x, ++nq) {
-        const int qs = nq % Q_STAGES, first = (x % nb) * QB, count = min(QB, rows - first), padded = (count + 15) & ~15;
+        const int qs = nq % Q_STAGES, first = (x % nb) * QB, count = min(QB, rows - first);
         if (nq >= Q_STAGES && (off = wait(&q_empty[qs], nq / Q_STAGES - 1))) break;
-        for (int r0 = 32 * pw; r0 < padded; r0 += 64) {
+        for (int r0 = 32 * pw; r0 < count; r0 += 64) {
           const int r = r0 + lane;
           const __nv_bfloat16* src = nullptr;
-          if (r < padded) {
-            float ls = 0.f;
-            int lim = 0;
-            if (r < count) {
-              const int i = (first + r) / a.G, head = f.h * a.G + (first + r - i * a.G);
-              const long long token = (long long)f.b * a.L + i;
-              ls = a.lse[token * (a.Hkv * a.G) + head] * LOG2E;
-              lim = a.visible ? min(len, a.visible[token]) : len;
-              if (ls == -INFINITY) ls = 0.f, lim = 0;        // a row that saw nothing
-              src = static_cast<const __nv_bfloat16*>(a.q.p) + f.b * a.q.seq + i * a.q.tok + head * a.q.head;
-            }
-            neg_lse[qs][r] = -ls;
-            row_lim[qs][r] = lim;
+          float ls = 0.f;
+          int lim = 0;
+          if (r < count) {
+            const int i = a.by_G.of(first + r), head = f.h * a.G + (first + r - i * a.G);
+            const long long token = (long long)f.b * a.L + i;
+            src = static_cast<const __nv_bfloat16*>(a.q.p) + f.b * a.q.seq + i * a.q.tok + head * a.q.head;
+            ls = a.lse[token * (a.Hkv * a.G) + head] * LOG2E;
+            lim = a.visible ? min(len, a.visible[token]) : len;
           }
-          const int c = lane & 15, last = min(32, padded - r0);
-          uint8_t* dst = sQ + qs * TILE + (c >> 3) * PANEL;
-          for (int i = 0; i < last; i += 2) {
-            const int in = i + (lane >> 4), at = r0 + in;
-            const unsigned long long from = __shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(src), in);
-            if (c >= np || in >= last) continue;
-            const uint32_t to = su32(dst + at * 128 + ((c & 7) ^ (at & 7)) * 16);
-            if (8 * c < a.D && from)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from + 16 * c) : "memory");
-            else
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
-          }
-          __syncwarp();
+          fetch_queries<DP>(src, a.D, sQ + qs * TILE, r0);
+          if (ls == -INFINITY) ls = 0.f, lim = 0;  // a row that saw nothing
+          neg_lse[qs][r] = -ls;
+          row_lim[qs][r] = lim;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         fence_async_smem();
