@@ -354,8 +354,8 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
           __syncwarp();
         }
       }
-      if (off)
-        for (unsigned p = cur > STAGES ? cur - STAGES : 0; p < cur; ++p) mbar_drain(&full[p % STAGES], (p / STAGES) & 1);
+      // (whoever reads the tiles may have given up: none is on its way when the CTA ends)
+      for (unsigned p = cur > STAGES ? cur - STAGES : 0; p < cur; ++p) mbar_drain(&full[p % STAGES], (p / STAGES) & 1);
     } else if (warp < 11) {
       // products of a slot, issued by one lane; the warp stays together around it. A warp a slot: one's
       // waits do not keep the tensor cores from the other's products.
@@ -497,6 +497,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       }
       tc_fence_before();
     }
+    rows_fetched();                                // (nor queries, where a wait gave up)
   }
   tc_fence_before();
   __syncthreads();
@@ -601,8 +602,8 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         __syncwarp();
       }
     }
-    if (off)
-      for (unsigned p = cur > STAGES ? cur - STAGES : 0; p < cur; ++p) mbar_drain(&full[p % STAGES], (p / STAGES) & 1);
+    // (whoever reads the tiles may have given up: none is on its way when the CTA ends)
+    for (unsigned p = cur > STAGES ? cur - STAGES : 0; p < cur; ++p) mbar_drain(&full[p % STAGES], (p / STAGES) & 1);
   } else if (warp == 5) {
     const int nd = (a.D + 15) / 16;                // 16 columns a step of Q K^T, and a unit of O's width
     const uint32_t id_o = idesc_bf16(SLOT, 16 * nd) | IDESC_B_MN;
@@ -740,6 +741,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       have = true;
       u += f.n;
     }
+    rows_fetched();                                // (queries, where a wait gave up)
   }
   tc_fence_before();
   __syncthreads();

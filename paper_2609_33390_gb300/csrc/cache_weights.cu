@@ -225,8 +225,8 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         __syncwarp();
       }
-    if (off)
-      for (int p = unit > STAGES ? unit - STAGES : 0; p < unit; ++p) mbar_drain(&k_full[p % STAGES], (p / STAGES) & 1);
+    // (whoever reads the tiles may have given up: none is on its way when the CTA ends)
+    for (int p = unit > STAGES ? unit - STAGES : 0; p < unit; ++p) mbar_drain(&k_full[p % STAGES], (p / STAGES) & 1);
   } else if (warp == 9) {
     const int nd = (a.D + 15) / 16;
     const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring));
