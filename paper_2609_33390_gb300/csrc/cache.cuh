@@ -8,7 +8,7 @@
 
 namespace brisk {
 
-constexpr int CACHE_MAX_B = 4096;    // sequences of a call (every CTA holds their tile counts)
+constexpr int CACHE_MAX_B = 4096;    // sequences of a call (the join's CTAs hold the tiles before each)
 constexpr int CACHE_MAX_D = 128;     // width of a head
 constexpr int CACHE_SMS = 152;
 
@@ -287,11 +287,19 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
 }
 
 // Keys of a tile, rows of it, and CTAs: bf16 on the tensor cores, fp32 on the FMA units. With bf16 and more
-// than SLOT_ROWS query rows a key head, the prefix has a kernel of its own.
+// than SLOT_ROWS query rows a key head, the prefix has a kernel of its own from APART_UNITS of its units on.
+// That kernel reads a key tile for twice the rows, but is one more launch and divides the prefix by itself: 32 query
+// heads on 8, own caches of up to 300, R rows a key head: U units of it take, with and without it,
+//   U 64 (R 512): 29.4 and 25.0 us; 256 (512): 34.8 and 34.8; 512 (1024): 34.5 and 42.6; 1024 (2048): 48.6 and 65.2;
+//   4096 (4096): 97 and 167.
 constexpr int TC_KT = 128, SLOT_ROWS = 128, PAIR_ROWS = 256, SIMT_KT = 64, SIMT_ROWS = 64;
 constexpr int SLOT_CTAS = 2 * CACHE_SMS;             // (the fp32 kernel's, too)
+constexpr int APART_UNITS = 2 * CACHE_SMS;
 inline void divide(AttendArgs* a) {
-  const bool tc = a->dt == BRISK_DT_BF16, apart = tc && a->P > 0 && (long long)a->B * a->L * a->G > SLOT_ROWS;
+  const bool tc = a->dt == BRISK_DT_BF16;
+  const long long R = (long long)a->B * a->L * a->G;
+  const long long units = a->Hkv * ((R + PAIR_ROWS - 1) / PAIR_ROWS) * (((long long)a->P + TC_KT - 1) / TC_KT);
+  const bool apart = tc && R > SLOT_ROWS && units >= APART_UNITS;
   a->kt = tc ? TC_KT : SIMT_KT;
   a->rt_o = tc ? SLOT_ROWS : SIMT_ROWS;
   a->rt_p = apart ? PAIR_ROWS : a->rt_o;
