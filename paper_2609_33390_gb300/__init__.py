@@ -2,12 +2,13 @@
 
 The compute runs in the CUDA library built from ``csrc/``; ``brisk`` is its
 thin ctypes binding (loaded on first use); ``loop`` drives captured tails block after
-block with double-buffered inputs. ``synth`` builds seeded synthetic inputs shaped like the
+block with double-buffered inputs; ``context`` decodes blocks over a shared prompt and bounded own
+caches. ``synth`` builds seeded synthetic inputs shaped like the
 paper's workloads.
 """
 import importlib
 
-__all__ = ["synth", "brisk", "build", "loop"]
+__all__ = ["synth", "brisk", "build", "loop", "context"]
 
 
 def __getattr__(name):
