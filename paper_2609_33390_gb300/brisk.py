@@ -446,6 +446,8 @@ class PrefixAttention:
         if ws == 0:
             raise BriskError(ERR_INVALID_ARG, "dims")
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=self.device)
+        if self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()   # calls may go to any stream
         self.scale = D ** -0.5
         self._d = ctypes.addressof(self.dims)
         self._ws = self.workspace.data_ptr()
@@ -529,10 +531,12 @@ class PrefixAttention:
 
     def alloc_evicted(self, keep, room=None):
         """Targets of evict(): caches [B, room, Hkv, D] (room: ``keep`` unless given), sums and kept
-        indices [B, Hkv, keep], lengths [B]."""
+        indices [B, Hkv, keep], lengths [B]; zeros, written on the current stream."""
+        return self._evicted(torch.zeros, keep, keep if room is None else room)
+
+    def _evicted(self, make, keep, room):
         B, Hkv, D = self.B, self.Hkv, self.D
-        room = keep if room is None else room
-        new = lambda shape, dt: torch.zeros(shape, dtype=dt, device=self.device)
+        new = lambda shape, dt: make(shape, dtype=dt, device=self.device)
         return {"k": new((B, room, Hkv, D), self.dtype), "v": new((B, room, Hkv, D), self.dtype),
                 "acc": new((B, Hkv, keep), torch.float32),
                 "own_len": new((B,), torch.int32), "kept": new((B, Hkv, keep), torch.int32)}
@@ -542,7 +546,8 @@ class PrefixAttention:
         all, to the caches of ``out`` (see alloc_evicted and brisk_cache_evict): between two layers,
         one spare pair of caches serves them all in turn."""
         if out is None:
-            out = self.alloc_evicted(keep)
+            # (the call writes all of them, on its own stream)
+            out = self._evicted(torch.empty, keep, keep)
         plain, view, at, f32, i32 = self._plain, self._view, self._at, torch.float32, torch.int32
         k_to, B, Hkv = out["k"], self.B, self.Hkv
         room = k_to.shape[1]

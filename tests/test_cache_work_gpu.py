@@ -213,3 +213,25 @@ def test_expired_waits_are_reported_and_the_next_call_is_right(B, size):
         acc2 = sums(again)
         assert att.device_status() == B.OK
         assert torch.equal(again["out"], ref["out"]) and torch.equal(again["lse"], ref["lse"]) and torch.equal(acc, acc2)
+
+
+def test_calls_on_a_stream_do_not_wait_for_the_current_one(B):
+    """What a call allocates is not written on the current stream, which may be far behind."""
+    size = (3, 2, 8, 2, 64, 100, 60)
+    x = inputs(*size, [60, 40, 5], False, BF)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def run(stream=None):
+        att = B.PrefixAttention(*size, BF)
+        if stream is not None:
+            torch.cuda._sleep(20_000_000)              # about 10 ms of the current stream
+        r = att.attend(x["q"], x["kp"], x["vp"], x["ko"], x["vo"], x["lens"], stream=stream)
+        w = att.weights(x["q"], r["lse"], x["ko"], x["lens"], stream=stream)
+        e = att.evict(x["ko"], x["vo"], w, x["lens"], 30, 5, stream=stream)
+        torch.cuda.synchronize()
+        assert att.device_status() == B.OK
+        return [r["out"], r["lse"], w, *e.values()]
+
+    for a, b in zip(run(), run(s)):
+        assert torch.equal(a, b)
