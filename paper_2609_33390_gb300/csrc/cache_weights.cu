@@ -118,6 +118,90 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   }
 }
 
+// At most R <= 8 query rows a head, as single tokens have them: 4 lanes share a key, 16 bytes of it in turn, from
+// memory to registers, and a warp has 16 keys. Bound by the keys' bytes (64 single tokens over 1000 to 2000 entries,
+// 32 heads on 8, D = 128: 95 us, 4.2 TB/s; 8 heads on 8, D = 64: 61 us, in tiles of 64 rows 161). The loads land in
+// L1, which therefore gets what shared memory does not need: with the least of L1 129 us.
+constexpr int CARVEOUT_LEAST_KB = 16;     // of shared memory: two CTAs' queries
+constexpr int WF_KEYS = 16 * (W_THREADS / 32);
+template <int R>
+__global__ void __launch_bounds__(W_THREADS, 2)
+weights_few_kernel(const __grid_constant__ WeightArgs a) {
+  constexpr int CH = CACHE_MAX_D / 16;
+  __shared__ __align__(16) float sQ[R][CACHE_MAX_D];
+  __shared__ float sL[R];
+  __shared__ int sLim[R];
+  const int tid = threadIdx.x, lane = tid & 31, D = a.D, rows = a.L * a.G;
+  const int tiles = (a.S + WF_KEYS - 1) / WF_KEYS;
+  const long long item = blockIdx.x / tiles;
+  const int t0 = (int)(blockIdx.x % tiles) * WF_KEYS, b = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
+  const int len = clamped_len(a, b);
+  if (blockIdx.x == 0) {                   // the call's status: the lengths that were clamped
+    bool bad = false;
+    for (int i = tid; i < a.B; i += W_THREADS) bad |= a.own_len[i] < 0 || a.own_len[i] > a.S;
+    bad = __syncthreads_or(bad);
+    if (tid == 0) *a.status = bad ? BRISK_ERR_INVALID_ARG : BRISK_OK;
+  }
+  float sum[2] = {0.f, 0.f};
+  const int key = t0 + (tid >> 5) * 16 + (lane >> 2);        // and 8 further
+  if (t0 < len) {
+    const float* kb = static_cast<const float*>(a.ko.p) + b * a.ko.seq + h * a.ko.head;
+    ulonglong2 k[2][CH];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const int c = 4 * (4 * j + (lane & 3));
+        k[e][j] = make_ulonglong2(0, 0);
+        if (key + 8 * e < len && c < D) k[e][j] = *reinterpret_cast<const ulonglong2*>(kb + (key + 8 * e) * a.ko.tok + c);
+      }
+    const int nq = 4 * ((D + 15) / 16);    // (columns that lanes without a piece of a key multiply by zeros)
+    for (int e = tid; e < rows * nq; e += W_THREADS) {
+      const int r = e / nq, c = 4 * (e - r * nq), i = r / a.G;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c < D) v = load4(static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok + (h * a.G + (r - i * a.G)) * a.q.head + c);
+      store4(&sQ[r][c], v);
+    }
+    if (tid < rows) {
+      const int i = tid / a.G;
+      const long long token = (long long)b * a.L + i;
+      const float ls = a.lse[token * (a.Hkv * a.G) + h * a.G + (tid - i * a.G)] * LOG2E;
+      sL[tid] = ls;
+      // (a row that saw nothing gives nothing)
+      sLim[tid] = ls == -INFINITY ? 0 : (a.visible ? min(len, a.visible[token]) : len);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= rows) break;
+      f32x2 x[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        if (16 * j >= D) break;
+        const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&sQ[r][4 * (4 * j + (lane & 3))]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[e] = fma2(q.y, k[e][j].y, fma2(q.x, k[e][j].x, x[e]));
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float y, z;
+        unpack2(x[e], y, z);
+        y += z;
+        y += __shfl_xor_sync(FULL_MASK, y, 1);
+        y += __shfl_xor_sync(FULL_MASK, y, 2);
+        if (key + 8 * e < sLim[r]) sum[e] += ex2(y * a.sl2 - sL[r]);
+      }
+    }
+  }
+  const int t = key + 8 * (lane & 1);      // two of a key's lanes have a key each to write
+  if ((lane & 3) < 2 && t < a.S) {
+    float w = sum[lane & 1];
+    const long long at = item * a.S + t;
+    if (a.acc_in && t < len) w += a.decay * a.acc_in[at];
+    a.acc_out[at] = t < len ? w : 0.f;
+  }
+}
+
 // ---------------------------------------------------------------- bf16, on the tensor cores
 // S^T = K Q^T: 128 keys are the rows of the product, up to 128 query rows its columns, so that a thread
 // holds one key's scores and adds up its weights. The CTAs share the units (sequence, head, key tile)
@@ -193,10 +277,10 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   int own = 0;
   scan_lengths<WT_THREADS>(a, KT, nullptr, warp_sum, &bad, &start, [&](int total) {
     own = total;
-    const Plan p(a.B, rows, a.Hkv, 0, 1, rows, KT, total, 0, a.grid);
+    const Plan p(a.B, rows, a.Hkv, 0, 1, rows, KT, total, 0, a.grid, 1);
     return units_of(blockIdx.x, p.share_o, p.UO).x / a.Hkv;
   });
-  const Plan plan(a.B, rows, a.Hkv, 0, 1, rows, KT, own, 0, a.grid);
+  const Plan plan(a.B, rows, a.Hkv, 0, 1, rows, KT, own, 0, a.grid, 1);
   const int2 range = units_of(blockIdx.x, plan.share_o, plan.UO);
   const int units = range.y - range.x;
   // sequences without entries have no units: zeros everywhere
@@ -426,15 +510,18 @@ cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream) {
 }
 
 cudaError_t launch_weights_simt(const WeightArgs& a, cudaStream_t stream) {
-  const size_t smem = sizeof(float) * (W_KEYS * WS + W_ROWS * CACHE_MAX_D + 2 * W_ROWS);
-  const long long grid = (long long)a.B * a.Hkv * ((a.S + W_KEYS - 1) / W_KEYS);
-  auto run = [&](auto kernel) {
-    cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
+  const int rows = a.L * a.G;
+  auto run = [&](auto kernel, int keys, size_t smem) {
+    cudaError_t e = set_up_kernel(kernel, smem ? CARVEOUT_FULL_KB : CARVEOUT_LEAST_KB, smem);
     if (e != cudaSuccess) return e;
+    const long long grid = (long long)a.B * a.Hkv * ((a.S + keys - 1) / keys);
     kernel<<<(unsigned)grid, W_THREADS, smem, stream>>>(a);
     return cudaGetLastError();
   };
-  return run(weights_simt_kernel);
+  if (rows <= 2) return run(weights_few_kernel<2>, WF_KEYS, 0);
+  if (rows <= 4) return run(weights_few_kernel<4>, WF_KEYS, 0);
+  if (rows <= FEW_ROWS) return run(weights_few_kernel<8>, WF_KEYS, 0);
+  return run(weights_simt_kernel, W_KEYS, sizeof(float) * (W_KEYS * WS + W_ROWS * CACHE_MAX_D + 2 * W_ROWS));
 }
 
 }  // namespace brisk
