@@ -43,7 +43,7 @@ struct AttendArgs {
   int dt;                            // brisk_dtype of q, keys, values and out
   // division of the work (see Plan): rows and keys of a tile; CTAs of the kernel for the prefix (0: the one
   // for the own caches has both) and of the one for the own caches
-  int rt_p, rt_o, kt, grid_p, grid_o;
+  int rt_p, rt_o, kt, grid_p, grid_o, weight;
   CacheView q, kp, vp, ko, vo;
   Divisor by_L, by_G, by_LG;         // L, G and L * G
   const int32_t* own_len;            // [B]
@@ -67,9 +67,12 @@ struct AttendArgs {
 // sequences form common tiles (its keys are read once for rt_p rows, whichever sequence they are of);
 // over the own caches, the rows of one sequence. The units stand in one sequence: first the prefix's
 // (by head, row tile, key tile), then the own caches' (by sequence, head, row tile, key tile), and
-// each CTA takes `share` of them, wherever that begins and ends; or the prefix's and the own caches' are
-// two sequences of two kernels (apart), the own caches' first. A row tile's keys may so be divided over several CTAs, each of
-// which leaves a part; the parts are joined by merge_kernel.
+// each CTA takes `share` of them, wherever that begins and ends; or the prefix's and the own caches' are two
+// sequences of two kernels (apart), the own caches' first. A row tile's keys may so be divided over several CTAs,
+// each of which leaves a part; the parts are joined by a merge kernel.
+// Where a prefix's unit takes far longer than an own one (fp32, few rows a sequence), it counts as `weight`
+// units, in the CTA that has the first of them. (A share is at least a weight: no CTA between two of the prefix's
+// parts is without one.)
 // Slots: walking through a sequence, (item index + CTA) grows with every (item, CTA) pair, so it
 // numbers the parts. Counts of units fit 31 bits (checked on the host).
 struct Plan {
@@ -77,10 +80,14 @@ struct Plan {
   int nPT, kP, nLT;                  // row tiles and key tiles of the prefix; row tiles of a sequence
   int R, UP, UO;                     // rows a key head; units of the prefix and of the own caches
   int own0;                          // number of the own caches' first unit
+  int weight;                        // units that one of the prefix's counts as
   int share_p, share_o;              // units a CTA
   int log_p, log_o;                  // rt_p and rt_o as powers of two, where they are
+  bool apart;                        // the prefix's units and the own caches' are two sequences
 
-  __device__ Plan(int b, int lg, int hkv, int p, int rtp, int rto, int kt_, int own_tiles, int grid_p, int grid_o) {
+  Plan() = default;
+  __device__ Plan(int b, int lg, int hkv, int p, int rtp, int rto, int kt_, int own_tiles, int grid_p, int grid_o,
+                  int weight_) {
     B = b; LG = lg; Hkv = hkv; rt_p = rtp; rt_o = rto; kt = kt_;
     R = B * LG;
     kP = (p + kt - 1) / kt;
@@ -88,15 +95,17 @@ struct Plan {
     nLT = (LG + rt_o - 1) / rt_o;
     UP = Hkv * nPT * kP;
     UO = Hkv * nLT * own_tiles;
-    const bool apart = grid_p > 0;
-    own0 = apart ? 0 : UP;
+    apart = grid_p > 0;
+    const unsigned all = (unsigned)UP * weight_ + UO;          // (UP and UO: up to 2e9 together)
+    weight = UP < (1 << 28) && all < (1u << 31) && all / grid_o >= (unsigned)weight_ ? weight_ : 1;
+    own0 = apart ? 0 : UP * weight;
     share_o = max(1, (int)(((unsigned)own0 + UO + grid_o - 1) / grid_o));
     log_p = 31 - __clz(rt_p);
     log_o = 31 - __clz(rt_o);
     share_p = apart ? max(1, (int)(((unsigned)UP + grid_p - 1) / grid_p)) : share_o;
   }
   __device__ Plan(const AttendArgs& a, int own_tiles)
-      : Plan(a.B, a.L * a.G, a.Hkv, a.P, a.rt_p, a.rt_o, a.kt, own_tiles, a.grid_p, a.grid_o) {}
+      : Plan(a.B, a.L * a.G, a.Hkv, a.P, a.rt_p, a.rt_o, a.kt, own_tiles, a.grid_p, a.grid_o, a.weight) {}
   __device__ int tiles(int len) const { return (len + kt - 1) / kt; }
 };
 
@@ -122,18 +131,25 @@ __device__ __forceinline__ int clamped_len(const Args& a, int b) {
   return min(max(a.own_len[b], 0), a.S);
 }
 
-// Walks through the units of a kernel that has the own caches' (and, unless apart, the prefix's).
+// Walks through a CTA's units: the prefix's (unless another kernel has them, apart), then the own caches'.
 struct Walk {
-  int u, end, c, b, base, n, len;    // b: sequence whose units begin at `base`, n key tiles
+  int pu, pend;                      // the prefix's next unit and their end
+  int u, end, c, b, base, n, len;    // the own ones'; b: sequence whose units begin at `base`, n key tiles
 
+  Walk() = default;
   template <typename Args>
   __device__ Walk(const Args& a, const Plan& p, int cta, const Start& start) {
     const int2 r = units_of(cta, p.share_o, p.own0 + p.UO);
-    u = r.x;
+    pu = pend = 0;
+    if (!p.apart && r.x < p.own0) {
+      pu = (r.x + p.weight - 1) / p.weight;
+      pend = (min(r.y, p.own0) + p.weight - 1) / p.weight;
+    }
+    u = max(r.x, p.own0);
     end = r.y;
     c = cta;
     b = base = n = len = 0;
-    if (u < end && end > p.own0) {   // (a CTA without own units has no start)
+    if (u < end) {                   // (a CTA without own units has no start)
       b = start.b;
       base = p.own0 + p.Hkv * p.nLT * start.before;
       len = clamped_len(a, b);
@@ -142,12 +158,11 @@ struct Walk {
   }
   template <typename Args>
   __device__ bool next(const Args& a, const Plan& p, Frag& f) {
-    if (u >= end) return false;
-    if (u < p.own0) {
-      const int item = u / p.kP;
+    if (pu < pend) {
+      const int item = pu / p.kP;
       f.prefix = 1;
-      f.k0 = u - item * p.kP;
-      f.n = min(p.kP - f.k0, end - u);
+      f.k0 = pu - item * p.kP;
+      f.n = min(p.kP - f.k0, pend - pu);
       f.h = item / p.nPT;
       f.b = 0;
       f.row0 = (item - f.h * p.nPT) * p.rt_p;
@@ -155,26 +170,28 @@ struct Walk {
       f.slot = item + c;
       f.whole = f.n == p.kP && a.S == 0;
       f.len = a.P;
-    } else {
-      const int per = p.Hkv * p.nLT;
-      while (u >= base + per * n) {
-        base += per * n;
-        ++b;
-        len = clamped_len(a, b);
-        n = p.tiles(len);
-      }
-      const int r = (u - base) / n, tile = r % p.nLT;
-      f.prefix = 0;
-      f.b = b;
-      f.h = r / p.nLT;
-      f.k0 = u - base - r * n;
-      f.n = min(n - f.k0, end - u);
-      f.row0 = tile * p.rt_o;
-      f.rows = min(p.rt_o, p.LG - f.row0);
-      f.slot = b * per + r + c;
-      f.whole = f.n == n && p.UP == 0;
-      f.len = len;
+      pu += f.n;
+      return true;
     }
+    if (u >= end) return false;
+    const int per = p.Hkv * p.nLT;
+    while (u >= base + per * n) {
+      base += per * n;
+      ++b;
+      len = clamped_len(a, b);
+      n = p.tiles(len);
+    }
+    const int r = (u - base) / n, tile = r % p.nLT;
+    f.prefix = 0;
+    f.b = b;
+    f.h = r / p.nLT;
+    f.k0 = u - base - r * n;
+    f.n = min(n - f.k0, end - u);
+    f.row0 = tile * p.rt_o;
+    f.rows = min(p.rt_o, p.LG - f.row0);
+    f.slot = b * per + r + c;
+    f.whole = f.n == n && p.UP == 0;
+    f.len = len;
     u += f.n;
     return true;
   }
@@ -253,8 +270,9 @@ struct Parts {
 __device__ __forceinline__ Parts prefix_parts(const AttendArgs& a, const Plan& p, const Divisor& by_share_p, int h, int r) {
   Parts x{0, min(p.rt_p, p.R), nullptr, nullptr};
   if (p.kP == 0) return x;
-  const int pt = r >> p.log_p, first = (h * p.nPT + pt) * p.kP, c0 = by_share_p.of(first), slot = h * p.nPT + pt + c0;
-  x.n = by_share_p.of(first + p.kP - 1) - c0 + 1;
+  const int pt = r >> p.log_p, first = (h * p.nPT + pt) * p.kP;
+  const int c0 = by_share_p.of(first * p.weight), slot = h * p.nPT + pt + c0;
+  x.n = by_share_p.of((first + p.kP - 1) * p.weight) - c0 + 1;
   x.sums = a.part_p + part_at(slot, x.per, a.D, r - (pt << p.log_p), 0);
   x.ml = a.ml_p + (long long)slot * x.per + (r - (pt << p.log_p));
   return x;
@@ -295,6 +313,11 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
 constexpr int TC_KT = 128, SLOT_ROWS = 128, PAIR_ROWS = 256, SIMT_KT = 64, SIMT_ROWS = 64;
 constexpr int SLOT_CTAS = 2 * CACHE_SMS;             // (the fp32 kernel's, too)
 constexpr int APART_UNITS = 2 * CACHE_SMS;
+// fp32: up to FEW_ROWS rows of a sequence have a form of their own (64 single tokens, 32 heads on 8, D = 128, over
+// 1000 to 2000 own and 2000 shared entries: 216 us, with the form for more rows 685 us). One of its units takes about
+// a sixth (up to 4 rows) or a fourth of the time of a prefix's unit of a full tile: counting the latter as 1, 4, 5
+// and 6 units 571, 239, 215 and 216 us, 8 rows 626, 366, 399 and 429 us.
+constexpr int FEW_ROWS = 8;
 inline void divide(AttendArgs* a) {
   const bool tc = a->dt == BRISK_DT_BF16;
   const long long R = (long long)a->B * a->L * a->G;
@@ -305,6 +328,8 @@ inline void divide(AttendArgs* a) {
   a->rt_p = apart ? PAIR_ROWS : a->rt_o;
   a->grid_p = apart ? CACHE_SMS : 0;
   a->grid_o = SLOT_CTAS;
+  const int rows = a->L * a->G;
+  a->weight = !tc && R > FEW_ROWS && rows <= FEW_ROWS ? (rows <= 4 ? 6 : 4) : 1;
 }
 
 // A tile of 128 rows in shared memory, as the products read it: panels of 64 columns, 128 bytes a row, the

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from test_cache_gpu import BF, F32, U, caches
+from test_cache_gpu import test_hidden_entries_do_not_reach_the_rows as hidden_entries
 
 pytestmark = pytest.mark.gpu
 
@@ -157,10 +158,23 @@ def test_one_sequence_much_longer_than_the_others(B, mask):
     (2, 50, 12, 3, 96, 0, 1000),
     (50, 20, 10, 10, 24, 130, 70),
     (3, 1, 1, 1, 8, 5000, 3000),
+    (4, 1, 2, 1, 128, 700, 5000),         # up to 8 rows: keys and values straight from memory
+    (9, 2, 14, 7, 72, 40, 2000),
+    (30, 1, 20, 4, 104, 0, 777),
+    (5, 3, 4, 2, 40, 3000, 1025),
+    (6, 2, 16, 4, 64, 2001, 600),
+    (1, 1, 7, 1, 120, 9000, 9000),
+    (5, 5, 10, 5, 56, 300, 400),          # 10
 ])
 def test_divided_work_fp32(B, size, mask):
     Bn, L, Hq, Hkv, D, P, S = size
     check(B, inputs(*size, lens_of(Bn, S), mask, F32), S)
+
+
+@pytest.mark.parametrize("L,G", [(2, 1), (2, 2), (4, 2)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_hidden_entries_with_few_rows(B, bad, L, G):
+    hidden_entries(B, bad, L, G, F32)
 
 
 def test_two_handles_on_two_streams(B):
