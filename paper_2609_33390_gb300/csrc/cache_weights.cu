@@ -207,9 +207,12 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
 // holds one key's scores and adds up its weights. The CTAs share the units (sequence, head, key tile)
 // evenly. One warp streams key tiles by TMA, one issues the products into four score buffers in TMEM,
 // two put blocks of 128 queries with their log-sums into a ring, and two groups of four warps take
-// the key tiles in turn. Up to two blocks of queries stay for all key tiles of a head; more are read again
-// for every tile. Bound by the keys' bytes up to about 256 query rows a head.
-constexpr int KT = 128, QB = 128, Q_STAGES = 3;
+// the key tiles in turn. A pass is up to two blocks of queries, which stay, over a run of key tiles: all of a
+// fragment where there are no more blocks; else the blocks take turns on runs of CHUNK tiles, and later passes add
+// to the sums that the first one wrote. Bound by the keys' bytes up to 128 rows a head, by the exponentials beyond:
+// 64 sequences of 4096 entries, 8 key heads of 128, 32, 128, 256, 384 and 512 rows a head 95 us (5.9 TB/s), 100, 170,
+// 238 and 324 us (862 TFLOP/s; runs of 8 and 16 tiles: 382 and 345, all blocks for every tile 964).
+constexpr int KT = 128, QB = 128, Q_STAGES = 3, CHUNK = 32;
 constexpr int WT_THREADS = 384;
 constexpr int PANEL = TILE_PANEL;
 
@@ -220,9 +223,38 @@ struct WShape {
   static constexpr int SMEM = 1024 + (Q_STAGES + STAGES) * TILE;
 };
 
-struct WInfo {
+// A pass: nq blocks of queries from q0 on over key tiles [k0, k0 + n); n = 0 after the last.
+struct Pass {
   int b, h, k0, n, len, low, last;       // low: entries from here on are hidden from some row; last: the
-};                                       // sequence's last tile is among these
+  int q0, nq, odd;                       // sequence's last tile is among these; odd: number of tiles before, modulo 2
+};
+
+// A CTA's passes in order.
+struct Passes {
+  Walk walk;
+  Frag f;
+  int at, n, q0, before;                 // tiles of the fragment before this run; the run's; the next block; tiles before the run
+
+  __device__ Passes(const WeightArgs& a, const Plan& plan, const Start& start, int nb) : walk(a, plan, blockIdx.x, start) {
+    f.n = at = n = before = 0;
+    q0 = nb;
+  }
+  __device__ bool next(const WeightArgs& a, const Plan& plan, int nb, Pass& p) {
+    if (q0 >= nb) {
+      at += n;
+      before += n;
+      q0 = 0;
+      if (at >= f.n) {
+        if (!walk.next(a, plan, f)) return false;
+        at = 0;
+      }
+      n = nb > 2 ? min(CHUNK, f.n - at) : f.n;
+    }
+    p = Pass{f.b, f.h, f.k0 + at, n, f.len, 0, f.k0 + at + n == plan.tiles(f.len), q0, min(2, nb - q0), before & 1};
+    q0 += 2;
+    return true;
+  }
+};
 
 template <int DP>
 __global__ void __launch_bounds__(WT_THREADS, 1)
@@ -237,7 +269,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ __align__(16) int row_lim[Q_STAGES][QB];
   __shared__ uint64_t k_full[STAGES], k_empty[STAGES], q_full[Q_STAGES], q_empty[Q_STAGES];
   __shared__ uint64_t s_full[4], s_empty[4], f_full[2], f_empty[2], done;
-  __shared__ WInfo info[2];
+  __shared__ Pass info[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int aborted, bad, warp_sum[WT_THREADS / 32];
   __shared__ Start start;
@@ -281,8 +313,6 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     return units_of(blockIdx.x, p.share_o, p.UO).x / a.Hkv;
   });
   const Plan plan(a.B, rows, a.Hkv, 0, 1, rows, KT, own, 0, a.grid, 1);
-  const int2 range = units_of(blockIdx.x, plan.share_o, plan.UO);
-  const int units = range.y - range.x;
   // sequences without entries have no units: zeros everywhere
   for (int b = blockIdx.x; b < a.B; b += gridDim.x)
     if (clamped_len(a, b) == 0)
@@ -290,15 +320,15 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 
   // (a warp that is told that a wait gave up leaves its loop for the barrier at the end)
   auto wait = [&](uint64_t* bar, int phase) { return warp_wait(bar, phase, abort_flag, a.wait_limit); };
-  int unit = 0, nf = 0, nq = 0;                    // units, fragments and blocks of queries before
+  unsigned unit = 0, nf = 0, nq = 0;               // tiles, passes and blocks of queries before
   bool off = false;
 
   if (warp == 8) {
-    Walk walk(a, plan, blockIdx.x, start);
-    Frag f;
-    while (!off && walk.next(a, plan, f))
+    Passes passes(a, plan, start, nb);
+    Pass f;
+    while (!off && passes.next(a, plan, nb, f))
       for (int j = 0; j < f.n; ++j, ++unit) {
-        const int st = unit % STAGES;
+        const unsigned st = unit % STAGES;
         off = unit >= STAGES && wait(&k_empty[st], unit / STAGES - 1);
         if (off) break;
         if (elect_one()) {
@@ -310,34 +340,35 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         __syncwarp();
       }
     // (whoever reads the tiles may have given up: none is on its way when the CTA ends)
-    for (int p = unit > STAGES ? unit - STAGES : 0; p < unit; ++p) mbar_drain(&k_full[p % STAGES], (p / STAGES) & 1);
+    for (unsigned p = unit > STAGES ? unit - STAGES : 0; p < unit; ++p) mbar_drain(&k_full[p % STAGES], (p / STAGES) & 1);
   } else if (warp == 9) {
     const int nd = (a.D + 15) / 16;
     const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring));
-    int ns[2] = {0, 0};                            // score buffers a group was given
+    unsigned ns[2] = {0, 0};                       // score buffers a group was given
     auto commit = [&](uint64_t* bar) {
       if (elect_one()) umma_commit(bar);
       __syncwarp();
     };
-    while (unit < units && !off) {
-      const int fs = nf & 1;
+    while (!off) {
+      const unsigned fs = nf & 1;
       off = wait(&f_full[fs], nf >> 1);
       if (off) break;
-      const int n = info[fs].n;
+      const int n = info[fs].n, q0 = info[fs].q0, blocks = info[fs].nq, odd = info[fs].odd;
       __syncwarp();
       if (lane == 0) mbar_arrive(&f_empty[fs]);
       ++nf;
+      if (n == 0) break;
       for (int j = 0; j < n && !off; ++j, ++unit) {
-        const int g = unit & 1, st = unit % STAGES;
+        const int g = (odd + j) & 1;
+        const unsigned st = unit % STAGES;
         off = wait(&k_full[st], unit / STAGES);
-        for (int blk = 0; blk < nb && !off; ++blk) {
-          const int qi = nq + (nb > 2 ? j * nb : 0) + blk, qs = qi % Q_STAGES;
-          const int buf = 2 * g + (ns[g] & 1);
+        for (int blk = 0; blk < blocks && !off; ++blk) {
+          const unsigned qi = nq + blk, qs = qi % Q_STAGES, buf = 2 * g + (ns[g] & 1);
           off = wait(&q_full[qs], qi / Q_STAGES) || (ns[g] >= 2 && wait(&s_empty[buf], (ns[g] >> 1) - 1));
           if (off) break;
           ++ns[g];
           tc_fence_after();
-          const int cols = (min(QB, rows - blk * QB) + 15) & ~15;
+          const int cols = (min(QB, rows - (q0 + blk) * QB) + 15) & ~15;
           const uint32_t id = idesc_bf16(KT, cols), q = q_lo + qs * (TILE >> 4), k = k_lo + st * (TILE >> 4);
           if (elect_one()) {
 #pragma unroll
@@ -348,38 +379,40 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             umma_commit(&s_full[buf]);
           }
           __syncwarp();
-          if (nb > 2) commit(&q_empty[qs]);
         }
         if (!off) commit(&k_empty[st]);
       }
-      if (nb <= 2 && !off)
-        for (int blk = 0; blk < nb; ++blk) commit(&q_empty[(nq + blk) % Q_STAGES]);
-      nq += nb > 2 ? n * nb : nb;
+      if (off) break;
+      for (int blk = 0; blk < blocks; ++blk) commit(&q_empty[(nq + blk) % Q_STAGES]);
+      nq += blocks;
     }
     commit(&done);
     mbar_drain(&done, 0);
   } else if (warp >= 10) {
     const int pw = warp - 10;
-    Walk walk(a, plan, blockIdx.x, start);
-    Frag f;
-    while (!off && walk.next(a, plan, f)) {
-      const int fs = nf & 1, len = f.len, loads = nb > 2 ? f.n * nb : nb;
+    Passes passes(a, plan, start, nb);
+    for (bool more = true; more && !off;) {
+      Pass f{};
+      more = passes.next(a, plan, nb, f);
+      const unsigned fs = nf & 1;
+      const int len = f.len;
       if (nf >= 2 && (off = wait(&f_empty[fs], (nf >> 1) - 1))) break;
-      // what no row of the head is kept from: needed before the first block is there
+      // what no row of the pass is kept from: needed before the first block is there
       int low = len;
-      for (int r = lane; r < rows; r += 32) {
+      for (int r = f.q0 * QB + lane; r < min(rows, (f.q0 + f.nq) * QB); r += 32) {
         const int i = a.by_G.of(r), g = r - i * a.G;
         const long long token = (long long)f.b * a.L + i;
         if (a.visible) low = min(low, max(0, a.visible[token]));
         if (a.lse[token * (a.Hkv * a.G) + f.h * a.G + g] == -INFINITY) low = 0;
       }
-      low = __reduce_min_sync(FULL_MASK, low);
-      if (pw == 0 && lane == 0) info[fs] = WInfo{f.b, f.h, f.k0, f.n, len, low, f.k0 + f.n == plan.tiles(len)};
+      f.low = __reduce_min_sync(FULL_MASK, low);
+      if (pw == 0 && lane == 0) info[fs] = f;
       __syncwarp();
       if (lane == 0) mbar_arrive(&f_full[fs]);
       ++nf;
-      for (int x = 0; x < loads; ++x, ++nq) {
-        const int qs = nq % Q_STAGES, first = (x % nb) * QB, count = min(QB, rows - first);
+      for (int x = 0; x < f.nq; ++x, ++nq) {
+        const unsigned qs = nq % Q_STAGES;
+        const int first = (f.q0 + x) * QB, count = min(QB, rows - first);
         if (nq >= Q_STAGES && (off = wait(&q_empty[qs], nq / Q_STAGES - 1))) break;
         for (int r0 = 32 * pw; r0 < count; r0 += 64) {
           const int r = r0 + lane;
@@ -408,83 +441,79 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     const int g = warp >> 2;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const f32x2 scale2 = pack2(a.sl2, a.sl2);
-    int ns = 0;
-    while (unit < units && !off) {
-      const int fs = nf & 1;
+    unsigned ns = 0;
+    while (!off) {
+      const unsigned fs = nf & 1;
       off = wait(&f_full[fs], nf >> 1);
       if (off) break;
-      const WInfo x = info[fs];
+      const Pass x = info[fs];
       __syncwarp();
       if (lane == 0) mbar_arrive(&f_empty[fs]);
       ++nf;
+      if (x.n == 0) break;
       float* out = a.acc_out + ((long long)x.b * a.Hkv + x.h) * a.S;
-      const float* in = a.acc_in ? a.acc_in + ((long long)x.b * a.Hkv + x.h) * a.S : nullptr;
-      for (int j = 0; j < x.n && !off; ++j, ++unit) {
-        const bool mine = (unit & 1) == g;
+      // later passes add to what the first one left, by the same threads
+      const float* in = x.q0 > 0 ? out : (a.acc_in ? a.acc_in + ((long long)x.b * a.Hkv + x.h) * a.S : nullptr);
+      const float decay = x.q0 > 0 ? 1.f : a.decay;
+      for (int j = 0; j < x.n && !off; ++j) {
+        if (((x.odd + j) & 1) != g) continue;
         const int t = (x.k0 + j) * KT + (warp & 3) * 32 + lane, t1 = (x.k0 + j + 1) * KT;
         float old = 0.f;
-        if (mine && in && t < x.len) old = in[t];
+        if (in && t < x.len) old = in[t];
         f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
-        for (int blk = 0; blk < nb && (mine || nb > 2); ++blk) {
-          const int qi = nq + (nb > 2 ? j * nb : 0) + blk, qs = qi % Q_STAGES;
+        for (int blk = 0; blk < x.nq; ++blk) {
+          const unsigned qi = nq + blk, qs = qi % Q_STAGES;
           off = wait(&q_full[qs], qi / Q_STAGES);
           if (off) break;
-          if (mine) {
-            const int buf = 2 * g + (ns & 1), count = min(QB, rows - blk * QB);
-            off = wait(&s_full[buf], ns >> 1);
-            if (off) break;
-            ++ns;
-            tc_fence_after();
+          const int buf = 2 * g + (ns & 1), count = min(QB, rows - (x.q0 + blk) * QB);
+          off = wait(&s_full[buf], ns >> 1);
+          if (off) break;
+          ++ns;
+          tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < count; c += 32) {
-              float v[32];
-              tmem_ld32(tmem + buf * 128 + lanes + c, v);
-              if (x.low < t1 || c + 32 > count) {
+          for (int c = 0; c < count; c += 32) {
+            float v[32];
+            tmem_ld32(tmem + buf * 128 + lanes + c, v);
+            if (x.low < t1 || c + 32 > count) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                  const float4 ls = *reinterpret_cast<const float4*>(&neg_lse[qs][c + i]);
-                  const int4 lim = *reinterpret_cast<const int4*>(&row_lim[qs][c + i]);
-                  const float w0 = ex2(fmaf(v[i], a.sl2, ls.x)), w1 = ex2(fmaf(v[i + 1], a.sl2, ls.y));
-                  const float w2 = ex2(fmaf(v[i + 2], a.sl2, ls.z)), w3 = ex2(fmaf(v[i + 3], a.sl2, ls.w));
-                  const int left = count - c - i;
-                  sum0 = add2(sum0, pack2(t < lim.x && left > 0 ? w0 : 0.f, t < lim.y && left > 1 ? w1 : 0.f));
-                  sum1 = add2(sum1, pack2(t < lim.z && left > 2 ? w2 : 0.f, t < lim.w && left > 3 ? w3 : 0.f));
-                }
-              } else {
+              for (int i = 0; i < 32; i += 4) {
+                const float4 ls = *reinterpret_cast<const float4*>(&neg_lse[qs][c + i]);
+                const int4 lim = *reinterpret_cast<const int4*>(&row_lim[qs][c + i]);
+                const float w0 = ex2(fmaf(v[i], a.sl2, ls.x)), w1 = ex2(fmaf(v[i + 1], a.sl2, ls.y));
+                const float w2 = ex2(fmaf(v[i + 2], a.sl2, ls.z)), w3 = ex2(fmaf(v[i + 3], a.sl2, ls.w));
+                const int left = count - c - i;
+                sum0 = add2(sum0, pack2(t < lim.x && left > 0 ? w0 : 0.f, t < lim.y && left > 1 ? w1 : 0.f));
+                sum1 = add2(sum1, pack2(t < lim.z && left > 2 ? w2 : 0.f, t < lim.w && left > 3 ? w3 : 0.f));
+              }
+            } else {
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                  const float4 ls = *reinterpret_cast<const float4*>(&neg_lse[qs][c + i]);
-                  float y[4];
-                  unpack2(fma2(pack2(v[i], v[i + 1]), scale2, pack2(ls.x, ls.y)), y[0], y[1]);
-                  unpack2(fma2(pack2(v[i + 2], v[i + 3]), scale2, pack2(ls.z, ls.w)), y[2], y[3]);
-                  sum0 = add2(sum0, pack2(ex2(y[0]), ex2(y[1])));
-                  sum1 = add2(sum1, pack2(ex2(y[2]), ex2(y[3])));
-                }
+              for (int i = 0; i < 32; i += 4) {
+                const float4 ls = *reinterpret_cast<const float4*>(&neg_lse[qs][c + i]);
+                float y[4];
+                unpack2(fma2(pack2(v[i], v[i + 1]), scale2, pack2(ls.x, ls.y)), y[0], y[1]);
+                unpack2(fma2(pack2(v[i + 2], v[i + 3]), scale2, pack2(ls.z, ls.w)), y[2], y[3]);
+                sum0 = add2(sum0, pack2(ex2(y[0]), ex2(y[1])));
+                sum1 = add2(sum1, pack2(ex2(y[2]), ex2(y[3])));
               }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&s_empty[buf]);
           }
-          if (nb > 2) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&q_empty[qs]);
-          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_empty[buf]);
         }
-        if (mine && !off && t < a.S) {
+        if (!off && t < a.S) {
           float y[2];
           unpack2(add2(sum0, sum1), y[0], y[1]);
-          out[t] = t < x.len ? fmaf(a.decay, old, y[0] + y[1]) : 0.f;
+          out[t] = t < x.len ? fmaf(decay, old, y[0] + y[1]) : 0.f;
         }
       }
-      if (nb <= 2)
-        for (int blk = 0; blk < nb && !off; ++blk) {
-          const int qi = nq + blk, qs = qi % Q_STAGES;
-          off = wait(&q_full[qs], qi / Q_STAGES);
-          if (!off && lane == 0) mbar_arrive(&q_empty[qs]);
-        }
-      nq += nb > 2 ? x.n * nb : nb;
-      if (x.last && g == 0)                        // the places behind the last tile
+      for (int blk = 0; blk < x.nq && !off; ++blk) {
+        const unsigned qi = nq + blk, qs = qi % Q_STAGES;
+        off = wait(&q_full[qs], qi / Q_STAGES);
+        if (!off && lane == 0) mbar_arrive(&q_empty[qs]);
+      }
+      nq += x.nq;
+      if (x.last && x.q0 == 0 && g == 0)           // the places behind the last tile
         for (int t = (x.k0 + x.n) * KT + tid; t < a.S; t += 128) out[t] = 0.f;
     }
   }

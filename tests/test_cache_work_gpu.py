@@ -125,6 +125,7 @@ BF_SIZES = [
     (9, 1, 28, 4, 120, 6000, 4000),       # all rows of a head in a slot, long caches
     (2, 64, 8, 2, 128, 0, 3100),          # own entries alone, two row tiles a sequence
     (3, 100, 12, 2, 104, 300, 1500),      # row tiles of a sequence that end inside
+    (16, 75, 32, 8, 64, 0, 2600),         # the weights' blocks of queries take turns on several runs of key tiles
 ]
 
 
