@@ -96,6 +96,8 @@ struct Plan {
     UP = Hkv * nPT * kP;
     UO = Hkv * nLT * own_tiles;
     apart = grid_p > 0;
+    // (an own fragment costs about one and a half of its units more, whatever its length)
+    if (weight_ > 1) weight_ = max(1, (int)(2ll * own_tiles * weight_ / (2ll * own_tiles + 3 * B)));
     const unsigned all = (unsigned)UP * weight_ + UO;          // (UP and UO: up to 2e9 together)
     weight = UP < (1 << 28) && all < (1u << 31) && all / grid_o >= (unsigned)weight_ ? weight_ : 1;
     own0 = apart ? 0 : UP * weight;
@@ -315,8 +317,8 @@ constexpr int SLOT_CTAS = 2 * CACHE_SMS;             // (the fp32 kernel's, too)
 constexpr int APART_UNITS = 2 * CACHE_SMS;
 // fp32: up to FEW_ROWS rows of a sequence have a form of their own (64 single tokens, 32 heads on 8, D = 128, over
 // 1000 to 2000 own and 2000 shared entries: 216 us, with the form for more rows 685 us). One of its units takes about
-// a sixth (up to 4 rows) or a fourth of the time of a prefix's unit of a full tile: counting the latter as 1, 4, 5
-// and 6 units 571, 239, 215 and 216 us, 8 rows 626, 366, 399 and 429 us.
+// a sixth (up to 4 rows) or a fourth of the time of a prefix's unit of a full tile, where own caches are long: counting
+// the latter as 1, 4, 5 and 6 units 571, 239, 215 and 216 us, 8 rows 626, 366, 399 and 429 us.
 constexpr int FEW_ROWS = 8;
 inline void divide(AttendArgs* a) {
   const bool tc = a->dt == BRISK_DT_BF16;

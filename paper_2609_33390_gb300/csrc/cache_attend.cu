@@ -6,6 +6,8 @@
 // each of its rows, the running maximum m of its scores, l = sum exp(s - m) and O = sum exp(s - m) v;
 // parts of one row join by l = sum_i l_i exp(m_i - m), O likewise, with m the largest of the m_i.
 // Scores, sums and parts are fp32; maxima and scores are held in log2 units.
+#include <type_traits>
+
 #include "cache.cuh"
 #include "tensor_core.cuh"
 
@@ -57,6 +59,18 @@ struct RowEnd {
   }
 };
 
+// A tile of keys or values on its way to shared memory, past L1; zeros behind the last entry.
+__device__ __forceinline__ void copy_tile(float* to, int stride, const float* from, long long tok, int t0, int len, int nv) {
+#pragma unroll 4
+  for (int e = threadIdx.x; e < KT * nv; e += SIMT_THREADS) {
+    const int r = e / nv, c = 4 * (e - r * nv);
+    const bool there = t0 + r < len;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(su32(to + r * stride + c)),
+                 "l"(there ? from + (t0 + r) * tok + c : from), "r"(there ? 16 : 0)
+                 : "memory");
+  }
+}
+
 template <int RPT>
 __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f, const SimtTile& t,
                                               int* lowest) {
@@ -102,20 +116,11 @@ __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f
 
   for (int kt = f.k0; kt < f.k0 + f.n; ++kt) {
     const int t0 = kt * KT;
-    bool odd = false;                  // an infinity or NaN that some row must not see
-#pragma unroll 4
-    for (int e = tid; e < KT * nv; e += SIMT_THREADS) {
-      const int r = e / nv, c = 4 * (e - r * nv), key = t0 + r;
-      float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-      if (key < len) {
-        k = load4(kb + key * kc.tok + c);
-        v = load4(vb + key * vc.tok + c);
-        if (key >= low) odd |= !(isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w));
-      }
-      store4(t.k + r * KS + c, k);
-      store4(t.v + r * CACHE_MAX_D + c, v);
-    }
-    odd = __syncthreads_or(odd);
+    copy_tile(t.k, KS, kb, kc.tok, t0, len, nv);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    copy_tile(t.v, CACHE_MAX_D, vb, vc.tok, t0, len, nv);
+    asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
+    __syncthreads();
 
     f32x2 s2[RPT][4];                  // sums over the even and the odd columns
 #pragma unroll
@@ -134,7 +139,16 @@ __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f
 #pragma unroll
         for (int j = 0; j < 4; ++j) s2[i][j] = fma2(q[i].y, k[j].y, fma2(q[i].x, k[j].x, s2[i][j]));
     }
-    __syncthreads();                   // the keys are read: the probabilities take their place
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    bool odd = false;                  // an infinity or NaN that some row must not see
+    if (t0 + KT > low)
+      for (int e = tid; e < KT * nv; e += SIMT_THREADS) {
+        const int r = e / nv;
+        if (t0 + r < low) continue;
+        const float4 v = load4(t.v + r * CACHE_MAX_D + 4 * (e - r * nv));
+        odd |= !(isfinite(v.x) && isfinite(v.y) && isfinite(v.z) && isfinite(v.w));
+      }
+    odd = __syncthreads_or(odd);       // the keys are read: the probabilities take their place
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       float s[4], top = -INFINITY;
@@ -165,7 +179,7 @@ __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f
     }
     __syncwarp();
     const int c0 = 4 * tx, c1 = 64 + 4 * tx;
-    if (!odd) {
+    auto add_values = [&](auto wide) {             // (up to 64 columns: the first four of a thread)
 #pragma unroll 2
       for (int y = 0; y < KT; y += 4) {
         float4 p[RPT];
@@ -174,18 +188,25 @@ __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const ulonglong2 v0 = *reinterpret_cast<const ulonglong2*>(t.v + (y + e) * CACHE_MAX_D + c0);
-          const ulonglong2 v1 = *reinterpret_cast<const ulonglong2*>(t.v + (y + e) * CACHE_MAX_D + c1);
+          ulonglong2 v1;
+          if (wide) v1 = *reinterpret_cast<const ulonglong2*>(t.v + (y + e) * CACHE_MAX_D + c1);
 #pragma unroll
           for (int i = 0; i < RPT; ++i) {
             const float w = e == 0 ? p[i].x : (e == 1 ? p[i].y : (e == 2 ? p[i].z : p[i].w));
             const f32x2 w2 = pack2(w, w);
             o[i][0] = fma2(w2, v0.x, o[i][0]);
             o[i][1] = fma2(w2, v0.y, o[i][1]);
-            o[i][2] = fma2(w2, v1.x, o[i][2]);
-            o[i][3] = fma2(w2, v1.y, o[i][3]);
+            if (wide) {
+              o[i][2] = fma2(w2, v1.x, o[i][2]);
+              o[i][3] = fma2(w2, v1.y, o[i][3]);
+            }
           }
         }
       }
+    };
+    if (!odd) {
+      if (D > 64) add_values(std::true_type{});
+      else add_values(std::false_type{});
     } else {
       for (int y = 0; y < KT; ++y)
 #pragma unroll
