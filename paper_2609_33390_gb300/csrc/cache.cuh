@@ -359,6 +359,21 @@ __device__ __forceinline__ void fetch_queries(const __nv_bfloat16* q, int D, uin
   }
 }
 
+// 16 bytes on their way to shared memory, past L1; zeros where there is nothing to copy (`from` is valid anyway).
+__device__ __forceinline__ void copy16(float* to, const float* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(su32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+// A tile of fp32 keys or values, by all threads of a CTA; zeros behind the last entry.
+template <int ROWS, int THREADS>
+__device__ __forceinline__ void copy_tile(float* to, int stride, const float* from, long long tok, int t0, int len, int nv) {
+#pragma unroll 4
+  for (int e = threadIdx.x; e < ROWS * nv; e += THREADS) {
+    const int r = e / nv, c = 4 * (e - r * nv);
+    const bool there = t0 + r < len;
+    copy16(to + r * stride + c, there ? from + (t0 + r) * tok + c : from, there);
+  }
+}
+
 // Tensor map of a cache's tiles of 64 columns x 128 entries (cache_attend_tc.cu).
 bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int toks, int seqs);
 
@@ -403,7 +418,7 @@ struct WeightArgs {
   long long wait_limit;
 };
 cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream);
-cudaError_t launch_weights_simt(const WeightArgs& a, cudaStream_t stream);
+cudaError_t launch_weights_f32(const WeightArgs& a, cudaStream_t stream);
 
 // ---------------------------------------------------------------- eviction
 struct EvictArgs {

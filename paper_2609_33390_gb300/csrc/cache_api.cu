@@ -166,7 +166,7 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   if (d->S == 0) return BRISK_OK;
   if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
   a.grid = CACHE_SMS;
-  return (d->dtype == BRISK_DT_BF16 ? launch_weights_tc(a, st) : launch_weights_simt(a, st)) == cudaSuccess
+  return (d->dtype == BRISK_DT_BF16 ? launch_weights_tc(a, st) : launch_weights_f32(a, st)) == cudaSuccess
              ? BRISK_OK : BRISK_ERR_CUDA;
 }
 

@@ -59,18 +59,6 @@ struct RowEnd {
   }
 };
 
-// A tile of keys or values on its way to shared memory, past L1; zeros behind the last entry.
-__device__ __forceinline__ void copy_tile(float* to, int stride, const float* from, long long tok, int t0, int len, int nv) {
-#pragma unroll 4
-  for (int e = threadIdx.x; e < KT * nv; e += SIMT_THREADS) {
-    const int r = e / nv, c = 4 * (e - r * nv);
-    const bool there = t0 + r < len;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(su32(to + r * stride + c)),
-                 "l"(there ? from + (t0 + r) * tok + c : from), "r"(there ? 16 : 0)
-                 : "memory");
-  }
-}
-
 template <int RPT>
 __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f, const SimtTile& t,
                                               int* lowest) {
@@ -116,9 +104,9 @@ __device__ __forceinline__ void simt_fragment(const AttendArgs& a, const Frag& f
 
   for (int kt = f.k0; kt < f.k0 + f.n; ++kt) {
     const int t0 = kt * KT;
-    copy_tile(t.k, KS, kb, kc.tok, t0, len, nv);
+    copy_tile<KT, SIMT_THREADS>(t.k, KS, kb, kc.tok, t0, len, nv);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    copy_tile(t.v, CACHE_MAX_D, vb, vc.tok, t0, len, nv);
+    copy_tile<KT, SIMT_THREADS>(t.v, CACHE_MAX_D, vb, vc.tok, t0, len, nv);
     asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
     __syncthreads();
 

@@ -12,6 +12,8 @@
 namespace brisk {
 namespace {
 
+// fp32, more than FEW_W rows a head (see weights_few_kernel): tiles of 64 keys and 64 rows, 4 rows and 4 keys a thread. Bound by FMA issue and
+// shared-memory reads (128 rows, 32 heads on 8, D = 128, 16 sequences of 1000 to 4000 entries: 326 us, 33 TFLOP/s).
 constexpr int W_THREADS = 256;
 constexpr int W_KEYS = 64, W_ROWS = 64;
 constexpr int WS = CACHE_MAX_D + 4;
@@ -25,8 +27,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   int* sLim = reinterpret_cast<int*>(sL + W_ROWS);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int tiles = (a.S + W_KEYS - 1) / W_KEYS, D = a.D, nv = D / 4;
-  const long long item = blockIdx.x / tiles;
-  const int t0 = (int)(blockIdx.x % tiles) * W_KEYS, b = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
+  const int item = blockIdx.x / tiles, t0 = (blockIdx.x - item * tiles) * W_KEYS, b = item / a.Hkv, h = item - b * a.Hkv;
   const int len = clamped_len(a, b);
   if (blockIdx.x == 0) {                   // the call's status: the lengths that were clamped
     bool bad = false;
@@ -38,25 +39,19 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   const int rows = a.L * a.G;
   if (t0 < len) {
     const float* kb = static_cast<const float*>(a.ko.p) + b * a.ko.seq + h * a.ko.head;
-    for (int e = tid; e < W_KEYS * nv; e += W_THREADS) {
-      const int r = e / nv, c = 4 * (e - r * nv);
-      store4(sK + r * WS + c, t0 + r < len ? load4(kb + (t0 + r) * a.ko.tok + c) : make_float4(0.f, 0.f, 0.f, 0.f));
-    }
+    copy_tile<W_KEYS, W_THREADS>(sK, WS, kb, a.ko.tok, t0, len, nv);
     for (int r0 = 0; r0 < rows; r0 += W_ROWS) {
       __syncthreads();
       for (int e = tid; e < (rows - r0 > 16 ? W_ROWS : 16) * nv; e += W_THREADS) {
-        const int r = e / nv, c = 4 * (e - r * nv), i = (r0 + r) / a.G;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r0 + r < rows)
-          v = load4(static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok +
-                    (h * a.G + (r0 + r - i * a.G)) * a.q.head + c);
-        store4(sQ + r * CACHE_MAX_D + c, v);
+        const int r = e / nv, c = 4 * (e - r * nv), row = min(r0 + r, rows - 1), i = a.by_G.of(row);
+        copy16(sQ + r * CACHE_MAX_D + c, static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok +
+               (h * a.G + (row - i * a.G)) * a.q.head + c, r0 + r < rows);
       }
       if (tid < W_ROWS) {
         int lim = 0;
         float ls = 0.f;
         if (r0 + tid < rows) {
-          const int i = (r0 + tid) / a.G, g = r0 + tid - i * a.G;
+          const int i = a.by_G.of(r0 + tid), g = r0 + tid - i * a.G;
           const long long token = (long long)b * a.L + i;
           lim = a.visible ? min(len, a.visible[token]) : len;
           ls = a.lse[token * (a.Hkv * a.G) + h * a.G + g] * LOG2E;
@@ -65,6 +60,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
         sLim[tid] = lim;
         sL[tid] = ls;
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       __syncthreads();
       // 4 rows and 4 keys a thread, two products an instruction; a row where there are 16 at most
       auto add = [&](auto rows_each) {
@@ -112,29 +108,30 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
     float w = 0.f;
 #pragma unroll
     for (int y = 0; y < 16; ++y) w += part[y * W_KEYS + tid];
-    const long long at = item * a.S + t;
+    const long long at = (long long)item * a.S + t;
     if (a.acc_in) w += a.decay * a.acc_in[at];
     a.acc_out[at] = t < len ? w : 0.f;
   }
 }
 
-// At most R <= 8 query rows a head, as single tokens have them: 4 lanes share a key, 16 bytes of it in turn, from
-// memory to registers, and a warp has 16 keys. Bound by the keys' bytes (64 single tokens over 1000 to 2000 entries,
-// 32 heads on 8, D = 128: 95 us, 4.2 TB/s; 8 heads on 8, D = 64: 61 us, in tiles of 64 rows 161). The loads land in
-// L1, which therefore gets what shared memory does not need: with the least of L1 129 us.
-constexpr int CARVEOUT_LEAST_KB = 16;     // of shared memory: two CTAs' queries
-constexpr int WF_KEYS = 16 * (W_THREADS / 32);
-template <int R>
+// fp32, up to FEW_W rows a head: a CTA has 128 keys, a warp 16, in registers: 4 lanes share a key, 16 bytes of it in
+// turn, and a lane has a piece of two. A lane's 16 bytes of a query then serve both keys, and the lanes' sums of two
+// rows and two keys are exchanged so that each has one pair's. Bound by the keys' bytes up to about 8 rows, by FMA
+// issue beyond: 32 heads on 8, D = 128, 64 single tokens over 1000 to 2000 entries 85 us (4.7 TB/s); 16 and 32 rows, 16
+// sequences of up to 4000, 69 and 108 us, as tiles 113 and 187. With 60 and 128 rows tiles are ahead: 6.5 us to
+// 11.7 (6 sequences), 326 to 369.
+constexpr int WF_KEYS = 16 * (W_THREADS / 32), FEW_W = 32;
+constexpr int CARVEOUT_FEW_KB = 40;        // of shared memory, two CTAs' queries: the keys' loads land in the L1 left
+
 __global__ void __launch_bounds__(W_THREADS, 2)
 weights_few_kernel(const __grid_constant__ WeightArgs a) {
   constexpr int CH = CACHE_MAX_D / 16;
-  __shared__ __align__(16) float sQ[R][CACHE_MAX_D];
-  __shared__ float sL[R];
-  __shared__ int sLim[R];
+  __shared__ __align__(16) float sQ[FEW_W][CACHE_MAX_D];
+  __shared__ float sL[FEW_W];              // log-sums in log2 units
+  __shared__ int sLim[FEW_W];
   const int tid = threadIdx.x, lane = tid & 31, D = a.D, rows = a.L * a.G;
-  const int tiles = (a.S + WF_KEYS - 1) / WF_KEYS;
-  const long long item = blockIdx.x / tiles;
-  const int t0 = (int)(blockIdx.x % tiles) * WF_KEYS, b = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
+  const int tiles = (a.S + WF_KEYS - 1) / WF_KEYS, item = blockIdx.x / tiles;
+  const int t0 = (blockIdx.x - item * tiles) * WF_KEYS, b = item / a.Hkv, h = item - b * a.Hkv;
   const int len = clamped_len(a, b);
   if (blockIdx.x == 0) {                   // the call's status: the lengths that were clamped
     bool bad = false;
@@ -142,8 +139,8 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
     bad = __syncthreads_or(bad);
     if (tid == 0) *a.status = bad ? BRISK_ERR_INVALID_ARG : BRISK_OK;
   }
-  float sum[2] = {0.f, 0.f};
-  const int key = t0 + (tid >> 5) * 16 + (lane >> 2);        // and 8 further
+  float sum = 0.f;                         // of key + 8 (lane & 1), over every other row
+  const int key = t0 + (tid >> 5) * 16 + (lane >> 2), mine = key + 8 * (lane & 1);
   if (t0 < len) {
     const float* kb = static_cast<const float*>(a.ko.p) + b * a.ko.seq + h * a.ko.head;
     ulonglong2 k[2][CH];
@@ -155,50 +152,63 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
         k[e][j] = make_ulonglong2(0, 0);
         if (key + 8 * e < len && c < D) k[e][j] = *reinterpret_cast<const ulonglong2*>(kb + (key + 8 * e) * a.ko.tok + c);
       }
-    const int nq = 4 * ((D + 15) / 16);    // (columns that lanes without a piece of a key multiply by zeros)
-    for (int e = tid; e < rows * nq; e += W_THREADS) {
-      const int r = e / nq, c = 4 * (e - r * nq), i = r / a.G;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c < D) v = load4(static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok + (h * a.G + (r - i * a.G)) * a.q.head + c);
-      store4(&sQ[r][c], v);
+    const int nq = 4 * ((D + 15) / 16);    // pieces of a row (lanes without a piece of a key multiply by zeros)
+    const int n = (rows + 1) & ~1;         // an even number of rows, and what they see
+    for (int e = tid; e < n * nq; e += W_THREADS) {
+      const int r = e / nq, c = 4 * (e - r * nq), row = min(r, rows - 1), i = a.by_G.of(row);
+      const float* q = static_cast<const float*>(a.q.p) + b * a.q.seq + i * a.q.tok + (h * a.G + (row - i * a.G)) * a.q.head;
+      copy16(&sQ[r][c], c < D ? q + c : q, c < D);
     }
-    if (tid < rows) {
-      const int i = tid / a.G;
-      const long long token = (long long)b * a.L + i;
-      const float ls = a.lse[token * (a.Hkv * a.G) + h * a.G + (tid - i * a.G)] * LOG2E;
+    if (tid < n) {
+      int lim = 0;
+      float ls = 0.f;
+      if (tid < rows) {
+        const int i = a.by_G.of(tid);
+        const long long token = (long long)b * a.L + i;
+        ls = a.lse[token * (a.Hkv * a.G) + h * a.G + (tid - i * a.G)] * LOG2E;
+        // (a row that saw nothing gives nothing)
+        lim = ls == -INFINITY ? 0 : (a.visible ? min(len, a.visible[token]) : len);
+      }
       sL[tid] = ls;
-      // (a row that saw nothing gives nothing)
-      sLim[tid] = ls == -INFINITY ? 0 : (a.visible ? min(len, a.visible[token]) : len);
+      sLim[tid] = lim;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
+    for (int r = 0; r < rows; r += 2) {
+      f32x2 x[2][2];                       // [row][key]: sums over the even and the odd columns
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (r >= rows) break;
-      f32x2 x[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+      for (int i = 0; i < 4; ++i) x[i >> 1][i & 1] = pack2(0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
         if (16 * j >= D) break;
-        const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&sQ[r][4 * (4 * j + (lane & 3))]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[e] = fma2(q.y, k[e][j].y, fma2(q.x, k[e][j].x, x[e]));
-      }
+        for (int i = 0; i < 2; ++i) {
+          const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&sQ[r + i][4 * (4 * j + (lane & 3))]);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float y, z;
-        unpack2(x[e], y, z);
-        y += z;
-        y += __shfl_xor_sync(FULL_MASK, y, 1);
-        y += __shfl_xor_sync(FULL_MASK, y, 2);
-        if (key + 8 * e < sLim[r]) sum[e] += ex2(y * a.sl2 - sL[r]);
+          for (int e = 0; e < 2; ++e) x[i][e] = fma2(q.y, k[e][j].y, fma2(q.x, k[e][j].x, x[i][e]));
+        }
       }
+      float y[2][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        unpack2(x[i >> 1][i & 1], lo, hi);
+        y[i >> 1][i & 1] = lo + hi;
+      }
+      // row r + (lane >> 1 & 1), key + 8 (lane & 1)
+      const bool up = lane & 2, odd = lane & 1;
+      const float z0 = (up ? y[1][0] : y[0][0]) + __shfl_xor_sync(FULL_MASK, up ? y[0][0] : y[1][0], 2);
+      const float z1 = (up ? y[1][1] : y[0][1]) + __shfl_xor_sync(FULL_MASK, up ? y[0][1] : y[1][1], 2);
+      const float z = (odd ? z1 : z0) + __shfl_xor_sync(FULL_MASK, odd ? z0 : z1, 1);
+      const int row = r + (lane >> 1 & 1);
+      if (mine < sLim[row]) sum += ex2(z * a.sl2 - sL[row]);
     }
   }
-  const int t = key + 8 * (lane & 1);      // two of a key's lanes have a key each to write
-  if ((lane & 3) < 2 && t < a.S) {
-    float w = sum[lane & 1];
-    const long long at = item * a.S + t;
-    if (a.acc_in && t < len) w += a.decay * a.acc_in[at];
-    a.acc_out[at] = t < len ? w : 0.f;
+  sum += __shfl_xor_sync(FULL_MASK, sum, 2);
+  if ((lane & 2) == 0 && mine < a.S) {
+    const long long at = (long long)item * a.S + mine;
+    if (a.acc_in && mine < len) sum += a.decay * a.acc_in[at];
+    a.acc_out[at] = mine < len ? sum : 0.f;
   }
 }
 
@@ -538,19 +548,16 @@ cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream) {
   return a.D > 64 ? run(weights_tc_kernel<128>, WShape<128>::SMEM) : run(weights_tc_kernel<64>, WShape<64>::SMEM);
 }
 
-cudaError_t launch_weights_simt(const WeightArgs& a, cudaStream_t stream) {
-  const int rows = a.L * a.G;
-  auto run = [&](auto kernel, int keys, size_t smem) {
-    cudaError_t e = set_up_kernel(kernel, smem ? CARVEOUT_FULL_KB : CARVEOUT_LEAST_KB, smem);
+cudaError_t launch_weights_f32(const WeightArgs& a, cudaStream_t stream) {
+  auto run = [&](auto kernel, int keys, int carveout, size_t smem) {
+    cudaError_t e = set_up_kernel(kernel, carveout, smem);
     if (e != cudaSuccess) return e;
     const long long grid = (long long)a.B * a.Hkv * ((a.S + keys - 1) / keys);
     kernel<<<(unsigned)grid, W_THREADS, smem, stream>>>(a);
     return cudaGetLastError();
   };
-  if (rows <= 2) return run(weights_few_kernel<2>, WF_KEYS, 0);
-  if (rows <= 4) return run(weights_few_kernel<4>, WF_KEYS, 0);
-  if (rows <= FEW_ROWS) return run(weights_few_kernel<8>, WF_KEYS, 0);
-  return run(weights_simt_kernel, W_KEYS, sizeof(float) * (W_KEYS * WS + W_ROWS * CACHE_MAX_D + 2 * W_ROWS));
+  if (a.L * a.G <= FEW_W) return run(weights_few_kernel, WF_KEYS, CARVEOUT_FEW_KB, 0);
+  return run(weights_simt_kernel, W_KEYS, CARVEOUT_FULL_KB, sizeof(float) * (W_KEYS * WS + W_ROWS * CACHE_MAX_D + 2 * W_ROWS));
 }
 
 }  // namespace brisk
