@@ -6,8 +6,7 @@
 namespace brisk {
 namespace {
 
-constexpr int SELECT_THREADS = 1024, SELECT_EACH = 4;
-constexpr int SELECT_BLOCK = SELECT_THREADS * SELECT_EACH;   // entries a pass takes at a time
+constexpr int SELECT_EACH = 4;           // neighbouring entries of a thread
 constexpr int BINS = 2048;
 
 // Order-preserving key of a weight: larger weights have larger keys, -0 equals 0, NaN is below all.
@@ -18,6 +17,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 // Inclusive sum over the CTA's threads; *total gets the sum of all. `part` holds a word a warp.
+template <int THREADS>
 __device__ __forceinline__ int block_scan(int x, int* part, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -28,7 +28,7 @@ __device__ __forceinline__ int block_scan(int x, int* part, int* total) {
   __syncthreads();                         // the last scan's words are read
   if (lane == 31) part[warp] = x;
   __syncthreads();
-  int w = part[lane];
+  int w = lane < THREADS / 32 ? part[lane] : 0;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int y = __shfl_up_sync(FULL_MASK, w, o);
@@ -40,9 +40,10 @@ __device__ __forceinline__ int block_scan(int x, int* part, int* total) {
 }
 
 // One CTA a (sequence, key head): the smallest kept key by three passes over 11, 11 and 10 of its bits,
-// then the kept indices in order. Bound by the barriers and the passes' latency: the weights, a
-// hundredth of the entries' bytes, stay in L1 after the first pass.
-__global__ void __launch_bounds__(SELECT_THREADS)
+// then the kept indices in order. Bound by the barriers and the passes' latency (2048 entries
+// 6 us): the weights, a hundredth of the entries' bytes, stay in L1 after the first pass.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 select_kernel(const __grid_constant__ EvictArgs a) {
   __shared__ int hist[BINS], part[32];
   __shared__ uint32_t s_prefix;
@@ -55,7 +56,7 @@ select_kernel(const __grid_constant__ EvictArgs a) {
   float* acc_to = a.acc_to + (long long)blockIdx.x * a.keep;
   int32_t* kept = a.kept + (long long)blockIdx.x * a.keep;
   if (n <= a.keep) {
-    for (int i = tid; i < a.keep; i += SELECT_THREADS) {
+    for (int i = tid; i < a.keep; i += THREADS) {
       kept[i] = i < n ? i : -1;
       acc_to[i] = i < n ? acc[i] : 0.f;
     }
@@ -69,23 +70,29 @@ select_kernel(const __grid_constant__ EvictArgs a) {
   if (some)
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : BINS;
-      hist[tid] = 0;
-      hist[tid + 1024] = 0;
+#pragma unroll
+      for (int i = 0; i < BINS; i += THREADS) hist[i + tid] = 0;
       __syncthreads();
-      for (int i = tid; i < m; i += SELECT_THREADS) {
+      for (int i = tid; i < m; i += THREADS) {
         const uint32_t k = weight_key(acc[i]);
         if ((k & known) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
       }
       __syncthreads();
-      // bins from the largest: thread j holds bins - 1 - 2j and the next lower one
-      const int top = bins - 1 - 2 * tid;
-      const int first = top > 0 ? hist[top] : 0, second = top > 0 ? hist[top - 1] : 0;
+      // bins from the largest: thread j holds EACH from bins - 1 - EACH j downwards
+      constexpr int EACH = BINS / THREADS;
+      const int top = bins - 1 - EACH * tid;
+      int count[EACH], mine = 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) mine += count[i] = top > 0 ? hist[top - i] : 0;
       int total;
-      const int upto = block_scan(first + second, part, &total), before = upto - first - second;
-      if (before < room && upto >= room) {
-        const bool in_first = before + first >= room;
-        s_prefix = prefix | ((uint32_t)(in_first ? top : top - 1) << shift);
-        s_room = room - before - (in_first ? 0 : first);
+      int before = block_scan<THREADS>(mine, part, &total) - mine;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        if (before < room && before + count[i] >= room) {
+          s_prefix = prefix | (uint32_t)(top - i) << shift;
+          s_room = room - before;
+        }
+        before += count[i];
       }
       __syncthreads();
       prefix = s_prefix;
@@ -94,7 +101,7 @@ select_kernel(const __grid_constant__ EvictArgs a) {
       __syncthreads();
     }
   int done = 0, equal = 0;                 // entries above the last key (and newest) seen, and its equals
-  for (int i0 = 0; i0 < n; i0 += SELECT_BLOCK) {
+  for (int i0 = 0; i0 < n; i0 += THREADS * SELECT_EACH) {
     const int i = i0 + tid * SELECT_EACH;
     float w[SELECT_EACH];
     int is = 0, in = 0;                    // two bits an entry: stays, equals
@@ -109,7 +116,7 @@ select_kernel(const __grid_constant__ EvictArgs a) {
     // both counts in one scan (a block has less than 2^15 entries)
     int total;
     const int mine = __popc(is) | __popc(in) << 16;
-    const int upto = block_scan(mine, part, &total) - mine;
+    const int upto = block_scan<THREADS>(mine, part, &total) - mine;
     int above = done + (upto & 0xffff), ties = equal + (upto >> 16);
 #pragma unroll
     for (int j = 0; j < SELECT_EACH; ++j) {
@@ -130,7 +137,7 @@ select_kernel(const __grid_constant__ EvictArgs a) {
 // The kept rows of keys and values, 16 bytes a thread at a time; zeros where there is none. The pieces of a
 // sequence's (place, head) rows lie as in the target's token-major order, so that writes are runs of whole
 // tokens; a thread's loads, of four pieces of the keys and of the values, are all on their way at once. Bound
-// by the rows' bytes, read and written once.
+// by the rows' bytes, read and written once (128 sequences cut to 2048 entries, 8 heads of 128: 319 us, 6.7 TB/s).
 constexpr int MOVE_THREADS = 256, MOVE_EACH = 4;
 __global__ void __launch_bounds__(MOVE_THREADS)
 move_kernel(const __grid_constant__ EvictArgs a, Divisor by_vec, Divisor by_heads) {
@@ -182,7 +189,11 @@ cudaError_t launch_evict(const EvictArgs& a, cudaStream_t stream) {
   Divisor by_vec, by_heads;
   by_vec.set(nvec);
   by_heads.set(a.Hkv);
-  select_kernel<<<a.B * a.Hkv, SELECT_THREADS, 0, stream>>>(a);
+  // with more CTAs than two an SM, smaller ones, of which four fit (1024 selections of 1500 to 4096 entries: the call
+  // 336 us, with the larger ones 342)
+  const int ctas = a.B * a.Hkv;
+  if (ctas > 2 * CACHE_SMS) select_kernel<512><<<ctas, 512, 0, stream>>>(a);
+  else select_kernel<1024><<<ctas, 1024, 0, stream>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const long long vecs = (long long)a.keep * a.Hkv * nvec, each = MOVE_THREADS * MOVE_EACH;

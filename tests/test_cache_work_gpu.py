@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from test_cache_gpu import BF, F32, U, caches
+from test_cache_gpu import check_evict, make
 from test_cache_gpu import test_hidden_entries_do_not_reach_the_rows as hidden_entries
 
 pytestmark = pytest.mark.gpu
@@ -176,6 +177,22 @@ def test_divided_work_fp32(B, size, mask):
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_hidden_entries_with_few_rows(B, bad, L, G):
     hidden_entries(B, bad, L, G, F32)
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "special"])
+@pytest.mark.parametrize("S,keep,recent", [(90, 40, 7), (2700, 1100, 300), (5000, 4999, 0), (2100, 1, 1)])
+def test_evict_of_many_sequences(B, S, keep, recent, kind):
+    Bn, Hkv = 80, 4
+    x = make(Bn, 1, Hkv, Hkv, 16, 0, S, BF, lens_of(Bn, S))
+    g = torch.Generator().manual_seed(S)
+    acc = torch.rand(Bn, Hkv, S, generator=g)
+    if kind == "ties":
+        acc = torch.floor(acc * 3)
+    if kind == "special":
+        pick = torch.randint(0, 8, acc.shape, generator=g)
+        for j, v in enumerate((float("nan"), float("inf"), -float("inf"), 0.0, -0.0, 1e-45, -1.0)):
+            acc = torch.where(pick == j, torch.tensor(v), acc)
+    check_evict(B, x, acc.cuda(), S, keep, recent)
 
 
 def test_two_handles_on_two_streams(B):
