@@ -507,27 +507,11 @@ merge_many_kernel(const __grid_constant__ AttendArgs a) {
   // where the head is narrow, several groups of rows share the warps
   const int slices = (D + COLS - 1) / COLS, groups = MERGE_WARPS / slices;
   const int sub = (threadIdx.x >> 5) / slices, c0 = ((threadIdx.x >> 5) - sub * slices) * COLS;
-  // Where the prefix's kernel leaves only rows whose prefix was divided, and a CTA of it has at least an item's
-  // units, those are the items in which a CTA's units end: they alone are gone through, so that CTAs have
-  // the same work.
-  bool many = false;
-  for (int b = threadIdx.x; b < a.B; b += MERGE_THREADS) many |= cum[b + 1] - cum[b] > plan.share_o;
-  const bool ends = !__syncthreads_or(many) && a.grid_p > 0 && plan.share_p >= plan.kP;
-  const int per_head = (plan.R + 31) / 32, per_item = a.rt_p / 32;
-  const int all = ends ? (plan.UP - 1) / plan.share_p * per_item : per_head * a.Hkv;
+  const int per_head = (plan.R + 31) / 32, all = per_head * a.Hkv;
   bool waited = false;
   for (int w = (int)blockIdx.x * groups + sub; w - sub < all; w += (int)gridDim.x * groups) {
     bool mine = w < all && sub < groups;           // (and not written by one of the kernels before)
-    int h, r;
-    if (ends) {
-      const int u = (w / per_item + 1) * plan.share_p, item = u / plan.kP;
-      h = item / plan.nPT;
-      r = (item - h * plan.nPT) * a.rt_p + (w % per_item) * 32 + lane;
-      mine = mine && u != item * plan.kP;
-    } else {
-      h = w / per_head;
-      r = (w - h * per_head) * 32 + lane;
-    }
+    const int h = w / per_head, r = (w - h * per_head) * 32 + lane;
     mine = mine && r < plan.R;
     Parts pre{}, own{};                            // over the prefix, over the own entries
     int token = 0;
