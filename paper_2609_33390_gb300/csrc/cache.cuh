@@ -259,7 +259,8 @@ __device__ void scan_lengths(const Args& a, int kt, int32_t* cum, int* warp_sum,
 }
 
 // Parts of a row's own entries that the prefix's kernel joins itself, where it has all the prefix for the row;
-// with more, whose loads would wait for one another, it leaves a part too.
+// with more, whose loads would wait for one another, it leaves a part too (128 blocks of 32 positions over 8192 + 256
+// to 1024 entries: none 459 us, one or two 440).
 constexpr int JOIN_PARTS = 2;
 
 // The parts of row `r` of a head, over the prefix or over the own entries: a run of `n` slots.
