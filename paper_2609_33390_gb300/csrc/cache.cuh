@@ -38,12 +38,32 @@ struct Divisor {
   }
 };
 
+// What the division of the work (see Plan) knows of a call before its lengths.
+struct Shape {
+  int kt, rt_p, rt_o;                // keys of a tile; rows of a tile over the prefix and over own caches
+  int grid_p, grid_o;                // CTAs of the kernel for the prefix (0: the one for the own caches has both), of that
+  int weight;
+  int R, kP, nPT, nLT;               // rows a key head; key and row tiles of the prefix; row tiles of a sequence
+  int log_kt, log_p, log_o;          // kt, rt_p and rt_o as powers of two (a weights call's rt_o is no power)
+  Divisor by_grid;                   // grid_o
+  void set(int B, int LG, int P) {
+    auto log2 = [](int x) { int l = 0; while ((2LL << l) <= x) ++l; return l; };
+    R = B * LG;
+    kP = (int)(((long long)P + kt - 1) / kt);
+    nPT = P > 0 ? (int)(((long long)R + rt_p - 1) / rt_p) : 0;
+    nLT = (int)(((long long)LG + rt_o - 1) / rt_o);
+    log_kt = log2(kt);
+    log_p = log2(rt_p);
+    log_o = log2(rt_o);
+    by_grid.set(grid_o);
+  }
+};
+
 struct AttendArgs {
+  static constexpr bool PREFIX = true;   // units of a prefix's, and items filled up (see Plan)
   int B, L, G, Hkv, D, P, S;         // G query heads a key head
   int dt;                            // brisk_dtype of q, keys, values and out
-  // division of the work (see Plan): rows and keys of a tile; CTAs of the kernel for the prefix (0: the one
-  // for the own caches has both) and of the one for the own caches
-  int rt_p, rt_o, kt, grid_p, grid_o, weight;
+  Shape sh;
   CacheView q, kp, vp, ko, vo;
   Divisor by_L, by_G, by_LG;         // L, G and L * G
   const int32_t* own_len;            // [B]
@@ -70,45 +90,58 @@ struct AttendArgs {
 // each CTA takes `share` of them, wherever that begins and ends; or the prefix's and the own caches' are two
 // sequences of two kernels (apart), the own caches' first. A row tile's keys may so be divided over several CTAs,
 // each of which leaves a part; the parts are joined by a merge kernel.
-// Where a prefix's unit takes far longer than an own one (fp32, few rows a sequence), it counts as `weight`
+// Where there are CTAs to spare, attention's items (the keys of a row tile) are filled up to whole shares with units
+// that hold nothing, so that no CTA has parts of two items, each with its own way from the first load to the stored
+// part (a block of 32 positions over 4096 and 1100 entries 23.6 -> 19.5 us, 13 blocks of 7 over 3001 and up to 777 30.2
+// -> 23.4). Where a prefix's unit takes far longer than an own one (fp32, few rows a sequence), it counts as `weight`
 // units, in the CTA that has the first of them. (A share is at least a weight: no CTA between two of the prefix's
 // parts is without one.)
 // Slots: walking through a sequence, (item index + CTA) grows with every (item, CTA) pair, so it
 // numbers the parts. Counts of units fit 31 bits (checked on the host).
 struct Plan {
-  int B, LG, Hkv, rt_p, rt_o, kt;
-  int nPT, kP, nLT;                  // row tiles and key tiles of the prefix; row tiles of a sequence
-  int R, UP, UO;                     // rows a key head; units of the prefix and of the own caches
+  int B, LG, Hkv;
+  int nPT, kP, nLT, R;               // as Shape's
+  int kPp;                           // units of a row tile over the prefix: kP, filled up
+  int UP, UO;                        // units of the prefix and of the own caches
   int own0;                          // number of the own caches' first unit
   int weight;                        // units that one of the prefix's counts as
   int share_p, share_o;              // units a CTA
-  int log_p, log_o;                  // rt_p and rt_o as powers of two, where they are
+  int filled;                        // what items are filled up to a multiple of
   bool apart;                        // the prefix's units and the own caches' are two sequences
 
   Plan() = default;
-  __device__ Plan(int b, int lg, int hkv, int p, int rtp, int rto, int kt_, int own_tiles, int grid_p, int grid_o,
-                  int weight_) {
-    B = b; LG = lg; Hkv = hkv; rt_p = rtp; rt_o = rto; kt = kt_;
-    R = B * LG;
-    kP = (p + kt - 1) / kt;
-    nPT = p > 0 ? (R + rt_p - 1) / rt_p : 0;
-    nLT = (LG + rt_o - 1) / rt_o;
-    UP = Hkv * nPT * kP;
+  // (own_tiles: of all sequences, filled up to multiples of pad)
+  template <typename Args>
+  __device__ Plan(const Args& a, int own_tiles, int pad) {
+    const Shape& sh = a.sh;
+    B = a.B; LG = a.L * a.G; Hkv = a.Hkv; nLT = sh.nLT; R = sh.R;
+    nPT = Args::PREFIX ? sh.nPT : 0;
+    kP = Args::PREFIX ? sh.kP : 0;
+    apart = Args::PREFIX && sh.grid_p > 0;
+    filled = Args::PREFIX ? pad : 1;
+    kPp = apart ? kP : fill(kP, pad);
+    UP = Hkv * nPT * kPp;
     UO = Hkv * nLT * own_tiles;
-    apart = grid_p > 0;
-    // (an own fragment costs about one and a half of its units more, whatever its length)
-    if (weight_ > 1) weight_ = max(1, (int)(2ll * own_tiles * weight_ / (2ll * own_tiles + 3 * B)));
-    const unsigned all = (unsigned)UP * weight_ + UO;          // (UP and UO: up to 2e9 together)
-    weight = UP < (1 << 28) && all < (1u << 31) && all / grid_o >= (unsigned)weight_ ? weight_ : 1;
+    weight = 1;
+    if (Args::PREFIX && pad == 1 && sh.weight > 1) {
+      // an own fragment costs about one and a half of its units more, whatever its length (rounded alike in all kernels)
+      const float t = (float)own_tiles;
+      const int w = max(1, (int)__fdiv_rn(__fmul_rn(t, (float)sh.weight), __fadd_rn(t, __fmul_rn(1.5f, (float)B))));
+      const unsigned all = (unsigned)UP * w + UO;            // (UP and UO: up to 2e9 together)
+      if (UP < (1 << 28) && all < 0x7ffff000u && sh.by_grid.of(all) >= w) weight = w;
+    }
     own0 = apart ? 0 : UP * weight;
-    share_o = max(1, (int)(((unsigned)own0 + UO + grid_o - 1) / grid_o));
-    log_p = 31 - __clz(rt_p);
-    log_o = 31 - __clz(rt_o);
-    share_p = apart ? max(1, (int)(((unsigned)UP + grid_p - 1) / grid_p)) : share_o;
+    share_o = max(1, sh.by_grid.of(own0 + UO + sh.grid_o - 1));
+    share_p = apart ? max(1, (UP + sh.grid_p - 1) / sh.grid_p) : share_o;
   }
-  __device__ Plan(const AttendArgs& a, int own_tiles)
-      : Plan(a.B, a.L * a.G, a.Hkv, a.P, a.rt_p, a.rt_o, a.kt, own_tiles, a.grid_p, a.grid_o, a.weight) {}
-  __device__ int tiles(int len) const { return (len + kt - 1) / kt; }
+  __device__ static int fill(int n, int pad) { return pad == 1 ? n : (n + pad - 1) / pad * pad; }
+  // Of a plan whose items are not filled up: its share, if filling them up to a multiple of it lets no CTA's share
+  // grow; else 1.
+  __device__ int fill_to(int grid_o) const {
+    if (share_o == 1) return 1;
+    const long long items = (long long)Hkv * ((long long)nLT * B + (apart ? 0 : nPT));
+    return weight == 1 && (long long)own0 + UO + items * (share_o - 1) <= (long long)share_o * grid_o ? share_o : 1;
+  }
 };
 
 // The units a CTA has of a sequence of `all`.
@@ -119,60 +152,67 @@ __device__ __forceinline__ int2 units_of(int cta, int share, int all) {
 
 // A CTA's share of one item (a row tile's keys): key tiles [k0, k0 + n).
 struct Frag {
-  int prefix, whole;                 // whole: no other part for these rows exists
+  int prefix, whole, last;           // whole: no other part for these rows exists; last: of the CTA
   int h, b, k0, n;
   int row0, rows;                    // rows of the head over the prefix, of the sequence else
   int slot, len;                     // len: entries of the prefix, or in use of the own cache
 };
 
-// The sequence of a CTA's first own unit, and the key tiles of the sequences before it (see scan_lengths).
+// The sequence of a CTA's first own unit, and the key tiles of the sequences before it (see make_plan).
 struct Start { int b, before; };
 
 template <typename Args>
 __device__ __forceinline__ int clamped_len(const Args& a, int b) {
   return min(max(a.own_len[b], 0), a.S);
 }
+template <typename Args>
+__device__ __forceinline__ int tiles_of(const Args& a, int len) {
+  return (len + a.sh.kt - 1) >> a.sh.log_kt;
+}
 
 // Walks through a CTA's units: the prefix's (unless another kernel has them, apart), then the own caches'.
 struct Walk {
   int pu, pend;                      // the prefix's next unit and their end
-  int u, end, c, b, base, n, len;    // the own ones'; b: sequence whose units begin at `base`, n key tiles
+  int u, end, c, b, base, n, len;    // the own ones'; b: sequence whose units begin at `base`, n for a row tile
+  int later;                         // the next sequence's length, on its way
 
   Walk() = default;
   template <typename Args>
   __device__ Walk(const Args& a, const Plan& p, int cta, const Start& start) {
     const int2 r = units_of(cta, p.share_o, p.own0 + p.UO);
     pu = pend = 0;
-    if (!p.apart && r.x < p.own0) {
+    if (Args::PREFIX && !p.apart && r.x < p.own0) {
       pu = (r.x + p.weight - 1) / p.weight;
       pend = (min(r.y, p.own0) + p.weight - 1) / p.weight;
     }
     u = max(r.x, p.own0);
     end = r.y;
     c = cta;
-    b = base = n = len = 0;
+    b = base = n = len = later = 0;
     if (u < end) {                   // (a CTA without own units has no start)
       b = start.b;
       base = p.own0 + p.Hkv * p.nLT * start.before;
       len = clamped_len(a, b);
-      n = p.tiles(len);
+      n = Plan::fill(tiles_of(a, len), p.filled);
+      later = a.own_len[min(b + 1, a.B - 1)];
     }
   }
   template <typename Args>
   __device__ bool next(const Args& a, const Plan& p, Frag& f) {
-    if (pu < pend) {
-      const int item = pu / p.kP;
+    if constexpr (Args::PREFIX) if (pu < pend) {
+      const int item = pu / p.kPp, stop = min((item + 1) * p.kPp, pend);
       f.prefix = 1;
-      f.k0 = pu - item * p.kP;
-      f.n = min(p.kP - f.k0, pend - pu);
+      f.k0 = pu - item * p.kPp;
+      f.n = min(p.kP - f.k0, stop - pu);
       f.h = item / p.nPT;
       f.b = 0;
-      f.row0 = (item - f.h * p.nPT) * p.rt_p;
-      f.rows = min(p.rt_p, p.R - f.row0);
+      f.row0 = (item - f.h * p.nPT) * a.sh.rt_p;
+      f.rows = min(a.sh.rt_p, p.R - f.row0);
       f.slot = item + c;
       f.whole = f.n == p.kP && a.S == 0;
       f.len = a.P;
-      pu += f.n;
+      pu = stop;
+      f.last = pu >= pend && u >= end;
       return true;
     }
     if (u >= end) return false;
@@ -180,21 +220,23 @@ struct Walk {
     while (u >= base + per * n) {
       base += per * n;
       ++b;
-      len = clamped_len(a, b);
-      n = p.tiles(len);
+      len = min(max(later, 0), a.S);
+      n = Plan::fill(tiles_of(a, len), p.filled);
+      later = a.own_len[min(b + 1, a.B - 1)];
     }
-    const int r = (u - base) / n, tile = r % p.nLT;
+    const int r = (u - base) / n, tile = r % p.nLT, real = tiles_of(a, len), stop = min(base + (r + 1) * n, end);
     f.prefix = 0;
     f.b = b;
     f.h = r / p.nLT;
     f.k0 = u - base - r * n;
-    f.n = min(n - f.k0, end - u);
-    f.row0 = tile * p.rt_o;
-    f.rows = min(p.rt_o, p.LG - f.row0);
+    f.n = min(real - f.k0, stop - u);
+    f.row0 = tile * a.sh.rt_o;
+    f.rows = min(a.sh.rt_o, p.LG - f.row0);
     f.slot = b * per + r + c;
-    f.whole = f.n == n && p.UP == 0;
+    f.whole = f.n == real && p.UP == 0;
     f.len = len;
-    u += f.n;
+    u = stop;
+    f.last = u >= end;
     return true;
   }
 };
@@ -219,43 +261,54 @@ __device__ __forceinline__ bool row_idle(const AttendArgs& a, int token) {
   return a.visible && a.visible[token] < 0;
 }
 
-// Sums the sequences' key tiles, by all THREADS threads of a CTA, and finds the sequence of key tile
-// first_own(sum) (of all sequences' in a row) in shared memory, valid after the call. The tiles before each
-// sequence go to `cum` unless that is nullptr; *bad is set where a length lies outside 0..S (the caller
-// clears it before a barrier).
-template <int THREADS, typename Args, typename First>
-__device__ void scan_lengths(const Args& a, int kt, int32_t* cum, int* warp_sum, int* bad, Start* start,
-                             First first_own) {
+// The plan of a call, by all THREADS threads of a CTA: sums the sequences' key tiles and finds the sequence of the first
+// own unit of `cta` (-1: not asked for) in shared memory, valid after the call. The tiles before each sequence go to
+// `cum` unless that is nullptr; *bad is set where a length lies outside 0..S (the caller clears it before a barrier).
+template <int THREADS, typename Args>
+__device__ Plan make_plan(const Args& a, int cta, int32_t* cum, int* warp_sum, int* bad, Start* start) {
   const int per = (a.B + THREADS - 1) / THREADS, tid = threadIdx.x, lane = tid & 31;
   const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
-  int sum = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int len = a.own_len[b];
+  const int mine = b0 < b1 ? a.own_len[b0] : 0;    // (seldom more than one a thread)
+  auto tiles = [&](int b, int pad) {
+    const int len = b == b0 ? mine : a.own_len[b];
     if (len < 0 || len > a.S) *bad = 1;
-    sum += (min(max(len, 0), a.S) + kt - 1) / kt;
-  }
-  int run = sum;
+    return Plan::fill(tiles_of(a, min(max(len, 0), a.S)), pad);
+  };
+  int pad = 1, before, total;
+  Plan plan;
+  for (;;) {
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) sum += tiles(b, pad);
+    int run = sum;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(FULL_MASK, run, o);
-    if (lane >= o) run += x;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(FULL_MASK, run, o);
+      if (lane >= o) run += x;
+    }
+    if (lane == 31) warp_sum[tid >> 5] = run;
+    __syncthreads();
+    before = run - sum;
+    total = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < (tid >> 5)) before += warp_sum[w];
+      total += warp_sum[w];
+    }
+    plan = Plan(a, total, pad);
+    if (pad > 1) break;
+    if constexpr (Args::PREFIX) pad = plan.fill_to(a.sh.grid_o);
+    if (pad == 1) break;
+    __syncthreads();                               // the sums are read
   }
-  if (lane == 31) warp_sum[tid >> 5] = run;
-  __syncthreads();
-  int before = run - sum, total = 0;
-  for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < (tid >> 5)) before += warp_sum[w];
-    total += warp_sum[w];
-  }
-  const int at = first_own(total);
+  const int at = cta < 0 ? -1 : max(0, units_of(cta, plan.share_o, plan.own0 + plan.UO).x - plan.own0) / (plan.Hkv * plan.nLT);
   for (int b = b0; b < b1; ++b) {
-    const int n = (clamped_len(a, b) + kt - 1) / kt;
+    const int n = tiles(b, pad);
     if (cum) cum[b] = before;
     if (at >= before && at < before + n) *start = Start{b, before};
     before += n;
   }
   if (cum && tid == 0) cum[a.B] = total;
   __syncthreads();
+  return plan;
 }
 
 // Parts of a row's own entries that the prefix's kernel joins itself, where it has all the prefix for the row;
@@ -271,26 +324,26 @@ struct Parts {
 };
 // (by_share_p, by_share_o: the plan's)
 __device__ __forceinline__ Parts prefix_parts(const AttendArgs& a, const Plan& p, const Divisor& by_share_p, int h, int r) {
-  Parts x{0, min(p.rt_p, p.R), nullptr, nullptr};
+  Parts x{0, min(a.sh.rt_p, p.R), nullptr, nullptr};
   if (p.kP == 0) return x;
-  const int pt = r >> p.log_p, first = (h * p.nPT + pt) * p.kP;
+  const int pt = r >> a.sh.log_p, first = (h * p.nPT + pt) * p.kPp;
   const int c0 = by_share_p.of(first * p.weight), slot = h * p.nPT + pt + c0;
-  x.n = by_share_p.of((first + p.kP - 1) * p.weight) - c0 + 1;
-  x.sums = a.part_p + part_at(slot, x.per, a.D, r - (pt << p.log_p), 0);
-  x.ml = a.ml_p + (long long)slot * x.per + (r - (pt << p.log_p));
+  x.n = by_share_p.of((first + p.kPp - 1) * p.weight) - c0 + 1;
+  x.sums = a.part_p + part_at(slot, x.per, a.D, r - (pt << a.sh.log_p), 0);
+  x.ml = a.ml_p + (long long)slot * x.per + (r - (pt << a.sh.log_p));
   return x;
 }
-// (cum as scan_lengths leaves it)
+// (cum as make_plan leaves it)
 __device__ __forceinline__ Parts own_parts(const AttendArgs& a, const Plan& p, const Divisor& by_share_o, const int32_t* cum,
                                            int h, int r) {
-  Parts x{0, min(p.rt_o, p.LG), nullptr, nullptr};
+  Parts x{0, min(a.sh.rt_o, p.LG), nullptr, nullptr};
   const int b = a.by_LG.of(r), before = cum[b], n = cum[b + 1] - before;
   if (n == 0) return x;
-  const int ro = r - b * p.LG, lt = ro >> p.log_o, of = h * p.nLT + lt, per = p.Hkv * p.nLT;
+  const int ro = r - b * p.LG, lt = ro >> a.sh.log_o, of = h * p.nLT + lt, per = p.Hkv * p.nLT;
   const int u = p.own0 + per * before + of * n, c0 = by_share_o.of(u), slot = b * per + of + c0;
   x.n = by_share_o.of(u + n - 1) - c0 + 1;
-  x.sums = a.part_o + part_at(slot, x.per, a.D, ro - (lt << p.log_o), 0);
-  x.ml = a.ml_o + (long long)slot * x.per + (ro - (lt << p.log_o));
+  x.sums = a.part_o + part_at(slot, x.per, a.D, ro - (lt << a.sh.log_o), 0);
+  x.ml = a.ml_o + (long long)slot * x.per + (ro - (lt << a.sh.log_o));
   return x;
 }
 
@@ -326,13 +379,14 @@ inline void divide(AttendArgs* a) {
   const long long R = (long long)a->B * a->L * a->G;
   const long long units = a->Hkv * ((R + PAIR_ROWS - 1) / PAIR_ROWS) * (((long long)a->P + TC_KT - 1) / TC_KT);
   const bool apart = tc && R > SLOT_ROWS && units >= APART_UNITS;
-  a->kt = tc ? TC_KT : SIMT_KT;
-  a->rt_o = tc ? SLOT_ROWS : SIMT_ROWS;
-  a->rt_p = apart ? PAIR_ROWS : a->rt_o;
-  a->grid_p = apart ? CACHE_SMS : 0;
-  a->grid_o = SLOT_CTAS;
   const int rows = a->L * a->G;
-  a->weight = !tc && R > FEW_ROWS && rows <= FEW_ROWS ? (rows <= 4 ? 6 : 4) : 1;
+  a->sh.kt = tc ? TC_KT : SIMT_KT;
+  a->sh.rt_o = tc ? SLOT_ROWS : SIMT_ROWS;
+  a->sh.rt_p = apart ? PAIR_ROWS : a->sh.rt_o;
+  a->sh.grid_p = apart ? CACHE_SMS : 0;
+  a->sh.grid_o = SLOT_CTAS;
+  a->sh.weight = !tc && R > FEW_ROWS && rows <= FEW_ROWS ? (rows <= 4 ? 6 : 4) : 1;
+  a->sh.set(a->B, rows, a->P);
 }
 
 // A tile of 128 rows in shared memory, as the products read it: panels of 64 columns, 128 bytes a row, the
@@ -406,7 +460,9 @@ cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream);
 
 // ---------------------------------------------------------------- attention weight of own entries
 struct WeightArgs {
-  int B, L, G, Hkv, D, P, S, dt;     // P: 0 (no units of the prefix's)
+  static constexpr bool PREFIX = false;  // (128 sequences of 1024 to 4096 entries: 132 us, items filled up 138)
+  int B, L, G, Hkv, D, S, dt;
+  Shape sh;
   CacheView q, ko;
   Divisor by_G;
   const int32_t *own_len, *visible;
@@ -415,9 +471,17 @@ struct WeightArgs {
   const float* acc_in;     // [B, Hkv, S] or nullptr (zeros)
   float* acc_out;          // [B, Hkv, S]
   int32_t* status;
-  int grid;
   long long wait_limit;
 };
+inline void divide(WeightArgs* a) {
+  const int rows = a->L * a->G;
+  a->sh.kt = TC_KT;
+  a->sh.rt_p = a->sh.weight = 1;
+  a->sh.rt_o = rows;                 // all rows of a sequence are one tile
+  a->sh.grid_p = 0;
+  a->sh.grid_o = CACHE_SMS;
+  a->sh.set(a->B, rows, 0);
+}
 cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream);
 cudaError_t launch_weights_f32(const WeightArgs& a, cudaStream_t stream);
 

@@ -63,14 +63,14 @@ CacheWs cache_ws(const brisk_cache_dims* d) {
   CacheWs w{};
   const AttendArgs a = sizes_of(d);
   const long long LG = a.L * a.G, R = d->B * LG;
-  const long long tiles_p = d->P > 0 ? (R + a.rt_p - 1) / a.rt_p * d->Hkv : 0;
-  const long long tiles_o = d->S > 0 ? (LG + a.rt_o - 1) / a.rt_o * d->Hkv * d->B : 0;
-  const long long rows_p = (tiles_p + (a.grid_p ? a.grid_p : a.grid_o)) * (R < a.rt_p ? R : a.rt_p);
-  const long long rows_o = (tiles_o + a.grid_o) * (LG < a.rt_o ? LG : a.rt_o);
+  const long long tiles_p = d->P > 0 ? (R + a.sh.rt_p - 1) / a.sh.rt_p * d->Hkv : 0;
+  const long long tiles_o = d->S > 0 ? (LG + a.sh.rt_o - 1) / a.sh.rt_o * d->Hkv * d->B : 0;
+  const long long rows_p = (tiles_p + (a.sh.grid_p ? a.sh.grid_p : a.sh.grid_o)) * (R < a.sh.rt_p ? R : a.sh.rt_p);
+  const long long rows_o = (tiles_o + a.sh.grid_o) * (LG < a.sh.rt_o ? LG : a.sh.rt_o);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t q = o; o = up(o + bytes); return q; };
   w.status = take(ALIGN);
-  w.errs = take(sizeof(int32_t) * (a.grid_p + a.grid_o));
+  w.errs = take(sizeof(int32_t) * (a.sh.grid_p + a.sh.grid_o));
   w.cum = take(sizeof(int32_t) * (d->B + 1));
   w.ml_p = take(sizeof(float2) * rows_p);
   w.ml_o = take(sizeof(float2) * rows_o);
@@ -84,8 +84,8 @@ CacheWs cache_ws(const brisk_cache_dims* d) {
 bool units_ok(const brisk_cache_dims* d) {
   const AttendArgs a = sizes_of(d);
   const long long LG = a.L * a.G, R = d->B * LG;
-  const double pre = (double)d->Hkv * ((R + a.rt_p - 1) / a.rt_p) * ((d->P + a.kt - 1) / a.kt);
-  const double own = (double)d->Hkv * d->B * ((LG + a.rt_o - 1) / a.rt_o) * ((d->S + a.kt - 1) / a.kt);
+  const double pre = (double)d->Hkv * ((R + a.sh.rt_p - 1) / a.sh.rt_p) * ((d->P + a.sh.kt - 1) / a.sh.kt);
+  const double own = (double)d->Hkv * d->B * ((LG + a.sh.rt_o - 1) / a.sh.rt_o) * ((d->S + a.sh.kt - 1) / a.sh.kt);
   return pre + own < 2.0e9;
 }
 
@@ -165,7 +165,7 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
     if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
   if (d->S == 0) return BRISK_OK;
   if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
-  a.grid = CACHE_SMS;
+  divide(&a);
   return (d->dtype == BRISK_DT_BF16 ? launch_weights_tc(a, st) : launch_weights_f32(a, st)) == cudaSuccess
              ? BRISK_OK : BRISK_ERR_CUDA;
 }

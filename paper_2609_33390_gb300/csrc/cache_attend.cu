@@ -431,12 +431,8 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   if (threadIdx.x == 0) bad = 0;
   __syncthreads();
   let_next_begin();
-  int own = 0;
-  scan_lengths<SIMT_THREADS>(a, KT, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start, [&](int total) {
-    own = total;
-    const Plan p(a, total);
-    return max(0, units_of(blockIdx.x, p.share_o, p.own0 + p.UO).x - p.own0) / (p.Hkv * p.nLT);
-  });
+  const Plan own_plan =
+      make_plan<SIMT_THREADS>(a, blockIdx.x, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start);
   // (one thread walks through the units, in shared memory: the others need their registers)
   __shared__ Plan plan;
   __shared__ Walk walk;
@@ -444,7 +440,7 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   __shared__ int more;
   if (threadIdx.x == 0) {
     a.errs[blockIdx.x] = bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK;
-    plan = Plan(a, own);
+    plan = own_plan;
     walk = Walk(a, plan, blockIdx.x, start);
   }
   for (;;) {
@@ -479,8 +475,7 @@ struct Merge {                                     // what both forms know, in s
   Start start;
 };
 __device__ __forceinline__ Plan begin_merge(const AttendArgs& a, int32_t* cum, Merge* k) {
-  scan_lengths<MERGE_THREADS>(a, a.kt, cum, k->warp_sum, &k->bad, &k->start, [](int) { return -1; });
-  const Plan plan(a, cum[a.B]);
+  const Plan plan = make_plan<MERGE_THREADS>(a, -1, cum, k->warp_sum, &k->bad, &k->start);
   if (threadIdx.x == 0) k->by_share_p.set(plan.share_p);
   if (threadIdx.x == 32) k->by_share_o.set(plan.share_o);
   __syncthreads();
@@ -488,12 +483,12 @@ __device__ __forceinline__ Plan begin_merge(const AttendArgs& a, int32_t* cum, M
 }
 // Whether a kernel before has written a row with these parts.
 __device__ __forceinline__ bool written(const AttendArgs& a, const Parts& pre, const Parts& own) {
-  return a.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0);
+  return a.sh.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0);
 }
 __device__ __forceinline__ void merge_status(const AttendArgs& a) {
   if (blockIdx.x != 0 || threadIdx.x >= 32) return;
   int code = BRISK_OK;                             // the largest: a wait that gave up before a bad length
-  for (int c = threadIdx.x; c < a.grid_p + a.grid_o; c += 32) code = max(code, a.errs[c]);
+  for (int c = threadIdx.x; c < a.sh.grid_p + a.sh.grid_o; c += 32) code = max(code, a.errs[c]);
   code = __reduce_max_sync(FULL_MASK, code);
   if (threadIdx.x == 0) *a.status = code;
 }
@@ -682,7 +677,7 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
     const size_t smem = few_smem > SIMT_SMEM ? few_smem : SIMT_SMEM;
     cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
     if (e != cudaSuccess) return e;
-    kernel<<<a.grid_o, SIMT_THREADS, smem, stream>>>(a);
+    kernel<<<a.sh.grid_o, SIMT_THREADS, smem, stream>>>(a);
     return cudaGetLastError();
   };
   const int rows = a.L * a.G;

@@ -13,7 +13,7 @@
 // attend_slot_kernel, over the own caches (and over the prefix where it has few units, see divide): two
 // CTAs an SM, each working through fragments of its own. Bound by the entries' bytes where the caches are
 // long (256 single tokens over 512 to 2048 entries each, 231 us, 5.8 TB/s), by what a fragment costs around its
-// tiles where they are short (a block of 32 positions over 4096 and 1100 entries: 18 us for two tiles a CTA).
+// tiles where they are short (a block of 32 positions over 4096 and 1100 entries: 14 us for two tiles a CTA).
 // The CTAs share the units of work evenly (see Plan). Where both kernels run, the own caches' is first; the
 // prefix's takes over SM by SM and joins the own entries' parts at the end of its fragments, which are long.
 //
@@ -338,7 +338,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   auto wait = [&](uint64_t* bar, int phase) { return warp_wait(bar, phase, abort_flag, a.wait_limit); };
 
   const int R = a.B * a.L * a.G, kP = (a.P + KT - 1) / KT, nPT = (R + PAIR_ROWS - 1) / PAIR_ROWS;
-  const int UP = a.Hkv * nPT * kP, share = (UP + a.grid_p - 1) / a.grid_p;
+  const int UP = a.Hkv * nPT * kP, share = (UP + a.sh.grid_p - 1) / a.sh.grid_p;
   const int2 range = units_of(blockIdx.x, share, UP);
   int u = range.x;
   bool off = false;                                // a wait gave up
@@ -490,7 +490,7 @@ attend_pair_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
         bool part = g.n < kP;
         if (!part) {                               // all of the prefix: the own entries' parts join here
           wait_for_previous();
-          const Plan plan(a, a.cum[a.B]);
+          const Plan plan(a, a.cum[a.B], 1);         // (the prefix's units are not filled up)
           Divisor by_share;
           by_share.set(plan.share_o);
           if (mine) own = own_parts(a, plan, by_share, a.cum, g.h, g.row0 + s * SLOT + r);
@@ -564,15 +564,9 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   const uint32_t tmem = tmem_slot;
   auto wait = [&](uint64_t* bar, int phase) { return warp_wait(bar, phase, abort_flag, a.wait_limit); };
 
-  int own = 0;
-  scan_lengths<SLOT_THREADS>(a, KT, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start, [&](int total) {
-    own = total;
-    const Plan p(a, total);
-    return max(0, units_of(blockIdx.x, p.share_o, p.own0 + p.UO).x - p.own0) / (p.Hkv * p.nLT);
-  });
-  const Plan plan(a, own);
+  const Plan plan = make_plan<SLOT_THREADS>(a, blockIdx.x, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start);
   const int2 range = units_of(blockIdx.x, plan.share_o, plan.own0 + plan.UO);
-  const int units = range.y - range.x;
+  const bool some = range.x < range.y;
   int unit = 0, nf = 0;                            // tiles and fragments before
   bool off = false;
 
@@ -614,11 +608,12 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     const uint32_t q = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
     const uint32_t tS = tmem, tO = tmem + 128;
     unsigned cur = 0;
-    while (unit < units && !off) {
+    for (bool more = some; more && !off;) {
       const int fs = nf & 3;
       off = wait(&q_full, nf++);                   // (info_full came before it)
       if (off) break;
       const int n = info[fs].n, k0 = info[fs].k0, len = info[fs].len;
+      more = !info[fs].last;
       for (int j = 0; j < n && !off; ++j, ++unit) {
         const unsigned sk = cur % STAGES, sv = (cur + 1) % STAGES;
         off = wait(&full[sk], cur / STAGES);
@@ -658,10 +653,8 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
     // this one's are there), this one's end. The first turn has no fragment yet, the last no next one.
     Row y{-1, 0, nullptr};
     Frag f{};
-    bool have = false;
-    int u = 0;                                     // tiles up to the end of this fragment
+    bool have = false, next = some;
     for (;; ++nf) {                                // this fragment is number nf - 1
-      const bool next = u < units;
       Row x{-1, 0, nullptr};
       if (next) {
         off = wait(&info_full[nf & 3], nf >> 2);
@@ -743,7 +736,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
       f = info[nf & 3];
       y = x;
       have = true;
-      u += f.n;
+      next = !f.last;
     }
     rows_fetched();                                // (queries, where a wait gave up)
   }
@@ -751,7 +744,7 @@ attend_slot_kernel(const __grid_constant__ AttendMaps maps, const __grid_constan
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, 256);
   if (tid == 0)
-    a.errs[a.grid_p + blockIdx.x] =
+    a.errs[a.sh.grid_p + blockIdx.x] =
         aborted ? BRISK_ERR_TIMEOUT : (bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK);
 }
 
@@ -789,11 +782,11 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   const size_t pair_smem = a.D > 64 ? PairShape<128>::SMEM : PairShape<64>::SMEM;
   const size_t slot_smem = a.D > 64 ? SlotShape<128>::SMEM : SlotShape<64>::SMEM;
   cudaError_t e = set_up_kernel(slot, CARVEOUT_FULL_KB, slot_smem);
-  if (e == cudaSuccess) e = launch_early(slot, a.grid_o, SLOT_THREADS, slot_smem, stream, false, maps, a);
-  if (e == cudaSuccess && a.grid_p > 0) {
+  if (e == cudaSuccess) e = launch_early(slot, a.sh.grid_o, SLOT_THREADS, slot_smem, stream, false, maps, a);
+  if (e == cudaSuccess && a.sh.grid_p > 0) {
     const AttendMaps first{kp, vp, kp, vp};
     e = set_up_kernel(pair, CARVEOUT_FULL_KB, pair_smem);
-    if (e == cudaSuccess) e = launch_early(pair, a.grid_p, PAIR_THREADS, pair_smem, stream, true, first, a);
+    if (e == cudaSuccess) e = launch_early(pair, a.sh.grid_p, PAIR_THREADS, pair_smem, stream, true, first, a);
   }
   return e;
 }

@@ -260,7 +260,7 @@ struct Passes {
       }
       n = nb > 2 ? min(CHUNK, f.n - at) : f.n;
     }
-    p = Pass{f.b, f.h, f.k0 + at, n, f.len, 0, f.k0 + at + n == plan.tiles(f.len), q0, min(2, nb - q0), before & 1};
+    p = Pass{f.b, f.h, f.k0 + at, n, f.len, 0, f.k0 + at + n == tiles_of(a, f.len), q0, min(2, nb - q0), before & 1};
     q0 += 2;
     return true;
   }
@@ -316,13 +316,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   const uint32_t tmem = tmem_slot;
 
   const int rows = a.L * a.G, nb = (rows + QB - 1) / QB;
-  int own = 0;
-  scan_lengths<WT_THREADS>(a, KT, nullptr, warp_sum, &bad, &start, [&](int total) {
-    own = total;
-    const Plan p(a.B, rows, a.Hkv, 0, 1, rows, KT, total, 0, a.grid, 1);
-    return units_of(blockIdx.x, p.share_o, p.UO).x / a.Hkv;
-  });
-  const Plan plan(a.B, rows, a.Hkv, 0, 1, rows, KT, own, 0, a.grid, 1);
+  const Plan plan = make_plan<WT_THREADS>(a, blockIdx.x, nullptr, warp_sum, &bad, &start);
   // sequences without entries have no units: zeros everywhere
   for (int b = blockIdx.x; b < a.B; b += gridDim.x)
     if (clamped_len(a, b) == 0)
@@ -542,7 +536,7 @@ cudaError_t launch_weights_tc(const WeightArgs& a, cudaStream_t stream) {
   auto run = [&](auto kernel, size_t smem) {
     cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
     if (e != cudaSuccess) return e;
-    kernel<<<a.grid, WT_THREADS, smem, stream>>>(map, a);
+    kernel<<<a.sh.grid_o, WT_THREADS, smem, stream>>>(map, a);
     return cudaGetLastError();
   };
   return a.D > 64 ? run(weights_tc_kernel<128>, WShape<128>::SMEM) : run(weights_tc_kernel<64>, WShape<64>::SMEM);
