@@ -12,13 +12,13 @@
 // heads on 8, D = 128, over 8192 entries 320 us, 1.7 PFLOP/s.
 // attend_slot_kernel, over the own caches (and over the prefix where it has few units, see divide): two
 // CTAs an SM, each working through fragments of its own. Bound by the entries' bytes where the caches are
-// long (256 single tokens over 512 to 2048 entries each, 231 us, 5.8 TB/s), by what a fragment costs around its
+// long (256 single tokens over 512 to 2048 entries each, 222 us, 6 TB/s), by what a fragment costs around its
 // tiles where they are short (a block of 32 positions over 4096 and 1100 entries: 14 us for two tiles a CTA).
 // The CTAs share the units of work evenly (see Plan). Where both kernels run, the own caches' is first; the
 // prefix's takes over SM by SM and joins the own entries' parts at the end of its fragments, which are long.
 //
 // The maximum a row subtracts is held back until a score exceeds it by 2^8: P and the sums then stay
-// below 2^8 times their number, and O is seldom rescaled (128 blocks as above, own entries too: 438 us, 479 with the
+// below 2^8 times their number, and O is seldom rescaled (128 blocks as above, own entries too: 437 us, 479 with the
 // exact maximum). Rounding P to bf16 costs at most 2^-9 of each
 // weight, as much as rounding the result; sums are fp32.
 //
