@@ -364,11 +364,11 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
 // than SLOT_ROWS query rows a key head, the prefix has a kernel of its own from APART_UNITS of its units on.
 // That kernel reads a key tile for twice the rows, but is one more launch and divides the prefix by itself: 32 query
 // heads on 8, own caches of up to 300, R rows a key head: U units of it take, with and without it,
-//   U 64 (R 512): 29.4 and 25.0 us; 256 (512): 34.8 and 34.8; 512 (1024): 34.5 and 42.6; 1024 (2048): 48.6 and 65.2;
-//   4096 (4096): 97 and 167.
+//   U 64 (R 512): 25.8 and 18.0 us; 256 (512): 32.2 and 29.2; 384 (640): 35.5 and 32.3; 432 (512): 34.2 and 35.4;
+//   480 (640): 33.0 and 32.5; 512 (1024): 34.0 and 39.5; 1024 (2048): 48.0 and 59.7; 4096 (4096): 95 and 155.
 constexpr int TC_KT = 128, SLOT_ROWS = 128, PAIR_ROWS = 256, SIMT_KT = 64, SIMT_ROWS = 64;
 constexpr int SLOT_CTAS = 2 * CACHE_SMS;             // (the fp32 kernel's, too)
-constexpr int APART_UNITS = 2 * CACHE_SMS;
+constexpr int APART_UNITS = 3 * CACHE_SMS;
 // fp32: up to FEW_ROWS rows of a sequence have a form of their own (64 single tokens, 32 heads on 8, D = 128, over
 // 1000 to 2000 own and 2000 shared entries: 216 us, with the form for more rows 685 us). One of its units takes about
 // a sixth (up to 4 rows) or a fourth of the time of a prefix's unit of a full tile, where own caches are long: counting

@@ -115,7 +115,8 @@ def lens_of(Bn, S, step=37):
 
 BF_SIZES = [
     # B, L, Hq, Hkv, D, P, S
-    (5, 32, 32, 8, 128, 2001, 700),       # 3 row tiles a head, the last one half full; 2 or 3 units a CTA
+    (5, 32, 32, 8, 128, 2001, 700),       # several row tiles a head, the last one half full
+    (9, 33, 32, 8, 128, 2001, 700),       # 5 row tiles, 4 or 5 units a CTA
     (40, 8, 16, 4, 64, 4000, 300),        # narrow heads, 5 row tiles
     (40, 8, 12, 4, 40, 5000, 90),
     (40, 16, 64, 32, 72, 384, 200),       # whole items a CTA: the items divided at the CTAs' ends alone
