@@ -168,6 +168,21 @@ def _stream(stream=None):
     return stream.cuda_stream
 
 
+def _results(stream, make):
+    """make()'s new tensors (a dict), for a call on ``stream`` to write. They are allocated for that stream:
+    memory of the current one may be what a kernel still pending there reads or writes, and would be free
+    for it again, once dropped, while the call still writes. Whoever reads them on the current stream
+    may drop them without waiting, too."""
+    if stream is None or stream.cuda_stream == _stream():
+        return make()
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        new = make()
+    for t in new.values():
+        t.record_stream(here)
+    return new
+
+
 def make_dims(B, L, V, d, K, r, logits_dtype, hidden_dtype) -> Dims:
     return Dims(B, L, V, d, K, r, _dt(logits_dtype), _dt(hidden_dtype))
 
@@ -436,6 +451,7 @@ class PrefixAttention:
     ``dtype`` (bf16 or fp32). Tensors are [.., positions, heads, D] with any strides whose rows
     start on 16 bytes (a transposed cache, a slice of a fused projection); lengths, sums and
     outputs are contiguous. The workspace is allocated once here, so calls of one object must not overlap.
+    What a call given a ``stream`` allocates itself is that stream's memory (see _results).
     """
 
     def __init__(self, B, L, Hq, Hkv, D, P, S, dtype, device="cuda"):
@@ -485,6 +501,13 @@ class PrefixAttention:
             raise ValueError(f"{what} is not on the GPU")
         return _p(t)
 
+    def _attended(self):
+        return {"out": torch.empty(self._shape_q, dtype=self.dtype, device=self.device),
+                "lse": torch.empty(self._shape_lse, dtype=torch.float32, device=self.device)}
+
+    def _weighed(self):
+        return {"acc": torch.empty(self._shape_acc, dtype=torch.float32, device=self.device)}
+
     def attend(self, q, k_prefix, v_prefix, k_own, v_own, own_len, visible=None, scale=None,
                out=None, stream=None):
         """out [B, L, Hq, D] and lse [B, L, Hq] of the queries q [B, L, Hq, D] over k/v_prefix
@@ -493,8 +516,7 @@ class PrefixAttention:
         of tensors to write to instead of new ones."""
         pre, own, view, plain, at = self._shape_pre, self._shape_own, self._view, self._plain, self._at
         if out is None:
-            out = {"out": torch.empty(self._shape_q, dtype=self.dtype, device=self.device),
-                   "lse": torch.empty(self._shape_lse, dtype=torch.float32, device=self.device)}
+            out = _results(stream, self._attended)
         _PACK5(self._views, 0, *view(q, self._shape_q, "q"), *(view(k_prefix, pre, "k_prefix") or _NONE),
                *(view(v_prefix, pre, "v_prefix") or _NONE), *(view(k_own, own, "k_own") or _NONE),
                *(view(v_own, own, "v_own") or _NONE))
@@ -516,7 +538,7 @@ class PrefixAttention:
         new tensor. acc None: zeros."""
         plain, at, f32, i32 = self._plain, self._at, torch.float32, torch.int32
         if out is None:
-            out = torch.empty(self._shape_acc, dtype=f32, device=self.device)
+            out = _results(stream, self._weighed)["acc"]
         _PACK2(self._views, 0, *self._view(q, self._shape_q, "q"),
                *(self._view(k_own, self._shape_own, "k_own") or _NONE))
         s = lib().brisk_cache_weights(
@@ -546,8 +568,8 @@ class PrefixAttention:
         all, to the caches of ``out`` (see alloc_evicted and brisk_cache_evict): between two layers,
         one spare pair of caches serves them all in turn."""
         if out is None:
-            # (the call writes all of them, on its own stream)
-            out = self._evicted(torch.empty, keep, keep)
+            # (the call writes all of them)
+            out = _results(stream, lambda: self._evicted(torch.empty, keep, keep))
         plain, view, at, f32, i32 = self._plain, self._view, self._at, torch.float32, torch.int32
         k_to, B, Hkv = out["k"], self.B, self.Hkv
         room = k_to.shape[1]

@@ -1,0 +1,63 @@
+"""Calls on a stream of their own beside a current stream that is far behind: what they allocate is
+neither what the current stream still has to read, nor free before the current stream has read it."""
+import pytest
+import torch
+
+from test_cache_gpu import BF, make
+
+pytestmark = pytest.mark.gpu
+
+BEHIND = 20_000_000                                    # cycles, about 10 ms
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2609_33390_gb300 import build
+    build.build()
+    from paper_2609_33390_gb300 import brisk
+    return brisk
+
+
+def cache_calls(B):
+    x = make(3, 2, 8, 2, 64, 100, 60, BF, [60, 40, 5])
+    att = B.PrefixAttention(3, 2, 8, 2, 64, 100, 60, BF)
+    lse = torch.full((3, 2, 8), 3.0, device="cuda")
+    acc = torch.rand(3, 2, 60, device="cuda")
+    return {"attend": lambda s: att.attend(x["q"], x["kp"], x["vp"], x["ko"], x["vo"], x["lens"], stream=s),
+            "weights": lambda s: {"acc": att.weights(x["q"], lse, x["ko"], x["lens"], stream=s)},
+            "evict": lambda s: att.evict(x["ko"], x["vo"], acc, x["lens"], 30, 5, stream=s)}
+
+
+def check_beside_a_late_stream(call):
+    want = {k: v.clone() for k, v in call(None).items()}
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    # memory that the current stream has yet to read, dropped
+    old = {k: torch.full_like(v, 7) for k, v in want.items()}
+    read = {k: torch.zeros_like(v) for k, v in want.items()}
+    torch.cuda._sleep(BEHIND)
+    for k, v in old.items():
+        read[k].copy_(v)
+    del old, v
+    got = call(s)
+    torch.cuda.synchronize()
+    for k in want:
+        assert (read[k] == 7).all() and torch.equal(got[k], want[k])
+    # results that the current stream has yet to read, dropped, and the next call
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda._sleep(BEHIND)
+    for k in want:
+        read[k].copy_(got[k])
+    del got
+    again = call(s)
+    with torch.cuda.stream(s):
+        for v in again.values():
+            v.fill_(3)
+    torch.cuda.synchronize()
+    for k in want:
+        assert torch.equal(read[k], want[k])
+
+
+@pytest.mark.parametrize("name", ["attend", "weights", "evict"])
+def test_results_do_not_race_with_a_current_stream_that_is_behind(B, name):
+    check_beside_a_late_stream(cache_calls(B)[name])

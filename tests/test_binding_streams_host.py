@@ -1,0 +1,80 @@
+"""Calls on a stream other than the current one: whose memory their results are, without a GPU. The
+library, the streams and the checks of places are stand-ins; the calls' own allocations are watched."""
+import contextlib
+
+import pytest
+import torch
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class Watch:
+    """What is allocated, under which stream, and which streams its memory is also kept for."""
+
+    def __init__(self):
+        self.under, self.made, self.kept = None, [], {}
+
+
+@pytest.fixture
+def B():
+    from paper_2609_33390_gb300 import build
+    build.build()
+    from paper_2609_33390_gb300 import brisk
+    return brisk
+
+
+@pytest.fixture
+def watch(B, monkeypatch):
+    w, real, here = Watch(), B.lib(), Stream(1)
+
+    class Lib:                                         # sizes are the library's, calls do nothing
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith("_bytes") else lambda *a: B.OK
+
+    @contextlib.contextmanager
+    def stream(s):
+        before, w.under = w.under, s
+        yield
+        w.under = before
+
+    def empty(*a, **k):
+        t = alloc(*a, **k)
+        w.made.append((t, w.under))
+        return t
+
+    alloc = torch.empty
+    monkeypatch.setattr(B, "lib", lambda: Lib())
+    monkeypatch.setattr(B, "_stream", lambda s=None: (here if s is None else s).cuda_stream)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: here)
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: w.kept.setdefault(id(t), []).append(s))
+    monkeypatch.setattr(B.PrefixAttention, "_view", lambda self, t, shape, what: (0, 0, 0, 0))
+    monkeypatch.setattr(B.PrefixAttention, "_plain", staticmethod(lambda t, shape, dtype, what: None))
+    w.here = here
+    return w
+
+
+def cache_calls(B):
+    att = B.PrefixAttention(2, 3, 4, 2, 64, 10, 20, torch.bfloat16, device="cpu")
+    return {"attend": lambda s: att.attend(*[None] * 6, stream=s),
+            "weights": lambda s: {"acc": att.weights(*[None] * 4, stream=s)},
+            "evict": lambda s: att.evict(*[None] * 4, 8, 2, stream=s)}
+
+
+def check_results(watch, call):
+    for given, other in ((None, False), (Stream(1), False), (Stream(2), True)):
+        watch.made, watch.kept = [], {}
+        r = call(given)
+        assert r and {id(t) for t in r.values()} == {id(t) for t, _ in watch.made}
+        for t, under in watch.made:
+            assert under is (given if other else None)
+            assert watch.kept.get(id(t), []) == ([watch.here] if other else [])
+
+
+@pytest.mark.parametrize("name", ["attend", "weights", "evict"])
+def test_results_are_memory_of_the_stream_that_writes_them(B, watch, name):
+    check_results(watch, cache_calls(B)[name])
