@@ -135,9 +135,11 @@ __device__ __forceinline__ void row_weights(uint32_t tS, uint32_t tO, int D, int
 #pragma unroll
   for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], v[KT - 4 + i]);
   const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
-  if (__any_sync(FULL_MASK, t > m + LAZY)) {
-    const float mn = fmaxf(m, t), alpha = ex2(m - (mn == -INFINITY ? 0.f : mn));
-    m = mn;
+  // (each row by its own scores: a row's bits must not hang on its neighbours', of which some may be no rows at all)
+  const bool over = t > m + LAZY;
+  if (__any_sync(FULL_MASK, over)) {
+    const float alpha = over ? ex2(m - t) : 1.f;   // (t is no -inf)
+    if (over) m = t;
     l *= alpha;
     if (!first)
 #pragma unroll 1
