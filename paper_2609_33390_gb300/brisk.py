@@ -216,7 +216,8 @@ class DecodeTail:
 
     ``weights`` holds the corrector parameters and E_in / E_out as CUDA tensors in the hidden
     dtype (see ``synth.make_weights``). The workspace and the folded tables are allocated once
-    here with torch; the library itself never allocates.
+    here with torch; the library itself never allocates. What a call given a ``stream`` allocates
+    itself is that stream's memory (see _results).
     """
 
     def __init__(self, B, L, V, d, K, r, logits_dtype, hidden_dtype, weights, device="cuda"):
@@ -251,54 +252,61 @@ class DecodeTail:
 
     def topk(self, logits_q, stream=None):
         B, L, K = self.B, self.L, self.K
-        ids, lp, lse = self._i32(B, L, K), self._f32(B, L, K), self._f32(B, L)
-        _check(lib().brisk_topk_candidates(ctypes.byref(self.dims), _p(logits_q), _p(ids), _p(lp),
-                                           _p(lse), _p(self.workspace), _stream(stream)), "topk")
-        return {"cand_ids": ids, "cand_logprob": lp, "lse_q": lse}
+        out = _results(stream, lambda: {"cand_ids": self._i32(B, L, K), "cand_logprob": self._f32(B, L, K),
+                                        "lse_q": self._f32(B, L)})
+        _check(lib().brisk_topk_candidates(ctypes.byref(self.dims), _p(logits_q), _p(out["cand_ids"]),
+                                           _p(out["cand_logprob"]), _p(out["lse_q"]), _p(self.workspace),
+                                           _stream(stream)), "topk")
+        return out
 
     def select(self, hidden, h_ctx, x0, logits_q, cand_ids, cand_logprob, select_mode=SELECT_GREEDY,
                u_sel=None, stream=None):
         B, L, K = self.B, self.L, self.K
-        sel, ref = self._i32(B, L), self._f32(B, L, K)
+        out = _results(stream, lambda: {"sel_tokens": self._i32(B, L), "refined": self._f32(B, L, K)})
         _check(lib().brisk_corrector_select(
             ctypes.byref(self.dims), ctypes.byref(self.params), _p(self.tables), _p(hidden), _p(h_ctx),
             _p(x0), _p(logits_q), _p(cand_ids), _p(cand_logprob), int(select_mode), _p(u_sel),
-            _p(sel), _p(ref), _p(self.workspace), _stream(stream)), "select")
-        return {"sel_tokens": sel, "refined": ref}
+            _p(out["sel_tokens"]), _p(out["refined"]), _p(self.workspace), _stream(stream)), "select")
+        return out
 
     def verify(self, logits_p, sel_tokens, cand_ids, refined, select_mode=SELECT_GREEDY,
                verify_mode=VERIFY_GREEDY, u_acc=None, u_res=None, stream=None):
         B, L = self.B, self.L
-        a, out, corr = self._i32(B), self._i32(B, L), self._i32(B)
+        out = _results(stream, lambda: {"accepted_len": self._i32(B), "out_tokens": self._i32(B, L),
+                                        "correction": self._i32(B)})
         _check(lib().brisk_verify_block(
             ctypes.byref(self.dims), _p(logits_p), _p(sel_tokens), _p(cand_ids), _p(refined),
-            int(select_mode), int(verify_mode), _p(u_acc), _p(u_res), _p(a), _p(out), _p(corr),
-            _p(self.workspace), _stream(stream)), "verify")
-        return {"accepted_len": a, "out_tokens": out, "correction": corr}
+            int(select_mode), int(verify_mode), _p(u_acc), _p(u_res), _p(out["accepted_len"]),
+            _p(out["out_tokens"]), _p(out["correction"]), _p(self.workspace), _stream(stream)), "verify")
+        return out
 
     def replay(self, block, select_mode=SELECT_GREEDY, stream=None):
         """Same-state replay diagnostics (App. B, Eq. 6) of one block (see synth.make_block)."""
         B, L, K = self.B, self.L, self.K
-        head, flags, fb, ref = self._i32(B, L), self._i32(B, L), self._i32(B), self._f32(B, L, K)
+        out = _results(stream, lambda: {"head_tokens": self._i32(B, L), "flags": self._i32(B, L),
+                                        "first_breaker": self._i32(B), "refined": self._f32(B, L, K)})
         _check(lib().brisk_replay_diagnostics(
             ctypes.byref(self.dims), ctypes.byref(self.params), _p(self.tables),
             _p(block["hidden"]), _p(block["h_c"]), _p(block["x0"]), _p(block["logits_q"]),
             _p(block["logits_p"]), int(select_mode), _p(block["u_sel"]), _p(block["u_acc"]),
-            _p(head), _p(flags), _p(fb), _p(ref), _p(self.workspace), _stream(stream)),
-            "replay_diagnostics")
-        return {"head_tokens": head, "flags": flags, "first_breaker": fb, "refined": ref}
+            _p(out["head_tokens"]), _p(out["flags"]), _p(out["first_breaker"]), _p(out["refined"]),
+            _p(self.workspace), _stream(stream)), "replay_diagnostics")
+        return out
 
     def distill_loss(self, logits_p, cand_ids, cand_logprob, refined, accepted_len, beta=0.01,
                      with_grad=True, stream=None):
         """Distillation loss of the refinement head (App. C.3, Eq. 10) and its gradient in the
         refined scores."""
-        loss = self._f32(1)
-        grad = self._f32(self.B, self.L, self.K) if with_grad else None
+        def new():
+            loss = {"loss": self._f32(1)}
+            return dict(loss, grad=self._f32(self.B, self.L, self.K)) if with_grad else loss
+        out = _results(stream, new)
         _check(lib().brisk_distill_loss(
             ctypes.byref(self.dims), _p(logits_p), _p(cand_ids), _p(cand_logprob), _p(refined),
-            _p(accepted_len), float(beta), _p(loss), _p(grad), _p(self.workspace),
+            _p(accepted_len), float(beta), _p(out["loss"]), _p(out.get("grad")), _p(self.workspace),
             _stream(stream)), "distill_loss")
-        return {"loss": loss, "grad": grad}
+        out.setdefault("grad", None)
+        return out
 
     def alloc_outputs(self, full=True):
         B, L, K = self.B, self.L, self.K
@@ -322,7 +330,7 @@ class DecodeTail:
              events=None, stream=None):
         """One fused decode-tail call on the tensors of ``block`` (see ``synth.make_block``)."""
         if out is None:
-            out = self.alloc_outputs()
+            out = _results(stream, self.alloc_outputs)
         io = self._io(block, out, x0)
         ev = None
         if events is not None:

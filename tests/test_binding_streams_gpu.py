@@ -3,6 +3,7 @@ neither what the current stream still has to read, nor free before the current s
 import pytest
 import torch
 
+from paper_2609_33390_gb300 import synth
 from test_cache_gpu import BF, make
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +62,26 @@ def check_beside_a_late_stream(call):
 @pytest.mark.parametrize("name", ["attend", "weights", "evict"])
 def test_results_do_not_race_with_a_current_stream_that_is_behind(B, name):
     check_beside_a_late_stream(cache_calls(B)[name])
+
+
+def tail_calls(B):
+    wl = synth.Workload("streams", B=3, L=6, V=2048, d=32, K=8, r=16)
+    tail = B.DecodeTail.for_workload(wl, synth.make_weights(wl, "cuda"))
+    tail.prepare()
+    block = synth.make_block(wl, "cuda")
+    c = tail.topk(block["logits_q"])
+    r = tail.select(block["hidden"], block["h_c"], block["x0"], block["logits_q"], c["cand_ids"], c["cand_logprob"])
+    accepted = torch.full((3,), 2, dtype=torch.int32, device="cuda")
+    return {"topk": lambda s: tail.topk(block["logits_q"], stream=s),
+            "select": lambda s: tail.select(block["hidden"], block["h_c"], block["x0"], block["logits_q"],
+                                            c["cand_ids"], c["cand_logprob"], stream=s),
+            "verify": lambda s: tail.verify(block["logits_p"], r["sel_tokens"], c["cand_ids"], r["refined"], stream=s),
+            "replay": lambda s: tail.replay(block, stream=s),
+            "distill_loss": lambda s: tail.distill_loss(block["logits_p"], c["cand_ids"], c["cand_logprob"],
+                                                        r["refined"], accepted, stream=s),
+            "tail": lambda s: tail.tail(block, stream=s)}
+
+
+@pytest.mark.parametrize("name", ["topk", "select", "verify", "replay", "distill_loss", "tail"])
+def test_results_of_a_tail_do_not_race_with_a_current_stream_that_is_behind(B, name):
+    check_beside_a_late_stream(tail_calls(B)[name])

@@ -78,3 +78,22 @@ def check_results(watch, call):
 @pytest.mark.parametrize("name", ["attend", "weights", "evict"])
 def test_results_are_memory_of_the_stream_that_writes_them(B, watch, name):
     check_results(watch, cache_calls(B)[name])
+
+
+def tail_calls(B):
+    tail = B.DecodeTail.__new__(B.DecodeTail)
+    tail.dims = B.make_dims(2, 3, 512, 16, 4, 16, torch.float32, torch.float32)
+    tail.B, tail.L, tail.K, tail.device = 2, 3, 4, torch.device("cpu")
+    tail.params, tail.tables, tail.workspace = B.Params(), torch.zeros(1), torch.zeros(1)
+    block = {n: None for n in ("logits_q", "logits_p", "hidden", "h_c", "x0", "u_sel", "u_acc")}
+    return {"topk": lambda s: tail.topk(None, stream=s),
+            "select": lambda s: tail.select(*[None] * 6, stream=s),
+            "verify": lambda s: tail.verify(*[None] * 4, stream=s),
+            "replay": lambda s: tail.replay(block, stream=s),
+            "distill_loss": lambda s: tail.distill_loss(*[None] * 5, stream=s),
+            "tail": lambda s: tail.tail(block, stream=s)}
+
+
+@pytest.mark.parametrize("name", ["topk", "select", "verify", "replay", "distill_loss", "tail"])
+def test_results_of_a_tail_are_memory_of_the_stream_that_writes_them(B, watch, name):
+    check_results(watch, tail_calls(B)[name])
