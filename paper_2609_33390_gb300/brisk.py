@@ -183,6 +183,14 @@ def _results(stream, make):
     return new
 
 
+def _lend(stream, *buffers):
+    """An object's own buffers to a call on ``stream``: dropped with the object, they are not free for the current
+    stream before the call has ended."""
+    if stream is not None and stream.cuda_stream != _stream():
+        for t in buffers:
+            t.record_stream(stream)
+
+
 def make_dims(B, L, V, d, K, r, logits_dtype, hidden_dtype) -> Dims:
     return Dims(B, L, V, d, K, r, _dt(logits_dtype), _dt(hidden_dtype))
 
@@ -240,6 +248,7 @@ class DecodeTail:
                    wl.hidden_dtype, weights, device)
 
     def prepare(self, stream=None):
+        _lend(stream, self.tables)
         _check(lib().brisk_corrector_prepare(ctypes.byref(self.dims), ctypes.byref(self.params),
                                              _p(self.tables), _stream(stream)), "prepare")
         self.prepared = True
@@ -254,6 +263,7 @@ class DecodeTail:
         B, L, K = self.B, self.L, self.K
         out = _results(stream, lambda: {"cand_ids": self._i32(B, L, K), "cand_logprob": self._f32(B, L, K),
                                         "lse_q": self._f32(B, L)})
+        _lend(stream, self.workspace, self.tables)
         _check(lib().brisk_topk_candidates(ctypes.byref(self.dims), _p(logits_q), _p(out["cand_ids"]),
                                            _p(out["cand_logprob"]), _p(out["lse_q"]), _p(self.workspace),
                                            _stream(stream)), "topk")
@@ -263,6 +273,7 @@ class DecodeTail:
                u_sel=None, stream=None):
         B, L, K = self.B, self.L, self.K
         out = _results(stream, lambda: {"sel_tokens": self._i32(B, L), "refined": self._f32(B, L, K)})
+        _lend(stream, self.workspace, self.tables)
         _check(lib().brisk_corrector_select(
             ctypes.byref(self.dims), ctypes.byref(self.params), _p(self.tables), _p(hidden), _p(h_ctx),
             _p(x0), _p(logits_q), _p(cand_ids), _p(cand_logprob), int(select_mode), _p(u_sel),
@@ -274,6 +285,7 @@ class DecodeTail:
         B, L = self.B, self.L
         out = _results(stream, lambda: {"accepted_len": self._i32(B), "out_tokens": self._i32(B, L),
                                         "correction": self._i32(B)})
+        _lend(stream, self.workspace, self.tables)
         _check(lib().brisk_verify_block(
             ctypes.byref(self.dims), _p(logits_p), _p(sel_tokens), _p(cand_ids), _p(refined),
             int(select_mode), int(verify_mode), _p(u_acc), _p(u_res), _p(out["accepted_len"]),
@@ -285,6 +297,7 @@ class DecodeTail:
         B, L, K = self.B, self.L, self.K
         out = _results(stream, lambda: {"head_tokens": self._i32(B, L), "flags": self._i32(B, L),
                                         "first_breaker": self._i32(B), "refined": self._f32(B, L, K)})
+        _lend(stream, self.workspace, self.tables)
         _check(lib().brisk_replay_diagnostics(
             ctypes.byref(self.dims), ctypes.byref(self.params), _p(self.tables),
             _p(block["hidden"]), _p(block["h_c"]), _p(block["x0"]), _p(block["logits_q"]),
@@ -301,6 +314,7 @@ class DecodeTail:
             loss = {"loss": self._f32(1)}
             return dict(loss, grad=self._f32(self.B, self.L, self.K)) if with_grad else loss
         out = _results(stream, new)
+        _lend(stream, self.workspace, self.tables)
         _check(lib().brisk_distill_loss(
             ctypes.byref(self.dims), _p(logits_p), _p(cand_ids), _p(cand_logprob), _p(refined),
             _p(accepted_len), float(beta), _p(out["loss"]), _p(out.get("grad")), _p(self.workspace),
@@ -332,6 +346,7 @@ class DecodeTail:
         if out is None:
             out = _results(stream, self.alloc_outputs)
         io = self._io(block, out, x0)
+        _lend(stream, self.workspace, self.tables)
         ev = None
         if events is not None:
             ev = ctypes.byref(Events(*[_vp(e.cuda_event) for e in events]))
@@ -367,6 +382,8 @@ class TailGraph:
             self.anchor = block["x0"]
         self.stream = stream
         self._iob = tail._io(block, self.out, self.anchor)
+        # (replays may be pending when the graph and its buffers are dropped)
+        _lend(stream, tail.workspace, tail.tables, self.anchor, *(t for t in self.out.values() if t is not None))
         saved = self.anchor.clone()
         torch.cuda.synchronize()
         h = _vp()
@@ -528,6 +545,7 @@ class PrefixAttention:
         _PACK5(self._views, 0, *view(q, self._shape_q, "q"), *(view(k_prefix, pre, "k_prefix") or _NONE),
                *(view(v_prefix, pre, "v_prefix") or _NONE), *(view(k_own, own, "k_own") or _NONE),
                *(view(v_own, own, "v_own") or _NONE))
+        _lend(stream, self.workspace)
         s = lib().brisk_prefix_attend(
             self._d, at[0], at[1], at[2], at[3], at[4],
             plain(own_len, self._shape_b, torch.int32, "own_len"),
@@ -549,6 +567,7 @@ class PrefixAttention:
             out = _results(stream, self._weighed)["acc"]
         _PACK2(self._views, 0, *self._view(q, self._shape_q, "q"),
                *(self._view(k_own, self._shape_own, "k_own") or _NONE))
+        _lend(stream, self.workspace)
         s = lib().brisk_cache_weights(
             self._d, at[0], plain(lse, self._shape_lse, f32, "lse"), at[1],
             plain(own_len, self._shape_b, i32, "own_len"),
@@ -586,6 +605,7 @@ class PrefixAttention:
         own, to, kept = self._shape_own, (B, room, Hkv, self.D), (B, Hkv, keep)
         _PACK4(self._views, 0, *(view(k_own, own, "k_own") or _NONE), *(view(v_own, own, "v_own") or _NONE),
                *view(k_to, to, "k"), *view(out["v"], to, "v"))
+        _lend(stream, self.workspace)
         s = lib().brisk_cache_evict(
             self._d, at[0], at[1], plain(acc, self._shape_acc, f32, "acc"),
             plain(own_len, self._shape_b, i32, "own_len"), keep, recent, at[2], at[3],

@@ -85,3 +85,22 @@ def tail_calls(B):
 @pytest.mark.parametrize("name", ["topk", "select", "verify", "replay", "distill_loss", "tail"])
 def test_results_of_a_tail_do_not_race_with_a_current_stream_that_is_behind(B, name):
     check_beside_a_late_stream(tail_calls(B)[name])
+
+
+def test_an_object_may_be_dropped_while_its_call_is_pending(B):
+    x = make(3, 2, 8, 2, 64, 100, 60, BF, [60, 40, 5])
+    new = lambda: B.PrefixAttention(3, 2, 8, 2, 64, 100, 60, BF)
+    run = lambda att, s=None: att.attend(x["q"], x["kp"], x["vp"], x["ko"], x["vo"], x["lens"], stream=s)
+    want = run(new())
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    att = new()
+    n = att.workspace.numel()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(BEHIND)
+    got = run(att, s)
+    del att
+    for _ in range(3):
+        torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])

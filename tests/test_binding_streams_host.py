@@ -97,3 +97,16 @@ def tail_calls(B):
 @pytest.mark.parametrize("name", ["topk", "select", "verify", "replay", "distill_loss", "tail"])
 def test_results_of_a_tail_are_memory_of_the_stream_that_writes_them(B, watch, name):
     check_results(watch, tail_calls(B)[name])
+
+
+@pytest.mark.parametrize("calls", [cache_calls, tail_calls])
+def test_an_objects_buffers_are_kept_for_the_stream_of_a_call(B, watch, monkeypatch, calls):
+    """Dropped with the object, they are not free before the call on the other stream has ended."""
+    lent = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: lent.append((t, s)))
+    other = Stream(2)
+    for call in calls(B).values():
+        for given in (None, Stream(1), other):
+            del lent[:]
+            call(given)
+            assert sum(s is other for _, s in lent) == (0 if given is not other else 1 if calls is cache_calls else 2)
