@@ -191,6 +191,13 @@ def _lend(stream, *buffers):
             t.record_stream(stream)
 
 
+def _settle(device):
+    """Waits for what the current stream does with new buffers (their clearing, and what their memory was used
+    for before): calls may go to any stream. Not under capture, where the calls are the capture's, too."""
+    if device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(device).synchronize()
+
+
 def make_dims(B, L, V, d, K, r, logits_dtype, hidden_dtype) -> Dims:
     return Dims(B, L, V, d, K, r, _dt(logits_dtype), _dt(hidden_dtype))
 
@@ -238,6 +245,7 @@ class DecodeTail:
             raise BriskError(ERR_INVALID_ARG, "dims")
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=self.device)
         self.tables = torch.empty(tb, dtype=torch.uint8, device=self.device)
+        _settle(self.device)
         self.weights = weights
         self.params = make_params(weights)
         self.prepared = False
@@ -487,8 +495,7 @@ class PrefixAttention:
         if ws == 0:
             raise BriskError(ERR_INVALID_ARG, "dims")
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=self.device)
-        if self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
-            torch.cuda.current_stream(self.device).synchronize()   # calls may go to any stream
+        _settle(self.device)
         self.scale = D ** -0.5
         self._d = ctypes.addressof(self.dims)
         self._ws = self.workspace.data_ptr()

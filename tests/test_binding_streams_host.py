@@ -110,3 +110,31 @@ def test_an_objects_buffers_are_kept_for_the_stream_of_a_call(B, watch, monkeypa
             del lent[:]
             call(given)
             assert sum(s is other for _, s in lent) == (0 if given is not other else 1 if calls is cache_calls else 2)
+
+
+@pytest.mark.parametrize("capturing", [False, True])
+@pytest.mark.parametrize("kind", ["cache", "tail"])
+def test_new_buffers_are_settled_before_calls_go_to_any_stream(B, monkeypatch, kind, capturing):
+    """The clearing of a workspace, on the current stream, is not still to come when a call runs on another."""
+    log = []
+
+    class Current:
+        def synchronize(self):
+            log.append("waited")
+
+    def make(real):
+        def new(*a, device=None, **k):
+            log.append("made")
+            return real(*a, **k)
+        return new
+
+    monkeypatch.setattr(torch, "zeros", make(torch.zeros))
+    monkeypatch.setattr(torch, "empty", make(torch.empty))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Current())
+    monkeypatch.setattr(B, "make_params", lambda w: B.Params())
+    if kind == "cache":
+        B.PrefixAttention(2, 3, 4, 2, 64, 10, 20, torch.bfloat16, device="cuda")
+    else:
+        B.DecodeTail(2, 3, 512, 16, 4, 16, torch.float32, torch.float32, {}, device="cuda")
+    assert "made" in log and (log[-1] == "waited") != capturing and log.count("waited") == (not capturing)
