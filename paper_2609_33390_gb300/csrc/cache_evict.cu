@@ -163,7 +163,8 @@ move_kernel(const __grid_constant__ EvictArgs a, Divisor by_vec, Divisor by_head
     at[j] = by_heads.of(row);
     h[j] = row - at[j] * a.Hkv;
     c[j] = (e - row * by_vec.d) * step;
-    src[j] = row < rows ? __ldg(a.kept + ((long long)b * a.Hkv + h[j]) * a.keep + at[j]) : -2;
+    // (select_kernel wrote it while this kernel was set up: no load that takes memory for unchanging)
+    src[j] = row < rows ? a.kept[((long long)b * a.Hkv + h[j]) * a.keep + at[j]] : -2;
   }
   uint4 x[MOVE_EACH], y[MOVE_EACH];
 #pragma unroll
