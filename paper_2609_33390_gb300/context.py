@@ -56,10 +56,15 @@ class ContextDecoder:
     def _write(self, x, where):
         self.k[self.rows, where], self.v[self.rows, where] = self._entries(x)
 
+    def _ids(self, x):
+        """Token ids as indices: a row without a finite logit, or a wait that gave up, may leave any number, which
+        is 0 then (the tail takes such anchors so, and reports them)."""
+        return torch.where((x >= 0) & (x < self.e_in.shape[0]), x, 0).long()
+
     def start(self, x0):
         """The first anchors [B] (int32) become the own caches' first entries."""
         self.own_len.fill_(1)
-        self._write(self.e_in[x0.long()][:, None], self.own_len[:, None].long() - 1)
+        self._write(self.e_in[self._ids(x0)][:, None], self.own_len[:, None].long() - 1)
         self.acc.zero_()
         self.most = 1
         self.x0 = x0
@@ -88,8 +93,8 @@ class ContextDecoder:
                       "hidden": hidden, "h_c": hidden[:, 0].contiguous(), "x0": self.x0})
         att.weights(q, r["lse"], self.k, in_use, acc=self.acc, decay=self.decay, visible=visible, out=self.acc)
         # the committed tokens' entries in place of the block's
-        self._write(self.e_in[out["out_tokens"].clamp(min=0).long()], where)
-        self.own_len += (out["accepted_len"] + 1).clamp(max=t.L)
+        self._write(self.e_in[self._ids(out["out_tokens"])], where)
+        self.own_len += (out["accepted_len"] + 1).clamp(1, t.L)
         self.acc.masked_fill_(self.places >= self.own_len[:, None, None], 0)
         self.most += t.L
         self.x0 = out["next_anchor"]
