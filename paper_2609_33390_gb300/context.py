@@ -42,6 +42,9 @@ class ContextDecoder:
         self.acc = torch.zeros(B, Hkv, S, device=dev)
         self.spare = self.attention.alloc_evicted(keep, room=S)
         self.own_len = torch.zeros(B, dtype=torch.int32, device=dev)
+        # a workspace's first word is its last call's status, which the next call of the step overwrites
+        self.words = [x.workspace[:4].view(torch.int32) for x in (self.attention, tail)]
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.most = 0                                  # no sequence has more entries
         self.at = torch.arange(L, device=dev, dtype=torch.int32)
         self.places = torch.arange(S, device=dev, dtype=torch.int32)
@@ -69,8 +72,13 @@ class ContextDecoder:
         self.most = 1
         self.x0 = x0
 
+    def _note(self, *words):
+        for word in words:
+            torch.maximum(self.status, word, out=self.status)
+
     def _cut(self):
         self.attention.evict(self.k, self.v, self.acc, self.own_len, self.keep, self.recent, out=self.spare)
+        self._note(self.words[0])
         self.k, self.v, self.spare["k"], self.spare["v"] = self.spare["k"], self.spare["v"], self.k, self.v
         self.own_len.copy_(self.spare["own_len"])
         self.acc[:, :, :self.keep] = self.spare["acc"]
@@ -88,10 +96,12 @@ class ContextDecoder:
         in_use = self.own_len + t.L
         q = (self.block @ self.w["q"]).view(t.B, t.L, self.Hq, self.D)
         r = att.attend(q, self.k_prefix, self.v_prefix, self.k, self.v, in_use, visible=visible)
+        self._note(self.words[0])
         hidden = self.block + r["out"].view(t.B, t.L, -1) @ self.w["o"]
         out = t.tail({"logits_q": hidden @ self.e_out.T, "logits_p": hidden @ self.w["p"] @ self.e_out.T,
                       "hidden": hidden, "h_c": hidden[:, 0].contiguous(), "x0": self.x0})
         att.weights(q, r["lse"], self.k, in_use, acc=self.acc, decay=self.decay, visible=visible, out=self.acc)
+        self._note(*self.words)
         # the committed tokens' entries in place of the block's
         self._write(self.e_in[self._ids(out["out_tokens"])], where)
         self.own_len += (out["accepted_len"] + 1).clamp(1, t.L)
@@ -101,5 +111,8 @@ class ContextDecoder:
         return out
 
     def device_status(self) -> int:
-        """The worst of the tail's and the attention's status words (see brisk_last_device_status)."""
-        return max(self.tail.device_status(), self.attention.device_status())
+        """The worst (largest) status that a call of the steps since the last query left, the tail's and each of the
+        attention's (see brisk_last_device_status). Waits for the steps, and begins anew."""
+        worst = int(self.status)
+        self.status.zero_()
+        return worst
