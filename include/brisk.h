@@ -390,9 +390,10 @@ size_t brisk_cache_workspace_bytes(const brisk_cache_dims *dims);
  * hold (infinities and NaN too).
  * q [B, L, Hq]; k_prefix, v_prefix [P, Hkv] (NULL if P == 0); k_own, v_own [B, S, Hkv] (NULL if
  * S == 0); own_len [B], visible [B, L] int32; out [B, L, Hq, D] dense, 16-byte aligned; lse
- * [B, L, Hq] f32 or NULL. 0 <= scale < inf. With bf16 the probabilities enter the sum of values rounded to
- * bf16; scores, maxima and sums are fp32. A length outside 0..S is clamped and reported as
- * BRISK_ERR_INVALID_ARG in the device status. Two kernels, or three (bf16, long prefix, many rows). */
+ * [B, L, Hq] f32 or NULL. 0 <= scale <= 2.35e38 (scale log2(e) is finite in fp32). With bf16 the
+ * probabilities enter the sum of values rounded to bf16; scores, maxima and sums are fp32. A length
+ * outside 0..S is clamped and reported as BRISK_ERR_INVALID_ARG in the device status. Two kernels,
+ * or three (bf16, long prefix, many rows). */
 brisk_status brisk_prefix_attend(const brisk_cache_dims *dims, const brisk_view *q,
                                  const brisk_view *k_prefix, const brisk_view *v_prefix,
                                  const brisk_view *k_own, const brisk_view *v_own,

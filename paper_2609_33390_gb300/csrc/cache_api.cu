@@ -92,7 +92,8 @@ bool units_ok(const brisk_cache_dims* d) {
 template <typename T>
 inline T* at(void* base, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(base) + off); }
 
-bool scale_ok(float s) { return s >= 0.f && s <= 3.0e38f; }
+// (kernels have scores in log2 units, in which the scale must be finite too: up to 2.35e38)
+bool scale_ok(float s) { return s >= 0.f && isfinite(s * LOG2E); }
 
 }  // namespace
 
