@@ -89,6 +89,10 @@ bool units_ok(const brisk_cache_dims* d) {
   return pre + own < 2.0e9;
 }
 
+// In the place of a scale of 0, which would make NaN of the masked scores' -inf: the smallest number above it (2^-149),
+// with which every finite score is below 2^-21.
+constexpr float SMALLEST = 1.40129846e-45f;
+
 template <typename T>
 inline T* at(void* base, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(base) + off); }
 
@@ -130,8 +134,7 @@ brisk_status brisk_prefix_attend(const brisk_cache_dims* d, const brisk_view* q,
   a.status = at<int32_t>(ws, w.status);
   a.wait_limit = wait_limit_cycles();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // a scale of 0 would make NaN of the masked scores' -inf; this one leaves every finite score at 0
-  if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
+  if (a.sl2 == 0.f) a.sl2 = SMALLEST;
   if ((d->dtype == BRISK_DT_BF16 ? launch_attend_tc(a, st) : launch_attend_f32(a, st)) != cudaSuccess)
     return BRISK_ERR_CUDA;
   if (launch_merge(a, st) != cudaSuccess) return BRISK_ERR_CUDA;
@@ -165,7 +168,7 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   if (d->S == 0 || d->dtype == BRISK_DT_BF16)   // (the fp32 kernel writes the word itself)
     if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
   if (d->S == 0) return BRISK_OK;
-  if (a.sl2 < 1.2e-38f) a.sl2 = 1.2e-38f;
+  if (a.sl2 == 0.f) a.sl2 = SMALLEST;
   divide(&a);
   return (d->dtype == BRISK_DT_BF16 ? launch_weights_tc(a, st) : launch_weights_f32(a, st)) == cudaSuccess
              ? BRISK_OK : BRISK_ERR_CUDA;
