@@ -467,7 +467,7 @@ struct WeightArgs {
   Divisor by_G;
   const int32_t *own_len, *visible;
   const float* lse;        // [B, L, Hkv * G]
-  float sl2, decay;
+  float scale, sl2, decay;           // sl2: scale * log2(e)
   const float* acc_in;     // [B, Hkv, S] or nullptr (zeros)
   float* acc_out;          // [B, Hkv, S]
   int32_t* status;

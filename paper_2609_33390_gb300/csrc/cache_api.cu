@@ -158,6 +158,7 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   a.own_len = own_len;
   a.visible = visible;
   a.lse = lse;
+  a.scale = scale;
   a.sl2 = scale * LOG2E;
   a.decay = decay;
   a.acc_in = acc_in;
@@ -168,7 +169,6 @@ brisk_status brisk_cache_weights(const brisk_cache_dims* d, const brisk_view* q,
   if (d->S == 0 || d->dtype == BRISK_DT_BF16)   // (the fp32 kernel writes the word itself)
     if (cudaMemsetAsync(a.status, 0, sizeof(int32_t), st) != cudaSuccess) return BRISK_ERR_CUDA;
   if (d->S == 0) return BRISK_OK;
-  if (a.sl2 == 0.f) a.sl2 = SMALLEST;
   divide(&a);
   return (d->dtype == BRISK_DT_BF16 ? launch_weights_tc(a, st) : launch_weights_f32(a, st)) == cudaSuccess
              ? BRISK_OK : BRISK_ERR_CUDA;

@@ -4,6 +4,10 @@
 //
 // with the rows' log-sums lse that attention left. The keys are the tile's rows here: a key's sum
 // over the query rows stays with its threads, so there are no atomics and the sums' order is fixed.
+// fp32 subtracts the log-sums as attention left them, in one fma with the scaled score, and takes the small difference
+// to log2 units: with either of them in log2 units first, its rounding would be that of numbers the size of the
+// scores, 4e-5 of a weight at scores of 500 (12 rows a head, 80 columns, scores of a few: error against 64 bits 1.0e-7,
+// that way 3.3e-7).
 #include <type_traits>
 
 #include "cache.cuh"
@@ -11,6 +15,10 @@
 
 namespace brisk {
 namespace {
+
+__device__ __forceinline__ float weight_of(float score, float scale, float lse) {
+  return ex2(fmaf(score, scale, -lse) * LOG2E);
+}
 
 // fp32, more than FEW_W rows a head (see weights_few_kernel): tiles of 64 keys and 64 rows, 4 rows and 4 keys a thread. Bound by FMA issue and
 // shared-memory reads (128 rows, 32 heads on 8, D = 128, 16 sequences of 1000 to 4000 entries: 326 us, 33 TFLOP/s).
@@ -23,7 +31,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
   extern __shared__ __align__(16) float smem[];
   float* sK = smem;                        // [W_KEYS][WS]
   float* sQ = sK + W_KEYS * WS;            // [W_ROWS][CACHE_MAX_D]
-  float* sL = sQ + W_ROWS * CACHE_MAX_D;   // [W_ROWS] log-sums in log2 units
+  float* sL = sQ + W_ROWS * CACHE_MAX_D;   // [W_ROWS] log-sums
   int* sLim = reinterpret_cast<int*>(sL + W_ROWS);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int tiles = (a.S + W_KEYS - 1) / W_KEYS, D = a.D, nv = D / 4;
@@ -54,7 +62,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
           const int i = a.by_G.of(r0 + tid), g = r0 + tid - i * a.G;
           const long long token = (long long)b * a.L + i;
           lim = a.visible ? min(len, a.visible[token]) : len;
-          ls = a.lse[token * (a.Hkv * a.G) + h * a.G + g] * LOG2E;
+          ls = a.lse[token * (a.Hkv * a.G) + h * a.G + g];
           if (ls == -INFINITY) lim = 0;    // a row that saw nothing
         }
         sLim[tid] = lim;
@@ -90,7 +98,7 @@ weights_simt_kernel(const __grid_constant__ WeightArgs a) {
           for (int j = 0; j < 4; ++j) {
             float x, y;
             unpack2(s2[i][j], x, y);
-            if (t0 + tx + 16 * j < lim) sum[j] += ex2((x + y) * a.sl2 - ls);
+            if (t0 + tx + 16 * j < lim) sum[j] += weight_of(x + y, a.scale, ls);
           }
         }
       };
@@ -127,7 +135,7 @@ __global__ void __launch_bounds__(W_THREADS, 2)
 weights_few_kernel(const __grid_constant__ WeightArgs a) {
   constexpr int CH = CACHE_MAX_D / 16;
   __shared__ __align__(16) float sQ[FEW_W][CACHE_MAX_D];
-  __shared__ float sL[FEW_W];              // log-sums in log2 units
+  __shared__ float sL[FEW_W];              // log-sums
   __shared__ int sLim[FEW_W];
   const int tid = threadIdx.x, lane = tid & 31, D = a.D, rows = a.L * a.G;
   const int tiles = (a.S + WF_KEYS - 1) / WF_KEYS, item = blockIdx.x / tiles;
@@ -165,7 +173,7 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
       if (tid < rows) {
         const int i = a.by_G.of(tid);
         const long long token = (long long)b * a.L + i;
-        ls = a.lse[token * (a.Hkv * a.G) + h * a.G + (tid - i * a.G)] * LOG2E;
+        ls = a.lse[token * (a.Hkv * a.G) + h * a.G + (tid - i * a.G)];
         // (a row that saw nothing gives nothing)
         lim = ls == -INFINITY ? 0 : (a.visible ? min(len, a.visible[token]) : len);
       }
@@ -201,7 +209,7 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
       const float z1 = (up ? y[1][1] : y[0][1]) + __shfl_xor_sync(FULL_MASK, up ? y[0][1] : y[1][1], 2);
       const float z = (odd ? z1 : z0) + __shfl_xor_sync(FULL_MASK, odd ? z0 : z1, 1);
       const int row = r + (lane >> 1 & 1);
-      if (mine < sLim[row]) sum += ex2(z * a.sl2 - sL[row]);
+      if (mine < sLim[row]) sum += weight_of(z, a.scale, sL[row]);
     }
   }
   sum += __shfl_xor_sync(FULL_MASK, sum, 2);
