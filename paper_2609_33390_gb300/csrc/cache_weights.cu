@@ -230,6 +230,15 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
 // to the sums that the first one wrote. Bound by the keys' bytes up to 128 rows a head, by the exponentials beyond:
 // 64 sequences of 4096 entries, 8 key heads of 128, 32, 128, 256, 384 and 512 rows a head 95 us (5.9 TB/s), 100, 170,
 // 238 and 324 us (862 TFLOP/s; runs of 8 and 16 tiles: 382 and 345, all blocks for every tile 964).
+//
+// The tensor cores cut a partial sum towards zero at every step of 16 columns: 2.6e-5 of a weight where a score is 128
+// positive products of 1, 9e-7 at scores of a few. So with more than 64 columns one step more, after the fourth, adds
+// -lse / scale rounded to bf16 (an extra column of the queries, where the keys have 1), and the remainder of the
+// log-sum is subtracted afterwards. Partial sums of the scores whose weights count are then above zero first
+// and below it later, what is cut off cancels, and what is rounded afterwards is small. 128 rows a head of 72, 80, 96, 112,
+// 120 and 128 columns, error against 64 bits in 1e-7: 3.3, 3.8, 1.1, 2.7, 2.3, 2.6; without 7.9, 7.6, 3.0, 13.5, 14.7, 9.0; with
+// 64 columns, 3.2 without. It costs 2 to 3 % of the time (128 rows 110 -> 113 us, 512 rows 318 -> 326; after
+// half of the steps in use, whatever their number, 331).
 constexpr int KT = 128, QB = 128, Q_STAGES = 3, CHUNK = 32;
 constexpr int WT_THREADS = 384;
 constexpr int PANEL = TILE_PANEL;
@@ -238,7 +247,8 @@ template <int DP>
 struct WShape {
   static constexpr int TILE = KT * DP * 2;
   static constexpr int STAGES = DP == 128 ? 3 : 6;
-  static constexpr int SMEM = 1024 + (Q_STAGES + STAGES) * TILE;
+  static constexpr bool HALF_WAY = DP == 128;      // log-sums come off half-way
+  static constexpr int SMEM = 1024 + (Q_STAGES + STAGES) * TILE + (HALF_WAY ? TILE_PANEL : 0);
 };
 
 // A pass: nq blocks of queries from q0 on over key tiles [k0, k0 + n); n = 0 after the last.
@@ -283,7 +293,8 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = base;
   uint8_t* ring = base + Q_STAGES * TILE;
-  __shared__ __align__(16) float neg_lse[Q_STAGES][QB];    // -lse, log2 units
+  uint8_t* extra = ring + STAGES * TILE;           // a panel: 16 more columns of each place of queries, and of any keys
+  __shared__ __align__(16) float neg_lse[Q_STAGES][QB];    // -lse but for what the products add, log2 units
   __shared__ __align__(16) int row_lim[Q_STAGES][QB];
   __shared__ uint64_t k_full[STAGES], k_empty[STAGES], q_full[Q_STAGES], q_empty[Q_STAGES];
   __shared__ uint64_t s_full[4], s_empty[4], f_full[2], f_empty[2], done;
@@ -318,6 +329,13 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     fence_async_smem();
   }
   if (warp == 0) tmem_alloc(&tmem_slot, 512);
+  if constexpr (Sh::HALF_WAY) {
+    for (int e = tid; e < TILE_PANEL / 16; e += WT_THREADS) {
+      const int r = e >> 3, c = (e ^ r) & 7;       // (a row's 16-byte pieces are swizzled; two a place)
+      *reinterpret_cast<uint4*>(extra + e * 16) = make_uint4(c == 2 * Q_STAGES ? 0x3f80u : 0u, 0u, 0u, 0u);
+    }
+    fence_async_smem();
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -355,7 +373,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     for (unsigned p = unit > STAGES ? unit - STAGES : 0; p < unit; ++p) mbar_drain(&k_full[p % STAGES], (p / STAGES) & 1);
   } else if (warp == 9) {
     const int nd = (a.D + 15) / 16;
-    const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring));
+    const uint32_t q_lo = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), x_lo = sw128_lo(su32(extra));
     unsigned ns[2] = {0, 0};                       // score buffers a group was given
     auto commit = [&](uint64_t* bar) {
       if (elect_one()) umma_commit(bar);
@@ -387,6 +405,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             for (int kk = 0; kk < DP / 16; ++kk) {
               const uint32_t o = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
               if (kk < nd) umma(tmem + buf * 128, sw128(k + o), sw128(q + o), id, kk > 0);
+              if (Sh::HALF_WAY && kk == 3) umma(tmem + buf * 128, sw128(x_lo + 2 * Q_STAGES), sw128(x_lo + 2 * qs), id, 1);
             }
             umma_commit(&s_full[buf]);
           }
@@ -435,12 +454,17 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             const int i = a.by_G.of(first + r), head = f.h * a.G + (first + r - i * a.G);
             const long long token = (long long)f.b * a.L + i;
             src = static_cast<const __nv_bfloat16*>(a.q.p) + f.b * a.q.seq + i * a.q.tok + head * a.q.head;
-            ls = a.lse[token * (a.Hkv * a.G) + head] * LOG2E;
+            ls = a.lse[token * (a.Hkv * a.G) + head];
             lim = a.visible ? min(len, a.visible[token]) : len;
           }
           fetch_queries<DP>(src, a.D, sQ + qs * TILE, r0);
           if (ls == -INFINITY) ls = 0.f, lim = 0;  // a row that saw nothing
-          neg_lse[qs][r] = -ls;
+          if constexpr (Sh::HALF_WAY) {            // (not where the quotient would be out of bounds, or NaN)
+            const float x = -ls / a.scale, added = fabsf(x) < 1e30f ? __bfloat162float(__float2bfloat16_rn(x)) : 0.f;
+            *reinterpret_cast<uint32_t*>(extra + r * 128 + ((2 * qs ^ r) & 7) * 16) = __float_as_uint(added) >> 16;
+            ls = fmaf(added, a.scale, ls);
+          }
+          neg_lse[qs][r] = -ls * LOG2E;
           row_lim[qs][r] = lim;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");

@@ -46,3 +46,30 @@ def test_fp32_weights_of_large_scores_keep_their_bits(B, L, G):
     want, _ = C.weights(n64(q), n64(lse), n64(k), n64(lens), None, scale, None, 1.0)
     rel = 3 * U * d + 2.0 ** -21 + (L * G + 4) * U
     assert (np.abs(got - want) <= rel * want).all(), np.max(np.abs(got - want) / np.maximum(want, 1e-30)) / rel
+
+
+def test_bf16_weights_do_not_lean_to_one_side(B):
+    """Scores of 128 positive products, of which every other is small, so that sums have more bits than fp32
+    holds: eight partial sums of about 16, 32, .. 130, each cut off towards zero by half a unit in the last place on
+    average, which is 2.8e-5 in all (2^-20 + 2 x 2^-19 + 4 x 2^-18 + 2^-17, the unit of 64 to 128 being 2^-17) and as much of
+    a weight. With the log-sum taken off half-way, four sums above zero lose 2^-20 + 2 x 2^-19 + 2^-18 = 8.6e-6 of
+    one sign and the others about as much of the other; that half of it is left over (scores are 130 +- 7, log-sums 5 to
+    20 above) is 4.3e-6. To this come sums of `rows` terms and the exponential."""
+    Bn, L, G, Hkv, D, S = 2, 8, 4, 2, 128, 1000
+    g = torch.Generator().manual_seed(0)
+    q, k = torch.rand(Bn, L, Hkv * G, D, generator=g) + 0.5, torch.rand(Bn, S, Hkv, D, generator=g) + 0.5
+    for t in (q, k):
+        t[..., 1::2] /= 4
+    q[..., ::2] *= 2
+    q, k = q.bfloat16(), k.bfloat16()
+    s = torch.einsum("blhgd,bshd->blhgs", q.view(Bn, L, Hkv, G, D).double(), k.double())
+    lse = torch.logsumexp(s, 4).view(Bn, L, Hkv * G).float().cuda()
+    lens = torch.tensor([S, S - 1], dtype=torch.int32).cuda()
+    q, k = q.cuda(), k.cuda()
+    att = B.PrefixAttention(Bn, L, Hkv * G, Hkv, D, 0, S, torch.bfloat16)
+    got = n64(att.weights(q, lse, k, lens, scale=1.0))
+    assert att.device_status() == B.OK
+    want, _ = C.weights(n64(q), n64(lse), n64(k), n64(lens), None, 1.0, None, 1.0)
+    tol = 4.3e-6 + (L * G + 4) * U + 2.0 ** -21
+    assert abs(got.sum() / want.sum() - 1) <= tol
+    assert np.linalg.norm(got - want) <= tol * np.linalg.norm(want)
