@@ -361,14 +361,28 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
 }
 
 // Keys of a tile, rows of it, and CTAs: bf16 on the tensor cores, fp32 on the FMA units. With bf16 and more
-// than SLOT_ROWS query rows a key head, the prefix has a kernel of its own from APART_UNITS of its units on.
-// That kernel reads a key tile for twice the rows, but is one more launch and divides the prefix by itself: 32 query
-// heads on 8, own caches of up to 300, R rows a key head: U units of it take, with and without it,
-//   U 64 (R 512): 25.8 and 18.0 us; 256 (512): 32.2 and 29.2; 384 (640): 35.5 and 32.3; 432 (512): 34.2 and 35.4;
-//   480 (640): 33.0 and 32.5; 512 (1024): 34.0 and 39.5; 1024 (2048): 48.0 and 59.7; 4096 (4096): 95 and 155.
+// than SLOT_ROWS query rows a key head, the prefix has a kernel of its own from apart_units() of its units on.
+// That kernel reads a key tile for twice the rows, but is one more launch, divides the prefix by itself, in whole
+// rounds of CTAs, and leaves rows with more than JOIN_PARTS own parts to the join. 32 query heads on 8, own caches with
+// room S, half of it to all in use, R rows a key head; U units of it take, with and without it, us:
+//   S 60 (0 to 60; 32 rows a sequence): R 512, U 512: 29.6 and 29.8; 768: 32.1, 38.8; 1024: 38.6, 47.6; 2048: 49.8, 76.5;
+//     R 2048: 512: 35.3, 38.2; 1024: 44.2, 55.7; 2048: 53.8, 84.6
+//   S 500, R 1024, 32 rows: U 512: 36.4, 32.7; 1024: 47.0, 42.0; 2048: 58.4, 64.2; 4096: 78.5, 97.7;
+//     R 4096, 128 rows: 512: 44.9, 47.1; 2048: 70.6, 82.7
+//   S 640, R 1024, 32 rows: U 1024: 49.4, 44.5; 2048: 59.1, 60.4; 4 rows: 1024: 125.6, 117.0; 2048: 134.9, 130.6
+//   S 800, R 1024, 32 rows: U 1024: 53.4, 44.2; 2048: 62.6, 58.1; 4096: 83.3, 88.2
+//   S 2048, R 1024, 32 rows: U 512: 62.9, 50.7; 1024: 72.7, 57.0; 2048: 81.8, 70.7; 4096: 101, 102; 8192: 150, 154;
+//     128 rows: 1024: 49.6, 37.1; 4096: 79.9, 82.4; 4 rows: 512: 277, 278; 4096: 314, 340.
+// Between the borders either side may be ahead by a tenth, as the rounds come out.
 constexpr int TC_KT = 128, SLOT_ROWS = 128, PAIR_ROWS = 256, SIMT_KT = 64, SIMT_ROWS = 64;
 constexpr int SLOT_CTAS = 2 * CACHE_SMS;             // (the fp32 kernel's, too)
-constexpr int APART_UNITS = 3 * CACHE_SMS;
+constexpr int APART_UNITS = 3 * CACHE_SMS;           // own caches whose parts it joins whatever their division
+constexpr int APART_UNITS_SOME = 8 * CACHE_SMS;      // up to SOME_TILES of own keys
+constexpr int APART_UNITS_LONG = 24 * CACHE_SMS;
+constexpr int SOME_TILES = 5;
+inline int apart_units(int S) {
+  return S <= JOIN_PARTS * TC_KT ? APART_UNITS : (S <= SOME_TILES * TC_KT ? APART_UNITS_SOME : APART_UNITS_LONG);
+}
 // fp32: up to FEW_ROWS rows of a sequence have a form of their own (64 single tokens, 32 heads on 8, D = 128, over
 // 1000 to 2000 own and 2000 shared entries: 216 us, with the form for more rows 685 us). One of its units takes about
 // a sixth (up to 4 rows) or a fourth of the time of a prefix's unit of a full tile, where own caches are long: counting
@@ -378,7 +392,7 @@ inline void divide(AttendArgs* a) {
   const bool tc = a->dt == BRISK_DT_BF16;
   const long long R = (long long)a->B * a->L * a->G;
   const long long units = a->Hkv * ((R + PAIR_ROWS - 1) / PAIR_ROWS) * (((long long)a->P + TC_KT - 1) / TC_KT);
-  const bool apart = tc && R > SLOT_ROWS && units >= APART_UNITS;
+  const bool apart = tc && R > SLOT_ROWS && units >= apart_units(a->S);
   const int rows = a->L * a->G;
   a->sh.kt = tc ? TC_KT : SIMT_KT;
   a->sh.rt_o = tc ? SLOT_ROWS : SIMT_ROWS;

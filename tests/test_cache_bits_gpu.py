@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from test_cache_gpu import BF, F32
+from test_cache_forms_gpu import apart
 from test_cache_work_gpu import inputs, lens_of
 
 pytestmark = pytest.mark.gpu
@@ -17,17 +18,23 @@ def B():
     return B
 
 
+def test_some_sizes_have_the_prefixs_own_kernel():
+    assert apart((256, 1, 32, 8, 128, 2048, 250)) and apart((35, 4, 28, 4, 64, 6000, 250))
+    assert apart((33, 4, 32, 4, 128, 3000, 250))
+
+
 def attend(att, x):
     return att.attend(x["q"], x["kp"], x["vp"], x["ko"], x["vo"], x["lens"], visible=x["vis"])
 
 
 @pytest.mark.parametrize("size", [
     # B, L, Hq, Hkv, D, P, S: tiles of 128 or 256 rows that are not full
-    (256, 1, 32, 8, 128, 2048, 1500),     # 4 rows of a sequence; full tiles over the prefix, by the kernel of its own
+    (256, 1, 32, 8, 128, 2048, 1500),     # 4 rows of a sequence, full tiles over the prefix
+    (256, 1, 32, 8, 128, 2048, 250),      # the latter by the prefix's own kernel
     (205, 4, 1, 1, 128, 11000, 400),      # 52 rows in the prefix's last tile
     (3, 10, 32, 4, 128, 12800, 18),       # 112
     (5, 18, 16, 8, 128, 800, 4600),       # 36 rows of a sequence
-    (35, 4, 28, 4, 64, 6000, 300),        # 212 of 256 rows in the last tile of the prefix's own kernel
+    (35, 4, 28, 4, 64, 6000, 250),        # 212 of 256 rows in the last tile of the prefix's own kernel
 ])
 def test_rows_repeat_their_bits_between_other_calls(B, size):
     Bn, L, Hq, Hkv, D, P, S = size
@@ -49,7 +56,7 @@ def test_rows_repeat_their_bits_between_other_calls(B, size):
 @pytest.mark.parametrize("size", [
     (3, 8, 8, 2, 64, 900, 700),           # 32 rows of a sequence, beside the prefix
     (3, 8, 8, 2, 128, 0, 700),
-    (33, 4, 32, 4, 128, 3000, 300),       # the prefix's own kernel (576 of its units)
+    (33, 4, 32, 4, 128, 3000, 250),       # the prefix's own kernel
 ])
 def test_rows_do_not_depend_on_other_rows(B, size, dt):
     """The last position's queries, and an entry that it alone sees, change; the other rows do not."""

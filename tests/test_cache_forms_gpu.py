@@ -34,7 +34,9 @@ def apart(size):
     Bn, L, Hq, Hkv, D, P, S = size
     R = Bn * L * Hq // Hkv
     units = Hkv * -(-R // constant("PAIR_ROWS")) * -(-P // constant("TC_KT"))
-    return R > constant("SLOT_ROWS") and units >= constant("APART_UNITS")
+    tiles = -(-S // constant("TC_KT"))
+    border = "" if tiles <= constant("JOIN_PARTS") else "_SOME" if tiles <= constant("SOME_TILES") else "_LONG"
+    return R > constant("SLOT_ROWS") and units >= constant("APART_UNITS" + border)
 
 
 def attend(att, x, **how):
@@ -42,9 +44,9 @@ def attend(att, x, **how):
 
 
 # 594 rows a head: the third tile's second slot has none
-ORDERS = (6, 33, 24, 8, 128, 2500, 260)
+ORDERS = (6, 33, 24, 8, 128, 6500, 260)
 # own entries of a row: none, one part, two, or more
-LONG = (40, 16, 64, 32, 72, 384, 3000)
+LONG = (40, 16, 64, 32, 72, 2940, 3000)
 
 
 def long_inputs(mask, seed=0):
@@ -113,7 +115,7 @@ def test_bad_entries_of_the_prefix_reach_all_rows_but_padding(B):
     assert torch.equal(got["out"][~hit], ref["out"][~hit]) and torch.equal(got["lse"], ref["lse"])
     assert torch.isnan(got["out"][hit]).all()
     x["vp"][200, 5, 7] = value
-    x["kp"][383] = float("nan")
+    x["kp"][2939] = float("nan")
     got = attend(att, x)
     gone = pad.expand_as(got["lse"])
     assert torch.isnan(got["lse"][~gone]).all() and torch.isnan(got["out"][~gone]).all()
@@ -121,7 +123,7 @@ def test_bad_entries_of_the_prefix_reach_all_rows_but_padding(B):
 
 
 def test_two_prefix_kernels_on_two_streams(B):
-    sizes = [(20, 16, 32, 8, 128, 2600, 300), (70, 1, 32, 8, 128, 3800, 800)]
+    sizes = [(20, 16, 32, 8, 128, 4000, 300), (70, 1, 32, 8, 128, 29200, 800)]
     assert all(apart(s) for s in sizes)
     xs = [inputs(*s, lens_of(s[0], s[6]), True, BF, seed=i) for i, s in enumerate(sizes)]
     atts = [B.PrefixAttention(*s, BF) for s in sizes]
@@ -156,6 +158,37 @@ def test_a_captured_call_of_all_three_kernels_replays_on_new_inputs(B):
         torch.cuda.synchronize()
         assert all(torch.equal(out[k], want[k]) for k in want)
     assert att.device_status() == B.OK
+
+
+@pytest.mark.parametrize("size", [(16, 32, 32, 8, 128, 3000, 250), (80, 8, 16, 4, 64, 6000, 200)])
+def test_expired_waits_of_the_prefixs_own_kernel(B, size):
+    assert apart(size)
+    x = inputs(*size, lens_of(size[0], size[6]), True, BF)
+    att = B.PrefixAttention(*size, BF)
+    ref = {k: v.clone() for k, v in attend(att, x).items()}
+    assert att.device_status() == B.OK
+    before = B.set_wait_limit(1)
+    try:
+        attend(att, x)
+        assert att.device_status() == B.ERR_TIMEOUT
+    finally:
+        B.set_wait_limit(before)
+    got = attend(att, x)
+    assert att.device_status() == B.OK and all(torch.equal(got[k], ref[k]) for k in ref)
+
+
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("size", [
+    (5, 32, 32, 8, 128, 9000, 600),       # several row tiles a head, the last one half full
+    (40, 8, 16, 4, 64, 4000, 250),        # narrow heads, 5 row tiles
+    (40, 8, 12, 4, 40, 5000, 90),
+    (40, 16, 64, 32, 72, 384, 0),         # no own entries
+    (300, 1, 32, 8, 128, 4096, 150),      # single tokens
+    (1025, 1, 16, 8, 64, 1300, 20),
+])
+def test_the_prefixs_own_kernel_of_many_sizes(B, size, mask):
+    assert apart(size)
+    check(B, inputs(*size, lens_of(size[0], size[6]), mask, BF), size[6])
 
 
 # ---------------------------------------------------------------- fp32, up to 8 rows of a sequence
