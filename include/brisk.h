@@ -361,6 +361,7 @@ double brisk_tpf_isd(int32_t N, double r);
  * positions of every sequence's block (L = 1: single tokens), Hq query heads over Hkv key heads
  * (head hq reads key head hq / (Hq / Hkv)) of width D. The paper takes the backbone as given;
  * these calls have no counterpart in it.
+ * A cache is one strided tensor: there is no page table.
  * Limits: 1 <= B <= 4096; L >= 1; Hq a multiple of Hkv; B * L * Hq <= 2^30; 8 <= D <= 128 and
  * D % 8 == 0; 0 <= P, S <= 2^30. dtype: q, keys, values and out (fp32 or bf16). */
 typedef struct brisk_cache_dims {

@@ -13,7 +13,8 @@
 // attend_slot_kernel, over the own caches (and over the prefix where it has few units, see divide): two
 // CTAs an SM, each working through fragments of its own. Bound by the entries' bytes where the caches are
 // long (256 single tokens over 512 to 2048 entries each, 222 us, 6 TB/s), by what a fragment costs around its
-// tiles where they are short (a block of 32 positions over 4096 and 1100 entries: 14 us for two tiles a CTA).
+// tiles where they are short (a block of 32 positions over 4096 and 1100 entries: 14 us for two tiles a CTA; 128 blocks
+// over 256 to 1024 own entries each: 97 us, where their bytes and the parts' take 62).
 // The CTAs share the units of work evenly (see Plan). Where both kernels run, the own caches' is first; the
 // prefix's takes over SM by SM and joins the own entries' parts at the end of its fragments, which are long.
 //

@@ -227,9 +227,10 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
 // two put blocks of 128 queries with their log-sums into a ring, and two groups of four warps take
 // the key tiles in turn. A pass is up to two blocks of queries, which stay, over a run of key tiles: all of a
 // fragment where there are no more blocks; else the blocks take turns on runs of CHUNK tiles, and later passes add
-// to the sums that the first one wrote. Bound by the keys' bytes up to 128 rows a head, by the exponentials beyond:
-// 64 sequences of 4096 entries, 8 key heads of 128, 32, 128, 256, 384 and 512 rows a head 95 us (5.9 TB/s), 100, 170,
-// 238 and 324 us (862 TFLOP/s; runs of 8 and 16 tiles: 382 and 345, all blocks for every tile 964).
+// to the sums that the first one wrote. Bound by the keys' bytes up to 128 rows a head; beyond, by the summing warps'
+// waits for columns of TMEM (512 rows: tensor cores 36 % active, exponentials 32 %, DRAM 32 %): 64 sequences of 4096
+// entries, 8 key heads of 128, 32, 128, 256, 384 and 512 rows a head 93 us (5.8 TB/s), 99, 168, 243 and 324 us (848
+// TFLOP/s; when it took 324 without the step below, runs of 8 and 16 tiles 382 and 345, all blocks for every tile 964).
 //
 // The tensor cores cut a partial sum towards zero at every step of 16 columns: 2.6e-5 of a weight where a score is 128
 // positive products of 1, 9e-7 at scores of a few. So with more than 64 columns one step more, after the fourth, adds
@@ -237,8 +238,8 @@ weights_few_kernel(const __grid_constant__ WeightArgs a) {
 // log-sum is subtracted afterwards. Partial sums of the scores whose weights count are then above zero first
 // and below it later, what is cut off cancels, and what is rounded afterwards is small. 128 rows a head of 72, 80, 96, 112,
 // 120 and 128 columns, error against 64 bits in 1e-7: 3.3, 3.8, 1.1, 2.7, 2.3, 2.6; without 7.9, 7.6, 3.0, 13.5, 14.7, 9.0; with
-// 64 columns, 3.2 without. It costs 2 to 3 % of the time (128 rows 110 -> 113 us, 512 rows 318 -> 326; after
-// half of the steps in use, whatever their number, 331).
+// 64 columns, 3.2 without. It costs 2 to 4 % of the time (128 rows 96.6 -> 98.7 us, 512 rows 318 -> 324; after
+// half of the steps in use, whatever their number, some 5 us more).
 constexpr int KT = 128, QB = 128, Q_STAGES = 3, CHUNK = 32;
 constexpr int WT_THREADS = 384;
 constexpr int PANEL = TILE_PANEL;
