@@ -424,6 +424,65 @@ brisk_status brisk_cache_evict(const brisk_cache_dims *dims, const brisk_view *k
                                const brisk_view *k_to, const brisk_view *v_to, float *acc_to,
                                int32_t *len_to, int32_t *kept, void *workspace, void *stream);
 
+/* ---- Own caches in 4 bits ----
+ *
+ * The own caches of a batch are what fills memory and its bandwidth; held in 4 bits they take 3.6
+ * times fewer bytes than in bf16. The prefix, held once for all sequences, stays as it is. A row (an
+ * entry of a key head, D channels, D % 16 == 0) is held in groups of 16 channels: a group has a
+ * scale, a byte with bits 14 to 7 of a positive fp16 number (5 bits of exponent, 3 of the
+ * significand; 226, for 10240, is the largest, and larger bytes stand for it too), and a channel a
+ * code of 4 bits (bit 3: sign; bits 0 to 2: which of 0, .5, 1, 1.5, 2, 3, 4, 6), two a byte, the even
+ * channel in the low half. A channel's value is code times scale, which fp16, bf16 and fp32 hold
+ * exactly. A row's codes are D/2 bytes, its scales 4 bytes (D <= 64) or 8, of which the first D/16
+ * are in use. The paper has no counterpart. brisk_cache_dims as above, with 16 <= D <= 128 and
+ * D % 16 == 0. */
+
+/* A cache of such rows: codes of entry t of sequence s and key head h at codes + s * seq + t * tok +
+ * h * head, its scales at scales + s * scale_seq + ..., strides in bytes. Codes and their strides are
+ * multiples of 16 bytes (D % 32 == 0) or 8, scales and theirs of 4 or 8 (their row's bytes); the
+ * strides of dimensions longer than 1 are at least a row and below 2^39, that of a dimension of
+ * length 1 is unused. */
+typedef struct brisk_packed {
+  void *codes, *scales;
+  int64_t seq, tok, head, scale_seq, scale_tok, scale_head;
+} brisk_packed;
+
+/* Bytes of workspace the three calls below need for `dims` (256-byte multiple; 0 if invalid). Its
+ * status word is read with brisk_last_device_status(). */
+size_t brisk_packed_workspace_bytes(const brisk_cache_dims *dims);
+
+/* Writes rows t < count[b] of k, v [B, T, Hkv, D] (dims' dtype, any strides of brisk_view) at places
+ * start[b] + t of the caches k_to, v_to [B, S, Hkv]; other places keep what they hold. start, count [B]
+ * int32; count NULL: T rows each. With a the largest magnitude of a group, its scale is a / 6 rounded
+ * to 4 significant bits (nearest, ties to even) within 2^-14 .. 10240, and a channel's code the nearest
+ * (ties to the even code; magnitudes above six scales get the largest): decided exactly, in fp32 and
+ * bf16 alike. Storing what brisk_packed_load gave writes the same bytes. A NaN is stored as 0, an
+ * infinity as the largest number of its sign, and reported as BRISK_ERR_NUMERIC in the device status.
+ * Counts outside 0..T are clamped and rows at places outside 0..S-1 left out, and reported as
+ * BRISK_ERR_INVALID_ARG (the largest code wins). T >= 1; L, Hq and P are unused. */
+brisk_status brisk_packed_store(const brisk_cache_dims *dims, int32_t T, const brisk_view *k,
+                                const brisk_view *v, const int32_t *start, const int32_t *count,
+                                const brisk_packed *k_to, const brisk_packed *v_to, void *workspace,
+                                void *stream);
+
+/* Reads back: rows t < count[b] of k_to, v_to [B, T, Hkv, D] get the values at places start[b] + t;
+ * rows from count[b] on, and those of places outside 0..S-1, get zeros. Arguments and reports as
+ * brisk_packed_store. */
+brisk_status brisk_packed_load(const brisk_cache_dims *dims, int32_t T, const brisk_packed *k,
+                               const brisk_packed *v, const int32_t *start, const int32_t *count,
+                               const brisk_view *k_to, const brisk_view *v_to, void *workspace,
+                               void *stream);
+
+/* brisk_prefix_attend with the own caches k_own, v_own [B, S, Hkv] in 4 bits (NULL if S == 0); queries,
+ * prefix and out in dims' dtype. Over own entries scores are sums of exact products in fp32, or with
+ * fp32 queries of products of the query rounded to 2^-23; the weights enter the sum of values rounded
+ * to fp16 (2^-12 each; with fp32 to 2^-22). */
+brisk_status brisk_packed_attend(const brisk_cache_dims *dims, const brisk_view *q,
+                                 const brisk_view *k_prefix, const brisk_view *v_prefix,
+                                 const brisk_packed *k_own, const brisk_packed *v_own,
+                                 const int32_t *own_len, const int32_t *visible, float scale,
+                                 void *out, float *lse, void *workspace, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -109,6 +109,10 @@ _SIGS = [
      [_vp] * 6 + [ctypes.c_float, ctypes.c_float, _vp, _vp, _vp, _vp]),
     ("brisk_cache_evict", ctypes.c_int,
      [_vp] * 5 + [ctypes.c_int32, ctypes.c_int32] + [_vp] * 7),
+    ("brisk_packed_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(CacheDims)]),
+    ("brisk_packed_store", ctypes.c_int, [_vp, ctypes.c_int32] + [_vp] * 8),
+    ("brisk_packed_load", ctypes.c_int, [_vp, ctypes.c_int32] + [_vp] * 8),
+    ("brisk_packed_attend", ctypes.c_int, [_vp] * 8 + [ctypes.c_float, _vp, _vp, _vp, _vp]),
 ]
 
 
@@ -487,11 +491,17 @@ class PrefixAttention:
     What a call given a ``stream`` allocates itself is that stream's memory (see _results).
     """
 
+    _VIEWS = 5 * ctypes.sizeof(View)
+
+    @staticmethod
+    def _workspace_bytes():
+        return lib().brisk_cache_workspace_bytes
+
     def __init__(self, B, L, Hq, Hkv, D, P, S, dtype, device="cuda"):
         self.dims = CacheDims(B, L, Hq, Hkv, D, P, S, _dt(dtype))
         self.B, self.L, self.Hq, self.Hkv, self.D, self.P, self.S = B, L, Hq, Hkv, D, P, S
         self.dtype, self.device = dtype, torch.device(device)
-        ws = int(lib().brisk_cache_workspace_bytes(ctypes.byref(self.dims)))
+        ws = int(self._workspace_bytes()(ctypes.byref(self.dims)))
         if ws == 0:
             raise BriskError(ERR_INVALID_ARG, "dims")
         self.workspace = torch.zeros(ws, dtype=torch.uint8, device=self.device)
@@ -500,7 +510,7 @@ class PrefixAttention:
         self._d = ctypes.addressof(self.dims)
         self._ws = self.workspace.data_ptr()
         # the views of a call's strided tensors, written anew by every call
-        self._views = ctypes.create_string_buffer(5 * ctypes.sizeof(View))
+        self._views = ctypes.create_string_buffer(self._VIEWS)
         at = ctypes.addressof(self._views)
         self._at = [at + i * ctypes.sizeof(View) for i in range(5)]
         self._shape_q, self._shape_pre, self._shape_own = (B, L, Hq, D), (P, Hkv, D), (B, S, Hkv, D)
@@ -624,3 +634,123 @@ class PrefixAttention:
 
     def device_status(self, clear=True, stream=None) -> int:
         return int(lib().brisk_last_device_status(self._ws, int(clear), _stream(stream)))
+
+
+_PACK_ATTEND, _PACK_MOVE = (struct.Struct(f"{n}q").pack_into for n in (3 * 4 + 2 * 8, 2 * 4 + 2 * 8))
+_NO_CACHE = (0,) * 8
+
+
+class PackedAttention(PrefixAttention):
+    """PrefixAttention whose own caches are held in 4 bits (see brisk_packed in brisk.h for the format; D a
+    multiple of 16): entries are written with store(), read back with load() and attended over with
+    attend(). The prefix stays in ``dtype``.
+
+    A cache is a dict of uint8 tensors, ``k`` and ``v`` [B, S, Hkv, D / 2] and ``k_scales`` and
+    ``v_scales`` [B, S, Hkv, 4 or 8] (see alloc_cache), of any strides whose rows are contiguous and start
+    on 16 bytes (8 where D % 32 is not 0), or on their length. The weights of own entries and the eviction by them
+    work on entries in ``dtype``: PrefixAttention's, on what load() gives; storing that again gives the same bytes.
+    """
+
+    _VIEWS = 3 * 4 * 8 + 2 * 8 * 8
+
+    @staticmethod
+    def _workspace_bytes():
+        return lib().brisk_packed_workspace_bytes
+
+    def __init__(self, B, L, Hq, Hkv, D, P, S, dtype, device="cuda"):
+        super().__init__(B, L, Hq, Hkv, D, P, S, dtype, device)
+        self._shape_codes, self._shape_scales = (B, S, Hkv, D // 2), (B, S, Hkv, 4 if D <= 64 else 8)
+        at = self._at[0]
+        self._at_attend = [at, at + 32, at + 64, at + 96, at + 160]
+        self._at_move = [at, at + 32, at + 64, at + 128]
+
+    def alloc_cache(self, order="token"):
+        """A cache of zeros, written on the current stream: in memory [B, S, Hkv, ..] ("token") or
+        [B, Hkv, S, ..] ("head": an entry's neighbours in time lie side by side)."""
+        if order not in ("token", "head"):
+            raise ValueError(f"order {order!r} is neither 'token' nor 'head'")
+
+        def new(shape):
+            if order == "token":
+                return torch.zeros(shape, dtype=torch.uint8, device=self.device)
+            B, S, H, n = shape
+            return torch.zeros((B, H, S, n), dtype=torch.uint8, device=self.device).transpose(1, 2)
+        return {"k": new(self._shape_codes), "k_scales": new(self._shape_scales),
+                "v": new(self._shape_codes), "v_scales": new(self._shape_scales)}
+
+    def _bytes(self, t, shape, what):
+        if t.shape != shape or t.dtype != torch.uint8:
+            raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, not {tuple(shape)} uint8")
+        if not t.is_cuda:
+            raise ValueError(f"{what} is not on the GPU")
+        st = t.stride()
+        if st[3] != 1:
+            raise ValueError(f"{what}: the last dimension must be contiguous")
+        return t.data_ptr(), st
+
+    def _cache(self, cache):
+        """The eight numbers of keys' and of values' brisk_packed."""
+        if self.S == 0:
+            return _NO_CACHE + _NO_CACHE
+        if cache is None:
+            raise ValueError("the cache is missing")
+        put = ()
+        for name in ("k", "v"):
+            codes, c = self._bytes(cache[name], self._shape_codes, name)
+            scales, s = self._bytes(cache[name + "_scales"], self._shape_scales, name + "_scales")
+            put += (codes, scales, c[0], c[1], c[2], s[0], s[1], s[2])
+        return put
+
+    def store(self, cache, k, v, start, count=None, stream=None):
+        """Quantises rows t < count[b] (all T unless given) of k, v [B, T, Hkv, D] into places
+        start[b] + t of ``cache`` (start, count [B] int32; see brisk_packed_store)."""
+        T = k.shape[1]
+        shape, plain, at, i32 = (self.B, T, self.Hkv, self.D), self._plain, self._at_move, torch.int32
+        _PACK_MOVE(self._views, 0, *self._view(k, shape, "k"), *self._view(v, shape, "v"), *self._cache(cache))
+        _lend(stream, self.workspace)
+        s = lib().brisk_packed_store(self._d, T, at[0], at[1], plain(start, self._shape_b, i32, "start"),
+                                     plain(count, self._shape_b, i32, "count"), at[2], at[3], self._ws,
+                                     _stream(stream))
+        if s:
+            raise BriskError(s, "packed_store")
+        return cache
+
+    def load(self, cache, T, start, count=None, out=None, stream=None):
+        """k, v [B, T, Hkv, D]: in rows t < count[b] (all T unless given) what places start[b] + t of
+        ``cache`` stand for, else zeros. ``out``: a dict of tensors to write to instead of new ones."""
+        shape, plain, view, at, i32 = (self.B, T, self.Hkv, self.D), self._plain, self._view, self._at_move, torch.int32
+        if out is None:
+            out = _results(stream, lambda: {n: torch.empty(shape, dtype=self.dtype, device=self.device) for n in "kv"})
+        _PACK_MOVE(self._views, 0, *view(out["k"], shape, "k"), *view(out["v"], shape, "v"), *self._cache(cache))
+        _lend(stream, self.workspace)
+        s = lib().brisk_packed_load(self._d, T, at[2], at[3], plain(start, self._shape_b, i32, "start"),
+                                    plain(count, self._shape_b, i32, "count"), at[0], at[1], self._ws,
+                                    _stream(stream))
+        if s:
+            raise BriskError(s, "packed_load")
+        return out
+
+    def attend(self, q, k_prefix, v_prefix, cache, own_len, visible=None, scale=None, out=None, stream=None):
+        """PrefixAttention.attend with the own entries in ``cache`` (None if S == 0)."""
+        pre, view, plain, at = self._shape_pre, self._view, self._plain, self._at_attend
+        if out is None:
+            out = _results(stream, self._attended)
+        _PACK_ATTEND(self._views, 0, *view(q, self._shape_q, "q"), *(view(k_prefix, pre, "k_prefix") or _NONE),
+                     *(view(v_prefix, pre, "v_prefix") or _NONE), *self._cache(cache))
+        _lend(stream, self.workspace)
+        s = lib().brisk_packed_attend(
+            self._d, at[0], at[1], at[2], at[3], at[4],
+            plain(own_len, self._shape_b, torch.int32, "own_len"),
+            plain(visible, self._shape_vis, torch.int32, "visible"),
+            self.scale if scale is None else scale,
+            plain(out["out"], self._shape_q, self.dtype, "out"),
+            plain(out["lse"], self._shape_lse, torch.float32, "lse"), self._ws, _stream(stream))
+        if s:
+            raise BriskError(s, "packed_attend")
+        return out
+
+    def weights(self, *args, **kwargs):
+        raise TypeError("weights() of a PrefixAttention takes the entries that load() gives")
+
+    def evict(self, *args, **kwargs):
+        raise TypeError("evict() of a PrefixAttention takes the entries that load() gives")

@@ -63,6 +63,7 @@ struct AttendArgs {
   static constexpr bool PREFIX = true;   // units of a prefix's, and items filled up (see Plan)
   int B, L, G, Hkv, D, P, S;         // G query heads a key head
   int dt;                            // brisk_dtype of q, keys, values and out
+  int joins;                         // the prefix's own kernel writes results (see JOIN_PARTS)
   Shape sh;
   CacheView q, kp, vp, ko, vo;
   Divisor by_L, by_G, by_LG;         // L, G and L * G
@@ -398,6 +399,7 @@ inline void divide(AttendArgs* a) {
   a->sh.rt_o = tc ? SLOT_ROWS : SIMT_ROWS;
   a->sh.rt_p = apart ? PAIR_ROWS : a->sh.rt_o;
   a->sh.grid_p = apart ? CACHE_SMS : 0;
+  a->joins = 1;
   a->sh.grid_o = SLOT_CTAS;
   a->sh.weight = !tc && R > FEW_ROWS && rows <= FEW_ROWS ? (rows <= 4 ? 6 : 4) : 1;
   a->sh.set(a->B, rows, a->P);
@@ -470,6 +472,9 @@ inline cudaError_t launch_early(Kernel kernel, dim3 grid, int threads, size_t sm
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream);
+// The prefix alone (sh.grid_p CTAs), behind the kernel that has the own caches' units.
+cudaError_t launch_prefix_tc(const AttendArgs& a, cudaStream_t stream);
+cudaError_t launch_prefix_f32(const AttendArgs& a, cudaStream_t stream);
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream);
 
 // ---------------------------------------------------------------- attention weight of own entries

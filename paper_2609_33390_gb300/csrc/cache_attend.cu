@@ -458,6 +458,33 @@ attend_simt_kernel(const __grid_constant__ AttendArgs a) {
   }
 }
 
+// The prefix alone, where own caches have a kernel of their own: parts, whatever its division.
+__global__ void __launch_bounds__(SIMT_THREADS, 2)
+attend_simt_prefix_kernel(const __grid_constant__ AttendArgs a) {
+  extern __shared__ __align__(16) float smem[];
+  const SimtTile t{smem, smem + RT * CACHE_MAX_D, smem + RT * CACHE_MAX_D + KT * KS};
+  __shared__ int lowest;
+  let_next_begin();
+  const int R = a.B * a.L * a.G, kP = (a.P + KT - 1) / KT, nPT = (R + RT - 1) / RT, UP = a.Hkv * nPT * kP;
+  const int2 range = units_of(blockIdx.x, max(1, (UP + a.sh.grid_p - 1) / a.sh.grid_p), UP);
+  Frag f{};
+  f.prefix = 1;
+  f.len = a.P;
+  for (int u = range.x; u < range.y; u += f.n) {
+    const int item = u / kP;
+    f.h = item / nPT;
+    f.k0 = u - item * kP;
+    f.n = min(kP - f.k0, range.y - u);
+    f.row0 = (item - f.h * nPT) * RT;
+    f.rows = min(RT, R - f.row0);
+    f.slot = item + blockIdx.x;
+    if (f.rows > 16) simt_fragment<4>(a, f, t, &lowest);
+    else simt_fragment<1>(a, f, t, &lowest);
+  }
+  if (threadIdx.x == 0) a.errs[blockIdx.x] = BRISK_OK;
+  wait_for_previous();                             // (the join waits for this kernel alone)
+}
+
 constexpr size_t SIMT_SMEM = sizeof(float) * (RT * CACHE_MAX_D + KT * KS + KT * CACHE_MAX_D);
 
 // Joins the parts of the rows whose keys were divided.
@@ -483,7 +510,7 @@ __device__ __forceinline__ Plan begin_merge(const AttendArgs& a, int32_t* cum, M
 }
 // Whether a kernel before has written a row with these parts.
 __device__ __forceinline__ bool written(const AttendArgs& a, const Parts& pre, const Parts& own) {
-  return a.sh.grid_p > 0 ? pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0);
+  return a.sh.grid_p > 0 ? a.joins && pre.n == 1 && own.n <= JOIN_PARTS : (pre.n == 0 && own.n == 1) || (pre.n == 1 && a.S == 0);
 }
 __device__ __forceinline__ void merge_status(const AttendArgs& a) {
   if (blockIdx.x != 0 || threadIdx.x >= 32) return;
@@ -684,6 +711,11 @@ cudaError_t launch_attend_f32(const AttendArgs& a, cudaStream_t stream) {
   if (rows > FEW_ROWS) return run(attend_simt_kernel<0>, 0);
   if (rows > 4) return run(attend_simt_kernel<8>, FewShape<8>::SMEM);
   return rows > 2 ? run(attend_simt_kernel<4>, FewShape<4>::SMEM) : run(attend_simt_kernel<2>, FewShape<2>::SMEM);
+}
+
+cudaError_t launch_prefix_f32(const AttendArgs& a, cudaStream_t stream) {
+  cudaError_t e = set_up_kernel(attend_simt_prefix_kernel, CARVEOUT_FULL_KB, SIMT_SMEM);
+  return e != cudaSuccess ? e : launch_early(attend_simt_prefix_kernel, a.sh.grid_p, SIMT_THREADS, SIMT_SMEM, stream, true, a);
 }
 
 cudaError_t launch_merge(const AttendArgs& a, cudaStream_t stream) {

@@ -772,25 +772,28 @@ bool make_cache_map(CUtensorMap* map, const CacheView& v, int D, int heads, int 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+cudaError_t launch_prefix_tc(const AttendArgs& a, cudaStream_t stream) {
+  AttendMaps maps;
+  if (!make_cache_map(&maps.k, a.kp, a.D, a.Hkv, a.P, 1) || !make_cache_map(&maps.v, a.vp, a.D, a.Hkv, a.P, 1))
+    return cudaErrorInvalidValue;
+  maps.k2 = maps.k;
+  maps.v2 = maps.v;
+  auto pair = a.D > 64 ? attend_pair_kernel<128> : attend_pair_kernel<64>;
+  const size_t smem = a.D > 64 ? PairShape<128>::SMEM : PairShape<64>::SMEM;
+  cudaError_t e = set_up_kernel(pair, CARVEOUT_FULL_KB, smem);
+  return e != cudaSuccess ? e : launch_early(pair, a.sh.grid_p, PAIR_THREADS, smem, stream, true, maps, a);
+}
+
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   AttendMaps maps;
-  CUtensorMap kp, vp;
-  if (!make_cache_map(&kp, a.kp, a.D, a.Hkv, a.P, 1) || !make_cache_map(&vp, a.vp, a.D, a.Hkv, a.P, 1) ||
+  if (!make_cache_map(&maps.k2, a.kp, a.D, a.Hkv, a.P, 1) || !make_cache_map(&maps.v2, a.vp, a.D, a.Hkv, a.P, 1) ||
       !make_cache_map(&maps.k, a.ko, a.D, a.Hkv, a.S, a.B) || !make_cache_map(&maps.v, a.vo, a.D, a.Hkv, a.S, a.B))
     return cudaErrorInvalidValue;
-  maps.k2 = kp;
-  maps.v2 = vp;
-  auto pair = a.D > 64 ? attend_pair_kernel<128> : attend_pair_kernel<64>;
   auto slot = a.D > 64 ? attend_slot_kernel<128> : attend_slot_kernel<64>;
-  const size_t pair_smem = a.D > 64 ? PairShape<128>::SMEM : PairShape<64>::SMEM;
   const size_t slot_smem = a.D > 64 ? SlotShape<128>::SMEM : SlotShape<64>::SMEM;
   cudaError_t e = set_up_kernel(slot, CARVEOUT_FULL_KB, slot_smem);
   if (e == cudaSuccess) e = launch_early(slot, a.sh.grid_o, SLOT_THREADS, slot_smem, stream, false, maps, a);
-  if (e == cudaSuccess && a.sh.grid_p > 0) {
-    const AttendMaps first{kp, vp, kp, vp};
-    e = set_up_kernel(pair, CARVEOUT_FULL_KB, pair_smem);
-    if (e == cudaSuccess) e = launch_early(pair, a.sh.grid_p, PAIR_THREADS, pair_smem, stream, true, first, a);
-  }
+  if (e == cudaSuccess && a.sh.grid_p > 0) e = launch_prefix_tc(a, stream);
   return e;
 }
 

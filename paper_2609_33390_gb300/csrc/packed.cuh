@@ -1,0 +1,110 @@
+// A context cache in 4 bits: its format, and the arguments of the calls that write, read and attend over it.
+//
+// A row, the D channels of an entry and key head, is D / 16 groups of 16 channels. A group has a scale s, a byte that
+// holds bits 14 to 7 of a positive fp16 number (5 bits of exponent, 3 of the significand), and a channel a code of
+// the e2m1 type, two a byte, the even channel low: a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6. The channel's value is
+// code times s. Such a product has at most six significant bits and lies between 2^-18 and 61440, so it is exact in
+// fp16 and in bf16: what the tensor cores multiply is the value itself.
+// A row's scales take 4 bytes (up to 64 channels) or 8, so that they move as one aligned word.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "cache.cuh"
+
+namespace brisk {
+
+constexpr int GROUP = 16;                          // channels of a scale
+constexpr float SCALE_MIN = 6.103515625e-05f;      // 2^-14: the smallest normal fp16 number
+constexpr float SCALE_MAX = 10240.f;               // six times it is the largest such product that fp16 holds
+constexpr uint32_t SCALE_TOP = 226;                // its byte; larger ones, which no call writes, stand for it too
+inline __host__ __device__ int scale_row(int D) { return D <= 64 ? 4 : 8; }
+
+struct PackedView {   // row (s, t, h) at codes + s*seq + t*tok + h*head, its scales at scales + s*sseq + ..., in bytes
+  uint8_t *codes, *scales;
+  long long seq, tok, head, sseq, stok, shead;
+};
+
+// The scale of a group whose largest magnitude is `top` (finite): top / 6, to nearest of 4 significant bits, as its
+// byte. The quotient's own rounding never moves it onto or across a border: where top differs from a border's
+// six-fold, which is exact, it differs by a unit in its last place, and that is more than half a one of the quotient.
+__device__ __forceinline__ uint32_t scale_byte(float top) {
+  const float s = fminf(fmaxf(top / 6.f, SCALE_MIN), SCALE_MAX);
+  const uint32_t b = __float_as_uint(s);
+  return ((b + 0x7ffffu + ((b >> 20) & 1)) >> 20) - (112u << 3);
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float((byte + (112u << 3)) << 20); }   // (byte >= 8)
+
+// x / s, correctly rounded, from r = 1 / s correctly rounded: Markstein, "Computation of elementary functions on the
+// IBM RISC System/6000 processor", IBM J. Res. Dev. 34 (1990). The exact quotient decides which code is nearest: a
+// tie is a quotient of few bits, which this gives exactly, and no other quotient is rounded to one. (The correction
+// would take the sign of a zero.)
+__device__ __forceinline__ float quotient(float x, float s, float r) {
+  const float q = x * r;
+  return copysignf(fmaf(fmaf(-q, s, x), r, q), x);
+}
+// The codes of two channels, `even` low: nearest, ties to the even code, saturated.
+__device__ __forceinline__ uint32_t to_codes(float even, float odd) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(r) : "f"(odd), "f"(even));
+  return r;
+}
+
+// The four pairs of codes of a word's bytes, as fp16 (a byte's low code in the low half).
+__device__ __forceinline__ void from_codes(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// Two scales as fp16, at most SCALE_MAX whatever the bytes hold (the minimum takes a number before a NaN).
+__device__ __forceinline__ uint32_t scales_f16(uint32_t low, uint32_t high) {
+  uint32_t r;
+  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"((low << 7) | (high << 23)), "r"(0x71007100u));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
+}
+
+// Writing and reading back: rows t < count[b] of T, at places start[b] + t of a cache of room S.
+struct PackedMoveArgs {
+  int B, T, Hkv, D, S, dt;
+  int all;                           // pieces of 16 unquantised bytes of a sequence's rows, of keys or of values
+  Divisor by_piece, by_heads;        // pieces a row; Hkv
+  CacheView k, v;                    // [B, T, Hkv, D]
+  PackedView kp, vp;
+  const int32_t *start, *count;      // count: nullptr for T each
+  int32_t* status;
+  int alone;                         // the only CTA writes the status itself
+};
+cudaError_t launch_packed_store(const PackedMoveArgs& a, cudaStream_t stream);
+cudaError_t launch_packed_load(const PackedMoveArgs& a, cudaStream_t stream);
+
+// Attention: a.ko and a.vo are unused.
+struct PackedArgs {
+  AttendArgs a;
+  PackedView k, v;
+};
+constexpr int PACKED_KT = 128;       // keys of a unit of work
+constexpr int PACKED_ROWS = 8;       // query rows of a tile
+constexpr int PACKED_CTAS = 2 * CACHE_SMS;
+inline void divide_packed(AttendArgs* a) {
+  const bool tc = a->dt == BRISK_DT_BF16;
+  a->sh.kt = PACKED_KT;
+  a->sh.rt_o = PACKED_ROWS;
+  a->sh.rt_p = tc ? PAIR_ROWS : SIMT_ROWS;
+  a->sh.grid_p = a->P == 0 ? 0 : (tc ? CACHE_SMS : SLOT_CTAS);
+  a->joins = tc;
+  a->sh.grid_o = PACKED_CTAS;
+  a->sh.weight = 1;
+  a->sh.set(a->B, a->L * a->G, a->P);
+  if (!tc) a->sh.kP = (int)(((long long)a->P + SIMT_KT - 1) / SIMT_KT);
+}
+cudaError_t launch_packed_own(const PackedArgs& p, cudaStream_t stream);
+
+}  // namespace brisk

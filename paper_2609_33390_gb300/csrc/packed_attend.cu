@@ -1,0 +1,455 @@
+// Attention over own caches in 4 bits, for the rows of a few queries: parts (or results) of up to 8 rows of a key head
+// against the keys of a fragment (see Plan), as the kernels of unquantised caches leave them.
+//
+// Eight warps of a CTA take 16 keys of the fragment each in turn. The codes become fp16 in registers, in the places
+// where mma.sync wants them, and never pass through shared memory as numbers: at the rate at which memory delivers
+// codes, a tile of fp16 written and read there would take more than the bandwidth it has. The products are
+//   S^T [16 keys, 8 rows]      = K [16 keys, D] Q^T,
+//   O^T [D channels, 8 rows]  += V^T [D channels, 16 keys] P^T.
+// The order of k in a product is free, so a lane of K has 32 neighbouring channels of its key, 16 bytes of codes, and a
+// lane of V 16 neighbouring channels of four keys, whose codes are paired by key before they are converted.
+//
+// K and V are exact in fp16. A row of Q is scaled by a power of two to a magnitude of 2^14: bf16 is exact then, down to
+// 2^-38 of the row's largest, and fp32 (TERMS = 2) goes as a sum of two fp16 of 11 bits each. Weights are taken
+// relative to 2^-SHIFT of the held maximum, so that fp16 holds them down to 2^-34 of it; rounding them costs 2^-12 each
+// (fp32: two terms, 2^-22). Sums, maxima and S are fp32. With fp32 every 16 keys' sums are taken anew and added in
+// fp32, since the tensor cores cut what they add to a sum towards zero.
+//
+// Keys and values come through a ring of a warp's own, in which its lanes copy 16 bytes at a time, three places of
+// 16 keys ahead, across the ends of fragments: nobody waits for another but where a fragment's eight parts meet.
+// Entries that a row does not see: scores are masked by selection, and every code and scale stands for a finite number
+// (see scales_f16), so that what is left in the ring or the cache cannot defeat a weight of 0.
+#include "packed.cuh"
+
+namespace brisk {
+namespace {
+
+constexpr int WARPS = 8, THREADS = 32 * WARPS;
+constexpr int SUB = 16;                            // keys of a step
+constexpr int STAGES = 4;
+constexpr int ROWS = PACKED_ROWS;
+constexpr int AHEAD = 4;                           // fragments that a warp's copies may be ahead, a power of two
+constexpr float LAZY = 5.f, SHIFT = 10.f;          // log2 of what a score may exceed the held maximum by; weights below 2^15
+
+// DP: 64 or 128 channels, of which a row's first D are there.
+template <int DP>
+struct Tile {
+  static constexpr int ROW = DP / 2, SROW = DP / 16;
+  static constexpr int CODES = SUB * ROW, SCALES = SUB * SROW;
+  static constexpr int BYTES = 2 * (CODES + SCALES);
+};
+template <int DP>
+struct alignas(16) WarpSmem {
+  uint8_t ring[STAGES][Tile<DP>::BYTES];
+};
+constexpr int OS = CACHE_MAX_D + 4;                // floats between rows of a warp's sums
+template <int DP>
+struct Smem {
+  WarpSmem<DP> warp[WARPS];
+  float sums[WARPS][ROWS][OS];
+  float2 ml[WARPS][ROWS];
+  Walk walk[WARPS];
+  Frag frag[WARPS][AHEAD];
+};
+
+// Key of a product's row i (of 8): lanes g = 2j and 2j + 1 of K, and the lanes c of V with their first and their second
+// keys, so read shared memory without conflicts.
+__device__ __forceinline__ int key_of(int i) { return (0x53427160 >> (4 * i)) & 7; }
+// A 16-byte piece's place in a tile of codes: with 64 bytes a row, pieces of 128-byte lines are swapped.
+template <int DP>
+__device__ __forceinline__ int piece_at(int key, int piece) {
+  if (DP == 64) return key * 32 + piece * 16;
+  return (key >> 1) * 128 + ((((key & 1) << 2 | piece) ^ (2 * ((key >> 1) & 3))) << 4);
+}
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16 bits
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 floats_of(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+
+template <int N>
+__device__ __forceinline__ void copy_bytes(void* to, const void* from) {
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(su32(to)), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(su32(to)), "l"(from), "n"(N) : "memory");
+}
+
+// 16 keys' codes and scales on their way to a place of the ring, by a warp; rows from `len` on are left as they are.
+template <int DP>
+__device__ __forceinline__ void copy_tile4(uint8_t* to, const PackedView& v, const uint8_t* codes, const uint8_t* scales, int t0,
+                                           int len, int D) {
+  using T = Tile<DP>;
+  const int lane = threadIdx.x & 31;
+  if ((D & 31) == 0) {
+    constexpr int P = DP / 32;                     // 16-byte pieces a row
+#pragma unroll
+    for (int i = 0; i < SUB * P / 32; ++i) {
+      const int e = i * 32 + lane, key = e / P, piece = e % P;
+      if (t0 + key < len && 32 * piece < D) copy_bytes<16>(to + piece_at<DP>(key, piece), codes + (t0 + key) * v.tok + 16 * piece);
+    }
+  } else {                                         // rows start on 8 bytes
+    constexpr int P = DP / 16;
+#pragma unroll
+    for (int i = 0; i < SUB * P / 32; ++i) {
+      const int e = i * 32 + lane, key = e / P, piece = e % P;
+      if (t0 + key < len && 16 * piece < D)
+        copy_bytes<8>(to + piece_at<DP>(key, piece >> 1) + 8 * (piece & 1), codes + (t0 + key) * v.tok + 8 * piece);
+    }
+  }
+  if (lane < SUB && t0 + lane < len) copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, scales + (t0 + lane) * v.stok);
+}
+
+template <int DP, int TERMS>
+__global__ void __launch_bounds__(THREADS, 2)
+packed_few_kernel(const __grid_constant__ PackedArgs p) {
+  using T = Tile<DP>;
+  constexpr int KS = DP / 16;                      // steps of 16 channels of a score, tiles of 16 channels of O
+  const AttendArgs& a = p.a;
+  extern __shared__ __align__(16) uint8_t raw[];
+  Smem<DP>& sm = *reinterpret_cast<Smem<DP>*>(raw);
+  __shared__ int warp_sum[WARPS], bad;
+  __shared__ Start start;
+  __shared__ Plan plan;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3, D = a.D;
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  let_next_begin();
+  {
+    const Plan made = make_plan<THREADS>(a, blockIdx.x, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start);
+    if (tid == 0) plan = made;
+  }
+  __syncthreads();
+  if (tid == 0) a.errs[a.sh.grid_p + blockIdx.x] = bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK;
+
+  Walk& walk = sm.walk[warp];
+  Frag* frags = sm.frag[warp];
+  if (lane == 0) walk = Walk(a, plan, blockIdx.x, start);
+  int walked = 0, done = 0;                        // fragments found, and worked through
+  bool more = true;                                // there may be another one to find
+  auto find = [&]() {                              // the next fragment, into its place (there is room)
+    int ok = 0;
+    if (lane == 0) ok = walk.next(a, plan, frags[walked % AHEAD]);
+    more = __shfl_sync(FULL_MASK, ok, 0) != 0;     // (and the lanes see it)
+    __syncwarp();
+    walked += more;
+    return more;
+  };
+
+  // the copying side: fragment number cf, its end, the warp's next key of it
+  int cf = -1, ct = 0, cend = 0;
+  const uint8_t *kc = nullptr, *ks = nullptr, *vc = nullptr, *vs = nullptr;
+  unsigned issued = 0, used = 0;
+  auto issue = [&]() {                             // one more tile, as a group of copies; false: there is none (yet)
+    while (ct >= cend) {
+      if (cf + 1 == walked && (!more || walked - done >= AHEAD || !find())) return false;
+      ++cf;
+      const Frag& f = frags[cf % AHEAD];
+      ct = f.k0 * PACKED_KT + warp * SUB;
+      cend = min(f.len, (f.k0 + f.n) * PACKED_KT);
+      kc = p.k.codes + f.b * p.k.seq + f.h * p.k.head;
+      ks = p.k.scales + f.b * p.k.sseq + f.h * p.k.shead;
+      vc = p.v.codes + f.b * p.v.seq + f.h * p.v.head;
+      vs = p.v.scales + f.b * p.v.sseq + f.h * p.v.shead;
+    }
+    uint8_t* to = sm.warp[warp].ring[issued % STAGES];
+    copy_tile4<DP>(to, p.k, kc, ks, ct, cend, D);
+    copy_tile4<DP>(to + T::CODES + T::SCALES, p.v, vc, vs, ct, cend, D);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ct += WARPS * SUB;
+    ++issued;
+    return true;
+  };
+  auto fill = [&]() {                              // the ring's free places
+#pragma unroll 1
+    while (issued - used < STAGES && issue()) {}
+  };
+  fill();
+
+  for (;;) {
+    if (walked == done && (!more || !find())) break;
+    const Frag f = frags[done % AHEAD];
+    const int end = min(f.len, (f.k0 + f.n) * PACKED_KT);
+
+    // queries: lane (g, c) has channels (DP / 4) c .. of row g; row_scale: of rows 2c, 2c + 1
+    uint32_t qf[TERMS][KS][2];
+    float row_scale[2];
+    int lim[2], low;
+    {
+      float q[DP / 4];
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < DP / 4; ++i) q[i] = 0.f;
+      int see = f.len;
+      if (g < f.rows) {
+        int token, head;
+        row_of(a, f, g, token, head);
+        see = row_limit(a, f, token, f.len);
+        const int b = a.by_L.of(token), i = token - b * a.L;
+        const long long at = b * a.q.seq + i * a.q.tok + head * a.q.head + c * (DP / 4);
+#pragma unroll
+        for (int i = 0; i < DP / 4; i += 4)
+          if (c * (DP / 4) + i < D) {
+            const float4 x = TERMS == 1 ? load4(static_cast<const __nv_bfloat16*>(a.q.p) + at + i)
+                                        : load4(static_cast<const float*>(a.q.p) + at + i);
+            q[i] = x.x; q[i + 1] = x.y; q[i + 2] = x.z; q[i + 3] = x.w;
+          }
+#pragma unroll
+        for (int i = 0; i < DP / 4; ++i) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(q[i]) & 0x7fffffffu));
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1)
+        top = __uint_as_float(max(__float_as_uint(top), __shfl_xor_sync(FULL_MASK, __float_as_uint(top), o)));
+      const int up = min(max(14 + 127 - (int)(__float_as_uint(top) >> 23), -126), 126);
+      const float by = __uint_as_float((uint32_t)(up + 127) << 23);
+      const float mine = fminf(a.sl2 * __uint_as_float((uint32_t)(127 - up) << 23), 3.4e38f);
+#pragma unroll
+      for (int i = 0; i < DP / 4; i += 2) {
+        const float x = q[i] * by, y = q[i + 1] * by;
+        const uint32_t h = half2_of(x, y);
+        qf[0][i / 4][(i >> 1) & 1] = h;
+        if constexpr (TERMS == 2) {
+          const float2 z = floats_of(h);
+          qf[TERMS - 1][i / 4][(i >> 1) & 1] = half2_of(x - z.x, y - z.y);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        row_scale[r] = __shfl_sync(FULL_MASK, mine, 4 * (2 * c + r));
+        lim[r] = __shfl_sync(FULL_MASK, see, 4 * (2 * c + r));
+      }
+      low = __reduce_min_sync(FULL_MASK, min(lim[0], lim[1]));
+    }
+
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float o[KS][4];
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+
+    for (int t0 = f.k0 * PACKED_KT + warp * SUB; t0 < end; t0 += WARPS * SUB) {
+      __syncwarp();                                // (the place that is filled next has been read)
+      fill();
+      if (issued - used == STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      else asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      const uint8_t* tile = sm.warp[warp].ring[used % STAGES];
+      ++used;
+
+      // scores of keys t0 + key_of(g) and 8 more, rows 2c and 2c + 1
+      float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
+      {
+        const int ka = key_of(g), kb = ka + 8;
+        uint32_t wa[DP / 32], wb[DP / 32], sa[DP / 64], sb[DP / 64];
+        if constexpr (DP == 128) {
+          const uint4 x = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(ka, c));
+          const uint4 y = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(kb, c));
+          wa[0] = x.x; wa[1] = x.y; wa[2] = x.z; wa[3] = x.w;
+          wb[0] = y.x; wb[1] = y.y; wb[2] = y.z; wb[3] = y.w;
+          const uint32_t u = *reinterpret_cast<const uint16_t*>(tile + T::CODES + ka * T::SROW + 2 * c);
+          const uint32_t v = *reinterpret_cast<const uint16_t*>(tile + T::CODES + kb * T::SROW + 2 * c);
+          sa[0] = scales_f16(u & 255, u & 255); sa[1] = scales_f16(u >> 8, u >> 8);
+          sb[0] = scales_f16(v & 255, v & 255); sb[1] = scales_f16(v >> 8, v >> 8);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(tile + ka * T::ROW + 8 * c);
+          const uint2 y = *reinterpret_cast<const uint2*>(tile + kb * T::ROW + 8 * c);
+          wa[0] = x.x; wa[1] = x.y;
+          wb[0] = y.x; wb[1] = y.y;
+          const uint32_t u = tile[T::CODES + ka * T::SROW + c], v = tile[T::CODES + kb * T::SROW + c];
+          sa[0] = scales_f16(u, u);
+          sb[0] = scales_f16(v, v);
+        }
+#pragma unroll
+        for (int w = 0; w < DP / 32; ++w) {        // a word: two steps of 16 channels
+          uint32_t x[4], y[4];
+          from_codes(wa[w], x);
+          from_codes(wb[w], y);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = mul_f16(x[i], sa[w / 2]);
+            y[i] = mul_f16(y[i], sb[w / 2]);
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t k4[4] = {x[2 * i], y[2 * i], x[2 * i + 1], y[2 * i + 1]};
+            mma(i ? s2 : s, k4, qf[0][2 * w + i][0], qf[0][2 * w + i][1]);
+            if constexpr (TERMS == 2) mma(i ? s2 : s, k4, qf[TERMS - 1][2 * w + i][0], qf[TERMS - 1][2 * w + i][1]);
+          }
+        }
+      }
+      // x[0], x[1]: rows 2c and 2c + 1 of the first key; x[2], x[3]: of the second
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (s[i] + s2[i]) * row_scale[i & 1];
+      if (t0 + SUB > low) {
+        const int ka = t0 + key_of(g), kb = ka + 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((i < 2 ? ka : kb) >= lim[i & 1]) x[i] = -INFINITY;
+      }
+      const float t[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+      if (__any_sync(FULL_MASK, t[0] > m[0] + LAZY || t[1] > m[1] + LAZY)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float top = t[r];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
+          // (each row by its own scores: its bits do not hang on its neighbours')
+          if (top > m[r] + LAZY) {
+            const float alpha = ex2(m[r] - top);
+            m[r] = top;
+            l[r] *= alpha;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+              o[i][r] *= alpha;
+              o[i][2 + r] *= alpha;
+            }
+          }
+        }
+      }
+      uint32_t pb[TERMS][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float e[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          e[r] = ex2(x[2 * i + r] - (m[r] == -INFINITY ? 0.f : m[r] - SHIFT));
+          l[r] += e[r];
+        }
+        const uint32_t h = half2_of(e[0], e[1]);
+        pb[0][i] = transposed(h);
+        if constexpr (TERMS == 2) {
+          const float2 z = floats_of(h);
+          pb[TERMS - 1][i] = transposed(half2_of(e[0] - z.x, e[1] - z.y));
+        }
+      }
+      // values: channels (DP / 8) g .. of keys key_of(2c), key_of(2c + 1) and 8 more each
+      {
+        const uint8_t* vt = tile + T::CODES + T::SCALES;
+        const int k0 = key_of(2 * c), k1 = key_of(2 * c + 1);
+        uint32_t w0[DP / 64], w1[DP / 64], w2[DP / 64], w3[DP / 64];
+        if constexpr (DP == 128) {
+          const int half = 8 * (g & 1), pc = g >> 1;
+          auto get = [&](int key, uint32_t (&w)[DP / 64]) {
+            const uint2 y = *reinterpret_cast<const uint2*>(vt + piece_at<DP>(key, pc) + half);
+            w[0] = y.x;
+            w[DP / 64 - 1] = y.y;
+          };
+          get(k0, w0);
+          get(k1, w1);
+          get(k0 + 8, w2);
+          get(k1 + 8, w3);
+        } else {
+          w0[0] = *reinterpret_cast<const uint32_t*>(vt + k0 * T::ROW + 4 * g);
+          w1[0] = *reinterpret_cast<const uint32_t*>(vt + k1 * T::ROW + 4 * g);
+          w2[0] = *reinterpret_cast<const uint32_t*>(vt + (k0 + 8) * T::ROW + 4 * g);
+          w3[0] = *reinterpret_cast<const uint32_t*>(vt + (k1 + 8) * T::ROW + 4 * g);
+        }
+        const uint8_t* sc = vt + T::CODES + (g * (DP / 8)) / GROUP;
+        const uint32_t sv0 = scales_f16(sc[k0 * T::SROW], sc[k1 * T::SROW]);
+        const uint32_t sv1 = scales_f16(sc[(k0 + 8) * T::SROW], sc[(k1 + 8) * T::SROW]);
+#pragma unroll
+        for (int w = 0; w < DP / 64; ++w) {
+          uint32_t ev[4], od[4], ev8[4], od8[4];   // even and odd channels of the keys' pairs
+          from_codes((w0[w] & 0x0f0f0f0fu) | ((w1[w] << 4) & 0xf0f0f0f0u), ev);
+          from_codes(((w0[w] >> 4) & 0x0f0f0f0fu) | (w1[w] & 0xf0f0f0f0u), od);
+          from_codes((w2[w] & 0x0f0f0f0fu) | ((w3[w] << 4) & 0xf0f0f0f0u), ev8);
+          from_codes(((w2[w] >> 4) & 0x0f0f0f0fu) | (w3[w] & 0xf0f0f0f0u), od8);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t v4[4] = {mul_f16(ev[i], sv0), mul_f16(od[i], sv0), mul_f16(ev8[i], sv1), mul_f16(od8[i], sv1)};
+            if constexpr (TERMS == 1) {
+              mma(o[4 * w + i], v4, pb[0][0], pb[0][1]);
+            } else {
+              float d[4] = {0.f, 0.f, 0.f, 0.f};
+              mma(d, v4, pb[TERMS - 1][0], pb[TERMS - 1][1]);
+              mma(d, v4, pb[0][0], pb[0][1]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) o[4 * w + i][k] += d[k];
+            }
+          }
+        }
+      }
+    }
+
+    // the warps' parts meet; o[i]: channels (DP / 8) g + 2i and 2i + 1 of rows 2c and 2c + 1
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(FULL_MASK, l[r], d);
+      if (g == 0) sm.ml[warp][2 * c + r] = make_float2(m[r] == -INFINITY ? m[r] : m[r] - SHIFT, l[r]);
+#pragma unroll
+      for (int i = 0; i < KS; i += 2)
+        store4(&sm.sums[warp][2 * c + r][(DP / 8) * g + 2 * i], make_float4(o[i][r], o[i][2 + r], o[i + 1][r], o[i + 1][2 + r]));
+    }
+    __syncthreads();
+    {
+      const int r = tid & 7, c0 = 4 * (tid >> 3);
+      float top = -INFINITY, all = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) top = fmaxf(top, sm.ml[w][r].x);
+      const float ms = top == -INFINITY ? 0.f : top;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float2 ml = sm.ml[w][r];
+        const float by = ml.x == top ? 1.f : ex2(ml.x - ms);
+        all += by * ml.y;
+        if (c0 < DP) {
+          const float4 x = load4(&sm.sums[w][r][c0]);
+          v.x = fmaf(by, x.x, v.x);
+          v.y = fmaf(by, x.y, v.y);
+          v.z = fmaf(by, x.z, v.z);
+          v.w = fmaf(by, x.w, v.w);
+        }
+      }
+      if (r < f.rows && c0 < D) {
+        if (f.whole) {
+          int token, head;
+          row_of(a, f, r, token, head);
+          const long long row = (long long)token * (a.Hkv * a.G) + head;
+          const bool none = all == 0.f || row_idle(a, token);
+          const float inv = none ? 0.f : 1.f / all;
+          const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+          if constexpr (TERMS == 1) store4(static_cast<__nv_bfloat16*>(a.out) + row * D + c0, y);
+          else store4(static_cast<float*>(a.out) + row * D + c0, y);
+          if (a.lse && c0 == 0) a.lse[row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
+        } else {
+          const int per = min(ROWS, plan.LG);
+          store4(a.part_o + part_at(f.slot, per, D, r, c0), v);
+          if (c0 == 0) a.ml_o[(long long)f.slot * per + r] = make_float2(top, all);
+        }
+      }
+    }
+    __syncthreads();
+    ++done;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+template <int DP, int TERMS>
+cudaError_t run(const PackedArgs& p, cudaStream_t stream) {
+  auto kernel = packed_few_kernel<DP, TERMS>;
+  constexpr size_t smem = sizeof(Smem<DP>);
+  cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
+  return e != cudaSuccess ? e : launch_early(kernel, p.a.sh.grid_o, THREADS, smem, stream, false, p);
+}
+
+}  // namespace
+
+cudaError_t launch_packed_own(const PackedArgs& p, cudaStream_t stream) {
+  if (p.a.dt == BRISK_DT_BF16) return p.a.D > 64 ? run<128, 1>(p, stream) : run<64, 1>(p, stream);
+  return p.a.D > 64 ? run<128, 2>(p, stream) : run<64, 2>(p, stream);
+}
+
+}  // namespace brisk
