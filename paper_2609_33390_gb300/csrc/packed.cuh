@@ -71,6 +71,15 @@ __device__ __forceinline__ uint32_t mul_f16(uint32_t x, uint32_t y) {
   return r;
 }
 
+// A row of queries whose largest magnitude has the bits `top` goes to the tensor cores times 2^up, as fp16 with a largest
+// magnitude of 2^14 to 2^15; its scores are then multiplied by query_scale. (Zeros, infinities and NaN stay what they
+// are. A scale too small for fp32 is the smallest number, with which -inf stays -inf.)
+__device__ __forceinline__ int query_shift(uint32_t top) { return min(max(14 + 127 - (int)(top >> 23), -126), 126); }
+__device__ __forceinline__ float exp2_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+__device__ __forceinline__ float query_scale(float sl2, int up) {
+  return fminf(fmaxf(sl2 * exp2_of(-up), 1.40129846e-45f), 3.4e38f);
+}
+
 // Writing and reading back: rows t < count[b] of T, at places start[b] + t of a cache of room S.
 struct PackedMoveArgs {
   int B, T, Hkv, D, S, dt;
@@ -91,12 +100,13 @@ struct PackedArgs {
   PackedView k, v;
 };
 constexpr int PACKED_KT = 128;       // keys of a unit of work
-constexpr int PACKED_ROWS = 8;       // query rows of a tile
+constexpr int PACKED_ROWS = 8;       // query rows of a tile of the kernel for few
+constexpr int PACKED_MANY = 16;      // bf16: from more rows a sequence and key head on, the kernel for many
 constexpr int PACKED_CTAS = 2 * CACHE_SMS;
 inline void divide_packed(AttendArgs* a) {
   const bool tc = a->dt == BRISK_DT_BF16;
   a->sh.kt = PACKED_KT;
-  a->sh.rt_o = PACKED_ROWS;
+  a->sh.rt_o = tc && a->L * a->G > PACKED_MANY ? SLOT_ROWS : PACKED_ROWS;
   a->sh.rt_p = tc ? PAIR_ROWS : SIMT_ROWS;
   a->sh.grid_p = a->P == 0 ? 0 : (tc ? CACHE_SMS : SLOT_CTAS);
   a->joins = tc;
@@ -105,6 +115,7 @@ inline void divide_packed(AttendArgs* a) {
   a->sh.set(a->B, a->L * a->G, a->P);
   if (!tc) a->sh.kP = (int)(((long long)a->P + SIMT_KT - 1) / SIMT_KT);
 }
-cudaError_t launch_packed_own(const PackedArgs& p, cudaStream_t stream);
+cudaError_t launch_packed_few(const PackedArgs& p, cudaStream_t stream);
+cudaError_t launch_packed_tc(const PackedArgs& p, cudaStream_t stream);
 
 }  // namespace brisk

@@ -109,7 +109,7 @@ brisk_status brisk_packed_attend(const brisk_cache_dims* d, const brisk_view* q,
   lay_out(&a, ws);
   a.wait_limit = wait_limit_cycles();
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_packed_own(p, st);
+  cudaError_t e = a.sh.rt_o == SLOT_ROWS ? launch_packed_tc(p, st) : launch_packed_few(p, st);
   if (e == cudaSuccess && d->P > 0) e = d->dtype == BRISK_DT_BF16 ? launch_prefix_tc(a, st) : launch_prefix_f32(a, st);
   if (e == cudaSuccess) e = launch_merge(a, st);
   return e == cudaSuccess ? BRISK_OK : BRISK_ERR_CUDA;

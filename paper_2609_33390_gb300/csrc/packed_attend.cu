@@ -209,9 +209,8 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
 #pragma unroll
       for (int o = 1; o < 4; o <<= 1)
         top = __uint_as_float(max(__float_as_uint(top), __shfl_xor_sync(FULL_MASK, __float_as_uint(top), o)));
-      const int up = min(max(14 + 127 - (int)(__float_as_uint(top) >> 23), -126), 126);
-      const float by = __uint_as_float((uint32_t)(up + 127) << 23);
-      const float mine = fminf(a.sl2 * __uint_as_float((uint32_t)(127 - up) << 23), 3.4e38f);
+      const int up = query_shift(__float_as_uint(top));
+      const float by = exp2_of(up), mine = query_scale(a.sl2, up);
 #pragma unroll
       for (int i = 0; i < DP / 4; i += 2) {
         const float x = q[i] * by, y = q[i + 1] * by;
@@ -447,7 +446,7 @@ cudaError_t run(const PackedArgs& p, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_packed_own(const PackedArgs& p, cudaStream_t stream) {
+cudaError_t launch_packed_few(const PackedArgs& p, cudaStream_t stream) {
   if (p.a.dt == BRISK_DT_BF16) return p.a.D > 64 ? run<128, 1>(p, stream) : run<64, 1>(p, stream);
   return p.a.D > 64 ? run<128, 2>(p, stream) : run<64, 2>(p, stream);
 }

@@ -1,0 +1,457 @@
+// Attention over own caches in 4 bits on the tensor cores of sm_103a, for many query rows a key head.
+//
+// As attend_slot_kernel (cache_attend_tc.cu), a slot of 128 query rows a CTA, two CTAs an SM, but the tiles of keys and
+// values are not copied: two warps read their codes, a tile ahead in registers, and write them as fp16, in which they
+// are exact, where the products take them from shared memory. The queries become fp16 too (both operands of a product
+// have one type), each row scaled by a power of two so that its largest magnitude is 2^14 to 2^15: exact down to 2^-38
+// of it. Weights are fp16, taken relative to 2^-10 of the held maximum. Codes that a row does not see stand for
+// finite numbers, and rows of a tile behind the last entry are written as zeros.
+#include "attend_tc.cuh"
+#include "packed.cuh"
+
+namespace brisk {
+namespace {
+
+using Weight = WeightAs<__half>;
+constexpr int CODE_WARPS = 2;
+constexpr int THREADS = SLOT + 128;                // a planning and an issuing warp, and those that read codes
+template <int DP>
+struct Shape4 {
+  static constexpr int TILE = KT * DP * 2;
+  static constexpr int STAGES = DP == 128 ? 2 : 4; // key and value tiles in turn
+  static constexpr int SMEM = 1024 + (1 + STAGES) * TILE + 4 * STAGE_BYTES;
+};
+
+// The part of a tile of codes that a warp reads: a lane has 16 bytes, 32 channels, of every eighth row (sixteenth, up to
+// 64 channels), so that eight neighbouring lanes write eight rows, whose pieces are swizzled into different banks.
+template <int DP>
+struct Codes {
+  static constexpr int PIECES = DP / 32, ROWS = 32 / PIECES, N = KT / CODE_WARPS / ROWS;
+  uint32_t w[N][4], s[N];
+};
+__device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ uint2 ldg8(const uint8_t* p) { return __ldg(reinterpret_cast<const uint2*>(p)); }
+
+// Where a tile's codes are: entries t0 .. of a head, `len` of them in use.
+struct Source {
+  const uint8_t *codes, *scales;
+  long long tok, stok;
+  int t0, len;
+};
+
+template <int DP>
+__device__ __forceinline__ void read_codes(Codes<DP>& x, int i, const Source& from, int cw, int D) {
+  using C = Codes<DP>;
+  const int lane = threadIdx.x & 31;
+  const int row = (lane & 7) | (C::PIECES == 2 ? (lane >> 4) << 3 : 0), piece = C::PIECES == 2 ? (lane >> 3) & 1 : lane >> 3;
+  const int t = from.t0 + cw * (KT / CODE_WARPS) + i * C::ROWS + row;
+  x.w[i][0] = x.w[i][1] = x.w[i][2] = x.w[i][3] = x.s[i] = 0;
+  if (t < from.len && 32 * piece < D) {
+    const uint8_t* p = from.codes + t * from.tok + 16 * piece;
+    if ((D & 31) == 0) {
+      const uint4 y = ldg16(p);
+      x.w[i][0] = y.x; x.w[i][1] = y.y; x.w[i][2] = y.z; x.w[i][3] = y.w;
+    } else {                                       // rows start on 8 bytes
+      const uint2 y = ldg8(p);
+      x.w[i][0] = y.x; x.w[i][1] = y.y;
+      if (32 * piece + 16 < D) {
+        const uint2 z = ldg8(p + 8);
+        x.w[i][2] = z.x; x.w[i][3] = z.y;
+      }
+    }
+    x.s[i] = __ldg(reinterpret_cast<const uint16_t*>(from.scales + t * from.stok + 2 * piece));
+  }
+}
+template <int DP>
+__device__ __forceinline__ void write_values(const Codes<DP>& x, int i, uint8_t* tile, int cw) {
+  using C = Codes<DP>;
+  const int lane = threadIdx.x & 31;
+  const int row = (lane & 7) | (C::PIECES == 2 ? (lane >> 4) << 3 : 0), piece = C::PIECES == 2 ? (lane >> 3) & 1 : lane >> 3;
+  const uint32_t s[2] = {scales_f16(x.s[i] & 255, x.s[i] & 255), scales_f16(x.s[i] >> 8, x.s[i] >> 8)};
+  uint8_t* to = tile + (piece >> 1) * PANEL + (cw * (KT / CODE_WARPS) + i * C::ROWS + row) * 128;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t h[4];
+    from_codes(x.w[i][k], h);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = mul_f16(h[j], s[k >> 1]);
+    *reinterpret_cast<uint4*>(to + ((((piece & 1) * 4 + k) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+  }
+}
+
+// A row of queries, as fetch_queries left it, becomes fp16 in its place; what its scores are to be multiplied by.
+template <int DP>
+__device__ __forceinline__ float scale_query(uint8_t* tile, int row, int D, float sl2) {
+  uint8_t* at = tile + row * 128;
+  uint32_t top = 0;
+#pragma unroll
+  for (int c = 0; c < DP / 8; ++c)
+    if (8 * c < D) {
+      const uint4 x = *reinterpret_cast<const uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4));
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
+    }
+  const int up = query_shift(top);
+  const float by = exp2_of(up);
+#pragma unroll
+  for (int c = 0; c < DP / 8; ++c)
+    if (8 * c < D) {
+      uint4* p = reinterpret_cast<uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4));
+      const uint4 x = *p;
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      uint32_t y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        y[i] = Weight::pair(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xffff0000u) * by);
+      *p = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+  return query_scale(sl2, up);
+}
+
+// row_weights (see there) in the registers that 256 threads of two CTAs leave: half the scores stay, the others are read
+// from TMEM twice.
+template <typename Half>
+__device__ __forceinline__ void row_weights_by_halves(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m,
+                                                      float& l, Half half) {
+  float v[64];
+  tmem_ld64(tS, v);
+  const bool hides = __any_sync(FULL_MASK, seen < KT);
+  auto hide = [&](float* x, int n, int c0) {
+    if (hides) {
+#pragma unroll
+      for (int c = 0; c < n; ++c) x[c] = c0 + c < seen ? x[c] : -INFINITY;
+    }
+  };
+  hide(v, 64, 0);
+  float top[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+  for (int c = 4; c < 64; c += 4)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], v[c + i]);
+#pragma unroll
+  for (int c0 = 64; c0 < KT; c0 += 32) {
+    float x[32];
+    tmem_ld32(tS + c0, x);
+    hide(x, 32, c0);
+#pragma unroll
+    for (int c = 0; c < 32; c += 4)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], x[c + i]);
+  }
+  const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
+  const bool over = t > m + Weight::LAZY;
+  if (__any_sync(FULL_MASK, over)) {
+    const float alpha = over ? ex2(m - t) : 1.f;   // (t is no -inf)
+    if (over) m = t;
+    l *= alpha;
+    if (!first)
+#pragma unroll 1
+      for (int c = 0; c < D; c += 16) {
+        float o[16];
+        tmem_ld16(tO + c, o);
+        uint32_t x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(o[i] * alpha);
+        tmem_st16(tO + c, x);
+      }
+  }
+  const float ms = m == -INFINITY ? 0.f : m - Weight::SHIFT;
+  const f32x2 scale2 = pack2(sl2, sl2), minus2 = pack2(-ms, -ms);
+  f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+  auto weigh = [&](const float* s, int c0) {       // 32 columns
+    uint32_t p[16];
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+      float x[4];
+      unpack2(fma2(pack2(s[c], s[c + 1]), scale2, minus2), x[0], x[1]);
+      unpack2(fma2(pack2(s[c + 2], s[c + 3]), scale2, minus2), x[2], x[3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = ex2(x[i]);
+      sum0 = add2(sum0, pack2(x[0], x[1]));
+      sum1 = add2(sum1, pack2(x[2], x[3]));
+      p[c / 2] = Weight::pair(x[0], x[1]);
+      p[c / 2 + 1] = Weight::pair(x[2], x[3]);
+    }
+    tmem_st16(tS + c0 / 2, p);
+  };
+  weigh(v, 0);
+  weigh(v + 32, 32);
+  tmem_st_wait();
+  half();
+#pragma unroll
+  for (int c0 = 64; c0 < KT; c0 += 32) {
+    float x[32];
+    tmem_ld32(tS + c0, x);
+    hide(x, 32, c0);
+    weigh(x, c0);
+  }
+  float x[2];
+  unpack2(add2(sum0, sum1), x[0], x[1]);
+  l += x[0] + x[1];
+  tmem_st_wait();
+}
+
+template <int DP>
+__global__ void __launch_bounds__(THREADS, 2)
+packed_slot_kernel(const __grid_constant__ PackedArgs p) {
+  constexpr int STAGES = Shape4<DP>::STAGES, TILE = Shape4<DP>::TILE;
+  const AttendArgs& a = p.a;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t *ring = sQ + TILE, *stage = ring + STAGES * TILE;
+  __shared__ uint64_t full[STAGES], empty[STAGES], s_full, p_ready[2], o_full, q_full, info_full[4], info_empty[4], done;
+  __shared__ Frag info[4];
+  __shared__ uint32_t tmem_slot;
+  __shared__ Start start;
+  __shared__ Plan plan;
+  __shared__ Walk walk;
+  __shared__ int aborted, bad, warp_sum[THREADS / 32];
+  volatile int* abort_flag = &aborted;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full[s], CODE_WARPS);
+      mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) mbar_init(&p_ready[s], 4);   // the slot's warps, for either half of the keys
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&info_full[s], 1);
+      mbar_init(&info_empty[s], 4 + CODE_WARPS);
+    }
+    mbar_init(&s_full, 1);
+    mbar_init(&o_full, 1);
+    mbar_init(&q_full, 4);
+    mbar_init(&done, 1);
+    aborted = 0;
+    bad = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == 0) tmem_alloc(&tmem_slot, 256);      // S | O
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  let_next_begin();
+  const uint32_t tmem = tmem_slot;
+  auto wait = [&](uint64_t* bar, int phase) { return warp_wait(bar, phase, abort_flag, a.wait_limit); };
+
+  // (the plan and the walk through it in shared memory: the others need their registers)
+  {
+    const Plan made = make_plan<THREADS>(a, blockIdx.x, blockIdx.x == 0 ? a.cum : nullptr, warp_sum, &bad, &start);
+    if (tid == 0) {
+      plan = made;
+      walk = Walk(a, made, blockIdx.x, start);
+    }
+  }
+  __syncthreads();
+  const bool some = walk.u < walk.end;
+  __syncthreads();                                 // (before it moves)
+  int unit = 0, nf = 0;                            // tiles and fragments before
+  bool off = false;
+
+  if (warp >= 4) {
+    if (warp == 4) {
+      // the fragments, each published while the one before is worked on
+      for (bool more = some; more && !off; ++nf) {
+        off = nf >= 4 && wait(&info_empty[nf & 3], (nf >> 2) - 1);
+        int last = 1;
+        if (!off && lane == 0) {
+          walk.next(a, plan, info[nf & 3]);
+          last = info[nf & 3].last;
+          mbar_arrive(&info_full[nf & 3]);
+        }
+        more = __shfl_sync(FULL_MASK, last, 0) == 0;
+      }
+    } else if (warp == 5) {
+      const int nd = a.D / 16;                     // steps of 16 columns of Q K^T, and units of O's width
+      const uint32_t id_s = idesc_f16(SLOT, KT), id_o = idesc_f16(SLOT, 16 * nd) | IDESC_B_MN;
+      const uint32_t q = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
+      const uint32_t tS = tmem, tO = tmem + 128;
+      unsigned cur = 0;
+      for (bool more = some; more && !off;) {
+        const int fs = nf & 3;
+        off = wait(&q_full, nf++);                 // (info_full came before it)
+        if (off) break;
+        const int n = info[fs].n, k0 = info[fs].k0, len = info[fs].len;
+        more = !info[fs].last;
+        for (int j = 0; j < n && !off; ++j, ++unit) {
+          const unsigned sk = cur % STAGES, sv = (cur + 1) % STAGES;
+          off = wait(&full[sk], cur / STAGES);
+          if (off) break;
+          tc_fence_after();
+          if (elect_one()) {
+            issue_scores<DP>(tS, q, k_lo + sk * (TILE >> 4), nd, id_s);
+            umma_commit(&s_full);
+            umma_commit(&empty[sk]);
+          }
+          __syncwarp();
+          const uint32_t v = v_lo + sv * (TILE >> 4);
+          const int steps = (len - (k0 + j) * KT + 15) / 16;
+          off = wait(&full[sv], (cur + 1) / STAGES) || wait(&p_ready[0], unit);
+          if (off) break;
+          tc_fence_after();
+          if (elect_one()) issue_values<0>(tO, tS, v, steps, id_o, j > 0);
+          __syncwarp();
+          off = wait(&p_ready[1], unit);
+          if (off) break;
+          tc_fence_after();
+          if (elect_one()) {
+            issue_values<1>(tO, tS, v, steps, id_o, true);
+            umma_commit(&empty[sv]);
+            if (j + 1 == n) umma_commit(&o_full);
+          }
+          __syncwarp();
+          cur += 2;
+        }
+      }
+      if (elect_one()) umma_commit(&done);
+      mbar_drain(&done, 0);
+    } else if (some) {
+      // codes to fp16: keys and values of a tile in turn, those of the next one on their way meanwhile
+      const int cw = warp - 6;
+      constexpr int N = Codes<DP>::N;
+      Codes<DP> x;
+      Source from{};
+      int j = 0, n = 0, k0 = 0, b = 0, h = 0, value = 1, last = 0;   // of the tile that is read
+      auto next = [&]() {                          // the next tile; false: there is none, or a wait gave up
+        if (!value) {
+          value = 1;
+          from.codes = p.v.codes + b * p.v.seq + h * p.v.head;
+          from.scales = p.v.scales + b * p.v.sseq + h * p.v.shead;
+          from.tok = p.v.tok;
+          from.stok = p.v.stok;
+          return true;
+        }
+        if (++j >= n) {
+          if (last) return false;
+          off = wait(&info_full[nf & 3], nf >> 2);
+          if (off) return false;
+          const Frag& f = info[nf & 3];
+          n = f.n; k0 = f.k0; b = f.b; h = f.h; last = f.last;
+          from.len = f.len;
+          j = 0;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&info_empty[nf & 3]);
+          ++nf;
+        }
+        value = 0;
+        from.t0 = (k0 + j) * KT;
+        from.codes = p.k.codes + b * p.k.seq + h * p.k.head;
+        from.scales = p.k.scales + b * p.k.sseq + h * p.k.shead;
+        from.tok = p.k.tok;
+        from.stok = p.k.stok;
+        return true;
+      };
+      bool more = next();
+      if (more)
+#pragma unroll
+        for (int i = 0; i < N; ++i) read_codes<DP>(x, i, from, cw, a.D);
+      for (unsigned cur = 0; more; ++cur) {
+        const unsigned st = cur % STAGES;
+        more = next();
+        if (off) break;
+        off = cur >= STAGES && wait(&empty[st], cur / STAGES - 1);
+        if (off) break;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          write_values<DP>(x, i, ring + st * TILE, cw);
+          if (more) read_codes<DP>(x, i, from, cw, a.D);
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[st]);
+      }
+    }
+  } else {
+    const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+    const uint32_t tS = tmem + lanes, tO = tmem + 128 + lanes;
+    // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
+    // this one's are there), this one's end. The first turn has no fragment yet, the last no next one.
+    Row y{-1, 0, nullptr};
+    float y_scale = 0.f;
+    Frag f{};
+    bool have = false, next = some;
+    for (;; ++nf) {                                // this fragment is number nf - 1
+      Row x{-1, 0, nullptr};
+      if (next) {
+        off = wait(&info_full[nf & 3], nf >> 2);
+        if (off) break;
+        x = find_row(a, info[nf & 3], tid);
+      }
+      const bool mine = have && tid < f.rows, live = __any_sync(FULL_MASK, mine);
+      float m = -INFINITY, l = 0.f;
+      if (have) {
+        auto ready = [&](int half) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_ready[half]);
+        };
+        for (int j = 0; j < f.n; ++j, ++unit) {
+          off = wait(&s_full, unit);
+          if (off) break;
+          tc_fence_after();
+          if (live)
+            row_weights_by_halves(tS, tO, a.D, mine ? y.lim - (f.k0 + j) * KT : KT, y_scale, j == 0, m, l, [&]() { ready(0); });
+          else ready(0);
+          ready(1);
+        }
+        if (off) break;
+      }
+      if (next) fetch_queries<DP>(x.q, a.D, sQ, 32 * warp);
+      if (have) {
+        off = wait(&o_full, nf - 1);
+        if (off) break;
+        tc_fence_after();
+      }
+      float x_scale = 0.f;
+      if (next) {
+        rows_fetched();
+        __syncwarp();
+        if (x.q) x_scale = scale_query<DP>(sQ, tid, a.D, a.sl2);
+        fence_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full);
+      }
+      if (have) {
+        if (live) {
+          const int per = min(SLOT, plan.LG);
+          float* part = f.whole ? nullptr : a.part_o + part_at(f.slot, per, a.D, tid, 0);
+          store_rows<false>(a, tO, y, mine, m == -INFINITY ? m : m - Weight::SHIFT, l, part,
+                            a.ml_o + (long long)f.slot * per + tid, per, stage + warp * STAGE_BYTES, Parts{});
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&info_empty[(nf - 1) & 3]);
+      }
+      if (!next) break;
+      off = wait(&q_full, nf);
+      if (off) break;
+      f = info[nf & 3];
+      y = x;
+      y_scale = x_scale;
+      have = true;
+      next = !f.last;
+    }
+    rows_fetched();                                // (queries, where a wait gave up)
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, 256);
+  if (tid == 0)
+    a.errs[a.sh.grid_p + blockIdx.x] =
+        aborted ? BRISK_ERR_TIMEOUT : (bad && blockIdx.x == 0 ? BRISK_ERR_INVALID_ARG : BRISK_OK);
+}
+
+}  // namespace
+
+cudaError_t launch_packed_tc(const PackedArgs& p, cudaStream_t stream) {
+  auto kernel = p.a.D > 64 ? packed_slot_kernel<128> : packed_slot_kernel<64>;
+  const size_t smem = p.a.D > 64 ? Shape4<128>::SMEM : Shape4<64>::SMEM;
+  cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
+  return e != cudaSuccess ? e : launch_early(kernel, p.a.sh.grid_o, THREADS, smem, stream, false, p);
+}
+
+}  // namespace brisk
