@@ -11,6 +11,7 @@ namespace brisk {
 constexpr int CACHE_MAX_B = 4096;    // sequences of a call (the join's CTAs hold the tiles before each)
 constexpr int CACHE_MAX_D = 128;     // width of a head
 constexpr int CACHE_SMS = 152;
+constexpr int UNIT_HEADS = 8;        // key heads of an own unit, at most
 
 struct CacheView {   // element (s, t, h, :) at p + s*seq + t*tok + h*head, strides in elements
   const void* p;
@@ -45,6 +46,7 @@ struct Shape {
   int weight;
   int R, kP, nPT, nLT;               // rows a key head; key and row tiles of the prefix; row tiles of a sequence
   int log_kt, log_p, log_o;          // kt, rt_p and rt_o as powers of two (a weights call's rt_o is no power)
+  int log_heads, slots_o;            // key heads of an own unit as a power of two; slots of each
   Divisor by_grid;                   // grid_o
   void set(int B, int LG, int P) {
     auto log2 = [](int x) { int l = 0; while ((2LL << l) <= x) ++l; return l; };
@@ -55,6 +57,7 @@ struct Shape {
     log_kt = log2(kt);
     log_p = log2(rt_p);
     log_o = log2(rt_o);
+    log_heads = slots_o = 0;
     by_grid.set(grid_o);
   }
 };
@@ -97,6 +100,8 @@ struct AttendArgs {
 // -> 23.4). Where a prefix's unit takes far longer than an own one (fp32, few rows a sequence), it counts as `weight`
 // units, in the CTA that has the first of them. (A share is at least a weight: no CTA between two of the prefix's
 // parts is without one.)
+// (An own unit may be the keys of several neighbouring heads at once, which a CTA's warps share: `own_heads` counts such
+// groups then, and a slot is one for each of them, slots_o apart.)
 // Slots: walking through a sequence, (item index + CTA) grows with every (item, CTA) pair, so it
 // numbers the parts. Counts of units fit 31 bits (checked on the host).
 struct Plan {
@@ -107,6 +112,7 @@ struct Plan {
   int own0;                          // number of the own caches' first unit
   int weight;                        // units that one of the prefix's counts as
   int share_p, share_o;              // units a CTA
+  int own_heads;                     // key heads of the own caches, or groups of them
   int filled;                        // what items are filled up to a multiple of
   bool apart;                        // the prefix's units and the own caches' are two sequences
 
@@ -121,8 +127,9 @@ struct Plan {
     apart = Args::PREFIX && sh.grid_p > 0;
     filled = Args::PREFIX ? pad : 1;
     kPp = apart ? kP : fill(kP, pad);
+    own_heads = Args::PREFIX ? Hkv >> sh.log_heads : Hkv;
     UP = Hkv * nPT * kPp;
-    UO = Hkv * nLT * own_tiles;
+    UO = own_heads * nLT * own_tiles;
     weight = 1;
     if (Args::PREFIX && pad == 1 && sh.weight > 1) {
       // an own fragment costs about one and a half of its units more, whatever its length (rounded alike in all kernels)
@@ -140,7 +147,7 @@ struct Plan {
   // grow; else 1.
   __device__ int fill_to(int grid_o) const {
     if (share_o == 1) return 1;
-    const long long items = (long long)Hkv * ((long long)nLT * B + (apart ? 0 : nPT));
+    const long long items = (long long)own_heads * nLT * B + (apart ? 0 : (long long)Hkv * nPT);
     return weight == 1 && (long long)own0 + UO + items * (share_o - 1) <= (long long)share_o * grid_o ? share_o : 1;
   }
 };
@@ -192,7 +199,7 @@ struct Walk {
     b = base = n = len = later = 0;
     if (u < end) {                   // (a CTA without own units has no start)
       b = start.b;
-      base = p.own0 + p.Hkv * p.nLT * start.before;
+      base = p.own0 + p.own_heads * p.nLT * start.before;
       len = clamped_len(a, b);
       n = Plan::fill(tiles_of(a, len), p.filled);
       later = a.own_len[min(b + 1, a.B - 1)];
@@ -217,7 +224,7 @@ struct Walk {
       return true;
     }
     if (u >= end) return false;
-    const int per = p.Hkv * p.nLT;
+    const int per = p.own_heads * p.nLT;
     while (u >= base + per * n) {
       base += per * n;
       ++b;
@@ -300,7 +307,7 @@ __device__ Plan make_plan(const Args& a, int cta, int32_t* cum, int* warp_sum, i
     if (pad == 1) break;
     __syncthreads();                               // the sums are read
   }
-  const int at = cta < 0 ? -1 : max(0, units_of(cta, plan.share_o, plan.own0 + plan.UO).x - plan.own0) / (plan.Hkv * plan.nLT);
+  const int at = cta < 0 ? -1 : max(0, units_of(cta, plan.share_o, plan.own0 + plan.UO).x - plan.own0) / (plan.own_heads * plan.nLT);
   for (int b = b0; b < b1; ++b) {
     const int n = tiles(b, pad);
     if (cum) cum[b] = before;
@@ -340,8 +347,10 @@ __device__ __forceinline__ Parts own_parts(const AttendArgs& a, const Plan& p, c
   Parts x{0, min(a.sh.rt_o, p.LG), nullptr, nullptr};
   const int b = a.by_LG.of(r), before = cum[b], n = cum[b + 1] - before;
   if (n == 0) return x;
-  const int ro = r - b * p.LG, lt = ro >> a.sh.log_o, of = h * p.nLT + lt, per = p.Hkv * p.nLT;
-  const int u = p.own0 + per * before + of * n, c0 = by_share_o.of(u), slot = b * per + of + c0;
+  const int group = h >> a.sh.log_heads;
+  const int ro = r - b * p.LG, lt = ro >> a.sh.log_o, of = group * p.nLT + lt, per = p.own_heads * p.nLT;
+  const int u = p.own0 + per * before + of * n, c0 = by_share_o.of(u);
+  const int slot = b * per + of + c0 + (h - (group << a.sh.log_heads)) * a.sh.slots_o;
   x.n = by_share_o.of(u + n - 1) - c0 + 1;
   x.sums = a.part_o + part_at(slot, x.per, a.D, ro - (lt << a.sh.log_o), 0);
   x.ml = a.ml_o + (long long)slot * x.per + (ro - (lt << a.sh.log_o));

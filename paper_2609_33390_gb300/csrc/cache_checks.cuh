@@ -65,7 +65,9 @@ inline CacheWs cache_ws(const AttendArgs& a) {
   const long long tiles_p = a.P > 0 ? (R + a.sh.rt_p - 1) / a.sh.rt_p * a.Hkv : 0;
   const long long tiles_o = a.S > 0 ? (LG + a.sh.rt_o - 1) / a.sh.rt_o * a.Hkv * a.B : 0;
   const long long rows_p = (tiles_p + (a.sh.grid_p ? a.sh.grid_p : a.sh.grid_o)) * (R < a.sh.rt_p ? R : a.sh.rt_p);
-  const long long rows_o = (tiles_o + a.sh.grid_o) * (LG < a.sh.rt_o ? LG : a.sh.rt_o);
+  // (a unit may be of up to UNIT_HEADS key heads, each with slots of its own)
+  const long long heads = a.sh.slots_o > 0 ? UNIT_HEADS : 1;
+  const long long rows_o = (tiles_o + heads * a.sh.grid_o) * (LG < a.sh.rt_o ? LG : a.sh.rt_o);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t q = o; o = up(o + bytes); return q; };
   w.status = take(ALIGN);

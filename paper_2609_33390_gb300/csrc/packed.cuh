@@ -59,10 +59,17 @@ __device__ __forceinline__ void from_codes(uint32_t w, uint32_t (&h)[4]) {
       "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
       "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
-// Two scales as fp16, at most SCALE_MAX whatever the bytes hold (the minimum takes a number before a NaN).
+// Two scales as fp16, at most SCALE_MAX whatever the bytes hold (the minimum takes a number before a NaN). Products, not
+// shifts: beside the conversions of codes, which take the units of integer logic two cycles each, those of
+// multiplication have room.
 __device__ __forceinline__ uint32_t scales_f16(uint32_t low, uint32_t high) {
   uint32_t r;
-  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"((low << 7) | (high << 23)), "r"(0x71007100u));
+  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(low * 0x80u + high * 0x800000u), "r"(0x71007100u));
+  return r;
+}
+__device__ __forceinline__ uint32_t scale_f16(uint32_t byte) {   // twice the same
+  uint32_t r;
+  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(byte * 0x800080u), "r"(0x71007100u));
   return r;
 }
 __device__ __forceinline__ uint32_t mul_f16(uint32_t x, uint32_t y) {
@@ -99,21 +106,33 @@ struct PackedArgs {
   AttendArgs a;
   PackedView k, v;
 };
-constexpr int PACKED_KT = 128;       // keys of a unit of work
 constexpr int PACKED_ROWS = 8;       // query rows of a tile of the kernel for few
 constexpr int PACKED_MANY = 16;      // bf16: from more rows a sequence and key head on, the kernel for many
 constexpr int PACKED_CTAS = 2 * CACHE_SMS;
+constexpr int PACKED_STEP = 32;      // keys that a warp of the kernel for few takes at a time
+constexpr int PACKED_WARPS = 8;
+constexpr int PACKED_PARTS = 64;     // parts of a row, about, that units of several heads may lead to
+// The kernel for few rows: a unit is the keys of several neighbouring heads, a head a warp or several warps a head, as many
+// heads as there are warps, while that leaves a row about PACKED_PARTS parts to join.
 inline void divide_packed(AttendArgs* a) {
-  const bool tc = a->dt == BRISK_DT_BF16;
-  a->sh.kt = PACKED_KT;
-  a->sh.rt_o = tc && a->L * a->G > PACKED_MANY ? SLOT_ROWS : PACKED_ROWS;
+  const bool tc = a->dt == BRISK_DT_BF16, many = tc && a->L * a->G > PACKED_MANY;
+  a->sh.kt = tc ? TC_KT : SIMT_KT;                 // (the prefix's)
+  a->sh.rt_o = many ? SLOT_ROWS : PACKED_ROWS;
   a->sh.rt_p = tc ? PAIR_ROWS : SIMT_ROWS;
   a->sh.grid_p = a->P == 0 ? 0 : (tc ? CACHE_SMS : SLOT_CTAS);
   a->joins = tc;
   a->sh.grid_o = PACKED_CTAS;
   a->sh.weight = 1;
   a->sh.set(a->B, a->L * a->G, a->P);
-  if (!tc) a->sh.kP = (int)(((long long)a->P + SIMT_KT - 1) / SIMT_KT);
+  const long long items = (long long)a->B * a->Hkv * a->sh.nLT;
+  int log_heads = 0;
+  while (!many && (2 << log_heads) <= UNIT_HEADS && a->Hkv % (2 << log_heads) == 0 &&
+         (long long)PACKED_CTAS * (2 << log_heads) <= PACKED_PARTS * items)
+    ++log_heads;
+  a->sh.log_kt = many || log_heads == 0 ? 7 : (log_heads == 1 ? 6 : 5);
+  a->sh.kt = 1 << a->sh.log_kt;
+  a->sh.log_heads = log_heads;
+  a->sh.slots_o = (int)((items >> log_heads) + PACKED_CTAS);
 }
 cudaError_t launch_packed_few(const PackedArgs& p, cudaStream_t stream);
 cudaError_t launch_packed_tc(const PackedArgs& p, cudaStream_t stream);

@@ -1,7 +1,7 @@
 // Attention over own caches in 4 bits, for the rows of a few queries: parts (or results) of up to 8 rows of a key head
 // against the keys of a fragment (see Plan), as the kernels of unquantised caches leave them.
 //
-// Eight warps of a CTA take 16 keys of the fragment each in turn. The codes become fp16 in registers, in the places
+// Eight warps of a CTA share the heads of a unit (see divide_packed); the warps of a head take 32 of its keys each in turn. The codes become fp16 in registers, in the places
 // where mma.sync wants them, and never pass through shared memory as numbers: at the rate at which memory delivers
 // codes, a tile of fp16 written and read there would take more than the bandwidth it has. The products are
 //   S^T [16 keys, 8 rows]      = K [16 keys, D] Q^T,
@@ -12,11 +12,11 @@
 // K and V are exact in fp16. A row of Q is scaled by a power of two to a magnitude of 2^14: bf16 is exact then, down to
 // 2^-38 of the row's largest, and fp32 (TERMS = 2) goes as a sum of two fp16 of 11 bits each. Weights are taken
 // relative to 2^-SHIFT of the held maximum, so that fp16 holds them down to 2^-34 of it; rounding them costs 2^-12 each
-// (fp32: two terms, 2^-22). Sums, maxima and S are fp32. With fp32 every 16 keys' sums are taken anew and added in
+// (fp32: two terms, 2^-22). Sums, maxima and S are fp32. With fp32 every 32 keys' sums are taken anew and added in
 // fp32, since the tensor cores cut what they add to a sum towards zero.
 //
-// Keys and values come through a ring of a warp's own, in which its lanes copy 16 bytes at a time, three places of
-// 16 keys ahead, across the ends of fragments: nobody waits for another but where a fragment's eight parts meet.
+// Keys and values come through a ring of a warp's own, in which its lanes copy 16 bytes at a time, a place of 32 keys
+// ahead, across the ends of fragments: nobody waits for another but where the parts of a head's warps meet.
 // Entries that a row does not see: scores are masked by selection, and every code and scale stands for a finite number
 // (see scales_f16), so that what is left in the ring or the cache cannot defeat a weight of 0.
 #include "packed.cuh"
@@ -24,9 +24,9 @@
 namespace brisk {
 namespace {
 
-constexpr int WARPS = 8, THREADS = 32 * WARPS;
-constexpr int SUB = 16;                            // keys of a step
-constexpr int STAGES = 4;
+constexpr int WARPS = PACKED_WARPS, THREADS = 32 * WARPS;
+constexpr int STEP = PACKED_STEP, HALVES = STEP / 16;
+constexpr int STAGES = 2;
 constexpr int ROWS = PACKED_ROWS;
 constexpr int AHEAD = 4;                           // fragments that a warp's copies may be ahead, a power of two
 constexpr float LAZY = 5.f, SHIFT = 10.f;          // log2 of what a score may exceed the held maximum by; weights below 2^15
@@ -35,7 +35,7 @@ constexpr float LAZY = 5.f, SHIFT = 10.f;          // log2 of what a score may e
 template <int DP>
 struct Tile {
   static constexpr int ROW = DP / 2, SROW = DP / 16;
-  static constexpr int CODES = SUB * ROW, SCALES = SUB * SROW;
+  static constexpr int CODES = STEP * ROW, SCALES = STEP * SROW;
   static constexpr int BYTES = 2 * (CODES + SCALES);
 };
 template <int DP>
@@ -63,13 +63,13 @@ __device__ __forceinline__ int piece_at(int key, int piece) {
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16 bits
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
@@ -79,35 +79,69 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
 __device__ __forceinline__ float2 floats_of(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
 template <int N>
-__device__ __forceinline__ void copy_bytes(void* to, const void* from) {
-  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(su32(to)), "l"(from) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(su32(to)), "l"(from), "n"(N) : "memory");
+__device__ __forceinline__ void copy_bytes(void* to, const void* from, bool there) {
+  if constexpr (N == 16)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(su32(to)),
+                 "l"(from), "r"((int)there) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %3;\n\t}" ::"r"(su32(to)),
+                 "l"(from), "r"((int)there), "n"(N) : "memory");
 }
 
-// 16 keys' codes and scales on their way to a place of the ring, by a warp; rows from `len` on are left as they are.
+// A lane's share of copying the codes and scales of STEP keys and values to a place of the ring: where from, of those that
+// are next. Rows from the cache's end on are left as they are.
 template <int DP>
-__device__ __forceinline__ void copy_tile4(uint8_t* to, const PackedView& v, const uint8_t* codes, const uint8_t* scales, int t0,
-                                           int len, int D) {
+struct Copies {
   using T = Tile<DP>;
-  const int lane = threadIdx.x & 31;
-  if ((D & 31) == 0) {
-    constexpr int P = DP / 32;                     // 16-byte pieces a row
-#pragma unroll
-    for (int i = 0; i < SUB * P / 32; ++i) {
-      const int e = i * 32 + lane, key = e / P, piece = e % P;
-      if (t0 + key < len && 32 * piece < D) copy_bytes<16>(to + piece_at<DP>(key, piece), codes + (t0 + key) * v.tok + 16 * piece);
-    }
-  } else {                                         // rows start on 8 bytes
-    constexpr int P = DP / 16;
-#pragma unroll
-    for (int i = 0; i < SUB * P / 32; ++i) {
-      const int e = i * 32 + lane, key = e / P, piece = e % P;
-      if (t0 + key < len && 16 * piece < D)
-        copy_bytes<8>(to + piece_at<DP>(key, piece >> 1) + 8 * (piece & 1), codes + (t0 + key) * v.tok + 8 * piece);
-    }
+  static constexpr int P = DP / 32;                // 16-byte pieces a row
+  static constexpr int VALUES = T::CODES + T::SCALES;
+  const uint8_t *k, *v, *ks, *vs;
+  int left;                                        // keys of the fragment from the first of these on
+  __device__ __forceinline__ void begin(const PackedArgs& p, const Frag& f, int t0, int end) {
+    const int lane = threadIdx.x & 31;
+    const bool wide = (p.a.D & 31) == 0;           // (else rows start on 8 bytes)
+    const int row = t0 + (wide ? lane / P : lane / (2 * P)), at = wide ? 16 * (lane % P) : 8 * (lane % (2 * P));
+    k = p.k.codes + f.b * p.k.seq + f.h * p.k.head + row * p.k.tok + at;
+    v = p.v.codes + f.b * p.v.seq + f.h * p.v.head + row * p.v.tok + at;
+    ks = p.k.scales + f.b * p.k.sseq + f.h * p.k.shead + (t0 + lane) * p.k.stok;
+    vs = p.v.scales + f.b * p.v.sseq + f.h * p.v.shead + (t0 + lane) * p.v.stok;
+    left = end - t0;
   }
-  if (lane < SUB && t0 + lane < len) copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, scales + (t0 + lane) * v.stok);
-}
+  __device__ __forceinline__ void copy(const PackedArgs& p, uint8_t* to, int step) {
+    const int lane = threadIdx.x & 31;
+    if ((p.a.D & 31) == 0) {
+      const int row = lane / P, piece = lane % P;
+      uint8_t* at = to + piece_at<DP>(row, piece);
+      const int end = 32 * piece < p.a.D ? left : 0;
+      const uint8_t *kf = k, *vf = v;
+      constexpr int R = 32 / P;                    // rows at once; the next are 512 bytes further
+#pragma unroll
+      for (int i = 0; i < STEP / R; ++i) {
+        copy_bytes<16>(at + 512 * i, kf, row + R * i < end);
+        copy_bytes<16>(at + 512 * i + VALUES, vf, row + R * i < end);
+        kf += R * p.k.tok;
+        vf += R * p.v.tok;
+      }
+    } else {
+      constexpr int R = 16 / P;
+      const int row = lane / (2 * P), piece = lane % (2 * P);
+      const int end = 16 * piece < p.a.D ? left : 0;
+#pragma unroll 1
+      for (int i = 0; i < STEP / R; ++i) {
+        uint8_t* at = to + piece_at<DP>(row + R * i, piece >> 1) + 8 * (piece & 1);
+        copy_bytes<8>(at, k + R * i * p.k.tok, row + R * i < end);
+        copy_bytes<8>(at + VALUES, v + R * i * p.v.tok, row + R * i < end);
+      }
+    }
+    copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks, lane < left);
+    copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs, lane < left);
+    k += step * p.k.tok;
+    v += step * p.v.tok;
+    ks += step * p.k.stok;
+    vs += step * p.v.stok;
+    left -= step;
+  }
+};
 
 template <int DP, int TERMS>
 __global__ void __launch_bounds__(THREADS, 2)
@@ -145,29 +179,32 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
     return more;
   };
 
-  // the copying side: fragment number cf, its end, the warp's next key of it
-  int cf = -1, ct = 0, cend = 0;
-  const uint8_t *kc = nullptr, *ks = nullptr, *vc = nullptr, *vs = nullptr;
+  // the copying side: fragment number cf, what is left of it for this warp, the place that is filled next
+  const int heads = 1 << a.sh.log_heads, sub = warp & (heads - 1), group = WARPS >> a.sh.log_heads, turn = warp >> a.sh.log_heads;
+  const int stride = STEP * group;                 // keys of the warps of a head: each has every group-th STEP
+  int cf = -1;
+  Copies<DP> next;
+  next.left = 0;
   unsigned issued = 0, used = 0;
+  uint8_t* const ring = sm.warp[warp].ring[0];
+  int write = 0, read = 0;                         // places of issued and used
   auto issue = [&]() {                             // one more tile, as a group of copies; false: there is none (yet)
-    while (ct >= cend) {
+    while (next.left <= 0) {
       if (cf + 1 == walked && (!more || walked - done >= AHEAD || !find())) return false;
       ++cf;
-      const Frag& f = frags[cf % AHEAD];
-      ct = f.k0 * PACKED_KT + warp * SUB;
-      cend = min(f.len, (f.k0 + f.n) * PACKED_KT);
-      kc = p.k.codes + f.b * p.k.seq + f.h * p.k.head;
-      ks = p.k.scales + f.b * p.k.sseq + f.h * p.k.shead;
-      vc = p.v.codes + f.b * p.v.seq + f.h * p.v.head;
-      vs = p.v.scales + f.b * p.v.sseq + f.h * p.v.shead;
+      Frag f = frags[cf % AHEAD];
+      f.h = f.h * heads + sub;
+      next.begin(p, f, (f.k0 << a.sh.log_kt) + turn * STEP, min(f.len, (f.k0 + f.n) << a.sh.log_kt));
     }
-    uint8_t* to = sm.warp[warp].ring[issued % STAGES];
-    copy_tile4<DP>(to, p.k, kc, ks, ct, cend, D);
-    copy_tile4<DP>(to + T::CODES + T::SCALES, p.v, vc, vs, ct, cend, D);
+    next.copy(p, ring + write, stride);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    ct += WARPS * SUB;
+    write = write == (STAGES - 1) * T::BYTES ? 0 : write + T::BYTES;
     ++issued;
     return true;
+  };
+  auto meet = [&]() {                              // of the warps of a head
+    if (group == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "r"(32 * group) : "memory");
   };
   auto fill = [&]() {                              // the ring's free places
 #pragma unroll 1
@@ -177,8 +214,9 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
 
   for (;;) {
     if (walked == done && (!more || !find())) break;
-    const Frag f = frags[done % AHEAD];
-    const int end = min(f.len, (f.k0 + f.n) * PACKED_KT);
+    Frag f = frags[done % AHEAD];
+    f.h = f.h * heads + sub;
+    const int end = min(f.len, (f.k0 + f.n) << a.sh.log_kt);
 
     // queries: lane (g, c) has channels (DP / 4) c .. of row g; row_scale: of rows 2c, 2c + 1
     uint32_t qf[TERMS][KS][2];
@@ -230,83 +268,94 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
     }
 
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float above[2] = {-INFINITY, -INFINITY}, less[2] = {0.f, 0.f};   // what a score is compared with, what is added to it
     float o[KS][4];
 #pragma unroll
     for (int i = 0; i < KS; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
 
-    for (int t0 = f.k0 * PACKED_KT + warp * SUB; t0 < end; t0 += WARPS * SUB) {
+    for (int t0 = (f.k0 << a.sh.log_kt) + turn * STEP; t0 < end; t0 += stride) {
       __syncwarp();                                // (the place that is filled next has been read)
       fill();
       if (issued - used == STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
       else asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
-      const uint8_t* tile = sm.warp[warp].ring[used % STAGES];
+      const uint8_t* tile = ring + read;
+      read = read == (STAGES - 1) * T::BYTES ? 0 : read + T::BYTES;
       ++used;
 
-      // scores of keys t0 + key_of(g) and 8 more, rows 2c and 2c + 1
-      float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
-      {
-        const int ka = key_of(g), kb = ka + 8;
+      // scores; x[u][0], x[u][1]: of key t0 + 16u + key_of(g), rows 2c and 2c + 1; x[u][2], x[u][3]: 8 keys further
+      float x[HALVES][4];
+#pragma unroll
+      for (int u = 0; u < HALVES; ++u) {
+        float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
+        const int ka = key_of(g) + 16 * u, kb = ka + 8;
         uint32_t wa[DP / 32], wb[DP / 32], sa[DP / 64], sb[DP / 64];
         if constexpr (DP == 128) {
-          const uint4 x = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(ka, c));
-          const uint4 y = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(kb, c));
-          wa[0] = x.x; wa[1] = x.y; wa[2] = x.z; wa[3] = x.w;
-          wb[0] = y.x; wb[1] = y.y; wb[2] = y.z; wb[3] = y.w;
-          const uint32_t u = *reinterpret_cast<const uint16_t*>(tile + T::CODES + ka * T::SROW + 2 * c);
-          const uint32_t v = *reinterpret_cast<const uint16_t*>(tile + T::CODES + kb * T::SROW + 2 * c);
-          sa[0] = scales_f16(u & 255, u & 255); sa[1] = scales_f16(u >> 8, u >> 8);
-          sb[0] = scales_f16(v & 255, v & 255); sb[1] = scales_f16(v >> 8, v >> 8);
+          const uint4 y = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(ka, c));
+          const uint4 z = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(kb, c));
+          wa[0] = y.x; wa[1] = y.y; wa[2] = y.z; wa[3] = y.w;
+          wb[0] = z.x; wb[1] = z.y; wb[2] = z.z; wb[3] = z.w;
+          const uint32_t e = *reinterpret_cast<const uint16_t*>(tile + T::CODES + ka * T::SROW + 2 * c);
+          const uint32_t f = *reinterpret_cast<const uint16_t*>(tile + T::CODES + kb * T::SROW + 2 * c);
+          sa[0] = scale_f16(e & 255); sa[1] = scale_f16(e >> 8);
+          sb[0] = scale_f16(f & 255); sb[1] = scale_f16(f >> 8);
         } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(tile + ka * T::ROW + 8 * c);
-          const uint2 y = *reinterpret_cast<const uint2*>(tile + kb * T::ROW + 8 * c);
-          wa[0] = x.x; wa[1] = x.y;
-          wb[0] = y.x; wb[1] = y.y;
-          const uint32_t u = tile[T::CODES + ka * T::SROW + c], v = tile[T::CODES + kb * T::SROW + c];
-          sa[0] = scales_f16(u, u);
-          sb[0] = scales_f16(v, v);
+          const uint2 y = *reinterpret_cast<const uint2*>(tile + ka * T::ROW + 8 * c);
+          const uint2 z = *reinterpret_cast<const uint2*>(tile + kb * T::ROW + 8 * c);
+          wa[0] = y.x; wa[1] = y.y;
+          wb[0] = z.x; wb[1] = z.y;
+          sa[0] = scale_f16(tile[T::CODES + ka * T::SROW + c]);
+          sb[0] = scale_f16(tile[T::CODES + kb * T::SROW + c]);
         }
 #pragma unroll
         for (int w = 0; w < DP / 32; ++w) {        // a word: two steps of 16 channels
-          uint32_t x[4], y[4];
-          from_codes(wa[w], x);
-          from_codes(wb[w], y);
+          uint32_t y[4], z[4];
+          from_codes(wa[w], y);
+          from_codes(wb[w], z);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            x[i] = mul_f16(x[i], sa[w / 2]);
-            y[i] = mul_f16(y[i], sb[w / 2]);
+            y[i] = mul_f16(y[i], sa[w / 2]);
+            z[i] = mul_f16(z[i], sb[w / 2]);
           }
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint32_t k4[4] = {x[2 * i], y[2 * i], x[2 * i + 1], y[2 * i + 1]};
+            const uint32_t k4[4] = {y[2 * i], z[2 * i], y[2 * i + 1], z[2 * i + 1]};
             mma(i ? s2 : s, k4, qf[0][2 * w + i][0], qf[0][2 * w + i][1]);
             if constexpr (TERMS == 2) mma(i ? s2 : s, k4, qf[TERMS - 1][2 * w + i][0], qf[TERMS - 1][2 * w + i][1]);
           }
         }
-      }
-      // x[0], x[1]: rows 2c and 2c + 1 of the first key; x[2], x[3]: of the second
-      float x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = (s[i] + s2[i]) * row_scale[i & 1];
-      if (t0 + SUB > low) {
-        const int ka = t0 + key_of(g), kb = ka + 8;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((i < 2 ? ka : kb) >= lim[i & 1]) x[i] = -INFINITY;
+        for (int i = 0; i < 4; ++i) x[u][i] = s[i] + s2[i];
       }
-      const float t[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
-      if (__any_sync(FULL_MASK, t[0] > m[0] + LAZY || t[1] > m[1] + LAZY)) {
+      if (t0 + STEP > low) {
+        const int key = t0 + key_of(g);
+#pragma unroll
+        for (int u = 0; u < HALVES; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key + 16 * u + (i < 2 ? 0 : 8) >= lim[i & 1]) x[u][i] = -INFINITY;
+      }
+      float t[2] = {fmaxf(x[0][0], x[0][2]), fmaxf(x[0][1], x[0][3])};
+#pragma unroll
+      for (int u = 1; u < HALVES; ++u)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) t[r] = fmaxf(t[r], fmaxf(x[u][r], x[u][2 + r]));
+#pragma unroll
+      for (int r = 0; r < 2; ++r) t[r] *= row_scale[r];
+      if (__any_sync(FULL_MASK, t[0] > above[0] || t[1] > above[1])) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float top = t[r];
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
           // (each row by its own scores: its bits do not hang on its neighbours')
-          if (top > m[r] + LAZY) {
+          if (top > above[r]) {
             const float alpha = ex2(m[r] - top);
             m[r] = top;
+            above[r] = top + LAZY;
+            less[r] = SHIFT - top;
             l[r] *= alpha;
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
@@ -316,68 +365,66 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
           }
         }
       }
-      uint32_t pb[TERMS][2];
+      uint32_t pb[HALVES][TERMS][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float e[2];
+      for (int u = 0; u < HALVES; ++u)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          e[r] = ex2(x[2 * i + r] - (m[r] == -INFINITY ? 0.f : m[r] - SHIFT));
-          l[r] += e[r];
+        for (int i = 0; i < 2; ++i) {
+          float e[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            e[r] = ex2(fmaf(x[u][2 * i + r], row_scale[r], less[r]));
+            l[r] += e[r];
+          }
+          const uint32_t h = half2_of(e[0], e[1]);
+          pb[u][0][i] = transposed(h);
+          if constexpr (TERMS == 2) {
+            const float2 z = floats_of(h);
+            pb[u][TERMS - 1][i] = transposed(half2_of(e[0] - z.x, e[1] - z.y));
+          }
         }
-        const uint32_t h = half2_of(e[0], e[1]);
-        pb[0][i] = transposed(h);
-        if constexpr (TERMS == 2) {
-          const float2 z = floats_of(h);
-          pb[TERMS - 1][i] = transposed(half2_of(e[0] - z.x, e[1] - z.y));
-        }
-      }
       // values: channels (DP / 8) g .. of keys key_of(2c), key_of(2c + 1) and 8 more each
-      {
-        const uint8_t* vt = tile + T::CODES + T::SCALES;
-        const int k0 = key_of(2 * c), k1 = key_of(2 * c + 1);
-        uint32_t w0[DP / 64], w1[DP / 64], w2[DP / 64], w3[DP / 64];
-        if constexpr (DP == 128) {
-          const int half = 8 * (g & 1), pc = g >> 1;
-          auto get = [&](int key, uint32_t (&w)[DP / 64]) {
-            const uint2 y = *reinterpret_cast<const uint2*>(vt + piece_at<DP>(key, pc) + half);
-            w[0] = y.x;
-            w[DP / 64 - 1] = y.y;
-          };
-          get(k0, w0);
-          get(k1, w1);
-          get(k0 + 8, w2);
-          get(k1 + 8, w3);
-        } else {
-          w0[0] = *reinterpret_cast<const uint32_t*>(vt + k0 * T::ROW + 4 * g);
-          w1[0] = *reinterpret_cast<const uint32_t*>(vt + k1 * T::ROW + 4 * g);
-          w2[0] = *reinterpret_cast<const uint32_t*>(vt + (k0 + 8) * T::ROW + 4 * g);
-          w3[0] = *reinterpret_cast<const uint32_t*>(vt + (k1 + 8) * T::ROW + 4 * g);
-        }
-        const uint8_t* sc = vt + T::CODES + (g * (DP / 8)) / GROUP;
-        const uint32_t sv0 = scales_f16(sc[k0 * T::SROW], sc[k1 * T::SROW]);
-        const uint32_t sv1 = scales_f16(sc[(k0 + 8) * T::SROW], sc[(k1 + 8) * T::SROW]);
+      const uint8_t* vt = tile + T::CODES + T::SCALES;
 #pragma unroll
-        for (int w = 0; w < DP / 64; ++w) {
+      for (int w = 0; w < DP / 64; ++w) {          // a word: eight channels
+        float d[4][4];
+        if constexpr (TERMS == 2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[i][k] = 0.f;
+#pragma unroll
+        for (int u = 0; u < HALVES; ++u) {
+          const int k0 = key_of(2 * c) + 16 * u, k1 = key_of(2 * c + 1) + 16 * u;
+          auto get = [&](int key) {
+            const int at = DP == 128 ? piece_at<DP>(key, g >> 1) + 8 * (g & 1) + 4 * w : key * T::ROW + 4 * g;
+            return *reinterpret_cast<const uint32_t*>(vt + at);
+          };
+          const uint32_t w0 = get(k0), w1 = get(k1), w2 = get(k0 + 8), w3 = get(k1 + 8);
+          const uint8_t* sc = vt + T::CODES + (g * (DP / 8)) / GROUP;
+          const uint32_t s0 = scales_f16(sc[k0 * T::SROW], sc[k1 * T::SROW]);
+          const uint32_t s1 = scales_f16(sc[(k0 + 8) * T::SROW], sc[(k1 + 8) * T::SROW]);
           uint32_t ev[4], od[4], ev8[4], od8[4];   // even and odd channels of the keys' pairs
-          from_codes((w0[w] & 0x0f0f0f0fu) | ((w1[w] << 4) & 0xf0f0f0f0u), ev);
-          from_codes(((w0[w] >> 4) & 0x0f0f0f0fu) | (w1[w] & 0xf0f0f0f0u), od);
-          from_codes((w2[w] & 0x0f0f0f0fu) | ((w3[w] << 4) & 0xf0f0f0f0u), ev8);
-          from_codes(((w2[w] >> 4) & 0x0f0f0f0fu) | (w3[w] & 0xf0f0f0f0u), od8);
+          from_codes((w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), ev);
+          from_codes(((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u), od);
+          from_codes((w2 & 0x0f0f0f0fu) | ((w3 << 4) & 0xf0f0f0f0u), ev8);
+          from_codes(((w2 >> 4) & 0x0f0f0f0fu) | (w3 & 0xf0f0f0f0u), od8);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t v4[4] = {mul_f16(ev[i], sv0), mul_f16(od[i], sv0), mul_f16(ev8[i], sv1), mul_f16(od8[i], sv1)};
-            if constexpr (TERMS == 1) {
-              mma(o[4 * w + i], v4, pb[0][0], pb[0][1]);
+            const uint32_t v4[4] = {mul_f16(ev[i], s0), mul_f16(od[i], s0), mul_f16(ev8[i], s1), mul_f16(od8[i], s1)};
+            if constexpr (TERMS == 2) {
+              mma(d[i], v4, pb[u][TERMS - 1][0], pb[u][TERMS - 1][1]);
+              mma(d[i], v4, pb[u][0][0], pb[u][0][1]);
             } else {
-              float d[4] = {0.f, 0.f, 0.f, 0.f};
-              mma(d, v4, pb[TERMS - 1][0], pb[TERMS - 1][1]);
-              mma(d, v4, pb[0][0], pb[0][1]);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) o[4 * w + i][k] += d[k];
+              mma(o[4 * w + i], v4, pb[u][0][0], pb[u][0][1]);
             }
           }
         }
+        if constexpr (TERMS == 2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[4 * w + i][k] += d[i][k];
       }
     }
 
@@ -391,46 +438,43 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
       for (int i = 0; i < KS; i += 2)
         store4(&sm.sums[warp][2 * c + r][(DP / 8) * g + 2 * i], make_float4(o[i][r], o[i][2 + r], o[i + 1][r], o[i + 1][2 + r]));
     }
-    __syncthreads();
-    {
-      const int r = tid & 7, c0 = 4 * (tid >> 3);
+    meet();
+#pragma unroll 1
+    for (int e = turn * 32 + lane; e < ROWS * (DP / 4); e += 32 * group) {
+      const int r = e & 7, c0 = 4 * (e >> 3);
+      if (r >= f.rows || c0 >= D) continue;
       float top = -INFINITY, all = 0.f;
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) top = fmaxf(top, sm.ml[w][r].x);
+      for (int w = sub; w < WARPS; w += heads) top = fmaxf(top, sm.ml[w][r].x);
       const float ms = top == -INFINITY ? 0.f : top;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
+      for (int w = sub; w < WARPS; w += heads) {
         const float2 ml = sm.ml[w][r];
         const float by = ml.x == top ? 1.f : ex2(ml.x - ms);
         all += by * ml.y;
-        if (c0 < DP) {
-          const float4 x = load4(&sm.sums[w][r][c0]);
-          v.x = fmaf(by, x.x, v.x);
-          v.y = fmaf(by, x.y, v.y);
-          v.z = fmaf(by, x.z, v.z);
-          v.w = fmaf(by, x.w, v.w);
-        }
+        const float4 y = load4(&sm.sums[w][r][c0]);
+        v.x = fmaf(by, y.x, v.x);
+        v.y = fmaf(by, y.y, v.y);
+        v.z = fmaf(by, y.z, v.z);
+        v.w = fmaf(by, y.w, v.w);
       }
-      if (r < f.rows && c0 < D) {
-        if (f.whole) {
-          int token, head;
-          row_of(a, f, r, token, head);
-          const long long row = (long long)token * (a.Hkv * a.G) + head;
-          const bool none = all == 0.f || row_idle(a, token);
-          const float inv = none ? 0.f : 1.f / all;
-          const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-          if constexpr (TERMS == 1) store4(static_cast<__nv_bfloat16*>(a.out) + row * D + c0, y);
-          else store4(static_cast<float*>(a.out) + row * D + c0, y);
-          if (a.lse && c0 == 0) a.lse[row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
-        } else {
-          const int per = min(ROWS, plan.LG);
-          store4(a.part_o + part_at(f.slot, per, D, r, c0), v);
-          if (c0 == 0) a.ml_o[(long long)f.slot * per + r] = make_float2(top, all);
-        }
+      if (f.whole) {
+        int token, head;
+        row_of(a, f, r, token, head);
+        const long long row = (long long)token * (a.Hkv * a.G) + head;
+        const bool none = all == 0.f || row_idle(a, token);
+        const float inv = none ? 0.f : 1.f / all;
+        const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        if constexpr (TERMS == 1) store4(static_cast<__nv_bfloat16*>(a.out) + row * D + c0, y);
+        else store4(static_cast<float*>(a.out) + row * D + c0, y);
+        if (a.lse && c0 == 0) a.lse[row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
+      } else {
+        const int per = min(ROWS, plan.LG);
+        const long long slot = (long long)sub * a.sh.slots_o + f.slot;
+        store4(a.part_o + part_at(slot, per, D, r, c0), v);
+        if (c0 == 0) a.ml_o[slot * per + r] = make_float2(top, all);
       }
     }
-    __syncthreads();
+    meet();
     ++done;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");

@@ -67,7 +67,7 @@ __device__ __forceinline__ void write_values(const Codes<DP>& x, int i, uint8_t*
   using C = Codes<DP>;
   const int lane = threadIdx.x & 31;
   const int row = (lane & 7) | (C::PIECES == 2 ? (lane >> 4) << 3 : 0), piece = C::PIECES == 2 ? (lane >> 3) & 1 : lane >> 3;
-  const uint32_t s[2] = {scales_f16(x.s[i] & 255, x.s[i] & 255), scales_f16(x.s[i] >> 8, x.s[i] >> 8)};
+  const uint32_t s[2] = {scale_f16(x.s[i] & 255), scale_f16(x.s[i] >> 8)};
   uint8_t* to = tile + (piece >> 1) * PANEL + (cw * (KT / CODE_WARPS) + i * C::ROWS + row) * 128;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {

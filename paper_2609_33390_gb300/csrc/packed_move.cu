@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) load_kernel(const __grid_constan
     if (!to[j]) continue;
     uint32_t x[4];
     from_codes(codes[j], x);
-    const uint32_t s = scales_f16(byte[j], byte[j]);
+    const uint32_t s = scale_f16(byte[j]);
     float f[C];
 #pragma unroll
     for (int i = 0; i < C / 2; ++i) {              // (the products are exact, in fp16 and in T)
