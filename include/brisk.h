@@ -440,8 +440,8 @@ brisk_status brisk_cache_evict(const brisk_cache_dims *dims, const brisk_view *k
 /* A cache of such rows: codes of entry t of sequence s and key head h at codes + s * seq + t * tok +
  * h * head, its scales at scales + s * scale_seq + ..., strides in bytes. Codes and their strides are
  * multiples of 16 bytes (D % 32 == 0) or 8, scales and theirs of 4 or 8 (their row's bytes); the
- * strides of dimensions longer than 1 are at least a row and below 2^39, that of a dimension of
- * length 1 is unused. */
+ * strides of dimensions longer than 1 are at least a row and below 2^39 (tok and scale_tok below 2^32),
+ * that of a dimension of length 1 is unused. */
 typedef struct brisk_packed {
   void *codes, *scales;
   int64_t seq, tok, head, scale_seq, scale_tok, scale_head;

@@ -22,7 +22,8 @@ inline __host__ __device__ int scale_row(int D) { return D <= 64 ? 4 : 8; }
 
 struct PackedView {   // row (s, t, h) at codes + s*seq + t*tok + h*head, its scales at scales + s*sseq + ..., in bytes
   uint8_t *codes, *scales;
-  long long seq, tok, head, sseq, stok, shead;
+  long long seq, head, sseq, shead;
+  uint32_t tok, stok;
 };
 
 // The scale of a group whose largest magnitude is `top` (finite): top / 6, to nearest of 4 significant bits, as its

@@ -19,7 +19,7 @@ bool strides_ok(const void* ptr, const int64_t (&in)[3], const long long (&ext)[
   if (!ptr || !aligned(ptr, step)) return false;
   for (int i = 0; i < 3; ++i) {
     out[i] = ext[i] > 1 ? in[i] : row;
-    if (out[i] < row || out[i] % step != 0 || out[i] >= (1LL << 39)) return false;
+    if (out[i] < row || out[i] % step != 0 || out[i] >= (1LL << (i == 1 ? 32 : 39))) return false;
   }
   return true;
 }
@@ -33,7 +33,7 @@ bool packed_ok(const brisk_packed* v, const brisk_cache_dims* d, PackedView* out
   if (!strides_ok(v->codes, codes, ext, d->D / 2, d->D % 32 == 0 ? 16 : 8, c) ||
       !strides_ok(v->scales, scales, ext, scale_row(d->D), scale_row(d->D), s))
     return false;
-  *out = PackedView{static_cast<uint8_t*>(v->codes), static_cast<uint8_t*>(v->scales), c[0], c[1], c[2], s[0], s[1], s[2]};
+  *out = PackedView{static_cast<uint8_t*>(v->codes), static_cast<uint8_t*>(v->scales), c[0], c[2], s[0], s[2], (uint32_t)c[1], (uint32_t)s[1]};
   return true;
 }
 

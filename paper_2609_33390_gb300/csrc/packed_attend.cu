@@ -12,7 +12,7 @@
 // K and V are exact in fp16. A row of Q is scaled by a power of two to a magnitude of 2^14: bf16 is exact then, down to
 // 2^-38 of the row's largest, and fp32 (TERMS = 2) goes as a sum of two fp16 of 11 bits each. Weights are taken
 // relative to 2^-SHIFT of the held maximum, so that fp16 holds them down to 2^-34 of it; rounding them costs 2^-12 each
-// (fp32: two terms, 2^-22). Sums, maxima and S are fp32. With fp32 every 32 keys' sums are taken anew and added in
+// (fp32: two terms, 2^-22). Sums, maxima and S are fp32. With fp32 every 16 keys' sums are taken anew and added in
 // fp32, since the tensor cores cut what they add to a sum towards zero.
 //
 // Keys and values come through a ring of a warp's own, in which its lanes copy 16 bytes at a time, a place of 32 keys
@@ -67,6 +67,11 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {   // to a sum of 0
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16 bits
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -97,14 +102,18 @@ struct Copies {
   static constexpr int VALUES = T::CODES + T::SCALES;
   const uint8_t *k, *v, *ks, *vs;
   int left;                                        // keys of the fragment from the first of these on
+  // (one multiplication of 32 bits each, beside the conversions that take the integer units)
+  static __device__ __forceinline__ const uint8_t* ahead(const uint8_t* p, int rows, uint32_t stride) {
+    return p + (unsigned long long)(uint32_t)rows * stride;
+  }
   __device__ __forceinline__ void begin(const PackedArgs& p, const Frag& f, int t0, int end) {
     const int lane = threadIdx.x & 31;
     const bool wide = (p.a.D & 31) == 0;           // (else rows start on 8 bytes)
     const int row = t0 + (wide ? lane / P : lane / (2 * P)), at = wide ? 16 * (lane % P) : 8 * (lane % (2 * P));
-    k = p.k.codes + f.b * p.k.seq + f.h * p.k.head + row * p.k.tok + at;
-    v = p.v.codes + f.b * p.v.seq + f.h * p.v.head + row * p.v.tok + at;
-    ks = p.k.scales + f.b * p.k.sseq + f.h * p.k.shead + (t0 + lane) * p.k.stok;
-    vs = p.v.scales + f.b * p.v.sseq + f.h * p.v.shead + (t0 + lane) * p.v.stok;
+    k = ahead(p.k.codes + f.b * p.k.seq + f.h * p.k.head + at, row, p.k.tok);
+    v = ahead(p.v.codes + f.b * p.v.seq + f.h * p.v.head + at, row, p.v.tok);
+    ks = ahead(p.k.scales + f.b * p.k.sseq + f.h * p.k.shead, t0 + lane, p.k.stok);
+    vs = ahead(p.v.scales + f.b * p.v.sseq + f.h * p.v.shead, t0 + lane, p.v.stok);
     left = end - t0;
   }
   __device__ __forceinline__ void copy(const PackedArgs& p, uint8_t* to, int step) {
@@ -113,14 +122,11 @@ struct Copies {
       const int row = lane / P, piece = lane % P;
       uint8_t* at = to + piece_at<DP>(row, piece);
       const int end = 32 * piece < p.a.D ? left : 0;
-      const uint8_t *kf = k, *vf = v;
       constexpr int R = 32 / P;                    // rows at once; the next are 512 bytes further
 #pragma unroll
       for (int i = 0; i < STEP / R; ++i) {
-        copy_bytes<16>(at + 512 * i, kf, row + R * i < end);
-        copy_bytes<16>(at + 512 * i + VALUES, vf, row + R * i < end);
-        kf += R * p.k.tok;
-        vf += R * p.v.tok;
+        copy_bytes<16>(at + 512 * i, ahead(k, R * i, p.k.tok), row + R * i < end);
+        copy_bytes<16>(at + 512 * i + VALUES, ahead(v, R * i, p.v.tok), row + R * i < end);
       }
     } else {
       constexpr int R = 16 / P;
@@ -129,16 +135,16 @@ struct Copies {
 #pragma unroll 1
       for (int i = 0; i < STEP / R; ++i) {
         uint8_t* at = to + piece_at<DP>(row + R * i, piece >> 1) + 8 * (piece & 1);
-        copy_bytes<8>(at, k + R * i * p.k.tok, row + R * i < end);
-        copy_bytes<8>(at + VALUES, v + R * i * p.v.tok, row + R * i < end);
+        copy_bytes<8>(at, ahead(k, R * i, p.k.tok), row + R * i < end);
+        copy_bytes<8>(at + VALUES, ahead(v, R * i, p.v.tok), row + R * i < end);
       }
     }
     copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks, lane < left);
     copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs, lane < left);
-    k += step * p.k.tok;
-    v += step * p.v.tok;
-    ks += step * p.k.stok;
-    vs += step * p.v.stok;
+    k = ahead(k, step, p.k.tok);
+    v = ahead(v, step, p.v.tok);
+    ks = ahead(ks, step, p.k.stok);
+    vs = ahead(vs, step, p.v.stok);
     left -= step;
   }
 };
@@ -212,6 +218,19 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
   };
   fill();
 
+  // where a lane reads a tile: its key's codes and scales, and those of its two values (each 8 and 16 rows further, too)
+  constexpr int VALUES = T::CODES + T::SCALES;
+  int at_k = DP == 128 ? piece_at<DP>(key_of(g), c) : key_of(g) * T::ROW + 8 * c, at_ks = T::CODES + key_of(g) * T::SROW + c * (DP / 64);
+  int at_v[2], at_vs[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int key = key_of(2 * c + i);
+    at_v[i] = VALUES + (DP == 128 ? piece_at<DP>(key, g >> 1) + 8 * (g & 1) : key * T::ROW + 4 * g);
+    at_vs[i] = VALUES + T::CODES + key * T::SROW + g * (DP / 8) / GROUP;
+  }
+  // (the compiler would rather work them out again at every step)
+  asm volatile("" : "+r"(at_k), "+r"(at_ks), "+r"(at_v[0]), "+r"(at_v[1]), "+r"(at_vs[0]), "+r"(at_vs[1]));
+
   for (;;) {
     if (walked == done && (!more || !find())) break;
     Frag f = frags[done % AHEAD];
@@ -221,13 +240,12 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
     // queries: lane (g, c) has channels (DP / 4) c .. of row g; row_scale: of rows 2c, 2c + 1
     uint32_t qf[TERMS][KS][2];
     float row_scale[2];
-    int lim[2], low;
+    int see = f.len, low;                          // entries that row g sees, and the row that sees fewest
     {
       float q[DP / 4];
       float top = 0.f;
 #pragma unroll
       for (int i = 0; i < DP / 4; ++i) q[i] = 0.f;
-      int see = f.len;
       if (g < f.rows) {
         int token, head;
         row_of(a, f, g, token, head);
@@ -262,12 +280,11 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         row_scale[r] = __shfl_sync(FULL_MASK, mine, 4 * (2 * c + r));
-        lim[r] = __shfl_sync(FULL_MASK, see, 4 * (2 * c + r));
       }
-      low = __reduce_min_sync(FULL_MASK, min(lim[0], lim[1]));
+      low = __reduce_min_sync(FULL_MASK, see);
     }
 
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float l[2] = {0.f, 0.f};
     float above[2] = {-INFINITY, -INFINITY}, less[2] = {0.f, 0.f};   // what a score is compared with, what is added to it
     float o[KS][4];
 #pragma unroll
@@ -287,50 +304,50 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
 
       // scores; x[u][0], x[u][1]: of key t0 + 16u + key_of(g), rows 2c and 2c + 1; x[u][2], x[u][3]: 8 keys further
       float x[HALVES][4];
+      {
+        constexpr int W = DP / 32;                 // words of a lane's row, two steps of 16 channels each
+        uint32_t wk[HALVES][2][W], sk[HALVES][2][DP / 64];
 #pragma unroll
-      for (int u = 0; u < HALVES; ++u) {
-        float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
-        const int ka = key_of(g) + 16 * u, kb = ka + 8;
-        uint32_t wa[DP / 32], wb[DP / 32], sa[DP / 64], sb[DP / 64];
-        if constexpr (DP == 128) {
-          const uint4 y = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(ka, c));
-          const uint4 z = *reinterpret_cast<const uint4*>(tile + piece_at<DP>(kb, c));
-          wa[0] = y.x; wa[1] = y.y; wa[2] = y.z; wa[3] = y.w;
-          wb[0] = z.x; wb[1] = z.y; wb[2] = z.z; wb[3] = z.w;
-          const uint32_t e = *reinterpret_cast<const uint16_t*>(tile + T::CODES + ka * T::SROW + 2 * c);
-          const uint32_t f = *reinterpret_cast<const uint16_t*>(tile + T::CODES + kb * T::SROW + 2 * c);
-          sa[0] = scale_f16(e & 255); sa[1] = scale_f16(e >> 8);
-          sb[0] = scale_f16(f & 255); sb[1] = scale_f16(f >> 8);
-        } else {
-          const uint2 y = *reinterpret_cast<const uint2*>(tile + ka * T::ROW + 8 * c);
-          const uint2 z = *reinterpret_cast<const uint2*>(tile + kb * T::ROW + 8 * c);
-          wa[0] = y.x; wa[1] = y.y;
-          wb[0] = z.x; wb[1] = z.y;
-          sa[0] = scale_f16(tile[T::CODES + ka * T::SROW + c]);
-          sb[0] = scale_f16(tile[T::CODES + kb * T::SROW + c]);
-        }
-#pragma unroll
-        for (int w = 0; w < DP / 32; ++w) {        // a word: two steps of 16 channels
-          uint32_t y[4], z[4];
-          from_codes(wa[w], y);
-          from_codes(wb[w], z);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            y[i] = mul_f16(y[i], sa[w / 2]);
-            z[i] = mul_f16(z[i], sb[w / 2]);
-          }
+        for (int u = 0; u < HALVES; ++u)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint32_t k4[4] = {y[2 * i], z[2 * i], y[2 * i + 1], z[2 * i + 1]};
-            mma(i ? s2 : s, k4, qf[0][2 * w + i][0], qf[0][2 * w + i][1]);
-            if constexpr (TERMS == 2) mma(i ? s2 : s, k4, qf[TERMS - 1][2 * w + i][0], qf[TERMS - 1][2 * w + i][1]);
-          }
-        }
+            const int row = 16 * u + 8 * i;
+            if constexpr (DP == 128) {
+              const uint4 y = *reinterpret_cast<const uint4*>(tile + at_k + row * T::ROW);
+              wk[u][i][0] = y.x; wk[u][i][1] = y.y; wk[u][i][W - 2] = y.z; wk[u][i][W - 1] = y.w;
+            } else {
+              const uint2 y = *reinterpret_cast<const uint2*>(tile + at_k + row * T::ROW);
+              wk[u][i][0] = y.x; wk[u][i][1] = y.y;
+            }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[u][i] = s[i] + s2[i];
+            for (int j = 0; j < DP / 64; ++j) sk[u][i][j] = scale_f16(tile[at_ks + row * T::SROW + j]);
+          }
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+          for (int u = 0; u < HALVES; ++u) {
+            uint32_t y[4], z[4];
+            from_codes(wk[u][0][w], y);
+            from_codes(wk[u][1][w], z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              y[i] = mul_f16(y[i], sk[u][0][w / 2]);
+              z[i] = mul_f16(z[i], sk[u][1][w / 2]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t k4[4] = {y[2 * i], z[2 * i], y[2 * i + 1], z[2 * i + 1]};
+              if (w == 0 && i == 0) mma_first(x[u], k4, qf[0][0][0], qf[0][0][1]);
+              else mma(x[u], k4, qf[0][2 * w + i][0], qf[0][2 * w + i][1]);
+              if constexpr (TERMS == 2) mma(x[u], k4, qf[TERMS - 1][2 * w + i][0], qf[TERMS - 1][2 * w + i][1]);
+            }
+          }
       }
       if (t0 + STEP > low) {
         const int key = t0 + key_of(g);
+        int lim[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) lim[r] = __shfl_sync(FULL_MASK, see, 4 * (2 * c + r));
 #pragma unroll
         for (int u = 0; u < HALVES; ++u)
 #pragma unroll
@@ -352,8 +369,7 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
           for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
           // (each row by its own scores: its bits do not hang on its neighbours')
           if (top > above[r]) {
-            const float alpha = ex2(m[r] - top);
-            m[r] = top;
+            const float alpha = ex2(above[r] - LAZY - top);
             above[r] = top + LAZY;
             less[r] = SHIFT - top;
             l[r] *= alpha;
@@ -384,47 +400,46 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
           }
         }
       // values: channels (DP / 8) g .. of keys key_of(2c), key_of(2c + 1) and 8 more each
-      const uint8_t* vt = tile + T::CODES + T::SCALES;
 #pragma unroll
-      for (int w = 0; w < DP / 64; ++w) {          // a word: eight channels
-        float d[4][4];
-        if constexpr (TERMS == 2)
+      for (int u = 0; u < HALVES; ++u) {
+        uint32_t w0[DP / 64], w1[DP / 64], w2[DP / 64], w3[DP / 64];
+        auto get = [&](int at, uint32_t (&w)[DP / 64]) {
+          if constexpr (DP == 128) {
+            const uint2 y = *reinterpret_cast<const uint2*>(tile + at);
+            w[0] = y.x;
+            w[DP / 64 - 1] = y.y;
+          } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(tile + at);
+          }
+        };
+        const int row = 16 * u * T::ROW, row8 = row + 8 * T::ROW, srow = 16 * u * T::SROW, srow8 = srow + 8 * T::SROW;
+        get(at_v[0] + row, w0);
+        get(at_v[1] + row, w1);
+        get(at_v[0] + row8, w2);
+        get(at_v[1] + row8, w3);
+        const uint32_t s0 = scales_f16(tile[at_vs[0] + srow], tile[at_vs[1] + srow]);
+        const uint32_t s1 = scales_f16(tile[at_vs[0] + srow8], tile[at_vs[1] + srow8]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) d[i][k] = 0.f;
-#pragma unroll
-        for (int u = 0; u < HALVES; ++u) {
-          const int k0 = key_of(2 * c) + 16 * u, k1 = key_of(2 * c + 1) + 16 * u;
-          auto get = [&](int key) {
-            const int at = DP == 128 ? piece_at<DP>(key, g >> 1) + 8 * (g & 1) + 4 * w : key * T::ROW + 4 * g;
-            return *reinterpret_cast<const uint32_t*>(vt + at);
-          };
-          const uint32_t w0 = get(k0), w1 = get(k1), w2 = get(k0 + 8), w3 = get(k1 + 8);
-          const uint8_t* sc = vt + T::CODES + (g * (DP / 8)) / GROUP;
-          const uint32_t s0 = scales_f16(sc[k0 * T::SROW], sc[k1 * T::SROW]);
-          const uint32_t s1 = scales_f16(sc[(k0 + 8) * T::SROW], sc[(k1 + 8) * T::SROW]);
+        for (int w = 0; w < DP / 64; ++w) {        // a word: eight channels
           uint32_t ev[4], od[4], ev8[4], od8[4];   // even and odd channels of the keys' pairs
-          from_codes((w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), ev);
-          from_codes(((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u), od);
-          from_codes((w2 & 0x0f0f0f0fu) | ((w3 << 4) & 0xf0f0f0f0u), ev8);
-          from_codes(((w2 >> 4) & 0x0f0f0f0fu) | (w3 & 0xf0f0f0f0u), od8);
+          from_codes((w0[w] & 0x0f0f0f0fu) | ((w1[w] << 4) & 0xf0f0f0f0u), ev);
+          from_codes(((w0[w] >> 4) & 0x0f0f0f0fu) | (w1[w] & 0xf0f0f0f0u), od);
+          from_codes((w2[w] & 0x0f0f0f0fu) | ((w3[w] << 4) & 0xf0f0f0f0u), ev8);
+          from_codes(((w2[w] >> 4) & 0x0f0f0f0fu) | (w3[w] & 0xf0f0f0f0u), od8);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t v4[4] = {mul_f16(ev[i], s0), mul_f16(od[i], s0), mul_f16(ev8[i], s1), mul_f16(od8[i], s1)};
-            if constexpr (TERMS == 2) {
-              mma(d[i], v4, pb[u][TERMS - 1][0], pb[u][TERMS - 1][1]);
-              mma(d[i], v4, pb[u][0][0], pb[u][0][1]);
+            if constexpr (TERMS == 2) {            // (these keys' sums, to be added in fp32)
+              float d[4];
+              mma_first(d, v4, pb[u][TERMS - 1][0], pb[u][TERMS - 1][1]);
+              mma(d, v4, pb[u][0][0], pb[u][0][1]);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) o[4 * w + i][k] += d[k];
             } else {
               mma(o[4 * w + i], v4, pb[u][0][0], pb[u][0][1]);
             }
           }
         }
-        if constexpr (TERMS == 2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) o[4 * w + i][k] += d[i][k];
       }
     }
 
@@ -433,7 +448,7 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(FULL_MASK, l[r], d);
-      if (g == 0) sm.ml[warp][2 * c + r] = make_float2(m[r] == -INFINITY ? m[r] : m[r] - SHIFT, l[r]);
+      if (g == 0) sm.ml[warp][2 * c + r] = make_float2(above[r] == -INFINITY ? -INFINITY : -less[r], l[r]);
 #pragma unroll
       for (int i = 0; i < KS; i += 2)
         store4(&sm.sums[warp][2 * c + r][(DP / 8) * g + 2 * i], make_float4(o[i][r], o[i][2 + r], o[i + 1][r], o[i + 1][2 + r]));

@@ -35,7 +35,7 @@ __device__ __forceinline__ uint2 ldg8(const uint8_t* p) { return __ldg(reinterpr
 // Where a tile's codes are: entries t0 .. of a head, `len` of them in use.
 struct Source {
   const uint8_t *codes, *scales;
-  long long tok, stok;
+  uint32_t tok, stok;
   int t0, len;
 };
 
@@ -47,7 +47,7 @@ __device__ __forceinline__ void read_codes(Codes<DP>& x, int i, const Source& fr
   const int t = from.t0 + cw * (KT / CODE_WARPS) + i * C::ROWS + row;
   x.w[i][0] = x.w[i][1] = x.w[i][2] = x.w[i][3] = x.s[i] = 0;
   if (t < from.len && 32 * piece < D) {
-    const uint8_t* p = from.codes + t * from.tok + 16 * piece;
+    const uint8_t* p = from.codes + (long long)t * from.tok + 16 * piece;
     if ((D & 31) == 0) {
       const uint4 y = ldg16(p);
       x.w[i][0] = y.x; x.w[i][1] = y.y; x.w[i][2] = y.z; x.w[i][3] = y.w;
@@ -59,7 +59,7 @@ __device__ __forceinline__ void read_codes(Codes<DP>& x, int i, const Source& fr
         x.w[i][2] = z.x; x.w[i][3] = z.y;
       }
     }
-    x.s[i] = __ldg(reinterpret_cast<const uint16_t*>(from.scales + t * from.stok + 2 * piece));
+    x.s[i] = __ldg(reinterpret_cast<const uint16_t*>(from.scales + (long long)t * from.stok + 2 * piece));
   }
 }
 template <int DP>

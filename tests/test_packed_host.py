@@ -71,7 +71,8 @@ def test_store_and_load_refuse(B):
                call(kt=_packed(d, codes=None)), call(vt=_packed(d, scales=None)), call(kt=_packed(d, FAKE + 8)),
                call(kt=_packed(d, scales=FAKE + 2)), call(kt=_packed(d, tok=d.Hkv * 32 + 8)),
                call(kt=_packed(d, scale_tok=0)), call(vt=_packed(d, head=16)), call(vt=_packed(d, scale_head=6)),
-               call(kt=_packed(d, seq=1 << 39)), call(kt=_packed(d, tok=-64))]
+               call(kt=_packed(d, seq=1 << 39)), call(kt=_packed(d, tok=-64)), call(kt=_packed(d, tok=1 << 32)),
+               call(vt=_packed(d, scale_tok=1 << 32))]
         assert bad == [B.ERR_INVALID_ARG] * len(bad), call.__name__
         assert call(d=_dims(B, Hkv=8, D=128), T=1 << 29, k=B.View(x.ptr, 1 << 37, 1024, 128),
                     v=B.View(y.ptr, 1 << 37, 1024, 128), kt=_packed(_dims(B, Hkv=8, D=128)),
