@@ -428,13 +428,14 @@ brisk_status brisk_cache_evict(const brisk_cache_dims *dims, const brisk_view *k
  *
  * The own caches of a batch are what fills memory and its bandwidth; held in 4 bits they take 3.6
  * times fewer bytes than in bf16. The prefix, held once for all sequences, stays as it is. A row (an
- * entry of a key head, D channels, D % 16 == 0) is held in groups of 16 channels: a group has a
+ * entry of a key head, D channels, D % 16 == 0) is held in groups of 16 channels. A group has a
  * scale, a byte with bits 14 to 7 of a positive fp16 number (5 bits of exponent, 3 of the
- * significand; 226, for 10240, is the largest, and larger bytes stand for it too), and a channel a
- * code of 4 bits (bit 3: sign; bits 0 to 2: which of 0, .5, 1, 1.5, 2, 3, 4, 6), two a byte, the even
- * channel in the low half. A channel's value is code times scale, which fp16, bf16 and fp32 hold
- * exactly. A row's codes are D/2 bytes, its scales 4 bytes (D <= 64) or 8, of which the first D/16
- * are in use. The paper has no counterpart. brisk_cache_dims as above, with 16 <= D <= 128 and
+ * significand), and a channel a code of 4 bits (bit 3: sign; bits 0 to 2: which of 0, .5, 1, 1.5, 2,
+ * 3, 4, 6), two a byte, the even channel in the low half. A channel's value is code times scale,
+ * which fp16, bf16 and fp32 hold exactly. The largest scale that is written is 226, for 10240;
+ * brisk_packed_load takes larger ones for it, and what they do to rows of attention that see them
+ * is not defined. A row's codes are D/2 bytes, its scales 4 bytes (D <= 64) or 8, of which the first
+ * D/16 are in use. The paper has no counterpart. brisk_cache_dims as above, with 16 <= D <= 128 and
  * D % 16 == 0. */
 
 /* A cache of such rows: codes of entry t of sequence s and key head h at codes + s * seq + t * tok +

@@ -60,17 +60,14 @@ __device__ __forceinline__ void from_codes(uint32_t w, uint32_t (&h)[4]) {
       "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
       "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
-// Two scales as fp16, at most SCALE_MAX whatever the bytes hold (the minimum takes a number before a NaN). Products, not
-// shifts: beside the conversions of codes, which take the units of integer logic two cycles each, those of
-// multiplication have room.
-__device__ __forceinline__ uint32_t scales_f16(uint32_t low, uint32_t high) {
+// Two scales as fp16, and one twice. Products, not shifts: beside the conversions of codes, which take the units of integer
+// logic two cycles each, those of multiplication have room.
+__device__ __forceinline__ uint32_t scales_plain(uint32_t low, uint32_t high) { return low * 0x80u + high * 0x800000u; }
+__device__ __forceinline__ uint32_t scale_plain(uint32_t byte) { return byte * 0x800080u; }
+// At most SCALE_MAX whatever the byte holds (the minimum takes a number before a NaN).
+__device__ __forceinline__ uint32_t scale_f16(uint32_t byte) {
   uint32_t r;
-  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(low * 0x80u + high * 0x800000u), "r"(0x71007100u));
-  return r;
-}
-__device__ __forceinline__ uint32_t scale_f16(uint32_t byte) {   // twice the same
-  uint32_t r;
-  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(byte * 0x800080u), "r"(0x71007100u));
+  asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(scale_plain(byte)), "r"(0x71007100u));
   return r;
 }
 __device__ __forceinline__ uint32_t mul_f16(uint32_t x, uint32_t y) {

@@ -17,8 +17,9 @@
 //
 // Keys and values come through a ring of a warp's own, in which its lanes copy 16 bytes at a time, a place of 32 keys
 // ahead, across the ends of fragments: nobody waits for another but where the parts of a head's warps meet.
-// Entries that a row does not see: scores are masked by selection, and every code and scale stands for a finite number
-// (see scales_f16), so that what is left in the ring or the cache cannot defeat a weight of 0.
+// Entries that a row does not see: scores are masked by selection, and the scales of the values of a step of which some
+// row does not see all are cut to ones that stand for numbers, so that what is left in the ring or the cache cannot
+// defeat a weight of 0.
 #include "packed.cuh"
 
 namespace brisk {
@@ -84,13 +85,9 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
 __device__ __forceinline__ float2 floats_of(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
 template <int N>
-__device__ __forceinline__ void copy_bytes(void* to, const void* from, bool there) {
-  if constexpr (N == 16)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(su32(to)),
-                 "l"(from), "r"((int)there) : "memory");
-  else
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %3;\n\t}" ::"r"(su32(to)),
-                 "l"(from), "r"((int)there), "n"(N) : "memory");
+__device__ __forceinline__ void copy_bytes(void* to, const void* from) {
+  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(su32(to)), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(su32(to)), "l"(from), "n"(N) : "memory");
 }
 
 // A lane's share of copying the codes and scales of STEP keys and values to a place of the ring: where from, of those that
@@ -118,29 +115,37 @@ struct Copies {
   }
   __device__ __forceinline__ void copy(const PackedArgs& p, uint8_t* to, int step) {
     const int lane = threadIdx.x & 31;
-    if ((p.a.D & 31) == 0) {
-      const int row = lane / P, piece = lane % P;
-      uint8_t* at = to + piece_at<DP>(row, piece);
-      const int end = 32 * piece < p.a.D ? left : 0;
+    if (p.a.D == DP && left >= STEP) {             // nothing to leave out
+      uint8_t* at = to + piece_at<DP>(lane / P, lane % P);
       constexpr int R = 32 / P;                    // rows at once; the next are 512 bytes further
 #pragma unroll
       for (int i = 0; i < STEP / R; ++i) {
-        copy_bytes<16>(at + 512 * i, ahead(k, R * i, p.k.tok), row + R * i < end);
-        copy_bytes<16>(at + 512 * i + VALUES, ahead(v, R * i, p.v.tok), row + R * i < end);
+        copy_bytes<16>(at + 512 * i, ahead(k, R * i, p.k.tok));
+        copy_bytes<16>(at + 512 * i + VALUES, ahead(v, R * i, p.v.tok));
       }
+      copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks);
+      copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs);
     } else {
-      constexpr int R = 16 / P;
-      const int row = lane / (2 * P), piece = lane % (2 * P);
-      const int end = 16 * piece < p.a.D ? left : 0;
+      const bool wide = (p.a.D & 31) == 0;
+      const int n = wide ? P : 2 * P, row = lane / n, piece = lane % n, bytes = wide ? 16 : 8;
 #pragma unroll 1
-      for (int i = 0; i < STEP / R; ++i) {
-        uint8_t* at = to + piece_at<DP>(row + R * i, piece >> 1) + 8 * (piece & 1);
-        copy_bytes<8>(at, ahead(k, R * i, p.k.tok), row + R * i < end);
-        copy_bytes<8>(at + VALUES, ahead(v, R * i, p.v.tok), row + R * i < end);
+      for (int r = row; r < STEP; r += 32 / n)
+        if (r < left && bytes * piece < p.a.D / 2) {
+          uint8_t* at = wide ? to + piece_at<DP>(r, piece) : to + piece_at<DP>(r, piece >> 1) + 8 * (piece & 1);
+          const uint8_t *kf = ahead(k, r - row, p.k.tok), *vf = ahead(v, r - row, p.v.tok);
+          if (wide) {
+            copy_bytes<16>(at, kf);
+            copy_bytes<16>(at + VALUES, vf);
+          } else {
+            copy_bytes<8>(at, kf);
+            copy_bytes<8>(at + VALUES, vf);
+          }
+        }
+      if (lane < left) {
+        copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks);
+        copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs);
       }
     }
-    copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks, lane < left);
-    copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs, lane < left);
     k = ahead(k, step, p.k.tok);
     v = ahead(v, step, p.v.tok);
     ks = ahead(ks, step, p.k.stok);
@@ -298,7 +303,7 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
       if (issued - used == STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
       else asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
-      const uint8_t* tile = ring + read;
+      uint8_t* tile = ring + read;
       read = read == (STAGES - 1) * T::BYTES ? 0 : read + T::BYTES;
       ++used;
 
@@ -320,7 +325,7 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
               wk[u][i][0] = y.x; wk[u][i][1] = y.y;
             }
 #pragma unroll
-            for (int j = 0; j < DP / 64; ++j) sk[u][i][j] = scale_f16(tile[at_ks + row * T::SROW + j]);
+            for (int j = 0; j < DP / 64; ++j) sk[u][i][j] = scale_plain(tile[at_ks + row * T::SROW + j]);
           }
 #pragma unroll
         for (int w = 0; w < W; ++w)
@@ -344,6 +349,11 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
           }
       }
       if (t0 + STEP > low) {
+        // (values that some row does not see: weights of 0 shall meet numbers, whatever the bytes)
+        uint32_t* vs = reinterpret_cast<uint32_t*>(tile + VALUES + T::CODES + lane * T::SROW);
+#pragma unroll
+        for (int i = 0; i < T::SROW / 4; ++i) vs[i] = __vminu4(vs[i], SCALE_TOP * 0x01010101u);
+        __syncwarp();
         const int key = t0 + key_of(g);
         int lim[2];
 #pragma unroll
@@ -417,8 +427,8 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
         get(at_v[1] + row, w1);
         get(at_v[0] + row8, w2);
         get(at_v[1] + row8, w3);
-        const uint32_t s0 = scales_f16(tile[at_vs[0] + srow], tile[at_vs[1] + srow]);
-        const uint32_t s1 = scales_f16(tile[at_vs[0] + srow8], tile[at_vs[1] + srow8]);
+        const uint32_t s0 = scales_plain(tile[at_vs[0] + srow], tile[at_vs[1] + srow]);
+        const uint32_t s1 = scales_plain(tile[at_vs[0] + srow8], tile[at_vs[1] + srow8]);
 #pragma unroll
         for (int w = 0; w < DP / 64; ++w) {        // a word: eight channels
           uint32_t ev[4], od[4], ev8[4], od8[4];   // even and odd channels of the keys' pairs
