@@ -1,8 +1,8 @@
 // Attention over own caches in 4 bits on the tensor cores of sm_103a, for many query rows a key head.
 //
 // As attend_slot_kernel (cache_attend_tc.cu), a slot of 128 query rows a CTA, two CTAs an SM, but the tiles of keys and
-// values are not copied: two warps read their codes, a tile ahead in registers, and write them as fp16, in which they
-// are exact, where the products take them from shared memory. The queries become fp16 too (both operands of a product
+// values are not copied: three warps each read their codes to registers and write them as fp16, in which they are
+// exact, where the products take them from shared memory. The queries become fp16 too (both operands of a product
 // have one type), each row scaled by a power of two so that its largest magnitude is 2^14 to 2^15: exact down to 2^-38
 // of it. Weights are fp16, taken relative to 2^-10 of the held maximum. Codes that a row does not see stand for
 // finite numbers, and rows of a tile behind the last entry are written as zeros.
@@ -13,8 +13,8 @@ namespace brisk {
 namespace {
 
 using Weight = WeightAs<__half>;
-constexpr int CODE_WARPS = 2;
-constexpr int THREADS = SLOT + 128;                // a planning and an issuing warp, and those that read codes
+constexpr int CODE_WARPS = 3;                      // that read the codes of keys, and as many for values
+constexpr int THREADS = SLOT + 64 + 64 * CODE_WARPS;   // a planning and an issuing warp, and those that read codes
 template <int DP>
 struct Shape4 {
   static constexpr int TILE = KT * DP * 2;
@@ -22,62 +22,70 @@ struct Shape4 {
   static constexpr int SMEM = 1024 + (1 + STAGES) * TILE + 4 * STAGE_BYTES;
 };
 
-// The part of a tile of codes that a warp reads: a lane has 16 bytes, 32 channels, of every eighth row (sixteenth, up to
-// 64 channels), so that eight neighbouring lanes write eight rows, whose pieces are swizzled into different banks.
+// The part of a tile of codes that a warp reads: a lane has 16 bytes, 32 channels, of a row of each group of 8 (16, up to
+// 64 channels), so that eight neighbouring lanes write eight rows, whose pieces are swizzled into different banks. Warp
+// w of the CODE_WARPS has groups w, w + CODE_WARPS, ...
 template <int DP>
 struct Codes {
-  static constexpr int PIECES = DP / 32, ROWS = 32 / PIECES, N = KT / CODE_WARPS / ROWS;
+  static constexpr int PIECES = DP / 32, ROWS = 32 / PIECES, GROUPS = KT / ROWS, N = (GROUPS + CODE_WARPS - 1) / CODE_WARPS;
+  static constexpr int STEP = CODE_WARPS * ROWS;   // rows between a lane's groups
   uint32_t w[N][4], s[N];
-};
-__device__ __forceinline__ uint4 ldg16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
-__device__ __forceinline__ uint2 ldg8(const uint8_t* p) { return __ldg(reinterpret_cast<const uint2*>(p)); }
+  const uint8_t *codes, *scales;                   // of the lane's first row of the next tile
+  int left;                                        // rows from that one on (none: channels that are not there)
+  static __device__ __forceinline__ int row() { return (threadIdx.x & 7) | (PIECES == 2 ? (threadIdx.x >> 1 & 8) : 0); }
+  static __device__ __forceinline__ int piece() { return PIECES == 2 ? threadIdx.x >> 3 & 1 : threadIdx.x >> 3 & 3; }
 
-// Where a tile's codes are: entries t0 .. of a head, `len` of them in use.
-struct Source {
-  const uint8_t *codes, *scales;
-  uint32_t tok, stok;
-  int t0, len;
-};
-
-template <int DP>
-__device__ __forceinline__ void read_codes(Codes<DP>& x, int i, const Source& from, int cw, int D) {
-  using C = Codes<DP>;
-  const int lane = threadIdx.x & 31;
-  const int row = (lane & 7) | (C::PIECES == 2 ? (lane >> 4) << 3 : 0), piece = C::PIECES == 2 ? (lane >> 3) & 1 : lane >> 3;
-  const int t = from.t0 + cw * (KT / CODE_WARPS) + i * C::ROWS + row;
-  x.w[i][0] = x.w[i][1] = x.w[i][2] = x.w[i][3] = x.s[i] = 0;
-  if (t < from.len && 32 * piece < D) {
-    const uint8_t* p = from.codes + (long long)t * from.tok + 16 * piece;
-    if ((D & 31) == 0) {
-      const uint4 y = ldg16(p);
-      x.w[i][0] = y.x; x.w[i][1] = y.y; x.w[i][2] = y.z; x.w[i][3] = y.w;
-    } else {                                       // rows start on 8 bytes
-      const uint2 y = ldg8(p);
-      x.w[i][0] = y.x; x.w[i][1] = y.y;
-      if (32 * piece + 16 < D) {
-        const uint2 z = ldg8(p + 8);
-        x.w[i][2] = z.x; x.w[i][3] = z.y;
+  __device__ __forceinline__ void begin(const PackedView& v, const Frag& f, int cw, int D) {
+    const int first = f.k0 * KT + cw * ROWS + row();
+    codes = v.codes + f.b * v.seq + f.h * v.head + (unsigned long long)(uint32_t)first * v.tok + 16 * piece();
+    scales = v.scales + f.b * v.sseq + f.h * v.shead + (unsigned long long)(uint32_t)first * v.stok + 2 * piece();
+    left = 32 * piece() < D ? f.len - first : -(1 << 30);
+  }
+  // (zeros where there is nothing to read)
+  __device__ __forceinline__ void read(uint32_t tok, uint32_t stok, int cw, int D) {
+    const bool wide = (D & 31) == 0, full = 32 * piece() + 16 < D;   // (else rows start on 8 bytes)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0;
+      s[i] = 0;
+      if (STEP * i < left && (i + 1 < N || cw + i * CODE_WARPS < GROUPS)) {
+        const uint8_t* p = codes + (unsigned long long)(STEP * i) * tok;
+        if (wide) {
+          const uint4 z = __ldg(reinterpret_cast<const uint4*>(p));
+          w[i][0] = z.x; w[i][1] = z.y; w[i][2] = z.z; w[i][3] = z.w;
+        } else {
+          const uint2 z = __ldg(reinterpret_cast<const uint2*>(p));
+          w[i][0] = z.x; w[i][1] = z.y;
+          if (full) {
+            const uint2 z8 = __ldg(reinterpret_cast<const uint2*>(p + 8));
+            w[i][2] = z8.x; w[i][3] = z8.y;
+          }
+        }
+        s[i] = __ldg(reinterpret_cast<const uint16_t*>(scales + (unsigned long long)(STEP * i) * stok));
       }
     }
-    x.s[i] = __ldg(reinterpret_cast<const uint16_t*>(from.scales + (long long)t * from.stok + 2 * piece));
+    codes += (unsigned long long)KT * tok;
+    scales += (unsigned long long)KT * stok;
+    left -= KT;
   }
-}
-template <int DP>
-__device__ __forceinline__ void write_values(const Codes<DP>& x, int i, uint8_t* tile, int cw) {
-  using C = Codes<DP>;
-  const int lane = threadIdx.x & 31;
-  const int row = (lane & 7) | (C::PIECES == 2 ? (lane >> 4) << 3 : 0), piece = C::PIECES == 2 ? (lane >> 3) & 1 : lane >> 3;
-  const uint32_t s[2] = {scale_f16(x.s[i] & 255), scale_f16(x.s[i] >> 8)};
-  uint8_t* to = tile + (piece >> 1) * PANEL + (cw * (KT / CODE_WARPS) + i * C::ROWS + row) * 128;
+  __device__ __forceinline__ void write(uint8_t* tile, int cw) const {
+    uint8_t* to = tile + (piece() >> 1) * PANEL + (cw * ROWS + row()) * 128;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint32_t h[4];
-    from_codes(x.w[i][k], h);
+    for (int i = 0; i < N; ++i) {
+      if (i + 1 == N && cw + i * CODE_WARPS >= GROUPS) break;
+      const uint32_t by[2] = {scale_f16(s[i] & 255), scale_f16(s[i] >> 8)};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) h[j] = mul_f16(h[j], s[k >> 1]);
-    *reinterpret_cast<uint4*>(to + ((((piece & 1) * 4 + k) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+      for (int k = 0; k < 4; ++k) {
+        uint32_t h[4];
+        from_codes(w[i][k], h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = mul_f16(h[j], by[k >> 1]);
+        *reinterpret_cast<uint4*>(to + STEP * i * 128 + ((((piece() & 1) * 4 + k) ^ (row() & 7)) << 4)) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+      }
+    }
   }
-}
+};
 
 // A row of queries, as fetch_queries left it, becomes fp16 in its place; what its scores are to be multiplied by.
 template <int DP>
@@ -109,35 +117,28 @@ __device__ __forceinline__ float scale_query(uint8_t* tile, int row, int D, floa
   return query_scale(sl2, up);
 }
 
-// row_weights (see there) in the registers that 256 threads of two CTAs leave: half the scores stay, the others are read
-// from TMEM twice.
+// row_weights (see there) in the registers that 384 threads of two CTAs leave: scores are read from TMEM twice, 32 at a
+// time, for their maximum and for their weights.
 template <typename Half>
-__device__ __forceinline__ void row_weights_by_halves(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m,
-                                                      float& l, Half half) {
-  float v[64];
-  tmem_ld64(tS, v);
+__device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m,
+                                                     float& l, Half half) {
   const bool hides = __any_sync(FULL_MASK, seen < KT);
-  auto hide = [&](float* x, int n, int c0) {
+  auto scores = [&](float (&x)[32], int c0) {
+    tmem_ld32(tS + c0, x);
     if (hides) {
 #pragma unroll
-      for (int c = 0; c < n; ++c) x[c] = c0 + c < seen ? x[c] : -INFINITY;
+      for (int c = 0; c < 32; ++c) x[c] = c0 + c < seen ? x[c] : -INFINITY;
     }
   };
-  hide(v, 64, 0);
-  float top[4] = {v[0], v[1], v[2], v[3]};
+  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-  for (int c = 4; c < 64; c += 4)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], v[c + i]);
-#pragma unroll
-  for (int c0 = 64; c0 < KT; c0 += 32) {
+  for (int c0 = 0; c0 < KT; c0 += 32) {
     float x[32];
-    tmem_ld32(tS + c0, x);
-    hide(x, 32, c0);
+    scores(x, c0);
 #pragma unroll
-    for (int c = 0; c < 32; c += 4)
+    for (int c = 0; c < 32; c += 8)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], x[c + i]);
+      for (int i = 0; i < 4; ++i) top[i] = fmaxf(fmaxf(top[i], x[c + i]), x[c + 4 + i]);
   }
   const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
   const bool over = t > m + Weight::LAZY;
@@ -159,7 +160,10 @@ __device__ __forceinline__ void row_weights_by_halves(uint32_t tS, uint32_t tO, 
   const float ms = m == -INFINITY ? 0.f : m - Weight::SHIFT;
   const f32x2 scale2 = pack2(sl2, sl2), minus2 = pack2(-ms, -ms);
   f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
-  auto weigh = [&](const float* s, int c0) {       // 32 columns
+#pragma unroll
+  for (int c0 = 0; c0 < KT; c0 += 32) {
+    float s[32];
+    scores(s, c0);
     uint32_t p[16];
 #pragma unroll
     for (int c = 0; c < 32; c += 4) {
@@ -174,17 +178,10 @@ __device__ __forceinline__ void row_weights_by_halves(uint32_t tS, uint32_t tO, 
       p[c / 2 + 1] = Weight::pair(x[2], x[3]);
     }
     tmem_st16(tS + c0 / 2, p);
-  };
-  weigh(v, 0);
-  weigh(v + 32, 32);
-  tmem_st_wait();
-  half();
-#pragma unroll
-  for (int c0 = 64; c0 < KT; c0 += 32) {
-    float x[32];
-    tmem_ld32(tS + c0, x);
-    hide(x, 32, c0);
-    weigh(x, c0);
+    if (c0 + 32 == KT / 2) {
+      tmem_st_wait();
+      half();
+    }
   }
   float x[2];
   unpack2(add2(sum0, sum1), x[0], x[1]);
@@ -218,7 +215,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
     for (int s = 0; s < 2; ++s) mbar_init(&p_ready[s], 4);   // the slot's warps, for either half of the keys
     for (int s = 0; s < 4; ++s) {
       mbar_init(&info_full[s], 1);
-      mbar_init(&info_empty[s], 4 + CODE_WARPS);
+      mbar_init(&info_empty[s], 4 + 2 * CODE_WARPS);
     }
     mbar_init(&s_full, 1);
     mbar_init(&o_full, 1);
@@ -309,59 +306,33 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       if (elect_one()) umma_commit(&done);
       mbar_drain(&done, 0);
     } else if (some) {
-      // codes to fp16: keys and values of a tile in turn, those of the next one on their way meanwhile
-      const int cw = warp - 6;
-      constexpr int N = Codes<DP>::N;
+      // codes to fp16, keys or values, those of the next tile on their way while this one's place is waited for
+      const int value = warp - 6 >= CODE_WARPS, cw = warp - 6 - value * CODE_WARPS;
       Codes<DP> x;
-      Source from{};
-      int j = 0, n = 0, k0 = 0, b = 0, h = 0, value = 1, last = 0;   // of the tile that is read
-      auto next = [&]() {                          // the next tile; false: there is none, or a wait gave up
-        if (!value) {
-          value = 1;
-          from.codes = p.v.codes + b * p.v.seq + h * p.v.head;
-          from.scales = p.v.scales + b * p.v.sseq + h * p.v.shead;
-          from.tok = p.v.tok;
-          from.stok = p.v.stok;
-          return true;
-        }
-        if (++j >= n) {
-          if (last) return false;
-          off = wait(&info_full[nf & 3], nf >> 2);
-          if (off) return false;
-          const Frag& f = info[nf & 3];
-          n = f.n; k0 = f.k0; b = f.b; h = f.h; last = f.last;
-          from.len = f.len;
-          j = 0;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&info_empty[nf & 3]);
-          ++nf;
-        }
-        value = 0;
-        from.t0 = (k0 + j) * KT;
-        from.codes = p.k.codes + b * p.k.seq + h * p.k.head;
-        from.scales = p.k.scales + b * p.k.sseq + h * p.k.shead;
-        from.tok = p.k.tok;
-        from.stok = p.k.stok;
-        return true;
-      };
-      bool more = next();
-      if (more)
-#pragma unroll
-        for (int i = 0; i < N; ++i) read_codes<DP>(x, i, from, cw, a.D);
-      for (unsigned cur = 0; more; ++cur) {
-        const unsigned st = cur % STAGES;
-        more = next();
+      unsigned cur = value;
+      for (int last = 0; !last && !off;) {
+        off = wait(&info_full[nf & 3], nf >> 2);
         if (off) break;
-        off = cur >= STAGES && wait(&empty[st], cur / STAGES - 1);
-        if (off) break;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          write_values<DP>(x, i, ring + st * TILE, cw);
-          if (more) read_codes<DP>(x, i, from, cw, a.D);
-        }
-        fence_async_smem();
+        const Frag& f = info[nf & 3];
+        const int n = f.n;
+        last = f.last;
+        if (value) x.begin(p.v, f, cw, a.D);
+        else x.begin(p.k, f, cw, a.D);
         __syncwarp();
-        if (lane == 0) mbar_arrive(&full[st]);
+        if (lane == 0) mbar_arrive(&info_empty[nf & 3]);
+        ++nf;
+#pragma unroll 1
+        for (int j = 0; j < n; ++j, cur += 2) {
+          // (behind the last tile's fence, which waits for what is on its way to registers, too)
+          x.read(value ? p.v.tok : p.k.tok, value ? p.v.stok : p.k.stok, cw, a.D);
+          const unsigned st = cur % STAGES;
+          off = cur >= STAGES && wait(&empty[st], cur / STAGES - 1);
+          if (off) break;
+          x.write(ring + st * TILE, cw);
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full[st]);
+        }
       }
     }
   } else {
@@ -369,18 +340,19 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
     const uint32_t tS = tmem + lanes, tO = tmem + 128 + lanes;
     // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
     // this one's are there), this one's end. The first turn has no fragment yet, the last no next one.
-    Row y{-1, 0, nullptr};
+    // (of a fragment's words only those that every tile wants stay in registers)
+    int y_id = -1, y_lim = 0;                      // this fragment's row of the thread: see Row
     float y_scale = 0.f;
-    Frag f{};
     bool have = false, next = some;
     for (;; ++nf) {                                // this fragment is number nf - 1
+      const Frag& f = info[(nf - 1) & 3];
       Row x{-1, 0, nullptr};
       if (next) {
         off = wait(&info_full[nf & 3], nf >> 2);
         if (off) break;
         x = find_row(a, info[nf & 3], tid);
       }
-      const bool mine = have && tid < f.rows, live = __any_sync(FULL_MASK, mine);
+      const bool live = __any_sync(FULL_MASK, have && tid < f.rows);
       float m = -INFINITY, l = 0.f;
       if (have) {
         auto ready = [&](int half) {
@@ -388,12 +360,12 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
           __syncwarp();
           if (lane == 0) mbar_arrive(&p_ready[half]);
         };
-        for (int j = 0; j < f.n; ++j, ++unit) {
+        int seen = tid < f.rows ? y_lim - f.k0 * KT : 0x3fffffff;
+        for (int j = f.n; j > 0; --j, ++unit, seen -= KT) {
           off = wait(&s_full, unit);
           if (off) break;
           tc_fence_after();
-          if (live)
-            row_weights_by_halves(tS, tO, a.D, mine ? y.lim - (f.k0 + j) * KT : KT, y_scale, j == 0, m, l, [&]() { ready(0); });
+          if (live) row_weights_by_parts(tS, tO, a.D, seen, y_scale, j == f.n, m, l, [&]() { ready(0); });
           else ready(0);
           ready(1);
         }
@@ -419,7 +391,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
         if (live) {
           const int per = min(SLOT, plan.LG);
           float* part = f.whole ? nullptr : a.part_o + part_at(f.slot, per, a.D, tid, 0);
-          store_rows<false>(a, tO, y, mine, m == -INFINITY ? m : m - Weight::SHIFT, l, part,
+          store_rows<false>(a, tO, Row{y_id, y_lim, nullptr}, tid < f.rows, m == -INFINITY ? m : m - Weight::SHIFT, l, part,
                             a.ml_o + (long long)f.slot * per + tid, per, stage + warp * STAGE_BYTES, Parts{});
         }
         tc_fence_before();
@@ -429,11 +401,11 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       if (!next) break;
       off = wait(&q_full, nf);
       if (off) break;
-      f = info[nf & 3];
-      y = x;
+      y_id = x.id;
+      y_lim = x.lim;
       y_scale = x_scale;
       have = true;
-      next = !f.last;
+      next = !info[nf & 3].last;
     }
     rows_fetched();                                // (queries, where a wait gave up)
   }
