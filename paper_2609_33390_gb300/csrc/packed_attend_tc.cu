@@ -2,7 +2,8 @@
 //
 // As attend_slot_kernel (cache_attend_tc.cu), a slot of 128 query rows a CTA, two CTAs an SM, but the tiles of keys and
 // values are not copied: three warps each read their codes to registers and write them as fp16, in which they are
-// exact, where the products take them from shared memory. The queries become fp16 too (both operands of a product
+// exact, where the products take them from shared memory. Scores are taken 64 keys at a time, in two places of TMEM, so
+// that the tensor cores work on the next while a slot's threads take exponentials. The queries become fp16 too (both operands of a product
 // have one type), each row scaled by a power of two so that its largest magnitude is 2^14 to 2^15: exact down to 2^-38
 // of it. Weights are fp16, taken relative to 2^-10 of the held maximum. Codes that a row does not see stand for
 // finite numbers, and rows of a tile behind the last entry are written as zeros.
@@ -117,12 +118,14 @@ __device__ __forceinline__ float scale_query(uint8_t* tile, int row, int D, floa
   return query_scale(sl2, up);
 }
 
-// row_weights (see there) in the registers that 384 threads of two CTAs leave: scores are read from TMEM twice, 32 at a
-// time, for their maximum and for their weights.
-template <typename Half>
+// row_weights (see there) of HALF keys in the registers that 384 threads of two CTAs leave: scores are read from TMEM
+// twice, 32 at a time, for their maximum and for their weights. before(): waits until nothing is on its way to O (false: in
+// vain).
+constexpr int HALF = 64;
+template <typename Before>
 __device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m,
-                                                     float& l, Half half) {
-  const bool hides = __any_sync(FULL_MASK, seen < KT);
+                                                     float& l, Before before) {
+  const bool hides = __any_sync(FULL_MASK, seen < HALF);
   auto scores = [&](float (&x)[32], int c0) {
     tmem_ld32(tS + c0, x);
     if (hides) {
@@ -132,7 +135,7 @@ __device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, i
   };
   float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-  for (int c0 = 0; c0 < KT; c0 += 32) {
+  for (int c0 = 0; c0 < HALF; c0 += 32) {
     float x[32];
     scores(x, c0);
 #pragma unroll
@@ -146,7 +149,7 @@ __device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, i
     const float alpha = over ? ex2(m - t) : 1.f;   // (t is no -inf)
     if (over) m = t;
     l *= alpha;
-    if (!first)
+    if (!first && before())
 #pragma unroll 1
       for (int c = 0; c < D; c += 16) {
         float o[16];
@@ -161,7 +164,7 @@ __device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, i
   const f32x2 scale2 = pack2(sl2, sl2), minus2 = pack2(-ms, -ms);
   f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-  for (int c0 = 0; c0 < KT; c0 += 32) {
+  for (int c0 = 0; c0 < HALF; c0 += 32) {
     float s[32];
     scores(s, c0);
     uint32_t p[16];
@@ -178,15 +181,29 @@ __device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, i
       p[c / 2 + 1] = Weight::pair(x[2], x[3]);
     }
     tmem_st16(tS + c0 / 2, p);
-    if (c0 + 32 == KT / 2) {
-      tmem_st_wait();
-      half();
-    }
   }
   float x[2];
   unpack2(add2(sum0, sum1), x[0], x[1]);
   l += x[0] + x[1];
   tmem_st_wait();
+}
+
+// The halves of a fragment's tiles that have entries.
+__device__ __forceinline__ int halves_of(const Frag& f) { return (min(f.len - f.k0 * KT, f.n * KT) + HALF - 1) / HALF; }
+
+// The products of a slot with a half of a tile: scores, and values for `steps` <= 4 steps of 16 keys.
+template <int DP>
+__device__ __forceinline__ void issue_half_scores(uint32_t tS, uint32_t q_lo, uint32_t k_lo, int nd, uint32_t idesc) {
+#pragma unroll
+  for (int kk = 0; kk < DP / 16; ++kk) {
+    const uint32_t o = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
+    if (kk < nd) umma(tS, sw128(q_lo + o), sw128(k_lo + o), idesc, kk > 0);
+  }
+}
+__device__ __forceinline__ void issue_half_values(uint32_t tO, uint32_t tP, uint32_t v_lo, int steps, uint32_t idesc, bool begun) {
+#pragma unroll
+  for (int kk = 0; kk < HALF / 16; ++kk)
+    if (kk < steps) umma_ts(tO, tP + 8 * kk, sw128(v_lo + kk * 128), idesc, begun || kk > 0);
 }
 
 template <int DP>
@@ -197,7 +214,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t *ring = sQ + TILE, *stage = ring + STAGES * TILE;
-  __shared__ uint64_t full[STAGES], empty[STAGES], s_full, p_ready[2], o_full, q_full, info_full[4], info_empty[4], done;
+  __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2], v_done[2], o_full, q_full, info_full[4], info_empty[4], done;
   __shared__ Frag info[4];
   __shared__ uint32_t tmem_slot;
   __shared__ Start start;
@@ -212,12 +229,15 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       mbar_init(&full[s], CODE_WARPS);
       mbar_init(&empty[s], 1);
     }
-    for (int s = 0; s < 2; ++s) mbar_init(&p_ready[s], 4);   // the slot's warps, for either half of the keys
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&s_full[s], 1);
+      mbar_init(&p_ready[s], 4);                   // the slot's warps
+      mbar_init(&v_done[s], 1);
+    }
     for (int s = 0; s < 4; ++s) {
       mbar_init(&info_full[s], 1);
       mbar_init(&info_empty[s], 4 + 2 * CODE_WARPS);
     }
-    mbar_init(&s_full, 1);
     mbar_init(&o_full, 1);
     mbar_init(&q_full, 4);
     mbar_init(&done, 1);
@@ -226,7 +246,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
-  if (warp == 0) tmem_alloc(&tmem_slot, 256);      // S | O
+  if (warp == 0) tmem_alloc(&tmem_slot, 256);      // S of two halves | O
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -245,7 +265,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
   __syncthreads();
   const bool some = walk.u < walk.end;
   __syncthreads();                                 // (before it moves)
-  int unit = 0, nf = 0;                            // tiles and fragments before
+  int half = 0, nf = 0;                            // halves of tiles and fragments before
   bool off = false;
 
   if (warp >= 4) {
@@ -263,45 +283,50 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       }
     } else if (warp == 5) {
       const int nd = a.D / 16;                     // steps of 16 columns of Q K^T, and units of O's width
-      const uint32_t id_s = idesc_f16(SLOT, KT), id_o = idesc_f16(SLOT, 16 * nd) | IDESC_B_MN;
+      const uint32_t id_s = idesc_f16(SLOT, HALF), id_o = idesc_f16(SLOT, 16 * nd) | IDESC_B_MN;
       const uint32_t q = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
-      const uint32_t tS = tmem, tO = tmem + 128;
-      unsigned cur = 0;
+      constexpr uint32_t ROWS = HALF * 128 >> 4;   // the second half's rows of a tile
+      unsigned tile = 0;                           // before this fragment
       for (bool more = some; more && !off;) {
         const int fs = nf & 3;
         off = wait(&q_full, nf++);                 // (info_full came before it)
         if (off) break;
-        const int n = info[fs].n, k0 = info[fs].k0, len = info[fs].len;
+        const int n = halves_of(info[fs]), tiles = info[fs].n, len = info[fs].len - info[fs].k0 * KT;
         more = !info[fs].last;
-        for (int j = 0; j < n && !off; ++j, ++unit) {
-          const unsigned sk = cur % STAGES, sv = (cur + 1) % STAGES;
-          off = wait(&full[sk], cur / STAGES);
+        // The scores of a half come two halves ahead of its values: while the slot's threads take one half's weights, the
+        // products with the values of the one before and the scores of the one behind run.
+        auto scores = [&](int h) {
+          const unsigned st = 2 * (tile + (h >> 1)) % STAGES;
+          if (!(h & 1)) off = wait(&full[st], 2 * (tile + (h >> 1)) / STAGES);
+          if (off) return;
+          tc_fence_after();
+          if (elect_one()) {
+            issue_half_scores<DP>(tmem + ((half + h) & 1) * HALF, q, k_lo + st * (TILE >> 4) + (h & 1) * ROWS, nd, id_s);
+            umma_commit(&s_full[(half + h) & 1]);
+            if ((h & 1) || h + 1 == n) umma_commit(&empty[st]);
+          }
+          __syncwarp();
+        };
+        scores(0);
+        if (n > 1 && !off) scores(1);
+        for (int h = 0; h < n && !off; ++h) {
+          const unsigned cur = 2 * (tile + (h >> 1)) + 1, st = cur % STAGES;
+          if (!(h & 1)) off = wait(&full[st], cur / STAGES);
+          off = off || wait(&p_ready[(half + h) & 1], (half + h) >> 1);
           if (off) break;
           tc_fence_after();
           if (elect_one()) {
-            issue_scores<DP>(tS, q, k_lo + sk * (TILE >> 4), nd, id_s);
-            umma_commit(&s_full);
-            umma_commit(&empty[sk]);
+            issue_half_values(tmem + 2 * HALF, tmem + ((half + h) & 1) * HALF, v_lo + st * (TILE >> 4) + (h & 1) * ROWS,
+                              (len - h * HALF + 15) / 16, id_o, h > 0);
+            umma_commit(&v_done[(half + h) & 1]);
+            if ((h & 1) || h + 1 == n) umma_commit(&empty[st]);
+            if (h + 1 == n) umma_commit(&o_full);
           }
           __syncwarp();
-          const uint32_t v = v_lo + sv * (TILE >> 4);
-          const int steps = (len - (k0 + j) * KT + 15) / 16;
-          off = wait(&full[sv], (cur + 1) / STAGES) || wait(&p_ready[0], unit);
-          if (off) break;
-          tc_fence_after();
-          if (elect_one()) issue_values<0>(tO, tS, v, steps, id_o, j > 0);
-          __syncwarp();
-          off = wait(&p_ready[1], unit);
-          if (off) break;
-          tc_fence_after();
-          if (elect_one()) {
-            issue_values<1>(tO, tS, v, steps, id_o, true);
-            umma_commit(&empty[sv]);
-            if (j + 1 == n) umma_commit(&o_full);
-          }
-          __syncwarp();
-          cur += 2;
+          if (h + 2 < n) scores(h + 2);
         }
+        half += n;
+        tile += tiles;
       }
       if (elect_one()) umma_commit(&done);
       mbar_drain(&done, 0);
@@ -337,7 +362,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
     }
   } else {
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
-    const uint32_t tS = tmem + lanes, tO = tmem + 128 + lanes;
+    const uint32_t tO = tmem + 2 * HALF + lanes;
     // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
     // this one's are there), this one's end. The first turn has no fragment yet, the last no next one.
     // (of a fragment's words only those that every tile wants stay in registers)
@@ -352,30 +377,33 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
         if (off) break;
         x = find_row(a, info[nf & 3], tid);
       }
-      const bool live = __any_sync(FULL_MASK, have && tid < f.rows);
+      const bool live = __any_sync(FULL_MASK, have && tid < f.rows);   // (rows of this fragment)
       float m = -INFINITY, l = 0.f;
       if (have) {
-        auto ready = [&](int half) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&p_ready[half]);
-        };
         int seen = tid < f.rows ? y_lim - f.k0 * KT : 0x3fffffff;
-        for (int j = f.n; j > 0; --j, ++unit, seen -= KT) {
-          off = wait(&s_full, unit);
+        const int n = halves_of(f);
+        for (int h = 0; h < n; ++h, ++half, seen -= HALF) {
+          off = wait(&s_full[half & 1], half >> 1);
           if (off) break;
           tc_fence_after();
-          if (live) row_weights_by_parts(tS, tO, a.D, seen, y_scale, j == f.n, m, l, [&]() { ready(0); });
-          else ready(0);
-          ready(1);
+          // (the last scores that read this fragment's queries are there)
+          if (h + 1 == n && next) fetch_queries<DP>(x.q, a.D, sQ, 32 * warp);
+          if (live)
+            row_weights_by_parts(tmem + (half & 1) * HALF + lanes, tO, a.D, seen, y_scale, h == 0, m, l, [&]() {
+              // (the half before's products; the ones before them came before these scores. A phase that no one may have
+              // waited for: the next of this barrier comes after this half's weights.)
+              off = wait(&v_done[(half - 1) & 1], (half - 1) >> 1);
+              tc_fence_after();
+              return !off;
+            });
+          if (off) break;
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_ready[half & 1]);
         }
         if (off) break;
-      }
-      if (next) fetch_queries<DP>(x.q, a.D, sQ, 32 * warp);
-      if (have) {
-        off = wait(&o_full, nf - 1);
-        if (off) break;
-        tc_fence_after();
+      } else if (next) {
+        fetch_queries<DP>(x.q, a.D, sQ, 32 * warp);
       }
       float x_scale = 0.f;
       if (next) {
@@ -388,6 +416,9 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
         if (lane == 0) mbar_arrive(&q_full);
       }
       if (have) {
+        off = wait(&o_full, nf - 1);
+        if (off) break;
+        tc_fence_after();
         if (live) {
           const int per = min(SLOT, plan.LG);
           float* part = f.whole ? nullptr : a.part_o + part_at(f.slot, per, a.D, tid, 0);
