@@ -2,11 +2,12 @@
 //
 // As attend_slot_kernel (cache_attend_tc.cu), a slot of 128 query rows a CTA, two CTAs an SM, but the tiles of keys and
 // values are not copied: three warps each read their codes to registers and write them as fp16, in which they are
-// exact, where the products take them from shared memory. Scores are taken 64 keys at a time, in two places of TMEM, so
-// that the tensor cores work on the next while a slot's threads take exponentials. The queries become fp16 too (both operands of a product
+// exact, where the products take them from shared memory. The queries become fp16 too (both operands of a product
 // have one type), each row scaled by a power of two so that its largest magnitude is 2^14 to 2^15: exact down to 2^-38
-// of it. Weights are fp16, taken relative to 2^-10 of the held maximum. Codes that a row does not see stand for
-// finite numbers, and rows of a tile behind the last entry are written as zeros.
+// of it. (Keys as bf16 instead cost more, in every tile, than the queries' change once a fragment: 217 and 197 us, 128
+// blocks.) Weights are fp16, taken relative to 2^-10 of the held maximum. Scores are taken 64 keys at a time, in two
+// places of TMEM, so that the tensor cores work on the next while a slot's threads take exponentials. Codes that a row
+// does not see stand for finite numbers, and rows of a tile behind the last entry are written as zeros.
 #include "attend_tc.cuh"
 #include "packed.cuh"
 
@@ -88,61 +89,59 @@ struct Codes {
   }
 };
 
-// A row of queries, as fetch_queries left it, becomes fp16 in its place; what its scores are to be multiplied by.
+// A row of queries, as fetch_queries left it, becomes fp16 in its place; what its scores are to be multiplied by. (The
+// row is read at once: one piece after the other took 6000 cycles, a tenth of the kernel's time.)
 template <int DP>
 __device__ __forceinline__ float scale_query(uint8_t* tile, int row, int D, float sl2) {
   uint8_t* at = tile + row * 128;
-  uint32_t top = 0;
+  uint32_t x[DP / 8][4];
 #pragma unroll
-  for (int c = 0; c < DP / 8; ++c)
-    if (8 * c < D) {
-      const uint4 x = *reinterpret_cast<const uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4));
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  for (int c = 0; c < DP / 8; ++c) {
+    const uint4 y = *reinterpret_cast<const uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4));
+    x[c][0] = y.x; x[c][1] = y.y; x[c][2] = y.z; x[c][3] = y.w;
+  }
+  uint32_t top = 0;                                // of both halves' 16 bits: magnitudes compare as their bits do
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
+  for (int c = 0; c < DP / 8; ++c) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = __vmaxu2(t, x[c][i] & 0x7fff7fffu);
+    top = 8 * c < D ? __vmaxu2(top, t) : top;      // (behind the row's end there may be anything)
+  }
+  const int up = query_shift(max(top << 16, top & 0xffff0000u));
+  const f32x2 by = pack2(exp2_of(up), exp2_of(up));
+#pragma unroll
+  for (int c = 0; c < DP / 8; ++c) {
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      unpack2(mul2(pack2(__uint_as_float(x[c][i] << 16), __uint_as_float(x[c][i] & 0xffff0000u)), by), lo, hi);
+      y[i] = Weight::pair(lo, hi);
     }
-  const int up = query_shift(top);
-  const float by = exp2_of(up);
-#pragma unroll
-  for (int c = 0; c < DP / 8; ++c)
-    if (8 * c < D) {
-      uint4* p = reinterpret_cast<uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4));
-      const uint4 x = *p;
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-      uint32_t y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        y[i] = Weight::pair(__uint_as_float(w[i] << 16) * by, __uint_as_float(w[i] & 0xffff0000u) * by);
-      *p = make_uint4(y[0], y[1], y[2], y[3]);
-    }
+    *reinterpret_cast<uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+  }
   return query_scale(sl2, up);
 }
 
-// row_weights (see there) of HALF keys in the registers that 384 threads of two CTAs leave: scores are read from TMEM
-// twice, 32 at a time, for their maximum and for their weights. before(): waits until nothing is on its way to O (false: in
-// vain).
+// row_weights (see there) of HALF keys. before(): waits until nothing is on its way to O (false: in vain).
 constexpr int HALF = 64;
 template <typename Before>
-__device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m,
-                                                     float& l, Before before) {
-  const bool hides = __any_sync(FULL_MASK, seen < HALF);
-  auto scores = [&](float (&x)[32], int c0) {
-    tmem_ld32(tS + c0, x);
-    if (hides) {
+__device__ __forceinline__ void half_weights(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m, float& l,
+                                             Before before) {
+  float s[HALF];
+  tmem_ld64(tS, s);
+  if (__any_sync(FULL_MASK, seen < HALF)) {
 #pragma unroll
-      for (int c = 0; c < 32; ++c) x[c] = c0 + c < seen ? x[c] : -INFINITY;
-    }
-  };
-  float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-  for (int c0 = 0; c0 < HALF; c0 += 32) {
-    float x[32];
-    scores(x, c0);
-#pragma unroll
-    for (int c = 0; c < 32; c += 8)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top[i] = fmaxf(fmaxf(top[i], x[c + i]), x[c + 4 + i]);
+    for (int c = 0; c < HALF; ++c) s[c] = c < seen ? s[c] : -INFINITY;
   }
+  float top[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+  for (int c = 4; c + 8 <= HALF; c += 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top[i] = fmaxf(fmaxf(top[i], s[c + i]), s[c + 4 + i]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], s[HALF - 4 + i]);
   const float t = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
   const bool over = t > m + Weight::LAZY;
   if (__any_sync(FULL_MASK, over)) {
@@ -165,14 +164,12 @@ __device__ __forceinline__ void row_weights_by_parts(uint32_t tS, uint32_t tO, i
   f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
   for (int c0 = 0; c0 < HALF; c0 += 32) {
-    float s[32];
-    scores(s, c0);
     uint32_t p[16];
 #pragma unroll
     for (int c = 0; c < 32; c += 4) {
       float x[4];
-      unpack2(fma2(pack2(s[c], s[c + 1]), scale2, minus2), x[0], x[1]);
-      unpack2(fma2(pack2(s[c + 2], s[c + 3]), scale2, minus2), x[2], x[3]);
+      unpack2(fma2(pack2(s[c0 + c], s[c0 + c + 1]), scale2, minus2), x[0], x[1]);
+      unpack2(fma2(pack2(s[c0 + c + 2], s[c0 + c + 3]), scale2, minus2), x[2], x[3]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = ex2(x[i]);
       sum0 = add2(sum0, pack2(x[0], x[1]));
@@ -268,7 +265,9 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
   int half = 0, nf = 0;                            // halves of tiles and fragments before
   bool off = false;
 
+  // (384 threads of 80 registers: 128 x 112 and 256 x 64)
   if (warp >= 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 4) {
       // the fragments, each published while the one before is worked on
       for (bool more = some; more && !off; ++nf) {
@@ -361,13 +360,14 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     const uint32_t tO = tmem + 2 * HALF + lanes;
     // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
     // this one's are there), this one's end. The first turn has no fragment yet, the last no next one.
     // (of a fragment's words only those that every tile wants stay in registers)
     int y_id = -1, y_lim = 0;                      // this fragment's row of the thread: see Row
-    float y_scale = 0.f;
+    float y_scale = 0.f;                           // what its scores are multiplied by
     bool have = false, next = some;
     for (;; ++nf) {                                // this fragment is number nf - 1
       const Frag& f = info[(nf - 1) & 3];
@@ -389,7 +389,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
           // (the last scores that read this fragment's queries are there)
           if (h + 1 == n && next) fetch_queries<DP>(x.q, a.D, sQ, 32 * warp);
           if (live)
-            row_weights_by_parts(tmem + (half & 1) * HALF + lanes, tO, a.D, seen, y_scale, h == 0, m, l, [&]() {
+            half_weights(tmem + (half & 1) * HALF + lanes, tO, a.D, seen, y_scale, h == 0, m, l, [&]() {
               // (the half before's products; the ones before them came before these scores. A phase that no one may have
               // waited for: the next of this barrier comes after this half's weights.)
               off = wait(&v_done[(half - 1) & 1], (half - 1) >> 1);
