@@ -17,11 +17,13 @@ namespace {
 using Weight = WeightAs<__half>;
 constexpr int CODE_WARPS = 3;                      // that read the codes of keys, and as many for values
 constexpr int THREADS = SLOT + 64 + 64 * CODE_WARPS;   // a planning and an issuing warp, and those that read codes
+constexpr int HALF = 64;                           // keys of a step: half a unit
+constexpr int HALF_PANEL = HALF * 128;             // bytes of a panel of its 64 columns
 template <int DP>
 struct Shape4 {
-  static constexpr int TILE = KT * DP * 2;
-  static constexpr int STAGES = DP == 128 ? 2 : 4; // key and value tiles in turn
-  static constexpr int SMEM = 1024 + (1 + STAGES) * TILE + 4 * STAGE_BYTES;
+  static constexpr int TILE = HALF * DP * 2;
+  static constexpr int STAGES = DP == 128 ? 4 : 8; // key and value tiles in turn
+  static constexpr int SMEM = 1024 + 2 * TILE + STAGES * TILE + 4 * STAGE_BYTES;
 };
 
 // The part of a tile of codes that a warp reads: a lane has 16 bytes, 32 channels, of a row of each group of 8 (16, up to
@@ -29,7 +31,7 @@ struct Shape4 {
 // w of the CODE_WARPS has groups w, w + CODE_WARPS, ...
 template <int DP>
 struct Codes {
-  static constexpr int PIECES = DP / 32, ROWS = 32 / PIECES, GROUPS = KT / ROWS, N = (GROUPS + CODE_WARPS - 1) / CODE_WARPS;
+  static constexpr int PIECES = DP / 32, ROWS = 32 / PIECES, GROUPS = HALF / ROWS, N = (GROUPS + CODE_WARPS - 1) / CODE_WARPS;
   static constexpr int STEP = CODE_WARPS * ROWS;   // rows between a lane's groups
   uint32_t w[N][4], s[N];
   const uint8_t *codes, *scales;                   // of the lane's first row of the next tile
@@ -44,10 +46,9 @@ struct Codes {
     left = 32 * piece() < D ? f.len - first : -(1 << 30);
   }
   // (zeros where there is nothing to read)
-  __device__ __forceinline__ void read(uint32_t tok, uint32_t stok, int cw, int D) {
+  __device__ __forceinline__ void read(int i, uint32_t tok, uint32_t stok, int cw, int D) {
     const bool wide = (D & 31) == 0, full = 32 * piece() + 16 < D;   // (else rows start on 8 bytes)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    {
       w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0;
       s[i] = 0;
       if (STEP * i < left && (i + 1 < N || cw + i * CODE_WARPS < GROUPS)) {
@@ -66,15 +67,15 @@ struct Codes {
         s[i] = __ldg(reinterpret_cast<const uint16_t*>(scales + (unsigned long long)(STEP * i) * stok));
       }
     }
-    codes += (unsigned long long)KT * tok;
-    scales += (unsigned long long)KT * stok;
-    left -= KT;
   }
-  __device__ __forceinline__ void write(uint8_t* tile, int cw) const {
-    uint8_t* to = tile + (piece() >> 1) * PANEL + (cw * ROWS + row()) * 128;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (i + 1 == N && cw + i * CODE_WARPS >= GROUPS) break;
+  __device__ __forceinline__ void go_on(uint32_t tok, uint32_t stok) {
+    codes += (unsigned long long)HALF * tok;
+    scales += (unsigned long long)HALF * stok;
+    left -= HALF;
+  }
+  __device__ __forceinline__ void write(int i, uint8_t* tile, int cw) const {
+    uint8_t* to = tile + (piece() >> 1) * HALF_PANEL + (cw * ROWS + row()) * 128;
+    if (i + 1 < N || cw + i * CODE_WARPS < GROUPS) {
       const uint32_t by[2] = {scale_f16(s[i] & 255), scale_f16(s[i] >> 8)};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -125,7 +126,6 @@ __device__ __forceinline__ float scale_query(uint8_t* tile, int row, int D, floa
 }
 
 // row_weights (see there) of HALF keys. before(): waits until nothing is on its way to O (false: in vain).
-constexpr int HALF = 64;
 template <typename Before>
 __device__ __forceinline__ void half_weights(uint32_t tS, uint32_t tO, int D, int seen, float sl2, bool first, float& m, float& l,
                                              Before before) {
@@ -185,7 +185,7 @@ __device__ __forceinline__ void half_weights(uint32_t tS, uint32_t tO, int D, in
   tmem_st_wait();
 }
 
-// The halves of a fragment's tiles that have entries.
+// The steps of a fragment that have entries.
 __device__ __forceinline__ int halves_of(const Frag& f) { return (min(f.len - f.k0 * KT, f.n * KT) + HALF - 1) / HALF; }
 
 // The products of a slot with a half of a tile: scores, and values for `steps` <= 4 steps of 16 keys.
@@ -193,8 +193,8 @@ template <int DP>
 __device__ __forceinline__ void issue_half_scores(uint32_t tS, uint32_t q_lo, uint32_t k_lo, int nd, uint32_t idesc) {
 #pragma unroll
   for (int kk = 0; kk < DP / 16; ++kk) {
-    const uint32_t o = (kk >> 2) * (PANEL >> 4) + 2 * (kk & 3);
-    if (kk < nd) umma(tS, sw128(q_lo + o), sw128(k_lo + o), idesc, kk > 0);
+    const uint32_t o = 2 * (kk & 3);
+    if (kk < nd) umma(tS, sw128(q_lo + (kk >> 2) * (PANEL >> 4) + o), sw128(k_lo + (kk >> 2) * (HALF_PANEL >> 4) + o), idesc, kk > 0);
   }
 }
 __device__ __forceinline__ void issue_half_values(uint32_t tO, uint32_t tP, uint32_t v_lo, int steps, uint32_t idesc, bool begun) {
@@ -210,7 +210,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
   const AttendArgs& a = p.a;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t *ring = sQ + TILE, *stage = ring + STAGES * TILE;
+  uint8_t *ring = sQ + 2 * TILE, *stage = ring + STAGES * TILE;
   __shared__ uint64_t full[STAGES], empty[STAGES], s_full[2], p_ready[2], v_done[2], o_full, q_full, info_full[4], info_empty[4], done;
   __shared__ Frag info[4];
   __shared__ uint32_t tmem_slot;
@@ -265,9 +265,9 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
   int half = 0, nf = 0;                            // halves of tiles and fragments before
   bool off = false;
 
-  // (384 threads of 80 registers: 128 x 112 and 256 x 64)
+  // (384 threads of 80 registers: 128 x 128 and 256 x 56)
   if (warp >= 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 4) {
       // the fragments, each published while the one before is worked on
       for (bool more = some; more && !off; ++nf) {
@@ -283,84 +283,100 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
     } else if (warp == 5) {
       const int nd = a.D / 16;                     // steps of 16 columns of Q K^T, and units of O's width
       const uint32_t id_s = idesc_f16(SLOT, HALF), id_o = idesc_f16(SLOT, 16 * nd) | IDESC_B_MN;
-      const uint32_t q = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), PANEL);
-      constexpr uint32_t ROWS = HALF * 128 >> 4;   // the second half's rows of a tile
-      unsigned tile = 0;                           // before this fragment
+      const uint32_t q = sw128_lo(su32(sQ)), k_lo = sw128_lo(su32(ring)), v_lo = sw128_lo_mn(su32(ring), HALF_PANEL);
       for (bool more = some; more && !off;) {
         const int fs = nf & 3;
         off = wait(&q_full, nf++);                 // (info_full came before it)
         if (off) break;
-        const int n = halves_of(info[fs]), tiles = info[fs].n, len = info[fs].len - info[fs].k0 * KT;
+        const int n = halves_of(info[fs]), len = info[fs].len - info[fs].k0 * KT;
         more = !info[fs].last;
-        // The scores of a half come two halves ahead of its values: while the slot's threads take one half's weights, the
+        // The scores of a step come two steps ahead of its values: while the slot's threads take one step's weights, the
         // products with the values of the one before and the scores of the one behind run.
         auto scores = [&](int h) {
-          const unsigned st = 2 * (tile + (h >> 1)) % STAGES;
-          if (!(h & 1)) off = wait(&full[st], 2 * (tile + (h >> 1)) / STAGES);
+          const unsigned cur = 2 * (half + h), st = cur % STAGES;
+          off = wait(&full[st], cur / STAGES);
           if (off) return;
+          fence_async_smem();
           tc_fence_after();
           if (elect_one()) {
-            issue_half_scores<DP>(tmem + ((half + h) & 1) * HALF, q, k_lo + st * (TILE >> 4) + (h & 1) * ROWS, nd, id_s);
+            issue_half_scores<DP>(tmem + ((half + h) & 1) * HALF, q, k_lo + st * (TILE >> 4), nd, id_s);
             umma_commit(&s_full[(half + h) & 1]);
-            if ((h & 1) || h + 1 == n) umma_commit(&empty[st]);
+            umma_commit(&empty[st]);
           }
           __syncwarp();
         };
         scores(0);
         if (n > 1 && !off) scores(1);
         for (int h = 0; h < n && !off; ++h) {
-          const unsigned cur = 2 * (tile + (h >> 1)) + 1, st = cur % STAGES;
-          if (!(h & 1)) off = wait(&full[st], cur / STAGES);
-          off = off || wait(&p_ready[(half + h) & 1], (half + h) >> 1);
+          const unsigned cur = 2 * (half + h) + 1, st = cur % STAGES;
+          off = wait(&full[st], cur / STAGES) || wait(&p_ready[(half + h) & 1], (half + h) >> 1);
           if (off) break;
+          fence_async_smem();
           tc_fence_after();
           if (elect_one()) {
-            issue_half_values(tmem + 2 * HALF, tmem + ((half + h) & 1) * HALF, v_lo + st * (TILE >> 4) + (h & 1) * ROWS,
+            issue_half_values(tmem + 2 * HALF, tmem + ((half + h) & 1) * HALF, v_lo + st * (TILE >> 4),
                               (len - h * HALF + 15) / 16, id_o, h > 0);
             umma_commit(&v_done[(half + h) & 1]);
-            if ((h & 1) || h + 1 == n) umma_commit(&empty[st]);
+            umma_commit(&empty[st]);
             if (h + 1 == n) umma_commit(&o_full);
           }
           __syncwarp();
           if (h + 2 < n) scores(h + 2);
         }
         half += n;
-        tile += tiles;
       }
       if (elect_one()) umma_commit(&done);
       mbar_drain(&done, 0);
     } else if (some) {
-      // codes to fp16, keys or values, those of the next tile on their way while this one's place is waited for
+      // codes to fp16, keys or values; a step's are on their way to registers while the one before is written
       const int value = warp - 6 >= CODE_WARPS, cw = warp - 6 - value * CODE_WARPS;
+      const uint32_t tok = value ? p.v.tok : p.k.tok, stok = value ? p.v.stok : p.k.stok;
+      constexpr int N = Codes<DP>::N;
       Codes<DP> x;
-      unsigned cur = value;
-      for (int last = 0; !last && !off;) {
-        off = wait(&info_full[nf & 3], nf >> 2);
-        if (off) break;
-        const Frag& f = info[nf & 3];
-        const int n = f.n;
-        last = f.last;
-        if (value) x.begin(p.v, f, cw, a.D);
-        else x.begin(p.k, f, cw, a.D);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&info_empty[nf & 3]);
-        ++nf;
-#pragma unroll 1
-        for (int j = 0; j < n; ++j, cur += 2) {
-          // (behind the last tile's fence, which waits for what is on its way to registers, too)
-          x.read(value ? p.v.tok : p.k.tok, value ? p.v.stok : p.k.stok, cw, a.D);
-          const unsigned st = cur % STAGES;
-          off = cur >= STAGES && wait(&empty[st], cur / STAGES - 1);
-          if (off) break;
-          x.write(ring + st * TILE, cw);
-          fence_async_smem();
+      int left = 0, last = 0;                      // steps of the fragment that are not read yet
+      auto next = [&]() {                          // whether there is another step to read
+        if (left == 0 && !last) {
+          off = wait(&info_full[nf & 3], nf >> 2);
+          if (off) return false;
+          const Frag& f = info[nf & 3];
+          left = halves_of(f);
+          last = f.last;
+          if (value) x.begin(p.v, f, cw, a.D);
+          else x.begin(p.k, f, cw, a.D);
           __syncwarp();
-          if (lane == 0) mbar_arrive(&full[st]);
+          if (lane == 0) mbar_arrive(&info_empty[nf & 3]);
+          ++nf;
         }
+        return left > 0;
+      };
+      bool more = next();
+      if (more) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x.read(i, tok, stok, cw, a.D);
+        x.go_on(tok, stok);
+        --left;
+      }
+      for (unsigned cur = value; more; cur += 2) {
+        const unsigned st = cur % STAGES;
+        more = next();
+        off = off || (cur >= STAGES && wait(&empty[st], cur / STAGES - 1));
+        if (off) break;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          x.write(i, ring + st * TILE, cw);
+          if (more) x.read(i, tok, stok, cw, a.D);
+        }
+        if (more) {
+          x.go_on(tok, stok);
+          --left;
+        }
+        // (the warp that issues the products fences them off: this one's fence would wait for its loads, too)
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[st]);
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     const uint32_t tO = tmem + 2 * HALF + lanes;
     // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
