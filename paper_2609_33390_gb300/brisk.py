@@ -637,7 +637,7 @@ class PrefixAttention:
 
 
 _PACK_ATTEND, _PACK_MOVE = (struct.Struct(f"{n}q").pack_into for n in (3 * 4 + 2 * 8, 2 * 4 + 2 * 8))
-_NO_CACHE = (0,) * 8
+_NO_CACHE = (0,) * 16
 
 
 class PackedAttention(PrefixAttention):
@@ -691,15 +691,15 @@ class PackedAttention(PrefixAttention):
     def _cache(self, cache):
         """The eight numbers of keys' and of values' brisk_packed."""
         if self.S == 0:
-            return _NO_CACHE + _NO_CACHE
+            return _NO_CACHE
         if cache is None:
             raise ValueError("the cache is missing")
-        put = ()
-        for name in ("k", "v"):
-            codes, c = self._bytes(cache[name], self._shape_codes, name)
-            scales, s = self._bytes(cache[name + "_scales"], self._shape_scales, name + "_scales")
-            put += (codes, scales, c[0], c[1], c[2], s[0], s[1], s[2])
-        return put
+        of, codes, scales = self._bytes, self._shape_codes, self._shape_scales
+        k, a = of(cache["k"], codes, "k")
+        ks, b = of(cache["k_scales"], scales, "k_scales")
+        v, c = of(cache["v"], codes, "v")
+        vs, d = of(cache["v_scales"], scales, "v_scales")
+        return (k, ks, a[0], a[1], a[2], b[0], b[1], b[2], v, vs, c[0], c[1], c[2], d[0], d[1], d[2])
 
     def store(self, cache, k, v, start, count=None, stream=None):
         """Quantises rows t < count[b] (all T unless given) of k, v [B, T, Hkv, D] into places
@@ -718,10 +718,16 @@ class PackedAttention(PrefixAttention):
     def load(self, cache, T, start, count=None, out=None, stream=None):
         """k, v [B, T, Hkv, D]: in rows t < count[b] (all T unless given) what places start[b] + t of
         ``cache`` stand for, else zeros. ``out``: a dict of tensors to write to instead of new ones."""
-        shape, plain, view, at, i32 = (self.B, T, self.Hkv, self.D), self._plain, self._view, self._at_move, torch.int32
+        H, D, plain, at, i32 = self.Hkv, self.D, self._plain, self._at_move, torch.int32
+        shape = (self.B, T, H, D)
         if out is None:
-            out = _results(stream, lambda: {n: torch.empty(shape, dtype=self.dtype, device=self.device) for n in "kv"})
-        _PACK_MOVE(self._views, 0, *view(out["k"], shape, "k"), *view(out["v"], shape, "v"), *self._cache(cache))
+            new = lambda: {"k": torch.empty(shape, dtype=self.dtype, device=self.device),
+                           "v": torch.empty(shape, dtype=self.dtype, device=self.device)}
+            out = new() if stream is None else _results(stream, new)
+            k, v = ((out[n].data_ptr(), T * H * D, H * D, D) for n in "kv")
+        else:
+            k, v = self._view(out["k"], shape, "k"), self._view(out["v"], shape, "v")
+        _PACK_MOVE(self._views, 0, *k, *v, *self._cache(cache))
         _lend(stream, self.workspace)
         s = lib().brisk_packed_load(self._d, T, at[2], at[3], plain(start, self._shape_b, i32, "start"),
                                     plain(count, self._shape_b, i32, "count"), at[0], at[1], self._ws,
@@ -734,7 +740,11 @@ class PackedAttention(PrefixAttention):
         """PrefixAttention.attend with the own entries in ``cache`` (None if S == 0)."""
         pre, view, plain, at = self._shape_pre, self._view, self._plain, self._at_attend
         if out is None:
-            out = _results(stream, self._attended)
+            out = self._attended() if stream is None else _results(stream, self._attended)
+            to, lse = out["out"].data_ptr(), out["lse"].data_ptr()
+        else:
+            to = plain(out["out"], self._shape_q, self.dtype, "out")
+            lse = plain(out["lse"], self._shape_lse, torch.float32, "lse")
         _PACK_ATTEND(self._views, 0, *view(q, self._shape_q, "q"), *(view(k_prefix, pre, "k_prefix") or _NONE),
                      *(view(v_prefix, pre, "v_prefix") or _NONE), *self._cache(cache))
         _lend(stream, self.workspace)
@@ -742,9 +752,7 @@ class PackedAttention(PrefixAttention):
             self._d, at[0], at[1], at[2], at[3], at[4],
             plain(own_len, self._shape_b, torch.int32, "own_len"),
             plain(visible, self._shape_vis, torch.int32, "visible"),
-            self.scale if scale is None else scale,
-            plain(out["out"], self._shape_q, self.dtype, "out"),
-            plain(out["lse"], self._shape_lse, torch.float32, "lse"), self._ws, _stream(stream))
+            self.scale if scale is None else scale, to, lse, self._ws, _stream(stream))
         if s:
             raise BriskError(s, "packed_attend")
         return out

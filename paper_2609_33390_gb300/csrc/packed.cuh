@@ -11,6 +11,7 @@
 #include <cuda_fp16.h>
 
 #include "cache.cuh"
+#include "tensor_core.cuh"
 
 namespace brisk {
 
@@ -26,28 +27,34 @@ struct PackedView {   // row (s, t, h) at codes + s*seq + t*tok + h*head, its sc
   uint32_t tok, stok;
 };
 
+// x / s, correctly rounded, from r = 1 / s correctly rounded: Markstein, "Computation of elementary functions on the
+// IBM RISC System/6000 processor", IBM J. Res. Dev. 34 (1990).
+__device__ __forceinline__ float quotient(float x, float s, float r) {
+  const float q = x * r;
+  return fmaf(fmaf(-q, s, x), r, q);
+}
+// The same of two numbers. The exact quotient decides which code is nearest: a tie is a quotient of few bits, which
+// this gives exactly, and no other quotient is rounded to one. (The correction would take the sign of a zero.)
+__device__ __forceinline__ float2 quotients(float x, float y, float s, float r) {
+  const f32x2 xy = pack2(x, y), r2 = pack2(r, r), q = mul2(xy, r2);
+  float2 z;
+  unpack2(fma2(fma2(q, pack2(-s, -s), xy), r2, q), z.x, z.y);
+  return make_float2(copysignf(z.x, x), copysignf(z.y, y));
+}
 // The scale of a group whose largest magnitude is `top` (finite): top / 6, to nearest of 4 significant bits, as its
 // byte. The quotient's own rounding never moves it onto or across a border: where top differs from a border's
 // six-fold, which is exact, it differs by a unit in its last place, and that is more than half a one of the quotient.
 __device__ __forceinline__ uint32_t scale_byte(float top) {
-  const float s = fminf(fmaxf(top / 6.f, SCALE_MIN), SCALE_MAX);
+  const float sixth = quotient(top, 6.f, 1.f / 6.f), s = fminf(fmaxf(sixth, SCALE_MIN), SCALE_MAX);
   const uint32_t b = __float_as_uint(s);
   return ((b + 0x7ffffu + ((b >> 20) & 1)) >> 20) - (112u << 3);
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float((byte + (112u << 3)) << 20); }   // (byte >= 8)
 
-// x / s, correctly rounded, from r = 1 / s correctly rounded: Markstein, "Computation of elementary functions on the
-// IBM RISC System/6000 processor", IBM J. Res. Dev. 34 (1990). The exact quotient decides which code is nearest: a
-// tie is a quotient of few bits, which this gives exactly, and no other quotient is rounded to one. (The correction
-// would take the sign of a zero.)
-__device__ __forceinline__ float quotient(float x, float s, float r) {
-  const float q = x * r;
-  return copysignf(fmaf(fmaf(-q, s, x), r, q), x);
-}
-// The codes of two channels, `even` low: nearest, ties to the even code, saturated.
-__device__ __forceinline__ uint32_t to_codes(float even, float odd) {
+// The codes of two channels, the first low: nearest, ties to the even code, saturated.
+__device__ __forceinline__ uint32_t to_codes(float2 x) {
   uint32_t r;
-  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(r) : "f"(odd), "f"(even));
+  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(r) : "f"(x.y), "f"(x.x));
   return r;
 }
 
@@ -88,8 +95,8 @@ __device__ __forceinline__ float query_scale(float sl2, int up) {
 // Writing and reading back: rows t < count[b] of T, at places start[b] + t of a cache of room S.
 struct PackedMoveArgs {
   int B, T, Hkv, D, S, dt;
-  int all;                           // pieces of 16 unquantised bytes of a sequence's rows, of keys or of values
-  Divisor by_piece, by_heads;        // pieces a row; Hkv
+  Divisor by_token, by_row;          // pieces of 16 unquantised bytes of a token, and of a row
+  int step;                          // tokens that a CTA's threads have at once
   CacheView k, v;                    // [B, T, Hkv, D]
   PackedView kp, vp;
   const int32_t *start, *count;      // count: nullptr for T each

@@ -45,12 +45,12 @@ brisk_status move_args(const brisk_cache_dims* d, int32_t T, const brisk_view* k
       !packed_ok(vp, d, &a->vp))
     return BRISK_ERR_INVALID_ARG;
   const int pieces = d->D * (int)esize(d->dtype) / 16;
-  // a sequence's pieces, and its last CTA's beyond them, in 31 bits
-  if (2.0 * T * d->Hkv * pieces >= 2.1e9) return BRISK_ERR_UNSUPPORTED;
+  // tokens that a grid's dimensions do not take
+  if ((double)d->Hkv * pieces > 65535.0 * 256) return BRISK_ERR_UNSUPPORTED;
   a->B = d->B; a->T = T; a->Hkv = d->Hkv; a->D = d->D; a->S = d->S; a->dt = d->dtype;
-  a->all = T * d->Hkv * pieces;
-  a->by_piece.set(pieces);
-  a->by_heads.set(d->Hkv);
+  a->by_row.set(pieces);
+  a->by_token.set(d->Hkv * pieces);
+  a->step = d->Hkv * pieces < 256 ? 256 / (d->Hkv * pieces) : 1;
   a->k = ck;
   a->v = cv;
   a->start = start;

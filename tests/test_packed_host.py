@@ -74,9 +74,9 @@ def test_store_and_load_refuse(B):
                call(kt=_packed(d, seq=1 << 39)), call(kt=_packed(d, tok=-64)), call(kt=_packed(d, tok=1 << 32)),
                call(vt=_packed(d, scale_tok=1 << 32))]
         assert bad == [B.ERR_INVALID_ARG] * len(bad), call.__name__
-        assert call(d=_dims(B, Hkv=8, D=128), T=1 << 29, k=B.View(x.ptr, 1 << 37, 1024, 128),
-                    v=B.View(y.ptr, 1 << 37, 1024, 128), kt=_packed(_dims(B, Hkv=8, D=128)),
-                    vt=_packed(_dims(B, Hkv=8, D=128), 2 * FAKE)) == B.ERR_UNSUPPORTED
+        e = _dims(B, B=1, L=1, Hkv=1 << 20, Hq=1 << 20, D=128)
+        assert call(d=e, T=1, k=_rows(B, e, 1), v=_rows(B, e, 1, FAKE * 16), kt=_packed(e),
+                    vt=_packed(e, 2 * FAKE)) == B.ERR_UNSUPPORTED
     # keys and values into one place
     assert store(vt=p) == B.ERR_INVALID_ARG
     assert store(vt=_packed(d, 2 * FAKE, scales=p.scales)) == B.ERR_INVALID_ARG
