@@ -73,8 +73,16 @@ struct Codes {
     scales += (unsigned long long)HALF * stok;
     left -= HALF;
   }
-  __device__ __forceinline__ void write(int i, uint8_t* tile, int cw) const {
-    uint8_t* to = tile + (piece() >> 1) * HALF_PANEL + (cw * ROWS + row()) * 128;
+  // Where the lane's words of its first row go in a tile: they differ in the bits that the swizzle changes.
+  static __device__ __forceinline__ void places(int (&at)[4], int cw) {
+    const int first = (piece() >> 1) * HALF_PANEL + (cw * ROWS + row()) * 128 + (((piece() & 1) * 4 ^ (row() & 7)) << 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      at[k] = first ^ k << 4;
+      asm volatile("" : "+r"(at[k]));              // (or they would be worked out again for every store)
+    }
+  }
+  __device__ __forceinline__ void write(int i, uint8_t* tile, const int (&at)[4], int cw) const {
     if (i + 1 < N || cw + i * CODE_WARPS < GROUPS) {
       const uint32_t by[2] = {scale_f16(s[i] & 255), scale_f16(s[i] >> 8)};
 #pragma unroll
@@ -83,8 +91,7 @@ struct Codes {
         from_codes(w[i][k], h);
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[j] = mul_f16(h[j], by[k >> 1]);
-        *reinterpret_cast<uint4*>(to + STEP * i * 128 + ((((piece() & 1) * 4 + k) ^ (row() & 7)) << 4)) =
-            make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(tile + at[k] + STEP * i * 128) = make_uint4(h[0], h[1], h[2], h[3]);
       }
     }
   }
@@ -265,9 +272,9 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
   int half = 0, nf = 0;                            // halves of tiles and fragments before
   bool off = false;
 
-  // (384 threads of 80 registers: 128 x 128 and 256 x 56)
+  // (384 threads of 80 registers: 128 x 112 and 256 x 64)
   if (warp >= 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 4) {
       // the fragments, each published while the one before is worked on
       for (bool more = some; more && !off; ++nf) {
@@ -333,6 +340,8 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       const uint32_t tok = value ? p.v.tok : p.k.tok, stok = value ? p.v.stok : p.k.stok;
       constexpr int N = Codes<DP>::N;
       Codes<DP> x;
+      int at[4];
+      Codes<DP>::places(at, cw);
       int left = 0, last = 0;                      // steps of the fragment that are not read yet
       auto next = [&]() {                          // whether there is another step to read
         if (left == 0 && !last) {
@@ -363,7 +372,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
         if (off) break;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          x.write(i, ring + st * TILE, cw);
+          x.write(i, ring + st * TILE, at, cw);
           if (more) x.read(i, tok, stok, cw, a.D);
         }
         if (more) {
@@ -376,7 +385,7 @@ packed_slot_kernel(const __grid_constant__ PackedArgs p) {
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
     const uint32_t tO = tmem + 2 * HALF + lanes;
     // One turn: the next fragment's rows, this one's tiles, the next one's queries (once the scores that read
