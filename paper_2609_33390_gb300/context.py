@@ -6,7 +6,11 @@ attends over the prompt and them, hands hidden states and logits to the decode t
 attention weight that own entries got, and replaces the block's entries by those of the committed
 tokens. Before a block that might not fit, all sequences' caches are cut to the entries of
 largest weight. Nothing is read back: the host knows an upper bound of the lengths. Projections are
-library products; attention, weights, eviction and the tail are the library's kernels."""
+library products; attention, weights, eviction and the tail are the library's kernels.
+
+The own caches are held in the layer's type, or (`packed`) in 4 bits: entries are quantised as they are written
+and attended over as they lie; weights and eviction work on what is read back into a pair of caches
+that the layers of a model share."""
 from __future__ import annotations
 
 import torch
@@ -27,23 +31,28 @@ class ContextDecoder:
 
     `tail`: the prepared DecodeTail (its weights hold the embedding rows E_in and E_out); `w`: see
     layer_weights. Own caches have room for `S` entries and are cut to `keep`, of which the
-    `recent` newest always stay; sums of weights shrink by `decay` a block."""
+    `recent` newest always stay; sums of weights shrink by `decay` a block. packed: own caches in 4 bits."""
 
-    def __init__(self, tail, w, prompt, Hq, Hkv, D, S, keep, recent=0, decay=1.0):
+    def __init__(self, tail, w, prompt, Hq, Hkv, D, S, keep, recent=0, decay=1.0, packed=False):
         if keep + tail.L > S:
             raise ValueError(f"a block of {tail.L} does not fit behind {keep} of {S} entries")
         self.tail, self.w, self.keep, self.recent, self.decay = tail, w, keep, recent, decay
         self.e_in, self.e_out = tail.weights["E_in"], tail.weights["E_out"]
         B, L, dev, dt = tail.B, tail.L, tail.device, self.e_in.dtype
         self.Hq, self.Hkv, self.D, self.S = Hq, Hkv, D, S
-        self.attention = brisk.PrefixAttention(B, L, Hq, Hkv, D, prompt.numel(), S, dt, dev)
+        kind = brisk.PackedAttention if packed else brisk.PrefixAttention
+        self.attention = kind(B, L, Hq, Hkv, D, prompt.numel(), S, dt, dev)
         self.k_prefix, self.v_prefix = self._entries(self.e_in[prompt])
         self.k, self.v = (torch.zeros(B, S, Hkv, D, dtype=dt, device=dev) for _ in range(2))
         self.acc = torch.zeros(B, Hkv, S, device=dev)
-        self.spare = self.attention.alloc_evicted(keep, room=S)
+        # weights and eviction: on k and v, which are the caches, or what is read back of them
+        self.entries = brisk.PrefixAttention(B, L, Hq, Hkv, D, 0, S, dt, dev) if packed else None
+        self.cache = self.attention.alloc_cache() if packed else None
+        self.first = torch.zeros(B, dtype=torch.int32, device=dev)
+        self.spare = (self.entries or self.attention).alloc_evicted(keep, room=keep if packed else S)
         self.own_len = torch.zeros(B, dtype=torch.int32, device=dev)
         # a workspace's first word is its last call's status, which the next call of the step overwrites
-        self.words = [x.workspace[:4].view(torch.int32) for x in (self.attention, tail)]
+        self.words = [x.workspace[:4].view(torch.int32) for x in (self.attention, tail, self.entries) if x]
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.most = 0                                  # no sequence has more entries
         self.at = torch.arange(L, device=dev, dtype=torch.int32)
@@ -57,7 +66,16 @@ class ContextDecoder:
         return (x @ self.w["k"]).view(shape), (x @ self.w["v"]).view(shape)
 
     def _write(self, x, where):
-        self.k[self.rows, where], self.v[self.rows, where] = self._entries(x)
+        if self.cache is None:
+            self.k[self.rows, where], self.v[self.rows, where] = self._entries(x)
+        else:
+            self.attention.store(self.cache, *self._entries(x), where[:, 0].int())
+            self._note(self.words[0])
+
+    def _read(self, count):
+        """The first `count` [B] entries of caches in 4 bits, in k and v."""
+        self.attention.load(self.cache, self.S, self.first, count, out={"k": self.k, "v": self.v})
+        self._note(self.words[0])
 
     def _ids(self, x):
         """Token ids as indices: a row without a finite logit, or a wait that gave up, may leave any number, which
@@ -77,9 +95,17 @@ class ContextDecoder:
             torch.maximum(self.status, word, out=self.status)
 
     def _cut(self):
-        self.attention.evict(self.k, self.v, self.acc, self.own_len, self.keep, self.recent, out=self.spare)
-        self._note(self.words[0])
-        self.k, self.v, self.spare["k"], self.spare["v"] = self.spare["k"], self.spare["v"], self.k, self.v
+        if self.cache is None:
+            self.attention.evict(self.k, self.v, self.acc, self.own_len, self.keep, self.recent, out=self.spare)
+            self._note(self.words[0])
+            self.k, self.v, self.spare["k"], self.spare["v"] = self.spare["k"], self.spare["v"], self.k, self.v
+        else:
+            self._read(self.own_len)
+            self.entries.evict(self.k, self.v, self.acc, self.own_len, self.keep, self.recent, out=self.spare)
+            self._note(self.words[2])
+            # (the same bytes as before, in their new places)
+            self.attention.store(self.cache, self.spare["k"], self.spare["v"], self.first, self.spare["own_len"])
+            self._note(self.words[0])
         self.own_len.copy_(self.spare["own_len"])
         self.acc[:, :, :self.keep] = self.spare["acc"]
         self.acc[:, :, self.keep:] = 0
@@ -95,11 +121,15 @@ class ContextDecoder:
         visible = self.own_len[:, None] + self.at + 1  # a position sees the context and the block up to itself
         in_use = self.own_len + t.L
         q = (self.block @ self.w["q"]).view(t.B, t.L, self.Hq, self.D)
-        r = att.attend(q, self.k_prefix, self.v_prefix, self.k, self.v, in_use, visible=visible)
+        own = (self.k, self.v) if self.cache is None else (self.cache,)
+        r = att.attend(q, self.k_prefix, self.v_prefix, *own, in_use, visible=visible)
         self._note(self.words[0])
         hidden = self.block + r["out"].view(t.B, t.L, -1) @ self.w["o"]
         out = t.tail({"logits_q": hidden @ self.e_out.T, "logits_p": hidden @ self.w["p"] @ self.e_out.T,
                       "hidden": hidden, "h_c": hidden[:, 0].contiguous(), "x0": self.x0})
+        if self.cache is not None:
+            self._read(in_use)
+            att = self.entries
         att.weights(q, r["lse"], self.k, in_use, acc=self.acc, decay=self.decay, visible=visible, out=self.acc)
         self._note(*self.words)
         # the committed tokens' entries in place of the block's

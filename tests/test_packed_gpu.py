@@ -503,3 +503,31 @@ def test_a_cache_beyond_32_bits(B):
     got = r["out"][0, 0].double().cpu()
     assert ((got - want).abs() <= (2.0 ** -8 + 2 * S * U) * mass + 2.0 ** -8 * want.abs() + 1e-9).all()
     assert (n64(r["lse"][0, 0]) - torch.logsumexp(s, 1).numpy() < 1e-3).all()
+
+
+@pytest.mark.parametrize("Pn", [0, 300])
+def test_a_wait_that_gives_up_is_reported_and_the_next_call_is_right(B, Pn):
+    """Many rows a key head (the kernel on the tensor cores, whose waits are bounded): a limit that runs out while the
+    tiles are being written, then the default again, with the same bits as before."""
+    x = make(6, 16, 8, 2, 128, Pn, 700, BF, [700, 300, 0, 650, 64, 1])
+    att, r = check(B, x, 700)
+    zeros = {"out": torch.zeros_like(r["out"]), "lse": torch.zeros_like(r["lse"])}
+    before = B.set_wait_limit(1)
+    try:
+        for _ in range(3):
+            att.attend(x["q"], x["kp"], x["vp"], x["cache"], x["lens"], out=zeros)
+            assert att.device_status() == B.ERR_TIMEOUT
+    finally:
+        B.set_wait_limit(before)
+    again = att.attend(x["q"], x["kp"], x["vp"], x["cache"], x["lens"])
+    assert att.device_status() == B.OK
+    assert torch.equal(again["out"], r["out"]) and torch.equal(again["lse"], r["lse"])
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("L, Hq, Hkv", [(1, 64, 64), (2, 12, 12), (3, 6, 6), (1, 16, 16), (4, 32, 4), (1, 9, 3)])
+def test_heads_share_units_whatever_their_number(B, dt, L, Hq, Hkv):
+    """Enough sequences that a unit is of several heads (as many as a power of two divides, up to eight)."""
+    lens = [(37 * i) % 300 for i in range(60)]
+    x = make(60, L, Hq, Hkv, 64, 0, 300, dt, lens, causal(lens, L))
+    check(B, x, 300)
