@@ -33,13 +33,39 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
   const float q = x * r;
   return fmaf(fmaf(-q, s, x), r, q);
 }
-// The same of two numbers. The exact quotient decides which code is nearest: a tie is a quotient of few bits, which
-// this gives exactly, and no other quotient is rounded to one. (The correction would take the sign of a zero.)
-__device__ __forceinline__ float2 quotients(float x, float y, float s, float r) {
-  const f32x2 xy = pack2(x, y), r2 = pack2(r, r), q = mul2(xy, r2);
-  float2 z;
-  unpack2(fma2(fma2(q, pack2(-s, -s), xy), r2, q), z.x, z.y);
-  return make_float2(copysignf(z.x, x), copysignf(z.y, y));
+// 1 / s of a scale: the approximate reciprocal and a Newton step, which make the correctly rounded one of all 219.
+__device__ __forceinline__ float reciprocal(float s) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  return fmaf(fmaf(-s, r, 1.f), r, r);
+}
+// The codes of channels x / s, nearest, ties to the even code, saturated; the first lowest. The exact quotient decides which
+// is nearest: a tie is a quotient of few bits, which `quotient` gives exactly, and no other one is rounded to it. Negated
+// quotients are taken, with which a zero's sign outlasts the correction, and the codes' signs turned.
+template <int N>
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], float s, float r) {
+  const f32x2 s2 = pack2(s, s), r2 = pack2(-r, -r);
+  float q[N];
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const f32x2 y = pack2(x[i], x[i + 1]), z = mul2(y, r2);
+    unpack2(fma2(fma2(z, s2, y), r2, z), q[i], q[i + 1]);
+  }
+  uint32_t put;
+  if constexpr (N == 8)
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}" : "=r"(put)
+        : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[N - 4]), "f"(q[N - 3]), "f"(q[N - 2]), "f"(q[N - 1]));
+  else
+    asm("{\n\t.reg .b8 a, b, z;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "mov.b32 %0, {a, b, a, b};\n\t}" : "=r"(put) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
+  return put ^ 0x88888888u;
 }
 // The scale of a group whose largest magnitude is `top` (finite): top / 6, to nearest of 4 significant bits, as its
 // byte. The quotient's own rounding never moves it onto or across a border: where top differs from a border's
@@ -50,13 +76,6 @@ __device__ __forceinline__ uint32_t scale_byte(float top) {
   return ((b + 0x7ffffu + ((b >> 20) & 1)) >> 20) - (112u << 3);
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float((byte + (112u << 3)) << 20); }   // (byte >= 8)
-
-// The codes of two channels, the first low: nearest, ties to the even code, saturated.
-__device__ __forceinline__ uint32_t to_codes(float2 x) {
-  uint32_t r;
-  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tcvt.u32.u8 %0, c;\n\t}" : "=r"(r) : "f"(x.y), "f"(x.x));
-  return r;
-}
 
 // The four pairs of codes of a word's bytes, as fp16 (a byte's low code in the low half).
 __device__ __forceinline__ void from_codes(uint32_t w, uint32_t (&h)[4]) {

@@ -1,7 +1,7 @@
 // Entries written into a cache in 4 bits, and read back.
 //
 // A thread has 16 bytes of an unquantised row (8 channels of bf16, 4 of fp32) at one place of a token, of EACH tokens'
-// keys and values in turn, so that every access of a warp, on either side, is a run of whole rows, and places are worked
+// keys and values in turn (EACH: see tokens_each), so that every access of a warp, on either side, is a run of whole rows, and places are worked
 // out once a thread. The lanes of a group of 16 channels find its largest magnitude together. Both kernels are to be
 // bound by the rows' bytes: they spend some 40 instructions on a piece that is read back and 80 on one that is written.
 #include "packed.cuh"
@@ -9,7 +9,7 @@
 namespace brisk {
 namespace {
 
-constexpr int MOVE_THREADS = 256, EACH = 4;
+constexpr int MOVE_THREADS = 256;
 
 __device__ __forceinline__ int rows_of(const PackedMoveArgs& a, int b, int* start, bool* bad) {
   const int first = a.start[b], n = a.count ? a.count[b] : a.T;
@@ -21,7 +21,7 @@ __device__ __forceinline__ int rows_of(const PackedMoveArgs& a, int b, int* star
 template <typename T> constexpr int channels() { return 16 / (int)sizeof(T); }
 
 // A thread's place: its first token and key head, its channel; `there`: it has one.
-template <typename T>
+template <typename T, int EACH>
 struct Place {
   int t, h, c;
   bool there;
@@ -39,14 +39,14 @@ __device__ __forceinline__ const char* row_at(const CacheView& v, int es, int b,
   return static_cast<const char*>(v.p) + (b * v.seq + h * v.head + c + t * v.tok) * es;
 }
 
-template <typename T>
+template <typename T, int EACH>
 __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_constant__ PackedMoveArgs a) {
   constexpr int C = channels<T>(), LANES = GROUP / C;      // channels of a thread, threads of a group
   const int b = blockIdx.y;
   int start;
   bool bad;
   const int n = rows_of(a, b, &start, &bad);
-  const Place<T> at(a);
+  const Place<T, EACH> at(a);
   uint4 x[2][EACH];
   {
     const char *k = row_at(a.k, sizeof(T), b, at.h, at.c, at.t), *v = row_at(a.v, sizeof(T), b, at.h, at.c, at.t);
@@ -96,10 +96,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_consta
 #pragma unroll
       for (int o = 1; o < LANES; o <<= 1) top = max(top, __shfl_xor_sync(FULL_MASK, top, o));
       const uint32_t byte = scale_byte(__uint_as_float(top));
-      const float s = scale_value(byte), r = __frcp_rn(s);
-      uint32_t put = 0;
-#pragma unroll
-      for (int i = 0; i < C; i += 2) put |= to_codes(quotients(f[i], f[i + 1], s, r)) << (4 * i);
+      const float s = scale_value(byte);
+      const uint32_t put = codes_of(f, s, reciprocal(s));
       if (!mine) continue;
       uint8_t* p = codes + (unsigned long long)(uint32_t)(j * a.step) * to.tok;
       if constexpr (C == 8) *reinterpret_cast<uint32_t*>(p) = put;
@@ -115,7 +113,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_consta
   }
 }
 
-template <typename T>
+template <typename T, int EACH>
 __global__ void __launch_bounds__(MOVE_THREADS) load_kernel(const __grid_constant__ PackedMoveArgs a) {
   constexpr int C = channels<T>();
   const int b = blockIdx.y;
@@ -133,7 +131,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) load_kernel(const __grid_constan
     any = __syncthreads_or(any);
     if (threadIdx.x == 0) *a.status = any ? BRISK_ERR_INVALID_ARG : BRISK_OK;
   }
-  const Place<T> at(a);
+  const Place<T, EACH> at(a);
   if (!at.there) return;
   const bool clear = n <= 0 || (start >= 0 && (long long)start + n <= a.S);
   const long long first = start + (long long)at.t;
@@ -188,29 +186,51 @@ __global__ void __launch_bounds__(MOVE_THREADS) load_kernel(const __grid_constan
   }
 }
 
-dim3 grid_of(const PackedMoveArgs& a) {
-  const int each = a.step * EACH;
-  return dim3((unsigned)((a.T + each - 1) / each), a.B, (unsigned)((a.by_token.d + MOVE_THREADS - 1) / MOVE_THREADS));
+dim3 grid_of(const PackedMoveArgs& a, int each) {
+  const int n = a.step * each;
+  return dim3((unsigned)((a.T + n - 1) / n), a.B, (unsigned)((a.by_token.d + MOVE_THREADS - 1) / MOVE_THREADS));
+}
+// Tokens of a thread: one while its CTAs are few, as calls' latency goes (32 rows of 8 sequences written and read back,
+// 8 heads of 128: one 8.2 us, two 9.4, four 12.4), then two, and four of calls that write many (16 prompts of 1500 to
+// 4096 rows written: one 92.7 us, two 86.3, four 82.1; 64 caches read back: one 130, two 105, four 109).
+int tokens_each(const PackedMoveArgs& a, bool writes) {
+  auto ctas = [&](int each) {
+    const dim3 g = grid_of(a, each);
+    return (long long)g.x * g.y * g.z;
+  };
+  if (ctas(1) <= 4 * CACHE_SMS) return 1;
+  return writes && ctas(4) >= 32 * CACHE_SMS ? 4 : 2;
+}
+template <typename T>
+cudaError_t store(const PackedMoveArgs& a, dim3 grid, int each, cudaStream_t stream) {
+  if (each == 1) store_kernel<T, 1><<<grid, MOVE_THREADS, 0, stream>>>(a);
+  else if (each == 2) store_kernel<T, 2><<<grid, MOVE_THREADS, 0, stream>>>(a);
+  else store_kernel<T, 4><<<grid, MOVE_THREADS, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t load(const PackedMoveArgs& a, dim3 grid, int each, cudaStream_t stream) {
+  if (each == 1) load_kernel<T, 1><<<grid, MOVE_THREADS, 0, stream>>>(a);
+  else load_kernel<T, 2><<<grid, MOVE_THREADS, 0, stream>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_packed_store(const PackedMoveArgs& args, cudaStream_t stream) {
   PackedMoveArgs a = args;
-  const dim3 grid = grid_of(a);
+  const int each = tokens_each(a, true);
+  const dim3 grid = grid_of(a, each);
   a.alone = grid.x == 1 && grid.y == 1 && grid.z == 1;
   cudaError_t e = a.alone ? cudaSuccess : cudaMemsetAsync(a.status, 0, sizeof(int32_t), stream);
   if (e != cudaSuccess) return e;
-  if (a.dt == BRISK_DT_BF16) store_kernel<__nv_bfloat16><<<grid, MOVE_THREADS, 0, stream>>>(a);
-  else store_kernel<float><<<grid, MOVE_THREADS, 0, stream>>>(a);
-  return cudaGetLastError();
+  return a.dt == BRISK_DT_BF16 ? store<__nv_bfloat16>(a, grid, each, stream) : store<float>(a, grid, each, stream);
 }
 
 cudaError_t launch_packed_load(const PackedMoveArgs& a, cudaStream_t stream) {
-  const dim3 grid = grid_of(a);
-  if (a.dt == BRISK_DT_BF16) load_kernel<__nv_bfloat16><<<grid, MOVE_THREADS, 0, stream>>>(a);
-  else load_kernel<float><<<grid, MOVE_THREADS, 0, stream>>>(a);
-  return cudaGetLastError();
+  const int each = tokens_each(a, false);
+  const dim3 grid = grid_of(a, each);
+  return a.dt == BRISK_DT_BF16 ? load<__nv_bfloat16>(a, grid, each, stream) : load<float>(a, grid, each, stream);
 }
 
 }  // namespace brisk

@@ -115,6 +115,33 @@ def test_store_and_load_are_exact(B, size, dt):
             assert (n64(back[name]) == want).all()
 
 
+def test_borders_of_every_scale_and_code(B):
+    """Every scale that is written: the numbers half-way between two codes, which go to the even one, and their neighbours
+    in fp32; and the largest magnitudes half-way between two scales, with their neighbours."""
+    half = np.array([.25, .75, 1.25, 1.75, 2.5, 3.5, 5], np.float32)
+    rows = []
+    for b in range(8, 227):
+        s = np.float32(P.scale_of(b))
+        x = half * s                                 # (exact)
+        top = np.float32(6) * s
+        for y in (x, np.nextafter(x, np.float32(0)), np.nextafter(x, np.float32(1e9))):
+            rows.append(np.concatenate([[top, -top], y, -y]))
+        if b < 226:
+            edge = np.float32(3) * (s + np.float32(P.scale_of(b + 1)))   # six times what lies half-way: exact
+            for top in (edge, np.nextafter(edge, np.float32(0)), np.nextafter(edge, np.float32(1e9))):
+                rows.append(np.concatenate([[top, -0.0], x, -x]))
+    x = torch.from_numpy(np.stack(rows).astype(np.float32)).view(1, -1, 1, 16)
+    T = x.shape[1]
+    att = B.PackedAttention(1, 1, 1, 1, 16, 0, T, F32)
+    cache = new_cache(1, T, 1, 16, fill=0)
+    att.store(cache, x.cuda(), (-x).cuda(), i32([0]))
+    assert att.device_status() == B.OK
+    for name, y in (("k", x), ("v", -x)):
+        c, s = P.store(n64(y))
+        got_c, got_s = raw(cache, name)
+        assert (got_s == s).all() and (got_c == c).all()
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_every_byte_reads_as_the_oracle_has_it(B, dt):
     """All scales, the ones that no call writes among them, with all codes."""
