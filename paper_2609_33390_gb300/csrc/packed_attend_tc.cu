@@ -97,37 +97,40 @@ struct Codes {
   }
 };
 
-// A row of queries, as fetch_queries left it, becomes fp16 in its place; what its scores are to be multiplied by. (The
-// row is read at once: one piece after the other took 6000 cycles, a tenth of the kernel's time.)
+// A row of queries, as fetch_queries left it, becomes fp16 in its place; what its scores are to be multiplied by. (Four
+// pieces are read at once: one after the other took 6000 cycles, a tenth of the kernel's time. No more, since this runs
+// once a fragment and its instructions have to be fetched.)
 template <int DP>
 __device__ __forceinline__ float scale_query(uint8_t* tile, int row, int D, float sl2) {
   uint8_t* at = tile + row * 128;
-  uint32_t x[DP / 8][4];
-#pragma unroll
-  for (int c = 0; c < DP / 8; ++c) {
-    const uint4 y = *reinterpret_cast<const uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4));
-    x[c][0] = y.x; x[c][1] = y.y; x[c][2] = y.z; x[c][3] = y.w;
-  }
+  auto piece = [&](int c) { return reinterpret_cast<uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4)); };
   uint32_t top = 0;                                // of both halves' 16 bits: magnitudes compare as their bits do
+#pragma unroll 1
+  for (int c0 = 0; 8 * c0 < D; c0 += 4) {
+    uint4 x[4];
 #pragma unroll
-  for (int c = 0; c < DP / 8; ++c) {
-    uint32_t t = 0;
+    for (int c = 0; c < 4; ++c) x[c] = *piece(c0 + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t = __vmaxu2(t, x[c][i] & 0x7fff7fffu);
-    top = 8 * c < D ? __vmaxu2(top, t) : top;      // (behind the row's end there may be anything)
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t t = __vmaxu2(__vmaxu2(x[c].x & 0x7fff7fffu, x[c].y & 0x7fff7fffu),
+                                  __vmaxu2(x[c].z & 0x7fff7fffu, x[c].w & 0x7fff7fffu));
+      if (8 * (c0 + c) < D) top = __vmaxu2(top, t);    // (behind the row's end there may be anything)
+    }
   }
   const int up = query_shift(max(top << 16, top & 0xffff0000u));
   const f32x2 by = pack2(exp2_of(up), exp2_of(up));
+  auto change = [&](uint32_t x) {
+    float lo, hi;
+    unpack2(mul2(pack2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)), by), lo, hi);
+    return Weight::pair(lo, hi);
+  };
+#pragma unroll 1
+  for (int c0 = 0; 8 * c0 < D; c0 += 4) {
+    uint4 x[4];
 #pragma unroll
-  for (int c = 0; c < DP / 8; ++c) {
-    uint32_t y[4];
+    for (int c = 0; c < 4; ++c) x[c] = *piece(c0 + c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float lo, hi;
-      unpack2(mul2(pack2(__uint_as_float(x[c][i] << 16), __uint_as_float(x[c][i] & 0xffff0000u)), by), lo, hi);
-      y[i] = Weight::pair(lo, hi);
-    }
-    *reinterpret_cast<uint4*>(at + (c >> 3) * PANEL + (((c ^ row) & 7) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+    for (int c = 0; c < 4; ++c) *piece(c0 + c) = make_uint4(change(x[c].x), change(x[c].y), change(x[c].z), change(x[c].w));
   }
   return query_scale(sl2, up);
 }
