@@ -132,8 +132,8 @@ struct PackedArgs {
 };
 constexpr int PACKED_ROWS = 8;       // query rows of a tile of the kernel for few
 constexpr int PACKED_MANY = 16;      // bf16: from more rows a sequence and key head on, the kernel for many
+constexpr int PACKED_QUAD = 4;       // bf16: up to as many, the kernel for few has a form of its own
 constexpr int PACKED_CTAS = 2 * CACHE_SMS;
-constexpr int PACKED_STEP = 32;      // keys that a warp of the kernel for few takes at a time
 constexpr int PACKED_WARPS = 8;
 constexpr int PACKED_PARTS = 64;     // parts of a row, about, that units of several heads may lead to
 // The kernel for few rows: a unit is the keys of several neighbouring heads, a head a warp or several warps a head, as many
@@ -151,12 +151,12 @@ inline void divide_packed(AttendArgs* a) {
   const long long items = (long long)a->B * a->Hkv * a->sh.nLT;
   int log_heads = 0;
   while (!many && (2 << log_heads) <= UNIT_HEADS && a->Hkv % (2 << log_heads) == 0 &&
-         (long long)PACKED_CTAS * (2 << log_heads) <= PACKED_PARTS * items)
+         (long long)a->sh.grid_o * (2 << log_heads) <= PACKED_PARTS * items)
     ++log_heads;
   a->sh.log_kt = many || log_heads == 0 ? 7 : (log_heads == 1 ? 6 : 5);
   a->sh.kt = 1 << a->sh.log_kt;
   a->sh.log_heads = log_heads;
-  a->sh.slots_o = (int)((items >> log_heads) + PACKED_CTAS);
+  a->sh.slots_o = (int)((items >> log_heads) + a->sh.grid_o);
 }
 cudaError_t launch_packed_few(const PackedArgs& p, cudaStream_t stream);
 cudaError_t launch_packed_tc(const PackedArgs& p, cudaStream_t stream);

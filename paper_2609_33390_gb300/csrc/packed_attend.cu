@@ -26,29 +26,28 @@ namespace brisk {
 namespace {
 
 constexpr int WARPS = PACKED_WARPS, THREADS = 32 * WARPS;
-constexpr int STEP = PACKED_STEP, HALVES = STEP / 16;
+constexpr int STEP = 32, HALVES = STEP / 16;        // keys that a warp takes at a time
 constexpr int STAGES = 2;
-constexpr int ROWS = PACKED_ROWS;
 constexpr int AHEAD = 4;                           // fragments that a warp's copies may be ahead, a power of two
 constexpr float LAZY = 5.f, SHIFT = 10.f;          // log2 of what a score may exceed the held maximum by; weights below 2^15
 
-// DP: 64 or 128 channels, of which a row's first D are there.
-template <int DP>
-struct Tile {
+// A form of the kernel. DP: 64 or 128 channels, of which a row's first D are there. TERMS: fp16 numbers that make up a query
+// and a weight. QUAD: up to four rows, each of which has two columns of the products.
+template <int DP_, int TERMS_, bool QUAD_>
+struct Form {
+  static constexpr int DP = DP_, TERMS = TERMS_, QUAD = QUAD_;
+  static constexpr int ROWS = QUAD ? 4 : 8;
   static constexpr int ROW = DP / 2, SROW = DP / 16;
   static constexpr int CODES = STEP * ROW, SCALES = STEP * SROW;
-  static constexpr int BYTES = 2 * (CODES + SCALES);
-};
-template <int DP>
-struct alignas(16) WarpSmem {
-  uint8_t ring[STAGES][Tile<DP>::BYTES];
+  static constexpr int VALUES = CODES + SCALES;    // of a tile: where the values' begin
+  static constexpr int BYTES = 2 * VALUES;
 };
 constexpr int OS = CACHE_MAX_D + 4;                // floats between rows of a warp's sums
-template <int DP>
+template <typename T>
 struct Smem {
-  WarpSmem<DP> warp[WARPS];
-  float sums[WARPS][ROWS][OS];
-  float2 ml[WARPS][ROWS];
+  alignas(16) uint8_t ring[WARPS][STAGES * T::BYTES];
+  float sums[WARPS][T::ROWS][OS];
+  float2 ml[WARPS][T::ROWS];
   Walk walk[WARPS];
   Frag frag[WARPS][AHEAD];
 };
@@ -92,11 +91,10 @@ __device__ __forceinline__ void copy_bytes(void* to, const void* from) {
 
 // A lane's share of copying the codes and scales of STEP keys and values to a place of the ring: where from, of those that
 // are next. Rows from the cache's end on are left as they are.
-template <int DP>
+template <typename T>
 struct Copies {
-  using T = Tile<DP>;
+  static constexpr int DP = T::DP, VALUES = T::VALUES;
   static constexpr int P = DP / 32;                // 16-byte pieces a row
-  static constexpr int VALUES = T::CODES + T::SCALES;
   const uint8_t *k, *v, *ks, *vs;
   int left;                                        // keys of the fragment from the first of these on
   // (one multiplication of 32 bits each, beside the conversions that take the integer units)
@@ -113,6 +111,11 @@ struct Copies {
     vs = ahead(p.v.scales + f.b * p.v.sseq + f.h * p.v.shead, t0 + lane, p.v.stok);
     left = end - t0;
   }
+  __device__ __forceinline__ void copy_scales(uint8_t* to) const {
+    const int at = T::CODES + (threadIdx.x & 31) * T::SROW;
+    copy_bytes<T::SROW>(to + at, ks);
+    copy_bytes<T::SROW>(to + VALUES + at, vs);
+  }
   __device__ __forceinline__ void copy(const PackedArgs& p, uint8_t* to, int step) {
     const int lane = threadIdx.x & 31;
     if (p.a.D == DP && left >= STEP) {             // nothing to leave out
@@ -123,8 +126,7 @@ struct Copies {
         copy_bytes<16>(at + 512 * i, ahead(k, R * i, p.k.tok));
         copy_bytes<16>(at + 512 * i + VALUES, ahead(v, R * i, p.v.tok));
       }
-      copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks);
-      copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs);
+      copy_scales(to);
     } else {
       const bool wide = (p.a.D & 31) == 0;
       const int n = wide ? P : 2 * P, row = lane / n, piece = lane % n, bytes = wide ? 16 : 8;
@@ -141,10 +143,7 @@ struct Copies {
             copy_bytes<8>(at + VALUES, vf);
           }
         }
-      if (lane < left) {
-        copy_bytes<T::SROW>(to + T::CODES + lane * T::SROW, ks);
-        copy_bytes<T::SROW>(to + VALUES + T::CODES + lane * T::SROW, vs);
-      }
+      if (lane < left) copy_scales(to);
     }
     k = ahead(k, step, p.k.tok);
     v = ahead(v, step, p.v.tok);
@@ -154,14 +153,17 @@ struct Copies {
   }
 };
 
-template <int DP, int TERMS>
+template <typename T>
 __global__ void __launch_bounds__(THREADS, 2)
 packed_few_kernel(const __grid_constant__ PackedArgs p) {
-  using T = Tile<DP>;
-  constexpr int KS = DP / 16;                      // steps of 16 channels of a score, tiles of 16 channels of O
+  constexpr int DP = T::DP, TERMS = T::TERMS, ROWS = T::ROWS;
+  constexpr bool QUAD = T::QUAD;
+  constexpr int KS = DP / 16;                      // steps of 16 channels of a score
+  constexpr int OT = QUAD ? DP / 32 : KS;          // tiles of O
+  constexpr int R = QUAD ? 1 : 2;                  // rows of a lane
   const AttendArgs& a = p.a;
   extern __shared__ __align__(16) uint8_t raw[];
-  Smem<DP>& sm = *reinterpret_cast<Smem<DP>*>(raw);
+  Smem<T>& sm = *reinterpret_cast<Smem<T>*>(raw);
   __shared__ int warp_sum[WARPS], bad;
   __shared__ Start start;
   __shared__ Plan plan;
@@ -194,11 +196,11 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
   const int heads = 1 << a.sh.log_heads, sub = warp & (heads - 1), group = WARPS >> a.sh.log_heads, turn = warp >> a.sh.log_heads;
   const int stride = STEP * group;                 // keys of the warps of a head: each has every group-th STEP
   int cf = -1;
-  Copies<DP> next;
+  Copies<T> next;
   next.left = 0;
-  unsigned issued = 0, used = 0;
-  uint8_t* const ring = sm.warp[warp].ring[0];
-  int write = 0, read = 0;                         // places of issued and used
+  int pending = 0;                                 // tiles of the ring that are not read yet
+  uint8_t* const ring = sm.ring[warp];
+  int write = 0, read = 0;                         // places of the next one copied, and of the next one read
   auto issue = [&]() {                             // one more tile, as a group of copies; false: there is none (yet)
     while (next.left <= 0) {
       if (cf + 1 == walked && (!more || walked - done >= AHEAD || !find())) return false;
@@ -209,22 +211,18 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
     }
     next.copy(p, ring + write, stride);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    write = write == (STAGES - 1) * T::BYTES ? 0 : write + T::BYTES;
-    ++issued;
+    write ^= T::BYTES;
+    ++pending;
     return true;
   };
   auto meet = [&]() {                              // of the warps of a head
     if (group == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "r"(32 * group) : "memory");
   };
-  auto fill = [&]() {                              // the ring's free places
-#pragma unroll 1
-    while (issued - used < STAGES && issue()) {}
-  };
-  fill();
+  static_assert(STAGES == 2, "places alternate");
 
   // where a lane reads a tile: its key's codes and scales, and those of its two values (each 8 and 16 rows further, too)
-  constexpr int VALUES = T::CODES + T::SCALES;
+  constexpr int VALUES = T::VALUES;
   int at_k = DP == 128 ? piece_at<DP>(key_of(g), c) : key_of(g) * T::ROW + 8 * c, at_ks = T::CODES + key_of(g) * T::SROW + c * (DP / 64);
   int at_v[2], at_vs[2];
 #pragma unroll
@@ -233,27 +231,32 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
     at_v[i] = VALUES + (DP == 128 ? piece_at<DP>(key, g >> 1) + 8 * (g & 1) : key * T::ROW + 4 * g);
     at_vs[i] = VALUES + T::CODES + key * T::SROW + g * (DP / 8) / GROUP;
   }
+  // of two weights of a row, the first and the second in the half that the lane's column stands for
+  const uint32_t pick[2] = {g & 1 ? 0x1044u : 0x4410u, g & 1 ? 0x3244u : 0x4432u};
   // (the compiler would rather work them out again at every step)
   asm volatile("" : "+r"(at_k), "+r"(at_ks), "+r"(at_v[0]), "+r"(at_v[1]), "+r"(at_vs[0]), "+r"(at_vs[1]));
 
   for (;;) {
     if (walked == done && (!more || !find())) break;
+#pragma unroll 1
+    while (pending < STAGES && issue()) {}
     Frag f = frags[done % AHEAD];
     f.h = f.h * heads + sub;
     const int end = min(f.len, (f.k0 + f.n) << a.sh.log_kt);
 
-    // queries: lane (g, c) has channels (DP / 4) c .. of row g; row_scale: of rows 2c, 2c + 1
+    // queries: lane (g, c) has channels (DP / 4) c .. of row g (QUAD: g / 2); row_scale: of rows 2c, 2c + 1 (c)
+    const int qrow = QUAD ? g >> 1 : g;
     uint32_t qf[TERMS][KS][2];
-    float row_scale[2];
-    int see = f.len, low;                          // entries that row g sees, and the row that sees fewest
+    float row_scale[R];
+    int see = f.len, low;                          // entries that row qrow sees, and the row that sees fewest
     {
       float q[DP / 4];
       float top = 0.f;
 #pragma unroll
       for (int i = 0; i < DP / 4; ++i) q[i] = 0.f;
-      if (g < f.rows) {
+      if (qrow < f.rows) {
         int token, head;
-        row_of(a, f, g, token, head);
+        row_of(a, f, qrow, token, head);
         see = row_limit(a, f, token, f.len);
         const int b = a.by_L.of(token), i = token - b * a.L;
         const long long at = b * a.q.seq + i * a.q.tok + head * a.q.head + c * (DP / 4);
@@ -283,31 +286,34 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
         }
       }
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        row_scale[r] = __shfl_sync(FULL_MASK, mine, 4 * (2 * c + r));
-      }
+      for (int r = 0; r < R; ++r) row_scale[r] = __shfl_sync(FULL_MASK, mine, 4 * (2 * c + r));
       low = __reduce_min_sync(FULL_MASK, see);
     }
 
-    float l[2] = {0.f, 0.f};
-    float above[2] = {-INFINITY, -INFINITY}, less[2] = {0.f, 0.f};   // what a score is compared with, what is added to it
-    float o[KS][4];
+    float l[R], above[R], less[R];                 // (above: what a score is compared with, less: what is added to it)
 #pragma unroll
-    for (int i = 0; i < KS; ++i)
+    for (int r = 0; r < R; ++r) {
+      l[r] = less[r] = 0.f;
+      above[r] = -INFINITY;
+    }
+    float o[OT][4];
+#pragma unroll
+    for (int i = 0; i < OT; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
 
     for (int t0 = (f.k0 << a.sh.log_kt) + turn * STEP; t0 < end; t0 += stride) {
       __syncwarp();                                // (the place that is filled next has been read)
-      fill();
-      if (issued - used == STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      if (pending < STAGES) issue();
+      if (pending == STAGES) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
       else asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
       uint8_t* tile = ring + read;
-      read = read == (STAGES - 1) * T::BYTES ? 0 : read + T::BYTES;
-      ++used;
+      read ^= T::BYTES;
+      --pending;
 
-      // scores; x[u][0], x[u][1]: of key t0 + 16u + key_of(g), rows 2c and 2c + 1; x[u][2], x[u][3]: 8 keys further
+      // scores; x[u][0], x[u][1]: of key t0 + 16u + key_of(g), rows 2c and 2c + 1 (QUAD: twice row c); x[u][2], x[u][3]: 8
+      // keys further
       float x[HALVES][4];
       {
         constexpr int W = DP / 32;                 // words of a lane's row, two steps of 16 channels each
@@ -350,9 +356,11 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
       }
       if (t0 + STEP > low) {
         // (values that some row does not see: weights of 0 shall meet numbers, whatever the bytes)
-        uint32_t* vs = reinterpret_cast<uint32_t*>(tile + VALUES + T::CODES + lane * T::SROW);
+        if (lane < STEP) {
+          uint32_t* vs = reinterpret_cast<uint32_t*>(tile + VALUES + T::CODES + lane * T::SROW);
 #pragma unroll
-        for (int i = 0; i < T::SROW / 4; ++i) vs[i] = __vminu4(vs[i], SCALE_TOP * 0x01010101u);
+          for (int i = 0; i < T::SROW / 4; ++i) vs[i] = __vminu4(vs[i], SCALE_TOP * 0x01010101u);
+        }
         __syncwarp();
         const int key = t0 + key_of(g);
         int lim[2];
@@ -364,16 +372,19 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
           for (int i = 0; i < 4; ++i)
             if (key + 16 * u + (i < 2 ? 0 : 8) >= lim[i & 1]) x[u][i] = -INFINITY;
       }
-      float t[2] = {fmaxf(x[0][0], x[0][2]), fmaxf(x[0][1], x[0][3])};
+      float t[R];
+      bool over = false;
 #pragma unroll
-      for (int u = 1; u < HALVES; ++u)
+      for (int r = 0; r < R; ++r) {
+        t[r] = fmaxf(x[0][r], x[0][2 + r]);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) t[r] = fmaxf(t[r], fmaxf(x[u][r], x[u][2 + r]));
+        for (int u = 1; u < HALVES; ++u) t[r] = fmaxf(t[r], fmaxf(x[u][r], x[u][2 + r]));
+        t[r] *= row_scale[r];
+        over |= t[r] > above[r];
+      }
+      if (__any_sync(FULL_MASK, over)) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) t[r] *= row_scale[r];
-      if (__any_sync(FULL_MASK, t[0] > above[0] || t[1] > above[1])) {
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < R; ++r) {
           float top = t[r];
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
@@ -384,29 +395,29 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
             less[r] = SHIFT - top;
             l[r] *= alpha;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-              o[i][r] *= alpha;
-              o[i][2 + r] *= alpha;
-            }
+            for (int i = 0; i < OT; ++i)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (QUAD || (k & 1) == r) o[i][k] *= alpha;
           }
         }
       }
-      uint32_t pb[HALVES][TERMS][2];
+      uint32_t pb[HALVES][TERMS][2];               // of the first and the second eight keys
 #pragma unroll
       for (int u = 0; u < HALVES; ++u)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float e[2];
+          float e[R];
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
+          for (int r = 0; r < R; ++r) {
             e[r] = ex2(fmaf(x[u][2 * i + r], row_scale[r], less[r]));
             l[r] += e[r];
           }
-          const uint32_t h = half2_of(e[0], e[1]);
+          const uint32_t h = half2_of(e[0], e[R - 1]);
           pb[u][0][i] = transposed(h);
           if constexpr (TERMS == 2) {
             const float2 z = floats_of(h);
-            pb[u][TERMS - 1][i] = transposed(half2_of(e[0] - z.x, e[1] - z.y));
+            pb[u][TERMS - 1][i] = transposed(half2_of(e[0] - z.x, e[R - 1] - z.y));
           }
         }
       // values: channels (DP / 8) g .. of keys key_of(2c), key_of(2c + 1) and 8 more each
@@ -427,6 +438,32 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
         get(at_v[1] + row, w1);
         get(at_v[0] + row8, w2);
         get(at_v[1] + row8, w3);
+        if constexpr (QUAD) {
+          // A product takes eight keys: a column is a row and one of the two codes of a byte, a weight meets the one and
+          // a zero the other, so that the codes of a key are converted as they lie.
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t s0 = scale_plain(tile[at_vs[0] + (i ? srow8 : srow)]), s1 = scale_plain(tile[at_vs[1] + (i ? srow8 : srow)]);
+            const uint32_t b0 = __byte_perm(pb[u][0][i], 0, pick[0]), b1 = __byte_perm(pb[u][0][i], 0, pick[1]);
+#pragma unroll
+            for (int w = 0; w < DP / 64; ++w) {
+              uint32_t y[4], z[4];
+              from_codes(i ? w2[w] : w0[w], y);
+              from_codes(i ? w3[w] : w1[w], z);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                y[k] = mul_f16(y[k], s0);
+                z[k] = mul_f16(z[k], s1);
+              }
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t v4[4] = {y[2 * k], y[2 * k + 1], z[2 * k], z[2 * k + 1]};
+                mma(o[2 * w + k], v4, b0, b1);
+              }
+            }
+          }
+          continue;
+        }
         const uint32_t s0 = scales_plain(tile[at_vs[0] + srow], tile[at_vs[1] + srow]);
         const uint32_t s1 = scales_plain(tile[at_vs[0] + srow8], tile[at_vs[1] + srow8]);
 #pragma unroll
@@ -444,29 +481,31 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
               mma_first(d, v4, pb[u][TERMS - 1][0], pb[u][TERMS - 1][1]);
               mma(d, v4, pb[u][0][0], pb[u][0][1]);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) o[4 * w + i][k] += d[k];
+              for (int k = 0; k < 4; ++k) o[(4 * w + i) % OT][k] += d[k];
             } else {
-              mma(o[4 * w + i], v4, pb[u][0][0], pb[u][0][1]);
+              mma(o[(4 * w + i) % OT], v4, pb[u][0][0], pb[u][0][1]);
             }
           }
         }
       }
     }
 
-    // the warps' parts meet; o[i]: channels (DP / 8) g + 2i and 2i + 1 of rows 2c and 2c + 1
+    // the warps' parts meet; o[i]: channels (DP / 8) g + 2i and 2i + 1 of rows 2c and 2c + 1, or four from 4i on of row c
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < R; ++r) {
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(FULL_MASK, l[r], d);
-      if (g == 0) sm.ml[warp][2 * c + r] = make_float2(above[r] == -INFINITY ? -INFINITY : -less[r], l[r]);
+      if (g == 0) sm.ml[warp][R * c + r] = make_float2(above[r] == -INFINITY ? -INFINITY : -less[r], l[r]);
+      float* to = &sm.sums[warp][R * c + r][(DP / 8) * g];
 #pragma unroll
-      for (int i = 0; i < KS; i += 2)
-        store4(&sm.sums[warp][2 * c + r][(DP / 8) * g + 2 * i], make_float4(o[i][r], o[i][2 + r], o[i + 1][r], o[i + 1][2 + r]));
+      for (int i = 0; i < DP / 8; i += 4)
+        store4(to + i, QUAD ? make_float4(o[i / 4][0], o[i / 4][1], o[i / 4][2], o[i / 4][3])
+                            : make_float4(o[i / 2 % OT][r], o[i / 2 % OT][2 + r], o[(i / 2 + 1) % OT][r], o[(i / 2 + 1) % OT][2 + r]));
     }
     meet();
 #pragma unroll 1
     for (int e = turn * 32 + lane; e < ROWS * (DP / 4); e += 32 * group) {
-      const int r = e & 7, c0 = 4 * (e >> 3);
+      const int r = e % ROWS, c0 = 4 * (e / ROWS);
       if (r >= f.rows || c0 >= D) continue;
       float top = -INFINITY, all = 0.f;
       for (int w = sub; w < WARPS; w += heads) top = fmaxf(top, sm.ml[w][r].x);
@@ -493,7 +532,7 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
         else store4(static_cast<float*>(a.out) + row * D + c0, y);
         if (a.lse && c0 == 0) a.lse[row] = none ? -INFINITY : (top + log2f(all)) * (1.f / LOG2E);
       } else {
-        const int per = min(ROWS, plan.LG);
+        const int per = min(PACKED_ROWS, plan.LG);
         const long long slot = (long long)sub * a.sh.slots_o + f.slot;
         store4(a.part_o + part_at(slot, per, D, r, c0), v);
         if (c0 == 0) a.ml_o[slot * per + r] = make_float2(top, all);
@@ -505,10 +544,10 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <int DP, int TERMS>
+template <typename T>
 cudaError_t run(const PackedArgs& p, cudaStream_t stream) {
-  auto kernel = packed_few_kernel<DP, TERMS>;
-  constexpr size_t smem = sizeof(Smem<DP>);
+  auto kernel = packed_few_kernel<T>;
+  constexpr size_t smem = sizeof(Smem<T>);
   cudaError_t e = set_up_kernel(kernel, CARVEOUT_FULL_KB, smem);
   return e != cudaSuccess ? e : launch_early(kernel, p.a.sh.grid_o, THREADS, smem, stream, false, p);
 }
@@ -516,8 +555,10 @@ cudaError_t run(const PackedArgs& p, cudaStream_t stream) {
 }  // namespace
 
 cudaError_t launch_packed_few(const PackedArgs& p, cudaStream_t stream) {
-  if (p.a.dt == BRISK_DT_BF16) return p.a.D > 64 ? run<128, 1>(p, stream) : run<64, 1>(p, stream);
-  return p.a.D > 64 ? run<128, 2>(p, stream) : run<64, 2>(p, stream);
+  const bool wide = p.a.D > 64;
+  if (p.a.dt != BRISK_DT_BF16) return wide ? run<Form<128, 2, false>>(p, stream) : run<Form<64, 2, false>>(p, stream);
+  if (p.a.L * p.a.G <= PACKED_QUAD) return wide ? run<Form<128, 1, true>>(p, stream) : run<Form<64, 1, true>>(p, stream);
+  return wide ? run<Form<128, 1, false>>(p, stream) : run<Form<64, 1, false>>(p, stream);
 }
 
 }  // namespace brisk
