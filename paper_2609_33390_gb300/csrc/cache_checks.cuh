@@ -65,9 +65,8 @@ inline CacheWs cache_ws(const AttendArgs& a) {
   const long long tiles_p = a.P > 0 ? (R + a.sh.rt_p - 1) / a.sh.rt_p * a.Hkv : 0;
   const long long tiles_o = a.S > 0 ? (LG + a.sh.rt_o - 1) / a.sh.rt_o * a.Hkv * a.B : 0;
   const long long rows_p = (tiles_p + (a.sh.grid_p ? a.sh.grid_p : a.sh.grid_o)) * (R < a.sh.rt_p ? R : a.sh.rt_p);
-  // (a unit may be of up to UNIT_HEADS key heads, each with slots of its own)
-  const long long heads = a.sh.slots_o > 0 ? UNIT_HEADS : 1;
-  const long long rows_o = (tiles_o + heads * a.sh.grid_o) * (LG < a.sh.rt_o ? LG : a.sh.rt_o);
+  // (a unit may be of several key heads, each with slots of its own)
+  const long long rows_o = (tiles_o + ((long long)a.sh.grid_o << a.sh.log_heads)) * (LG < a.sh.rt_o ? LG : a.sh.rt_o);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t q = o; o = up(o + bytes); return q; };
   w.status = take(ALIGN);
@@ -85,7 +84,7 @@ inline CacheWs cache_ws(const AttendArgs& a) {
 inline bool units_ok(const AttendArgs& a) {
   const long long LG = a.L * a.G, R = a.B * LG;
   const double pre = (double)a.Hkv * ((R + a.sh.rt_p - 1) / a.sh.rt_p) * a.sh.kP;
-  const double own = (double)a.Hkv * a.B * ((LG + a.sh.rt_o - 1) / a.sh.rt_o) * ((a.S + a.sh.kt - 1) / a.sh.kt);
+  const double own = (double)(a.Hkv >> a.sh.log_heads) * a.B * ((LG + a.sh.rt_o - 1) / a.sh.rt_o) * ((a.S + a.sh.kt - 1) / a.sh.kt);
   return pre + own < 2.0e9;
 }
 
