@@ -663,6 +663,12 @@ class PackedAttention(PrefixAttention):
         at = self._at[0]
         self._at_attend = [at, at + 32, at + 64, at + 96, at + 160]
         self._at_move = [at, at + 32, at + 64, at + 128]
+        # a call in its usual form is marshalled there; the ways below are for results given, other streams, refusals
+        from . import _marshal as quick
+        self._quick_store, self._quick_load, self._quick_attend = quick.store, quick.load, quick.attend
+        entry = lambda f: ctypes.cast(f, _vp).value
+        self._f_store, self._f_load = entry(lib().brisk_packed_store), entry(lib().brisk_packed_load)
+        self._f_attend = entry(lib().brisk_packed_attend)
 
     def alloc_cache(self, order="token"):
         """A cache of zeros, written on the current stream: in memory [B, S, Hkv, ..] ("token") or
@@ -704,6 +710,11 @@ class PackedAttention(PrefixAttention):
     def store(self, cache, k, v, start, count=None, stream=None):
         """Quantises rows t < count[b] (all T unless given) of k, v [B, T, Hkv, D] into places
         start[b] + t of ``cache`` (start, count [B] int32; see brisk_packed_store)."""
+        if stream is None:
+            s = self._quick_store(self._f_store, self._d, self.workspace, cache, k, v, start, count)
+            if s is not None:
+                _check(s, "packed_store")
+                return cache
         T = k.shape[1]
         shape, plain, at, i32 = (self.B, T, self.Hkv, self.D), self._plain, self._at_move, torch.int32
         _PACK_MOVE(self._views, 0, *self._view(k, shape, "k"), *self._view(v, shape, "v"), *self._cache(cache))
@@ -718,6 +729,12 @@ class PackedAttention(PrefixAttention):
     def load(self, cache, T, start, count=None, out=None, stream=None):
         """k, v [B, T, Hkv, D]: in rows t < count[b] (all T unless given) what places start[b] + t of
         ``cache`` stand for, else zeros. ``out``: a dict of tensors to write to instead of new ones."""
+        if out is None and stream is None:
+            r = self._quick_load(self._f_load, self._d, self.workspace, cache, T, start, count)
+            if r.__class__ is dict:
+                return r
+            if r is not None:
+                raise BriskError(r, "packed_load")
         H, D, plain, at, i32 = self.Hkv, self.D, self._plain, self._at_move, torch.int32
         shape = (self.B, T, H, D)
         if out is None:
@@ -738,6 +755,14 @@ class PackedAttention(PrefixAttention):
 
     def attend(self, q, k_prefix, v_prefix, cache, own_len, visible=None, scale=None, out=None, stream=None):
         """PrefixAttention.attend with the own entries in ``cache`` (None if S == 0)."""
+        scale = self.scale if scale is None else scale
+        if out is None and stream is None:
+            r = self._quick_attend(self._f_attend, self._d, self.workspace, scale, q, k_prefix, v_prefix, cache,
+                                   own_len, visible)
+            if r.__class__ is dict:
+                return r
+            if r is not None:
+                raise BriskError(r, "packed_attend")
         pre, view, plain, at = self._shape_pre, self._view, self._plain, self._at_attend
         if out is None:
             out = self._attended() if stream is None else _results(stream, self._attended)
@@ -752,7 +777,7 @@ class PackedAttention(PrefixAttention):
             self._d, at[0], at[1], at[2], at[3], at[4],
             plain(own_len, self._shape_b, torch.int32, "own_len"),
             plain(visible, self._shape_vis, torch.int32, "visible"),
-            self.scale if scale is None else scale, to, lse, self._ws, _stream(stream))
+            scale, to, lse, self._ws, _stream(stream))
         if s:
             raise BriskError(s, "packed_attend")
         return out

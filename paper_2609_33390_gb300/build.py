@@ -1,19 +1,23 @@
-"""Builds the CUDA library ``libbrisk.so`` in-tree for sm_103a with nvcc.
+"""Builds the CUDA library ``libbrisk.so`` in-tree for sm_103a with nvcc, and the binding's ``_marshal.so``.
 
 Each translation unit compiles in parallel, then one shared link. The runtime
 is linked statically, so the library loads on a machine without a GPU driver
-(the driver is opened on first use).
+(the driver is opened on first use). ``_marshal.so`` is a module of the interpreter, compiled on its headers and
+torch's, beside the library.
 """
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbrisk.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-Xptxas", "-warn-spills"]
@@ -30,34 +34,61 @@ def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
+def current(target, deps):
+    return os.path.exists(target) and all(os.path.getmtime(p) <= os.path.getmtime(target) for p in deps)
+
+
+def run(cmd, what):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
+    return r.stdout + r.stderr
+
+
+def build_marshal(src):
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    cuda = os.path.join(os.path.dirname(nvcc()), "..", "include")
+    tmp = MARSHAL + ".tmp"
+    run([shutil.which(os.environ.get("CXX", "g++")) or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", tmp,
+         f"-I{sysconfig.get_paths()['include']}", f"-I{torch}/include", f"-I{cuda}",
+         f"-L{torch}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"],
+        f"compiling {src} failed")
+    os.replace(tmp, MARSHAL)
+
+
 def build(verbose: bool = False, force: bool = False) -> str:
+    header = os.path.join(HERE, "..", "include", "brisk.h")
+    marshal = os.path.join(CSRC, "marshal.cpp")
+    with ThreadPoolExecutor(max_workers=1) as ex:
+        other = None
+        if force or not current(MARSHAL, [marshal, header, __file__]):
+            other = ex.submit(build_marshal, marshal)
+        path = build_library(header, verbose, force)
+        if other:
+            other.result()
+    return path
+
+
+def build_library(header, verbose, force):
     os.makedirs(BUILD, exist_ok=True)
     srcs = sources()
     deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
-    deps.append(os.path.join(HERE, "..", "include", "brisk.h"))
-    if not force and os.path.exists(LIB):
-        t = os.path.getmtime(LIB)
-        if all(os.path.getmtime(p) <= t for p in deps) and os.path.getmtime(__file__) <= t:
-            return LIB
+    if not force and current(LIB, [*deps, header, __file__]):
+        return LIB
     cc = nvcc()
 
     def compile_one(src):
         obj = os.path.join(BUILD, os.path.basename(src)[:-3] + ".o")
         cmd = [cc, *ARCH, *FLAGS, "-c", src, "-o", obj]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed for {src}:\n{r.stdout}\n{r.stderr}")
-        if verbose and (r.stdout or r.stderr):
-            print(r.stdout + r.stderr, file=sys.stderr)
+        said = run(cmd, f"nvcc failed for {src}")
+        if verbose and said:
+            print(said, file=sys.stderr)
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(compile_one, srcs))
     tmp = LIB + ".tmp"
-    cmd = [cc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    run([cc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs], "link failed")
     os.replace(tmp, LIB)
     return LIB
 

@@ -558,3 +558,62 @@ def test_heads_share_units_whatever_their_number(B, dt, L, Hq, Hkv):
     lens = [(37 * i) % 300 for i in range(60)]
     x = make(60, L, Hq, Hkv, 64, 0, 300, dt, lens, causal(lens, L))
     check(B, x, 300)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("Pn", [0, 37])
+def test_calls_in_their_usual_form_and_with_results_given(B, monkeypatch, dt, Pn):
+    """Two ways of marshalling, the same bits; the first looks at nothing in the interpreter."""
+    x = make(3, 2, 8, 2, 64, Pn, 40, dt, [40, 0, 17])
+    att = att_of(B, x, 40)
+    start, count = i32([1, 0, 9]), i32([30, 0, 11])
+    given = {"out": torch.empty(3, 2, 8, 64, dtype=dt, device="cuda"), "lse": torch.empty(3, 2, 8, device="cuda")}
+    back = {n: torch.empty(3, 30, 2, 64, dtype=dt, device="cuda") for n in "kv"}
+    args = (x["q"], x["kp"] if Pn else None, x["vp"] if Pn else None, x["cache"], x["lens"])
+    att.attend(*args, visible=i32([[40, 3], [0, 0], [1, 17]]), scale=0.5, out=given)
+    att.load(x["cache"], 30, start, count, out=back)
+    other = att.alloc_cache()
+    att.store(other, back["k"], back["v"], start, count, stream=torch.cuda.current_stream())
+    with monkeypatch.context() as m:
+        for name in ("_view", "_plain", "_bytes", "_cache"):
+            m.setattr(B.PackedAttention, name, None)
+        r = att.attend(*args, visible=i32([[40, 3], [0, 0], [1, 17]]), scale=0.5)
+        kv = att.load(x["cache"], 30, start, count)
+        mine = att.alloc_cache("head")
+        assert att.store(mine, kv["k"], kv["v"], start, count) is mine
+    for got, want in ((r, given), (kv, back), (mine, other)):
+        assert got.keys() == want.keys()
+        for n in want:
+            assert got[n].dtype == want[n].dtype and torch.equal(got[n], want[n]), n
+
+
+def test_the_usual_form_refuses_what_the_other_does(B):
+    x = make(3, 2, 8, 2, 64, 20, 40, BF, [40, 0, 17])
+    att, c = att_of(B, x, 40), x["cache"]
+    k = torch.zeros(3, 5, 2, 64, dtype=BF, device="cuda")
+    start = i32([0, 0, 0])
+    good = dict(q=x["q"], k_prefix=x["kp"], v_prefix=x["vp"], cache=c, own_len=x["lens"], visible=None)
+    for name, bad in [("q", x["q"].float()), ("q", x["q"][:, :1]), ("q", x["q"].cpu()), ("q", None),
+                      ("k_prefix", x["kp"][:5]), ("v_prefix", None), ("own_len", x["lens"].long()),
+                      ("own_len", x["lens"].cpu()), ("own_len", i32([1] * 6)[::2]), ("visible", x["lens"]),
+                      ("q", torch.zeros(3, 2, 8, 128, dtype=BF, device="cuda")[..., ::2]), ("cache", None),
+                      ("cache", dict(c, k=c["k"].int())), ("cache", dict(c, v_scales=c["v_scales"].cpu())),
+                      ("cache", dict(c, k_scales=c["k"])), ("cache", dict(c, v=c["v"][:, :39]))]:
+        with pytest.raises(ValueError):
+            att.attend(**dict(good, **{name: bad}))
+    odd = torch.zeros(3 * 2 * 8 * 64 + 1, dtype=BF, device="cuda")[1:].view(3, 2, 8, 64)
+    for bad in (dict(good, q=odd), dict(good, own_len=None), dict(good, scale=-1.0)):
+        with pytest.raises(B.BriskError):
+            att.attend(**bad)
+    with pytest.raises(KeyError):
+        att.attend(**dict(good, cache={"k": c["k"]}))
+    for bad in ((k.float(), k, start), (k, k[:, :4], start), (k, k, start.long()), (k, k, start, start[:2])):
+        with pytest.raises(ValueError):
+            att.store(c, *bad)
+    with pytest.raises(ValueError):
+        att.load(c, 5, start.long())
+    for call in (lambda: att.store(c, k[:, :0], k[:, :0], start), lambda: att.load(c, 0, start),
+                 lambda: att.store(c, k, k, None), lambda: att.load(c, 5, None)):
+        with pytest.raises(B.BriskError):
+            call()
+    assert att.device_status() == B.OK

@@ -131,3 +131,11 @@ def test_binding_refuses_shapes_types_and_places(B):
         with pytest.raises(TypeError):
             call()
     assert att.alloc_cache("head")["k"].shape == (1, 4, 1, 8)
+
+
+def test_calls_without_a_gpu_are_refused(B):
+    att = B.PackedAttention(1, 1, 1, 1, 16, 0, 4, torch.bfloat16, device="cpu")
+    c, x, n = att.alloc_cache(), torch.zeros(1, 1, 1, 16, dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32)
+    for call in (lambda: att.store(c, x, x, n), lambda: att.load(c, 1, n), lambda: att.attend(x, None, None, c, n)):
+        with pytest.raises(ValueError, match="not on the GPU"):
+            call()
