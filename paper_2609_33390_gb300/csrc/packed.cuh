@@ -39,18 +39,15 @@ __device__ __forceinline__ float reciprocal(float s) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
   return fmaf(fmaf(-s, r, 1.f), r, r);
 }
-// The codes of channels x / s, nearest, ties to the even code, saturated; the first lowest. The exact quotient decides which
-// is nearest: a tie is a quotient of few bits, which `quotient` gives exactly, and no other one is rounded to it. Negated
-// quotients are taken, with which a zero's sign outlasts the correction, and the codes' signs turned.
+// The same rounded upwards. (What is left, of a number of few units, is exact; its square is too little to matter.)
+__device__ __forceinline__ float reciprocal_above(float s) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  return __fmaf_ru(fmaf(-s, r, 1.f), r, r);
+}
+// The codes of numbers q, nearest, ties to the even code, saturated; the first lowest.
 template <int N>
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], float s, float r) {
-  const f32x2 s2 = pack2(s, s), r2 = pack2(-r, -r);
-  float q[N];
-#pragma unroll
-  for (int i = 0; i < N; i += 2) {
-    const f32x2 y = pack2(x[i], x[i + 1]), z = mul2(y, r2);
-    unpack2(fma2(fma2(z, s2, y), r2, z), q[i], q[i + 1]);
-  }
+__device__ __forceinline__ uint32_t nearest_codes(const float (&q)[N]) {
   uint32_t put;
   if constexpr (N == 8)
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
@@ -65,14 +62,39 @@ __device__ __forceinline__ uint32_t codes_of(const float (&x)[N], float s, float
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
         "mov.b32 %0, {a, b, a, b};\n\t}" : "=r"(put) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
-  return put ^ 0x88888888u;
+  return put;
+}
+// The codes of channels x / s. The exact quotient decides which is nearest.
+// fp32: a tie is a quotient of few bits, which `quotient` gives exactly, and no other one is rounded to it. Negated
+// quotients are taken, with which a zero's sign outlasts the correction, and the codes' signs turned.
+// bf16: 8 bits over 4 differ from a tie, if at all, by 2^-11 of it, so one product decides, if it gives ties exactly: by
+// 1 / s from above, cut off. (All 256 significands over all 8, on the host; one product to nearest misses some ties.)
+template <typename T, int N>
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[N], float s) {
+  constexpr bool NARROW = sizeof(T) == 2;
+  const float r = NARROW ? reciprocal_above(s) : reciprocal(s);
+  const f32x2 s2 = pack2(s, s), r2 = NARROW ? pack2(r, r) : pack2(-r, -r);
+  float q[N];
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const f32x2 y = pack2(x[i], x[i + 1]);
+    if constexpr (NARROW) {
+      unpack2(mul2_cut(y, r2), q[i], q[i + 1]);
+    } else {
+      const f32x2 z = mul2(y, r2);
+      unpack2(fma2(fma2(z, s2, y), r2, z), q[i], q[i + 1]);
+    }
+  }
+  return NARROW ? nearest_codes(q) : nearest_codes(q) ^ 0x88888888u;
 }
 // The scale of a group whose largest magnitude is `top` (finite): top / 6, to nearest of 4 significant bits, as its
 // byte. The quotient's own rounding never moves it onto or across a border: where top differs from a border's
 // six-fold, which is exact, it differs by a unit in its last place, and that is more than half a one of the quotient.
+// (bf16: a product with 1 / 6 gives the same of every top.)
+template <typename T>
 __device__ __forceinline__ uint32_t scale_byte(float top) {
-  const float sixth = quotient(top, 6.f, 1.f / 6.f), s = fminf(fmaxf(sixth, SCALE_MIN), SCALE_MAX);
-  const uint32_t b = __float_as_uint(s);
+  const float sixth = sizeof(T) == 2 ? top * (1.f / 6.f) : quotient(top, 6.f, 1.f / 6.f);
+  const uint32_t b = __float_as_uint(fminf(fmaxf(sixth, SCALE_MIN), SCALE_MAX));
   return ((b + 0x7ffffu + ((b >> 20) & 1)) >> 20) - (112u << 3);
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float((byte + (112u << 3)) << 20); }   // (byte >= 8)

@@ -46,6 +46,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_consta
   int start;
   bool bad;
   const int n = rows_of(a, b, &start, &bad);
+  // rows of a padded batch that are not there (16 prompts of 1500 to 4096: 119 us with what they took, BBB without)
+  if ((int)blockIdx.x * EACH * a.step >= n && !bad && !a.alone) return;
   const Place<T, EACH> at(a);
   uint4 x[2][EACH];
   {
@@ -95,9 +97,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_consta
       }
 #pragma unroll
       for (int o = 1; o < LANES; o <<= 1) top = max(top, __shfl_xor_sync(FULL_MASK, top, o));
-      const uint32_t byte = scale_byte(__uint_as_float(top));
-      const float s = scale_value(byte);
-      const uint32_t put = codes_of(f, s, reciprocal(s));
+      const uint32_t byte = scale_byte<T>(__uint_as_float(top));
+      const uint32_t put = codes_of<T>(f, scale_value(byte));
       if (!mine) continue;
       uint8_t* p = codes + (unsigned long long)(uint32_t)(j * a.step) * to.tok;
       if constexpr (C == 8) *reinterpret_cast<uint32_t*>(p) = put;

@@ -279,6 +279,11 @@ __device__ __forceinline__ f32x2 mul2(f32x2 x, f32x2 y) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
   return r;
 }
+__device__ __forceinline__ f32x2 mul2_cut(f32x2 x, f32x2 y) {   // (rounded towards zero)
+  f32x2 r;
+  asm("mul.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
 __device__ __forceinline__ f32x2 add2(f32x2 x, f32x2 y) {
   f32x2 r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));

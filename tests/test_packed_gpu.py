@@ -142,6 +142,33 @@ def test_borders_of_every_scale_and_code(B):
         assert (got_s == s).all() and (got_c == c).all()
 
 
+def test_every_number_of_bf16_under_every_scale(B):
+    """Every scale that is written with every magnitude of 2^-4 to 6 times it (smaller ones are 0), and every finite number
+    as the largest of its group."""
+    def bf(bits):
+        return torch.from_numpy((np.asarray(bits).astype(np.uint32) << 16).view(np.float32)).to(BF)
+
+    every = bf(np.arange(0x7f80))
+    rows = []
+    for b in range(8, 227):
+        s = P.scale_of(b)
+        x = every[(every.double() >= s / 16) & (every.double() <= 6 * s)]
+        top = torch.full_like(x[:1], 6 * s)          # (exact)
+        x = torch.cat([x, x.new_zeros(-len(x) % 15)]).view(-1, 15)
+        x[:, ::2] *= -1
+        rows.append(torch.cat([top.expand(len(x), 1), x], 1))
+    tops = every[:, None] * torch.tensor([1, -.75, .3125, -.125, .0, -.0, .625, -.4375] * 2).to(BF)
+    x = torch.cat([*rows, tops]).view(1, -1, 1, 16)
+    att = B.PackedAttention(1, 1, 1, 1, 16, 0, x.shape[1], BF)
+    cache = new_cache(1, x.shape[1], 1, 16, fill=0)
+    att.store(cache, x.cuda(), (-x).cuda(), i32([0]))
+    assert att.device_status() == B.OK
+    for name, y in (("k", x), ("v", -x)):
+        c, s = P.store(n64(y))
+        got_c, got_s = raw(cache, name)
+        assert (got_s == s).all() and (got_c == c).all()
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_every_byte_reads_as_the_oracle_has_it(B, dt):
     """All scales, the ones that no call writes among them, with all codes."""
