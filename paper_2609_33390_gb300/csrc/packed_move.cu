@@ -1,9 +1,13 @@
 // Entries written into a cache in 4 bits, and read back.
 //
 // A thread has 16 bytes of an unquantised row (8 channels of bf16, 4 of fp32) at one place of a token, of EACH tokens'
-// keys and values in turn (EACH: see tokens_each), so that every access of a warp, on either side, is a run of whole rows, and places are worked
-// out once a thread. The lanes of a group of 16 channels find its largest magnitude together. Both kernels are to be
-// bound by the rows' bytes: they spend some 40 instructions on a piece that is read back and 80 on one that is written.
+// keys and values in turn (see tokens_each), so that every access of a warp, on either side, is a run of whole rows, and
+// places are worked out once a thread. The lanes of a group of 16 channels find its largest magnitude together.
+// Both are bound by the rows' bytes as soon as these are many: 16 times 4096 rows of 8 heads of 128, 336 MB, are written
+// in 60 us (5.6 TB/s; the instructions, some 90 a piece, fill two thirds of the slots) and read back in 56 (6.0 TB/s).
+// Few rows are bound by latency: lengths, rows, the scale's chain, 4 us.
+#include <climits>
+
 #include "packed.cuh"
 
 namespace brisk {
@@ -34,21 +38,35 @@ struct Place {
     t = (int)blockIdx.x * EACH * a.step + (a.by_token.d > MOVE_THREADS ? 0 : r);
   }
 };
+// Which rows of a thread, counted from its first token's, are there and have a place in the cache.
+struct Inside {
+  int from;
+  uint32_t n;
+  __device__ __forceinline__ Inside(const PackedMoveArgs& a, int start, int rows, bool there, int t) {
+    const int low = start < 0 ? (start == INT_MIN ? INT_MAX : -start) : 0;
+    const int high = (int)min((long long)rows, (long long)a.S - start);
+    from = t - low;
+    n = there && high > low ? (uint32_t)(high - low) : 0;
+  }
+  __device__ __forceinline__ bool operator()(int on) const { return (uint32_t)(from + on) < n; }
+};
 // A thread's address in a tensor, `t` tokens on.
 __device__ __forceinline__ const char* row_at(const CacheView& v, int es, int b, int h, int c, int t) {
   return static_cast<const char*>(v.p) + (b * v.seq + h * v.head + c + t * v.tok) * es;
 }
 
+// (Four tokens a thread: with 64 registers there are four CTAs an SM, not three: 16 prompts 51.7 -> 43.7 us.)
 template <typename T, int EACH>
-__global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_constant__ PackedMoveArgs a) {
+__global__ void __launch_bounds__(MOVE_THREADS, EACH == 4 ? 4 : 1) store_kernel(const __grid_constant__ PackedMoveArgs a) {
   constexpr int C = channels<T>(), LANES = GROUP / C;      // channels of a thread, threads of a group
   const int b = blockIdx.y;
   int start;
   bool bad;
   const int n = rows_of(a, b, &start, &bad);
-  // rows of a padded batch that are not there (16 prompts of 1500 to 4096: 119 us with what they took, BBB without)
+  // rows of a padded batch that are not there (16 prompts of 1500 to 4096: written and read back in 119 us with what they took, 107 without)
   if ((int)blockIdx.x * EACH * a.step >= n && !bad && !a.alone) return;
   const Place<T, EACH> at(a);
+  const Inside in(a, start, n, at.there, at.t);
   uint4 x[2][EACH];
   {
     const char *k = row_at(a.k, sizeof(T), b, at.h, at.c, at.t), *v = row_at(a.v, sizeof(T), b, at.h, at.c, at.t);
@@ -56,13 +74,12 @@ __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_consta
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       x[0][j] = x[1][j] = make_uint4(0, 0, 0, 0);
-      if (at.there && at.t + j * a.step < n) {
+      if (in(j * a.step)) {
         x[0][j] = ld_stream_v4(k + j * ks);
         x[1][j] = ld_stream_v4(v + j * vs);
       }
     }
   }
-  const bool clear = n <= 0 || (start >= 0 && (long long)start + n <= a.S);   // all places are the cache's
   const long long first = start + (long long)at.t;
   int code = bad ? BRISK_ERR_INVALID_ARG : BRISK_OK;
 #pragma unroll
@@ -85,7 +102,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) store_kernel(const __grid_consta
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = max(top, w[i] & 0x7fffffffu);
       }
-      const bool mine = at.there && at.t + j * a.step < n && (clear || (first + j * a.step >= 0 && first + j * a.step < a.S));
+      const bool mine = in(j * a.step);
       if (top >= 0x7f800000u) {                    // an infinity or NaN
         top = 0;
 #pragma unroll
@@ -134,7 +151,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) load_kernel(const __grid_constan
   }
   const Place<T, EACH> at(a);
   if (!at.there) return;
-  const bool clear = n <= 0 || (start >= 0 && (long long)start + n <= a.S);
+  const Inside in(a, start, n, true, at.t);
   const long long first = start + (long long)at.t;
   uint32_t codes[2][EACH], byte[2][EACH];
 #pragma unroll
@@ -145,7 +162,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) load_kernel(const __grid_constan
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       codes[value][j] = byte[value][j] = 0;
-      if (at.t + j * a.step < n && (clear || (first + j * a.step >= 0 && first + j * a.step < a.S))) {
+      if (in(j * a.step)) {
         const uint8_t* q = p + (unsigned long long)(uint32_t)(j * a.step) * from.tok;
         if constexpr (C == 8) codes[value][j] = __ldg(reinterpret_cast<const uint32_t*>(q));
         else codes[value][j] = __ldg(reinterpret_cast<const uint16_t*>(q));
@@ -192,15 +209,16 @@ dim3 grid_of(const PackedMoveArgs& a, int each) {
   return dim3((unsigned)((a.T + n - 1) / n), a.B, (unsigned)((a.by_token.d + MOVE_THREADS - 1) / MOVE_THREADS));
 }
 // Tokens of a thread: one while its CTAs are few, as calls' latency goes (32 rows of 8 sequences written and read back,
-// 8 heads of 128: one 8.2 us, two 9.4, four 12.4), then two, and four of calls that write many (16 prompts of 1500 to
-// 4096 rows written: one 92.7 us, two 86.3, four 82.1; 64 caches read back: one 130, two 105, four 109).
+// 8 heads of 128: one 8.2 us, two 9.4, four 12.4), then two, and four of calls that write many (64 times 512 rows
+// written: two 37.1 us, four 31.7; 16 prompts of 1500 to 4096: two 49.5, four 43.9; 64 caches read back: one 130,
+// two 105, four 109).
 int tokens_each(const PackedMoveArgs& a, bool writes) {
   auto ctas = [&](int each) {
     const dim3 g = grid_of(a, each);
     return (long long)g.x * g.y * g.z;
   };
   if (ctas(1) <= 4 * CACHE_SMS) return 1;
-  return writes && ctas(4) >= 32 * CACHE_SMS ? 4 : 2;
+  return writes && ctas(4) >= 8 * CACHE_SMS ? 4 : 2;
 }
 template <typename T>
 cudaError_t store(const PackedMoveArgs& a, dim3 grid, int each, cudaStream_t stream) {
