@@ -5,7 +5,7 @@ Every block, `ContextDecoder.step` writes the block's keys and values behind the
 attends over the prompt and them, hands hidden states and logits to the decode tail, adds up the
 attention weight that own entries got, and replaces the block's entries by those of the committed
 tokens. Before a block that might not fit, all sequences' caches are cut to the entries of
-largest weight. Nothing is read back: the host knows an upper bound of the lengths. Projections are
+largest weight. The host waits for nothing: it knows an upper bound of the lengths. Projections are
 library products; attention, weights, eviction and the tail are the library's kernels.
 
 The own caches are held in the layer's type, or (`packed`) in 4 bits: entries are quantised as they are written

@@ -153,11 +153,26 @@ struct PackedArgs {
   PackedView k, v;
 };
 constexpr int PACKED_ROWS = 8;       // query rows of a tile of the kernel for few
-constexpr int PACKED_MANY = 16;      // bf16: from more rows a sequence and key head on, the kernel for many
-constexpr int PACKED_QUAD = 4;       // bf16: up to as many, the kernel for few has a form of its own
 constexpr int PACKED_CTAS = 2 * CACHE_SMS;
 constexpr int PACKED_WARPS = 8;
-constexpr int PACKED_PARTS = 64;     // parts of a row, about, that units of several heads may lead to
+// bf16: from more rows a sequence and key head on, the kernel for many. Its tile costs the same for 1 to 128 rows, the other
+// kernel reads a key again for every 8 (us, for many | for few; 32 heads on 8 of 128 channels, no prefix):
+//   rows                                    12            16            20            32            128
+//   1 sequence, 2000 entries           16.5 | 14.5   16.5 | 14.5   16.7 | 16.6   16.6 | 18.6   18.9 | 24.7
+//   16 of 500 to 1000                  25.3 | 26.8   25.0 | 24.9   25.6 | 30.9   25.3 | 33.9   31.8 | 67.7
+//   128 of 500 to 1000                 88.7 | 69.8   88.3 | 68.0   90.9 | 89.7   92.5 | 114    114  | 381
+//   32 of 4000 to 8000                               99.9 | 98.6    101 | 135                  122  | 610
+constexpr int PACKED_MANY = 16;
+// bf16: up to as many rows, the kernel for few has a form of its own (single tokens of 4 query heads a key head: 256
+// sequences of 512 to 2048 entries over 2048 shared 115 us without it, 104 with; one of 130001 47.5 and 43.4).
+constexpr int PACKED_QUAD = 4;
+// Parts of a row, about, that units of several heads may lead to. In token order such units read whole lines of
+// a cache (64 sequences: 1.7 times the bytes without), but divide fewer items over the CTAs, into more parts to
+// join (us, single tokens; units of several heads with up to 64 parts | never | always):
+//   token order  1 of 30000: 22.7 | 22.8 | 30.5   1 of 4000: 14.3 | 14.5 | 18.6   64 of 4000: 61.9 | 81.5 | 61.9
+//                64 of 500:  22.8 | 26.7 | 22.7   8 of 4000: 22.0 | 22.6 | 21.5
+//   head order   1 of 30000: 21.6 | 21.5 | 28.8   64 of 4000: 55.8 | 58.9 | 55.9
+constexpr int PACKED_PARTS = 64;
 // The kernel for few rows: a unit is the keys of several neighbouring heads, a head a warp or several warps a head, as many
 // heads as there are warps, while that leaves a row about PACKED_PARTS parts to join.
 inline void divide_packed(AttendArgs* a) {

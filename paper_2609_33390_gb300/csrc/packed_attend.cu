@@ -1,9 +1,11 @@
 // Attention over own caches in 4 bits, for the rows of a few queries: parts (or results) of up to 8 rows of a key head
 // against the keys of a fragment (see Plan), as the kernels of unquantised caches leave them.
 //
-// Eight warps of a CTA share the heads of a unit (see divide_packed); the warps of a head take 32 of its keys each in turn. The codes become fp16 in registers, in the places
-// where mma.sync wants them, and never pass through shared memory as numbers: at the rate at which memory delivers
-// codes, a tile of fp16 written and read there would take more than the bandwidth it has. The products are
+// Eight warps of a CTA share the heads of a unit (see divide_packed); the warps of a head take 32 of its keys each in
+// turn. The codes become fp16 in registers, in the places where mma.sync wants them, and never pass through shared memory
+// as numbers: at the rate at which memory delivers codes, a tile of fp16 written and read there would take more than the
+// bandwidth it has. (tcgen05 takes its tiles of keys from shared memory alone, and 128 rows of queries where there are
+// 1 to 16.) The products are
 //   S^T [16 keys, 8 rows]      = K [16 keys, D] Q^T,
 //   O^T [D channels, 8 rows]  += V^T [D channels, 16 keys] P^T.
 // The order of k in a product is free, so a lane of K has 32 neighbouring channels of its key, 16 bytes of codes, and a
@@ -20,6 +22,13 @@
 // Entries that a row does not see: scores are masked by selection, and the scales of the values of a step of which some
 // row does not see all are cut to ones that stand for numbers, so that what is left in the ring or the cache cannot
 // defeat a weight of 0.
+//
+// Bound by the instructions of a step and their latencies with four warps a scheduler, not by bytes (which are few):
+// 256 instructions for 16 keys of a head of 128, of which 93 wait their turn for the units of integer logic (the
+// conversions take these two cycles each) and 16 are products; 474 cycles, 357 without the copies. Single tokens of 256
+// sequences over 512 to 2048 own and 2048 shared entries take 104 us, 377 MB of codes among it; one over 130001 entries
+// 43 us, 3.5 TB/s. Steps of 16 keys with three CTAs an SM (125 and 54 us) and a third place in the ring (106 and 45) did
+// not help.
 #include "packed.cuh"
 
 namespace brisk {
