@@ -644,3 +644,57 @@ def test_the_usual_form_refuses_what_the_other_does(B):
         with pytest.raises(B.BriskError):
             call()
     assert att.device_status() == B.OK
+
+
+def test_calls_in_their_usual_form_captured(B):
+    """Results that the calls allocate while they are captured are the graph's, and are written by every replay."""
+    Bn, L, S, H, D = 2, 3, 90, 2, 80
+    att = B.PackedAttention(Bn, L, 4, H, D, 33, S, BF)
+    x = make(Bn, L, 4, H, D, 33, S, BF, [70, 12])
+    rows = {n: spread_rows((Bn, L, H, D), BF, i).cuda() for i, n in enumerate("kv")}
+    start = i32([5, 0])
+    att.store(x["cache"], rows["k"], rows["v"], start)
+    torch.cuda.synchronize()
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=s):
+        att.store(x["cache"], rows["k"], rows["v"], start)
+        r = att.attend(x["q"], x["kp"], x["vp"], x["cache"], x["lens"])
+        back = att.load(x["cache"], L, start)
+    for turn in range(3):
+        for m in "kv":
+            rows[m].copy_(torch.randn(Bn, L, H, D).to(BF))
+        start.copy_(i32([7 * turn, 30 * turn]))
+        g.replay()
+        torch.cuda.synchronize()
+        assert att.device_status() == B.OK
+        for m in "kv":
+            assert (n64(back[m]) == P.values(*P.store(n64(rows[m])))).all()
+            x[m] = P.values(*raw(x["cache"], m))
+        compare(r, wanted(x, att.scale), x, S)
+
+
+def test_calls_of_two_threads(B):
+    """Two host threads, each with an object and a stream of its own."""
+    import threading
+    x = [make(3, 2, 8, 2, 64, 50, 200, BF, [200, 3, 77], seed=i) for i in range(2)]
+    att = [att_of(B, y, 200) for y in x]
+    want = [a.attend(y["q"], y["kp"], y["vp"], y["cache"], y["lens"]) for a, y in zip(att, x)]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(100):
+                y = x[i]
+                r = att[i].attend(y["q"], y["kp"], y["vp"], y["cache"], y["lens"])
+                s.synchronize()
+                if not (torch.equal(r["out"], want[i]["out"]) and torch.equal(r["lse"], want[i]["lse"])):
+                    wrong.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
