@@ -646,6 +646,8 @@ def test_the_usual_form_refuses_what_the_other_does(B):
     assert att.device_status() == B.OK
 
 
+# Streams come from a pool of 32 in turn, so that one may be another test's capture stream: these take theirs from the other
+# pool, and leave the turns of the tests behind them as they are.
 def test_calls_in_their_usual_form_captured(B):
     """Results that the calls allocate while they are captured are the graph's, and are written by every replay."""
     Bn, L, S, H, D = 2, 3, 90, 2, 80
@@ -655,7 +657,7 @@ def test_calls_in_their_usual_form_captured(B):
     start = i32([5, 0])
     att.store(x["cache"], rows["k"], rows["v"], start)
     torch.cuda.synchronize()
-    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream(priority=-1)
     with torch.cuda.graph(g, stream=s):
         att.store(x["cache"], rows["k"], rows["v"], start)
         r = att.attend(x["q"], x["kp"], x["vp"], x["cache"], x["lens"])
@@ -683,7 +685,7 @@ def test_calls_of_two_threads(B):
     wrong = []
 
     def work(i):
-        s = torch.cuda.Stream()
+        s = torch.cuda.Stream(priority=-1)
         with torch.cuda.stream(s):
             for _ in range(100):
                 y = x[i]
