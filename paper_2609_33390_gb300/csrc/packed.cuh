@@ -156,13 +156,19 @@ constexpr int PACKED_ROWS = 8;       // query rows of a tile of the kernel for f
 constexpr int PACKED_CTAS = 2 * CACHE_SMS;
 constexpr int PACKED_WARPS = 8;
 // bf16: from more rows a sequence and key head on, the kernel for many. Its tile costs the same for 1 to 128 rows, the other
-// kernel reads a key again for every 8 (us, for many | for few; 32 heads on 8 of 128 channels, no prefix):
-//   rows                                    12            16            20            32            128
+// kernel reads a key again for every 8, which costs half with 64 channels (us, for many | for few; 32 heads on 8, no prefix):
+//   rows of 128 channels                    12            16            20            32            128
 //   1 sequence, 2000 entries           16.5 | 14.5   16.5 | 14.5   16.7 | 16.6   16.6 | 18.6   18.9 | 24.7
 //   16 of 500 to 1000                  25.3 | 26.8   25.0 | 24.9   25.6 | 30.9   25.3 | 33.9   31.8 | 67.7
 //   128 of 500 to 1000                 88.7 | 69.8   88.3 | 68.0   90.9 | 89.7   92.5 | 114    114  | 381
 //   32 of 4000 to 8000                               99.9 | 98.6    101 | 135                  122  | 610
-constexpr int PACKED_MANY = 16;
+//   rows of 64 channels                     16            24            32            40            48
+//   1 sequence, 2000 entries           14.4 | 12.4   15.0 | 14.4   14.6 | 14.7   16.3 | 14.8   16.5 | 15.4
+//   16 of 500 to 1000                  21.7 | 18.6   22.6 | 24.0   21.1 | 24.6   22.7 | 24.9   22.6 | 26.7
+//   128 of 500 to 1000                 67.5 | 41.2   68.8 | 54.8   68.0 | 66.0   76.9 | 78.7   77.1 | 92.2
+//   189 of 200 to 400                  66.7 | 35.0   68.0 | 45.4   68.8 | 55.5   76.9 | 65.9   76.3 | 76.1
+// (80 channels behave as 128: 128 sequences 77 | 82 with 12 rows, 78 | 111 with 20.)
+inline int packed_many(int D) { return D <= 64 ? 32 : 16; }
 // bf16: up to as many rows, the kernel for few has a form of its own (single tokens of 4 query heads a key head: 256
 // sequences of 512 to 2048 entries over 2048 shared 115 us without it, 104 with; one of 130001 47.5 and 43.4).
 constexpr int PACKED_QUAD = 4;
@@ -176,7 +182,7 @@ constexpr int PACKED_PARTS = 64;
 // The kernel for few rows: a unit is the keys of several neighbouring heads, a head a warp or several warps a head, as many
 // heads as there are warps, while that leaves a row about PACKED_PARTS parts to join.
 inline void divide_packed(AttendArgs* a) {
-  const bool tc = a->dt == BRISK_DT_BF16, many = tc && a->L * a->G > PACKED_MANY;
+  const bool tc = a->dt == BRISK_DT_BF16, many = tc && a->L * a->G > packed_many(a->D);
   a->sh.kt = tc ? TC_KT : SIMT_KT;                 // (the prefix's)
   a->sh.rt_o = many ? SLOT_ROWS : PACKED_ROWS;
   a->sh.rt_p = tc ? PAIR_ROWS : SIMT_ROWS;

@@ -10,7 +10,7 @@
 // does not see stand for finite numbers, and rows of a tile behind the last entry are written as zeros.
 //
 // Bound by a unit's chain (codes, tiles, scores, exponentials, values) with two CTAs an SM to overlap: 128 blocks of 32
-// positions, 32 heads on 8, D = 128, over 512 to 2048 own entries each 125 us, where the products alone would take 45.
+// positions, 32 heads on 8, D = 128, over 512 to 2048 own entries each 121 us, where the products alone would take 45.
 // Tensor cores are active 26 % of the time, 48 % of the issue slots are used; a fragment's ends (its queries' change, its
 // parts) take about as long as three of its units of 128 keys.
 // Codes copied to shared memory first (cp.async) took 275 us of the whole call, where reading them to registers took 260.

@@ -349,6 +349,8 @@ SIZES = [
     (1, 1, 16, 1, 96, 0, 5000, [4999]),               # one row tile's keys over many CTAs
     (40, 2, 8, 4, 32, 0, 90, [(11 * i) % 91 for i in range(40)]),   # CTAs with many short fragments
     (1, 20, 8, 2, 128, 0, 1500, [1490]),
+    (3, 12, 8, 2, 64, 90, 260, [260, 100, 0]),         # 48 rows, and 32, of up to 64 channels
+    (3, 8, 8, 2, 48, 90, 260, [260, 100, 0]),
 ]
 
 
