@@ -39,7 +39,8 @@ __device__ __forceinline__ float reciprocal(float s) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
   return fmaf(fmaf(-s, r, 1.f), r, r);
 }
-// The same rounded upwards. (What is left, of a number of few units, is exact; its square is too little to matter.)
+// 1 / s of a scale, rounded upwards: the Newton step's sum, rounded so, misses 1 / s by the approximation's error squared,
+// 2^-45, and no 1 / s but a power of two, where the error is none, lies so near a number of fp32.
 __device__ __forceinline__ float reciprocal_above(float s) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
