@@ -435,8 +435,8 @@ brisk_status brisk_cache_evict(const brisk_cache_dims *dims, const brisk_view *k
  * which fp16, bf16 and fp32 hold exactly. The largest scale that is written is 226, for 10240;
  * brisk_packed_load takes larger ones for it, and what they do to rows of attention that see them
  * is not defined. A row's codes are D/2 bytes, its scales 4 bytes (D <= 64) or 8, of which the first
- * D/16 are in use. The paper has no counterpart. brisk_cache_dims as above, with 16 <= D <= 128 and
- * D % 16 == 0. */
+ * D/16 are in use; the others may hold anything and keep it. The paper has no counterpart.
+ * brisk_cache_dims as above, with 16 <= D <= 128 and D % 16 == 0. */
 
 /* A cache of such rows: codes of entry t of sequence s and key head h at codes + s * seq + t * tok +
  * h * head, its scales at scales + s * scale_seq + ..., strides in bytes. Codes and their strides are

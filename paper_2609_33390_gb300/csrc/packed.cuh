@@ -112,7 +112,8 @@ __device__ __forceinline__ void from_codes(uint32_t w, uint32_t (&h)[4]) {
 // Two scales as fp16, and one twice. Products, not shifts: beside the conversions of codes, which take the units of integer
 // logic two cycles each, those of multiplication have room.
 __device__ __forceinline__ uint32_t scales_plain(uint32_t low, uint32_t high) { return low * 0x80u + high * 0x800000u; }
-__device__ __forceinline__ uint32_t scale_plain(uint32_t byte) { return byte * 0x800080u; }
+constexpr uint32_t SCALE_PLAIN = 0x800080;
+__device__ __forceinline__ uint32_t scale_plain(uint32_t byte) { return byte * SCALE_PLAIN; }
 // At most SCALE_MAX whatever the byte holds (the minimum takes a number before a NaN).
 __device__ __forceinline__ uint32_t scale_f16(uint32_t byte) {
   uint32_t r;

@@ -244,6 +244,11 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
   const uint32_t pick[2] = {g & 1 ? 0x1044u : 0x4410u, g & 1 ? 0x3244u : 0x4432u};
   // (the compiler would rather work them out again at every step)
   asm volatile("" : "+r"(at_k), "+r"(at_ks), "+r"(at_v[0]), "+r"(at_v[1]), "+r"(at_vs[0]), "+r"(at_vs[1]));
+  // What a byte of a key's scales is multiplied by (see scale_plain): 0 from channel D on, where the byte is not in use and
+  // may be anything, so that the queries' zeros meet zeros. (Codes of what is not there are numbers, whatever they are.)
+  uint32_t there[DP / 64];
+#pragma unroll
+  for (int j = 0; j < DP / 64; ++j) there[j] = c * (DP / 4) + GROUP * j < D ? SCALE_PLAIN : 0;
 
   for (;;) {
     if (walked == done && (!more || !find())) break;
@@ -340,7 +345,7 @@ packed_few_kernel(const __grid_constant__ PackedArgs p) {
               wk[u][i][0] = y.x; wk[u][i][1] = y.y;
             }
 #pragma unroll
-            for (int j = 0; j < DP / 64; ++j) sk[u][i][j] = scale_plain(tile[at_ks + row * T::SROW + j]);
+            for (int j = 0; j < DP / 64; ++j) sk[u][i][j] = tile[at_ks + row * T::SROW + j] * there[j];
           }
 #pragma unroll
         for (int w = 0; w < W; ++w)
