@@ -65,8 +65,9 @@ struct Checks {
     ok = false;
     return nullptr;
   }
-  // codes and scales under `name` and `scales`
-  brisk_packed packed(PyObject* cache, const char* name, const char* scales) {
+  // codes and scales under `name` and `scales`. `written`: asked for as memory to write, which a tensor that shares its
+  // memory with the one it is a lazy clone of gets a copy for.
+  brisk_packed packed(PyObject* cache, const char* name, const char* scales, bool written = false) {
     brisk_packed p{};
     if (d->S == 0) return p;
     const at::Tensor* t[2] = {};
@@ -83,8 +84,8 @@ struct Checks {
       return p;
     }
     const Sizes c = t[0]->strides(), s = t[1]->strides();
-    return brisk_packed{const_cast<void*>(t[0]->const_data_ptr()), const_cast<void*>(t[1]->const_data_ptr()),
-                        c[0], c[1], c[2], s[0], s[1], s[2]};
+    auto at = [&](const at::Tensor& x) { return written ? x.mutable_data_ptr() : const_cast<void*>(x.const_data_ptr()); };
+    return brisk_packed{at(*t[0]), at(*t[1]), c[0], c[1], c[2], s[0], s[1], s[2]};
   }
   at::Tensor make(at::ScalarType type, Sizes shape) const {
     return at::empty(shape, at::TensorOptions().dtype(type).device(at::kCUDA, device));
@@ -148,7 +149,7 @@ PyObject* store(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (T < 1 || T > 1 << 30) Py_RETURN_NONE;
   const int64_t shape[4] = {d->B, T, d->Hkv, d->D};
   const brisk_view k = c.view(a[4], shape), v = c.view(a[5], shape);
-  const brisk_packed kp = c.packed(a[3], "k", "k_scales"), vp = c.packed(a[3], "v", "v_scales");
+  const brisk_packed kp = c.packed(a[3], "k", "k_scales", true), vp = c.packed(a[3], "v", "v_scales", true);
   const void* start = c.plain(a[6], at::kInt, {d->B});
   const void* count = c.plain(a[7], at::kInt, {d->B}, true);
   if (!c.ok) Py_RETURN_NONE;
