@@ -9,8 +9,8 @@ largest weight. The host waits for nothing: it knows an upper bound of the lengt
 library products; attention, weights, eviction and the tail are the library's kernels.
 
 The own caches are held in the layer's type, or (`packed`) in 4 bits: entries are quantised as they are written
-and attended over as they lie; weights and eviction work on what is read back into a pair of caches
-that the layers of a model share."""
+and attended over as they lie, while weights and eviction work on what every step reads back into a pair of caches in
+the layer's type (`scratch`), which decoders whose steps follow one another may share."""
 from __future__ import annotations
 
 import torch
@@ -31,11 +31,17 @@ class ContextDecoder:
 
     `tail`: the prepared DecodeTail (its weights hold the embedding rows E_in and E_out); `w`: see
     layer_weights. Own caches have room for `S` entries and are cut to `keep`, of which the
-    `recent` newest always stay; sums of weights shrink by `decay` a block. packed: own caches in 4 bits."""
+    `recent` newest always stay; sums of weights shrink by `decay` a block. packed: own caches in 4 bits.
 
-    def __init__(self, tail, w, prompt, Hq, Hkv, D, S, keep, recent=0, decay=1.0, packed=False):
+    scratch: of a packed decoder, the `scratch` of another one of the same sizes, type and device, in place of its
+    own: entries read back and eviction's targets, which hold nothing from one step to the next. The steps of
+    decoders that share it go to one stream, one after the other."""
+
+    def __init__(self, tail, w, prompt, Hq, Hkv, D, S, keep, recent=0, decay=1.0, packed=False, scratch=None):
         if keep + tail.L > S:
             raise ValueError(f"a block of {tail.L} does not fit behind {keep} of {S} entries")
+        if scratch is not None and not packed:
+            raise ValueError("caches that are not packed hold entries from step to step: no scratch")
         self.tail, self.w, self.keep, self.recent, self.decay = tail, w, keep, recent, decay
         self.e_in, self.e_out = tail.weights["E_in"], tail.weights["E_out"]
         B, L, dev, dt = tail.B, tail.L, tail.device, self.e_in.dtype
@@ -43,13 +49,19 @@ class ContextDecoder:
         kind = brisk.PackedAttention if packed else brisk.PrefixAttention
         self.attention = kind(B, L, Hq, Hkv, D, prompt.numel(), S, dt, dev)
         self.k_prefix, self.v_prefix = self._entries(self.e_in[prompt])
-        self.k, self.v = (torch.zeros(B, S, Hkv, D, dtype=dt, device=dev) for _ in range(2))
+        if scratch is None:
+            self.k, self.v = (torch.zeros(B, S, Hkv, D, dtype=dt, device=dev) for _ in range(2))
+        else:
+            self._check_scratch(scratch, keep, dt)
+            self.k, self.v = scratch["k"], scratch["v"]
         self.acc = torch.zeros(B, Hkv, S, device=dev)
         # weights and eviction: on k and v, which are the caches, or what is read back of them
         self.entries = brisk.PrefixAttention(B, L, Hq, Hkv, D, 0, S, dt, dev) if packed else None
         self.cache = self.attention.alloc_cache() if packed else None
         self.first = torch.zeros(B, dtype=torch.int32, device=dev)
-        self.spare = (self.entries or self.attention).alloc_evicted(keep, room=keep if packed else S)
+        self.spare = scratch["spare"] if scratch else \
+            (self.entries or self.attention).alloc_evicted(keep, room=keep if packed else S)
+        self.scratch = {"k": self.k, "v": self.v, "spare": self.spare} if packed else None
         self.own_len = torch.zeros(B, dtype=torch.int32, device=dev)
         # a workspace's first word is its last call's status, which the next call of the step overwrites
         self.words = [x.workspace[:4].view(torch.int32) for x in (self.attention, tail, self.entries) if x]
@@ -60,6 +72,14 @@ class ContextDecoder:
         self.rows = torch.arange(B, device=dev)[:, None]
         pos = torch.arange(L, device=dev)[:, None] / 10000 ** torch.linspace(0, 1, tail.d, device=dev)
         self.block = (w["mask"] + torch.cos(pos)).to(dt).expand(B, L, tail.d)
+
+    def _check_scratch(self, scratch, keep, dt):
+        dev = self.e_in.device
+        want, kept = (self.tail.B, self.S, self.Hkv, self.D), (self.tail.B, keep, self.Hkv, self.D)
+        for name, t, shape in (("k", scratch["k"], want), ("v", scratch["v"], want),
+                               ("spare k", scratch["spare"]["k"], kept), ("spare v", scratch["spare"]["v"], kept)):
+            if t.shape != shape or t.dtype != dt or t.device != dev:
+                raise ValueError(f"scratch {name}: {tuple(t.shape)} {t.dtype} on {t.device}, not {shape} {dt} on {dev}")
 
     def _entries(self, x):
         shape = (*x.shape[:-1], self.Hkv, self.D)
