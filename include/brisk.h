@@ -475,9 +475,11 @@ brisk_status brisk_packed_load(const brisk_cache_dims *dims, int32_t T, const br
                                void *stream);
 
 /* brisk_prefix_attend with the own caches k_own, v_own [B, S, Hkv] in 4 bits (NULL if S == 0); queries,
- * prefix and out in dims' dtype. Over own entries scores are sums of exact products in fp32, or with
- * fp32 queries of products of the query rounded to 2^-23; the weights enter the sum of values rounded
- * to fp16 (2^-12 each; with fp32 to 2^-22). */
+ * prefix and out in dims' dtype. Over own entries scores are sums in fp32 of products that are exact but
+ * for the query's rounding: none of bf16 channels from 2^-31 of the row's largest magnitude on, one of
+ * at most 2^-39 of that largest below; of fp32 channels the larger of 2^-23 of themselves and 2^-39 of
+ * the largest. The weights enter the sum of values rounded by at most the larger of 2^-11 of themselves
+ * (with fp32 2^-22) and 2^-35 of the row's largest weight; log-sums take them as they are. */
 brisk_status brisk_packed_attend(const brisk_cache_dims *dims, const brisk_view *q,
                                  const brisk_view *k_prefix, const brisk_view *v_prefix,
                                  const brisk_packed *k_own, const brisk_packed *v_own,

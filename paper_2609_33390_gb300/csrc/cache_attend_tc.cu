@@ -20,7 +20,7 @@
 //
 // The maximum a row subtracts is held back until a score exceeds it by 2^8: P and the sums then stay
 // below 2^8 times their number, and O is seldom rescaled (128 blocks as above, own entries too: 437 us, 479 with the
-// exact maximum). Rounding P to bf16 costs at most 2^-9 of each
+// exact maximum). Rounding P to bf16 costs at most 2^-8 of each
 // weight, as much as rounding the result; sums are fp32.
 //
 // Entries that a row must not see: scores are masked by selection; a value row that some row of the

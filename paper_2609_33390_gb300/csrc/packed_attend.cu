@@ -11,10 +11,11 @@
 // The order of k in a product is free, so a lane of K has 32 neighbouring channels of its key, 16 bytes of codes, and a
 // lane of V 16 neighbouring channels of four keys, whose codes are paired by key before they are converted.
 //
-// K and V are exact in fp16. A row of Q is scaled by a power of two to a magnitude of 2^14: bf16 is exact then, down to
-// 2^-38 of the row's largest, and fp32 (TERMS = 2) goes as a sum of two fp16 of 11 bits each. Weights are taken
-// relative to 2^-SHIFT of the held maximum, so that fp16 holds them down to 2^-34 of it; rounding them costs 2^-12 each
-// (fp32: two terms, 2^-22). Sums, maxima and S are fp32. With fp32 every 16 keys' sums are taken anew and added in
+// K and V are exact in fp16. A row of Q is scaled by a power of two to a magnitude of 2^14 to 2^15, where steps of fp16 end at
+// 2^-24: bf16 is exact then from 2^-31 of the row's largest on, and fp32 (TERMS = 2) goes as a sum of two fp16 of 11 bits
+// each, off by 2^-23 of itself; what is smaller by up to 2^-25, 2^-39 of the largest. Weights are taken relative to
+// 2^-SHIFT of the held maximum; rounding them costs 2^-11 each (fp32: two terms, less than 2^-22), or that 2^-25, which is
+// 2^-35 of the maximum, if it is more. Sums, maxima and S are fp32. With fp32 every 16 keys' sums are taken anew and added in
 // fp32, since the tensor cores cut what they add to a sum towards zero.
 //
 // Keys and values come through a ring of a warp's own, in which its lanes copy 16 bytes at a time, a place of 32 keys

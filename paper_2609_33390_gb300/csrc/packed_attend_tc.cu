@@ -3,10 +3,10 @@
 // As attend_slot_kernel (cache_attend_tc.cu), a slot of 128 query rows a CTA, two CTAs an SM, but the tiles of keys and
 // values are not copied: three warps for each read their codes to registers and write them as fp16, in which they are
 // exact, where the products take them from shared memory. The queries become fp16 too (both operands of a product
-// have one type), each row scaled by a power of two so that its largest magnitude is 2^14 to 2^15: exact down to 2^-38
-// of it. (Keys as bf16 instead cost more, in every tile, than the queries' change once a fragment: 217 and 197 us, 128
-// blocks.) Weights are fp16, taken relative to 2^-10 of the held maximum. Scores are taken 64 keys at a time, in two
-// places of TMEM, so that the tensor cores work on the next while a slot's threads take exponentials. Codes that a row
+// have one type), each row scaled by a power of two so that its largest magnitude is 2^14 to 2^15: exact from 2^-31 of it
+// on, below off by up to 2^-39 of it. (Keys as bf16 instead cost more, in every tile, than the queries' change once a
+// fragment: 217 and 197 us, 128 blocks.) Weights are fp16, taken relative to 2^-10 of the held maximum: off by 2^-11 of
+// themselves, or 2^-35 of the maximum. Scores are taken 64 keys at a time, in two places of TMEM, so that the tensor cores work on the next while a slot's threads take exponentials. Codes that a row
 // does not see stand for finite numbers, and rows of a tile behind the last entry are written as zeros.
 //
 // Bound by a unit's chain (codes, tiles, scores, exponentials, values) with two CTAs an SM to overlap: 128 blocks of 32
