@@ -1,11 +1,10 @@
-"""Builds the CUDA library ``libbrisk.so`` in-tree for sm_103a with nvcc, and the binding's ``_marshal.so``.
+"""Builds the CUDA library ``libbrisk.so`` in-tree for sm_103a with nvcc, and the binding's module ``_marshal``.
 
 Each translation unit compiles in parallel, then one shared link. The runtime
 is linked statically, so the library loads on a machine without a GPU driver
-(the driver is opened on first use). ``_marshal.so`` is a module of the interpreter, compiled on its headers and
-torch's, beside the library.
+(the driver is opened on first use). ``_marshal`` is a module of the interpreter, compiled on its headers and
+torch's, beside the library; it is compiled anew for another interpreter, which its name tells, and another torch.
 """
-import importlib.util
 import os
 import shutil
 import subprocess
@@ -17,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbrisk.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")
+MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+MARSHAL_OF = os.path.join(BUILD, "marshal.torch")   # the version of the torch that it is for
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-Xptxas", "-warn-spills"]
@@ -45,8 +45,16 @@ def run(cmd, what):
     return r.stdout + r.stderr
 
 
+def is_for(version):
+    if not os.path.exists(MARSHAL_OF):
+        return False
+    with open(MARSHAL_OF) as f:
+        return f.read() == version
+
+
 def build_marshal(src):
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    import torch
+    torch = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.path.dirname(nvcc()), "..", "include")
     tmp = MARSHAL + ".tmp"
     run([shutil.which(os.environ.get("CXX", "g++")) or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", tmp,
@@ -57,20 +65,23 @@ def build_marshal(src):
 
 
 def build(verbose: bool = False, force: bool = False) -> str:
+    import torch
     header = os.path.join(HERE, "..", "include", "brisk.h")
     marshal = os.path.join(CSRC, "marshal.cpp")
+    os.makedirs(BUILD, exist_ok=True)
     with ThreadPoolExecutor(max_workers=1) as ex:
         other = None
-        if force or not current(MARSHAL, [marshal, header, __file__]):
+        if force or not is_for(torch.__version__) or not current(MARSHAL, [marshal, header, __file__]):
             other = ex.submit(build_marshal, marshal)
         path = build_library(header, verbose, force)
         if other:
             other.result()
+            with open(MARSHAL_OF, "w") as f:
+                f.write(torch.__version__)
     return path
 
 
 def build_library(header, verbose, force):
-    os.makedirs(BUILD, exist_ok=True)
     srcs = sources()
     deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
     if not force and current(LIB, [*deps, header, __file__]):
