@@ -116,13 +116,15 @@ _SIGS = [
 ]
 
 
+_BUILD_IT = "build it with `python -c 'import __graft_entry__ as g; g.build()'`"
+
+
 def lib():
     """The loaded library; raises if it has not been built."""
     global _lib
     if _lib is None:
         if not os.path.exists(LIB_PATH):
-            raise RuntimeError(f"{LIB_PATH} is missing: build it with "
-                               "`python -c 'import __graft_entry__ as g; g.build()'`")
+            raise RuntimeError(f"{LIB_PATH} is missing: {_BUILD_IT}")
         h = ctypes.CDLL(LIB_PATH)
         for name, res, args in _SIGS:
             f = getattr(h, name)
@@ -130,6 +132,15 @@ def lib():
             f.argtypes = args
         _lib = h
     return _lib
+
+
+def marshal():
+    """The module that marshals calls in their usual form; raises if it has not been built for this interpreter and torch."""
+    try:
+        from . import _marshal
+    except ImportError as e:
+        raise RuntimeError(f"the binding's module _marshal is missing, or another torch's ({e}): {_BUILD_IT}") from e
+    return _marshal
 
 
 def set_wait_limit(cycles: int) -> int:
@@ -664,7 +675,7 @@ class PackedAttention(PrefixAttention):
         self._at_attend = [at, at + 32, at + 64, at + 96, at + 160]
         self._at_move = [at, at + 32, at + 64, at + 128]
         # a call in its usual form is marshalled there; the ways below are for results given, other streams, refusals
-        from . import _marshal as quick
+        quick = marshal()
         self._quick_store, self._quick_load, self._quick_attend = quick.store, quick.load, quick.attend
         entry = lambda f: ctypes.cast(f, _vp).value
         self._f_store, self._f_load = entry(lib().brisk_packed_store), entry(lib().brisk_packed_load)

@@ -61,3 +61,15 @@ def test_its_name_tells_the_interpreter(monkeypatch):
     assert os.path.basename(build.MARSHAL) == "_marshal" + sysconfig.get_config_var("EXT_SUFFIX")
     from paper_2609_33390_gb300 import _marshal
     assert os.path.samefile(_marshal.__file__, build.MARSHAL)
+
+
+def test_a_missing_module_is_named(monkeypatch):
+    import sys
+    import paper_2609_33390_gb300 as package
+    from paper_2609_33390_gb300 import brisk, build
+    build.build()
+    monkeypatch.delattr(package, "_marshal", raising=False)
+    monkeypatch.setitem(sys.modules, package.__name__ + "._marshal", None)
+    with pytest.raises(RuntimeError, match="_marshal is missing.*g.build()"):
+        brisk.PackedAttention(1, 1, 1, 1, 16, 0, 4, torch.bfloat16, device="cpu")
+    brisk.PrefixAttention(1, 1, 1, 1, 16, 0, 4, torch.bfloat16, device="cpu")
