@@ -658,7 +658,7 @@ class PackedAttention(PrefixAttention):
 
     A cache is a dict of uint8 tensors, ``k`` and ``v`` [B, S, Hkv, D / 2] and ``k_scales`` and
     ``v_scales`` [B, S, Hkv, 4 or 8] (see alloc_cache), of any strides whose rows are contiguous and start
-    on 16 bytes (8 where D % 32 is not 0), or on their length. The weights of own entries and the eviction by them
+    on 16 bytes (8 where D % 32 is not 0), or on their length; bytes of scales behind the first D / 16 may hold anything. The weights of own entries and the eviction by them
     work on entries in ``dtype``: PrefixAttention's, on what load() gives; storing that again gives the same bytes.
     """
 

@@ -10,7 +10,8 @@ library products; attention, weights, eviction and the tail are the library's ke
 
 The own caches are held in the layer's type, or (`packed`) in 4 bits: entries are quantised as they are written
 and attended over as they lie, while weights and eviction work on what every step reads back into a pair of caches in
-the layer's type (`scratch`), which decoders whose steps follow one another may share."""
+the layer's type (`scratch`), which decoders whose steps follow one another may share. So 4 bits save memory where
+several decoders share, and no time: a step moves more bytes than over caches in the layer's type."""
 from __future__ import annotations
 
 import torch

@@ -169,7 +169,9 @@ constexpr int PACKED_WARPS = 8;
 //   16 of 500 to 1000                  21.7 | 18.6   22.6 | 24.0   21.1 | 24.6   22.7 | 24.9   22.6 | 26.7
 //   128 of 500 to 1000                 67.5 | 41.2   68.8 | 54.8   68.0 | 66.0   76.9 | 78.7   77.1 | 92.2
 //   189 of 200 to 400                  66.7 | 35.0   68.0 | 45.4   68.8 | 55.5   76.9 | 65.9   76.3 | 76.1
-// (80 channels behave as 128: 128 sequences 77 | 82 with 12 rows, 78 | 111 with 20.)
+// (80 channels behave as 128: 128 sequences 77 | 82 with 12 rows, 78 | 111 with 20. 16 to 48 channels nearly as 64, with 24 rows
+// and 32: 1 sequence 12 | 11 and 12 | 13, 16 sequences 18 to 19 | 19 to 21 and 18 to 19 | 21 to 22, 128 sequences 63 to 68 |
+// 54 to 62 and 62 to 66 | 68 to 78, 189 short ones 63 to 67 | 42 to 47 and 62 to 67 | 53 to 59.)
 inline int packed_many(int D) { return D <= 64 ? 32 : 16; }
 // bf16: up to as many rows, the kernel for few has a form of its own (single tokens of 4 query heads a key head: 256
 // sequences of 512 to 2048 entries over 2048 shared 115 us without it, 104 with; one of 130001 47.5 and 43.4).
@@ -187,6 +189,9 @@ inline void divide_packed(AttendArgs* a) {
   const bool tc = a->dt == BRISK_DT_BF16, many = tc && a->L * a->G > packed_many(a->D);
   a->sh.kt = tc ? TC_KT : SIMT_KT;                 // (the prefix's)
   a->sh.rt_o = many ? SLOT_ROWS : PACKED_ROWS;
+  // (bf16: tiles of 256 rows also where there are fewer. One sequence's rows behind a prefix alone, us, and with tiles of 128 in one
+  // launch, as prefix and own entries in bf16 have it: 4 rows over 2048 entries 14.4 | 11.5, over 32768 41.5 | 33.1, over
+  // 131072 101 | 90; 128 rows over 2048 16.9 | 14.6, over 32768 42.8 | 41.8.)
   a->sh.rt_p = tc ? PAIR_ROWS : SIMT_ROWS;
   a->sh.grid_p = a->P == 0 ? 0 : (tc ? CACHE_SMS : SLOT_CTAS);
   a->joins = tc;

@@ -27,9 +27,9 @@
 // Bound by the instructions of a step and their latencies with four warps a scheduler, not by bytes (which are few):
 // 256 instructions for 16 keys of a head of 128, of which 93 wait their turn for the units of integer logic (the
 // conversions take these two cycles each) and 16 are products; 474 cycles, 357 without the copies. Single tokens of 256
-// sequences over 512 to 2048 own and 2048 shared entries take 104 us, 377 MB of codes among it; one over 130001 entries
-// 43 us, 3.5 TB/s. Steps of 16 keys with three CTAs an SM (125 and 54 us) and a third place in the ring (106 and 45) did
-// not help.
+// sequences over 512 to 2048 own and 2048 shared entries take 104 us, 377 MB of codes among it (0.6 us less without the
+// factors that leave out channels that are not there); one over 130001 entries 43 us, 3.5 TB/s. Steps of 16 keys with
+// three CTAs an SM (125 and 54 us) and a third place in the ring (106 and 45) did not help.
 #include "packed.cuh"
 
 namespace brisk {
