@@ -54,12 +54,12 @@ def is_for(version):
 
 def build_marshal(src):
     import torch
-    torch = os.path.dirname(torch.__file__)
+    at = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.path.dirname(nvcc()), "..", "include")
     tmp = MARSHAL + ".tmp"
     run([shutil.which(os.environ.get("CXX", "g++")) or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", tmp,
-         f"-I{sysconfig.get_paths()['include']}", f"-I{torch}/include", f"-I{cuda}",
-         f"-L{torch}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"],
+         f"-I{sysconfig.get_paths()['include']}", f"-I{at}/include", f"-I{cuda}",
+         f"-L{at}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"],
         f"compiling {src} failed")
     os.replace(tmp, MARSHAL)
 
